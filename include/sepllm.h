@@ -262,6 +262,82 @@ sepllm_status sepllm_attn_bwd(const sepllm_attn_desc* desc, const sepllm_index_d
                               const void* O, const float* LSE, const void* index, void* dQ,
                               void* dK, void* dV, void* workspace, void* stream);
 
+/* ---- rotary positions of queries and keys -----------------------------------
+ * The attention calls take Q and K with their positions already encoded; these
+ * two calls encode them.  The paper names no rotary formula; with r = rot_dim,
+ * i < r/2, position p and angle a = p * f_i the pair (x, y) becomes
+ *   ( m (x cos a - y sin a),  m (y cos a + x sin a) )
+ * where the pair is elements (i, i + r/2) of the head (SEPLLM_ROPE_HALF) or
+ * (2i, 2i + 1) (SEPLLM_ROPE_INTERLEAVED).  Elements r .. d-1 are copied.  The
+ * frequencies are f_i = base^(-2i/r), changed for longer contexts by `scaling`
+ * (s = factor >= what the context grew by, N = orig_len, the context trained on):
+ *   NONE     unchanged
+ *   LINEAR   f_i / s
+ *   NTK      base replaced by base * s^(r/(r-2))            (r > 2)
+ *   YARN     f_i (1-g_i) + (f_i / s) g_i with g_i = clamp((i-lo)/(hi-lo), 0, 1),
+ *            lo = max(0, floor(t(high))), hi = min(r-1, ceil(t(low))),
+ *            t(n) = r ln(N / (2 pi n)) / (2 ln base): pairs that turn more than
+ *            `high` times over N positions stay, those below `low` are stretched
+ *            (hi = lo: hi is taken 0.001 larger)
+ *   LLAMA3   f_i k_i + (f_i / s) (1-k_i), k_i = clamp((n_i-low)/(high-low), 0, 1),
+ *            n_i = N f_i / (2 pi) the turns of the pair over N positions
+ *   FACTORS  f_i / freq_factors[i]   (host array of r/2, read during the call)
+ * m = attn_factor; 0 means 0.1 ln(s) + 1 for YARN with s > 1 and 1 otherwise.
+ * Angles are products in 64 bits, reduced to a part of a turn before they are
+ * rounded to 32 bits: exact to about 1e-6 for |p| up to 2^31.
+ * rot_dim = 0 means d; any even rot_dim up to d.  d as for the attention calls.
+ * pos_first: position of the first token where `positions` is NULL (token l has
+ *   position pos_first + l).  pos_stride: elements between two sequences' rows
+ *   of `positions` (L for a [B][L] array, 0 where all sequences share a row). */
+enum { SEPLLM_ROPE_HALF = 0, SEPLLM_ROPE_INTERLEAVED = 1 };
+enum {
+  SEPLLM_ROPE_NONE = 0,
+  SEPLLM_ROPE_LINEAR = 1,
+  SEPLLM_ROPE_NTK = 2,
+  SEPLLM_ROPE_YARN = 3,
+  SEPLLM_ROPE_LLAMA3 = 4,
+  SEPLLM_ROPE_FACTORS = 5
+};
+typedef struct {
+  int32_t B, L, Hq, Hkv, d, rot_dim, layout, scaling;
+  double base, factor, low, high, orig_len, attn_factor;
+  const double* freq_factors;
+  int64_t pos_first, pos_stride;
+} sepllm_rope_desc;
+
+/* One [B][H][L][d] tensor by its strides in elements (d contiguous), so that a
+ * slice of a fused projection [B][L][Hq+2Hkv][d] is read or written in place.
+ * dtype: 0 = bf16, 1 = fp32.  data = NULL: no such tensor. */
+typedef struct {
+  void* data;
+  int64_t stride_b, stride_h, stride_l;
+  int32_t dtype, reserved;
+} sepllm_rope_view;
+
+/* f_i (host [rot_dim/2], 64 bits) and m of a descriptor. */
+sepllm_status sepllm_rope_frequencies(const sepllm_rope_desc* desc, double* freq, double* m);
+
+/* Encodes positions: in / out are host arrays of three views, Q, K and V.  Q and
+ * K are rotated, V is copied (in the same launch, so that a fused projection is
+ * split and laid out for the attention calls in one pass).  A tensor that is NULL
+ * in both arrays is skipped; at least one is there.  All inputs have one dtype and
+ * all outputs have one; every sum is 32 bits and is rounded once.
+ *   positions dev int64, or NULL
+ * Inputs may have any non-negative strides (0 = broadcast).  Elements of an output
+ * must not share memory; an output may be its own input (same data, strides and
+ * dtype: in place) but no other overlap of inputs and outputs is allowed.  Rows of
+ * padding are handled like any other (the attention calls read them). */
+sepllm_status sepllm_rope_fwd(const sepllm_rope_desc* desc, const int64_t* positions,
+                              const sepllm_rope_view* in, const sepllm_rope_view* out,
+                              void* stream);
+
+/* Gradient of sepllm_rope_fwd: in = dL/d(its outputs), as sepllm_attn_bwd writes
+ * them (bf16 or fp32), out = dL/d(its inputs): the rotation by -a with the same m.
+ * Arguments as there. */
+sepllm_status sepllm_rope_bwd(const sepllm_rope_desc* desc, const int64_t* positions,
+                              const sepllm_rope_view* in, const sepllm_rope_view* out,
+                              void* stream);
+
 /* ---- streaming cache (Section 3.3, Tailored Streaming Design) --------------
  * Kc and Vc are bf16 [B][Hkv][slots][d] with slots = c + s: slots [0,a) are the
  * Initial Cache, [a, a+s) a ring holding the Separator Cache, [a+s, c+s) a ring

@@ -766,6 +766,46 @@ def rope_rotate(x: np.ndarray, pos, base: float) -> np.ndarray:
     return np.concatenate([lo * c - hi * s, hi * c + lo * s], axis=-1)
 
 
+def rope_frequencies(r: int, base: float, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
+                     high: float = 4.0, orig_len: float = 8192.0, freq_factors=None) -> np.ndarray:
+    """Angle per position of the r / 2 pairs, with the stretches for longer contexts: every
+    frequency by `factor` ("linear"), a larger base ("ntk"), by the pair's index between the pairs
+    that turn `high` and `low` times over orig_len positions ("yarn"), by the number of turns itself
+    ("llama3"), or one factor per pair ("factors")."""
+    i = np.arange(r // 2, dtype=np.float64)
+    if scaling == "ntk":
+        base = base * factor ** (r / (r - 2.0))
+    f = np.exp(-np.log(base) * 2.0 * i / r)
+    if scaling == "linear":
+        return f / factor
+    if scaling == "factors":
+        return f / np.asarray(freq_factors, dtype=np.float64)
+    if scaling == "yarn":
+        lo = max(0.0, np.floor(r * np.log(orig_len / (2 * np.pi * high)) / (2 * np.log(base))))
+        hi = min(r - 1.0, np.ceil(r * np.log(orig_len / (2 * np.pi * low)) / (2 * np.log(base))))
+        g = np.clip((i - lo) / (hi - lo if hi != lo else 0.001), 0.0, 1.0)
+        return f * (1 - g) + f / factor * g
+    if scaling == "llama3":
+        k = np.clip((orig_len * f / (2 * np.pi) - low) / (high - low), 0.0, 1.0)
+        return f * k + f / factor * (1 - k)
+    return f
+
+
+def rope_apply(x: np.ndarray, pos: np.ndarray, freq: np.ndarray, layout: str = "half", m: float = 1.0,
+               inverse: bool = False) -> np.ndarray:
+    """x [..., L, d] with its first 2 len(freq) elements turned pair by pair by pos[..., L] * freq
+    (pairs (i, i + r/2) or (2i, 2i + 1)) and scaled by m; inverse: by the negative angle, which with
+    the same m is the transposed map."""
+    n = len(freq)
+    ang = np.asarray(pos, dtype=np.float64)[..., None] * freq * (-1.0 if inverse else 1.0)
+    turn = m * np.exp(1j * ang)
+    out = np.array(x, dtype=np.float64)
+    a, b = (slice(0, n), slice(n, 2 * n)) if layout == "half" else (slice(0, 2 * n, 2), slice(1, 2 * n, 2))
+    z = (out[..., a] + 1j * out[..., b]) * turn
+    out[..., a], out[..., b] = z.real, z.imag
+    return out
+
+
 def decode_attention_rope(q, Kc, Vc, base: float, q_pos=None, k_pos=None, scale: float | None = None):
     """One un-rotated query over un-rotated retained keys given in cache order:
     key r sits at position r and the query at position R-1 (positions within

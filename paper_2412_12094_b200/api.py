@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -49,6 +50,32 @@ class CacheDesc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("B", "Hkv", "Hq", "d", "a", "s", "w", "c", "flags")]
 
 
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "llama3": 4, "factors": 5}
+
+
+class RopeDesc(C.Structure):
+    """sepllm_rope_desc.  rot_dim 0 = d; layout and scaling by name; freq_factors: a sequence of
+    rot_dim / 2 numbers; pos_stride defaults to L (positions [B][L])."""
+    _fields_ = ([(n, C.c_int32) for n in ("B", "L", "Hq", "Hkv", "d", "rot_dim", "layout", "scaling")]
+                + [(n, C.c_double) for n in ("base", "factor", "low", "high", "orig_len", "attn_factor")]
+                + [("freq_factors", C.POINTER(C.c_double)), ("pos_first", C.c_int64), ("pos_stride", C.c_int64)])
+
+    def __init__(self, B, L, Hq, Hkv, d, rot_dim=0, layout="half", scaling="none", base=10000.0, factor=1.0,
+                 low=1.0, high=4.0, orig_len=8192.0, attn_factor=0.0, freq_factors=None, pos_first=0,
+                 pos_stride=None):
+        self._keep = None
+        if freq_factors is not None:
+            n = (rot_dim or d) // 2
+            if len(freq_factors) != n:
+                raise ValueError(f"freq_factors has {len(freq_factors)} entries, not rot_dim / 2 = {n}")
+            self._keep = (C.c_double * n)(*freq_factors)
+        super().__init__(B, L, Hq, Hkv, d, rot_dim, ROPE_LAYOUTS.get(layout, layout),
+                         ROPE_SCALINGS.get(scaling, scaling), base, factor, low, high, orig_len, attn_factor,
+                         C.cast(self._keep, C.POINTER(C.c_double)) if self._keep else None, pos_first,
+                         L if pos_stride is None else pos_stride)
+
+
 class IndexHeader(C.Structure):
     _fields_ = [("status", C.c_int32), ("magic", C.c_uint32), ("version", C.c_uint32),
                 ("desc", IndexDesc), ("n_tiles", C.c_int32),
@@ -74,6 +101,7 @@ EXPORTS = [
     "sepllm_cache_from_prompt", "sepllm_cache_update_rope",
     "sepllm_decode_workspace_bytes", "sepllm_decode", "sepllm_rope_table_bytes",
     "sepllm_rope_table_build", "sepllm_decode_rope", "sepllm_last_device_status",
+    "sepllm_rope_frequencies", "sepllm_rope_fwd", "sepllm_rope_bwd",
     "sepllm_status_string",
 ]
 
@@ -118,6 +146,16 @@ def _ptr(t):
 
 def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _same_device(*tensors):
+    """The calls launch on the current device and its current stream: memory of another device is
+    refused here rather than read from there."""
+    cur = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != cur:
+            raise ValueError(f"tensor on {t.device}, current device is cuda:{cur}: "
+                             "make the tensors' device current for the call")
 
 
 def _sep_array(sep_ids):
@@ -219,6 +257,56 @@ def sepllm_attn_bwd(desc, idesc, dO, Q, K, V, O, LSE, index, dQ, dK, dV, workspa
     _check(lib().sepllm_attn_bwd(C.byref(desc), C.byref(idesc), _ptr(dO), _ptr(Q), _ptr(K), _ptr(V),
                                  _ptr(O), _ptr(LSE), _ptr(index), _ptr(dQ), _ptr(dK), _ptr(dV),
                                  _ptr(workspace), _stream()), "sepllm_attn_bwd")
+
+
+# ---------------------------------------------------------------- rotary positions
+def sepllm_rope_frequencies(desc: RopeDesc):
+    """(frequencies [rot_dim / 2] as numpy float64, factor on the rotated pair)."""
+    f, m = np.zeros(64), C.c_double(0.0)
+    _check(lib().sepllm_rope_frequencies(C.byref(desc), f.ctypes.data_as(C.c_void_p), C.byref(m)),
+           "sepllm_rope_frequencies")
+    return f[:(desc.rot_dim or desc.d) // 2].copy(), m.value
+
+
+_ROPE_DTYPES = {torch.bfloat16: 0, torch.float32: 1}
+_ROPE_VIEWS = struct.Struct("=" + "Qqqqii" * 3)   # three sepllm_rope_view
+
+
+def _rope_views(desc, tensors, what):
+    vals = []
+    for t, h in zip(tensors, (desc.Hq, desc.Hkv, desc.Hkv)):
+        if t is None:
+            vals += (0, 0, 0, 0, 0, 0)
+            continue
+        if t.shape != (desc.B, h, desc.L, desc.d):
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, the descriptor says {(desc.B, h, desc.L, desc.d)}")
+        sb, sh, sl, se = t.stride()
+        if t.dtype not in _ROPE_DTYPES or se != 1:
+            raise ValueError(f"{what}: bf16 or fp32 with contiguous head vectors, not {t.dtype} with strides "
+                             f"{t.stride()}")
+        vals += (t.data_ptr(), sb, sh, sl, _ROPE_DTYPES[t.dtype], 0)
+    return _ROPE_VIEWS.pack(*vals)
+
+
+def _rope(fn, where, desc, positions, ins, outs):
+    _same_device(positions, *ins, *outs)
+    if positions is not None and (positions.dtype != torch.int64 or not positions.is_contiguous()
+                                  or positions.numel() < (desc.B - 1) * desc.pos_stride + desc.L):
+        raise ValueError(f"{where}: positions are contiguous int64, pos_stride elements from row to row")
+    _check(fn(C.byref(desc), _ptr(positions), _rope_views(desc, ins, where), _rope_views(desc, outs, where),
+              _stream()), where)
+
+
+def sepllm_rope_fwd(desc: RopeDesc, positions, q, k, v, q_out, k_out, v_out):
+    """Rotates q and k and copies v.  Every tensor is [B][H][L][d] with any strides (the last one 1), so a
+    slice of a fused projection goes in as qkv.view(B, L, Hq + 2 * Hkv, d).transpose(1, 2).split(...);
+    a tensor and its output may both be None.  positions: int64 [B][L] (see desc.pos_stride) or None."""
+    _rope(lib().sepllm_rope_fwd, "sepllm_rope_fwd", desc, positions, (q, k, v), (q_out, k_out, v_out))
+
+
+def sepllm_rope_bwd(desc: RopeDesc, positions, dq_out, dk_out, dv_out, dq, dk, dv):
+    """Gradients of sepllm_rope_fwd's inputs from those of its outputs."""
+    _rope(lib().sepllm_rope_bwd, "sepllm_rope_bwd", desc, positions, (dq_out, dk_out, dv_out), (dq, dk, dv))
 
 
 # ---------------------------------------------------------------- cache

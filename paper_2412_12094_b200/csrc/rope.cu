@@ -1,0 +1,379 @@
+// Rotary positions of queries and keys, and their gradient.
+//
+// Pair (x, y) of a head at position p becomes m (x cos a - y sin a), m (y cos a + x sin a) with
+// a = p f_i; the gradient is the same map with -a.  Bound by HBM: every element of Q, K (and V,
+// which is only laid out) is read once and written once.  cos and sin depend on (token, pair) and
+// not on the head, so a thread takes one token and eight pairs, computes their cos and sin once and
+// walks the heads with them; there is no table to build, size or read.
+#include <cmath>
+
+#include "attn_common.cuh"
+
+namespace sepllm {
+
+namespace {
+
+constexpr int kRopeThreads = 128;
+constexpr int kMaxPairs = 64;
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+
+struct RopeTensor {
+  const void* in;
+  void* out;
+  int64_t ib, ih, il, ob, oh, ol;  // strides in elements
+  int heads;
+};
+
+struct RopeParams {
+  RopeTensor t[3];
+  const int64_t* pos;
+  int64_t pos_first, pos_stride;
+  int64_t tokens;         // B * L
+  int L, d, rot, n_heads, heads_per_block;
+  float m, sign;          // sign: +1 forward, -1 gradient
+  double turns[kMaxPairs];  // f_i / (2 pi)
+};
+
+// m cos and m sin of pair i at position p.  The angle is p f_i turns of which only the fraction
+// matters: the product and its reduction are 64 bits (p up to 2^31 leaves 2e-7 of a turn), what
+// is left is at most half a turn and is rounded to 32 bits.
+__device__ __forceinline__ float2 rope_cos_sin(const RopeParams& p, double pos, int i) {
+  const double t = pos * p.turns[i];
+  float sn, cs;
+  sincospif(2.f * float(t - rint(t)), &sn, &cs);
+  return make_float2(p.m * cs, p.m * p.sign * sn);
+}
+
+__device__ __forceinline__ double rope_position(const RopeParams& p, int64_t b, int l) {
+  return double(p.pos ? p.pos[b * p.pos_stride + l] : p.pos_first + l);
+}
+
+// Eight elements as floats, 16-byte accesses.
+__device__ __forceinline__ void load8(const __nv_bfloat16* s, float (&x)[8]) {
+  const uint4 u = *reinterpret_cast<const uint4*>(s);
+  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 f = __bfloat1622float2(h[k]);
+    x[2 * k] = f.x;
+    x[2 * k + 1] = f.y;
+  }
+}
+__device__ __forceinline__ void load8(const float* s, float (&x)[8]) {
+  const float4 a = reinterpret_cast<const float4*>(s)[0], c = reinterpret_cast<const float4*>(s)[1];
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+  x[4] = c.x; x[5] = c.y; x[6] = c.z; x[7] = c.w;
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* s, const float (&x)[8]) {
+  *reinterpret_cast<uint4*>(s) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]),
+                                            pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+__device__ __forceinline__ void store8(float* s, const float (&x)[8]) {
+  reinterpret_cast<float4*>(s)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(s)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ float load1(const __nv_bfloat16* s) { return __bfloat162float(*s); }
+__device__ __forceinline__ float load1(const float* s) { return *s; }
+__device__ __forceinline__ void store1(__nv_bfloat16* s, float x) { *s = __float2bfloat16(x); }
+__device__ __forceinline__ void store1(float* s, float x) { *s = x; }
+
+// A thread owns 16 elements of a row (two 16-byte pieces c0, c1) and walks the heads: eight pairs
+// whose halves are the two pieces (HALF), or four pairs in each piece (interleaved), or elements
+// that are only copied.  d / 16 neighbouring threads cover a row.
+template <class Tin, class Tout, bool HALF>
+__global__ void __launch_bounds__(kRopeThreads) rope_rows(const __grid_constant__ RopeParams p) {
+  const int per_row = p.d / 16;
+  const int64_t id = int64_t(blockIdx.x) * kRopeThreads + threadIdx.x;
+  const int64_t n = id / per_row;
+  if (n >= p.tokens) return;
+  const int t = int(id - n * per_row);
+  const int64_t b = n / p.L;
+  const int l = int(n - b * p.L);
+  int c0, c1;         // first elements of the two pieces
+  bool turn0, turn1;  // rotated (for Q and K)
+  if (HALF) {
+    const bool pair = t < p.rot / 16;
+    c0 = pair ? 8 * t : p.rot + 16 * (t - p.rot / 16);
+    c1 = pair ? c0 + p.rot / 2 : c0 + 8;
+    turn0 = turn1 = pair;
+  } else {
+    c0 = 16 * t;
+    c1 = c0 + 8;
+    turn0 = c0 < p.rot;
+    turn1 = c1 < p.rot;
+  }
+  const int h0 = blockIdx.y * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
+  float2 cs[8];
+  if (turn0 && h0 < p.t[0].heads + p.t[1].heads) {
+    const double pos = rope_position(p, b, l);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      cs[k] = (HALF || k < 4 || turn1) ? rope_cos_sin(p, pos, 8 * t + k) : make_float2(1.f, 0.f);
+  }
+  int first = 0;  // heads of the tensors before this one
+#pragma unroll
+  for (int w = 0; w < 3; ++w) {
+    const RopeTensor& x = p.t[w];
+    const int a = max(h0 - first, 0), e = min(h1 - first, x.heads);
+    first += x.heads;
+    const Tin* src = static_cast<const Tin*>(x.in) + b * x.ib + l * x.il;
+    Tout* dst = static_cast<Tout*>(x.out) + b * x.ob + l * x.ol;
+#pragma unroll 4
+    for (int h = a; h < e; ++h) {
+      float u[8], v[8];
+      load8(src + h * x.ih + c0, u);
+      load8(src + h * x.ih + c1, v);
+      if (w < 2) {
+        if (HALF) {
+          if (turn0) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float y0 = u[k] * cs[k].x - v[k] * cs[k].y;
+              v[k] = v[k] * cs[k].x + u[k] * cs[k].y;
+              u[k] = y0;
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (turn0) {
+              const float y0 = u[2 * k] * cs[k].x - u[2 * k + 1] * cs[k].y;
+              u[2 * k + 1] = u[2 * k + 1] * cs[k].x + u[2 * k] * cs[k].y;
+              u[2 * k] = y0;
+            }
+            if (turn1) {
+              const float y1 = v[2 * k] * cs[4 + k].x - v[2 * k + 1] * cs[4 + k].y;
+              v[2 * k + 1] = v[2 * k + 1] * cs[4 + k].x + v[2 * k] * cs[4 + k].y;
+              v[2 * k] = y1;
+            }
+          }
+        }
+      }
+      store8(dst + h * x.oh + c0, u);
+      store8(dst + h * x.oh + c1, v);
+    }
+  }
+}
+
+// Any rot_dim, stride and alignment: a thread owns one pair or one copied element.
+template <class Tin, class Tout, bool HALF>
+__global__ void __launch_bounds__(kRopeThreads) rope_elements(const __grid_constant__ RopeParams p) {
+  const int half = p.rot / 2, per_row = p.d - half;
+  const int64_t id = int64_t(blockIdx.x) * kRopeThreads + threadIdx.x;
+  const int64_t n = id / per_row;
+  if (n >= p.tokens) return;
+  const int t = int(id - n * per_row);
+  const int64_t b = n / p.L;
+  const int l = int(n - b * p.L);
+  const bool pair = t < half;
+  const int c0 = pair ? (HALF ? t : 2 * t) : t + half;
+  const int c1 = pair ? (HALF ? t + half : 2 * t + 1) : c0;
+  const int h0 = blockIdx.y * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
+  float2 cs = make_float2(1.f, 0.f);
+  if (pair && h0 < p.t[0].heads + p.t[1].heads) cs = rope_cos_sin(p, rope_position(p, b, l), t);
+  int first = 0;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) {
+    const RopeTensor& x = p.t[w];
+    const int a = max(h0 - first, 0), e = min(h1 - first, x.heads);
+    first += x.heads;
+    const Tin* src = static_cast<const Tin*>(x.in) + b * x.ib + l * x.il;
+    Tout* dst = static_cast<Tout*>(x.out) + b * x.ob + l * x.ol;
+#pragma unroll 4
+    for (int h = a; h < e; ++h) {
+      float u = load1(src + h * x.ih + c0);
+      float v = pair ? load1(src + h * x.ih + c1) : 0.f;
+      if (w < 2 && pair) {
+        const float y0 = u * cs.x - v * cs.y;
+        v = v * cs.x + u * cs.y;
+        u = y0;
+      }
+      store1(dst + h * x.oh + c0, u);
+      if (pair) store1(dst + h * x.oh + c1, v);
+    }
+  }
+}
+
+bool finite_positive(double x) { return x > 0.0 && std::isfinite(x); }
+
+sepllm_status check_rope(const sepllm_rope_desc* d) {
+  if (!d) return SEPLLM_INVALID_ARG;
+  if (d->B <= 0 || d->L <= 0 || d->Hq <= 0 || d->Hkv <= 0) return SEPLLM_INVALID_ARG;
+  if (d->d < 64 || d->d > 128 || d->d % 16 != 0) return SEPLLM_UNSUPPORTED;
+  const int r = d->rot_dim ? d->rot_dim : d->d;
+  if (r < 2 || r > d->d || r % 2 != 0) return SEPLLM_INVALID_ARG;
+  if (d->layout != SEPLLM_ROPE_HALF && d->layout != SEPLLM_ROPE_INTERLEAVED) return SEPLLM_INVALID_ARG;
+  if (d->scaling < SEPLLM_ROPE_NONE || d->scaling > SEPLLM_ROPE_FACTORS) return SEPLLM_INVALID_ARG;
+  if (!(d->base > 1.0) || !std::isfinite(d->base)) return SEPLLM_INVALID_ARG;
+  if (d->attn_factor != 0.0 && !finite_positive(d->attn_factor)) return SEPLLM_INVALID_ARG;
+  if (d->pos_stride < 0) return SEPLLM_INVALID_ARG;
+  if (d->scaling >= SEPLLM_ROPE_LINEAR && d->scaling <= SEPLLM_ROPE_LLAMA3 && !finite_positive(d->factor))
+    return SEPLLM_INVALID_ARG;
+  if (d->scaling == SEPLLM_ROPE_NTK && r == 2) return SEPLLM_INVALID_ARG;
+  if (d->scaling == SEPLLM_ROPE_YARN || d->scaling == SEPLLM_ROPE_LLAMA3)
+    if (!finite_positive(d->orig_len) || !finite_positive(d->low) || !finite_positive(d->high) ||
+        !(d->low < d->high))
+      return SEPLLM_INVALID_ARG;
+  if (d->scaling == SEPLLM_ROPE_FACTORS) {
+    if (!d->freq_factors) return SEPLLM_INVALID_ARG;
+    for (int i = 0; i < r / 2; ++i)
+      if (!finite_positive(d->freq_factors[i])) return SEPLLM_INVALID_ARG;
+  }
+  return SEPLLM_OK;
+}
+
+double clamp01(double x) { return x < 0.0 ? 0.0 : (x > 1.0 ? 1.0 : x); }
+
+// f_i, i < r/2, and m of a checked descriptor.
+void rope_frequencies(const sepllm_rope_desc* d, double* f, double* m) {
+  const int r = d->rot_dim ? d->rot_dim : d->d;
+  const double s = d->factor;
+  double base = d->base, lo = 0.0, hi = 0.0;
+  if (d->scaling == SEPLLM_ROPE_NTK) base *= std::pow(s, double(r) / (r - 2));
+  if (d->scaling == SEPLLM_ROPE_YARN) {
+    auto pair_of = [&](double turns) {
+      return r * std::log(d->orig_len / (kTwoPi * turns)) / (2.0 * std::log(base));
+    };
+    lo = std::fmax(0.0, std::floor(pair_of(d->high)));
+    hi = std::fmin(r - 1.0, std::ceil(pair_of(d->low)));
+    if (hi == lo) hi += 0.001;
+  }
+  for (int i = 0; i < r / 2; ++i) {
+    double v = std::pow(base, -2.0 * i / r);
+    if (d->scaling == SEPLLM_ROPE_LINEAR) v /= s;
+    if (d->scaling == SEPLLM_ROPE_FACTORS) v /= d->freq_factors[i];
+    if (d->scaling == SEPLLM_ROPE_YARN) {
+      const double g = clamp01((i - lo) / (hi - lo));
+      v = v * (1.0 - g) + v / s * g;
+    }
+    if (d->scaling == SEPLLM_ROPE_LLAMA3) {
+      const double k = clamp01((d->orig_len * v / kTwoPi - d->low) / (d->high - d->low));
+      v = v * k + v / s * (1.0 - k);
+    }
+    f[i] = v;
+  }
+  *m = d->attn_factor != 0.0 ? d->attn_factor
+       : (d->scaling == SEPLLM_ROPE_YARN && s > 1.0) ? 0.1 * std::log(s) + 1.0
+                                                     : 1.0;
+}
+
+// No two elements of [B][heads][L][d] share memory.  Sufficient: every stride covers the extent of
+// the dimensions with smaller strides.
+bool disjoint(const sepllm_rope_view& v, int64_t B, int64_t heads, int64_t L, int64_t d) {
+  int64_t size[3] = {B, heads, L}, stride[3] = {v.stride_b, v.stride_h, v.stride_l};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (stride[j] > stride[j + 1]) {
+        const int64_t a = stride[j], c = size[j];
+        stride[j] = stride[j + 1]; size[j] = size[j + 1];
+        stride[j + 1] = a; size[j + 1] = c;
+      }
+  int64_t extent = d;  // elements from the first to one past the last of the dimensions so far
+  for (int i = 0; i < 3; ++i) {
+    if (size[i] == 1) continue;
+    if (stride[i] < extent) return false;
+    extent += stride[i] * (size[i] - 1);
+  }
+  return true;
+}
+
+bool vector_access(const void* data, int64_t sb, int64_t sh, int64_t sl) {
+  return aligned(data, 16) && sb % 8 == 0 && sh % 8 == 0 && sl % 8 == 0;
+}
+
+template <class Tin, class Tout>
+void launch_rope(const RopeParams& p, bool rows, bool half, dim3 grid, cudaStream_t stream) {
+  if (rows) {
+    if (half) rope_rows<Tin, Tout, true><<<grid, kRopeThreads, 0, stream>>>(p);
+    else rope_rows<Tin, Tout, false><<<grid, kRopeThreads, 0, stream>>>(p);
+  } else {
+    if (half) rope_elements<Tin, Tout, true><<<grid, kRopeThreads, 0, stream>>>(p);
+    else rope_elements<Tin, Tout, false><<<grid, kRopeThreads, 0, stream>>>(p);
+  }
+}
+
+sepllm_status rope(const sepllm_rope_desc* d, const int64_t* positions, const sepllm_rope_view* in,
+                   const sepllm_rope_view* out, float sign, cudaStream_t stream) {
+  sepllm_status st = check_rope(d);
+  if (st != SEPLLM_OK) return st;
+  if (!in || !out || !aligned(positions, 8)) return SEPLLM_INVALID_ARG;
+  RopeParams p{};
+  p.rot = d->rot_dim ? d->rot_dim : d->d;
+  const bool half = d->layout == SEPLLM_ROPE_HALF;
+  // whole 16-byte pieces are rotated or copied as one (rope_rows), else element by element
+  bool rows = half ? p.rot % 16 == 0 : p.rot % 8 == 0;
+  int dt_in = -1, dt_out = -1;
+  for (int w = 0; w < 3; ++w) {
+    const sepllm_rope_view &a = in[w], &z = out[w];
+    if (!a.data && !z.data) continue;
+    if (!a.data || !z.data) return SEPLLM_INVALID_ARG;
+    if ((a.dtype != 0 && a.dtype != 1) || (z.dtype != 0 && z.dtype != 1)) return SEPLLM_INVALID_ARG;
+    if ((dt_in >= 0 && a.dtype != dt_in) || (dt_out >= 0 && z.dtype != dt_out)) return SEPLLM_INVALID_ARG;
+    dt_in = a.dtype;
+    dt_out = z.dtype;
+    if (!aligned(a.data, dt_in ? 4 : 2) || !aligned(z.data, dt_out ? 4 : 2)) return SEPLLM_INVALID_ARG;
+    if (a.stride_b < 0 || a.stride_h < 0 || a.stride_l < 0 || z.stride_b < 0 || z.stride_h < 0 ||
+        z.stride_l < 0)
+      return SEPLLM_INVALID_ARG;
+    const int heads = w == 0 ? d->Hq : d->Hkv;
+    if (!disjoint(z, d->B, heads, d->L, d->d)) return SEPLLM_INVALID_ARG;
+    // strides of dimensions of size 1 are never used
+    const int64_t ib = d->B > 1 ? a.stride_b : 0, ih = heads > 1 ? a.stride_h : 0, il = d->L > 1 ? a.stride_l : 0;
+    const int64_t ob = d->B > 1 ? z.stride_b : 0, oh = heads > 1 ? z.stride_h : 0, ol = d->L > 1 ? z.stride_l : 0;
+    if (a.data == z.data && (a.dtype != z.dtype || ib != ob || ih != oh || il != ol)) return SEPLLM_INVALID_ARG;
+    rows = rows && vector_access(a.data, ib, ih, il) && vector_access(z.data, ob, oh, ol);
+    p.t[w] = RopeTensor{a.data, z.data, ib, ih, il, ob, oh, ol, heads};
+    p.n_heads += heads;
+  }
+  if (p.n_heads == 0) return SEPLLM_INVALID_ARG;
+  double freq[kMaxPairs], m;
+  rope_frequencies(d, freq, &m);
+  for (int i = 0; i < p.rot / 2; ++i) p.turns[i] = freq[i] / kTwoPi;
+  p.m = float(m);
+  p.sign = sign;
+  p.pos = positions;
+  p.pos_first = d->pos_first;
+  p.pos_stride = d->pos_stride;
+  p.tokens = int64_t(d->B) * d->L;
+  p.L = d->L;
+  p.d = d->d;
+  const int64_t threads = p.tokens * (rows ? d->d / 16 : d->d - p.rot / 2);
+  const int64_t blocks = (threads + kRopeThreads - 1) / kRopeThreads;
+  if (blocks > 0x7fffffff) return SEPLLM_UNSUPPORTED;
+  p.heads_per_block = p.n_heads;
+  const int64_t groups = (p.n_heads + p.heads_per_block - 1) / p.heads_per_block;
+  if (groups > 65535) return SEPLLM_UNSUPPORTED;
+  const dim3 grid{unsigned(blocks), unsigned(groups)};
+  if (dt_in == 0 && dt_out == 0) launch_rope<__nv_bfloat16, __nv_bfloat16>(p, rows, half, grid, stream);
+  else if (dt_in == 0) launch_rope<__nv_bfloat16, float>(p, rows, half, grid, stream);
+  else if (dt_out == 0) launch_rope<float, __nv_bfloat16>(p, rows, half, grid, stream);
+  else launch_rope<float, float>(p, rows, half, grid, stream);
+  SEPLLM_CUDA_TRY(cudaGetLastError());
+  return SEPLLM_OK;
+}
+
+}  // namespace
+
+}  // namespace sepllm
+
+using namespace sepllm;
+
+extern "C" sepllm_status sepllm_rope_frequencies(const sepllm_rope_desc* desc, double* freq, double* m) {
+  sepllm_status st = check_rope(desc);
+  if (st != SEPLLM_OK) return st;
+  if (!freq || !m) return SEPLLM_INVALID_ARG;
+  rope_frequencies(desc, freq, m);
+  return SEPLLM_OK;
+}
+
+extern "C" sepllm_status sepllm_rope_fwd(const sepllm_rope_desc* desc, const int64_t* positions,
+                                         const sepllm_rope_view* in, const sepllm_rope_view* out,
+                                         void* stream_) {
+  return rope(desc, positions, in, out, 1.f, static_cast<cudaStream_t>(stream_));
+}
+
+extern "C" sepllm_status sepllm_rope_bwd(const sepllm_rope_desc* desc, const int64_t* positions,
+                                         const sepllm_rope_view* in, const sepllm_rope_view* out,
+                                         void* stream_) {
+  return rope(desc, positions, in, out, -1.f, static_cast<cudaStream_t>(stream_));
+}
