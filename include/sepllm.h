@@ -461,6 +461,44 @@ sepllm_status sepllm_decode_rope(const sepllm_cache_desc* desc, float scale, con
                                  const void* rope_table, void* o, float* lse, void* workspace,
                                  void* stream);
 
+/* ---- a prefix that the whole batch shares -----------------------------------
+ * Sequences that continue one text (a system prompt, a document) need its keys
+ * and values once, not once each.  (The paper treats one sequence at a time;
+ * the reading taken: what a prompt leaves behind under Section 3.2, its initial
+ * tokens, separators and last neighbours, stays in full view of every sequence
+ * that continues it.)  The shared prefix is
+ *   Kp, Vp     dev bf16 [Hkv][P][d], 16-byte aligned, keys rotated already where
+ *              the model has positions (sepllm_rope_fwd)
+ *   prefix_len dev int32 [B] or NULL: sequence b sees rows [0, prefix_len[b]) of
+ *              it (values are clamped to [0, P]; 0: none of it; NULL: all P), so
+ *              sequences that branch off early can share the same block
+ * Rows from the largest prefix_len on may hold anything; the rows before it have
+ * to be finite, also for sequences that do not see them.  P >= 1. */
+
+/* The retained entries of a cache of one sequence (desc->B = 1), in the order
+ * initial, separator (oldest first), neighbour (oldest first), become rows 0 ..
+ * Size_run-1 of Kp and Vp, and Size_run is written to the n_len words of
+ * prefix_len (n_len = 0: to none).  Other rows are left as they are.  P >= c
+ * (SEPLLM_BUFFER_TOO_SMALL otherwise).  Kc may be the rotated copy Kr. */
+sepllm_status sepllm_prefix_from_cache(const sepllm_cache_desc* desc, const void* state,
+                                       const void* Kc, const void* Vc, int32_t P, void* Kp,
+                                       void* Vp, int32_t* prefix_len, int32_t n_len,
+                                       void* stream);
+
+/* sepllm_decode with a shared prefix in front of every sequence's own cache: one
+ * softmax over prefix rows [0, prefix_len[b]) and the retained entries of sequence
+ * b.  A sequence that sees no entry at all gets o = 0 and lse = -inf.  o 16-byte
+ * aligned; workspace of sepllm_decode_prefix_workspace_bytes, 256-byte aligned
+ * (its first word is the device status); other arguments as sepllm_decode and
+ * above.  The prefix is read once for all sequences. */
+sepllm_status sepllm_decode_prefix_workspace_bytes(const sepllm_cache_desc* desc, int32_t P,
+                                                   size_t* bytes);
+sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int32_t P, float scale,
+                                   const void* q, const void* state, const void* Kc,
+                                   const void* Vc, const void* Kp, const void* Vp,
+                                   const int32_t* prefix_len, void* o, float* lse,
+                                   void* workspace, void* stream);
+
 /* Copies the device status word at the start of an index, workspace or state
  * buffer to *out (host) after synchronising `stream`. */
 sepllm_status sepllm_last_device_status(const void* buffer, int32_t* out, void* stream);

@@ -102,6 +102,7 @@ EXPORTS = [
     "sepllm_decode_workspace_bytes", "sepllm_decode", "sepllm_rope_table_bytes",
     "sepllm_rope_table_build", "sepllm_decode_rope", "sepllm_last_device_status",
     "sepllm_rope_frequencies", "sepllm_rope_fwd", "sepllm_rope_bwd",
+    "sepllm_prefix_from_cache", "sepllm_decode_prefix_workspace_bytes", "sepllm_decode_prefix",
     "sepllm_status_string",
 ]
 
@@ -367,6 +368,50 @@ def sepllm_decode_rope(desc, scale, q, state, Kr, Vc, rope_table, o, lse, worksp
     _check(lib().sepllm_decode_rope(C.byref(desc), C.c_float(scale), _ptr(q), _ptr(state), _ptr(Kr),
                                     _ptr(Vc), _ptr(rope_table), _ptr(o), _ptr(lse), _ptr(workspace),
                                     _stream()), "sepllm_decode_rope")
+
+
+# ---------------------------------------------------------------- shared prefix
+def _expect(where, **tensors):
+    """name = (tensor, shape, dtype): contiguous tensors of the current device."""
+    for name, (t, shape, dtype) in tensors.items():
+        if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous()):
+            raise ValueError(f"{where}: {name} is contiguous {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)} "
+                             f"with strides {t.stride()}")
+
+
+def sepllm_prefix_from_cache(desc, state, Kc, Vc, P, Kp, Vp, prefix_len=None):
+    """The retained entries of a cache of one sequence become rows 0 .. Size_run-1 of Kp, Vp [Hkv][P][d];
+    prefix_len: int32 of any length, every word is set to Size_run, or None."""
+    _same_device(state, Kc, Vc, Kp, Vp, prefix_len)
+    _expect("sepllm_prefix_from_cache", Kp=(Kp, (desc.Hkv, P, desc.d), torch.bfloat16),
+            Vp=(Vp, (desc.Hkv, P, desc.d), torch.bfloat16))
+    n = 0
+    if prefix_len is not None:
+        n = prefix_len.numel()
+        _expect("sepllm_prefix_from_cache", prefix_len=(prefix_len, (n,), torch.int32))
+    _check(lib().sepllm_prefix_from_cache(C.byref(desc), _ptr(state), _ptr(Kc), _ptr(Vc), C.c_int32(P), _ptr(Kp),
+                                          _ptr(Vp), _ptr(prefix_len), C.c_int32(n), _stream()),
+           "sepllm_prefix_from_cache")
+
+
+def sepllm_decode_prefix_workspace_bytes(desc, P):
+    b = C.c_size_t(0)
+    _check(lib().sepllm_decode_prefix_workspace_bytes(C.byref(desc), C.c_int32(P), C.byref(b)),
+           "sepllm_decode_prefix_workspace_bytes")
+    return b.value
+
+
+def sepllm_decode_prefix(desc, P, scale, q, state, Kc, Vc, Kp, Vp, prefix_len, o, lse, workspace):
+    """sepllm_decode with the shared prefix Kp, Vp [Hkv][P][d] in front of every cache; prefix_len: int32 [B]
+    or None (all P rows)."""
+    _same_device(q, state, Kc, Vc, Kp, Vp, prefix_len, o, lse, workspace)
+    bf, B, Hq, d = torch.bfloat16, desc.B, desc.Hq, desc.d
+    _expect("sepllm_decode_prefix", q=(q, (B, Hq, d), bf), o=(o, (B, Hq, d), bf), Kp=(Kp, (desc.Hkv, P, d), bf),
+            Vp=(Vp, (desc.Hkv, P, d), bf), prefix_len=(prefix_len, (B,), torch.int32),
+            lse=(lse, (B, Hq), torch.float32))
+    _check(lib().sepllm_decode_prefix(C.byref(desc), C.c_int32(P), C.c_float(scale), _ptr(q), _ptr(state), _ptr(Kc),
+                                      _ptr(Vc), _ptr(Kp), _ptr(Vp), _ptr(prefix_len), _ptr(o), _ptr(lse),
+                                      _ptr(workspace), _stream()), "sepllm_decode_prefix")
 
 
 def read_cache_state(state: torch.Tensor) -> dict:

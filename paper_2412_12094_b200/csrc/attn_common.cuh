@@ -179,4 +179,31 @@ void launch_gather(const sepllm_attn_desc* d, const sepllm_index_desc* id, int c
                    const void* K, const void* V, const int32_t* side_pos, const int32_t* n_side,
                    void* Ks, void* Vs, int32_t* status, cudaStream_t stream);
 
+// Attention over a prefix shared by the batch (prefix.cu).
+struct PrefixParams {
+  int B, Hkv, G, T, d, P;     // G query heads per kv head, T query tokens per sequence
+  int key_tiles, splits;      // 128-row tiles of the prefix, and how many CTAs share them
+  int rt, bt, row_tiles;      // row tile: rt rows of each of bt sequences; tiles per sequence
+  int m_tiles, alternate;     // row tiles per kv head; 1: one tile whose key tiles the slots take in turn
+  float scale_log2;
+  const int32_t* prefix_len;  // [B] or null (P for all)
+  const int32_t* seq_len;     // [B] or null: rows of tokens behind it are not written
+  float* part_ml;             // [row][splits << alternate] (reference exponent, sum)
+  float* part_acc;            // [row][splits << alternate][D]
+  const float* own_O;         // [row][D] the row's own part, normalised, and its log-sum-exp [row]
+  const float* own_lse;
+  int merge_O;                // 1: the kernel joins both parts itself (one split)
+  __nv_bfloat16* O;           // [row][d]
+  float* LSE;
+  int32_t* status;
+};
+// Sizes, tiles and splits (false: too large).  Rows are [B][Hkv][G * T].
+bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P);
+size_t prefix_part_bytes(const PrefixParams& p);
+void place_prefix_parts(PrefixParams* p, uint8_t* ws);
+sepllm_status launch_prefix(const PrefixParams& p, const void* Q, const void* Kp, const void* Vp,
+                            cudaStream_t stream);
+sepllm_status launch_prefix_join(const PrefixParams& p, const float* own_ml, const float* own_acc,
+                                 int own_parts, cudaStream_t stream);
+
 }  // namespace sepllm

@@ -924,14 +924,17 @@ extern "C" sepllm_status sepllm_cache_from_prompt(const sepllm_cache_desc* desc,
   return SEPLLM_OK;
 }
 
+static size_t own_part_bytes(const sepllm_cache_desc* desc, int splits) {
+  const size_t units = size_t(desc->B) * desc->Hq * splits;
+  return align_up(units * 2 * sizeof(float)) + align_up(units * desc->d * sizeof(float));
+}
+
 extern "C" sepllm_status sepllm_decode_workspace_bytes(const sepllm_cache_desc* desc,
                                                        size_t* bytes) {
   sepllm_cache_header h;
   sepllm_status st = fill_cache_header(desc, &h);
   if (st != SEPLLM_OK) return st;
-  const int splits = decode_splits(desc);
-  const size_t units = size_t(desc->B) * desc->Hq * splits;
-  if (bytes) *bytes = kAlign + align_up(units * 2 * sizeof(float)) + align_up(units * desc->d * sizeof(float));
+  if (bytes) *bytes = kAlign + own_part_bytes(desc, decode_splits(desc));
   return SEPLLM_OK;
 }
 
@@ -963,6 +966,20 @@ static sepllm_status dispatch_decode(bool with_rope, bool wide, const sepllm_cac
 #undef SEPLLM_DEC
 }
 
+// The partial results of a decode over the sequences' own caches, at `parts`.
+static sepllm_status launch_own_parts(const sepllm_cache_header& h, float scale, const void* q, const void* state,
+                                      const void* Kc, const void* Vc, const float2* rope, int splits, float* ml,
+                                      float* acc, int32_t* status, cudaStream_t stream) {
+  const sepllm_cache_desc& d = h.desc;
+  if (scale == 0.f) scale = 1.0f / sqrtf(float(d.d));
+  const float scale_log2 = scale * 1.4426950408889634f;
+  const bool wide = d.Hq / d.Hkv > 8;
+  return (d.d == 128) ? dispatch_decode<128>(rope != nullptr, wide, h, scale_log2, q, state, Kc, Vc, ml, acc,
+                                             splits, rope, status, stream)
+                      : dispatch_decode<64>(rope != nullptr, wide, h, scale_log2, q, state, Kc, Vc, ml, acc,
+                                            splits, rope, status, stream);
+}
+
 static sepllm_status decode_impl(const sepllm_cache_desc* desc, float scale, const void* q,
                                  const void* state, const void* Kc, const void* Vc,
                                  const float2* rope, void* o, float* lse, void* workspace,
@@ -983,14 +1000,7 @@ static sepllm_status decode_impl(const sepllm_cache_desc* desc, float scale, con
   // workspace's status word as OK itself, which saves a memset node per generated token)
   float* ml = reinterpret_cast<float*>(ws + kAlign);
   float* acc = reinterpret_cast<float*>(ws + kAlign + align_up(units * 2 * sizeof(float)));
-  if (scale == 0.f) scale = 1.0f / sqrtf(float(desc->d));
-  const float scale_log2 = scale * 1.4426950408889634f;
-  const bool wide = desc->Hq / desc->Hkv > 8;
-  st = (desc->d == 128)
-           ? dispatch_decode<128>(rope != nullptr, wide, h, scale_log2, q, state, Kc, Vc, ml, acc, splits, rope,
-                                  reinterpret_cast<int32_t*>(ws), stream)
-           : dispatch_decode<64>(rope != nullptr, wide, h, scale_log2, q, state, Kc, Vc, ml, acc, splits, rope,
-                                 reinterpret_cast<int32_t*>(ws), stream);
+  st = launch_own_parts(h, scale, q, state, Kc, Vc, rope, splits, ml, acc, reinterpret_cast<int32_t*>(ws), stream);
   if (st != SEPLLM_OK) return st;
   if (desc->d == 128)
     decode_combine<128><<<dim3(desc->Hq, desc->B), 128, 0, stream>>>(
@@ -1036,4 +1046,98 @@ extern "C" sepllm_status sepllm_decode_rope(const sepllm_cache_desc* desc, float
   if (!rope_table || !aligned(rope_table, 16)) return SEPLLM_INVALID_ARG;
   return decode_impl(desc, scale, q, state, Kc, Vc, static_cast<const float2*>(rope_table), o, lse,
                      workspace, stream_);
+}
+
+// ---------------------------------------------------------------------------
+// Decode behind a shared prefix
+// ---------------------------------------------------------------------------
+extern "C" sepllm_status sepllm_decode_prefix_workspace_bytes(const sepllm_cache_desc* desc, int32_t P,
+                                                              size_t* bytes) {
+  sepllm_cache_header h;
+  sepllm_status st = fill_cache_header(desc, &h);
+  if (st != SEPLLM_OK) return st;
+  if (P < 1) return SEPLLM_INVALID_ARG;
+  PrefixParams p{};
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P)) return SEPLLM_UNSUPPORTED;
+  if (bytes) *bytes = kAlign + own_part_bytes(desc, decode_splits(desc)) + prefix_part_bytes(p);
+  return SEPLLM_OK;
+}
+
+extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int32_t P, float scale, const void* q,
+                                              const void* state, const void* Kc, const void* Vc, const void* Kp,
+                                              const void* Vp, const int32_t* prefix_len, void* o, float* lse,
+                                              void* workspace, void* stream_) {
+  sepllm_cache_header h;
+  sepllm_status st = fill_cache_header(desc, &h);
+  if (st != SEPLLM_OK) return st;
+  if (P < 1 || !q || !state || !Kc || !Vc || !Kp || !Vp || !o || !workspace) return SEPLLM_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(Kp, 16) || !aligned(Vp, 16) ||
+      !aligned(workspace, kAlign) || !aligned(state, kAlign) || !aligned(o, 16) || !aligned(lse, 4) ||
+      !aligned(prefix_len, 4))
+    return SEPLLM_INVALID_ARG;
+  if (desc->B > 65535 || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
+  PrefixParams p{};
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P)) return SEPLLM_UNSUPPORTED;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const int own_parts = decode_splits(desc);
+  float* ml = reinterpret_cast<float*>(ws + kAlign);
+  float* acc = reinterpret_cast<float*>(
+      ws + kAlign + align_up(size_t(desc->B) * desc->Hq * own_parts * 2 * sizeof(float)));
+  place_prefix_parts(&p, ws + kAlign + own_part_bytes(desc, own_parts));
+  p.prefix_len = prefix_len;
+  p.O = static_cast<__nv_bfloat16*>(o);
+  p.LSE = lse;
+  p.status = reinterpret_cast<int32_t*>(ws);
+  p.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
+  // (the own part goes first: it writes the status word that the prefix kernel may set)
+  st = launch_own_parts(h, scale, q, state, Kc, Vc, nullptr, own_parts, ml, acc, p.status, stream);
+  if (st != SEPLLM_OK) return st;
+  if ((st = launch_prefix(p, q, Kp, Vp, stream)) != SEPLLM_OK) return st;
+  return launch_prefix_join(p, ml, acc, own_parts, stream);
+}
+
+// grid (row blocks, Hkv).  Row v of the prefix is retained entry v of the (only) sequence.
+template <int D>
+__global__ void __launch_bounds__(256)
+prefix_copy(sepllm_cache_header h, const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ Kc,
+            const __nv_bfloat16* __restrict__ Vc, int P, __nv_bfloat16* __restrict__ Kp,
+            __nv_bfloat16* __restrict__ Vp, int32_t* __restrict__ prefix_len, int n_len) {
+  constexpr int kVec = D / 8, kRows = 256 / kVec;  // 16-byte pieces of a row; rows per block
+  CacheView cv = cache_view(const_cast<uint8_t*>(state), h);
+  const sepllm_cache_seq q = cv.seq[0];
+  const int run = min(P, q.size_init + q.size_sep + q.size_win);
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int i = threadIdx.x; i < n_len; i += 256) prefix_len[i] = run;
+  const int v = blockIdx.x * kRows + threadIdx.x / kVec, ch = threadIdx.x % kVec;
+  if (v >= run) return;
+  const size_t src = (size_t(blockIdx.y) * h.slots + virtual_to_slot(v, q, h.desc)) * kVec + ch;
+  const size_t dst = (size_t(blockIdx.y) * P + v) * kVec + ch;
+  const uint4 k = reinterpret_cast<const uint4*>(Kc)[src], w = reinterpret_cast<const uint4*>(Vc)[src];
+  reinterpret_cast<uint4*>(Kp)[dst] = k;
+  reinterpret_cast<uint4*>(Vp)[dst] = w;
+}
+
+extern "C" sepllm_status sepllm_prefix_from_cache(const sepllm_cache_desc* desc, const void* state, const void* Kc,
+                                                  const void* Vc, int32_t P, void* Kp, void* Vp,
+                                                  int32_t* prefix_len, int32_t n_len, void* stream_) {
+  sepllm_cache_header h;
+  sepllm_status st = fill_cache_header(desc, &h);
+  if (st != SEPLLM_OK) return st;
+  if (desc->B != 1 || P < 1 || n_len < 0 || (n_len > 0 && !prefix_len)) return SEPLLM_INVALID_ARG;
+  if (!state || !Kc || !Vc || !Kp || !Vp) return SEPLLM_INVALID_ARG;
+  if (!aligned(state, kAlign) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(Kp, 16) || !aligned(Vp, 16) ||
+      !aligned(prefix_len, 4))
+    return SEPLLM_INVALID_ARG;
+  if (P < desc->c) return SEPLLM_BUFFER_TOO_SMALL;
+  if (desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  const int rows = 256 / (desc->d / 8);
+  const dim3 grid((desc->c + rows - 1) / rows, desc->Hkv);   // Size_run never passes c
+  auto kernel = desc->d == 128 ? prefix_copy<128> : prefix_copy<64>;
+  kernel<<<grid, 256, 0, stream>>>(h, static_cast<const uint8_t*>(state), static_cast<const __nv_bfloat16*>(Kc),
+                                   static_cast<const __nv_bfloat16*>(Vc), P, static_cast<__nv_bfloat16*>(Kp),
+                                   static_cast<__nv_bfloat16*>(Vp), prefix_len, n_len);
+  SEPLLM_CUDA_TRY(cudaGetLastError());
+  return SEPLLM_OK;
 }

@@ -1,0 +1,82 @@
+"""Shared-prefix calls, host side: sizes and refusals (no GPU; the addresses are never used)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2412_12094_b200 import api, build
+
+A = C.c_void_p(1 << 20)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    build.build()
+
+
+def _desc(**kw):
+    return api.CacheDesc(**dict(dict(B=3, Hkv=2, Hq=8, d=64, a=2, s=8, w=8, c=32, flags=0), **kw))
+
+
+def test_decode_workspace_holds_both_parts():
+    d = _desc()
+    own = api.sepllm_decode_workspace_bytes(d)
+    for P in (1, 127, 128, 129, 100000):
+        n = api.sepllm_decode_prefix_workspace_bytes(d, P)
+        assert n % 256 == 0 and n >= own + 3 * 8 * (64 + 2) * 4
+    with pytest.raises(api.SepllmError) as e:
+        api.sepllm_decode_prefix_workspace_bytes(d, 0)
+    assert e.value.code == api.INVALID_ARG
+    with pytest.raises(api.SepllmError) as e:
+        api.sepllm_decode_prefix_workspace_bytes(_desc(d=80), 5)
+    assert e.value.code == api.UNSUPPORTED
+
+
+def _decode(desc=None, P=100, **over):
+    names = ("q", "state", "Kc", "Vc", "Kp", "Vp", "prefix_len", "o", "lse", "workspace")
+    v = dict({n: A for n in names}, **over)
+    desc = _desc() if desc is None else desc
+    return api.lib().sepllm_decode_prefix(C.byref(desc), C.c_int32(P), C.c_float(0.0), v["q"], v["state"], v["Kc"],
+                                          v["Vc"], v["Kp"], v["Vp"], v["prefix_len"], v["o"], v["lse"],
+                                          v["workspace"], None)
+
+
+def test_decode_refusals():
+    for name in ("q", "state", "Kc", "Vc", "Kp", "Vp", "o", "workspace"):
+        assert _decode(**{name: None}) == api.INVALID_ARG
+        assert _decode(**{name: C.c_void_p((1 << 20) + 8)}) == api.INVALID_ARG
+    for name in ("prefix_len", "lse"):
+        assert _decode(**{name: C.c_void_p((1 << 20) + 2)}) == api.INVALID_ARG
+    assert _decode(P=0) == api.INVALID_ARG and _decode(P=-5) == api.INVALID_ARG
+    assert _decode(_desc(B=0)) == api.INVALID_ARG and _decode(_desc(w=0)) == api.INVALID_ARG
+    assert _decode(_desc(Hq=7)) == api.INVALID_ARG
+    assert _decode(_desc(d=80)) == api.UNSUPPORTED and _decode(_desc(Hq=34)) == api.UNSUPPORTED
+    assert _decode(_desc(B=65536)) == api.UNSUPPORTED
+
+
+def _copy(desc=None, P=32, n=3, **over):
+    v = dict({k: A for k in ("state", "Kc", "Vc", "Kp", "Vp", "prefix_len")}, **over)
+    desc = _desc(B=1) if desc is None else desc
+    return api.lib().sepllm_prefix_from_cache(C.byref(desc), v["state"], v["Kc"], v["Vc"], C.c_int32(P), v["Kp"],
+                                              v["Vp"], v["prefix_len"], C.c_int32(n), None)
+
+
+def test_prefix_from_cache_refusals():
+    for name in ("state", "Kc", "Vc", "Kp", "Vp"):
+        assert _copy(**{name: None}) == api.INVALID_ARG
+        assert _copy(**{name: C.c_void_p((1 << 20) + 8)}) == api.INVALID_ARG
+    assert _copy(prefix_len=None) == api.INVALID_ARG
+    assert _copy(prefix_len=C.c_void_p((1 << 20) + 2)) == api.INVALID_ARG
+    assert _copy(n=-1) == api.INVALID_ARG and _copy(P=0) == api.INVALID_ARG
+    assert _copy(_desc(B=2)) == api.INVALID_ARG
+    assert _copy(P=31) == api.BUFFER_TOO_SMALL
+
+
+def test_binding_refuses_other_shapes_and_types():
+    with pytest.raises(ValueError):
+        api._expect("x", q=(torch.zeros(2, 3), (2, 4), torch.float32))
+    with pytest.raises(ValueError):
+        api._expect("x", q=(torch.zeros(2, 4), (2, 4), torch.bfloat16))
+    with pytest.raises(ValueError):
+        api._expect("x", q=(torch.zeros(4, 2).t(), (2, 4), torch.float32))
+    api._expect("x", q=(None, (2, 4), torch.float32))
