@@ -499,6 +499,24 @@ sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int32_t P, flo
                                    const int32_t* prefix_len, void* o, float* lse,
                                    void* workspace, void* stream);
 
+/* sepllm_attn_fwd with the shared prefix in front of every sequence: pre-filling
+ * the tokens that follow it.  Row i of sequence b attends to prefix rows
+ * [0, prefix_len[b]) in full and to the keys of its own row that the index keeps
+ * (Eq. 2's mask; where the prefix brings the initial tokens, n_init = 0; in a row
+ * that packs several documents each of them continues the prefix), under one
+ * softmax.  Rows behind a sequence's end (sepllm_build_index_varlen) are not
+ * written at all.  desc->events and flags as there; workspace of
+ * sepllm_attn_prefix_workspace_bytes, 256-byte aligned.  Serving only: there is no
+ * gradient. */
+sepllm_status sepllm_attn_prefix_workspace_bytes(const sepllm_attn_desc* desc,
+                                                 const sepllm_index_desc* idesc, int32_t P,
+                                                 size_t* bytes);
+sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc,
+                                     int32_t P, const void* Q, const void* K, const void* V,
+                                     const void* index, const void* Kp, const void* Vp,
+                                     const int32_t* prefix_len, void* O, float* LSE,
+                                     void* workspace, void* stream);
+
 /* Copies the device status word at the start of an index, workspace or state
  * buffer to *out (host) after synchronising `stream`. */
 sepllm_status sepllm_last_device_status(const void* buffer, int32_t* out, void* stream);

@@ -103,6 +103,7 @@ EXPORTS = [
     "sepllm_rope_table_build", "sepllm_decode_rope", "sepllm_last_device_status",
     "sepllm_rope_frequencies", "sepllm_rope_fwd", "sepllm_rope_bwd",
     "sepllm_prefix_from_cache", "sepllm_decode_prefix_workspace_bytes", "sepllm_decode_prefix",
+    "sepllm_attn_prefix_workspace_bytes", "sepllm_attn_prefix_fwd",
     "sepllm_status_string",
 ]
 
@@ -412,6 +413,26 @@ def sepllm_decode_prefix(desc, P, scale, q, state, Kc, Vc, Kp, Vp, prefix_len, o
     _check(lib().sepllm_decode_prefix(C.byref(desc), C.c_int32(P), C.c_float(scale), _ptr(q), _ptr(state), _ptr(Kc),
                                       _ptr(Vc), _ptr(Kp), _ptr(Vp), _ptr(prefix_len), _ptr(o), _ptr(lse),
                                       _ptr(workspace), _stream()), "sepllm_decode_prefix")
+
+
+def sepllm_attn_prefix_workspace_bytes(desc: AttnDesc, idesc: IndexDesc, P):
+    b = C.c_size_t(0)
+    _check(lib().sepllm_attn_prefix_workspace_bytes(C.byref(desc), C.byref(idesc), C.c_int32(P), C.byref(b)),
+           "sepllm_attn_prefix_workspace_bytes")
+    return b.value
+
+
+def sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, prefix_len, O, LSE, workspace):
+    """sepllm_attn_fwd with the shared prefix Kp, Vp [Hkv][P][d] in front of every sequence; prefix_len:
+    int32 [B] or None (all P rows)."""
+    _same_device(Q, K, V, index, Kp, Vp, prefix_len, O, LSE, workspace)
+    bf, B, Hq, Hkv, L, d = torch.bfloat16, desc.B, desc.Hq, desc.Hkv, desc.L, desc.d
+    _expect("sepllm_attn_prefix_fwd", Q=(Q, (B, Hq, L, d), bf), K=(K, (B, Hkv, L, d), bf), V=(V, (B, Hkv, L, d), bf),
+            O=(O, (B, Hq, L, d), bf), Kp=(Kp, (Hkv, P, d), bf), Vp=(Vp, (Hkv, P, d), bf),
+            prefix_len=(prefix_len, (B,), torch.int32), LSE=(LSE, (B, Hq, L), torch.float32))
+    _check(lib().sepllm_attn_prefix_fwd(C.byref(desc), C.byref(idesc), C.c_int32(P), _ptr(Q), _ptr(K), _ptr(V),
+                                        _ptr(index), _ptr(Kp), _ptr(Vp), _ptr(prefix_len), _ptr(O), _ptr(LSE),
+                                        _ptr(workspace), _stream()), "sepllm_attn_prefix_fwd")
 
 
 def read_cache_state(state: torch.Tensor) -> dict:

@@ -116,6 +116,7 @@ struct FwdParams {
   const int32_t* doc_start;  // [B][L]   (packed index only)
   const int32_t* doc_end;    // [B][L]
   __nv_bfloat16* O;
+  float* O32;                // the F32 kernels write rows of D floats here instead of O
   float* LSE;
   int32_t* status;
   int L, T, Hq, Hkv, n_neighbor, side_cap, side_tiles_cap, pair_heads;
@@ -156,6 +157,12 @@ __global__ void gather_side_kv(const __nv_bfloat16* __restrict__ K,
 sepllm_status launch_fwd_pair(const sepllm_attn_desc* d, const FwdParams& p, int n_tiles,
                               const CUtensorMap& mq, const CUtensorMap& mk64, const CUtensorMap& mv,
                               const CUtensorMap& mks64, const CUtensorMap& mvs, cudaStream_t stream);
+
+// The forward with its output left in 32 bits, to be joined with another part: O32
+// [B][Hq][L][kernel_head_dim(d)].  Arguments as sepllm_attn_fwd, checked by the caller.
+sepllm_status attn_fwd_f32(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc, const void* Q,
+                           const void* K, const void* V, const void* index, float* O32, float* LSE,
+                           void* workspace, cudaStream_t stream);
 
 // Number of SMs of the current device (persistent kernels launch one CTA per SM).
 inline int sm_count() {

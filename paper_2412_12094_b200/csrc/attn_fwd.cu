@@ -110,7 +110,8 @@ struct FwdCfg {
 
 constexpr int kFwdThreads = 384;
 
-template <int D>
+// F32: the output stays in 32 bits (rows of D floats) for a caller that joins it with another part.
+template <int D, bool F32>
 __global__ void __launch_bounds__(kFwdThreads, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
                 const __grid_constant__ CUtensorMap mapV, const __grid_constant__ CUtensorMap mapKs,
@@ -416,7 +417,14 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         uint32_t oreg[32];
         tmem_ld32(tO + c * 32, oreg);
         tmem_ld_wait();
-        if (row < p.L) {
+        if (F32) {
+          if (row < p.L)
+#pragma unroll
+            for (int q8 = 0; q8 < 8; ++q8)
+              *reinterpret_cast<float4*>(p.O32 + (size_t(q_plane) * p.L + row) * D + c * 32 + q8 * 4) =
+                  make_float4(__uint_as_float(oreg[4 * q8]) * inv_l, __uint_as_float(oreg[4 * q8 + 1]) * inv_l,
+                              __uint_as_float(oreg[4 * q8 + 2]) * inv_l, __uint_as_float(oreg[4 * q8 + 3]) * inv_l);
+        } else if (row < p.L) {
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
             uint4 val;
@@ -487,7 +495,7 @@ void launch_gather(const sepllm_attn_desc* d, const sepllm_index_desc* id, int c
   }
 }
 
-template <int D>
+template <int D, bool F32>
 static sepllm_status launch_fwd(const sepllm_attn_desc* d, const sepllm_index_desc* id,
                                 const sepllm_index_header& ih, const void* Q, const void* K,
                                 const void* V, const uint8_t* index, void* O, float* LSE,
@@ -521,7 +529,8 @@ static sepllm_status launch_fwd(const sepllm_attn_desc* d, const sepllm_index_de
   p.seq_len = reinterpret_cast<const int32_t*>(index + ih.off_seq_len);
   p.doc_start = reinterpret_cast<const int32_t*>(index + ih.off_doc_start);
   p.doc_end = reinterpret_cast<const int32_t*>(index + ih.off_doc_end);
-  p.O = static_cast<__nv_bfloat16*>(O);
+  p.O = F32 ? nullptr : static_cast<__nv_bfloat16*>(O);
+  p.O32 = F32 ? static_cast<float*>(O) : nullptr;
   p.LSE = LSE;
   p.status = reinterpret_cast<int32_t*>(ws);
   p.L = d->L;
@@ -547,11 +556,11 @@ static sepllm_status launch_fwd(const sepllm_attn_desc* d, const sepllm_index_de
     return st;
   }
   const uint32_t smem = FwdCfg<D>::kRequest;
-  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(attn_fwd_kernel<D>,
+  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(attn_fwd_kernel<D, F32>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
   const dim3 grid = p.pair_heads ? dim3(d->Hq / 2 * d->B, ih.n_tiles)
                                  : dim3(d->Hq * d->B, (ih.n_tiles + 1) / 2);
-  attn_fwd_kernel<D><<<grid, kFwdThreads, smem, stream>>>(mq, mk, mv, mks, mvs, p);
+  attn_fwd_kernel<D, F32><<<grid, kFwdThreads, smem, stream>>>(mq, mk, mv, mks, mvs, p);
   record_event(d, 2, stream);
   SEPLLM_CUDA_TRY(cudaGetLastError());
   return SEPLLM_OK;
@@ -560,6 +569,27 @@ static sepllm_status launch_fwd(const sepllm_attn_desc* d, const sepllm_index_de
 }  // namespace sepllm
 
 using namespace sepllm;
+
+// (the side gather, the call's first launch, resets the status word)
+template <bool F32>
+static sepllm_status forward(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc, const void* Q,
+                             const void* K, const void* V, const void* index, void* O, float* LSE,
+                             void* workspace, cudaStream_t stream) {
+  sepllm_status st;
+  sepllm_index_header ih;
+  if ((st = fill_index_header(idesc, &ih)) != SEPLLM_OK) return st;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  if (desc->flags & SEPLLM_ATTN_SIDE_READY) SEPLLM_CUDA_TRY(cudaMemsetAsync(ws, 0, sizeof(int32_t), stream));
+  if (kernel_head_dim(desc->d) == 64)
+    return launch_fwd<64, F32>(desc, idesc, ih, Q, K, V, static_cast<const uint8_t*>(index), O, LSE, ws, stream);
+  return launch_fwd<128, F32>(desc, idesc, ih, Q, K, V, static_cast<const uint8_t*>(index), O, LSE, ws, stream);
+}
+
+sepllm_status sepllm::attn_fwd_f32(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc, const void* Q,
+                                   const void* K, const void* V, const void* index, float* O32, float* LSE,
+                                   void* workspace, cudaStream_t stream) {
+  return forward<true>(desc, idesc, Q, K, V, index, O32, LSE, workspace, stream);
+}
 
 extern "C" sepllm_status sepllm_attn_fwd(const sepllm_attn_desc* desc,
                                          const sepllm_index_desc* idesc, const void* Q,
@@ -571,15 +601,5 @@ extern "C" sepllm_status sepllm_attn_fwd(const sepllm_attn_desc* desc,
   if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(O, 16) ||
       !aligned(LSE, 4) || !aligned(index, kAlign) || !aligned(workspace, kAlign))
     return SEPLLM_INVALID_ARG;
-  sepllm_index_header ih;
-  if ((st = fill_index_header(idesc, &ih)) != SEPLLM_OK) return st;
-  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
-  // (the side gather, the call's first launch, resets the status word)
-  if (desc->flags & SEPLLM_ATTN_SIDE_READY) SEPLLM_CUDA_TRY(cudaMemsetAsync(ws, 0, sizeof(int32_t), stream));
-  if (kernel_head_dim(desc->d) == 64)
-    return launch_fwd<64>(desc, idesc, ih, Q, K, V, static_cast<const uint8_t*>(index), O, LSE, ws,
-                          stream);
-  return launch_fwd<128>(desc, idesc, ih, Q, K, V, static_cast<const uint8_t*>(index), O, LSE, ws,
-                         stream);
+  return forward<false>(desc, idesc, Q, K, V, index, O, LSE, workspace, static_cast<cudaStream_t>(stream_));
 }

@@ -52,6 +52,8 @@ static_assert(PairSmem::kRequest <= 227 * 1024, "shared memory budget");
 constexpr int kPairThreads = 384;
 constexpr long long kSlotOffsetCycles = 1600;
 
+// F32: the output stays in 32 bits for a caller that joins it with another part.
+template <bool F32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK64,
                      const __grid_constant__ CUtensorMap mapV, const __grid_constant__ CUtensorMap mapKs64,
@@ -398,7 +400,14 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
       uint32_t oreg[32];
       tmem_ld32(tO + c * 32, oreg);
       tmem_ld_wait();
-      if (row < p.L) {
+      if (F32) {
+        if (row < p.L)
+#pragma unroll
+          for (int q8 = 0; q8 < 8; ++q8)
+            *reinterpret_cast<float4*>(p.O32 + (size_t(q_plane) * p.L + row) * kD + c * 32 + q8 * 4) =
+                make_float4(__uint_as_float(oreg[4 * q8]) * inv_l, __uint_as_float(oreg[4 * q8 + 1]) * inv_l,
+                            __uint_as_float(oreg[4 * q8 + 2]) * inv_l, __uint_as_float(oreg[4 * q8 + 3]) * inv_l);
+      } else if (row < p.L) {
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
           uint4 val;
@@ -424,11 +433,11 @@ sepllm_status launch_fwd_pair(const sepllm_attn_desc* d, const FwdParams& p, int
                               const CUtensorMap& mq, const CUtensorMap& mk64, const CUtensorMap& mv,
                               const CUtensorMap& mks64, const CUtensorMap& mvs, cudaStream_t stream) {
   const uint32_t smem = PairSmem::kRequest;
-  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(attn_fwd_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       int(smem)));
+  auto kernel = p.O32 ? attn_fwd_pair_kernel<true> : attn_fwd_pair_kernel<false>;
+  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
   // x = pairs of query heads of every sequence: even, and a cluster never straddles two kv heads
   const dim3 grid(d->Hq / 2 * d->B, n_tiles);
-  attn_fwd_pair_kernel<<<grid, kPairThreads, smem, stream>>>(mq, mk64, mv, mks64, mvs, p);
+  kernel<<<grid, kPairThreads, smem, stream>>>(mq, mk64, mv, mks64, mvs, p);
   SEPLLM_CUDA_TRY(cudaGetLastError());
   return SEPLLM_OK;
 }

@@ -543,3 +543,70 @@ sepllm_status launch_prefix_join(const PrefixParams& p, const float* own_ml, con
 }
 
 }  // namespace sepllm
+
+using namespace sepllm;
+
+// Workspace of a forward behind a prefix: the forward's own | O32 | LSE of the own part | parts.
+namespace {
+struct AttnPrefixLayout {
+  size_t off_o, off_lse, off_parts, bytes;
+};
+AttnPrefixLayout attn_prefix_layout(const sepllm_attn_desc* d, const sepllm_index_desc* id, const PrefixParams& p) {
+  AttnPrefixLayout a;
+  const size_t rows = size_t(d->B) * d->Hq * d->L;
+  a.off_o = attn_layout(d, id).fwd_bytes;
+  a.off_lse = a.off_o + align_up(rows * kernel_head_dim(d->d) * sizeof(float));
+  a.off_parts = a.off_lse + align_up(rows * sizeof(float));
+  a.bytes = a.off_parts + (p.splits > 1 || p.alternate ? prefix_part_bytes(p) : 0);
+  return a;
+}
+}  // namespace
+
+extern "C" sepllm_status sepllm_attn_prefix_workspace_bytes(const sepllm_attn_desc* desc,
+                                                            const sepllm_index_desc* idesc, int32_t P,
+                                                            size_t* bytes) {
+  sepllm_status st = check_attn(desc, idesc);
+  if (st != SEPLLM_OK) return st;
+  if (P < 1) return SEPLLM_INVALID_ARG;
+  PrefixParams p{};
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P)) return SEPLLM_UNSUPPORTED;
+  if (bytes) *bytes = attn_prefix_layout(desc, idesc, p).bytes;
+  return SEPLLM_OK;
+}
+
+extern "C" sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc,
+                                                int32_t P, const void* Q, const void* K, const void* V,
+                                                const void* index, const void* Kp, const void* Vp,
+                                                const int32_t* prefix_len, void* O, float* LSE, void* workspace,
+                                                void* stream_) {
+  sepllm_status st = check_attn(desc, idesc);
+  if (st != SEPLLM_OK) return st;
+  if (P < 1 || !Q || !K || !V || !index || !Kp || !Vp || !O || !LSE || !workspace) return SEPLLM_INVALID_ARG;
+  if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(Kp, 16) || !aligned(Vp, 16) ||
+      !aligned(O, 16) || !aligned(LSE, 4) || !aligned(prefix_len, 4) || !aligned(index, kAlign) ||
+      !aligned(workspace, kAlign))
+    return SEPLLM_INVALID_ARG;
+  sepllm_index_header ih;
+  if ((st = fill_index_header(idesc, &ih)) != SEPLLM_OK) return st;
+  PrefixParams p{};
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P)) return SEPLLM_UNSUPPORTED;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const AttnPrefixLayout lay = attn_prefix_layout(desc, idesc, p);
+  float* own_O = reinterpret_cast<float*>(ws + lay.off_o);
+  float* own_lse = reinterpret_cast<float*>(ws + lay.off_lse);
+  // the rows' own tokens first (Eq. 2's mask); their result waits in 32 bits so that O is rounded once
+  if ((st = attn_fwd_f32(desc, idesc, Q, K, V, index, own_O, own_lse, ws, stream)) != SEPLLM_OK) return st;
+  place_prefix_parts(&p, ws + lay.off_parts);
+  p.prefix_len = prefix_len;
+  p.seq_len = reinterpret_cast<const int32_t*>(static_cast<const uint8_t*>(index) + ih.off_seq_len);
+  p.own_O = own_O;
+  p.own_lse = own_lse;
+  p.merge_O = p.splits == 1 && !p.alternate;
+  p.O = static_cast<__nv_bfloat16*>(O);
+  p.LSE = LSE;
+  p.status = reinterpret_cast<int32_t*>(ws);
+  p.scale_log2 = (desc->scale != 0.f ? desc->scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
+  if ((st = launch_prefix(p, Q, Kp, Vp, stream)) != SEPLLM_OK) return st;
+  return p.merge_O ? SEPLLM_OK : launch_prefix_join(p, nullptr, nullptr, 0, stream);
+}

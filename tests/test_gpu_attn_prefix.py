@@ -1,0 +1,252 @@
+"""sepllm_attn_prefix_fwd against the oracle's masked softmax over the joined keys, and a serving run
+through the shared prefix from the prompt to generated tokens."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import sepllm_oracle as orc
+from paper_2412_12094_b200 import api, inputs
+from tests._gpu_util import TOL_LSE, TOL_O, build_index
+from tests.test_gpu_cache import GpuCache
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def _normal(g, *shape):
+    return torch.randn(shape, generator=g, device="cuda").to(BF)
+
+
+def _index(ids, n, a=0, seq_len=None, doc_first=None):
+    B, L = ids.shape
+    if seq_len is None and doc_first is None:
+        return build_index(ids, inputs.SEP_IDS, a, n)
+    desc = api.IndexDesc(B, L, a, n, len(inputs.SEP_IDS), 128, 128, L)
+    ib, sb = api.sepllm_index_bytes(desc)
+    index, scratch = api.alloc_bytes(ib), api.alloc_bytes(sb)
+    ids_d = torch.from_numpy(np.ascontiguousarray(ids)).cuda()
+    len_d = None if seq_len is None else torch.tensor(seq_len, dtype=torch.int32, device="cuda")
+    if doc_first is not None:
+        api.sepllm_build_index_packed(desc, ids_d, torch.from_numpy(doc_first).cuda(), len_d, inputs.SEP_IDS, index)
+    else:
+        api.sepllm_build_index_varlen(desc, ids_d, len_d, inputs.SEP_IDS, index, scratch)
+    return desc, index
+
+
+def _run(Q, K, V, idesc, index, Kp, Vp, plen, scale=0.0, out=None):
+    B, Hq, L, d = Q.shape
+    P = Kp.shape[1]
+    desc = api.AttnDesc(B, Hq, K.shape[1], d, L, scale, 0)
+    ws = api.alloc_bytes(api.sepllm_attn_prefix_workspace_bytes(desc, idesc, P))
+    ws.fill_(0xff)
+    O, LSE = out or (torch.full_like(Q, 3.5), torch.full((B, Hq, L), -2.5, device="cuda"))
+    api.sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, plen, O, LSE, ws)
+    torch.cuda.synchronize()
+    assert api.sepllm_last_device_status(ws) == 0
+    return O, LSE
+
+
+def _check(Q, K, V, Kp, Vp, masks, plen, seq_len, O, LSE, scale=None, heads=None):
+    """Beside the common bounds an entry gets what its terms cost: weights rounded to bf16 (2^-9 at
+    most relative to the running reference, five deviations of the terms' root sum of squares) and
+    half a step of the bf16 output."""
+    B, Hq, L, d = Q.shape
+    G = Hq // K.shape[1]
+    num, den = 0.0, 0.0
+    for b in range(B):
+        n, m = seq_len[b], plen[b]
+        M = np.concatenate((np.ones((n, m), bool), masks[b][:n, :n]), 1)
+        for h in heads or range(Hq):
+            q = Q[b, h, :n].double().cpu().numpy()
+            k, v = (np.concatenate((x[h // G, :m].double().cpu().numpy(), y[b, h // G, :n].double().cpu().numpy()))
+                    for x, y in ((Kp, K), (Vp, V)))
+            ref, lref, A = orc.attn_fwd_rows(q, k, v, M, scale)
+            rss = np.sqrt(A ** 2 @ v ** 2)
+            err = np.abs(O[b, h, :n].double().cpu().numpy() - ref)
+            tol = np.maximum(TOL_O["max_abs"], 5 * 2.0 ** -9 * rss + 2.0 ** -8 * np.abs(ref))
+            assert (err <= tol).all(), (b, h, float((err / tol).max()))
+            num, den = num + (err ** 2).sum(), den + (ref ** 2).sum()
+            assert np.abs(LSE[b, h, :n].double().cpu().numpy() - lref).max(initial=0.0) <= TOL_LSE, (b, h)
+            # rows behind the end are left as they were
+            assert (O[b, h, n:] == 3.5).all() and (LSE[b, h, n:] == -2.5).all()
+    assert np.sqrt(num / den) <= TOL_O["rel_fro"]
+
+
+SHAPES = [
+    # B, Hq, Hkv, d, L, P
+    (1, 1, 1, 64, 1, 1), (2, 4, 1, 128, 1, 300), (3, 4, 2, 64, 5, 129), (1, 8, 2, 128, 16, 700), (2, 4, 1, 128, 32, 256),
+    (3, 6, 2, 80, 43, 200), (2, 3, 1, 96, 50, 333), (2, 5, 5, 64, 130, 128), (1, 8, 2, 128, 257, 1000),
+    (2, 4, 4, 112, 129, 64), (9, 8, 1, 64, 3, 500), (5, 8, 2, 128, 100, 640), (1, 2, 1, 64, 700, 2000),
+    (40, 4, 4, 128, 140, 260),
+]
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("B,Hq,Hkv,d,L,P", SHAPES)
+def test_forward(B, Hq, Hkv, d, L, P, ragged):
+    g = torch.Generator(device="cuda").manual_seed(B * L + P)
+    rng = np.random.default_rng(L)
+    ids, n = inputs.token_ids(P, B, L, 0.15), max(1, L // 6)
+    seq_len = [int(x) for x in rng.integers(0, L + 1, B)] if ragged else [L] * B
+    if ragged and seq_len[0] == 0:
+        seq_len[0] = L
+    plen = [int(x) for x in rng.integers(0, P + 1, B)] if ragged else [P] * B
+    idesc, index = _index(ids, n, 0, seq_len if ragged else None)
+    Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hkv, L, d), _normal(g, B, Hkv, L, d)
+    Q = (Q.float() * 2).to(BF)
+    Kp, Vp = _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
+    far = max(plen)
+    Kp[:, far:], Vp[:, far:] = float("nan"), float("inf")      # behind the longest prefix: anything
+    pl = torch.tensor(plen, dtype=torch.int32, device="cuda") if ragged else None
+    O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, pl)
+    f = np.isin(ids, inputs.SEP_IDS)
+    masks = [orc.mask_matrix(f[b], 0, n) for b in range(B)]
+    heads = None if B * Hq * L < 4000 else [0, Hq - 1]
+    if B == 40:    # the many-sequence form: a few sequences are enough
+        sel = slice(0, 40, 13)
+        Q, K, V, O, LSE, masks, plen, seq_len = (x[sel] for x in (Q, K, V, O, LSE, masks, plen, seq_len))
+    _check(Q, K, V, Kp, Vp, masks, plen, seq_len, O, LSE, heads=heads)
+
+
+def test_initial_tokens_of_their_own_and_a_scale():
+    g = torch.Generator(device="cuda").manual_seed(1)
+    ids = inputs.token_ids(3, 2, 150, 0.1)
+    idesc, index = _index(ids, 10, a=4)
+    Q, K, V = _normal(g, 2, 4, 150, 64), _normal(g, 2, 2, 150, 64), _normal(g, 2, 2, 150, 64)
+    Kp, Vp = _normal(g, 2, 77, 64), _normal(g, 2, 77, 64)
+    O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, None, 0.2)
+    f = np.isin(ids, inputs.SEP_IDS)
+    _check(Q, K, V, Kp, Vp, [orc.mask_matrix(f[b], 4, 10) for b in range(2)], [77, 77], [150, 150], O, LSE,
+           scale=float(np.float32(0.2)))
+
+
+def test_rows_that_pack_documents_all_continue_the_prefix():
+    g = torch.Generator(device="cuda").manual_seed(2)
+    B, L, n, a = 2, 300, 16, 2
+    ids, df = inputs.token_ids(4, B, L, 0.1), inputs.doc_first(4, B, L, 70.0)
+    idesc, index = _index(ids, n, a, doc_first=df)
+    Q, K, V = _normal(g, B, 4, L, 128), _normal(g, B, 1, L, 128), _normal(g, B, 1, L, 128)
+    Kp, Vp = _normal(g, 1, 200, 128), _normal(g, 1, 200, 128)
+    O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, torch.tensor([200, 50], dtype=torch.int32, device="cuda"))
+    f = np.isin(ids, inputs.SEP_IDS)
+    _check(Q, K, V, Kp, Vp, [orc.packed_mask_matrix(f[b], df[b], a, n) for b in range(B)], [200, 50], [L, L], O, LSE)
+
+
+def test_no_prefix_in_sight_is_the_plain_forward():
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for B, Hq, Hkv, d, L in ((2, 4, 2, 64, 200), (1, 8, 2, 128, 300)):
+        ids = inputs.token_ids(5, B, L, 0.1)
+        idesc, index = _index(ids, 20, 3)
+        Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hkv, L, d), _normal(g, B, Hkv, L, d)
+        Kp = torch.full((Hkv, 90, d), float("nan"), dtype=BF, device="cuda")
+        O, LSE = _run(Q, K, V, idesc, index, Kp, Kp, torch.zeros(B, dtype=torch.int32, device="cuda"))
+        desc = api.AttnDesc(B, Hq, Hkv, d, L, 0.0, 0)
+        ws = api.alloc_bytes(api.sepllm_attn_workspace_bytes(desc, idesc)[0])
+        O2, LSE2 = torch.empty_like(O), torch.empty_like(LSE)
+        api.sepllm_attn_fwd(desc, idesc, Q, K, V, index, O2, LSE2, ws)
+        torch.cuda.synchronize()
+        # the same 32-bit result; the join scales it by a quotient of two equal numbers
+        assert (O.float() - O2.float()).abs().max() <= 2.0 ** -7 * O2.float().abs().max()
+        assert (LSE - LSE2).abs().max() <= 1e-5
+
+
+def test_graph_and_other_stream_and_kept_side_rows():
+    g = torch.Generator(device="cuda").manual_seed(4)
+    B, Hq, Hkv, d, L, P = 2, 8, 2, 128, 150, 400
+    ids = inputs.token_ids(6, B, L, 0.1)
+    idesc, index = _index(ids, 20, 0)
+    Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hkv, L, d), _normal(g, B, Hkv, L, d)
+    Kp, Vp = _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
+    want = _run(Q, K, V, idesc, index, Kp, Vp, None)
+    desc = api.AttnDesc(B, Hq, Hkv, d, L, 0.0, 0)
+    ws = api.alloc_bytes(api.sepllm_attn_prefix_workspace_bytes(desc, idesc, P))
+    outs = [(torch.zeros_like(want[0]), torch.zeros_like(want[1])) for _ in range(3)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        api.sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, None, *outs[0], ws)
+    torch.cuda.current_stream().wait_stream(s)
+    desc.flags = api.SIDE_READY      # the workspace holds the side rows of these K and V
+    api.sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, None, *outs[1], ws)
+    desc.flags = 0
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        api.sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, None, *outs[2], ws)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[0]) and torch.equal(l, want[1]) for o, l in outs)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,rot,layout", [(4, 2, 64, 32, "interleaved"), (8, 2, 128, 128, "half")])
+def test_a_serving_run_through_a_shared_prefix(Hq, Hkv, d, rot, layout):
+    """Prompt -> rotation -> forward -> its retained entries become the shared prefix; every sequence's own
+    turn is rotated to the positions behind the prompt, pre-filled behind the prefix and handed to its
+    cache; then tokens are generated over prefix and cache.  Every step against the oracle, from the
+    keys and values as the rotation left them."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    Lp, B, L, steps, a, s, w, c, n = 700, 3, 90, 12, 4, 200, 24, 260, 24
+    sep = inputs.SEP_IDS
+
+    def rotate(qkv, pos, first=0):
+        b, l = qkv.shape[:2]
+        desc = api.RopeDesc(b, l, Hq, Hkv, d, rot_dim=rot, layout=layout, scaling="llama3", base=500000.0,
+                            factor=8.0, pos_first=first)
+        out = [torch.empty((b, h, l, d), dtype=BF, device="cuda") for h in (Hq, Hkv, Hkv)]
+        api.sepllm_rope_fwd(desc, pos, *qkv.transpose(1, 2).split((Hq, Hkv, Hkv), 1), *out)
+        return out
+    # the shared prompt
+    pids = inputs.token_ids(40, 1, Lp, 0.12)
+    Qs, Ks, Vs = rotate(_normal(g, 1, Lp, Hq + 2 * Hkv, d), None)
+    idesc1, index1 = _index(pids, n, a)
+    one = GpuCache(1, Hkv, Hq, d, a, s, w, c)
+    api.sepllm_cache_from_prompt(one.desc, idesc1, index1, None, Ks, Vs, one.state, one.Kc, one.Vc)
+    Kp, Vp = (torch.full((Hkv, c, d), float("nan"), dtype=BF, device="cuda") for _ in range(2))
+    plen = torch.zeros(B, dtype=torch.int32, device="cuda")
+    api.sepllm_prefix_from_cache(one.desc, one.state, one.Kc, one.Vc, c, Kp, Vp, plen)
+    kept = orc.cache_after_prompt(np.isin(pids[0], sep).tolist(), a, s, w, c).retained()
+    R = len(kept)
+    torch.cuda.synchronize()
+    assert plen.tolist() == [R] * B
+    for x, y in ((Kp, Ks), (Vp, Vs)):
+        assert torch.equal(x[:, :R], y[0][:, kept])
+    # the sequences' own turns, of unequal lengths
+    ids = inputs.token_ids(41, B, L + steps, 0.12)
+    f = np.isin(ids, sep)
+    lens = [L, 37, 1]
+    qkv = _normal(g, B, L + steps, Hq + 2 * Hkv, d)
+    Q, K, V = rotate(qkv[:, :L].contiguous(), None, first=Lp)
+    idesc, index = _index(ids[:, :L], n, 0, lens)
+    O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, plen)
+    _check(Q, K, V, Kp, Vp, [orc.mask_matrix(f[b, :L], 0, n) for b in range(B)], [R] * B, lens, O, LSE)
+    own = GpuCache(B, Hkv, Hq, d, 0, s, w, c)
+    lens_d = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    api.sepllm_cache_from_prompt(own.desc, idesc, index, lens_d, K, V, own.state, own.Kc, own.Vc)
+    # generation: sequence b's t-th token has position Lp + lens[b] + t
+    ws = api.alloc_bytes(api.sepllm_decode_prefix_workspace_bytes(own.desc, c))
+    hist = [([K[b, :, j] for j in range(lens[b])], [V[b, :, j] for j in range(lens[b])]) for b in range(B)]
+    oc = [orc.cache_after_prompt(f[b, :lens[b]].tolist(), 0, s, w, c) for b in range(B)]
+    o = torch.empty((B, Hq, d), dtype=BF, device="cuda")
+    lse = torch.empty((B, Hq), dtype=torch.float32, device="cuda")
+    rows = torch.arange(B, device="cuda")
+    for t in range(steps):
+        pos = (lens_d.long() + Lp + t)[:, None].contiguous()
+        q, k, v = rotate(qkv[rows, lens_d.long() + t][:, None].contiguous(), pos)
+        tok = torch.from_numpy(ids)[np.arange(B), np.array(lens) + t].to(torch.int32).cuda()
+        api.sepllm_cache_update(own.desc, own.state, own.Kc, own.Vc, tok, sep, k[:, :, 0].contiguous(),
+                                v[:, :, 0].contiguous())
+        q0 = q[:, :, 0].contiguous()
+        api.sepllm_decode_prefix(own.desc, c, 0.0, q0, own.state, own.Kc, own.Vc, Kp, Vp, plen, o, lse, ws)
+        torch.cuda.synchronize()
+        assert api.sepllm_last_device_status(ws) == 0
+        for b in range(B):
+            hist[b][0].append(k[b, :, 0])
+            hist[b][1].append(v[b, :, 0])
+            oc[b].update(bool(f[b, lens[b] + t]))
+            kk, vv = (torch.cat((x[:, :R], torch.stack([hist[b][i][j] for j in oc[b].retained()], 1)), 1)
+                      .double().cpu().numpy() for i, x in ((0, Kp), (1, Vp)))
+            for h in range(Hq):
+                ref, lref = orc.decode_attention(q0[b, h].double().cpu().numpy(), kk[h // (Hq // Hkv)],
+                                                 vv[h // (Hq // Hkv)])
+                assert np.abs(o[b, h].double().cpu().numpy() - ref).max() <= TOL_O["max_abs"], (t, b, h)
+                assert abs(float(lse[b, h]) - lref) <= TOL_LSE

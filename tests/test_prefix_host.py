@@ -72,6 +72,32 @@ def test_prefix_from_cache_refusals():
     assert _copy(P=31) == api.BUFFER_TOO_SMALL
 
 
+def _attn(P=100, L=50, Hq=4, d=64, idesc=None, **over):
+    names = ("Q", "K", "V", "index", "Kp", "Vp", "prefix_len", "O", "LSE", "workspace")
+    v = dict({n: A for n in names}, **over)
+    desc = api.AttnDesc(2, Hq, 2, d, L, 0.0, 0)
+    idesc = idesc or api.IndexDesc(2, L, 0, 8, 1, 128, 128, L)
+    return api.lib().sepllm_attn_prefix_fwd(C.byref(desc), C.byref(idesc), C.c_int32(P), v["Q"], v["K"], v["V"],
+                                            v["index"], v["Kp"], v["Vp"], v["prefix_len"], v["O"], v["LSE"],
+                                            v["workspace"], None)
+
+
+def test_attention_refusals_and_workspace():
+    for name in ("Q", "K", "V", "index", "Kp", "Vp", "O", "LSE", "workspace"):
+        assert _attn(**{name: None}) == api.INVALID_ARG
+        assert _attn(**{name: C.c_void_p((1 << 20) + 2)}) == api.INVALID_ARG
+    assert _attn(prefix_len=C.c_void_p((1 << 20) + 2)) == api.INVALID_ARG
+    assert _attn(P=0) == api.INVALID_ARG and _attn(Hq=3) == api.INVALID_ARG and _attn(L=0) == api.INVALID_ARG
+    assert _attn(d=72) == api.UNSUPPORTED
+    assert _attn(idesc=api.IndexDesc(2, 51, 0, 8, 1, 128, 128, 51)) == api.INVALID_ARG
+    assert _attn(idesc=api.IndexDesc(2, 50, 0, 8, 1, 64, 128, 50)) == api.UNSUPPORTED
+    desc, idesc = api.AttnDesc(2, 4, 2, 80, 50, 0.0, 0), api.IndexDesc(2, 50, 0, 8, 1, 128, 128, 50)
+    fwd, _ = api.sepllm_attn_workspace_bytes(desc, idesc)
+    assert api.sepllm_attn_prefix_workspace_bytes(desc, idesc, 300) >= fwd + 2 * 4 * 50 * (128 + 1) * 4
+    with pytest.raises(api.SepllmError):
+        api.sepllm_attn_prefix_workspace_bytes(desc, idesc, 0)
+
+
 def test_binding_refuses_other_shapes_and_types():
     with pytest.raises(ValueError):
         api._expect("x", q=(torch.zeros(2, 3), (2, 4), torch.float32))
