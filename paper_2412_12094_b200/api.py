@@ -107,6 +107,16 @@ EXPORTS = [
     "sepllm_status_string",
 ]
 
+# Calls of the per-token and per-layer kind take plain integers as addresses (ctypes converts them
+# faster than it builds an object for each).
+_P, _I = C.c_void_p, C.c_int32
+_ARGTYPES = {
+    "sepllm_rope_fwd": [_P] * 5, "sepllm_rope_bwd": [_P] * 5,
+    "sepllm_prefix_from_cache": [_P] * 4 + [_I] + [_P] * 3 + [_I, _P],
+    "sepllm_decode_prefix": [_P, _I, C.c_float] + [_P] * 11,
+    "sepllm_attn_prefix_fwd": [_P, _P, _I] + [_P] * 10,
+}
+
 _lib = None
 
 
@@ -123,6 +133,8 @@ def lib() -> C.CDLL:
         for name in EXPORTS:
             if name != "sepllm_status_string":
                 getattr(_lib, name).restype = C.c_int
+        for name, types in _ARGTYPES.items():
+            getattr(_lib, name).argtypes = types
     return _lib
 
 
@@ -147,17 +159,31 @@ def _ptr(t):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return C.c_void_p(_raw_stream())
 
 
-def _same_device(*tensors):
-    """The calls launch on the current device and its current stream: memory of another device is
-    refused here rather than read from there."""
+def _raw_stream() -> int:
+    # the handle of torch.cuda.current_stream() without the Python object around it (3 us a call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _addresses(where, tensors):
+    """Device addresses (0 for None) of contiguous tensors of the current device: the calls launch on
+    it and on its current stream, so memory of another device is refused here rather than read from
+    there."""
     cur = torch.cuda.current_device()
+    out = []
     for t in tensors:
-        if t is not None and t.get_device() != cur:
-            raise ValueError(f"tensor on {t.device}, current device is cuda:{cur}: "
-                             "make the tensors' device current for the call")
+        if t is None:
+            out.append(0)
+        elif t.get_device() != cur:
+            raise ValueError(f"{where}: tensor on {t.device}, current device is cuda:{cur}: make the tensors' "
+                             "device current for the call")
+        elif not t.is_contiguous():
+            raise ValueError(f"{where}: contiguous tensors only, not strides {t.stride()}")
+        else:
+            out.append(t.data_ptr())
+    return out
 
 
 def _sep_array(sep_ids):
@@ -274,7 +300,7 @@ _ROPE_DTYPES = {torch.bfloat16: 0, torch.float32: 1}
 _ROPE_VIEWS = struct.Struct("=" + "Qqqqii" * 3)   # three sepllm_rope_view
 
 
-def _rope_views(desc, tensors, what):
+def _rope_views(desc, tensors, what, device=None):
     vals = []
     for t, h in zip(tensors, (desc.Hq, desc.Hkv, desc.Hkv)):
         if t is None:
@@ -283,20 +309,25 @@ def _rope_views(desc, tensors, what):
         if t.shape != (desc.B, h, desc.L, desc.d):
             raise ValueError(f"{what}: shape {tuple(t.shape)}, the descriptor says {(desc.B, h, desc.L, desc.d)}")
         sb, sh, sl, se = t.stride()
-        if t.dtype not in _ROPE_DTYPES or se != 1:
+        dtype = _ROPE_DTYPES.get(t.dtype)
+        if dtype is None or se != 1:
             raise ValueError(f"{what}: bf16 or fp32 with contiguous head vectors, not {t.dtype} with strides "
                              f"{t.stride()}")
-        vals += (t.data_ptr(), sb, sh, sl, _ROPE_DTYPES[t.dtype], 0)
+        if device is not None and t.get_device() != device:
+            raise ValueError(f"{what}: tensor on {t.device}, current device is cuda:{device}: make the tensors' "
+                             "device current for the call")
+        vals += (t.data_ptr(), sb, sh, sl, dtype, 0)
     return _ROPE_VIEWS.pack(*vals)
 
 
 def _rope(fn, where, desc, positions, ins, outs):
-    _same_device(positions, *ins, *outs)
-    if positions is not None and (positions.dtype != torch.int64 or not positions.is_contiguous()
+    device = torch.cuda.current_device()
+    pos, = _addresses(where, (positions,))
+    if positions is not None and (positions.dtype != torch.int64
                                   or positions.numel() < (desc.B - 1) * desc.pos_stride + desc.L):
         raise ValueError(f"{where}: positions are contiguous int64, pos_stride elements from row to row")
-    _check(fn(C.byref(desc), _ptr(positions), _rope_views(desc, ins, where), _rope_views(desc, outs, where),
-              _stream()), where)
+    _check(fn(C.byref(desc), pos, _rope_views(desc, ins, where, device), _rope_views(desc, outs, where, device),
+              torch._C._cuda_getCurrentRawStream(device)), where)
 
 
 def sepllm_rope_fwd(desc: RopeDesc, positions, q, k, v, q_out, k_out, v_out):
@@ -372,27 +403,22 @@ def sepllm_decode_rope(desc, scale, q, state, Kr, Vc, rope_table, o, lse, worksp
 
 
 # ---------------------------------------------------------------- shared prefix
-def _expect(where, **tensors):
-    """name = (tensor, shape, dtype): contiguous tensors of the current device."""
-    for name, (t, shape, dtype) in tensors.items():
-        if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous()):
-            raise ValueError(f"{where}: {name} is contiguous {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)} "
-                             f"with strides {t.stride()}")
+def _expect(where, *tensors):
+    """(name, tensor or None, shape, dtype) each."""
+    for name, t, shape, dtype in tensors:
+        if t is not None and (t.shape != shape or t.dtype != dtype):
+            raise ValueError(f"{where}: {name} is {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
 
 
 def sepllm_prefix_from_cache(desc, state, Kc, Vc, P, Kp, Vp, prefix_len=None):
     """The retained entries of a cache of one sequence become rows 0 .. Size_run-1 of Kp, Vp [Hkv][P][d];
     prefix_len: int32 of any length, every word is set to Size_run, or None."""
-    _same_device(state, Kc, Vc, Kp, Vp, prefix_len)
-    _expect("sepllm_prefix_from_cache", Kp=(Kp, (desc.Hkv, P, desc.d), torch.bfloat16),
-            Vp=(Vp, (desc.Hkv, P, desc.d), torch.bfloat16))
-    n = 0
-    if prefix_len is not None:
-        n = prefix_len.numel()
-        _expect("sepllm_prefix_from_cache", prefix_len=(prefix_len, (n,), torch.int32))
-    _check(lib().sepllm_prefix_from_cache(C.byref(desc), _ptr(state), _ptr(Kc), _ptr(Vc), C.c_int32(P), _ptr(Kp),
-                                          _ptr(Vp), _ptr(prefix_len), C.c_int32(n), _stream()),
-           "sepllm_prefix_from_cache")
+    where = "sepllm_prefix_from_cache"
+    shape, n = (desc.Hkv, P, desc.d), 0 if prefix_len is None else prefix_len.numel()
+    _expect(where, ("Kp", Kp, shape, torch.bfloat16), ("Vp", Vp, shape, torch.bfloat16),
+            ("prefix_len", prefix_len, (n,), torch.int32))
+    st, kc, vc, kp, vp, pl = _addresses(where, (state, Kc, Vc, Kp, Vp, prefix_len))
+    _check(lib().sepllm_prefix_from_cache(C.byref(desc), st, kc, vc, P, kp, vp, pl, n, _raw_stream()), where)
 
 
 def sepllm_decode_prefix_workspace_bytes(desc, P):
@@ -404,15 +430,14 @@ def sepllm_decode_prefix_workspace_bytes(desc, P):
 
 def sepllm_decode_prefix(desc, P, scale, q, state, Kc, Vc, Kp, Vp, prefix_len, o, lse, workspace):
     """sepllm_decode with the shared prefix Kp, Vp [Hkv][P][d] in front of every cache; prefix_len: int32 [B]
-    or None (all P rows)."""
-    _same_device(q, state, Kc, Vc, Kp, Vp, prefix_len, o, lse, workspace)
-    bf, B, Hq, d = torch.bfloat16, desc.B, desc.Hq, desc.d
-    _expect("sepllm_decode_prefix", q=(q, (B, Hq, d), bf), o=(o, (B, Hq, d), bf), Kp=(Kp, (desc.Hkv, P, d), bf),
-            Vp=(Vp, (desc.Hkv, P, d), bf), prefix_len=(prefix_len, (B,), torch.int32),
-            lse=(lse, (B, Hq), torch.float32))
-    _check(lib().sepllm_decode_prefix(C.byref(desc), C.c_int32(P), C.c_float(scale), _ptr(q), _ptr(state), _ptr(Kc),
-                                      _ptr(Vc), _ptr(Kp), _ptr(Vp), _ptr(prefix_len), _ptr(o), _ptr(lse),
-                                      _ptr(workspace), _stream()), "sepllm_decode_prefix")
+    or None (all P rows); lse may be None."""
+    where, bf, B, row = "sepllm_decode_prefix", torch.bfloat16, desc.B, (desc.B, desc.Hq, desc.d)
+    shape = (desc.Hkv, P, desc.d)
+    _expect(where, ("q", q, row, bf), ("Kp", Kp, shape, bf), ("Vp", Vp, shape, bf),
+            ("prefix_len", prefix_len, (B,), torch.int32), ("o", o, row, bf),
+            ("lse", lse, row[:2], torch.float32))
+    _check(lib().sepllm_decode_prefix(C.byref(desc), P, scale, *_addresses(
+        where, (q, state, Kc, Vc, Kp, Vp, prefix_len, o, lse, workspace)), _raw_stream()), where)
 
 
 def sepllm_attn_prefix_workspace_bytes(desc: AttnDesc, idesc: IndexDesc, P):
@@ -425,14 +450,13 @@ def sepllm_attn_prefix_workspace_bytes(desc: AttnDesc, idesc: IndexDesc, P):
 def sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, prefix_len, O, LSE, workspace):
     """sepllm_attn_fwd with the shared prefix Kp, Vp [Hkv][P][d] in front of every sequence; prefix_len:
     int32 [B] or None (all P rows)."""
-    _same_device(Q, K, V, index, Kp, Vp, prefix_len, O, LSE, workspace)
-    bf, B, Hq, Hkv, L, d = torch.bfloat16, desc.B, desc.Hq, desc.Hkv, desc.L, desc.d
-    _expect("sepllm_attn_prefix_fwd", Q=(Q, (B, Hq, L, d), bf), K=(K, (B, Hkv, L, d), bf), V=(V, (B, Hkv, L, d), bf),
-            O=(O, (B, Hq, L, d), bf), Kp=(Kp, (Hkv, P, d), bf), Vp=(Vp, (Hkv, P, d), bf),
-            prefix_len=(prefix_len, (B,), torch.int32), LSE=(LSE, (B, Hq, L), torch.float32))
-    _check(lib().sepllm_attn_prefix_fwd(C.byref(desc), C.byref(idesc), C.c_int32(P), _ptr(Q), _ptr(K), _ptr(V),
-                                        _ptr(index), _ptr(Kp), _ptr(Vp), _ptr(prefix_len), _ptr(O), _ptr(LSE),
-                                        _ptr(workspace), _stream()), "sepllm_attn_prefix_fwd")
+    where, bf, B, L = "sepllm_attn_prefix_fwd", torch.bfloat16, desc.B, desc.L
+    row, key, shape = (B, desc.Hq, L, desc.d), (B, desc.Hkv, L, desc.d), (desc.Hkv, P, desc.d)
+    _expect(where, ("Q", Q, row, bf), ("K", K, key, bf), ("V", V, key, bf), ("Kp", Kp, shape, bf),
+            ("Vp", Vp, shape, bf), ("prefix_len", prefix_len, (B,), torch.int32), ("O", O, row, bf),
+            ("LSE", LSE, row[:3], torch.float32))
+    _check(lib().sepllm_attn_prefix_fwd(C.byref(desc), C.byref(idesc), P, *_addresses(
+        where, (Q, K, V, index, Kp, Vp, prefix_len, O, LSE, workspace)), _raw_stream()), where)
 
 
 def read_cache_state(state: torch.Tensor) -> dict:

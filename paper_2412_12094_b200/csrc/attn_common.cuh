@@ -187,30 +187,36 @@ void launch_gather(const sepllm_attn_desc* d, const sepllm_index_desc* id, int c
                    void* Ks, void* Vs, int32_t* status, cudaStream_t stream);
 
 // Attention over a prefix shared by the batch (prefix.cu).
+constexpr int kSmCount = 148;
 struct PrefixParams {
-  int B, Hkv, G, T, d, P;     // G query heads per kv head, T query tokens per sequence
-  int key_tiles, splits;      // 128-row tiles of the prefix, and how many CTAs share them
-  int rt, bt, row_tiles;      // row tile: rt rows of each of bt sequences; tiles per sequence
-  int m_tiles, alternate;     // row tiles per kv head; 1: one tile whose key tiles the slots take in turn
+  int B, Hkv, G, T, d, P;       // G query heads per kv head, T query tokens per sequence
+  int key_tiles;                // 128-row tiles of the prefix
+  int gt, tt, bt;               // row tile: gt heads of the group x tt tokens x bt sequences
+  int g_tiles, t_tiles, m_tiles;  // row tiles along heads and tokens, and in all, per kv head
+  int alternate;                // 1: one row tile, whose key tiles the slots take in turn
+  int whole_parts;              // 1: units that one CTA walks in full leave a part too
+  int pair_base, pairs;         // pairs of row tiles of this launch
+  int max_ctas;
   float scale_log2;
-  const int32_t* prefix_len;  // [B] or null (P for all)
-  const int32_t* seq_len;     // [B] or null: rows of tokens behind it are not written
-  float* part_ml;             // [row][splits << alternate] (reference exponent, sum)
-  float* part_acc;            // [row][splits << alternate][D]
-  const float* own_O;         // [row][D] the row's own part, normalised, and its log-sum-exp [row]
+  const int32_t* prefix_len;    // [B] or null (P for all)
+  const int32_t* seq_len;       // [B] or null: rows of tokens behind it are not written
+  float* part_ml;               // [part][slot][128] (reference exponent, sum)
+  float* part_acc;              // [part][slot][128][D]
+  int4* unit_parts;             // [Hkv][pairs] (parts, first part, CTA of the first part)
+  int32_t* cut_units;           // [CTA] the unit whose first key tiles, not all, were the CTA's; -1: none
+  const float* own_O;           // [row][D] the row's own part, normalised, and its log-sum-exp [row]
   const float* own_lse;
-  int merge_O;                // 1: the kernel joins both parts itself (one split)
-  __nv_bfloat16* O;           // [row][d]
+  __nv_bfloat16* O;             // [row][d], rows [B][Hkv][G][T]
   float* LSE;
   int32_t* status;
 };
-// Sizes, tiles and splits (false: too large).  Rows are [B][Hkv][G * T].
-bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P);
+// Sizes and tiles (false: too large).
+bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, bool whole_parts);
 size_t prefix_part_bytes(const PrefixParams& p);
 void place_prefix_parts(PrefixParams* p, uint8_t* ws);
-sepllm_status launch_prefix(const PrefixParams& p, const void* Q, const void* Kp, const void* Vp,
-                            cudaStream_t stream);
-sepllm_status launch_prefix_join(const PrefixParams& p, const float* own_ml, const float* own_acc,
-                                 int own_parts, cudaStream_t stream);
+// The prefix part and the join with the rows' own parts: own_parts of the decode kernel, or
+// (own_parts = 0) p.own_O and p.own_lse.
+sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const void* Vp, const float* own_ml,
+                            const float* own_acc, int own_parts, cudaStream_t stream);
 
 }  // namespace sepllm

@@ -1058,7 +1058,7 @@ extern "C" sepllm_status sepllm_decode_prefix_workspace_bytes(const sepllm_cache
   if (st != SEPLLM_OK) return st;
   if (P < 1) return SEPLLM_INVALID_ARG;
   PrefixParams p{};
-  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P)) return SEPLLM_UNSUPPORTED;
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P, true)) return SEPLLM_UNSUPPORTED;
   if (bytes) *bytes = kAlign + own_part_bytes(desc, decode_splits(desc)) + prefix_part_bytes(p);
   return SEPLLM_OK;
 }
@@ -1077,7 +1077,7 @@ extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int
     return SEPLLM_INVALID_ARG;
   if (desc->B > 65535 || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
   PrefixParams p{};
-  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P)) return SEPLLM_UNSUPPORTED;
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P, true)) return SEPLLM_UNSUPPORTED;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const int own_parts = decode_splits(desc);
@@ -1093,8 +1093,7 @@ extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int
   // (the own part goes first: it writes the status word that the prefix kernel may set)
   st = launch_own_parts(h, scale, q, state, Kc, Vc, nullptr, own_parts, ml, acc, p.status, stream);
   if (st != SEPLLM_OK) return st;
-  if ((st = launch_prefix(p, q, Kp, Vp, stream)) != SEPLLM_OK) return st;
-  return launch_prefix_join(p, ml, acc, own_parts, stream);
+  return launch_prefix(p, q, Kp, Vp, ml, acc, own_parts, stream);
 }
 
 // grid (row blocks, Hkv).  Row v of the prefix is retained entry v of the (only) sequence.

@@ -2,12 +2,12 @@
 //
 // Every query row (sequence b, head h, token t) attends to the first prefix_len[b] rows of one
 // K/V block Kp, Vp [Hkv][P][d] and to keys of its own (the sequence's cache, or the kept tokens of
-// its own row).  The two sets are disjoint, so the softmax over both is joined from two partial
-// results: with reference exponents m1, m2, sums l1, l2 and unnormalised values a1, a2,
-//   O = (a1 2^(m1-M) + a2 2^(m2-M)) / (l1 2^(m1-M) + l2 2^(m2-M)),  M = max(m1, m2).
-// This file has the prefix half: all B * G * T rows that read one kv head (G query heads per kv head,
-// T tokens) are the rows of one matrix product, 128 to a tile, so the prefix is read once per
-// 256 rows instead of once per sequence.
+// its own row).  The two sets are disjoint, so the softmax over both is joined from partial
+// results: with reference exponents m_i, sums l_i and unnormalised values a_i,
+//   O = sum a_i 2^(m_i-M) / sum l_i 2^(m_i-M),  M = max m_i.
+// This file has the prefix part: the rows of all sequences, tokens and heads that read one kv head
+// are the rows of one matrix product, 128 to a tile, so the prefix is read once per 256 rows instead
+// of once per sequence.
 #include <algorithm>
 
 #include "attn_common.cuh"
@@ -17,6 +17,7 @@ namespace sepllm {
 namespace {
 
 constexpr int kPfxThreads = 384;
+constexpr int kMaxPairs = 2048;   // pairs of row tiles per launch (their lengths sit in shared memory)
 
 template <int D>
 struct PfxCfg {
@@ -26,16 +27,88 @@ struct PfxCfg {
   static constexpr uint32_t kQ = 0;
   static constexpr uint32_t kK = kQ + 2 * kTile;
   static constexpr uint32_t kV = kK + NST * kTile;
-  static constexpr uint32_t kBar = kV + NST * kTile;
-  static constexpr uint32_t kTotal = kBar + 512;
+  static constexpr uint32_t kTab = kV + NST * kTile;
+  static constexpr uint32_t kBar = kTab + kMaxPairs * 8;
+  static constexpr uint32_t kTotal = kBar + 1024;
   static constexpr uint32_t kRequest = kTotal + 1024;
   static constexpr uint32_t kS0 = 0, kS1 = 128, kO0 = 256, kO1 = 256 + D;  // tensor-memory columns
 };
 static_assert(PfxCfg<128>::kRequest <= 227 * 1024 && PfxCfg<64>::kRequest > 114 * 1024,
               "one CTA per SM owns all 512 tensor-memory columns");
 
-// One CTA: one kv head, one split of the key tiles, two slots of 128 query rows.
-//   pair mode        slot x holds row tile 2 * blockIdx.x + x; both slots walk the same key tiles
+// Row tile i holds rows (b, t, g) of one kv head: bt sequences x tt tokens x gt heads of the group,
+// heads fastest.
+struct RowTile {
+  int b0, t0, g0;
+};
+__device__ __forceinline__ RowTile row_tile(const PrefixParams& p, int i) {
+  RowTile r;
+  r.g0 = (i % p.g_tiles) * p.gt;
+  i /= p.g_tiles;
+  r.t0 = (i % p.t_tiles) * p.tt;
+  r.b0 = (i / p.t_tiles) * p.bt;
+  return r;
+}
+// Longest prefix that sequence b's rows of a tile see; -1: the tile holds none of its tokens.
+__device__ __forceinline__ int seen_length(const PrefixParams& p, int b, int t0) {
+  if (b >= p.B || (p.seq_len && t0 >= p.seq_len[b])) return -1;
+  return p.prefix_len ? max(0, min(p.P, p.prefix_len[b])) : p.P;
+}
+// Key tiles of a pair of row tiles with these longest prefixes.  A pair that sees nothing of the
+// prefix still takes one (wholly masked) tile: its rows have to be finished by someone.
+__device__ __forceinline__ int pair_tiles(int2 len) {
+  const int m = max(len.x, len.y);
+  return m < 0 ? 0 : max(1, (m + kBN - 1) / kBN);
+}
+
+// The work is the key tiles of every (kv head, pair) in that order, cut into equal runs, one per
+// CTA: a CTA's run is a sequence of segments, each a range of key tiles of one (kv head, pair).
+// Every warp walks the run by itself; its place sits in shared memory (a warp's copy each), so that
+// nothing of it takes registers in the softmax loop.
+struct Segment {
+  int64_t left;     // key tiles of the run behind this segment
+  int hk, pair;
+  int j0, j1, nt;   // key tiles [j0, j1) of nt
+  int len[2];       // longest prefix of the row tile in slot x (-1: no rows)
+};
+// Advances to the next segment (false: none left).  WARP: called by all lanes of a warp, else by one
+// thread.
+template <bool WARP>
+__device__ __forceinline__ bool next_segment(Segment* sg, const int2* tab, int pairs) {
+  const int64_t left = sg->left;
+  int hk = sg->hk, pair = sg->pair, off = sg->j1, nt;
+  if (WARP) __syncwarp();
+  if (left <= 0) return false;
+  while ((nt = pair_tiles(tab[pair])) <= off) {   // finished, or without rows
+    off = 0;
+    if (++pair == pairs) { pair = 0; ++hk; }
+  }
+  if (!WARP || (threadIdx.x & 31) == 0) {
+    sg->hk = hk; sg->pair = pair; sg->j0 = off; sg->nt = nt;
+    sg->j1 = int(min(int64_t(nt), off + left));
+    sg->left = left - (sg->j1 - off);
+    sg->len[0] = tab[pair].x;
+    sg->len[1] = tab[pair].y;
+  }
+  if (WARP) __syncwarp();
+  return true;
+}
+// Key tiles of the segment that slot x works on: in pair mode the first ones (as far as its longest
+// prefix goes), in alternate mode those with j % 2 = x.
+__device__ __forceinline__ int slot_tiles(const Segment* sg, bool alt, int x) {
+  const int n = sg->j1 - sg->j0, len = sg->len[x];
+  if (alt) return (n - x + 1) / 2;
+  return len < 0 ? 0 : max(0, min(n, max(1, (len + kBN - 1) / kBN) - sg->j0));
+}
+// The segment's last tile holds the end of the longest prefix: V rows behind it may hold anything
+// (rows behind P are zero already).
+__device__ __forceinline__ bool ends_inside(const Segment* sg, int P) {
+  const int m = max(sg->len[0], sg->len[1]);
+  return m < P && sg->j1 * kBN > m;
+}
+
+// One CTA: two slots of 128 query rows, walked over the segments of its run.
+//   pair mode        slot x holds row tile 2 * pair + x; both slots walk the same key tiles
 //   alternate mode   (one row tile in all) both slots hold that tile and take the key tiles in turn,
 //                    so that one slot's softmax runs under the other's loads and products; each
 //                    slot leaves a partial result of its own
@@ -53,41 +126,42 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   uint8_t* sQ = smem + C::kQ;
   uint8_t* sK = smem + C::kK;
   uint8_t* sV = smem + C::kV;
+  int2* tab = reinterpret_cast<int2*>(smem + C::kTab);   // [pairs] longest prefix of each row tile
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBar);
   uint64_t* bar_q = bars;          // [2]   Q of slot x landed
   uint64_t* bar_s = bars + 2;      // [2]   S_x complete (and every earlier MMA)
   uint64_t* bar_p = bars + 4;      // [2]   P_x written by the 4 softmax warps of slot x
-  uint64_t* bar_o = bars + 6;      //       every MMA of the CTA complete
+  uint64_t* bar_o = bars + 6;      //       every MMA of the segment complete
   uint64_t* bar_z = bars + 7;      //       V rows behind the prefix cleared
   uint64_t* bar_g = bars + 8;      //       V of the last tile landed: clear the rows behind the prefix
-  uint64_t* bar_kf = bars + 9;     // [NST] K stage full
+  uint64_t* bar_qe = bars + 9;     //       Q of the segment read for the last time
+  uint64_t* bar_e = bars + 10;     //       O of the segment read by the 8 softmax warps
+  uint64_t* bar_kf = bars + 11;    // [NST] K stage full
   uint64_t* bar_ke = bar_kf + NST; // [NST] K stage free
   uint64_t* bar_vf = bar_ke + NST; // [NST]
   uint64_t* bar_ve = bar_vf + NST; // [NST]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 9 + 4 * NST);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 11 + 4 * NST);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
-  int* s_max = reinterpret_cast<int*>(tmem_slot + 4);  // [2] largest prefix length of slot x
+  int* s_warp = reinterpret_cast<int*>(tmem_slot + 4);   // [12] key tiles per warp of the scan
+  int* s_start = s_warp + 12;                            // [2] pair and offset where the run starts
+  int64_t* s_run = reinterpret_cast<int64_t*>(s_warp + 14);  // end of the run, key tiles in all, runs
+  Segment* s_seg = reinterpret_cast<Segment*>(s_run + 3);    // [12] place of each warp in the run
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int hk = blockIdx.y, split = blockIdx.z;
-  const int GT = p.G * p.T;
   const bool alt = p.alternate != 0;
-  // row tile of slot x: sequences [b0, b0 + bt), rows [r0, r0 + rt) of each
-  auto tile_of = [&](int x) { return alt ? 0 : 2 * int(blockIdx.x) + x; };
-  auto tile_b0 = [&](int i) { return GT <= 128 ? i * p.bt : i / p.row_tiles; };
-  auto tile_r0 = [&](int i) { return GT <= 128 ? 0 : (i % p.row_tiles) * 128; };
-  const bool have1 = alt || tile_of(1) < p.m_tiles;
+  const int rows = p.gt * p.tt * p.bt;
 
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) { mbar_init(bar_q + i, 1); mbar_init(bar_s + i, 1); mbar_init(bar_p + i, 4); }
     mbar_init(bar_o, 1);
     mbar_init(bar_z, 1);
     mbar_init(bar_g, 1);
+    mbar_init(bar_qe, 1);
+    mbar_init(bar_e, 8);
     for (int i = 0; i < NST; ++i) {
       mbar_init(bar_kf + i, 1); mbar_init(bar_ke + i, 1); mbar_init(bar_vf + i, 1); mbar_init(bar_ve + i, 1);
     }
     *abort_flag = 0;
-    s_max[0] = s_max[1] = 0;
     fence_mbar_init();
     tma_prefetch_desc(&mapQ); tma_prefetch_desc(&mapK); tma_prefetch_desc(&mapV);
   }
@@ -96,34 +170,79 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     tmem_alloc(tmem_slot, 512);
     tmem_relinquish();
   }
-  // rows of the tile that no load fills are zero: their scores are finite and nothing is stored
-  const int rows = p.rt * p.bt;
+  // rows of a tile that no load fills are zero: their scores are finite and nothing of them is stored
   for (int i = tid; i < (128 - rows) * 8 * NB * 2; i += kPfxThreads) {
     const int ch = i & 7, blk = (i >> 3) % (2 * NB), r = rows + (i >> 3) / (2 * NB);
     *reinterpret_cast<uint4*>(sQ + blk * kTileBlockBytes + r * 128 + ch * 16) = make_uint4(0, 0, 0, 0);
   }
   fence_proxy_async_smem();
-  __syncthreads();   // s_max is set
-  for (int i = tid; i < 2 * p.bt; i += kPfxThreads) {
-    const int x = i >= p.bt, ti = tile_of(x), b = tile_b0(ti) + (x ? i - p.bt : i);
-    if (ti < p.m_tiles && b < p.B) atomicMax(s_max + x, p.prefix_len ? max(0, min(p.P, p.prefix_len[b])) : p.P);
+
+  // longest prefix of every row tile: a warp per pair with its lanes over the sequences, or, where a
+  // tile has few of them (and there may be many tiles), a thread per pair
+  const bool by_warp = p.bt > 8;
+  for (int i = by_warp ? warp : tid; i < p.pairs; i += by_warp ? kPfxThreads / 32 : kPfxThreads) {
+    int len[2] = {-1, -1};
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int ti = 2 * (p.pair_base + i) + x;
+      if (ti >= p.m_tiles) break;
+      const RowTile rt = row_tile(p, ti);
+      for (int k = by_warp ? lane : 0; k < p.bt; k += by_warp ? 32 : 1)
+        len[x] = max(len[x], seen_length(p, rt.b0 + k, rt.t0));
+    }
+    if (by_warp) {
+      len[0] = __reduce_max_sync(0xffffffffu, len[0]);
+      len[1] = __reduce_max_sync(0xffffffffu, len[1]);
+    }
+    if (!by_warp || lane == 0) tab[i] = make_int2(len[0], len[1]);
   }
+  __syncthreads();
+  // where the run starts: key tiles of one kv head summed over the pairs
+  const int per = (p.pairs + kPfxThreads - 1) / kPfxThreads;
+  const int i0 = min(p.pairs, tid * per), i1 = min(p.pairs, i0 + per);
+  int mine = 0;
+  for (int i = i0; i < i1; ++i) mine += pair_tiles(tab[i]);
+  int incl = mine;
+#pragma unroll
+  for (int k = 1; k < 32; k <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, k);
+    if (lane >= k) incl += v;
+  }
+  if (lane == 31) s_warp[warp] = incl;
+  __syncthreads();
+  int before = incl - mine, per_head = 0;
+  for (int w = 0; w < kPfxThreads / 32; ++w) {
+    if (w < warp) before += s_warp[w];
+    per_head += s_warp[w];
+  }
+  const int64_t total = int64_t(per_head) * p.Hkv;
+  // CTAs that get a run: none an empty one, in alternate mode one tile for each slot.  With one
+  // pair in all and short runs, a whole number of runs per kv head: a run that straddles two heads
+  // loads queries and leaves parts twice (costs about two tiles, saves less than one).
+  int64_t n_runs = min(int64_t(gridDim.x), alt ? (total + 1) / 2 : total);
+  if (p.pairs == 1 && n_runs >= p.Hkv && total < 16 * n_runs) n_runs -= n_runs % p.Hkv;
+  const int64_t run0 = blockIdx.x < n_runs ? total * blockIdx.x / n_runs : 0;
+  const int64_t run1 = blockIdx.x < n_runs ? total * (blockIdx.x + 1) / n_runs : 0;
+  const int in_head = per_head > 0 ? int(run0 % per_head) : 0;
+  if (run0 < run1 && in_head >= before && in_head < before + mine) {
+    int at = before, i = i0;
+    while (at + pair_tiles(tab[i]) <= in_head) at += pair_tiles(tab[i++]);
+    s_start[0] = i;
+    s_start[1] = in_head - at;
+  }
+  if (tid == 0) { s_run[0] = run1; s_run[1] = total; s_run[2] = n_runs; }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-
-  // key tiles of this split, cut at the longest prefix among the rows
-  const int kt0 = int(int64_t(p.key_tiles) * split / p.splits);
-  const int kt1 = int(int64_t(p.key_tiles) * (split + 1) / p.splits);
-  const int max0 = s_max[0], max1 = s_max[1], max_len = max(max0, max1);
-  const int n_tiles = max(0, min(kt1, (max_len + kBN - 1) / kBN) - kt0);
-  // slot x works on key tile j of the split
-  auto active = [&](int x, int j) {
-    return alt ? (j & 1) == x : (kt0 + j) * kBN < (x ? max1 : max0);
-  };
-  // the last tile holds the end of the longest prefix: V rows behind it may hold anything
-  const bool clear_v = n_tiles > 0 && (kt0 + n_tiles) * kBN > max_len;
+  Segment* sg = s_seg + warp;
+  if (lane == 0) {
+    sg->left = run1 - run0;
+    sg->hk = per_head > 0 ? int(run0 / per_head) : 0;
+    sg->pair = s_start[0];
+    sg->j1 = s_start[1];
+  }
+  __syncwarp();
 
   bool ok = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -137,93 +256,119 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0 && lane == 0) {
       // ---------------- TMA producer ----------------
-      if (n_tiles > 0) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int ti = tile_of(x);
-          if (alt ? x == 1 : !active(x, 0)) continue;   // a slot without work loads (and waits for) nothing
-          mbar_expect_tx(bar_q + x, uint32_t(NB * rows) * 128u);
+      int it = 0;  // key tiles loaded
+      for (int n = 0; next_segment<false>(sg, tab, p.pairs); ++n) {
+        const int hk = sg->hk, j0 = sg->j0, n_tiles = sg->j1 - j0;
+        for (int j = 0; j < n_tiles; ++j, ++it) {
+          const int st = it % NST, use = it / NST, y = (j0 + j) * kBN;
+          if (use > 0) wait(bar_ke + st, (use - 1) & 1);
+          mbar_expect_tx(bar_kf + st, C::kTile);
           for (int nb = 0; nb < NB; ++nb)
-            tma_load_4d(sQ + x * C::kTile + nb * kTileBlockBytes, &mapQ, bar_q + x, nb * 64, tile_r0(ti), hk,
-                        tile_b0(ti));
+            tma_load_3d(sK + st * C::kTile + nb * kTileBlockBytes, &mapK, bar_kf + st, nb * 64, y, hk);
+          if (j == 0) {
+            if (n > 0) wait(bar_qe, (n - 1) & 1);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              if (alt ? x == 1 : slot_tiles(sg, false, x) == 0) continue;   // a slot without work loads nothing
+              const RowTile rt = row_tile(p, 2 * (p.pair_base + sg->pair) + x);
+              mbar_expect_tx(bar_q + x, uint32_t(NB * rows) * 128u);
+              for (int nb = 0; nb < NB; ++nb)
+                tma_load_5d(sQ + x * C::kTile + nb * kTileBlockBytes, &mapQ, bar_q + x, nb * 64, rt.g0, rt.t0,
+                            hk, rt.b0);
+            }
+          }
+          if (use > 0) wait(bar_ve + st, (use - 1) & 1);
+          mbar_expect_tx(bar_vf + st, C::kTile);
+          for (int nb = 0; nb < NB; ++nb)
+            tma_load_3d(sV + st * C::kTile + nb * kTileBlockBytes, &mapV, bar_vf + st, nb * 64, y, hk);
         }
-      }
-      for (int j = 0; j < n_tiles; ++j) {
-        const int st = j % NST, use = j / NST, y = (kt0 + j) * kBN;
-        if (use > 0) wait(bar_ke + st, (use - 1) & 1);
-        mbar_expect_tx(bar_kf + st, C::kTile);
-        for (int nb = 0; nb < NB; ++nb)
-          tma_load_3d(sK + st * C::kTile + nb * kTileBlockBytes, &mapK, bar_kf + st, nb * 64, y, hk);
-        if (use > 0) wait(bar_ve + st, (use - 1) & 1);
-        mbar_expect_tx(bar_vf + st, C::kTile);
-        for (int nb = 0; nb < NB; ++nb)
-          tma_load_3d(sV + st * C::kTile + nb * kTileBlockBytes, &mapV, bar_vf + st, nb * 64, y, hk);
       }
     } else if (warp == 1 && lane == 0) {
       // ---------------- MMA issuer ----------------
       constexpr uint32_t idesc_s = make_idesc_bf16(128, 128, 0, 0);
       constexpr uint32_t idesc_o = make_idesc_bf16(128, D, 0, 1);
-      const uint32_t q_lo[2] = {desc_lo(smem_u32(sQ), 16), desc_lo(smem_u32(sQ + (alt ? 0 : C::kTile)), 16)};
+      const uint32_t q_lo0 = desc_lo(smem_u32(sQ), 16);
       const uint32_t k_lo0 = desc_lo(smem_u32(sK), 16);
       const uint32_t v_lo0 = desc_lo(smem_u32(sV), kTileBlockBytes);
-      int n_pv[2] = {0, 0};  // PV MMAs issued per slot
-      bool q_seen[2] = {false, false};
-      bool k_waited, v_waited;
-      auto scores = [&](int x, int j) {   // S_x = Q_x K(j)^T
-        const int st = j % NST, qx = alt ? 0 : x;
-        if (!q_seen[qx]) { wait(bar_q + qx, 0); q_seen[qx] = true; }
-        if (!k_waited) { wait(bar_kf + st, (j / NST) & 1); k_waited = true; }
-        const uint32_t tS = tmem + (x ? C::kS1 : C::kS0), k_lo = k_lo0 + st * (C::kTile >> 4);
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-          umma_ss_lo(tS, q_lo[x] + kmajor_step(k, kTileBlockBytes), k_lo + kmajor_step(k, kTileBlockBytes),
-                     idesc_s, k > 0);
-        tc_commit(bar_s + x);
-      };
-      auto values = [&](int x, int j) {   // O_x += P_x V(j)
-        const int st = j % NST;
-        wait(bar_p + x, n_pv[x] & 1);
-        if (!v_waited) {
-          wait(bar_vf + st, (j / NST) & 1);
-          if (clear_v && j == n_tiles - 1) { mbar_arrive(bar_g); wait(bar_z, 0); }
-          v_waited = true;
-        }
-        tc_fence_after();
-        const uint32_t tS = tmem + (x ? C::kS1 : C::kS0), tO = tmem + (x ? C::kO1 : C::kO0);
-        const uint32_t v_lo = v_lo0 + st * (C::kTile >> 4);
-        umma_ts_lo(tO, tS, v_lo, idesc_o, n_pv[x] > 0);
-#pragma unroll
-        for (int k = 1; k < kBN / 16; ++k)
-          umma_ts_lo(tO, tS + k * 8, v_lo + mnmajor_step(k), idesc_o, 1);
-        ++n_pv[x];
-      };
-      for (int s = 0; s <= n_tiles; ++s) {
-        k_waited = v_waited = false;
-        if (alt) {   // the slots never share a step: the next scores go first
-          if (s < n_tiles) scores(s & 1, s);
-          if (s >= 1) values((s - 1) & 1, s - 1);
-        } else {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            if (s >= 1 && active(x, s - 1)) values(x, s - 1);
-            if (s < n_tiles && active(x, s)) scores(x, s);
+      // per slot one bit each (a slot number known only at run time would put arrays in memory)
+      uint32_t ph_p = 0, ph_q = 0;   // phase of P_x / Q_x
+      uint32_t ph_z = 0;
+      int it0 = 0;                   // key tiles of earlier segments
+      for (int n = 0; next_segment<false>(sg, tab, p.pairs); ++n) {
+        const int n_tiles = sg->j1 - sg->j0;
+        const int n_mine0 = slot_tiles(sg, alt, 0), n_mine1 = slot_tiles(sg, alt, 1);
+        const bool clear_v = ends_inside(sg, p.P);
+        uint32_t q_seen = 0, o_begun = 0;
+        bool k_waited, v_waited, o_free = n == 0;
+        auto scores = [&](int x, int j) {   // S_x = Q_x K(j)^T
+          const int it = it0 + j, st = it % NST, qx = alt ? 0 : x;
+          if (!(q_seen >> qx & 1)) {
+            wait(bar_q + qx, ph_q >> qx & 1);
+            ph_q ^= 1u << qx;
+            q_seen |= 1u << qx;
           }
+          if (!k_waited) { wait(bar_kf + st, (it / NST) & 1); k_waited = true; }
+          const uint32_t tS = tmem + C::kS0 + x * (C::kS1 - C::kS0), k_lo = k_lo0 + st * (C::kTile >> 4);
+          const uint32_t q_lo = q_lo0 + qx * (C::kTile >> 4);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            umma_ss_lo(tS, q_lo + kmajor_step(k, kTileBlockBytes), k_lo + kmajor_step(k, kTileBlockBytes),
+                       idesc_s, k > 0);
+          tc_commit(bar_s + x);
+        };
+        auto values = [&](int x, int j) {   // O_x += P_x V(j)
+          const int it = it0 + j, st = it % NST;
+          wait(bar_p + x, ph_p >> x & 1);
+          ph_p ^= 1u << x;
+          if (!v_waited) {
+            wait(bar_vf + st, (it / NST) & 1);
+            if (clear_v && j == n_tiles - 1) { mbar_arrive(bar_g); wait(bar_z, ph_z); ph_z ^= 1; }
+            v_waited = true;
+          }
+          if (!o_free) { wait(bar_e, (n - 1) & 1); o_free = true; }
+          tc_fence_after();
+          const uint32_t tS = tmem + C::kS0 + x * (C::kS1 - C::kS0), tO = tmem + C::kO0 + x * (C::kO1 - C::kO0);
+          const uint32_t v_lo = v_lo0 + st * (C::kTile >> 4);
+          umma_ts_lo(tO, tS, v_lo, idesc_o, o_begun >> x & 1);
+          o_begun |= 1u << x;
+#pragma unroll
+          for (int k = 1; k < kBN / 16; ++k)
+            umma_ts_lo(tO, tS + k * 8, v_lo + mnmajor_step(k), idesc_o, 1);
+        };
+        for (int s = 0; s <= n_tiles; ++s) {
+          k_waited = v_waited = false;
+          if (alt) {   // the slots never share a step: the next scores go first
+            if (s < n_tiles) scores(s & 1, s);
+            if (s >= 1) values((s - 1) & 1, s - 1);
+          } else {
+            if (s >= 1 && s <= n_mine0) values(0, s - 1);
+            if (s < n_mine0) scores(0, s);
+            if (s >= 1 && s <= n_mine1) values(1, s - 1);
+            if (s < n_mine1) scores(1, s);
+          }
+          if (s < n_tiles) tc_commit(bar_ke + (it0 + s) % NST);
+          if (s == n_tiles - 1) tc_commit(bar_qe);
+          if (s >= 1) tc_commit(bar_ve + (it0 + s - 1) % NST);
         }
-        if (s < n_tiles) tc_commit(bar_ke + s % NST);
-        if (s >= 1) tc_commit(bar_ve + (s - 1) % NST);
+        tc_commit(bar_o);
+        it0 += n_tiles;
       }
-      tc_commit(bar_o);
-    } else if (warp == 2 && clear_v) {
+    } else if (warp == 2) {
       // ---------------- V rows behind the longest prefix ----------------
-      const int st = (n_tiles - 1) % NST;
-      wait(bar_g, 0);
-      for (int i = lane; i < (kBN - max_len % kBN) * 8 * NB; i += 32) {
-        const int ch = i & 7, blk = (i >> 3) % NB, r = max_len % kBN + (i >> 3) / NB;
-        *reinterpret_cast<uint4*>(sV + st * C::kTile + blk * kTileBlockBytes + r * 128 + ch * 16) =
-            make_uint4(0, 0, 0, 0);
+      int n_clear = 0, it0 = 0;
+      while (next_segment<true>(sg, tab, p.pairs)) {
+        it0 += sg->j1 - sg->j0;
+        if (!ends_inside(sg, p.P)) continue;
+        const int st = (it0 - 1) % NST, r0 = max(sg->len[0], sg->len[1]) - (sg->j1 - 1) * kBN;
+        wait(bar_g, n_clear++ & 1);
+        for (int i = lane; i < (kBN - r0) * 8 * NB; i += 32) {
+          const int ch = i & 7, blk = (i >> 3) % NB, r = r0 + (i >> 3) / NB;
+          *reinterpret_cast<uint4*>(sV + st * C::kTile + blk * kTileBlockBytes + r * 128 + ch * 16) =
+              make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+        mbar_arrive_warp(bar_z);
       }
-      fence_proxy_async_smem();
-      mbar_arrive_warp(bar_z);
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
@@ -233,30 +378,32 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     const uint32_t lane_base = uint32_t((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + lane_base + (x ? C::kS1 : C::kS0);
     const uint32_t tO = tmem + lane_base + (x ? C::kO1 : C::kO0);
-    if (x == 0 || have1) {
-      const int ti = tile_of(x);
-      // the row: sequence b, row rr = head in group * T + token
-      int b, rr;
-      if (GT <= 128) { b = tile_b0(ti) + r / GT; rr = r % GT; }
-      else { b = tile_b0(ti); rr = tile_r0(ti) + r; }
-      bool store = r < rows && b < p.B && rr < GT;
-      int len = x ? max1 : max0;
-      if (store) {
-        if (p.prefix_len) len = max(0, min(p.P, p.prefix_len[b]));
-        if (p.seq_len && rr % p.T >= p.seq_len[b]) store = false;   // a row of padding
+    int n_s = 0;              // S tiles taken
+    int cut = -1;
+    for (int n = 0; next_segment<true>(sg, tab, p.pairs); ++n) {
+      // the row: sequence b, token t, head g of the group
+      auto place = [&](int& b, int& t, int& g) {
+        const int ti = alt ? 0 : 2 * (p.pair_base + sg->pair) + x;
+        const RowTile rt = row_tile(p, ti);
+        b = rt.b0 + r / (p.gt * p.tt); t = rt.t0 + r / p.gt % p.tt; g = rt.g0 + r % p.gt;
+        return ti < p.m_tiles && r < rows && b < p.B && t < p.T && g < p.G && !(p.seq_len && t >= p.seq_len[b]);
+      };
+      const int n_mine = slot_tiles(sg, alt, x);
+      int c_hi = sg->len[alt ? 0 : x];   // keys of the next tile, and behind it, that the row sees
+      {
+        int b, t, g;
+        if (place(b, t, g) && p.prefix_len) c_hi = max(0, min(p.P, p.prefix_len[b]));
+        c_hi -= (sg->j0 + (alt ? x : 0)) * kBN;
       }
       float m_ref = -INFINITY;  // reference exponent (log2 units), may lag the true row maximum
       float l_sum = 0.f;
-      int n_done = 0;
       uint32_t sreg[4][32];
-      for (int j = 0; j < n_tiles; ++j) {
-        if (!active(x, j)) continue;
-        wait(bar_s + x, n_done & 1);
+      for (int j = 0; j < n_mine; ++j) {
+        wait(bar_s + x, n_s++ & 1);
         tc_fence_after();
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, sreg[c]);
         tmem_ld_wait();
-        const int c_hi = len - (kt0 + j) * kBN;   // keys of the tile that the row sees
         if (c_hi < kBN) {
 #pragma unroll
           for (int c = 0; c < 4; ++c)
@@ -264,6 +411,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
             for (int e = 0; e < 32; ++e) sreg[c][e] = (c * 32 + e < c_hi) ? sreg[c][e] : 0xff800000u;  // -inf
         }
         __syncwarp();
+        c_hi -= alt ? 2 * kBN : kBN;
         float mx;
         {
           float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -291,20 +439,25 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         const unsigned long long scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
         const unsigned long long negm2 = pack_f32x2(neg_m, neg_m);
         unsigned long long ps2[4] = {0ull, 0ull, 0ull, 0ull};
+        // P goes over the first 64 columns of S_x, column c holding keys 2c, 2c+1, sixteen columns as soon
+        // as they are ready (S is in registers)
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 4; ++c) {
+          uint32_t pk[16];
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
             const float2 a = unpack_f32x2(fma_f32x2(
                 pack_f32x2(__uint_as_float(sreg[c][e]), __uint_as_float(sreg[c][e + 1])), scale2, negm2));
             const float p0 = ex2(a.x), p1 = ex2(a.y);
             ps2[(e >> 1) & 3] = add_f32x2(ps2[(e >> 1) & 3], pack_f32x2(p0, p1));
-            sreg[c][e >> 1] = pack_bf16(p0, p1);
+            pk[e >> 1] = pack_bf16(p0, p1);
           }
+          tmem_st16(tS + c * 16, pk);
+        }
         const float2 sm = unpack_f32x2(add_f32x2(add_f32x2(ps2[0], ps2[1]), add_f32x2(ps2[2], ps2[3])));
         l_sum = l_sum * corr + (sm.x + sm.y);
         // S_x of this tile complete means P V of the slot's previous tile is: O_x is at rest
-        if (n_done > 0 && __any_sync(0xffffffffu, rescale)) {
+        if (j > 0 && __any_sync(0xffffffffu, rescale)) {
           uint32_t oreg[32];
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
@@ -315,26 +468,21 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
             tmem_st32(tO + c * 32, oreg);
           }
         }
-        // P as packed bf16 over the first 64 columns of S_x: column c holds keys 2c, 2c+1
-        {
-          uint32_t pk[32];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) { pk[e] = sreg[2 * h][e]; pk[16 + e] = sreg[2 * h + 1][e]; }
-            tmem_st32(tS + h * 32, pk);
-          }
-        }
         tmem_st_wait();
         tc_fence_before();
         mbar_arrive_warp(bar_p + x);
-        ++n_done;
       }
 
-      if (n_done > 0) wait(bar_o, 0);
+      wait(bar_o, n & 1);   // also by a slot without work, which would lose count of the phases
       tc_fence_after();
-      const size_t row = (size_t(b) * p.Hkv + hk) * GT + rr;
-      if (p.merge_O) {
+      int b, t, g;
+      const bool store = place(b, t, g);
+      const int unit = sg->hk * p.pairs + sg->pair;
+      const bool whole = sg->j0 == 0 && sg->j1 == sg->nt;
+      const int part = whole ? 2 * int(gridDim.x) + unit : 2 * int(blockIdx.x) + (n > 0 ? 1 : 0);
+      const bool finish = whole && !p.whole_parts;   // nothing to wait for: the row is joined here
+      if (finish) {
+        const size_t row = ((size_t(b) * p.Hkv + sg->hk) * p.G + g) * p.T + t;
         // joined with the row's own part (fp32, normalised, with its log-sum-exp) and rounded once
         const float lo = store ? p.own_lse[row] * 1.4426950408889634f : 0.f;
         const float lp = l_sum > 0.f ? m_ref + log2f(l_sum) : -INFINITY;
@@ -348,7 +496,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t oreg[32];
-          if (n_done > 0) { tmem_ld32(tO + c * 32, oreg); tmem_ld_wait(); }
+          if (n_mine > 0) { tmem_ld32(tO + c * 32, oreg); tmem_ld_wait(); }
           if (store) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -358,18 +506,20 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
               *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(own + c * 32 + q * 8 + 4);
 #pragma unroll
               for (int e = 0; e < 8; ++e)
-                v[e] = v[e] * fo + (n_done > 0 ? __uint_as_float(oreg[q * 8 + e]) * fp : 0.f);
+                v[e] = v[e] * fo + (n_mine > 0 ? __uint_as_float(oreg[q * 8 + e]) * fp : 0.f);
               *reinterpret_cast<uint4*>(orow + c * 32 + q * 8) =
                   make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
                              pack_bf16(v[6], v[7]));
             }
           }
+          __syncwarp();
         }
       } else {
-        const int parts = p.splits << (alt ? 1 : 0);
-        const size_t u = row * parts + (alt ? 2 * split + x : split);
+        // a part: a cut unit's go to the CTA's two places (its first segment, its last one), a whole
+        // unit's to a place of its own
+        const size_t u = (size_t(part) * 2 + x) * 128 + r;
         if (store) *reinterpret_cast<float2*>(p.part_ml + 2 * u) = make_float2(m_ref, l_sum);
-        if (n_done > 0) {
+        if (n_mine > 0) {
           float* dst = p.part_acc + u * D;
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
@@ -381,38 +531,85 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
               for (int q = 0; q < 8; ++q)
                 *reinterpret_cast<uint4*>(dst + c * 32 + q * 4) =
                     make_uint4(oreg[4 * q], oreg[4 * q + 1], oreg[4 * q + 2], oreg[4 * q + 3]);
+            __syncwarp();
           }
         }
       }
+      tc_fence_before();
+      mbar_arrive_warp(bar_e);
+      // where the unit's parts are, from the CTA that has its first key tile
+      if (sg->j0 == 0 && tid == 128) {
+        // number of the unit's last key tile, and the CTA that has it
+        const int64_t last = s_run[0] - sg->left - 1 + (sg->nt - sg->j1);
+        const int c1 = int(((last + 1) * s_run[2] + s_run[1] - 1) / s_run[1]) - 1;
+        p.unit_parts[unit] = make_int4(finish ? 0 : c1 - int(blockIdx.x) + 1, part, blockIdx.x, 0);
+        if (!whole) cut = unit;
+      }
     }
+    // a run starts at most one unit that other CTAs go on with: its last one
+    if (tid == 128) p.cut_units[blockIdx.x] = cut;
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
-// Joins the partial results of a row: `parts` of the prefix and, of its own keys, own_parts of the
-// decode kernel or one normalised result with its log-sum-exp (own_lse).  One warp per row, in a
-// fixed order.  A part with no key (l = 0) has no values and is not read.
-constexpr int kJoinWarps = 4;
-template <int D>
-__global__ void __launch_bounds__(kJoinWarps * 32) prefix_join(const PrefixParams p, const float* own_ml,
-                                                               const float* own_acc, int own_parts,
-                                                               int64_t n_rows) {
+// Joins the partial results of a row: those of the prefix and, of its own keys, own_parts of the
+// decode kernel or one normalised result with its log-sum-exp (own_lse).  WARPS warps per row, in
+// a fixed order.  A part with no key (l = 0) has no values and is not read.
+//   CUT false: grid over all rows;   CUT true: grid (256 rows, CTAs of the prefix kernel), the rows
+//   of the unit that the CTA left unfinished (all others are finished already)
+constexpr int kJoinThreads = 128;
+template <int D, int WARPS, bool CUT>
+__global__ void __launch_bounds__(kJoinThreads) prefix_join(const PrefixParams p, const float* own_ml,
+                                                            const float* own_acc, int own_parts, int n_rows) {
   constexpr int E = D / 32;  // elements per lane
   using Vec = typename std::conditional<E == 4, float4, float2>::type;
-  const int lane = threadIdx.x & 31;
-  const int64_t row = int64_t(blockIdx.x) * kJoinWarps + (threadIdx.x >> 5);
-  if (row >= n_rows) return;
-  if (p.seq_len && int(row % p.T) >= p.seq_len[row / (int64_t(p.Hkv) * p.G * p.T)]) return;
-  const int parts = p.splits << (p.alternate ? 1 : 0);
-  const float2* pml = reinterpret_cast<const float2*>(p.part_ml) + row * parts;
+  constexpr int kRows = kJoinThreads / 32 / WARPS;
+  __shared__ float s_l[kJoinThreads / 32];
+  __shared__ Vec s_acc[kJoinThreads / 32][32];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, w0 = wid % WARPS;
+  const int idx = int(blockIdx.x) * kRows + wid / WARPS;
+  bool here;
+  int unit = 0, x = 0, r = 0;
+  size_t row = 0;
+  if (CUT) {
+    unit = p.cut_units[blockIdx.y];
+    if (unit < 0) return;
+    x = idx >> 7;
+    r = idx & 127;
+    const RowTile rt = row_tile(p, 2 * (p.pair_base + unit % p.pairs) + x);
+    const int b = rt.b0 + r / (p.gt * p.tt), t = rt.t0 + r / p.gt % p.tt, g = rt.g0 + r % p.gt;
+    here = r < p.gt * p.tt * p.bt && b < p.B && t < p.T && g < p.G && !(p.seq_len && t >= p.seq_len[b]);
+    row = ((size_t(b) * p.Hkv + unit / p.pairs) * p.G + g) * p.T + t;
+  } else {
+    here = idx < n_rows;
+    row = idx;
+    if (here) {
+      const int t = idx % p.T, g = idx / p.T % p.G, q = idx / (p.T * p.G), hk = q % p.Hkv, b = q / p.Hkv;
+      const int ti = (b / p.bt * p.t_tiles + t / p.tt) * p.g_tiles + g / p.gt;
+      const int pair = ti / 2 - p.pair_base;
+      here = pair >= 0 && pair < p.pairs && !(p.seq_len && t >= p.seq_len[b]);
+      unit = hk * p.pairs + pair;
+      x = ti & 1;
+      r = (b % p.bt * p.tt + t % p.tt) * p.gt + g % p.gt;
+    }
+  }
+  if (WARPS == 1 && !here) return;
+  const int4 parts = here ? p.unit_parts[unit] : make_int4(0, 0, 0, 0);
+  const int n_sub = p.alternate ? 2 : 1;   // alternate mode: both slots hold the row
+  const int n_pfx = here ? parts.x * n_sub : 0, n_own = here ? own_parts : 0;
+  auto place = [&](int i) -> size_t {
+    const int k = i / n_sub, part = k == 0 ? parts.y : 2 * (parts.z + k);
+    return (size_t(part) * 2 + (n_sub == 2 ? i % 2 : x)) * 128 + r;
+  };
+  const float2* pml = reinterpret_cast<const float2*>(p.part_ml);
   const float2* oml = reinterpret_cast<const float2*>(own_ml) + row * own_parts;
   float mm = -INFINITY;
-  for (int s = lane; s < parts; s += 32) mm = fmaxf(mm, pml[s].y > 0.f ? pml[s].x : -INFINITY);
-  for (int s = lane; s < own_parts; s += 32) mm = fmaxf(mm, oml[s].y > 0.f ? oml[s].x : -INFINITY);
+  for (int i = lane; i < n_pfx; i += 32) { const float2 v = pml[place(i)]; if (v.y > 0.f) mm = fmaxf(mm, v.x); }
+  for (int i = lane; i < n_own; i += 32) { const float2 v = oml[i]; if (v.y > 0.f) mm = fmaxf(mm, v.x); }
   float lo = -INFINITY;
-  if (p.own_lse) { lo = p.own_lse[row] * 1.4426950408889634f; mm = fmaxf(mm, lo); }
+  if (p.own_lse && here) { lo = p.own_lse[row] * 1.4426950408889634f; mm = fmaxf(mm, lo); }
 #pragma unroll
   for (int k = 16; k; k >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, k));
   float l = 0.f, acc[E];
@@ -424,26 +621,41 @@ __global__ void __launch_bounds__(kJoinWarps * 32) prefix_join(const PrefixParam
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] += f[e] * w;
   };
-#pragma unroll 4
-  for (int s = 0; s < parts; ++s) {
-    const float2 ml = pml[s];
+#pragma unroll 8
+  for (int i = w0; i < n_pfx; i += WARPS) {
+    const size_t u = place(i);
+    const float2 ml = pml[u];
     if (!(ml.y > 0.f)) continue;
     const float w = ex2(ml.x - mm);
     l += ml.y * w;
-    add(p.part_acc + (row * parts + s) * D, w);
+    add(p.part_acc + u * D, w);
   }
 #pragma unroll 4
-  for (int s = 0; s < own_parts; ++s) {
-    const float2 ml = oml[s];
+  for (int i = w0; i < n_own; i += WARPS) {
+    const float2 ml = oml[i];
     if (!(ml.y > 0.f)) continue;
     const float w = ex2(ml.x - mm);
     l += ml.y * w;
-    add(own_acc + (row * own_parts + s) * D, w);
+    add(own_acc + (row * own_parts + i) * D, w);
   }
-  if (p.own_lse) {
+  if (p.own_lse && here && w0 == 0) {
     const float w = ex2(lo - mm);
     l += w;
     add(p.own_O + row * D, w);
+  }
+  if (WARPS > 1) {
+    if (lane == 0) s_l[wid] = l;
+    s_acc[wid][lane] = *reinterpret_cast<Vec*>(acc);
+    __syncthreads();
+    if (w0 != 0 || !here) return;
+#pragma unroll
+    for (int k = 1; k < WARPS; ++k) {
+      l += s_l[wid + k];
+      const Vec v = s_acc[wid + k][lane];
+      const float* f = reinterpret_cast<const float*>(&v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += f[e];
+    }
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;   // a row that sees no key at all: 0, log-sum-exp -inf
   if (lane * E < p.d) {
@@ -455,90 +667,118 @@ __global__ void __launch_bounds__(kJoinWarps * 32) prefix_join(const PrefixParam
   if (p.LSE && lane == 0) p.LSE[row] = l > 0.f ? (mm + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-// bf16 [B][Hkv][rows][d] as (d, rows, Hkv, B); box of 64 columns x rt rows x bt sequences.
+// bf16 [B][Hkv][G][T][d] as (d, G, T, Hkv, B); box of 64 columns x gt heads x tt tokens x bt sequences.
 sepllm_status make_query_map(CUtensorMap* map, const void* base, const PrefixParams& p) {
   EncodeTiledFn enc = get_encode_tiled();
   if (!enc) return SEPLLM_CUDA_ERROR;
-  const cuuint64_t GT = cuuint64_t(p.G) * p.T, d = cuuint64_t(p.d);
-  cuuint64_t dims[4] = {d, GT, cuuint64_t(p.Hkv), cuuint64_t(p.B)};
-  cuuint64_t strides[3] = {d * 2, GT * d * 2, GT * d * 2 * p.Hkv};
-  cuuint32_t box[4] = {64, cuuint32_t(p.rt), 1, cuuint32_t(p.bt)};
-  cuuint32_t estr[4] = {1, 1, 1, 1};
-  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+  const cuuint64_t row = cuuint64_t(p.d) * 2;
+  cuuint64_t dims[5] = {cuuint64_t(p.d), cuuint64_t(p.G), cuuint64_t(p.T), cuuint64_t(p.Hkv), cuuint64_t(p.B)};
+  cuuint64_t strides[4] = {row * p.T, row, row * p.T * p.G, row * p.T * p.G * p.Hkv};
+  cuuint32_t box[5] = {64, cuuint32_t(p.gt), cuuint32_t(p.tt), 1, cuuint32_t(p.bt)};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, estr,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? SEPLLM_OK : SEPLLM_CUDA_ERROR;
 }
 
 template <int D>
-sepllm_status launch_prefix_d(const PrefixParams& p, const CUtensorMap& mq, const CUtensorMap& mk,
+sepllm_status launch_prefix_d(const PrefixParams& p, int grid, const CUtensorMap& mq, const CUtensorMap& mk,
                               const CUtensorMap& mv, cudaStream_t stream) {
   SEPLLM_CUDA_TRY(cudaFuncSetAttribute(prefix_attn<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        int(PfxCfg<D>::kRequest)));
-  const dim3 grid(p.alternate ? 1 : (p.m_tiles + 1) / 2, p.Hkv, p.splits);
   prefix_attn<D><<<grid, kPfxThreads, PfxCfg<D>::kRequest, stream>>>(mq, mk, mv, p);
   SEPLLM_CUDA_TRY(cudaGetLastError());
   return SEPLLM_OK;
 }
 
+int all_pairs(const PrefixParams& p) { return (p.m_tiles + 1) / 2; }
+// per launch: what the table holds, and a count of key tiles per kv head within 31 bits
+int launch_pairs(const PrefixParams& p) {
+  return std::min(all_pairs(p), std::min(kMaxPairs, (1 << 30) / p.key_tiles));
+}
+
+// CTAs of a launch over `pairs` pairs: one per SM, none without a key tile (two in alternate mode).
+int prefix_grid(const PrefixParams& p, int pairs) {
+  const int64_t work = int64_t(pairs) * p.Hkv * (p.alternate ? (p.key_tiles + 1) / 2 : p.key_tiles);
+  return int(std::min<int64_t>(p.max_ctas, work));
+}
+
+int64_t max_parts(const PrefixParams& p) {
+  // two places per CTA, and one per unit where whole units leave parts (decode)
+  const int pairs = launch_pairs(p);
+  return 2ll * prefix_grid(p, pairs) + (p.whole_parts ? int64_t(pairs) * p.Hkv : 0);
+}
+
 }  // namespace
 
-bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P) {
+bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, bool whole_parts) {
   p->B = B;
   p->Hkv = Hkv;
   p->G = Hq / Hkv;
   p->T = T;
   p->d = d;
   p->P = P;
-  const int64_t GT = int64_t(p->G) * T;
   p->key_tiles = (P + kBN - 1) / kBN;
-  p->rt = int(std::min<int64_t>(GT, 128));
-  p->bt = GT <= 128 ? std::min(128 / int(GT), B) : 1;
-  p->row_tiles = int((GT + 127) / 128);
-  const int64_t m_tiles = GT <= 128 ? (B + p->bt - 1) / p->bt : int64_t(B) * p->row_tiles;
-  if (GT > 0x7fffffff || m_tiles > 0x7fffffff || Hkv > 65535 || P > (1 << 30)) return false;
+  p->gt = std::min(p->G, 128);
+  p->tt = std::min(T, 128 / p->gt);
+  p->bt = p->tt == T && p->gt == p->G ? std::min(B, 128 / (p->gt * p->tt)) : 1;
+  p->g_tiles = (p->G + p->gt - 1) / p->gt;
+  p->t_tiles = (T + p->tt - 1) / p->tt;
+  const int64_t m_tiles = int64_t((B + p->bt - 1) / p->bt) * p->t_tiles * p->g_tiles;
+  if (m_tiles > 0x3fffffff || Hkv > 65535 || P > (1 << 30)) return false;
   p->m_tiles = int(m_tiles);
   p->alternate = m_tiles == 1 ? 1 : 0;
-  // one CTA per SM: split the key tiles until the SMs are full
-  const int64_t units = (p->alternate ? 1 : (m_tiles + 1) / 2) * Hkv;
-  int64_t s = std::max<int64_t>(1, 148 / units);
-  s = std::min<int64_t>(s, p->alternate ? (p->key_tiles + 1) / 2 : p->key_tiles);
-  p->splits = int(s);
+  p->whole_parts = whole_parts || p->alternate;   // alternate mode: two parts of every row, joined later
+  p->max_ctas = kSmCount;
   return true;
 }
 
 size_t prefix_part_bytes(const PrefixParams& p) {
-  const size_t units = size_t(p.B) * p.Hkv * p.G * p.T * (size_t(p.splits) << p.alternate);
-  return align_up(units * 2 * sizeof(float)) + align_up(units * kernel_head_dim(p.d) * sizeof(float));
+  const size_t rows = size_t(max_parts(p)) * 256;
+  return align_up(rows * 2 * sizeof(float)) + align_up(rows * kernel_head_dim(p.d) * sizeof(float)) +
+         align_up(size_t(launch_pairs(p)) * p.Hkv * sizeof(int4)) + align_up(kSmCount * sizeof(int32_t));
 }
 
 void place_prefix_parts(PrefixParams* p, uint8_t* ws) {
-  const size_t units = size_t(p->B) * p->Hkv * p->G * p->T * (size_t(p->splits) << p->alternate);
+  const size_t rows = size_t(max_parts(*p)) * 256;
   p->part_ml = reinterpret_cast<float*>(ws);
-  p->part_acc = reinterpret_cast<float*>(ws + align_up(units * 2 * sizeof(float)));
+  ws += align_up(rows * 2 * sizeof(float));
+  p->part_acc = reinterpret_cast<float*>(ws);
+  ws += align_up(rows * kernel_head_dim(p->d) * sizeof(float));
+  p->unit_parts = reinterpret_cast<int4*>(ws);
+  p->cut_units = reinterpret_cast<int32_t*>(ws + align_up(size_t(launch_pairs(*p)) * p->Hkv * sizeof(int4)));
 }
 
-sepllm_status launch_prefix(const PrefixParams& p, const void* Q, const void* Kp, const void* Vp,
-                            cudaStream_t stream) {
+sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const void* Vp, const float* own_ml,
+                            const float* own_acc, int own_parts, cudaStream_t stream) {
   CUtensorMap mq, mk, mv;
   sepllm_status st;
   if ((st = make_query_map(&mq, Q, p)) != SEPLLM_OK) return st;
   if ((st = make_tile_map(&mk, Kp, p.d, p.P, p.Hkv, p.d, int64_t(p.P) * p.d, 128)) != SEPLLM_OK) return st;
   if ((st = make_tile_map(&mv, Vp, p.d, p.P, p.Hkv, p.d, int64_t(p.P) * p.d, 128)) != SEPLLM_OK) return st;
-  return kernel_head_dim(p.d) == 64 ? launch_prefix_d<64>(p, mq, mk, mv, stream)
-                                    : launch_prefix_d<128>(p, mq, mk, mv, stream);
-}
-
-sepllm_status launch_prefix_join(const PrefixParams& p, const float* own_ml, const float* own_acc,
-                                 int own_parts, cudaStream_t stream) {
   const int64_t rows = int64_t(p.B) * p.Hkv * p.G * p.T;
-  const int64_t blocks = (rows + kJoinWarps - 1) / kJoinWarps;
-  if (blocks > 0x7fffffff) return SEPLLM_UNSUPPORTED;
-  if (kernel_head_dim(p.d) == 64)
-    prefix_join<64><<<unsigned(blocks), kJoinWarps * 32, 0, stream>>>(p, own_ml, own_acc, own_parts, rows);
-  else
-    prefix_join<128><<<unsigned(blocks), kJoinWarps * 32, 0, stream>>>(p, own_ml, own_acc, own_parts, rows);
-  SEPLLM_CUDA_TRY(cudaGetLastError());
+  if (rows > 0x7fffffff) return SEPLLM_UNSUPPORTED;
+  const bool d64 = kernel_head_dim(p.d) == 64;
+  // few rows have many parts each: four warps per row (measured at 1024 rows of 36 parts: 9 us
+  // against 16; at 8192 rows of 7 parts: 23 against 12)
+  const bool wide = rows <= 2048;
+  for (p.pair_base = 0; p.pair_base < all_pairs(p); p.pair_base += p.pairs) {
+    p.pairs = std::min(launch_pairs(p), all_pairs(p) - p.pair_base);
+    const int grid = prefix_grid(p, p.pairs);
+    st = d64 ? launch_prefix_d<64>(p, grid, mq, mk, mv, stream) : launch_prefix_d<128>(p, grid, mq, mk, mv, stream);
+    if (st != SEPLLM_OK) return st;
+    if (!p.whole_parts) {
+      auto join = d64 ? prefix_join<64, 1, true> : prefix_join<128, 1, true>;
+      join<<<dim3(64, grid), kJoinThreads, 0, stream>>>(p, own_ml, own_acc, own_parts, 0);
+    } else {
+      auto join = d64 ? (wide ? prefix_join<64, 4, false> : prefix_join<64, 1, false>)
+                      : (wide ? prefix_join<128, 4, false> : prefix_join<128, 1, false>);
+      join<<<unsigned(wide ? rows : (rows + 3) / 4), kJoinThreads, 0, stream>>>(p, own_ml, own_acc, own_parts,
+                                                                                int(rows));
+    }
+    SEPLLM_CUDA_TRY(cudaGetLastError());
+  }
   return SEPLLM_OK;
 }
 
@@ -557,7 +797,7 @@ AttnPrefixLayout attn_prefix_layout(const sepllm_attn_desc* d, const sepllm_inde
   a.off_o = attn_layout(d, id).fwd_bytes;
   a.off_lse = a.off_o + align_up(rows * kernel_head_dim(d->d) * sizeof(float));
   a.off_parts = a.off_lse + align_up(rows * sizeof(float));
-  a.bytes = a.off_parts + (p.splits > 1 || p.alternate ? prefix_part_bytes(p) : 0);
+  a.bytes = a.off_parts + prefix_part_bytes(p);
   return a;
 }
 }  // namespace
@@ -569,7 +809,7 @@ extern "C" sepllm_status sepllm_attn_prefix_workspace_bytes(const sepllm_attn_de
   if (st != SEPLLM_OK) return st;
   if (P < 1) return SEPLLM_INVALID_ARG;
   PrefixParams p{};
-  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P)) return SEPLLM_UNSUPPORTED;
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P, false)) return SEPLLM_UNSUPPORTED;
   if (bytes) *bytes = attn_prefix_layout(desc, idesc, p).bytes;
   return SEPLLM_OK;
 }
@@ -589,7 +829,7 @@ extern "C" sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, co
   sepllm_index_header ih;
   if ((st = fill_index_header(idesc, &ih)) != SEPLLM_OK) return st;
   PrefixParams p{};
-  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P)) return SEPLLM_UNSUPPORTED;
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P, false)) return SEPLLM_UNSUPPORTED;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const AttnPrefixLayout lay = attn_prefix_layout(desc, idesc, p);
@@ -602,11 +842,9 @@ extern "C" sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, co
   p.seq_len = reinterpret_cast<const int32_t*>(static_cast<const uint8_t*>(index) + ih.off_seq_len);
   p.own_O = own_O;
   p.own_lse = own_lse;
-  p.merge_O = p.splits == 1 && !p.alternate;
   p.O = static_cast<__nv_bfloat16*>(O);
   p.LSE = LSE;
   p.status = reinterpret_cast<int32_t*>(ws);
   p.scale_log2 = (desc->scale != 0.f ? desc->scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
-  if ((st = launch_prefix(p, Q, Kp, Vp, stream)) != SEPLLM_OK) return st;
-  return p.merge_O ? SEPLLM_OK : launch_prefix_join(p, nullptr, nullptr, 0, stream);
+  return launch_prefix(p, Q, Kp, Vp, nullptr, nullptr, 0, stream);
 }

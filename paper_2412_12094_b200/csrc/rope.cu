@@ -238,8 +238,13 @@ void rope_frequencies(const sepllm_rope_desc* d, double* f, double* m) {
     hi = std::fmin(r - 1.0, std::ceil(pair_of(d->low)));
     if (hi == lo) hi += 0.001;
   }
+  // base^(-2i/r) as base^(-16 (i/8)/r) * base^(-2 (i%8)/r): sixteen powers instead of sixty-four (a
+  // call computes them anew), within two roundings
+  double small[8], large = 1.0;
+  for (int i = 0; i < 8 && i < r / 2; ++i) small[i] = std::pow(base, -2.0 * i / r);
   for (int i = 0; i < r / 2; ++i) {
-    double v = std::pow(base, -2.0 * i / r);
+    if (i % 8 == 0) large = std::pow(base, -2.0 * i / r);
+    double v = large * small[i % 8];
     if (d->scaling == SEPLLM_ROPE_LINEAR) v /= s;
     if (d->scaling == SEPLLM_ROPE_FACTORS) v /= d->freq_factors[i];
     if (d->scaling == SEPLLM_ROPE_YARN) {

@@ -100,9 +100,19 @@ def test_attention_refusals_and_workspace():
 
 def test_binding_refuses_other_shapes_and_types():
     with pytest.raises(ValueError):
-        api._expect("x", q=(torch.zeros(2, 3), (2, 4), torch.float32))
+        api._expect("x", ("q", torch.zeros(2, 3), (2, 4), torch.float32))
     with pytest.raises(ValueError):
-        api._expect("x", q=(torch.zeros(2, 4), (2, 4), torch.bfloat16))
+        api._expect("x", ("q", torch.zeros(2, 4), (2, 4), torch.bfloat16))
+    api._expect("x", ("q", None, (2, 4), torch.float32), ("k", torch.zeros(2, 4), (2, 4), torch.float32))
+
+
+def test_binding_refuses_other_devices_and_strided_buffers(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     with pytest.raises(ValueError):
-        api._expect("x", q=(torch.zeros(4, 2).t(), (2, 4), torch.float32))
-    api._expect("x", q=(None, (2, 4), torch.float32))
+        api._addresses("x", (torch.zeros(2),))           # host memory
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)   # a CPU tensor's device number
+    assert api._addresses("x", (None, torch.zeros(0))) == [0, 0]
+    with pytest.raises(ValueError):
+        api._addresses("x", (torch.zeros(2, 4).t(),))
+    with pytest.raises(ValueError):
+        api._rope_views(api.RopeDesc(1, 4, 2, 1, 64), (torch.zeros(1, 2, 4, 64), None, None), "x", 0)
