@@ -17,23 +17,25 @@ namespace sepllm {
 namespace {
 
 constexpr int kPfxThreads = 384;
-constexpr int kMaxPairs = 2048;   // pairs of row tiles per launch (their lengths sit in shared memory)
+constexpr int kMaxPairs = 128;    // pairs of row tiles per launch (their lengths sit in shared memory)
 
 template <int D>
 struct PfxCfg {
   static constexpr int NB = D / 64;               // 64-column blocks per row
-  static constexpr int NST = (D == 128) ? 2 : 4;  // K and V ring depth
+  static constexpr int NST = (D == 128) ? 3 : 8;  // ring of K and V tiles
   static constexpr uint32_t kTile = NB * kTileBlockBytes;
-  static constexpr uint32_t kQ = 0;
-  static constexpr uint32_t kK = kQ + 2 * kTile;
-  static constexpr uint32_t kV = kK + NST * kTile;
-  static constexpr uint32_t kTab = kV + NST * kTile;
+  static constexpr uint32_t kPTile = 2 * kTileBlockBytes;   // 128 rows x 128 keys
+  static constexpr uint32_t kQ = 0;                         // 2 slots
+  static constexpr uint32_t kP = kQ + 2 * kTile;            // 2 slots
+  static constexpr uint32_t kKV = kP + 2 * kPTile;
+  static constexpr uint32_t kTab = kKV + NST * kTile;
   static constexpr uint32_t kBar = kTab + kMaxPairs * 8;
   static constexpr uint32_t kTotal = kBar + 1024;
   static constexpr uint32_t kRequest = kTotal + 1024;
   static constexpr uint32_t kS0 = 0, kS1 = 128, kO0 = 256, kO1 = 256 + D;  // tensor-memory columns
 };
-static_assert(PfxCfg<128>::kRequest <= 227 * 1024 && PfxCfg<64>::kRequest > 114 * 1024,
+static_assert(PfxCfg<128>::kRequest <= 227 * 1024 && PfxCfg<64>::kRequest <= 227 * 1024 &&
+                  PfxCfg<64>::kRequest > 114 * 1024,
               "one CTA per SM owns all 512 tensor-memory columns");
 
 // Row tile i holds rows (b, t, g) of one kv head: bt sequences x tt tokens x gt heads of the group,
@@ -112,8 +114,11 @@ __device__ __forceinline__ bool ends_inside(const Segment* sg, int P) {
 //   alternate mode   (one row tile in all) both slots hold that tile and take the key tiles in turn,
 //                    so that one slot's softmax runs under the other's loads and products; each
 //                    slot leaves a partial result of its own
-// Warps as in the forward kernel: 0 TMA, 1 MMA issue, 2 clears V rows behind the prefix, 4-7 and
-// 8-11 softmax of slot 0 and 1, one thread per row; P goes back to tensor memory as bf16 over S.
+// Warps: 0 TMA; 1 and 2 MMA issue of slot 0 and 1; 3 clears V rows behind the prefix; 4-7 and 8-11
+// softmax of slot 0 and 1, one thread per row.  P goes to shared memory as bf16: S is free as soon as
+// it is in registers, so S of the slot's next key tile is issued at once and the softmax threads go
+// from tile to tile without waiting for the tensor pipe.  K and V tiles share one ring in the order in
+// which they are used: K0, K1, V0, K2, V1, ...
 template <int D>
 __global__ void __launch_bounds__(kPfxThreads, 1)
 prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
@@ -124,23 +129,23 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
   uint8_t* sQ = smem + C::kQ;
-  uint8_t* sK = smem + C::kK;
-  uint8_t* sV = smem + C::kV;
+  uint8_t* sP = smem + C::kP;
+  uint8_t* sKV = smem + C::kKV;
   int2* tab = reinterpret_cast<int2*>(smem + C::kTab);   // [pairs] longest prefix of each row tile
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBar);
   uint64_t* bar_q = bars;          // [2]   Q of slot x landed
-  uint64_t* bar_s = bars + 2;      // [2]   S_x complete (and every earlier MMA)
-  uint64_t* bar_p = bars + 4;      // [2]   P_x written by the 4 softmax warps of slot x
-  uint64_t* bar_o = bars + 6;      //       every MMA of the segment complete
-  uint64_t* bar_z = bars + 7;      //       V rows behind the prefix cleared
-  uint64_t* bar_g = bars + 8;      //       V of the last tile landed: clear the rows behind the prefix
-  uint64_t* bar_qe = bars + 9;     //       Q of the segment read for the last time
-  uint64_t* bar_e = bars + 10;     //       O of the segment read by the 8 softmax warps
-  uint64_t* bar_kf = bars + 11;    // [NST] K stage full
-  uint64_t* bar_ke = bar_kf + NST; // [NST] K stage free
-  uint64_t* bar_vf = bar_ke + NST; // [NST]
-  uint64_t* bar_ve = bar_vf + NST; // [NST]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 11 + 4 * NST);
+  uint64_t* bar_qe = bars + 2;     // [2]   slot x has read the segment's Q for the last time
+  uint64_t* bar_s = bars + 4;      // [2]   S_x complete
+  uint64_t* bar_sl = bars + 6;     // [2]   S_x read into registers by the 4 softmax warps
+  uint64_t* bar_p = bars + 8;      // [2]   P_x written
+  uint64_t* bar_pv = bars + 10;    // [2]   P_x V complete: P_x may be rewritten, O_x is at rest
+  uint64_t* bar_g = bars + 12;     //       V of the last tile landed: clear the rows behind the prefix
+  uint64_t* bar_z = bars + 13;     //       they are cleared
+  uint64_t* bar_d = bars + 14;     // [2]   every product and arrival of slot x done
+  uint64_t* bar_t = bars + 16;     // [2]   slot x may run its exponentials
+  uint64_t* bar_f = bars + 18;     // [NST] ring stage full
+  uint64_t* bar_r = bar_f + NST;   // [NST] ring stage free (both slots)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 18 + 2 * NST);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
   int* s_warp = reinterpret_cast<int*>(tmem_slot + 4);   // [12] key tiles per warp of the scan
   int* s_start = s_warp + 12;                            // [2] pair and offset where the run starts
@@ -152,15 +157,14 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   const int rows = p.gt * p.tt * p.bt;
 
   if (tid == 0) {
-    for (int i = 0; i < 2; ++i) { mbar_init(bar_q + i, 1); mbar_init(bar_s + i, 1); mbar_init(bar_p + i, 4); }
-    mbar_init(bar_o, 1);
-    mbar_init(bar_z, 1);
-    mbar_init(bar_g, 1);
-    mbar_init(bar_qe, 1);
-    mbar_init(bar_e, 8);
-    for (int i = 0; i < NST; ++i) {
-      mbar_init(bar_kf + i, 1); mbar_init(bar_ke + i, 1); mbar_init(bar_vf + i, 1); mbar_init(bar_ve + i, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_q + i, 1); mbar_init(bar_qe + i, 1); mbar_init(bar_s + i, 1);
+      mbar_init(bar_sl + i, 4); mbar_init(bar_p + i, 4); mbar_init(bar_pv + i, 1);
+      mbar_init(bar_d + i, 1); mbar_init(bar_t + i, 4);
     }
+    mbar_init(bar_g, 1);
+    mbar_init(bar_z, 1);
+    for (int i = 0; i < NST; ++i) { mbar_init(bar_f + i, 1); mbar_init(bar_r + i, 2); }
     *abort_flag = 0;
     fence_mbar_init();
     tma_prefetch_desc(&mapQ); tma_prefetch_desc(&mapK); tma_prefetch_desc(&mapV);
@@ -254,19 +258,26 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    // place of K(j) and V(j) of a segment of n key tiles in the order of the loads
+    auto k_place = [](int j) { return j == 0 ? 0 : 2 * j - 1; };
+    auto v_place = [](int j, int n) { return j < n - 1 ? 2 * j + 2 : 2 * n - 1; };
     if (warp == 0 && lane == 0) {
       // ---------------- TMA producer ----------------
-      int it = 0;  // key tiles loaded
+      int at = 0;  // tiles loaded
       for (int n = 0; next_segment<false>(sg, tab, p.pairs); ++n) {
         const int hk = sg->hk, j0 = sg->j0, n_tiles = sg->j1 - j0;
-        for (int j = 0; j < n_tiles; ++j, ++it) {
-          const int st = it % NST, use = it / NST, y = (j0 + j) * kBN;
-          if (use > 0) wait(bar_ke + st, (use - 1) & 1);
-          mbar_expect_tx(bar_kf + st, C::kTile);
+        for (int i = 0; i < 2 * n_tiles; ++i, ++at) {
+          // 0: K(0), odd: K((i + 1) / 2), even: V(i / 2 - 1), and the last one V(n - 1)
+          const bool is_v = i == 2 * n_tiles - 1 || (i > 0 && i % 2 == 0);
+          const int j = is_v ? (i % 2 ? n_tiles - 1 : i / 2 - 1) : (i + 1) / 2;
+          const int st = at % NST, use = at / NST;
+          if (use > 0) wait(bar_r + st, (use - 1) & 1);
+          mbar_expect_tx(bar_f + st, C::kTile);
           for (int nb = 0; nb < NB; ++nb)
-            tma_load_3d(sK + st * C::kTile + nb * kTileBlockBytes, &mapK, bar_kf + st, nb * 64, y, hk);
-          if (j == 0) {
-            if (n > 0) wait(bar_qe, (n - 1) & 1);
+            tma_load_3d(sKV + st * C::kTile + nb * kTileBlockBytes, is_v ? &mapV : &mapK, bar_f + st, nb * 64,
+                        (j0 + j) * kBN, hk);
+          if (i == 0) {
+            if (n > 0) { wait(bar_qe, (n - 1) & 1); wait(bar_qe + 1, (n - 1) & 1); }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               if (alt ? x == 1 : slot_tiles(sg, false, x) == 0) continue;   // a slot without work loads nothing
@@ -277,93 +288,103 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
                             hk, rt.b0);
             }
           }
-          if (use > 0) wait(bar_ve + st, (use - 1) & 1);
-          mbar_expect_tx(bar_vf + st, C::kTile);
-          for (int nb = 0; nb < NB; ++nb)
-            tma_load_3d(sV + st * C::kTile + nb * kTileBlockBytes, &mapV, bar_vf + st, nb * 64, y, hk);
         }
       }
-    } else if (warp == 1 && lane == 0) {
-      // ---------------- MMA issuer ----------------
+    } else if ((warp == 1 || warp == 2) && lane == 0) {
+      // ---------------- MMA issuers: one thread per slot ----------------
+      // A slot's products go in its own order: S(j+1) as soon as S(j) has been read, P V(j) as soon as
+      // P(j) is written.  A stage of the ring is free when both slots are through with it; a slot that
+      // does not use a tile lets it go as soon as it has landed.
+      const int x = warp - 1, qx = alt ? 0 : x;
       constexpr uint32_t idesc_s = make_idesc_bf16(128, 128, 0, 0);
       constexpr uint32_t idesc_o = make_idesc_bf16(128, D, 0, 1);
-      const uint32_t q_lo0 = desc_lo(smem_u32(sQ), 16);
-      const uint32_t k_lo0 = desc_lo(smem_u32(sK), 16);
-      const uint32_t v_lo0 = desc_lo(smem_u32(sV), kTileBlockBytes);
-      // per slot one bit each (a slot number known only at run time would put arrays in memory)
-      uint32_t ph_p = 0, ph_q = 0;   // phase of P_x / Q_x
-      uint32_t ph_z = 0;
-      int it0 = 0;                   // key tiles of earlier segments
+      const uint32_t q_lo = desc_lo(smem_u32(sQ + qx * C::kTile), 16);
+      const uint32_t p_lo = desc_lo(smem_u32(sP + x * C::kPTile), 16);
+      const uint32_t k_lo0 = desc_lo(smem_u32(sKV), 16), v_lo0 = desc_lo(smem_u32(sKV), kTileBlockBytes);
+      const uint32_t tS = tmem + (x ? C::kS1 : C::kS0), tO = tmem + (x ? C::kO1 : C::kO0);
+      uint32_t ph_sl = 0, ph_p = 0, ph_q = 0, ph_z = 0;   // phases
+      int at0 = 0;                                        // tiles loaded for earlier segments
       for (int n = 0; next_segment<false>(sg, tab, p.pairs); ++n) {
-        const int n_tiles = sg->j1 - sg->j0;
-        const int n_mine0 = slot_tiles(sg, alt, 0), n_mine1 = slot_tiles(sg, alt, 1);
+        const int n_tiles = sg->j1 - sg->j0, n_mine = slot_tiles(sg, alt, x);
         const bool clear_v = ends_inside(sg, p.P);
-        uint32_t q_seen = 0, o_begun = 0;
-        bool k_waited, v_waited, o_free = n == 0;
-        auto scores = [&](int x, int j) {   // S_x = Q_x K(j)^T
-          const int it = it0 + j, st = it % NST, qx = alt ? 0 : x;
-          if (!(q_seen >> qx & 1)) {
-            wait(bar_q + qx, ph_q >> qx & 1);
-            ph_q ^= 1u << qx;
-            q_seen |= 1u << qx;
+        // the slot that uses the last tile (the first such one) has its V cleared
+        const bool clears = clear_v && (alt ? ((n_tiles - 1) & 1) == x
+                                            : n_mine == n_tiles && (x == 0 || slot_tiles(sg, false, 0) < n_tiles));
+        auto mine = [&](int j) { return alt ? (j & 1) == x : j < n_mine; };
+        int left_s = n_mine;      // S products still to issue
+        bool s_out = false;       // an S product has been issued in this segment
+        auto scores = [&](int j) {
+          const int at = at0 + k_place(j), st = at % NST;
+          if (mine(j)) {
+            if (!s_out) { wait(bar_q + qx, ph_q); ph_q ^= 1; }
+            else { wait(bar_sl + x, ph_sl); ph_sl ^= 1; }
+            s_out = true;
           }
-          if (!k_waited) { wait(bar_kf + st, (it / NST) & 1); k_waited = true; }
-          const uint32_t tS = tmem + C::kS0 + x * (C::kS1 - C::kS0), k_lo = k_lo0 + st * (C::kTile >> 4);
-          const uint32_t q_lo = q_lo0 + qx * (C::kTile >> 4);
+          wait(bar_f + st, (at / NST) & 1);
+          if (!mine(j)) { mbar_arrive(bar_r + st); return; }
+          tc_fence_after();
+          const uint32_t k_lo = k_lo0 + st * (C::kTile >> 4);
 #pragma unroll
           for (int k = 0; k < D / 16; ++k)
             umma_ss_lo(tS, q_lo + kmajor_step(k, kTileBlockBytes), k_lo + kmajor_step(k, kTileBlockBytes),
                        idesc_s, k > 0);
           tc_commit(bar_s + x);
+          tc_commit(bar_r + st);
+          if (--left_s == 0) tc_commit(bar_qe + x);
         };
-        auto values = [&](int x, int j) {   // O_x += P_x V(j)
-          const int it = it0 + j, st = it % NST;
-          wait(bar_p + x, ph_p >> x & 1);
-          ph_p ^= 1u << x;
-          if (!v_waited) {
-            wait(bar_vf + st, (it / NST) & 1);
-            if (clear_v && j == n_tiles - 1) { mbar_arrive(bar_g); wait(bar_z, ph_z); ph_z ^= 1; }
-            v_waited = true;
+        bool o_begun = false;
+        auto values = [&](int j) {
+          const int at = at0 + v_place(j, n_tiles), st = at % NST;
+          if (mine(j)) { wait(bar_p + x, ph_p); ph_p ^= 1; }
+          wait(bar_f + st, (at / NST) & 1);
+          if (clear_v && j == n_tiles - 1) {
+            if (clears) mbar_arrive(bar_g);
+            if (mine(j)) wait(bar_z, ph_z);
           }
-          if (!o_free) { wait(bar_e, (n - 1) & 1); o_free = true; }
+          if (!mine(j)) { mbar_arrive(bar_r + st); return; }
           tc_fence_after();
-          const uint32_t tS = tmem + C::kS0 + x * (C::kS1 - C::kS0), tO = tmem + C::kO0 + x * (C::kO1 - C::kO0);
           const uint32_t v_lo = v_lo0 + st * (C::kTile >> 4);
-          umma_ts_lo(tO, tS, v_lo, idesc_o, o_begun >> x & 1);
-          o_begun |= 1u << x;
+          umma_ss_lo(tO, p_lo, v_lo, idesc_o, o_begun);
+          o_begun = true;
 #pragma unroll
           for (int k = 1; k < kBN / 16; ++k)
-            umma_ts_lo(tO, tS + k * 8, v_lo + mnmajor_step(k), idesc_o, 1);
+            umma_ss_lo(tO, p_lo + kmajor_step(k, kTileBlockBytes), v_lo + mnmajor_step(k), idesc_o, 1);
+          tc_commit(bar_r + st);
+          tc_commit(bar_pv + x);
         };
-        for (int s = 0; s <= n_tiles; ++s) {
-          k_waited = v_waited = false;
-          if (alt) {   // the slots never share a step: the next scores go first
-            if (s < n_tiles) scores(s & 1, s);
-            if (s >= 1) values((s - 1) & 1, s - 1);
-          } else {
-            if (s >= 1 && s <= n_mine0) values(0, s - 1);
-            if (s < n_mine0) scores(0, s);
-            if (s >= 1 && s <= n_mine1) values(1, s - 1);
-            if (s < n_mine1) scores(1, s);
-          }
-          if (s < n_tiles) tc_commit(bar_ke + (it0 + s) % NST);
-          if (s == n_tiles - 1) tc_commit(bar_qe);
-          if (s >= 1) tc_commit(bar_ve + (it0 + s - 1) % NST);
+        scores(0);
+        for (int j = 0; j < n_tiles; ++j) {
+          if (j + 1 < n_tiles) scores(j + 1);
+          values(j);
         }
-        tc_commit(bar_o);
-        it0 += n_tiles;
+        if (n_mine > 0) {
+          // the last S has no successor that waits for its reading: catch up with that phase
+          wait(bar_sl + x, ph_sl);
+          ph_sl ^= 1;
+        } else {
+          if (alt) { wait(bar_q, ph_q); ph_q ^= 1; }   // the other slot's load, for the same reason
+          // (at the end, when the producer is past its wait for the segment before)
+          mbar_arrive(bar_qe + x);
+        }
+        if (clear_v) ph_z ^= 1;
+        at0 += 2 * n_tiles;
       }
-    } else if (warp == 2) {
+      // no arrival may be under way when the CTA ends
+      tc_commit(bar_d + x);
+      wait(bar_d + x, 0);
+    } else if (warp == 3) {
       // ---------------- V rows behind the longest prefix ----------------
-      int n_clear = 0, it0 = 0;
+      int n_clear = 0, at0 = 0;
       while (next_segment<true>(sg, tab, p.pairs)) {
-        it0 += sg->j1 - sg->j0;
+        const int n_tiles = sg->j1 - sg->j0;
+        const int st = (at0 + v_place(n_tiles - 1, n_tiles)) % NST;
+        at0 += 2 * n_tiles;
         if (!ends_inside(sg, p.P)) continue;
-        const int st = (it0 - 1) % NST, r0 = max(sg->len[0], sg->len[1]) - (sg->j1 - 1) * kBN;
+        const int r0 = max(sg->len[0], sg->len[1]) - (sg->j1 - 1) * kBN;
         wait(bar_g, n_clear++ & 1);
         for (int i = lane; i < (kBN - r0) * 8 * NB; i += 32) {
           const int ch = i & 7, blk = (i >> 3) % NB, r = r0 + (i >> 3) / NB;
-          *reinterpret_cast<uint4*>(sV + st * C::kTile + blk * kTileBlockBytes + r * 128 + ch * 16) =
+          *reinterpret_cast<uint4*>(sKV + st * C::kTile + blk * kTileBlockBytes + r * 128 + ch * 16) =
               make_uint4(0, 0, 0, 0);
         }
         fence_proxy_async_smem();
@@ -378,7 +399,9 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     const uint32_t lane_base = uint32_t((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + lane_base + (x ? C::kS1 : C::kS0);
     const uint32_t tO = tmem + lane_base + (x ? C::kO1 : C::kO0);
+    uint8_t* sPx = sP + x * C::kPTile;
     int n_s = 0;              // S tiles taken
+    uint32_t ph_t = 0;        // phase of bar_t
     int cut = -1;
     for (int n = 0; next_segment<true>(sg, tab, p.pairs); ++n) {
       // the row: sequence b, token t, head g of the group
@@ -388,7 +411,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         b = rt.b0 + r / (p.gt * p.tt); t = rt.t0 + r / p.gt % p.tt; g = rt.g0 + r % p.gt;
         return ti < p.m_tiles && r < rows && b < p.B && t < p.T && g < p.G && !(p.seq_len && t >= p.seq_len[b]);
       };
-      const int n_mine = slot_tiles(sg, alt, x);
+      const int n_mine = slot_tiles(sg, alt, x), n_both = min(n_mine, slot_tiles(sg, alt, x ^ 1));
       int c_hi = sg->len[alt ? 0 : x];   // keys of the next tile, and behind it, that the row sees
       {
         int b, t, g;
@@ -404,6 +427,8 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, sreg[c]);
         tmem_ld_wait();
+        tc_fence_before();
+        mbar_arrive_warp(bar_sl + x);   // S_x may be overwritten by the next key tile's scores
         if (c_hi < kBN) {
 #pragma unroll
           for (int c = 0; c < 4; ++c)
@@ -435,45 +460,59 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         }
         // P = 2^(S * scale - m_ref), rounded to bf16 for the second product (its operand type); the
         // row sum takes the unrounded values
+        // The slots take turns at this block: side by side they halve each other's rate at the
+        // special-function unit (16 a clock and SM), in turn one slot's exponentials run under the
+        // other's loads, maxima and stores.
+        if (x == 1 ? j < n_both : j > 0 && j < n_both) { wait(bar_t + x, ph_t); ph_t ^= 1; }
         const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
         const unsigned long long scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
         const unsigned long long negm2 = pack_f32x2(neg_m, neg_m);
         unsigned long long ps2[4] = {0ull, 0ull, 0ull, 0ull};
-        // P goes over the first 64 columns of S_x, column c holding keys 2c, 2c+1, sixteen columns as soon
-        // as they are ready (S is in registers)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t pk[16];
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
             const float2 a = unpack_f32x2(fma_f32x2(
                 pack_f32x2(__uint_as_float(sreg[c][e]), __uint_as_float(sreg[c][e + 1])), scale2, negm2));
             const float p0 = ex2(a.x), p1 = ex2(a.y);
             ps2[(e >> 1) & 3] = add_f32x2(ps2[(e >> 1) & 3], pack_f32x2(p0, p1));
-            pk[e >> 1] = pack_bf16(p0, p1);
+            sreg[c][e >> 1] = pack_bf16(p0, p1);
           }
-          tmem_st16(tS + c * 16, pk);
-        }
         const float2 sm = unpack_f32x2(add_f32x2(add_f32x2(ps2[0], ps2[1]), add_f32x2(ps2[2], ps2[3])));
+        if (x == 0 ? j < n_both : j + 1 < n_both) mbar_arrive_warp(bar_t + (x ^ 1));
         l_sum = l_sum * corr + (sm.x + sm.y);
-        // S_x of this tile complete means P V of the slot's previous tile is: O_x is at rest
-        if (j > 0 && __any_sync(0xffffffffu, rescale)) {
-          uint32_t oreg[32];
+        // P V of the slot's previous tile is complete: the buffer of P is free and O_x is at rest
+        if (j > 0) {
+          wait(bar_pv + x, (n_s - 2) & 1);
+          if (__any_sync(0xffffffffu, rescale)) {
+            tc_fence_after();
+            uint32_t oreg[32];
 #pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            tmem_ld32(tO + c * 32, oreg);
-            tmem_ld_wait();
+            for (int c = 0; c < D / 32; ++c) {
+              tmem_ld32(tO + c * 32, oreg);
+              tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 32; ++e) oreg[e] = __float_as_uint(__uint_as_float(oreg[e]) * corr);
-            tmem_st32(tO + c * 32, oreg);
+              for (int e = 0; e < 32; ++e) oreg[e] = __float_as_uint(__uint_as_float(oreg[e]) * corr);
+              tmem_st32(tO + c * 32, oreg);
+            }
+            tmem_st_wait();
+            tc_fence_before();
           }
         }
-        tmem_st_wait();
-        tc_fence_before();
+        // row r of P: 16 pieces of 8 keys, piece q in block q / 8 at swizzled place q % 8
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int q = 4 * c + i;
+            *reinterpret_cast<uint4*>(sPx + (q >> 3) * kTileBlockBytes + swz128(uint32_t(r), uint32_t(q & 7))) =
+                make_uint4(sreg[c][4 * i], sreg[c][4 * i + 1], sreg[c][4 * i + 2], sreg[c][4 * i + 3]);
+          }
+        fence_proxy_async_smem();
         mbar_arrive_warp(bar_p + x);
       }
 
-      wait(bar_o, n & 1);   // also by a slot without work, which would lose count of the phases
+      if (n_mine > 0) wait(bar_pv + x, (n_s - 1) & 1);
       tc_fence_after();
       int b, t, g;
       const bool store = place(b, t, g);
@@ -535,8 +574,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
           }
         }
       }
-      tc_fence_before();
-      mbar_arrive_warp(bar_e);
+      tc_fence_before();   // O_x is read: the next segment's first product into it waits for P of this thread
       // where the unit's parts are, from the CTA that has its first key tile
       if (sg->j0 == 0 && tid == 128) {
         // number of the unit's last key tile, and the CTA that has it
