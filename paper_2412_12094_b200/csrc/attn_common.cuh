@@ -1,5 +1,7 @@
 // Declarations shared by the attention translation units.
 #pragma once
+#include <functional>
+
 #include "common.cuh"
 
 namespace sepllm {
@@ -116,7 +118,8 @@ struct FwdParams {
   const int32_t* doc_start;  // [B][L]   (packed index only)
   const int32_t* doc_end;    // [B][L]
   __nv_bfloat16* O;
-  float* O32;                // the F32 kernels write rows of D floats here instead of O
+  float* O32;                // the F32 kernels write [B][Hq][T][D / 4][128 rows][4] here instead of O:
+                             // neighbouring rows (threads) next to each other
   float* LSE;
   int32_t* status;
   int L, T, Hq, Hkv, n_neighbor, side_cap, side_tiles_cap, pair_heads;
@@ -159,7 +162,7 @@ sepllm_status launch_fwd_pair(const sepllm_attn_desc* d, const FwdParams& p, int
                               const CUtensorMap& mks64, const CUtensorMap& mvs, cudaStream_t stream);
 
 // The forward with its output left in 32 bits, to be joined with another part: O32
-// [B][Hq][L][kernel_head_dim(d)].  Arguments as sepllm_attn_fwd, checked by the caller.
+// [B][Hq][ceil(L / 128)][D / 4][128][4], D = kernel_head_dim(d).  Arguments as sepllm_attn_fwd, checked by the caller.
 sepllm_status attn_fwd_f32(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc, const void* Q,
                            const void* K, const void* V, const void* index, float* O32, float* LSE,
                            void* workspace, cudaStream_t stream);
@@ -197,26 +200,29 @@ struct PrefixParams {
   int whole_parts;              // 1: units that one CTA walks in full leave a part too
   int pair_base, pairs;         // pairs of row tiles of this launch
   int max_ctas;
+  int reset_status;             // 1: the kernel starts the call (a decode) and resets its status word
   float scale_log2;
   const int32_t* prefix_len;    // [B] or null (P for all)
   const int32_t* seq_len;       // [B] or null: rows of tokens behind it are not written
   float* part_ml;               // [part][slot][128] (reference exponent, sum)
-  float* part_acc;              // [part][slot][128][D]
+  float* part_acc;              // [part][slot][D / 4][128 rows][4]
   int4* unit_parts;             // [Hkv][pairs] (parts, first part, CTA of the first part)
   int32_t* cut_units;           // [CTA] the unit whose first key tiles, not all, were the CTA's; -1: none
-  const float* own_O;           // [row][D] the row's own part, normalised, and its log-sum-exp [row]
-  const float* own_lse;
+  const float* own_O;           // the rows' own part, normalised (layout of FwdParams::O32), and its
+  const float* own_lse;         // log-sum-exp [row]
   __nv_bfloat16* O;             // [row][d], rows [B][Hkv][G][T]
   float* LSE;
   int32_t* status;
 };
 // Sizes and tiles (false: too large).
-bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, bool whole_parts);
+// own_us: time of the rows' own part where it runs beside the prefix kernel, 0 where it does not.
+bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, bool whole_parts, double own_us);
 size_t prefix_part_bytes(const PrefixParams& p);
 void place_prefix_parts(PrefixParams* p, uint8_t* ws);
-// The prefix part and the join with the rows' own parts: own_parts of the decode kernel, or
-// (own_parts = 0) p.own_O and p.own_lse.
-sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const void* Vp, const float* own_ml,
-                            const float* own_acc, int own_parts, cudaStream_t stream);
+// The prefix part and the join with the rows' own parts: own_parts of the decode kernel, launched by
+// `beside` once the (first) prefix kernel is, or (own_parts = 0) p.own_O and p.own_lse.
+sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const void* Vp, cudaStream_t stream,
+                            const std::function<sepllm_status()>& beside, const float* own_ml,
+                            const float* own_acc, int own_parts);
 
 }  // namespace sepllm

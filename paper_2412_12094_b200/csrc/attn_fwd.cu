@@ -110,7 +110,7 @@ struct FwdCfg {
 
 constexpr int kFwdThreads = 384;
 
-// F32: the output stays in 32 bits (rows of D floats) for a caller that joins it with another part.
+// F32: the output stays in 32 bits for a caller that joins it with another part (layout: FwdParams).
 template <int D, bool F32>
 __global__ void __launch_bounds__(kFwdThreads, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
@@ -418,11 +418,10 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         tmem_ld32(tO + c * 32, oreg);
         tmem_ld_wait();
         if (F32) {
-          if (row < p.L)
 #pragma unroll
-            for (int q8 = 0; q8 < 8; ++q8)
-              *reinterpret_cast<float4*>(p.O32 + (size_t(q_plane) * p.L + row) * D + c * 32 + q8 * 4) =
-                  make_float4(__uint_as_float(oreg[4 * q8]) * inv_l, __uint_as_float(oreg[4 * q8 + 1]) * inv_l,
+          for (int q8 = 0; q8 < 8; ++q8)
+            reinterpret_cast<float4*>(p.O32)[((size_t(q_plane) * p.T + t) * (D / 4) + c * 8 + q8) * kBM + r] =
+                make_float4(__uint_as_float(oreg[4 * q8]) * inv_l, __uint_as_float(oreg[4 * q8 + 1]) * inv_l,
                               __uint_as_float(oreg[4 * q8 + 2]) * inv_l, __uint_as_float(oreg[4 * q8 + 3]) * inv_l);
         } else if (row < p.L) {
 #pragma unroll

@@ -401,11 +401,10 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
       tmem_ld32(tO + c * 32, oreg);
       tmem_ld_wait();
       if (F32) {
-        if (row < p.L)
 #pragma unroll
-          for (int q8 = 0; q8 < 8; ++q8)
-            *reinterpret_cast<float4*>(p.O32 + (size_t(q_plane) * p.L + row) * kD + c * 32 + q8 * 4) =
-                make_float4(__uint_as_float(oreg[4 * q8]) * inv_l, __uint_as_float(oreg[4 * q8 + 1]) * inv_l,
+        for (int q8 = 0; q8 < 8; ++q8)
+          reinterpret_cast<float4*>(p.O32)[((size_t(q_plane) * p.T + t) * (kD / 4) + c * 8 + q8) * kBM + r] =
+              make_float4(__uint_as_float(oreg[4 * q8]) * inv_l, __uint_as_float(oreg[4 * q8 + 1]) * inv_l,
                             __uint_as_float(oreg[4 * q8 + 2]) * inv_l, __uint_as_float(oreg[4 * q8 + 3]) * inv_l);
       } else if (row < p.L) {
 #pragma unroll

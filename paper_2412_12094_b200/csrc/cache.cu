@@ -540,6 +540,10 @@ constexpr int decode_smem_bytes() {
 // WIDE: groups of 9 to 16 query heads per kv head use both row halves of the MMA tile (a lane
 // then carries the softmax state of rows frow and frow + 8); narrower groups leave the upper
 // half zero and skip its arithmetic.
+//
+// status null: the kernel runs beside the prefix kernel launched before it (which writes the status
+// word) and shares no memory with it; its last CTA ends only when that kernel has, so that what is
+// launched next finds both complete.
 template <int D, bool ROPE, bool WIDE>
 __global__ void __launch_bounds__(kDecThreads, 3)   // three CTAs per SM: at most 168 registers
 decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __restrict__ q_in,
@@ -559,7 +563,7 @@ decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __res
   const int G = d.Hq / d.Hkv;
   const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  if (tid == 0 && (split | hk | b) == 0) *status = SEPLLM_OK;
+  if (status && tid == 0 && (split | hk | b) == 0) *status = SEPLLM_OK;
   CacheView cv = cache_view(const_cast<uint8_t*>(state), h);
   const sepllm_cache_seq sq = cv.seq[b];
   const int size_run = sq.size_init + sq.size_sep + sq.size_win;
@@ -750,6 +754,8 @@ decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __res
     part_acc[uo * D + e] = aa;
     if (e == 0) { part_ml[uo * 2] = mm; part_ml[uo * 2 + 1] = ll; }
   }
+  if (!status && split == int(gridDim.x) - 1 && hk == int(gridDim.y) - 1 && b == int(gridDim.z) - 1)
+    wait_for_prior();
 }
 
 // grid (Hq, B), D threads.
@@ -947,10 +953,16 @@ static sepllm_status launch_decode(const sepllm_cache_header& h, float scale_log
   static_assert(smem >= (kDecThreads / 32) * 16 * (8 + D * 4), "partials fit in the stage buffers");
   SEPLLM_CUDA_TRY(cudaFuncSetAttribute(decode_split<D, ROPE, WIDE>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  decode_split<D, ROPE, WIDE><<<dim3(splits, h.desc.Hkv, h.desc.B), kDecThreads, smem, stream>>>(
-      h, scale_log2, static_cast<const __nv_bfloat16*>(q), static_cast<const uint8_t*>(state),
-      static_cast<const __nv_bfloat16*>(Kc), static_cast<const __nv_bfloat16*>(Vc), ml, acc, splits,
-      rope, status);
+  const dim3 grid(splits, h.desc.Hkv, h.desc.B);
+  auto qb = static_cast<const __nv_bfloat16*>(q), kb = static_cast<const __nv_bfloat16*>(Kc),
+       vb = static_cast<const __nv_bfloat16*>(Vc);
+  auto sb = static_cast<const uint8_t*>(state);
+  if (status)
+    decode_split<D, ROPE, WIDE><<<grid, kDecThreads, smem, stream>>>(h, scale_log2, qb, sb, kb, vb, ml, acc, splits,
+                                                                     rope, status);
+  else
+    SEPLLM_CUDA_TRY(launch_overlapped(decode_split<D, ROPE, WIDE>, grid, kDecThreads, smem, stream, h, scale_log2,
+                                      qb, sb, kb, vb, ml, acc, splits, rope, status));
   return SEPLLM_OK;
 }
 
@@ -1051,6 +1063,14 @@ extern "C" sepllm_status sepllm_decode_rope(const sepllm_cache_desc* desc, float
 // ---------------------------------------------------------------------------
 // Decode behind a shared prefix
 // ---------------------------------------------------------------------------
+// Microseconds that the own part takes alone: its bytes at 6.2 TB/s, with the long-run mean of
+// Size_run (Eq. 4; with a fixed window the separators are taken half full).
+static double own_part_us(const sepllm_cache_desc* d) {
+  const double run = (d->flags & SEPLLM_CACHE_FIXED_WINDOW) ? d->a + 0.5 * d->s + d->w
+                                                            : 0.5 * (double(d->a) + d->s + d->w + d->c);
+  return double(d->B) * d->Hkv * run * d->d * 4 / 6.2e6;
+}
+
 extern "C" sepllm_status sepllm_decode_prefix_workspace_bytes(const sepllm_cache_desc* desc, int32_t P,
                                                               size_t* bytes) {
   sepllm_cache_header h;
@@ -1058,7 +1078,7 @@ extern "C" sepllm_status sepllm_decode_prefix_workspace_bytes(const sepllm_cache
   if (st != SEPLLM_OK) return st;
   if (P < 1) return SEPLLM_INVALID_ARG;
   PrefixParams p{};
-  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P, true)) return SEPLLM_UNSUPPORTED;
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P, true, own_part_us(desc))) return SEPLLM_UNSUPPORTED;
   if (bytes) *bytes = kAlign + own_part_bytes(desc, decode_splits(desc)) + prefix_part_bytes(p);
   return SEPLLM_OK;
 }
@@ -1077,7 +1097,7 @@ extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int
     return SEPLLM_INVALID_ARG;
   if (desc->B > 65535 || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
   PrefixParams p{};
-  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P, true)) return SEPLLM_UNSUPPORTED;
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P, true, own_part_us(desc))) return SEPLLM_UNSUPPORTED;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const int own_parts = decode_splits(desc);
@@ -1090,10 +1110,12 @@ extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int
   p.LSE = lse;
   p.status = reinterpret_cast<int32_t*>(ws);
   p.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
-  // (the own part goes first: it writes the status word that the prefix kernel may set)
-  st = launch_own_parts(h, scale, q, state, Kc, Vc, nullptr, own_parts, ml, acc, p.status, stream);
-  if (st != SEPLLM_OK) return st;
-  return launch_prefix(p, q, Kp, Vp, ml, acc, own_parts, stream);
+  // The prefix kernel (tensor cores, one CTA per SM on some of the SMs) and the own part (HBM) run side by
+  // side: the second is let in while the first runs.
+  st = launch_prefix(p, q, Kp, Vp, stream, [&]() {
+    return launch_own_parts(h, scale, q, state, Kc, Vc, nullptr, own_parts, ml, acc, nullptr, stream);
+  }, ml, acc, own_parts);
+  return st;
 }
 
 // grid (row blocks, Hkv).  Row v of the prefix is retained entry v of the (only) sequence.

@@ -9,6 +9,7 @@
 // are the rows of one matrix product, 128 to a tile, so the prefix is read once per 256 rows instead
 // of once per sequence.
 #include <algorithm>
+#include <cmath>
 
 #include "attn_common.cuh"
 
@@ -61,6 +62,13 @@ __device__ __forceinline__ int seen_length(const PrefixParams& p, int b, int t0)
 __device__ __forceinline__ int pair_tiles(int2 len) {
   const int m = max(len.x, len.y);
   return m < 0 ? 0 : max(1, (m + kBN - 1) / kBN);
+}
+
+// The row's own part in FwdParams::O32: four columns k at [k * 128].
+template <int D>
+__device__ __forceinline__ const float4* own_row(const PrefixParams& p, int b, int h, int t) {
+  return reinterpret_cast<const float4*>(p.own_O) +
+         ((size_t(b) * p.Hkv * p.G + h) * ((p.T + 127) / 128) + t / 128) * (D / 4) * 128 + t % 128;
 }
 
 // The work is the key tiles of every (kv head, pair) in that order, cut into equal runs, one per
@@ -156,6 +164,10 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   const bool alt = p.alternate != 0;
   const int rows = p.gt * p.tt * p.bt;
 
+  if (p.reset_status) {   // a decode: its own part may share the GPU with this kernel
+    let_dependents_start();
+    if (blockIdx.x == 0 && tid == 0) *p.status = SEPLLM_OK;
+  }
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_q + i, 1); mbar_init(bar_qe + i, 1); mbar_init(bar_s + i, 1);
@@ -529,7 +541,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         const float wo = ex2(lo - mm), wp = l_sum > 0.f ? ex2(m_ref - mm) : 0.f;
         const float den = wo + l_sum * wp, inv = 1.f / den;
         if (store) p.LSE[row] = (mm + log2f(den)) * 0.6931471805599453f;
-        const float* own = p.own_O + row * D;
+        const float4* own = own_row<D>(p, b, sg->hk * p.G + g, t);
         __nv_bfloat16* orow = p.O + row * p.d;
         const float fo = wo * inv, fp = wp * inv;
 #pragma unroll
@@ -541,8 +553,8 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
             for (int q = 0; q < 4; ++q) {
               if (c * 32 + q * 8 >= p.d) continue;
               float v[8];
-              *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(own + c * 32 + q * 8);
-              *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(own + c * 32 + q * 8 + 4);
+              *reinterpret_cast<float4*>(v) = own[(c * 8 + q * 2) * 128];
+              *reinterpret_cast<float4*>(v + 4) = own[(c * 8 + q * 2 + 1) * 128];
 #pragma unroll
               for (int e = 0; e < 8; ++e)
                 v[e] = v[e] * fo + (n_mine > 0 ? __uint_as_float(oreg[q * 8 + e]) * fp : 0.f);
@@ -559,7 +571,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         const size_t u = (size_t(part) * 2 + x) * 128 + r;
         if (store) *reinterpret_cast<float2*>(p.part_ml + 2 * u) = make_float2(m_ref, l_sum);
         if (n_mine > 0) {
-          float* dst = p.part_acc + u * D;
+          float4* dst = reinterpret_cast<float4*>(p.part_acc) + (size_t(part) * 2 + x) * (D / 4) * 128 + r;
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
             uint32_t oreg[32];
@@ -568,8 +580,9 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
             if (store)
 #pragma unroll
               for (int q = 0; q < 8; ++q)
-                *reinterpret_cast<uint4*>(dst + c * 32 + q * 4) =
-                    make_uint4(oreg[4 * q], oreg[4 * q + 1], oreg[4 * q + 2], oreg[4 * q + 3]);
+                dst[(c * 8 + q) * 128] =
+                    make_float4(__uint_as_float(oreg[4 * q]), __uint_as_float(oreg[4 * q + 1]),
+                                __uint_as_float(oreg[4 * q + 2]), __uint_as_float(oreg[4 * q + 3]));
             __syncwarp();
           }
         }
@@ -592,117 +605,130 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
-// Joins the partial results of a row: those of the prefix and, of its own keys, own_parts of the
-// decode kernel or one normalised result with its log-sum-exp (own_lse).  WARPS warps per row, in
-// a fixed order.  A part with no key (l = 0) has no values and is not read.
-//   CUT false: grid over all rows;   CUT true: grid (256 rows, CTAs of the prefix kernel), the rows
-//   of the unit that the CTA left unfinished (all others are finished already)
+// Joins the partial results of 32 rows of a row tile: those of the prefix and, of the rows' own keys,
+// own_parts of the decode kernel ([row][part][D]) or one normalised result with its log-sum-exp
+// (own_lse).  Lane = row; a warp takes CPW times four columns, and SPLIT warps share the parts (each
+// a fixed subset in a fixed order).  A part with no key (l = 0) holds no values: what lies there is
+// read and dropped.
+//   grid (8 * units, column groups): 32 rows of every unit's two slots; CUT: 8 per CTA of the prefix
+//   kernel, the unit that it left unfinished (all others are finished already)
 constexpr int kJoinThreads = 128;
-template <int D, int WARPS, bool CUT>
+template <int D, bool CUT, int CPW, int SPLIT>
 __global__ void __launch_bounds__(kJoinThreads) prefix_join(const PrefixParams p, const float* own_ml,
-                                                            const float* own_acc, int own_parts, int n_rows) {
-  constexpr int E = D / 32;  // elements per lane
-  using Vec = typename std::conditional<E == 4, float4, float2>::type;
-  constexpr int kRows = kJoinThreads / 32 / WARPS;
-  __shared__ float s_l[kJoinThreads / 32];
-  __shared__ Vec s_acc[kJoinThreads / 32][32];
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, w0 = wid % WARPS;
-  const int idx = int(blockIdx.x) * kRows + wid / WARPS;
-  bool here;
-  int unit = 0, x = 0, r = 0;
-  size_t row = 0;
-  if (CUT) {
-    unit = p.cut_units[blockIdx.y];
-    if (unit < 0) return;
-    x = idx >> 7;
-    r = idx & 127;
-    const RowTile rt = row_tile(p, 2 * (p.pair_base + unit % p.pairs) + x);
-    const int b = rt.b0 + r / (p.gt * p.tt), t = rt.t0 + r / p.gt % p.tt, g = rt.g0 + r % p.gt;
-    here = r < p.gt * p.tt * p.bt && b < p.B && t < p.T && g < p.G && !(p.seq_len && t >= p.seq_len[b]);
-    row = ((size_t(b) * p.Hkv + unit / p.pairs) * p.G + g) * p.T + t;
-  } else {
-    here = idx < n_rows;
-    row = idx;
-    if (here) {
-      const int t = idx % p.T, g = idx / p.T % p.G, q = idx / (p.T * p.G), hk = q % p.Hkv, b = q / p.Hkv;
-      const int ti = (b / p.bt * p.t_tiles + t / p.tt) * p.g_tiles + g / p.gt;
-      const int pair = ti / 2 - p.pair_base;
-      here = pair >= 0 && pair < p.pairs && !(p.seq_len && t >= p.seq_len[b]);
-      unit = hk * p.pairs + pair;
-      x = ti & 1;
-      r = (b % p.bt * p.tt + t % p.tt) * p.gt + g % p.gt;
-    }
-  }
-  if (WARPS == 1 && !here) return;
-  const int4 parts = here ? p.unit_parts[unit] : make_int4(0, 0, 0, 0);
-  const int n_sub = p.alternate ? 2 : 1;   // alternate mode: both slots hold the row
-  const int n_pfx = here ? parts.x * n_sub : 0, n_own = here ? own_parts : 0;
-  auto place = [&](int i) -> size_t {
-    const int k = i / n_sub, part = k == 0 ? parts.y : 2 * (parts.z + k);
-    return (size_t(part) * 2 + (n_sub == 2 ? i % 2 : x)) * 128 + r;
+                                                            const float* own_acc, int own_parts) {
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, sp = wid % SPLIT;
+  const int col4 = (blockIdx.y * (4 / SPLIT) + wid / SPLIT) * CPW;
+  const int unit = CUT ? p.cut_units[blockIdx.x / 8] : int(blockIdx.x) / 8;
+  const int x = blockIdx.x / 4 % 2, r = blockIdx.x % 4 * 32 + lane;
+  const int ti = 2 * (p.pair_base + unit % p.pairs) + x;
+  if (unit < 0 || ti >= p.m_tiles) return;
+  const RowTile rt = row_tile(p, ti);
+  const int hk = unit / p.pairs, b = rt.b0 + r / (p.gt * p.tt), t = rt.t0 + r / p.gt % p.tt, g = rt.g0 + r % p.gt;
+  const bool here = r < p.gt * p.tt * p.bt && b < p.B && t < p.T && g < p.G && !(p.seq_len && t >= p.seq_len[b]);
+  if (SPLIT == 1 && !here) return;
+  const size_t row = ((size_t(b) * p.Hkv + hk) * p.G + g) * p.T + t;
+  const int4 parts = p.unit_parts[unit];
+  const int sub = p.alternate ? 1 : 0;     // alternate mode: both slots hold the row
+  const int n_pfx = here ? parts.x << sub : 0, n_own = here ? own_parts : 0;
+  auto place = [&](int i) -> size_t {      // part and slot of the row's i-th prefix part
+    const int k = i >> sub, part = k == 0 ? parts.y : 2 * (parts.z + k);
+    return size_t(part) * 2 + (sub ? i & 1 : x);
   };
-  const float2* pml = reinterpret_cast<const float2*>(p.part_ml);
+  const float2* pml = reinterpret_cast<const float2*>(p.part_ml) + r;
   const float2* oml = reinterpret_cast<const float2*>(own_ml) + row * own_parts;
+  // reference exponent of the warp's parts
   float mm = -INFINITY;
-  for (int i = lane; i < n_pfx; i += 32) { const float2 v = pml[place(i)]; if (v.y > 0.f) mm = fmaxf(mm, v.x); }
-  for (int i = lane; i < n_own; i += 32) { const float2 v = oml[i]; if (v.y > 0.f) mm = fmaxf(mm, v.x); }
-  float lo = -INFINITY;
-  if (p.own_lse && here) { lo = p.own_lse[row] * 1.4426950408889634f; mm = fmaxf(mm, lo); }
-#pragma unroll
-  for (int k = 16; k; k >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, k));
-  float l = 0.f, acc[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = 0.f;
-  auto add = [&](const float* a, float w) {
-    const Vec v = *reinterpret_cast<const Vec*>(a + lane * E);
-    const float* f = reinterpret_cast<const float*>(&v);
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] += f[e] * w;
-  };
 #pragma unroll 8
-  for (int i = w0; i < n_pfx; i += WARPS) {
-    const size_t u = place(i);
-    const float2 ml = pml[u];
-    if (!(ml.y > 0.f)) continue;
-    const float w = ex2(ml.x - mm);
-    l += ml.y * w;
-    add(p.part_acc + u * D, w);
+  for (int i = sp; i < n_pfx; i += SPLIT) {
+    const float2 v = pml[place(i) * 128];
+    mm = fmaxf(mm, v.y > 0.f ? v.x : -INFINITY);
   }
 #pragma unroll 4
-  for (int i = w0; i < n_own; i += WARPS) {
-    const float2 ml = oml[i];
-    if (!(ml.y > 0.f)) continue;
-    const float w = ex2(ml.x - mm);
-    l += ml.y * w;
-    add(own_acc + (row * own_parts + i) * D, w);
+  for (int i = sp; i < n_own; i += SPLIT) {
+    const float2 v = oml[i];
+    mm = fmaxf(mm, v.y > 0.f ? v.x : -INFINITY);
   }
-  if (p.own_lse && here && w0 == 0) {
-    const float w = ex2(lo - mm);
-    l += w;
-    add(p.own_O + row * D, w);
-  }
-  if (WARPS > 1) {
-    if (lane == 0) s_l[wid] = l;
-    s_acc[wid][lane] = *reinterpret_cast<Vec*>(acc);
-    __syncthreads();
-    if (w0 != 0 || !here) return;
+  float lo = -INFINITY;
+  if (p.own_lse && here && sp == 0) { lo = p.own_lse[row] * 1.4426950408889634f; mm = fmaxf(mm, lo); }
+  float l = 0.f;
+  float4 acc[CPW];
 #pragma unroll
-    for (int k = 1; k < WARPS; ++k) {
-      l += s_l[wid + k];
-      const Vec v = s_acc[wid + k][lane];
-      const float* f = reinterpret_cast<const float*>(&v);
+  for (int c = 0; c < CPW; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float2 ml, const float4* v, size_t step) {
+    const bool any = ml.y > 0.f;
+    const float w = any ? ex2(ml.x - mm) : 0.f;
+    l += any ? ml.y * w : 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] += f[e];
+    for (int c = 0; c < CPW; ++c) {
+      const float4 a = v[c * step];
+      acc[c].x += any ? a.x * w : 0.f;
+      acc[c].y += any ? a.y * w : 0.f;
+      acc[c].z += any ? a.z * w : 0.f;
+      acc[c].w += any ? a.w * w : 0.f;
     }
+  };
+  const float4* pacc = reinterpret_cast<const float4*>(p.part_acc) + size_t(col4) * 128 + r;
+  constexpr int kUnroll = CPW == 1 ? 8 : 2;
+#pragma unroll kUnroll
+  for (int i = sp; i < n_pfx; i += SPLIT) {
+    const size_t u = place(i);
+    add(pml[u * 128], pacc + u * (D / 4) * 128, 128);
+  }
+#pragma unroll 2
+  for (int i = sp; i < n_own; i += SPLIT)
+    add(oml[i], reinterpret_cast<const float4*>(own_acc) + (row * own_parts + i) * (D / 4) + col4, 1);
+  if (p.own_lse && here && sp == 0)
+    add(make_float2(lo, 1.f), own_row<D>(p, b, hk * p.G + g, t) + col4 * 128, 128);
+  if (SPLIT > 1) {
+    __shared__ float2 s_ml[kJoinThreads];
+    __shared__ float4 s_acc[kJoinThreads * CPW];
+    s_ml[threadIdx.x] = make_float2(mm, l);
+#pragma unroll
+    for (int c = 0; c < CPW; ++c) s_acc[c * kJoinThreads + threadIdx.x] = acc[c];
+    __syncthreads();
+    if (sp != 0 || !here) return;
+    float m = mm;
+#pragma unroll
+    for (int k = 1; k < SPLIT; ++k) m = fmaxf(m, s_ml[threadIdx.x + 32 * k].x);
+    float ls = 0.f;
+    float4 sum[CPW];
+#pragma unroll
+    for (int c = 0; c < CPW; ++c) sum[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < SPLIT; ++k) {
+      const float2 ml = s_ml[threadIdx.x + 32 * k];
+      const float w = ml.y > 0.f ? ex2(ml.x - m) : 0.f;
+      ls += ml.y * w;
+#pragma unroll
+      for (int c = 0; c < CPW; ++c) {
+        const float4 a = s_acc[c * kJoinThreads + threadIdx.x + 32 * k];
+        sum[c].x += a.x * w; sum[c].y += a.y * w; sum[c].z += a.z * w; sum[c].w += a.w * w;
+      }
+    }
+    mm = m;
+    l = ls;
+#pragma unroll
+    for (int c = 0; c < CPW; ++c) acc[c] = sum[c];
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;   // a row that sees no key at all: 0, log-sum-exp -inf
-  if (lane * E < p.d) {
-    __nv_bfloat16* o = p.O + row * p.d + lane * E;
 #pragma unroll
-    for (int e = 0; e < E; e += 2)
-      *reinterpret_cast<uint32_t*>(o + e) = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
-  }
-  if (p.LSE && lane == 0) p.LSE[row] = l > 0.f ? (mm + log2f(l)) * 0.6931471805599453f : -INFINITY;
+  for (int c = 0; c < CPW; ++c)
+    if ((col4 + c) * 4 < p.d)
+      *reinterpret_cast<uint2*>(p.O + row * p.d + (col4 + c) * 4) =
+          make_uint2(pack_bf16(acc[c].x * inv, acc[c].y * inv), pack_bf16(acc[c].z * inv, acc[c].w * inv));
+  if (p.LSE && col4 == 0) p.LSE[row] = l > 0.f ? (mm + log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <int D>
+void launch_join(const PrefixParams& p, int prefix_ctas, const float* own_ml, const float* own_acc, int own_parts,
+                 cudaStream_t stream) {
+  const unsigned units = unsigned(p.pairs * p.Hkv);
+  if (!p.whole_parts)
+    prefix_join<D, true, D / 16, 1><<<dim3(8 * prefix_ctas, 1), kJoinThreads, 0, stream>>>(p, own_ml, own_acc, own_parts);
+  else if (units >= 24)
+    prefix_join<D, false, D / 16, 1><<<dim3(8 * units, 1), kJoinThreads, 0, stream>>>(p, own_ml, own_acc, own_parts);
+  else   // few rows, many parts each
+    prefix_join<D, false, 1, 4><<<dim3(8 * units, D / 4), kJoinThreads, 0, stream>>>(p, own_ml, own_acc, own_parts);
 }
 
 // bf16 [B][Hkv][G][T][d] as (d, G, T, Hkv, B); box of 64 columns x gt heads x tt tokens x bt sequences.
@@ -750,7 +776,7 @@ int64_t max_parts(const PrefixParams& p) {
 
 }  // namespace
 
-bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, bool whole_parts) {
+bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, bool whole_parts, double own_us) {
   p->B = B;
   p->Hkv = Hkv;
   p->G = Hq / Hkv;
@@ -769,6 +795,19 @@ bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, b
   p->alternate = m_tiles == 1 ? 1 : 0;
   p->whole_parts = whole_parts || p->alternate;   // alternate mode: two parts of every row, joined later
   p->max_ctas = kSmCount;
+  if (own_us > 0.0) {
+    // The own part runs on the SMs that the prefix kernel leaves, and on all of them when it is done.
+    // With n CTAs the prefix takes 8 us and 2.4 us for each pair of row tiles and key tile of a CTA
+    // (measured); the own part, bound by HBM, loses nothing while it has four fifths of the SMs.
+    const double steps = double(launch_pairs(*p)) * Hkv * p->key_tiles * (p->alternate ? 0.5 : 1.0);
+    double best = 1e300;
+    for (int n = 4; n <= kSmCount; n += 4) {
+      const double t = 8.0 + 2.4 * std::ceil(steps / n), rate = std::min(1.0, 1.25 * (kSmCount - n) / kSmCount);
+      const double total = rate * t >= own_us ? t : own_us + (1.0 - rate) * t;
+      if (total < best) { best = total; p->max_ctas = n; }
+    }
+    if (p->alternate && p->max_ctas > Hkv) p->max_ctas -= p->max_ctas % Hkv;   // (see n_runs)
+  }
   return true;
 }
 
@@ -788,8 +827,9 @@ void place_prefix_parts(PrefixParams* p, uint8_t* ws) {
   p->cut_units = reinterpret_cast<int32_t*>(ws + align_up(size_t(launch_pairs(*p)) * p->Hkv * sizeof(int4)));
 }
 
-sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const void* Vp, const float* own_ml,
-                            const float* own_acc, int own_parts, cudaStream_t stream) {
+sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const void* Vp, cudaStream_t stream,
+                            const std::function<sepllm_status()>& beside, const float* own_ml,
+                            const float* own_acc, int own_parts) {
   CUtensorMap mq, mk, mv;
   sepllm_status st;
   if ((st = make_query_map(&mq, Q, p)) != SEPLLM_OK) return st;
@@ -798,23 +838,15 @@ sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const
   const int64_t rows = int64_t(p.B) * p.Hkv * p.G * p.T;
   if (rows > 0x7fffffff) return SEPLLM_UNSUPPORTED;
   const bool d64 = kernel_head_dim(p.d) == 64;
-  // few rows have many parts each: four warps per row (measured at 1024 rows of 36 parts: 9 us
-  // against 16; at 8192 rows of 7 parts: 23 against 12)
-  const bool wide = rows <= 2048;
   for (p.pair_base = 0; p.pair_base < all_pairs(p); p.pair_base += p.pairs) {
     p.pairs = std::min(launch_pairs(p), all_pairs(p) - p.pair_base);
     const int grid = prefix_grid(p, p.pairs);
+    p.reset_status = beside && p.pair_base == 0;
     st = d64 ? launch_prefix_d<64>(p, grid, mq, mk, mv, stream) : launch_prefix_d<128>(p, grid, mq, mk, mv, stream);
     if (st != SEPLLM_OK) return st;
-    if (!p.whole_parts) {
-      auto join = d64 ? prefix_join<64, 1, true> : prefix_join<128, 1, true>;
-      join<<<dim3(64, grid), kJoinThreads, 0, stream>>>(p, own_ml, own_acc, own_parts, 0);
-    } else {
-      auto join = d64 ? (wide ? prefix_join<64, 4, false> : prefix_join<64, 1, false>)
-                      : (wide ? prefix_join<128, 4, false> : prefix_join<128, 1, false>);
-      join<<<unsigned(wide ? rows : (rows + 3) / 4), kJoinThreads, 0, stream>>>(p, own_ml, own_acc, own_parts,
-                                                                                int(rows));
-    }
+    if (beside && p.pair_base == 0 && (st = beside()) != SEPLLM_OK) return st;
+    if (d64) launch_join<64>(p, grid, own_ml, own_acc, own_parts, stream);
+    else launch_join<128>(p, grid, own_ml, own_acc, own_parts, stream);
     SEPLLM_CUDA_TRY(cudaGetLastError());
   }
   return SEPLLM_OK;
@@ -833,7 +865,7 @@ AttnPrefixLayout attn_prefix_layout(const sepllm_attn_desc* d, const sepllm_inde
   AttnPrefixLayout a;
   const size_t rows = size_t(d->B) * d->Hq * d->L;
   a.off_o = attn_layout(d, id).fwd_bytes;
-  a.off_lse = a.off_o + align_up(rows * kernel_head_dim(d->d) * sizeof(float));
+  a.off_lse = a.off_o + align_up(size_t(d->B) * d->Hq * ((d->L + 127) / 128 * 128) * kernel_head_dim(d->d) * sizeof(float));
   a.off_parts = a.off_lse + align_up(rows * sizeof(float));
   a.bytes = a.off_parts + prefix_part_bytes(p);
   return a;
@@ -847,7 +879,7 @@ extern "C" sepllm_status sepllm_attn_prefix_workspace_bytes(const sepllm_attn_de
   if (st != SEPLLM_OK) return st;
   if (P < 1) return SEPLLM_INVALID_ARG;
   PrefixParams p{};
-  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P, false)) return SEPLLM_UNSUPPORTED;
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P, false, 0.0)) return SEPLLM_UNSUPPORTED;
   if (bytes) *bytes = attn_prefix_layout(desc, idesc, p).bytes;
   return SEPLLM_OK;
 }
@@ -867,7 +899,7 @@ extern "C" sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, co
   sepllm_index_header ih;
   if ((st = fill_index_header(idesc, &ih)) != SEPLLM_OK) return st;
   PrefixParams p{};
-  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P, false)) return SEPLLM_UNSUPPORTED;
+  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P, false, 0.0)) return SEPLLM_UNSUPPORTED;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const AttnPrefixLayout lay = attn_prefix_layout(desc, idesc, p);
@@ -884,5 +916,5 @@ extern "C" sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, co
   p.LSE = LSE;
   p.status = reinterpret_cast<int32_t*>(ws);
   p.scale_log2 = (desc->scale != 0.f ? desc->scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
-  return launch_prefix(p, Q, Kp, Vp, nullptr, nullptr, 0, stream);
+  return launch_prefix(p, Q, Kp, Vp, stream, nullptr, nullptr, nullptr, 0);
 }
