@@ -5,6 +5,7 @@
 // which is only laid out) is read once and written once.  cos and sin depend on (token, pair) and
 // not on the head, so a thread takes one token and eight pairs, computes their cos and sin once and
 // walks the heads with them; there is no table to build, size or read.
+#include <algorithm>
 #include <cmath>
 
 #include "attn_common.cuh"
@@ -48,10 +49,20 @@ __device__ __forceinline__ double rope_position(const RopeParams& p, int64_t b, 
   return double(p.pos ? p.pos[b * p.pos_stride + l] : p.pos_first + l);
 }
 
-// Eight elements as floats, 16-byte accesses.
-__device__ __forceinline__ void load8(const __nv_bfloat16* s, float (&x)[8]) {
-  const uint4 u = *reinterpret_cast<const uint4*>(s);
-  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
+// Eight elements by 16-byte accesses: as they lie in memory, and as floats.
+template <class T>
+struct Eight {
+  uint4 w[sizeof(T) / 2];
+};
+template <class T>
+__device__ __forceinline__ Eight<T> load8(const T* s) {
+  Eight<T> r;
+#pragma unroll
+  for (int k = 0; k < int(sizeof(T) / 2); ++k) r.w[k] = reinterpret_cast<const uint4*>(s)[k];
+  return r;
+}
+__device__ __forceinline__ void to_floats(const Eight<__nv_bfloat16>& r, float (&x)[8]) {
+  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(r.w);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const float2 f = __bfloat1622float2(h[k]);
@@ -59,10 +70,10 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* s, float (&x)[8]) {
     x[2 * k + 1] = f.y;
   }
 }
-__device__ __forceinline__ void load8(const float* s, float (&x)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(s)[0], c = reinterpret_cast<const float4*>(s)[1];
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-  x[4] = c.x; x[5] = c.y; x[6] = c.z; x[7] = c.w;
+__device__ __forceinline__ void to_floats(const Eight<float>& r, float (&x)[8]) {
+  const float* f = reinterpret_cast<const float*>(r.w);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[k] = f[k];
 }
 __device__ __forceinline__ void store8(__nv_bfloat16* s, const float (&x)[8]) {
   *reinterpret_cast<uint4*>(s) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]),
@@ -89,26 +100,28 @@ __global__ void __launch_bounds__(kRopeThreads) rope_rows(const __grid_constant_
   const int t = int(id - n * per_row);
   const int64_t b = n / p.L;
   const int l = int(n - b * p.L);
-  int c0, c1;         // first elements of the two pieces
-  bool turn0, turn1;  // rotated (for Q and K)
+  int c0, c1;  // first elements of the two pieces
+  bool turn0;  // (some of) the thread's elements are rotated (in Q and K)
+  // (neighbouring threads take neighbouring pieces, so that an access of a warp is contiguous in a row)
   if (HALF) {
-    const bool pair = t < p.rot / 16;
-    c0 = pair ? 8 * t : p.rot + 16 * (t - p.rot / 16);
-    c1 = pair ? c0 + p.rot / 2 : c0 + 8;
-    turn0 = turn1 = pair;
+    const int pairs = p.rot / 16;
+    turn0 = t < pairs;
+    c0 = 8 * (turn0 ? t : t + pairs);
+    c1 = c0 + (turn0 ? p.rot / 2 : (p.d - p.rot) / 2);
   } else {
-    c0 = 16 * t;
-    c1 = c0 + 8;
+    c0 = 8 * t;
+    c1 = c0 + p.d / 2;
     turn0 = c0 < p.rot;
-    turn1 = c1 < p.rot;
   }
   const int h0 = blockIdx.y * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
   float2 cs[8];
   if (turn0 && h0 < p.t[0].heads + p.t[1].heads) {
     const double pos = rope_position(p, b, l);
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      cs[k] = (HALF || k < 4 || turn1) ? rope_cos_sin(p, pos, 8 * t + k) : make_float2(1.f, 0.f);
+    for (int k = 0; k < 8; ++k) {
+      const int i = HALF ? c0 + k : (k < 4 ? c0 / 2 + k : c1 / 2 + k - 4);
+      cs[k] = 2 * i < p.rot ? rope_cos_sin(p, pos, i) : make_float2(1.f, 0.f);
+    }
   }
   int first = 0;  // heads of the tensors before this one
 #pragma unroll
@@ -118,11 +131,10 @@ __global__ void __launch_bounds__(kRopeThreads) rope_rows(const __grid_constant_
     first += x.heads;
     const Tin* src = static_cast<const Tin*>(x.in) + b * x.ib + l * x.il;
     Tout* dst = static_cast<Tout*>(x.out) + b * x.ob + l * x.ol;
-#pragma unroll 4
-    for (int h = a; h < e; ++h) {
+    auto finish = [&](int h, const Eight<Tin>& ru, const Eight<Tin>& rv) {
       float u[8], v[8];
-      load8(src + h * x.ih + c0, u);
-      load8(src + h * x.ih + c1, v);
+      to_floats(ru, u);
+      to_floats(rv, v);
       if (w < 2) {
         if (HALF) {
           if (turn0) {
@@ -134,14 +146,15 @@ __global__ void __launch_bounds__(kRopeThreads) rope_rows(const __grid_constant_
             }
           }
         } else {
+          // (rot may end inside a piece, never inside a pair)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            if (turn0) {
+            if (c0 + 2 * k < p.rot) {
               const float y0 = u[2 * k] * cs[k].x - u[2 * k + 1] * cs[k].y;
               u[2 * k + 1] = u[2 * k + 1] * cs[k].x + u[2 * k] * cs[k].y;
               u[2 * k] = y0;
             }
-            if (turn1) {
+            if (c1 + 2 * k < p.rot) {
               const float y1 = v[2 * k] * cs[4 + k].x - v[2 * k + 1] * cs[4 + k].y;
               v[2 * k + 1] = v[2 * k + 1] * cs[4 + k].x + v[2 * k] * cs[4 + k].y;
               v[2 * k] = y1;
@@ -151,6 +164,85 @@ __global__ void __launch_bounds__(kRopeThreads) rope_rows(const __grid_constant_
       }
       store8(dst + h * x.oh + c0, u);
       store8(dst + h * x.oh + c1, v);
+    };
+    // several heads' loads go out before the first store (the compiler may not move a load over a
+    // store: an output may be its input)
+    constexpr int kBatch = sizeof(Tin) == 2 ? 4 : 2;   // 32 registers either way
+    int h = a;
+    for (; h + kBatch <= e; h += kBatch) {
+      Eight<Tin> ru[kBatch], rv[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        ru[i] = load8(src + (h + i) * x.ih + c0);
+        rv[i] = load8(src + (h + i) * x.ih + c1);
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) finish(h + i, ru[i], rv[i]);
+    }
+    for (; h < e; ++h) finish(h, load8(src + h * x.ih + c0), load8(src + h * x.ih + c1));
+  }
+}
+
+// Halves whose length is no multiple of a 16-byte piece: a thread owns one piece of a row, a warp whole
+// rows, and the other elements of the pairs come from the row in shared memory.
+template <class Tin, class Tout>
+__global__ void __launch_bounds__(kRopeThreads) rope_halves(const __grid_constant__ RopeParams p) {
+  __shared__ __align__(16) float s_rows[kRopeThreads / 32][2][32 * 8];
+  const int per_row = p.d / 8, rows = 32 / per_row, half = p.rot / 2;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const int rr = lane / per_row, c0 = (lane % per_row) * 8;
+  const int64_t n = (int64_t(blockIdx.x) * (kRopeThreads / 32) + wid) * rows + rr;
+  const bool here = rr < rows && n < p.tokens;
+  const int64_t b = here ? n / p.L : 0;
+  const int l = here ? int(n - b * p.L) : 0;
+  const int h0 = blockIdx.y * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
+  float2 cs[8];   // of each element: cos, and sin with the sign that its partner takes
+  int other[8];   // place of the partner in the warp's rows; an element that is copied is its own
+  const double pos = here ? rope_position(p, b, l) : 0.0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int e = c0 + k;
+    other[k] = rr * p.d + (e < half ? e + half : e < p.rot ? e - half : e);
+    cs[k] = make_float2(1.f, 0.f);
+    if (e < p.rot && h0 < p.t[0].heads + p.t[1].heads) {
+      cs[k] = rope_cos_sin(p, pos, e < half ? e : e - half);
+      if (e < half) cs[k].y = -cs[k].y;
+    }
+  }
+  int first = 0;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) {
+    const RopeTensor& x = p.t[w];
+    const int a = max(h0 - first, 0), z = min(h1 - first, x.heads);
+    first += x.heads;
+    const Tin* src = static_cast<const Tin*>(x.in) + b * x.ib + l * x.il + c0;
+    Tout* dst = static_cast<Tout*>(x.out) + b * x.ob + l * x.ol + c0;
+    for (int h = a; h < z; h += 2) {
+      float u[2][8];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (here && h + i < z) to_floats(load8(src + (h + i) * x.ih), u[i]);
+      if (w < 2) {
+        if (here) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (h + i < z) store8(s_rows[wid][i] + rr * p.d + c0, u[i]);
+        }
+        __syncwarp();
+        if (here) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (h + i < z) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                if (c0 + k < p.rot) u[i][k] = u[i][k] * cs[k].x + s_rows[wid][i][other[k]] * cs[k].y;
+            }
+        }
+        __syncwarp();
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (here && h + i < z) store8(dst + (h + i) * x.oh, u[i]);
     }
   }
 }
@@ -288,7 +380,9 @@ bool vector_access(const void* data, int64_t sb, int64_t sh, int64_t sl) {
 
 template <class Tin, class Tout>
 void launch_rope(const RopeParams& p, bool rows, bool half, dim3 grid, cudaStream_t stream) {
-  if (rows) {
+  if (rows && half && p.rot % 16 != 0) {
+    rope_halves<Tin, Tout><<<grid, kRopeThreads, 0, stream>>>(p);
+  } else if (rows) {
     if (half) rope_rows<Tin, Tout, true><<<grid, kRopeThreads, 0, stream>>>(p);
     else rope_rows<Tin, Tout, false><<<grid, kRopeThreads, 0, stream>>>(p);
   } else {
@@ -305,8 +399,7 @@ sepllm_status rope(const sepllm_rope_desc* d, const int64_t* positions, const se
   RopeParams p{};
   p.rot = d->rot_dim ? d->rot_dim : d->d;
   const bool half = d->layout == SEPLLM_ROPE_HALF;
-  // whole 16-byte pieces are rotated or copied as one (rope_rows), else element by element
-  bool rows = half ? p.rot % 16 == 0 : p.rot % 8 == 0;
+  bool rows = true;   // 16-byte accesses are possible
   int dt_in = -1, dt_out = -1;
   for (int w = 0; w < 3; ++w) {
     const sepllm_rope_view &a = in[w], &z = out[w];
@@ -342,10 +435,18 @@ sepllm_status rope(const sepllm_rope_desc* d, const int64_t* positions, const se
   p.tokens = int64_t(d->B) * d->L;
   p.L = d->L;
   p.d = d->d;
-  const int64_t threads = p.tokens * (rows ? d->d / 16 : d->d - p.rot / 2);
+  // threads: 16 elements of a row each (rope_rows), 8 with whole rows to a warp (rope_halves), or one
+  // pair or copied element (rope_elements)
+  const int64_t warp_rows = 32 / (d->d / 8);
+  const int64_t threads = !rows                      ? p.tokens * (d->d - p.rot / 2)
+                          : half && p.rot % 16 != 0 ? (p.tokens + warp_rows - 1) / warp_rows * 32
+                                                     : p.tokens * (d->d / 16);
   const int64_t blocks = (threads + kRopeThreads - 1) / kRopeThreads;
   if (blocks > 0x7fffffff) return SEPLLM_UNSUPPORTED;
-  p.heads_per_block = p.n_heads;
+  // Heads are walked by one thread as long as that leaves enough threads to fill the SMs (2048 each);
+  // a thread of its own costs every group of heads another eight sines and cosines.
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(p.n_heads, int64_t(kSmCount) * 2048 / threads));
+  p.heads_per_block = int((p.n_heads + want - 1) / want);
   const int64_t groups = (p.n_heads + p.heads_per_block - 1) / p.heads_per_block;
   if (groups > 65535) return SEPLLM_UNSUPPORTED;
   const dim3 grid{unsigned(blocks), unsigned(groups)};

@@ -50,6 +50,7 @@ CASES = [
     (1, 1, 1, 1, 64, 64), (3, 7, 4, 2, 64, 16), (2, 33, 5, 1, 80, 20), (2, 5, 3, 3, 80, 80), (1, 130, 2, 1, 96, 24),
     (2, 17, 4, 4, 112, 112), (2, 65, 8, 2, 128, 128), (1, 9, 10, 2, 128, 64), (2, 3, 2, 1, 128, 2),
     (1, 1000, 32, 8, 128, 128), (32, 1, 32, 8, 128, 128), (2, 6, 2, 1, 96, 40),
+    (3, 11, 3, 1, 64, 6), (2, 13, 5, 2, 112, 90), (1, 25, 2, 2, 128, 118), (2, 10, 1, 1, 80, 78),
 ]
 
 
