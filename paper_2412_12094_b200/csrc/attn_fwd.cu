@@ -136,6 +136,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 8 + 4 * NST);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
 
+  if (F32) let_dependents_start();   // the prefix kernel may start while this one ends
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // grid (heads x batch, tiles): consecutive CTAs take the same tile position of every head and
   // sequence, longest tiles first, so work is handed out longest-first over the whole launch and

@@ -85,6 +85,7 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_tok + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
 
+  if (F32) let_dependents_start();   // the prefix kernel may start while this one ends
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_ctarank();   // 0 = even CTA, issues the MMAs
   // grid (pairs of query heads x batch, tiles), longest tiles first; the two CTAs of a cluster are

@@ -76,7 +76,7 @@ __device__ __forceinline__ const float4* own_row(const PrefixParams& p, int b, i
 // Every warp walks the run by itself; its place sits in shared memory (a warp's copy each), so that
 // nothing of it takes registers in the softmax loop.
 struct Segment {
-  int64_t left;     // key tiles of the run behind this segment
+  int left;         // key tiles of the run behind this segment
   int hk, pair;
   int j0, j1, nt;   // key tiles [j0, j1) of nt
   int len[2];       // longest prefix of the row tile in slot x (-1: no rows)
@@ -85,7 +85,7 @@ struct Segment {
 // thread.
 template <bool WARP>
 __device__ __forceinline__ bool next_segment(Segment* sg, const int2* tab, int pairs) {
-  const int64_t left = sg->left;
+  const int left = sg->left;
   int hk = sg->hk, pair = sg->pair, off = sg->j1, nt;
   if (WARP) __syncwarp();
   if (left <= 0) return false;
@@ -95,7 +95,7 @@ __device__ __forceinline__ bool next_segment(Segment* sg, const int2* tab, int p
   }
   if (!WARP || (threadIdx.x & 31) == 0) {
     sg->hk = hk; sg->pair = pair; sg->j0 = off; sg->nt = nt;
-    sg->j1 = int(min(int64_t(nt), off + left));
+    sg->j1 = min(nt, off + left);
     sg->left = left - (sg->j1 - off);
     sg->len[0] = tab[pair].x;
     sg->len[1] = tab[pair].y;
@@ -157,8 +157,8 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
   int* s_warp = reinterpret_cast<int*>(tmem_slot + 4);   // [12] key tiles per warp of the scan
   int* s_start = s_warp + 12;                            // [2] pair and offset where the run starts
-  int64_t* s_run = reinterpret_cast<int64_t*>(s_warp + 14);  // end of the run, key tiles in all, runs
-  Segment* s_seg = reinterpret_cast<Segment*>(s_run + 3);    // [12] place of each warp in the run
+  int* s_run = s_warp + 14;                              // end of the run, tiles per run, longer runs
+  Segment* s_seg = reinterpret_cast<Segment*>(s_run + 4);    // [12] place of each warp in the run
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const bool alt = p.alternate != 0;
@@ -231,22 +231,24 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     if (w < warp) before += s_warp[w];
     per_head += s_warp[w];
   }
-  const int64_t total = int64_t(per_head) * p.Hkv;
+  const int total = per_head * p.Hkv;
   // CTAs that get a run: none an empty one, in alternate mode one tile for each slot.  With one
   // pair in all and short runs, a whole number of runs per kv head: a run that straddles two heads
   // loads queries and leaves parts twice (costs about two tiles, saves less than one).
-  int64_t n_runs = min(int64_t(gridDim.x), alt ? (total + 1) / 2 : total);
+  int n_runs = min(int(gridDim.x), alt ? (total + 1) / 2 : total);
   if (p.pairs == 1 && n_runs >= p.Hkv && total < 16 * n_runs) n_runs -= n_runs % p.Hkv;
-  const int64_t run0 = blockIdx.x < n_runs ? total * blockIdx.x / n_runs : 0;
-  const int64_t run1 = blockIdx.x < n_runs ? total * (blockIdx.x + 1) / n_runs : 0;
-  const int in_head = per_head > 0 ? int(run0 % per_head) : 0;
+  // runs of `run` tiles, the first `longer` of them of one more
+  const int blk = blockIdx.x, run = n_runs > 0 ? total / n_runs : 0, longer = total - run * n_runs;
+  const int run0 = blk < n_runs ? blk * run + min(blk, longer) : 0;
+  const int run1 = blk < n_runs ? run0 + run + (blk < longer) : 0;
+  const int hk0 = per_head > 0 ? run0 / per_head : 0, in_head = run0 - hk0 * per_head;
   if (run0 < run1 && in_head >= before && in_head < before + mine) {
     int at = before, i = i0;
     while (at + pair_tiles(tab[i]) <= in_head) at += pair_tiles(tab[i++]);
     s_start[0] = i;
     s_start[1] = in_head - at;
   }
-  if (tid == 0) { s_run[0] = run1; s_run[1] = total; s_run[2] = n_runs; }
+  if (tid == 0) { s_run[0] = run1; s_run[1] = run; s_run[2] = longer; }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -254,7 +256,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   Segment* sg = s_seg + warp;
   if (lane == 0) {
     sg->left = run1 - run0;
-    sg->hk = per_head > 0 ? int(run0 / per_head) : 0;
+    sg->hk = hk0;
     sg->pair = s_start[0];
     sg->j1 = s_start[1];
   }
@@ -533,6 +535,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
       const int part = whole ? 2 * int(gridDim.x) + unit : 2 * int(blockIdx.x) + (n > 0 ? 1 : 0);
       const bool finish = whole && !p.whole_parts;   // nothing to wait for: the row is joined here
       if (finish) {
+        wait_for_prior();   // the forward over the rows' own tokens, which this kernel may run beside
         const size_t row = ((size_t(b) * p.Hkv + sg->hk) * p.G + g) * p.T + t;
         // joined with the row's own part (fp32, normalised, with its log-sum-exp) and rounded once
         const float lo = store ? p.own_lse[row] * 1.4426950408889634f : 0.f;
@@ -591,8 +594,8 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
       // where the unit's parts are, from the CTA that has its first key tile
       if (sg->j0 == 0 && tid == 128) {
         // number of the unit's last key tile, and the CTA that has it
-        const int64_t last = s_run[0] - sg->left - 1 + (sg->nt - sg->j1);
-        const int c1 = int(((last + 1) * s_run[2] + s_run[1] - 1) / s_run[1]) - 1;
+        const int last = s_run[0] - sg->left - 1 + (sg->nt - sg->j1), run = s_run[1], longer = s_run[2];
+        const int c1 = last < longer * (run + 1) ? last / (run + 1) : longer + (last - longer * (run + 1)) / run;
         p.unit_parts[unit] = make_int4(finish ? 0 : c1 - int(blockIdx.x) + 1, part, blockIdx.x, 0);
         if (!whole) cut = unit;
       }
@@ -600,6 +603,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     // a run starts at most one unit that other CTAs go on with: its last one
     if (tid == 128) p.cut_units[blockIdx.x] = cut;
   }
+  wait_for_prior();   // this kernel's end stands for the end of the one it ran beside
   tc_fence_before();
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, 512);
@@ -616,6 +620,7 @@ constexpr int kJoinThreads = 128;
 template <int D, bool CUT, int CPW, int SPLIT>
 __global__ void __launch_bounds__(kJoinThreads) prefix_join(const PrefixParams p, const float* own_ml,
                                                             const float* own_acc, int own_parts) {
+  wait_for_prior();   // (launched while the kernel before it ends)
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, sp = wid % SPLIT;
   const int col4 = (blockIdx.y * (4 / SPLIT) + wid / SPLIT) * CPW;
   const int unit = CUT ? p.cut_units[blockIdx.x / 8] : int(blockIdx.x) / 8;
@@ -720,15 +725,18 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join(const PrefixParams p
 }
 
 template <int D>
-void launch_join(const PrefixParams& p, int prefix_ctas, const float* own_ml, const float* own_acc, int own_parts,
+cudaError_t launch_join(const PrefixParams& p, int prefix_ctas, const float* own_ml, const float* own_acc, int own_parts,
                  cudaStream_t stream) {
   const unsigned units = unsigned(p.pairs * p.Hkv);
   if (!p.whole_parts)
-    prefix_join<D, true, D / 16, 1><<<dim3(8 * prefix_ctas, 1), kJoinThreads, 0, stream>>>(p, own_ml, own_acc, own_parts);
-  else if (units >= 24)
-    prefix_join<D, false, D / 16, 1><<<dim3(8 * units, 1), kJoinThreads, 0, stream>>>(p, own_ml, own_acc, own_parts);
-  else   // few rows, many parts each
-    prefix_join<D, false, 1, 4><<<dim3(8 * units, D / 4), kJoinThreads, 0, stream>>>(p, own_ml, own_acc, own_parts);
+    return launch_overlapped(prefix_join<D, true, D / 16, 1>, dim3(8 * prefix_ctas), dim3(kJoinThreads), 0, stream, p,
+                             own_ml, own_acc, own_parts);
+  if (units >= 24)
+    return launch_overlapped(prefix_join<D, false, D / 16, 1>, dim3(8 * units), dim3(kJoinThreads), 0, stream, p,
+                             own_ml, own_acc, own_parts);
+  // few rows, many parts each
+  return launch_overlapped(prefix_join<D, false, 1, 4>, dim3(8 * units, D / 4), dim3(kJoinThreads), 0, stream, p,
+                           own_ml, own_acc, own_parts);
 }
 
 // bf16 [B][Hkv][G][T][d] as (d, G, T, Hkv, B); box of 64 columns x gt heads x tt tokens x bt sequences.
@@ -751,15 +759,20 @@ sepllm_status launch_prefix_d(const PrefixParams& p, int grid, const CUtensorMap
                               const CUtensorMap& mv, cudaStream_t stream) {
   SEPLLM_CUDA_TRY(cudaFuncSetAttribute(prefix_attn<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        int(PfxCfg<D>::kRequest)));
-  prefix_attn<D><<<grid, kPfxThreads, PfxCfg<D>::kRequest, stream>>>(mq, mk, mv, p);
+  // behind a forward it may start while that ends (a decode's prefix kernel is its call's first)
+  if (p.reset_status || p.pair_base > 0)
+    prefix_attn<D><<<grid, kPfxThreads, PfxCfg<D>::kRequest, stream>>>(mq, mk, mv, p);
+  else
+    SEPLLM_CUDA_TRY(launch_overlapped(prefix_attn<D>, dim3(grid), dim3(kPfxThreads), PfxCfg<D>::kRequest, stream, mq,
+                                      mk, mv, p));
   SEPLLM_CUDA_TRY(cudaGetLastError());
   return SEPLLM_OK;
 }
 
 int all_pairs(const PrefixParams& p) { return (p.m_tiles + 1) / 2; }
-// per launch: what the table holds, and a count of key tiles per kv head within 31 bits
+// per launch: what the table holds, and a count of key tiles within 31 bits
 int launch_pairs(const PrefixParams& p) {
-  return std::min(all_pairs(p), std::min(kMaxPairs, (1 << 30) / p.key_tiles));
+  return int(std::min<int64_t>(std::min(all_pairs(p), kMaxPairs), (int64_t(1) << 30) / (int64_t(p.key_tiles) * p.Hkv)));
 }
 
 // CTAs of a launch over `pairs` pairs: one per SM, none without a key tile (two in alternate mode).
@@ -790,7 +803,7 @@ bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, b
   p->g_tiles = (p->G + p->gt - 1) / p->gt;
   p->t_tiles = (T + p->tt - 1) / p->tt;
   const int64_t m_tiles = int64_t((B + p->bt - 1) / p->bt) * p->t_tiles * p->g_tiles;
-  if (m_tiles > 0x3fffffff || Hkv > 65535 || P > (1 << 30)) return false;
+  if (m_tiles > 0x3fffffff || Hkv > 65535 || P > (1 << 30) || int64_t(p->key_tiles) * Hkv > (1 << 30)) return false;
   p->m_tiles = int(m_tiles);
   p->alternate = m_tiles == 1 ? 1 : 0;
   p->whole_parts = whole_parts || p->alternate;   // alternate mode: two parts of every row, joined later
@@ -845,9 +858,8 @@ sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const
     st = d64 ? launch_prefix_d<64>(p, grid, mq, mk, mv, stream) : launch_prefix_d<128>(p, grid, mq, mk, mv, stream);
     if (st != SEPLLM_OK) return st;
     if (beside && p.pair_base == 0 && (st = beside()) != SEPLLM_OK) return st;
-    if (d64) launch_join<64>(p, grid, own_ml, own_acc, own_parts, stream);
-    else launch_join<128>(p, grid, own_ml, own_acc, own_parts, stream);
-    SEPLLM_CUDA_TRY(cudaGetLastError());
+    SEPLLM_CUDA_TRY(d64 ? launch_join<64>(p, grid, own_ml, own_acc, own_parts, stream)
+                        : launch_join<128>(p, grid, own_ml, own_acc, own_parts, stream));
   }
   return SEPLLM_OK;
 }
