@@ -547,8 +547,19 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         const float4* own = own_row<D>(p, b, sg->hk * p.G + g, t);
         __nv_bfloat16* orow = p.O + row * p.d;
         const float fo = wo * inv, fp = wp * inv;
+        // The row's own part comes through this slot's buffer of P, which is free now, 64 columns at a time
+        // (a thread's pieces in the places of its row number, neighbours next to each other): sixteen
+        // loads under way that take no registers.
+        const uint32_t stage = smem_u32(sPx) + r * 16;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
+          if (c % 2 == 0) {
+            if (store)
+#pragma unroll
+              for (int q = 0; q < 16; ++q) cp_async16(stage + q * 2048, own + (c * 8 + q) * 128, 16);
+            cp_async_commit();
+            cp_async_wait<0>();
+          }
           uint32_t oreg[32];
           if (n_mine > 0) { tmem_ld32(tO + c * 32, oreg); tmem_ld_wait(); }
           if (store) {
@@ -556,8 +567,8 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
             for (int q = 0; q < 4; ++q) {
               if (c * 32 + q * 8 >= p.d) continue;
               float v[8];
-              *reinterpret_cast<float4*>(v) = own[(c * 8 + q * 2) * 128];
-              *reinterpret_cast<float4*>(v + 4) = own[(c * 8 + q * 2 + 1) * 128];
+              *reinterpret_cast<float4*>(v) = reinterpret_cast<const float4*>(sPx)[(c % 2 * 8 + q * 2) * 128 + r];
+              *reinterpret_cast<float4*>(v + 4) = reinterpret_cast<const float4*>(sPx)[(c % 2 * 8 + q * 2 + 1) * 128 + r];
 #pragma unroll
               for (int e = 0; e < 8; ++e)
                 v[e] = v[e] * fo + (n_mine > 0 ? __uint_as_float(oreg[q * 8 + e]) * fp : 0.f);
