@@ -1,7 +1,5 @@
 // Declarations shared by the attention translation units.
 #pragma once
-#include <functional>
-
 #include "common.cuh"
 
 namespace sepllm {
@@ -220,9 +218,9 @@ bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, b
 size_t prefix_part_bytes(const PrefixParams& p);
 void place_prefix_parts(PrefixParams* p, uint8_t* ws);
 // The prefix part and the join with the rows' own parts: own_parts of the decode kernel, launched by
-// `beside` once the (first) prefix kernel is, or (own_parts = 0) p.own_O and p.own_lse.
+// beside(ctx) once the (first) prefix kernel is, or (beside null, own_parts = 0) p.own_O and p.own_lse.
 sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const void* Vp, cudaStream_t stream,
-                            const std::function<sepllm_status()>& beside, const float* own_ml,
-                            const float* own_acc, int own_parts);
+                            sepllm_status (*beside)(void*), void* ctx, const float* own_ml, const float* own_acc,
+                            int own_parts);
 
 }  // namespace sepllm

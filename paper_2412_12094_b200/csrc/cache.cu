@@ -1101,10 +1101,12 @@ extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int
   p.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
   // The prefix kernel (tensor cores, one CTA per SM on some of the SMs) and the own part (HBM) run side by
   // side: the second is let in while the first runs.
-  st = launch_prefix(p, q, Kp, Vp, stream, [&]() {
+  auto beside = [&]() {
     return launch_own_parts(h, scale, q, state, Kc, Vc, nullptr, own_parts, ml, acc, nullptr, stream);
-  }, ml, acc, own_parts);
-  return st;
+  };
+  using Beside = decltype(beside);
+  return launch_prefix(p, q, Kp, Vp, stream, [](void* f) { return (*static_cast<Beside*>(f))(); }, &beside, ml, acc,
+                       own_parts);
 }
 
 // grid (row blocks, Hkv).  Row v of the prefix is retained entry v of the (only) sequence.

@@ -579,6 +579,8 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
           }
           __syncwarp();
         }
+        // the slot's other warps may still read here what this one's next P would overwrite
+        asm volatile("bar.sync %0, 128;" ::"r"(1 + x) : "memory");
       } else {
         // a part: a cut unit's go to the CTA's two places (its first segment, its last one), a whole
         // unit's to a place of its own
@@ -852,8 +854,8 @@ void place_prefix_parts(PrefixParams* p, uint8_t* ws) {
 }
 
 sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const void* Vp, cudaStream_t stream,
-                            const std::function<sepllm_status()>& beside, const float* own_ml,
-                            const float* own_acc, int own_parts) {
+                            sepllm_status (*beside)(void*), void* ctx, const float* own_ml, const float* own_acc,
+                            int own_parts) {
   CUtensorMap mq, mk, mv;
   sepllm_status st;
   if ((st = make_query_map(&mq, Q, p)) != SEPLLM_OK) return st;
@@ -868,7 +870,7 @@ sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const
     p.reset_status = beside && p.pair_base == 0;
     st = d64 ? launch_prefix_d<64>(p, grid, mq, mk, mv, stream) : launch_prefix_d<128>(p, grid, mq, mk, mv, stream);
     if (st != SEPLLM_OK) return st;
-    if (beside && p.pair_base == 0 && (st = beside()) != SEPLLM_OK) return st;
+    if (beside && p.pair_base == 0 && (st = beside(ctx)) != SEPLLM_OK) return st;
     SEPLLM_CUDA_TRY(d64 ? launch_join<64>(p, grid, own_ml, own_acc, own_parts, stream)
                         : launch_join<128>(p, grid, own_ml, own_acc, own_parts, stream));
   }
@@ -939,5 +941,5 @@ extern "C" sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, co
   p.LSE = LSE;
   p.status = reinterpret_cast<int32_t*>(ws);
   p.scale_log2 = (desc->scale != 0.f ? desc->scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
-  return launch_prefix(p, Q, Kp, Vp, stream, nullptr, nullptr, nullptr, 0);
+  return launch_prefix(p, Q, Kp, Vp, stream, nullptr, nullptr, nullptr, nullptr, 0);
 }

@@ -108,6 +108,72 @@ def test_forward(B, Hq, Hkv, d, L, P, ragged):
     _check(Q, K, V, Kp, Vp, masks, plen, seq_len, O, LSE, heads=heads)
 
 
+def test_more_row_tiles_than_one_launch_takes():
+    """Sequences and lengths whose row tiles go beyond one launch of the prefix kernel, with units cut
+    between its CTAs and whole ones; sampled sequences against the oracle."""
+    g = torch.Generator(device="cuda").manual_seed(12)
+    B, Hq, Hkv, d, L, P = 300, 2, 1, 64, 130, 400      # 300 sequences x 3 tiles = 450 pairs
+    ids = inputs.token_ids(7, B, L, 0.1)
+    lens = [int(x) for x in np.random.default_rng(7).integers(0, L + 1, B)]
+    plen = [int(x) for x in np.random.default_rng(8).integers(0, P + 1, B)]
+    lens[0], lens[-1], plen[-1], plen[1] = L, L, P, 0
+    idesc, index = _index(ids, 20, 0, lens)
+    Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hkv, L, d), _normal(g, B, Hkv, L, d)
+    Kp, Vp = _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
+    O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, torch.tensor(plen, dtype=torch.int32, device="cuda"))
+    f = np.isin(ids, inputs.SEP_IDS)
+    sel = sorted({0, 1, 2, B - 1, *range(5, B, 17)})
+    _check(Q[sel], K[sel], V[sel], Kp, Vp, [orc.mask_matrix(f[b], 0, 20) for b in sel], [plen[b] for b in sel],
+           [lens[b] for b in sel], O[sel], LSE[sel])
+
+
+def test_groups_wider_than_a_row_tile():
+    """200 query heads on one kv head: a token's heads take two row tiles."""
+    g = torch.Generator(device="cuda").manual_seed(13)
+    B, Hq, d, L, P = 2, 200, 64, 3, 150
+    ids = inputs.token_ids(9, B, L, 0.2)
+    idesc, index = _index(ids, 2, 0)
+    Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, 1, L, d), _normal(g, B, 1, L, d)
+    Kp, Vp = _normal(g, 1, P, d), _normal(g, 1, P, d)
+    O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, torch.tensor([P, 7], dtype=torch.int32, device="cuda"))
+    f = np.isin(ids, inputs.SEP_IDS)
+    _check(Q, K, V, Kp, Vp, [orc.mask_matrix(f[b], 0, 2) for b in range(B)], [P, 7], [L, L], O, LSE)
+
+
+def test_many_kv_heads_and_a_short_prefix():
+    """More (kv head, pair) units than SMs, each with a single key tile."""
+    g = torch.Generator(device="cuda").manual_seed(14)
+    for B, Hq, d, L, P in ((1, 400, 64, 2, 5), (3, 180, 128, 150, 128)):
+        ids = inputs.token_ids(10, B, L, 0.2)
+        idesc, index = _index(ids, 3, 0)
+        Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hq, L, d), _normal(g, B, Hq, L, d)
+        Kp, Vp = _normal(g, Hq, P, d), _normal(g, Hq, P, d)
+        O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, None)
+        f = np.isin(ids, inputs.SEP_IDS)
+        _check(Q, K, V, Kp, Vp, [orc.mask_matrix(f[b], 0, 3) for b in range(B)], [P] * B, [L] * B, O, LSE,
+               heads=[0, 1, 77, Hq - 1])
+
+
+def test_repeated_calls_without_waiting_use_one_workspace():
+    """Calls of different prefix lengths back to back on one workspace: each gives what it gives alone."""
+    g = torch.Generator(device="cuda").manual_seed(15)
+    B, Hq, Hkv, d, L, P = 2, 8, 2, 128, 300, 900
+    ids = inputs.token_ids(11, B, L, 0.1)
+    idesc, index = _index(ids, 32, 0)
+    Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hkv, L, d), _normal(g, B, Hkv, L, d)
+    Kp, Vp = _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
+    plens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([900, 10], [0, 0], [333, 900], [128, 129])]
+    want = [_run(Q, K, V, idesc, index, Kp, Vp, p) for p in plens]
+    desc = api.AttnDesc(B, Hq, Hkv, d, L, 0.0, 0)
+    ws = api.alloc_bytes(api.sepllm_attn_prefix_workspace_bytes(desc, idesc, P))
+    outs = [(torch.empty_like(Q), torch.empty((B, Hq, L), device="cuda")) for _ in plens]
+    for _ in range(10):
+        for p, (O, LSE) in zip(plens, outs):
+            api.sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, p, O, LSE, ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) for a, b in zip(outs, want))
+
+
 def test_initial_tokens_of_their_own_and_a_scale():
     g = torch.Generator(device="cuda").manual_seed(1)
     ids = inputs.token_ids(3, 2, 150, 0.1)

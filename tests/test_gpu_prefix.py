@@ -154,6 +154,47 @@ def test_equals_decode_of_caches_that_carry_the_prefix_themselves():
     assert (lse - lse2).abs().max() <= TOL_LSE and (o.float() - o2.float()).abs().max() <= 2 * TOL_O["max_abs"]
 
 
+@pytest.mark.parametrize("Hkv,Hq,B,P", [(400, 400, 2, 3), (1, 16, 2600, 140), (200, 200, 300, 130)])
+def test_more_units_than_sms(Hkv, Hq, B, P):
+    """Many kv heads, or so many sequences that one kv head has more row tiles than a launch takes:
+    units that one CTA walks in full leave parts of their own."""
+    g = torch.Generator(device="cuda").manual_seed(Hkv)
+    rng = np.random.default_rng(Hkv)
+    runs, plen = rng.integers(0, 12, B), rng.integers(0, P + 1, B)
+    cache = Cache(g, B, Hkv, Hq, 64, 0, 3, 2, 12, runs.tolist())
+    q, Kp, Vp = _normal(g, B, Hq, 64), _normal(g, Hkv, P, 64), _normal(g, Hkv, P, 64)
+    o, lse = _decode(cache, P, q, Kp, Vp, torch.from_numpy(plen.astype(np.int32)).cuda())
+    rows = [(int(rng.integers(0, B)), int(rng.integers(0, Hq))) for _ in range(150)] + [(B - 1, Hq - 1), (0, 0)]
+    _check_decode(cache, q, Kp, Vp, plen, o, lse, rows=rows)
+
+
+def test_back_to_back_calls_on_one_workspace():
+    """Update, decode, update, decode without waiting in between, the caches' sizes and the prefix
+    lengths changing: each decode gives what it gives when waited for."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    B, Hkv, Hq, d, P, steps = 40, 2, 8, 128, 600, 12
+    Kp, Vp = _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
+    k, v, q = _normal(g, steps, B, Hkv, d), _normal(g, steps, B, Hkv, d), _normal(g, steps, B, Hq, d)
+    ids = torch.from_numpy(inputs.decode_stream_ids(9, B, steps, 0.3).T.copy()).cuda()
+    plen = torch.randint(0, P + 1, (steps, B), generator=g, device="cuda").to(torch.int32)
+    outs = []
+    for wait in (True, False):
+        cache = Cache(g, B, Hkv, Hq, d, 1, 4, 3, 10, [0] * B)
+        desc = cache.desc
+        cache.Kc.zero_(), cache.Vc.zero_()
+        ws = api.alloc_bytes(api.sepllm_decode_prefix_workspace_bytes(desc, P))
+        o, lse = torch.empty((steps, B, Hq, d), dtype=BF, device="cuda"), torch.empty((steps, B, Hq), device="cuda")
+        api.sepllm_cache_init(desc, cache.state)
+        for t in range(steps):
+            api.sepllm_cache_update(desc, cache.state, cache.Kc, cache.Vc, ids[t], inputs.SEP_IDS, k[t], v[t])
+            api.sepllm_decode_prefix(desc, P, 0.0, q[t], cache.state, cache.Kc, cache.Vc, Kp, Vp, plen[t], o[t], lse[t], ws)
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        outs.append((o, lse))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
 def test_sharp_scores_and_growing_maxima():
     """Scores of many hundreds, rising along the prefix, so that the reference exponent moves often."""
     g = torch.Generator(device="cuda").manual_seed(6)
