@@ -81,6 +81,13 @@ __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+// Named barriers 1 to 15 of the CTA: `threads` of them, all lanes of the warps that take part.
+__device__ __forceinline__ void named_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ void named_arrive(int id, int threads) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
 // One arrival for the whole warp, after every lane has reached this point (lanes make their own
 // tensor-memory stores visible with tcgen05.wait::st / fence::before_thread_sync before calling).
 __device__ __forceinline__ void mbar_arrive_warp(uint64_t* bar) {

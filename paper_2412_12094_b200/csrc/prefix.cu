@@ -150,10 +150,9 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   uint64_t* bar_g = bars + 12;     //       V of the last tile landed: clear the rows behind the prefix
   uint64_t* bar_z = bars + 13;     //       they are cleared
   uint64_t* bar_d = bars + 14;     // [2]   every product and arrival of slot x done
-  uint64_t* bar_t = bars + 16;     // [2]   slot x may run its exponentials
-  uint64_t* bar_f = bars + 18;     // [NST] ring stage full
+  uint64_t* bar_f = bars + 16;     // [NST] ring stage full
   uint64_t* bar_r = bar_f + NST;   // [NST] ring stage free (both slots)
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 18 + 2 * NST);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 16 + 2 * NST);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
   int* s_warp = reinterpret_cast<int*>(tmem_slot + 4);   // [12] key tiles per warp of the scan
   int* s_start = s_warp + 12;                            // [2] pair and offset where the run starts
@@ -172,7 +171,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_q + i, 1); mbar_init(bar_qe + i, 1); mbar_init(bar_s + i, 1);
       mbar_init(bar_sl + i, 4); mbar_init(bar_p + i, 4); mbar_init(bar_pv + i, 1);
-      mbar_init(bar_d + i, 1); mbar_init(bar_t + i, 4);
+      mbar_init(bar_d + i, 1);
     }
     mbar_init(bar_g, 1);
     mbar_init(bar_z, 1);
@@ -415,7 +414,6 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     const uint32_t tO = tmem + lane_base + (x ? C::kO1 : C::kO0);
     uint8_t* sPx = sP + x * C::kPTile;
     int n_s = 0;              // S tiles taken
-    uint32_t ph_t = 0;        // phase of bar_t
     int cut = -1;
     for (int n = 0; next_segment<true>(sg, tab, p.pairs); ++n) {
       // the row: sequence b, token t, head g of the group
@@ -476,8 +474,9 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         // row sum takes the unrounded values
         // The slots take turns at this block: side by side they halve each other's rate at the
         // special-function unit (16 a clock and SM), in turn one slot's exponentials run under the
-        // other's loads, maxima and stores.
-        if (x == 1 ? j < n_both : j > 0 && j < n_both) { wait(bar_t + x, ph_t); ph_t ^= 1; }
+        // other's loads, maxima and stores.  Warps 4 + i and 8 + i share a scheduler and its part of that
+        // unit, so the turn passes between these two, over named barriers (mbarriers: 500 cycles a turn).
+        if (x == 1 ? j < n_both : j > 0 && j < n_both) named_sync(x == 0 ? 7 + (warp & 3) : 3 + (warp & 3), 64);
         const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
         const unsigned long long scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
         const unsigned long long negm2 = pack_f32x2(neg_m, neg_m);
@@ -493,7 +492,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
             sreg[c][e >> 1] = pack_bf16(p0, p1);
           }
         const float2 sm = unpack_f32x2(add_f32x2(add_f32x2(ps2[0], ps2[1]), add_f32x2(ps2[2], ps2[3])));
-        if (x == 0 ? j < n_both : j + 1 < n_both) mbar_arrive_warp(bar_t + (x ^ 1));
+        if (x == 0 ? j < n_both : j + 1 < n_both) named_arrive(x == 0 ? 3 + (warp & 3) : 7 + (warp & 3), 64);
         l_sum = l_sum * corr + (sm.x + sm.y);
         // P V of the slot's previous tile is complete: the buffer of P is free and O_x is at rest
         if (j > 0) {
@@ -580,7 +579,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
           __syncwarp();
         }
         // the slot's other warps may still read here what this one's next P would overwrite
-        asm volatile("bar.sync %0, 128;" ::"r"(1 + x) : "memory");
+        named_sync(1 + x, 128);
       } else {
         // a part: a cut unit's go to the CTA's two places (its first segment, its last one), a whole
         // unit's to a place of its own
@@ -823,12 +822,12 @@ bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, b
   p->max_ctas = kSmCount;
   if (own_us > 0.0) {
     // The own part runs on the SMs that the prefix kernel leaves, and on all of them when it is done.
-    // With n CTAs the prefix takes 8 us and 2.4 us for each pair of row tiles and key tile of a CTA
+    // With n CTAs the prefix takes 8 us and 2.1 us for each pair of row tiles and key tile of a CTA
     // (measured); the own part, bound by HBM, loses nothing while it has four fifths of the SMs.
     const double steps = double(launch_pairs(*p)) * Hkv * p->key_tiles * (p->alternate ? 0.5 : 1.0);
     double best = 1e300;
     for (int n = 4; n <= kSmCount; n += 4) {
-      const double t = 8.0 + 2.4 * std::ceil(steps / n), rate = std::min(1.0, 1.25 * (kSmCount - n) / kSmCount);
+      const double t = 8.0 + 2.1 * std::ceil(steps / n), rate = std::min(1.0, 1.25 * (kSmCount - n) / kSmCount);
       const double total = rate * t >= own_us ? t : own_us + (1.0 - rate) * t;
       if (total < best) { best = total; p->max_ctas = n; }
     }
