@@ -658,12 +658,12 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join(const PrefixParams p
 #pragma unroll 8
   for (int i = sp; i < n_pfx; i += SPLIT) {
     const float2 v = pml[place(i) * 128];
-    mm = fmaxf(mm, v.y > 0.f ? v.x : -INFINITY);
+    mm = fmaxf(mm, v.y != 0.f ? v.x : -INFINITY);
   }
 #pragma unroll 4
   for (int i = sp; i < n_own; i += SPLIT) {
     const float2 v = oml[i];
-    mm = fmaxf(mm, v.y > 0.f ? v.x : -INFINITY);
+    mm = fmaxf(mm, v.y != 0.f ? v.x : -INFINITY);
   }
   float lo = -INFINITY;
   if (p.own_lse && here && sp == 0) { lo = p.own_lse[row] * 1.4426950408889634f; mm = fmaxf(mm, lo); }
@@ -672,7 +672,7 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join(const PrefixParams p
 #pragma unroll
   for (int c = 0; c < CPW; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](float2 ml, const float4* v, size_t step) {
-    const bool any = ml.y > 0.f;
+    const bool any = ml.y != 0.f;   // (a NaN is no empty part: it goes through to the output)
     const float w = any ? ex2(ml.x - mm) : 0.f;
     l += any ? ml.y * w : 0.f;
 #pragma unroll
@@ -714,7 +714,8 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join(const PrefixParams p
 #pragma unroll
     for (int k = 0; k < SPLIT; ++k) {
       const float2 ml = s_ml[threadIdx.x + 32 * k];
-      const float w = ml.y > 0.f ? ex2(ml.x - m) : 0.f;
+      if (!(ml.y != 0.f)) continue;
+      const float w = ex2(ml.x - m);
       ls += ml.y * w;
 #pragma unroll
       for (int c = 0; c < CPW; ++c) {
@@ -727,13 +728,13 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join(const PrefixParams p
 #pragma unroll
     for (int c = 0; c < CPW; ++c) acc[c] = sum[c];
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;   // a row that sees no key at all: 0, log-sum-exp -inf
+  const float inv = l != 0.f ? 1.f / l : 0.f;   // a row that sees no key at all: 0, log-sum-exp -inf
 #pragma unroll
   for (int c = 0; c < CPW; ++c)
     if ((col4 + c) * 4 < p.d)
       *reinterpret_cast<uint2*>(p.O + row * p.d + (col4 + c) * 4) =
           make_uint2(pack_bf16(acc[c].x * inv, acc[c].y * inv), pack_bf16(acc[c].z * inv, acc[c].w * inv));
-  if (p.LSE && col4 == 0) p.LSE[row] = l > 0.f ? (mm + log2f(l)) * 0.6931471805599453f : -INFINITY;
+  if (p.LSE && col4 == 0) p.LSE[row] = l != 0.f ? (mm + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <int D>

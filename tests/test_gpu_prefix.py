@@ -168,6 +168,28 @@ def test_more_units_than_sms(Hkv, Hq, B, P):
     _check_decode(cache, q, Kp, Vp, plen, o, lse, rows=rows)
 
 
+def test_non_finite_inputs_reach_the_rows_that_see_them_and_no_others():
+    g = torch.Generator(device="cuda").manual_seed(10)
+    B, Hkv, Hq, d, P = 5, 2, 4, 64, 300
+    cache = Cache(g, B, Hkv, Hq, d, 0, 4, 3, 20, [7, 0, 5, 0, 9])
+    q, Kp, Vp = _normal(g, B, Hq, d), _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
+    plen = torch.tensor([300, 300, 0, 0, 129], dtype=torch.int32, device="cuda")
+    want = _decode(cache, P, q, Kp, Vp, plen)
+    q2 = q.clone()
+    q2[0, 1] = float("nan")      # a query that sees both parts, one the prefix alone, one its cache alone
+    q2[1, 2, 5] = float("nan")
+    q2[2, 0, 7] = float("inf")
+    o, lse = _decode(cache, P, q2, Kp, Vp, plen)
+    hit = torch.zeros((B, Hq), dtype=torch.bool, device="cuda")
+    hit[0, 1] = hit[1, 2] = hit[2, 0] = True
+    assert torch.isnan(o[hit]).all() and torch.isnan(lse[0, 1]) and torch.isnan(lse[1, 2])
+    assert torch.equal(o[~hit], want[0][~hit]) and torch.equal(lse[~hit], want[1][~hit])
+    Kp[1, 200] = float("nan")    # a key that the first two sequences see, and heads 2 and 3 only
+    o, lse = _decode(cache, P, q, Kp, Vp, plen)
+    assert torch.isnan(o[:2, 2:]).all() and torch.isnan(lse[:2, 2:]).all()
+    assert torch.equal(o[2:], want[0][2:]) and torch.equal(o[:2, :2], want[0][:2, :2])
+
+
 def test_back_to_back_calls_on_one_workspace():
     """Update, decode, update, decode without waiting in between, the caches' sizes and the prefix
     lengths changing: each decode gives what it gives when waited for."""
