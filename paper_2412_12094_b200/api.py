@@ -301,15 +301,19 @@ _ROPE_VIEWS = struct.Struct("=" + "Qqqqii" * 3)   # three sepllm_rope_view
 
 
 def _rope_views(desc, tensors, what, device=None):
+    """The views of (q, k, v), or of inputs and outputs, one bytes object per three tensors."""
+    B, L, d = desc.B, desc.L, desc.d
+    q_shape, k_shape = (B, desc.Hq, L, d), (B, desc.Hkv, L, d)
     vals = []
-    for t, h in zip(tensors, (desc.Hq, desc.Hkv, desc.Hkv)):
+    for i, t in enumerate(tensors):
         if t is None:
             vals += (0, 0, 0, 0, 0, 0)
             continue
-        if t.shape != (desc.B, h, desc.L, desc.d):
-            raise ValueError(f"{what}: shape {tuple(t.shape)}, the descriptor says {(desc.B, h, desc.L, desc.d)}")
         sb, sh, sl, se = t.stride()
         dtype = _ROPE_DTYPES.get(t.dtype)
+        if t.shape != (k_shape if i % 3 else q_shape):
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, the descriptor says "
+                             f"{k_shape if i % 3 else q_shape}")
         if dtype is None or se != 1:
             raise ValueError(f"{what}: bf16 or fp32 with contiguous head vectors, not {t.dtype} with strides "
                              f"{t.stride()}")
@@ -317,29 +321,31 @@ def _rope_views(desc, tensors, what, device=None):
             raise ValueError(f"{what}: tensor on {t.device}, current device is cuda:{device}: make the tensors' "
                              "device current for the call")
         vals += (t.data_ptr(), sb, sh, sl, dtype, 0)
-    return _ROPE_VIEWS.pack(*vals)
+    return [_ROPE_VIEWS.pack(*vals[i:i + 18]) for i in range(0, len(vals), 18)]
 
 
-def _rope(fn, where, desc, positions, ins, outs):
+def _rope(fn, where, desc, positions, tensors):
     device = torch.cuda.current_device()
-    pos, = _addresses(where, (positions,))
-    if positions is not None and (positions.dtype != torch.int64
-                                  or positions.numel() < (desc.B - 1) * desc.pos_stride + desc.L):
-        raise ValueError(f"{where}: positions are contiguous int64, pos_stride elements from row to row")
-    _check(fn(C.byref(desc), pos, _rope_views(desc, ins, where, device), _rope_views(desc, outs, where, device),
-              torch._C._cuda_getCurrentRawStream(device)), where)
+    pos = 0
+    if positions is not None:
+        pos, = _addresses(where, (positions,))
+        if positions.dtype != torch.int64 or positions.numel() < (desc.B - 1) * desc.pos_stride + desc.L:
+            raise ValueError(f"{where}: positions are contiguous int64, pos_stride elements from row to row")
+    ins, outs = _rope_views(desc, tensors, where, device)
+    _check(fn(C.byref(desc), pos, ins, outs, torch._C._cuda_getCurrentRawStream(device)), where)
 
 
 def sepllm_rope_fwd(desc: RopeDesc, positions, q, k, v, q_out, k_out, v_out):
     """Rotates q and k and copies v.  Every tensor is [B][H][L][d] with any strides (the last one 1), so a
     slice of a fused projection goes in as qkv.view(B, L, Hq + 2 * Hkv, d).transpose(1, 2).split(...);
     a tensor and its output may both be None.  positions: int64 [B][L] (see desc.pos_stride) or None."""
-    _rope(lib().sepllm_rope_fwd, "sepllm_rope_fwd", desc, positions, (q, k, v), (q_out, k_out, v_out))
+    _rope(lib().sepllm_rope_fwd, "sepllm_rope_fwd", desc, positions, (q, k, v, q_out, k_out, v_out))
 
 
 def sepllm_rope_bwd(desc: RopeDesc, positions, dq_out, dk_out, dv_out, dq, dk, dv):
     """Gradients of sepllm_rope_fwd's inputs from those of its outputs."""
-    _rope(lib().sepllm_rope_bwd, "sepllm_rope_bwd", desc, positions, (dq_out, dk_out, dv_out), (dq, dk, dv))
+    _rope(lib().sepllm_rope_bwd, "sepllm_rope_bwd", desc, positions,
+          (dq_out, dk_out, dv_out, dq, dk, dv))
 
 
 # ---------------------------------------------------------------- cache
