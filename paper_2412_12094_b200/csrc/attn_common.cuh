@@ -198,6 +198,7 @@ struct PrefixParams {
   int whole_parts;              // 1: units that one CTA walks in full leave a part too
   int pair_base, pairs;         // pairs of row tiles of this launch
   int max_ctas;
+  double est_us;                // estimated time of a decode's prefix and own part together
   int reset_status;             // 1: the kernel starts the call (a decode) and resets its status word
   float scale_log2;
   const int32_t* prefix_len;    // [B] or null (P for all)

@@ -533,13 +533,21 @@ constexpr int decode_smem_bytes() {
 // status null: the kernel runs beside the prefix kernel launched before it (which writes the status
 // word) and shares no memory with it; its last CTA ends only when that kernel has, so that what is
 // launched next finds both complete.
-template <int D, bool ROPE, bool WIDE>
+//
+// PFX: the entries are those of a shared prefix, rows [0, prefix_len[b]) of Kp, Vp, followed by the
+// sequence's own.
+struct SharedPrefix {
+  const __nv_bfloat16 *Kp, *Vp;
+  const int32_t* prefix_len;  // null: P for all
+  int P;
+};
+template <int D, bool ROPE, bool WIDE, bool PFX>
 __global__ void __launch_bounds__(kDecThreads, 3)   // three CTAs per SM: at most 168 registers
 decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __restrict__ q_in,
              const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ Kc,
              const __nv_bfloat16* __restrict__ Vc, float* __restrict__ part_ml,
              float* __restrict__ part_acc, int splits, const float2* __restrict__ rope,
-             int32_t* __restrict__ status) {
+             int32_t* __restrict__ status, const SharedPrefix pfx) {
   constexpr int CH = D / 8;                 // 16-byte chunks per row
   constexpr int ROWB = D * 2;               // bytes per row
   constexpr int TILEB = kDecTile * ROWB;    // bytes of one K (or V) tile
@@ -555,7 +563,8 @@ decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __res
   if (status && tid == 0 && (split | hk | b) == 0) *status = SEPLLM_OK;
   CacheView cv = cache_view(const_cast<uint8_t*>(state), h);
   const sepllm_cache_seq sq = cv.seq[b];
-  const int size_run = sq.size_init + sq.size_sep + sq.size_win;
+  const int plen = !PFX ? 0 : pfx.prefix_len ? max(0, min(pfx.P, pfx.prefix_len[b])) : pfx.P;
+  const int size_run = plen + sq.size_init + sq.size_sep + sq.size_win;
   const int per = ((size_run + splits - 1) / splits + kDecTile - 1) / kDecTile * kDecTile;
   const int v0 = split * per, v1 = min(size_run, v0 + per);
   const int n_tiles = (v1 > v0) ? (v1 - v0 + kDecTile - 1) / kDecTile : 0;
@@ -605,11 +614,19 @@ decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __res
       const int r = pss * RPP + crow;
       const int v = vbase + r;
       const bool valid = v < v1;
-      const int slot = virtual_to_slot(valid ? v : v1 - 1, sq, d);
       const uint32_t off = uint32_t(r) * ROWB + (uint32_t(cch ^ (r & 7)) << 4);
-      const size_t goff = size_t(slot) * ROWB + cch * 16;
-      cp_async16(sK + off, Kp + goff, valid ? 16u : 0u);
-      cp_async16(sV + off, Vp + goff, valid ? 16u : 0u);
+      const int vr = valid ? v : v1 - 1;
+      const uint8_t *ks = Kp, *vs = Vp;
+      size_t goff;
+      if (PFX && vr < plen) {
+        ks = reinterpret_cast<const uint8_t*>(pfx.Kp);
+        vs = reinterpret_cast<const uint8_t*>(pfx.Vp);
+        goff = (size_t(hk) * pfx.P + vr) * ROWB + cch * 16;
+      } else {
+        goff = size_t(virtual_to_slot(vr - plen, sq, d)) * ROWB + cch * 16;
+      }
+      cp_async16(sK + off, ks + goff, valid ? 16u : 0u);
+      cp_async16(sV + off, vs + goff, valid ? 16u : 0u);
     }
   };
 
@@ -747,8 +764,8 @@ decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __res
     wait_for_prior();
 }
 
-// grid (Hq, B), D threads.
-template <int D>
+// grid (Hq, B), D threads.  NAN_THROUGH: a row whose sum is NaN gives NaN, not the 0 of an empty row.
+template <int D, bool NAN_THROUGH>
 __global__ void decode_combine(sepllm_cache_header h, const float* __restrict__ part_ml,
                                const float* __restrict__ part_acc, int splits,
                                __nv_bfloat16* __restrict__ o, float* __restrict__ lse) {
@@ -764,8 +781,9 @@ __global__ void decode_combine(sepllm_cache_header h, const float* __restrict__ 
     aa += part_acc[(u0 + s) * D + e] * sc;
   }
   const size_t row = size_t(b) * h.desc.Hq + hq;
-  o[row * D + e] = __float2bfloat16(ll > 0.f ? aa / ll : 0.f);
-  if (lse && e == 0) lse[row] = (ll > 0.f) ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
+  const bool any = NAN_THROUGH ? ll != 0.f : ll > 0.f;
+  o[row * D + e] = __float2bfloat16(any ? aa / ll : 0.f);
+  if (lse && e == 0) lse[row] = any ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
 }
 
 // (cos, sin) of position * base^(-2i/D) for every position a cache entry can have and every
@@ -781,11 +799,11 @@ __global__ void rope_table_kernel(float2* __restrict__ table, int positions, int
   table[idx] = make_float2(cs, sn);
 }
 
-static int decode_splits(const sepllm_cache_desc* d) {
+static int decode_splits(const sepllm_cache_desc* d, int P = 0) {
   // about four CTAs per SM over the whole grid, each with at least 256 rows (64 per warp)
   const int units = d->B * d->Hkv;
   int s = (148 * 4 + units - 1) / units;
-  const int max_by_rows = (d->c + 255) / 256;
+  const int max_by_rows = int((int64_t(d->c) + P + 255) / 256);
   if (s > max_by_rows) s = max_by_rows;
   if (s < 1) s = 1;
   if (s > 64) s = 64;
@@ -933,25 +951,24 @@ extern "C" sepllm_status sepllm_decode_workspace_bytes(const sepllm_cache_desc* 
   return SEPLLM_OK;
 }
 
-template <int D, bool ROPE, bool WIDE>
+template <int D, bool ROPE, bool WIDE, bool PFX = false>
 static sepllm_status launch_decode(const sepllm_cache_header& h, float scale_log2, const void* q,
                                    const void* state, const void* Kc, const void* Vc, float* ml,
                                    float* acc, int splits, const float2* rope, int32_t* status,
-                                   cudaStream_t stream) {
+                                   cudaStream_t stream, const SharedPrefix& pfx = SharedPrefix{}) {
   constexpr int smem = decode_smem_bytes<D>();
   static_assert(smem >= (kDecThreads / 32) * 16 * (8 + D * 4), "partials fit in the stage buffers");
-  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(decode_split<D, ROPE, WIDE>,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  auto kernel = decode_split<D, ROPE, WIDE, PFX>;
+  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   const dim3 grid(splits, h.desc.Hkv, h.desc.B);
   auto qb = static_cast<const __nv_bfloat16*>(q), kb = static_cast<const __nv_bfloat16*>(Kc),
        vb = static_cast<const __nv_bfloat16*>(Vc);
   auto sb = static_cast<const uint8_t*>(state);
   if (status)
-    decode_split<D, ROPE, WIDE><<<grid, kDecThreads, smem, stream>>>(h, scale_log2, qb, sb, kb, vb, ml, acc, splits,
-                                                                     rope, status);
+    kernel<<<grid, kDecThreads, smem, stream>>>(h, scale_log2, qb, sb, kb, vb, ml, acc, splits, rope, status, pfx);
   else
-    SEPLLM_CUDA_TRY(launch_overlapped(decode_split<D, ROPE, WIDE>, grid, kDecThreads, smem, stream, h, scale_log2,
-                                      qb, sb, kb, vb, ml, acc, splits, rope, status));
+    SEPLLM_CUDA_TRY(launch_overlapped(kernel, grid, kDecThreads, smem, stream, h, scale_log2, qb, sb, kb, vb, ml, acc,
+                                      splits, rope, status, pfx));
   return SEPLLM_OK;
 }
 
@@ -981,6 +998,20 @@ static sepllm_status launch_own_parts(const sepllm_cache_header& h, float scale,
                                             splits, rope, status, stream);
 }
 
+template <bool NAN_THROUGH>
+static sepllm_status launch_combine(const sepllm_cache_header& h, const float* ml, const float* acc, int splits,
+                                    void* o, float* lse, cudaStream_t stream) {
+  const sepllm_cache_desc* desc = &h.desc;
+  if (desc->d == 128)
+    decode_combine<128, NAN_THROUGH><<<dim3(desc->Hq, desc->B), 128, 0, stream>>>(
+        h, ml, acc, splits, static_cast<__nv_bfloat16*>(o), lse);
+  else
+    decode_combine<64, NAN_THROUGH><<<dim3(desc->Hq, desc->B), 64, 0, stream>>>(
+        h, ml, acc, splits, static_cast<__nv_bfloat16*>(o), lse);
+  SEPLLM_CUDA_TRY(cudaGetLastError());
+  return SEPLLM_OK;
+}
+
 static sepllm_status decode_impl(const sepllm_cache_desc* desc, float scale, const void* q,
                                  const void* state, const void* Kc, const void* Vc,
                                  const float2* rope, void* o, float* lse, void* workspace,
@@ -1003,14 +1034,7 @@ static sepllm_status decode_impl(const sepllm_cache_desc* desc, float scale, con
   float* acc = reinterpret_cast<float*>(ws + kAlign + align_up(units * 2 * sizeof(float)));
   st = launch_own_parts(h, scale, q, state, Kc, Vc, rope, splits, ml, acc, reinterpret_cast<int32_t*>(ws), stream);
   if (st != SEPLLM_OK) return st;
-  if (desc->d == 128)
-    decode_combine<128><<<dim3(desc->Hq, desc->B), 128, 0, stream>>>(
-        h, ml, acc, splits, static_cast<__nv_bfloat16*>(o), lse);
-  else
-    decode_combine<64><<<dim3(desc->Hq, desc->B), 64, 0, stream>>>(
-        h, ml, acc, splits, static_cast<__nv_bfloat16*>(o), lse);
-  SEPLLM_CUDA_TRY(cudaGetLastError());
-  return SEPLLM_OK;
+  return launch_combine<false>(h, ml, acc, splits, o, lse, stream);
 }
 
 extern "C" sepllm_status sepllm_decode(const sepllm_cache_desc* desc, float scale, const void* q,
@@ -1060,15 +1084,42 @@ static double own_part_us(const sepllm_cache_desc* d) {
   return double(d->B) * d->Hkv * run * d->d * 4 / 6.2e6;
 }
 
+// How a call is carried out.  direct: the decode kernel reads the prefix once per sequence (and
+// joins with the decode's combine kernel); otherwise the prefix kernel reads it once for all, beside
+// the own part.  Sharing costs about 14 us of launches, start and join, so it waits for a prefix that
+// is long or read by many: direct takes 6 us and its bytes at 6.2 TB/s.  Both measured (us, direct /
+// shared; 32 heads on 8 of 128, 150 own entries): 1 sequence x 1000 entries 8.4 / 14.3, 1 x 8000 12.5 /
+// 23.7, 4 x 2000 11.1 / 15.5, 4 x 8000 24.9 / 23.6, 4 x 32 000 79 / 39, 16 x 1000 16.8 / 15.2, 64 x 1000
+// 43 / 25, 64 x 4000 125 / 31; 12 heads of 64: 8 x 1000 8.4 / 13.3, 8 x 8000 29.8 / 24.4.  The rule took
+// the faster form in each of these.
+struct PrefixDecodePlan {
+  bool direct;
+  int own_parts;
+  PrefixParams p;
+  size_t off_acc, off_pfx, bytes;
+};
+static sepllm_status plan_decode_prefix(const sepllm_cache_desc* desc, int P, PrefixDecodePlan* plan) {
+  const double own_us = own_part_us(desc);
+  plan->p = PrefixParams{};
+  if (P < 1) return SEPLLM_INVALID_ARG;
+  if (!plan_prefix(&plan->p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P, true, own_us)) return SEPLLM_UNSUPPORTED;
+  const double direct_us = 6.0 + own_us + double(desc->B) * desc->Hkv * P * desc->d * 4 / 6.2e6;
+  plan->direct = direct_us < plan->p.est_us + 6.0;
+  plan->own_parts = decode_splits(desc, plan->direct ? P : 0);
+  plan->off_acc = kAlign + align_up(size_t(desc->B) * desc->Hq * plan->own_parts * 2 * sizeof(float));
+  plan->off_pfx = kAlign + own_part_bytes(desc, plan->own_parts);
+  plan->bytes = plan->off_pfx + (plan->direct ? 0 : prefix_part_bytes(plan->p));
+  return SEPLLM_OK;
+}
+
 extern "C" sepllm_status sepllm_decode_prefix_workspace_bytes(const sepllm_cache_desc* desc, int32_t P,
                                                               size_t* bytes) {
   sepllm_cache_header h;
   sepllm_status st = fill_cache_header(desc, &h);
   if (st != SEPLLM_OK) return st;
-  if (P < 1) return SEPLLM_INVALID_ARG;
-  PrefixParams p{};
-  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P, true, own_part_us(desc))) return SEPLLM_UNSUPPORTED;
-  if (bytes) *bytes = kAlign + own_part_bytes(desc, decode_splits(desc)) + prefix_part_bytes(p);
+  PrefixDecodePlan plan;
+  if ((st = plan_decode_prefix(desc, P, &plan)) != SEPLLM_OK) return st;
+  if (bytes) *bytes = plan.bytes;
   return SEPLLM_OK;
 }
 
@@ -1085,15 +1136,28 @@ extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int
       !aligned(prefix_len, 4))
     return SEPLLM_INVALID_ARG;
   if (desc->B > 65535 || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
-  PrefixParams p{};
-  if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, 1, desc->d, P, true, own_part_us(desc))) return SEPLLM_UNSUPPORTED;
+  PrefixDecodePlan plan;
+  if ((st = plan_decode_prefix(desc, P, &plan)) != SEPLLM_OK) return st;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  const int own_parts = decode_splits(desc);
+  const int own_parts = plan.own_parts;
   float* ml = reinterpret_cast<float*>(ws + kAlign);
-  float* acc = reinterpret_cast<float*>(
-      ws + kAlign + align_up(size_t(desc->B) * desc->Hq * own_parts * 2 * sizeof(float)));
-  place_prefix_parts(&p, ws + kAlign + own_part_bytes(desc, own_parts));
+  float* acc = reinterpret_cast<float*>(ws + plan.off_acc);
+  if (plan.direct) {
+    const SharedPrefix pfx{static_cast<const __nv_bfloat16*>(Kp), static_cast<const __nv_bfloat16*>(Vp), prefix_len, P};
+    const bool wide = desc->Hq / desc->Hkv > 8;
+    const float scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
+#define SEPLLM_DEC(D, W)                                                                                      \
+  launch_decode<D, false, W, true>(h, scale_log2, q, state, Kc, Vc, ml, acc, own_parts, nullptr,            \
+                                   reinterpret_cast<int32_t*>(ws), stream, pfx)
+    st = desc->d == 128 ? (wide ? SEPLLM_DEC(128, true) : SEPLLM_DEC(128, false))
+                        : (wide ? SEPLLM_DEC(64, true) : SEPLLM_DEC(64, false));
+#undef SEPLLM_DEC
+    if (st != SEPLLM_OK) return st;
+    return launch_combine<true>(h, ml, acc, own_parts, o, lse, stream);
+  }
+  PrefixParams& p = plan.p;
+  place_prefix_parts(&p, ws + plan.off_pfx);
   p.prefix_len = prefix_len;
   p.O = static_cast<__nv_bfloat16*>(o);
   p.LSE = lse;
@@ -1109,7 +1173,8 @@ extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int
                        own_parts);
 }
 
-// grid (row blocks, Hkv).  Row v of the prefix is retained entry v of the (only) sequence.
+// grid (row blocks, Hkv).  Row v of the prefix is retained entry v of the (only) sequence.  A copy, bound
+// by HBM: 15 001 entries of 8 x 128, 246 MB read and written, in 20 us with part of it from L2.
 template <int D>
 __global__ void __launch_bounds__(256)
 prefix_copy(sepllm_cache_header h, const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ Kc,

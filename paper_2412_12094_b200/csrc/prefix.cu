@@ -843,6 +843,7 @@ bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, b
       const double total = rate * t >= own_us ? t : own_us + (1.0 - rate) * t;
       if (total < best) { best = total; p->max_ctas = n; }
     }
+    p->est_us = std::max(best, own_us + double(Hkv) * P * d * 4 / 6.2e6);   // not below the bytes of both
     if (p->alternate && p->max_ctas > Hkv) p->max_ctas -= p->max_ctas % Hkv;   // (see n_runs)
   }
   return true;

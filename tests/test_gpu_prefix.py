@@ -78,8 +78,10 @@ def _decode(cache, P, q, Kp, Vp, plen, scale=0.0):
 SHAPES = [
     # B, Hkv, Hq, d, P
     (1, 1, 1, 64, 1), (1, 1, 1, 128, 127), (2, 2, 4, 64, 128), (3, 1, 4, 128, 129), (5, 3, 3, 64, 1000),
-    (1, 2, 32, 128, 257), (9, 2, 30, 64, 640), (33, 1, 4, 128, 300), (130, 1, 2, 64, 513), (70, 2, 8, 128, 1030),
-    (300, 1, 1, 64, 200), (64, 2, 24, 128, 260),
+    (1, 2, 32, 128, 257), (9, 2, 30, 64, 640), (33, 1, 4, 128, 300), (130, 1, 2, 64, 513), (1, 8, 32, 128, 5001),
+    # a prefix long enough, or read by enough sequences, for the kernel that shares it
+    (30, 1, 4, 128, 9000), (9, 2, 30, 64, 30000), (128, 1, 1, 64, 4001), (33, 1, 4, 128, 8191), (130, 1, 2, 64, 4100),
+    (70, 2, 8, 128, 2050), (300, 1, 1, 64, 1920), (64, 2, 24, 128, 1999), (3, 12, 12, 64, 20011), (40, 4, 64, 128, 1500),
 ]
 
 
@@ -109,20 +111,21 @@ def test_decode_of_ragged_batches(B, Hkv, Hq, d, P):
     _check_decode(cache, q, Kp, Vp, plen, o, lse, rows=some)
 
 
-@pytest.mark.parametrize("B", [3, 40])
-def test_whole_prefix_without_lengths_and_a_scale(B):
+@pytest.mark.parametrize("B,P", [(3, 900), (40, 900), (12, 9001), (120, 2900)])
+def test_whole_prefix_without_lengths_and_a_scale(B, P):
     g = torch.Generator(device="cuda").manual_seed(3)
     cache = Cache(g, B, 2, 8, 128, 1, 4, 3, 20, [b % 20 for b in range(B)])
-    q, Kp, Vp = _normal(g, B, 8, 128), _normal(g, 2, 900, 128), _normal(g, 2, 900, 128)
-    o, lse = _decode(cache, 900, q, Kp, Vp, None, 0.31)
-    _check_decode(cache, q, Kp, Vp, [900] * B, o, lse, scale=float(np.float32(0.31)))
-    o2, lse2 = _decode(cache, 900, q, Kp, Vp, torch.full((B,), 900, dtype=torch.int32, device="cuda"), 0.31)
+    q, Kp, Vp = _normal(g, B, 8, 128), _normal(g, 2, P, 128), _normal(g, 2, P, 128)
+    o, lse = _decode(cache, P, q, Kp, Vp, None, 0.31)
+    _check_decode(cache, q, Kp, Vp, [P] * B, o, lse, scale=float(np.float32(0.31)))
+    o2, lse2 = _decode(cache, P, q, Kp, Vp, torch.full((B,), P, dtype=torch.int32, device="cuda"), 0.31)
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
 def test_rows_behind_the_longest_prefix_may_hold_anything():
     g = torch.Generator(device="cuda").manual_seed(4)
-    for B, P, n in ((4, 1000, 300), (4, 1000, 384), (80, 700, 1), (4, 130, 0)):
+    for B, P, n in ((4, 1000, 300), (4, 1000, 384), (80, 700, 1), (4, 130, 0), (80, 9000, 5000), (80, 9000, 5120),
+                    (12, 40000, 39999), (200, 4000, 0)):
         cache = Cache(g, B, 1, 4, 64, 2, 4, 3, 20, [7] * B)
         q, Kp, Vp = _normal(g, B, 4, 64), _normal(g, 1, P, 64), _normal(g, 1, P, 64)
         plen = torch.randint(0, n + 1, (B,), generator=g, device="cuda").to(torch.int32)
@@ -154,7 +157,7 @@ def test_equals_decode_of_caches_that_carry_the_prefix_themselves():
     assert (lse - lse2).abs().max() <= TOL_LSE and (o.float() - o2.float()).abs().max() <= 2 * TOL_O["max_abs"]
 
 
-@pytest.mark.parametrize("Hkv,Hq,B,P", [(400, 400, 2, 3), (1, 16, 2600, 140), (200, 200, 300, 130)])
+@pytest.mark.parametrize("Hkv,Hq,B,P", [(400, 400, 2, 3), (1, 16, 2600, 140), (200, 200, 300, 130), (1, 16, 2600, 300), (400, 400, 9, 150)])
 def test_more_units_than_sms(Hkv, Hq, B, P):
     """Many kv heads, or so many sequences that one kv head has more row tiles than a launch takes:
     units that one CTA walks in full leave parts of their own."""
@@ -168,12 +171,13 @@ def test_more_units_than_sms(Hkv, Hq, B, P):
     _check_decode(cache, q, Kp, Vp, plen, o, lse, rows=rows)
 
 
-def test_non_finite_inputs_reach_the_rows_that_see_them_and_no_others():
+@pytest.mark.parametrize("P", [300, 30000])
+def test_non_finite_inputs_reach_the_rows_that_see_them_and_no_others(P):
     g = torch.Generator(device="cuda").manual_seed(10)
-    B, Hkv, Hq, d, P = 5, 2, 4, 64, 300
+    B, Hkv, Hq, d = 5, 2, 4, 64
     cache = Cache(g, B, Hkv, Hq, d, 0, 4, 3, 20, [7, 0, 5, 0, 9])
     q, Kp, Vp = _normal(g, B, Hq, d), _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
-    plen = torch.tensor([300, 300, 0, 0, 129], dtype=torch.int32, device="cuda")
+    plen = torch.tensor([P, P, 0, 0, 129], dtype=torch.int32, device="cuda")
     want = _decode(cache, P, q, Kp, Vp, plen)
     q2 = q.clone()
     q2[0, 1] = float("nan")      # a query that sees both parts, one the prefix alone, one its cache alone
@@ -190,11 +194,12 @@ def test_non_finite_inputs_reach_the_rows_that_see_them_and_no_others():
     assert torch.equal(o[2:], want[0][2:]) and torch.equal(o[:2, :2], want[0][:2, :2])
 
 
-def test_back_to_back_calls_on_one_workspace():
+@pytest.mark.parametrize("P", [600, 4000])
+def test_back_to_back_calls_on_one_workspace(P):
     """Update, decode, update, decode without waiting in between, the caches' sizes and the prefix
     lengths changing: each decode gives what it gives when waited for."""
     g = torch.Generator(device="cuda").manual_seed(9)
-    B, Hkv, Hq, d, P, steps = 40, 2, 8, 128, 600, 12
+    B, Hkv, Hq, d, steps = 40, 2, 8, 128, 12
     Kp, Vp = _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
     k, v, q = _normal(g, steps, B, Hkv, d), _normal(g, steps, B, Hkv, d), _normal(g, steps, B, Hq, d)
     ids = torch.from_numpy(inputs.decode_stream_ids(9, B, steps, 0.3).T.copy()).cuda()
@@ -217,11 +222,12 @@ def test_back_to_back_calls_on_one_workspace():
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
 
 
-def test_sharp_scores_and_growing_maxima():
+@pytest.mark.parametrize("B,P", [(3, 2000), (100, 6000)])
+def test_sharp_scores_and_growing_maxima(B, P):
     """Scores of many hundreds, rising along the prefix, so that the reference exponent moves often."""
     g = torch.Generator(device="cuda").manual_seed(6)
-    B, P, d = 3, 2000, 64
-    cache = Cache(g, B, 1, 2, d, 0, 4, 3, 20, [0, 5, 19])
+    d = 64
+    cache = Cache(g, B, 1, 2, d, 0, 4, 3, 20, [0, 5, 19] + [1] * (B - 3))
     q = torch.ones((B, 2, d), device="cuda", dtype=BF)
     q[1] = -1
     ramp = torch.linspace(-30, 30, P, device="cuda")[None, :, None].expand(1, P, d)
@@ -229,7 +235,7 @@ def test_sharp_scores_and_growing_maxima():
     Vp = _normal(g, 1, P, d)
     o, lse = _decode(cache, P, q, Kp, Vp, None)
     kp, vp = Kp.double().cpu().numpy()[0], Vp.double().cpu().numpy()[0]
-    for b in range(B):
+    for b in range(3):
         k = np.concatenate((kp, cache.Kc[b, 0].double().cpu().numpy()[cache.slots[b]]))
         v = np.concatenate((vp, cache.Vc[b, 0].double().cpu().numpy()[cache.slots[b]]))
         ref, lref = orc.decode_attention(q[b, 0].double().cpu().numpy(), k, v)
@@ -238,9 +244,9 @@ def test_sharp_scores_and_growing_maxima():
         assert np.abs(o[b, 0].double().cpu().numpy() - ref).max() <= 2.0 ** -8 * np.abs(v).max() + TOL_O["max_abs"]
 
 
-def test_other_stream_graph_and_shared_workspace():
+@pytest.mark.parametrize("B,P", [(6, 500), (60, 5000)])
+def test_other_stream_graph_and_shared_workspace(B, P):
     g = torch.Generator(device="cuda").manual_seed(7)
-    B, P = 6, 500
     cache = Cache(g, B, 2, 8, 64, 2, 6, 5, 40, [30] * B)
     q, Kp, Vp = _normal(g, B, 8, 64), _normal(g, 2, P, 64), _normal(g, 2, P, 64)
     plen = torch.full((B,), P, dtype=torch.int32, device="cuda")

@@ -21,9 +21,11 @@ def _desc(**kw):
 def test_decode_workspace_holds_both_parts():
     d = _desc()
     own = api.sepllm_decode_workspace_bytes(d)
-    for P in (1, 127, 128, 129, 100000):
+    for P in (1, 127, 128, 129, 100000, 10 ** 7):
         n = api.sepllm_decode_prefix_workspace_bytes(d, P)
-        assert n % 256 == 0 and n >= own + 3 * 8 * (64 + 2) * 4
+        assert n % 256 == 0 and n >= own
+    big = _desc(B=200, Hkv=8, Hq=32, d=128)      # a prefix read by many: parts of the shared kernel as well
+    assert api.sepllm_decode_prefix_workspace_bytes(big, 40000) >= api.sepllm_decode_workspace_bytes(big) + (1 << 20)
     with pytest.raises(api.SepllmError) as e:
         api.sepllm_decode_prefix_workspace_bytes(d, 0)
     assert e.value.code == api.INVALID_ARG
