@@ -1174,7 +1174,7 @@ extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int
 }
 
 // grid (row blocks, Hkv).  Row v of the prefix is retained entry v of the (only) sequence.  A copy, bound
-// by HBM: 15 001 entries of 8 x 128, 246 MB read and written, in 20 us with part of it from L2.
+// by HBM: 15 001 entries of 8 x 128, 123 MB read and written, in 20 us (6.1 TB/s).
 template <int D>
 __global__ void __launch_bounds__(256)
 prefix_copy(sepllm_cache_header h, const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ Kc,
