@@ -205,7 +205,7 @@ struct PrefixParams {
   const int32_t* seq_len;       // [B] or null: rows of tokens behind it are not written
   float* part_ml;               // [part][slot][128] (reference exponent, sum)
   float* part_acc;              // [part][slot][D / 4][128 rows][4]
-  int4* unit_parts;             // [Hkv][pairs] (parts, first part, CTA of the first part)
+  int4* unit_parts;             // [Hkv][pairs] (parts, first part, CTA of the first part, row tiles)
   int32_t* cut_units;           // [CTA] the unit whose first key tiles, not all, were the CTA's; -1: none
   const float* own_O;           // the rows' own part, normalised (layout of FwdParams::O32), and its
   const float* own_lse;         // log-sum-exp [row]

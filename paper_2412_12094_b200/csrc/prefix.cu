@@ -32,7 +32,7 @@ constexpr int kMaxPairs = 128;    // pairs of row tiles per launch (their length
 template <int D>
 struct PfxCfg {
   static constexpr int NB = D / 64;               // 64-column blocks per row
-  static constexpr int NST = (D == 128) ? 3 : 8;  // ring of K and V tiles
+  static constexpr int NST = (D == 128) ? 3 : 7;  // ring of K and V tiles
   static constexpr uint32_t kTile = NB * kTileBlockBytes;
   static constexpr uint32_t kPTile = 2 * kTileBlockBytes;   // 128 rows x 128 keys
   static constexpr uint32_t kQ = 0;                         // 2 slots
@@ -66,10 +66,10 @@ __device__ __forceinline__ int seen_length(const PrefixParams& p, int b, int t0)
   if (b >= p.B || (p.seq_len && t0 >= p.seq_len[b])) return -1;
   return p.prefix_len ? max(0, min(p.P, p.prefix_len[b])) : p.P;
 }
-// Key tiles of a pair of row tiles with these longest prefixes.  A pair that sees nothing of the
+// Key tiles of a pair of row tiles whose longest prefixes are len[0] and len[1].  A pair that sees nothing of the
 // prefix still takes one (wholly masked) tile: its rows have to be finished by someone.
-__device__ __forceinline__ int pair_tiles(int2 len) {
-  const int m = max(len.x, len.y);
+__device__ __forceinline__ int pair_tiles(const int* len) {
+  const int m = max(len[0], len[1]);
   return m < 0 ? 0 : max(1, (m + kBN - 1) / kBN);
 }
 
@@ -93,12 +93,12 @@ struct Segment {
 // Advances to the next segment (false: none left).  WARP: called by all lanes of a warp, else by one
 // thread.
 template <bool WARP>
-__device__ __forceinline__ bool next_segment(Segment* sg, const int2* tab, int pairs) {
+__device__ __forceinline__ bool next_segment(Segment* sg, const int* tab, int pairs) {
   const int left = sg->left;
   int hk = sg->hk, pair = sg->pair, off = sg->j1, nt;
   if (WARP) __syncwarp();
   if (left <= 0) return false;
-  while ((nt = pair_tiles(tab[pair])) <= off) {   // finished, or without rows
+  while ((nt = pair_tiles(tab + 2 * pair)) <= off) {   // finished
     off = 0;
     if (++pair == pairs) { pair = 0; ++hk; }
   }
@@ -106,8 +106,8 @@ __device__ __forceinline__ bool next_segment(Segment* sg, const int2* tab, int p
     sg->hk = hk; sg->pair = pair; sg->j0 = off; sg->nt = nt;
     sg->j1 = min(nt, off + left);
     sg->left = left - (sg->j1 - off);
-    sg->len[0] = tab[pair].x;
-    sg->len[1] = tab[pair].y;
+    sg->len[0] = tab[2 * pair];
+    sg->len[1] = tab[2 * pair + 1];
   }
   if (WARP) __syncwarp();
   return true;
@@ -127,7 +127,7 @@ __device__ __forceinline__ bool ends_inside(const Segment* sg, int P) {
 }
 
 // One CTA: two slots of 128 query rows, walked over the segments of its run.
-//   pair mode        slot x holds row tile 2 * pair + x; both slots walk the same key tiles
+//   pair mode        slot x holds the x-th row tile of a pair; both slots walk the same key tiles
 //   alternate mode   (one row tile in all) both slots hold that tile and take the key tiles in turn,
 //                    so that one slot's softmax runs under the other's loads and products; each
 //                    slot leaves a partial result of its own
@@ -148,7 +148,8 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   uint8_t* sQ = smem + C::kQ;
   uint8_t* sP = smem + C::kP;
   uint8_t* sKV = smem + C::kKV;
-  int2* tab = reinterpret_cast<int2*>(smem + C::kTab);   // [pairs] longest prefix of each row tile
+  int* tab = reinterpret_cast<int*>(smem + C::kTab);   // [2 * pairs] longest prefix of each row tile that
+                                                       // has rows, two and two a pair
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBar);
   uint64_t* bar_q = bars;          // [2]   Q of slot x landed
   uint64_t* bar_qe = bars + 2;     // [2]   slot x has read the segment's Q for the last time
@@ -165,8 +166,9 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
   int* s_warp = reinterpret_cast<int*>(tmem_slot + 4);   // [12] key tiles per warp of the scan
   int* s_start = s_warp + 12;                            // [2] pair and offset where the run starts
-  int* s_run = s_warp + 14;                              // end of the run, tiles per run, longer runs
+  int* s_run = s_warp + 14;                              // end of the run, tiles per run, longer runs, pairs
   Segment* s_seg = reinterpret_cast<Segment*>(s_run + 4);    // [12] place of each warp in the run
+  uint8_t* s_id = reinterpret_cast<uint8_t*>(s_seg + 12);    // [2 * pairs] number of those row tiles
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const bool alt = p.alternate != 0;
@@ -201,31 +203,41 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   }
   fence_proxy_async_smem();
 
-  // longest prefix of every row tile: a warp per pair with its lanes over the sequences, or, where a
-  // tile has few of them (and there may be many tiles), a thread per pair
+  // longest prefix of every row tile: a warp per tile with its lanes over the sequences, or, where a
+  // tile has few of them (and there may be many tiles), a thread per tile
   const bool by_warp = p.bt > 8;
-  for (int i = by_warp ? warp : tid; i < p.pairs; i += by_warp ? kPfxThreads / 32 : kPfxThreads) {
-    int len[2] = {-1, -1};
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int ti = 2 * (p.pair_base + i) + x;
-      if (ti >= p.m_tiles) break;
+  for (int i = by_warp ? warp : tid; i < 2 * p.pairs; i += by_warp ? kPfxThreads / 32 : kPfxThreads) {
+    int len = -1;
+    const int ti = 2 * p.pair_base + i;
+    if (ti < p.m_tiles) {
       const RowTile rt = row_tile(p, ti);
       for (int k = by_warp ? lane : 0; k < p.bt; k += by_warp ? 32 : 1)
-        len[x] = max(len[x], seen_length(p, rt.b0 + k, rt.t0));
+        len = max(len, seen_length(p, rt.b0 + k, rt.t0));
     }
-    if (by_warp) {
-      len[0] = __reduce_max_sync(0xffffffffu, len[0]);
-      len[1] = __reduce_max_sync(0xffffffffu, len[1]);
-    }
-    if (!by_warp || lane == 0) tab[i] = make_int2(len[0], len[1]);
+    if (by_warp) len = __reduce_max_sync(0xffffffffu, len);
+    if (!by_warp || lane == 0) tab[i] = len;
   }
   __syncthreads();
+  int n_pairs = p.pairs;
+  {
+    // tiles of padding drop out, so that every pair but the last has two tiles with rows
+    const int len = tid < 2 * p.pairs ? tab[tid] : -1;
+    const uint32_t with_rows = __ballot_sync(0xffffffffu, len >= 0);
+    if (lane == 0) s_warp[warp] = __popc(with_rows);
+    __syncthreads();
+    int at = __popc(with_rows & ((1u << lane) - 1)), all = 0;
+    for (int w = 0; w < kPfxThreads / 32; ++w) {
+      if (w < warp) at += s_warp[w];
+      all += s_warp[w];
+    }
+    n_pairs = (all + 1) / 2;
+    if (len >= 0) { tab[at] = len; s_id[at] = uint8_t(tid); }
+    if (tid == 0 && all % 2) tab[all] = -1;
+    __syncthreads();
+  }
   // where the run starts: key tiles of one kv head summed over the pairs
-  const int per = (p.pairs + kPfxThreads - 1) / kPfxThreads;
-  const int i0 = min(p.pairs, tid * per), i1 = min(p.pairs, i0 + per);
-  int mine = 0;
-  for (int i = i0; i < i1; ++i) mine += pair_tiles(tab[i]);
+  static_assert(2 * kMaxPairs <= kPfxThreads && 2 * kMaxPairs <= 256, "a thread per row tile, its number in a byte");
+  const int mine = tid < n_pairs ? pair_tiles(tab + 2 * tid) : 0;
   int incl = mine;
 #pragma unroll
   for (int k = 1; k < 32; k <<= 1) {
@@ -251,12 +263,10 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   const int run1 = blk < n_runs ? run0 + run + (blk < longer) : 0;
   const int hk0 = per_head > 0 ? run0 / per_head : 0, in_head = run0 - hk0 * per_head;
   if (run0 < run1 && in_head >= before && in_head < before + mine) {
-    int at = before, i = i0;
-    while (at + pair_tiles(tab[i]) <= in_head) at += pair_tiles(tab[i++]);
-    s_start[0] = i;
-    s_start[1] = in_head - at;
+    s_start[0] = tid;
+    s_start[1] = in_head - before;
   }
-  if (tid == 0) { s_run[0] = run1; s_run[1] = run; s_run[2] = longer; }
+  if (tid == 0) { s_run[0] = run1; s_run[1] = run; s_run[2] = longer; s_run[3] = n_pairs; }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -286,7 +296,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     if (warp == 0 && lane == 0) {
       // ---------------- TMA producer ----------------
       int at = 0;  // tiles loaded
-      for (int n = 0; next_segment<false>(sg, tab, p.pairs); ++n) {
+      for (int n = 0; next_segment<false>(sg, tab, s_run[3]); ++n) {
         const int hk = sg->hk, j0 = sg->j0, n_tiles = sg->j1 - j0;
         for (int i = 0; i < 2 * n_tiles; ++i, ++at) {
           // 0: K(0), odd: K((i + 1) / 2), even: V(i / 2 - 1), and the last one V(n - 1)
@@ -303,7 +313,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               if (alt ? x == 1 : slot_tiles(sg, false, x) == 0) continue;   // a slot without work loads nothing
-              const RowTile rt = row_tile(p, 2 * (p.pair_base + sg->pair) + x);
+              const RowTile rt = row_tile(p, 2 * p.pair_base + s_id[2 * sg->pair + x]);
               mbar_expect_tx(bar_q + x, uint32_t(NB * rows) * 128u);
               for (int nb = 0; nb < NB; ++nb)
                 tma_load_5d(sQ + x * C::kTile + nb * kTileBlockBytes, &mapQ, bar_q + x, nb * 64, rt.g0, rt.t0,
@@ -326,7 +336,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
       const uint32_t tS = tmem + (x ? C::kS1 : C::kS0), tO = tmem + (x ? C::kO1 : C::kO0);
       uint32_t ph_sl = 0, ph_p = 0, ph_q = 0, ph_z = 0;   // phases
       int at0 = 0;                                        // tiles loaded for earlier segments
-      for (int n = 0; next_segment<false>(sg, tab, p.pairs); ++n) {
+      for (int n = 0; next_segment<false>(sg, tab, s_run[3]); ++n) {
         const int n_tiles = sg->j1 - sg->j0, n_mine = slot_tiles(sg, alt, x);
         const bool clear_v = ends_inside(sg, p.P);
         // the slot that uses the last tile (the first such one) has its V cleared
@@ -397,7 +407,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     } else if (warp == 3) {
       // ---------------- V rows behind the longest prefix ----------------
       int n_clear = 0, at0 = 0;
-      while (next_segment<true>(sg, tab, p.pairs)) {
+      while (next_segment<true>(sg, tab, s_run[3])) {
         const int n_tiles = sg->j1 - sg->j0;
         const int st = (at0 + v_place(n_tiles - 1, n_tiles)) % NST;
         at0 += 2 * n_tiles;
@@ -424,13 +434,13 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     uint8_t* sPx = sP + x * C::kPTile;
     int n_s = 0;              // S tiles taken
     int cut = -1;
-    for (int n = 0; next_segment<true>(sg, tab, p.pairs); ++n) {
+    for (int n = 0; next_segment<true>(sg, tab, s_run[3]); ++n) {
       // the row: sequence b, token t, head g of the group
       auto place = [&](int& b, int& t, int& g) {
-        const int ti = alt ? 0 : 2 * (p.pair_base + sg->pair) + x;
-        const RowTile rt = row_tile(p, ti);
+        if (!alt && sg->len[x] < 0) return false;
+        const RowTile rt = row_tile(p, 2 * p.pair_base + s_id[2 * sg->pair + (alt ? 0 : x)]);
         b = rt.b0 + r / (p.gt * p.tt); t = rt.t0 + r / p.gt % p.tt; g = rt.g0 + r % p.gt;
-        return ti < p.m_tiles && r < rows && b < p.B && t < p.T && g < p.G && !(p.seq_len && t >= p.seq_len[b]);
+        return r < rows && b < p.B && t < p.T && g < p.G && !(p.seq_len && t >= p.seq_len[b]);
       };
       const int n_mine = slot_tiles(sg, alt, x), n_both = min(n_mine, slot_tiles(sg, alt, x ^ 1));
       int c_hi = sg->len[alt ? 0 : x];   // keys of the next tile, and behind it, that the row sees
@@ -617,7 +627,9 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         // number of the unit's last key tile, and the CTA that has it
         const int last = s_run[0] - sg->left - 1 + (sg->nt - sg->j1), run = s_run[1], longer = s_run[2];
         const int c1 = last < longer * (run + 1) ? last / (run + 1) : longer + (last - longer * (run + 1)) / run;
-        p.unit_parts[unit] = make_int4(finish ? 0 : c1 - int(blockIdx.x) + 1, part, blockIdx.x, 0);
+        const int second = sg->len[1] < 0 ? 0xffff : int(s_id[2 * sg->pair + 1]);
+        p.unit_parts[unit] = make_int4(finish ? 0 : c1 - int(blockIdx.x) + 1, part, blockIdx.x,
+                                       s_id[2 * sg->pair] | second << 16);
         if (!whole) cut = unit;
       }
     }
@@ -648,14 +660,17 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join(const PrefixParams p
   const int col4 = (blockIdx.y * (4 / SPLIT) + wid / SPLIT) * CPW;
   const int unit = CUT ? p.cut_units[blockIdx.x / 8] : int(blockIdx.x) / 8;
   const int x = blockIdx.x / 4 % 2, r = blockIdx.x % 4 * 32 + lane;
-  const int ti = 2 * (p.pair_base + unit % p.pairs) + x;
-  if (unit < 0 || ti >= p.m_tiles) return;
+  if (unit < 0) return;
+  // the row tile: what the prefix kernel says (CUT), or, where no tile drops out, by its number
+  const int4 parts = p.unit_parts[unit];
+  const int of_pair = CUT ? int(x ? unsigned(parts.w) >> 16 : parts.w & 0xffff) : 2 * (unit % p.pairs) + x;
+  const int ti = 2 * p.pair_base + of_pair;
+  if (of_pair == 0xffff || ti >= p.m_tiles) return;
   const RowTile rt = row_tile(p, ti);
   const int hk = unit / p.pairs, b = rt.b0 + r / (p.gt * p.tt), t = rt.t0 + r / p.gt % p.tt, g = rt.g0 + r % p.gt;
   const bool here = r < p.gt * p.tt * p.bt && b < p.B && t < p.T && g < p.G && !(p.seq_len && t >= p.seq_len[b]);
   if (SPLIT == 1 && !here) return;
   const size_t row = ((size_t(b) * p.Hkv + hk) * p.G + g) * p.T + t;
-  const int4 parts = p.unit_parts[unit];
   const int sub = p.alternate ? 1 : 0;     // alternate mode: both slots hold the row
   const int n_pfx = here ? parts.x << sub : 0, n_own = here ? own_parts : 0;
   auto place = [&](int i) -> size_t {      // part and slot of the row's i-th prefix part
