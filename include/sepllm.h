@@ -505,9 +505,10 @@ sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int32_t P, flo
  * (Eq. 2's mask; where the prefix brings the initial tokens, n_init = 0; in a row
  * that packs several documents each of them continues the prefix), under one
  * softmax.  Rows behind a sequence's end (sepllm_build_index_varlen) are not
- * written at all.  desc->events and flags as there; workspace of
- * sepllm_attn_prefix_workspace_bytes, 256-byte aligned.  Serving only: there is no
- * gradient. */
+ * written at all.  desc->events as there (the launches behind the attention are
+ * not marked); SEPLLM_ATTN_SIDE_READY is not looked at, and the workspace holds no
+ * side rows for later calls.  workspace of sepllm_attn_prefix_workspace_bytes,
+ * 256-byte aligned.  Serving only: there is no gradient. */
 sepllm_status sepllm_attn_prefix_workspace_bytes(const sepllm_attn_desc* desc,
                                                  const sepllm_index_desc* idesc, int32_t P,
                                                  size_t* bytes);

@@ -33,10 +33,17 @@ __device__ __forceinline__ DocView doc_view(const sepllm_index_header* hdr, cons
 struct SlotGeom {
   int t, hq, side_full, ns, wlo, whi, s0, full_lo, ws_last;
 };
+// Forms of the forward kernels.  kFwdF32: the output stays in 32 bits (FwdParams::O32) for a caller that
+// joins it with another part.  kFwdPrefix: the side list of sequence b begins with the prefix_of(b)
+// rows of a prefix that all sequences share, which every row keeps, and rows of padding are not written.
+enum FwdMode { kFwdPlain = 0, kFwdF32 = 1, kFwdPrefix = 2 };
 // A tile that starts at or behind the end of its sequence (seq_len from the index) is empty too.
+// PFX: `plen` entries stand in front of the side list, whose limits per row are `lim`.
+template <bool PFX = false>
 __device__ __forceinline__ SlotGeom load_slot(const int32_t* tile_meta, const int32_t* seq_len, int b,
                                               int T, int t, int hq, int side_tiles_cap,
-                                              const DocView& dv, int L, int n_neighbor) {
+                                              const DocView& dv, int L, int n_neighbor, int plen = 0,
+                                              const int32_t* lim = nullptr, int side_cap = 0) {
   SlotGeom g;
   const int len = seq_len[b];
   g.t = (t >= 0 && t * kBM < len) ? t : -1;
@@ -57,6 +64,14 @@ __device__ __forceinline__ SlotGeom load_slot(const int32_t* tile_meta, const in
       g.full_lo = (dv.cnt[size_t(b) * (L + 1) + s] + kBN - 1) / kBN;
       g.ws_last = max(r1 - n_neighbor + 1, s);
     }
+    if (PFX) {
+      const int r0 = t * kBM, r1 = min(len, r0 + kBM) - 1;
+      g.side_full = (plen + min(lim[size_t(b) * L + r0], side_cap)) / kBN;
+      g.ns = min((plen + min(lim[size_t(b) * L + r1], side_cap) + kBN - 1) / kBN, side_tiles_cap);
+      g.s0 = 0;
+      if (dv.doc_start)
+        g.full_lo = (plen + dv.cnt[size_t(b) * (L + 1) + dv.doc_start[size_t(b) * L + r1]] + kBN - 1) / kBN;
+    }
   } else {
     g.side_full = 0; g.ns = 0; g.wlo = 0x3fffffff; g.whi = 0;
     g.s0 = 0x3fffffff; g.full_lo = 0; g.ws_last = 0;
@@ -75,8 +90,9 @@ __device__ __forceinline__ bool slot_active(const SlotGeom& g, int sbase, int ns
 struct RowGeom {
   int lim, lo, ws;
 };
+template <bool PFX = false>
 __device__ __forceinline__ RowGeom row_geom(const int32_t* lim, const DocView& dv, int b, int L,
-                                            int row, int n_neighbor, int side_cap) {
+                                            int row, int n_neighbor, int side_cap, int plen = 0) {
   RowGeom r;
   r.lim = 0;
   r.lo = 0;
@@ -88,18 +104,23 @@ __device__ __forceinline__ RowGeom row_geom(const int32_t* lim, const DocView& d
       r.lo = min(dv.cnt[size_t(b) * (L + 1) + s], side_cap);
       r.ws = max(r.ws, s);
     }
+    if (PFX) { r.lim += plen; r.lo += plen; }   // (and the entries before plen)
   }
   return r;
 }
-// Kept columns [c_lo, c_hi) of one key tile for one row, and whether any row of the query tile
-// needs the mask at all.  tile: side tile index, or window tile index (keys tile*kBN ...).
+// Kept columns [c_lo, c_hi) of one key tile for one row (PFX: and those before c_px), and whether any
+// row of the query tile needs the mask at all.  tile: side tile index, or window tile index (keys tile*kBN ...).
+template <bool PFX = false>
 __device__ __forceinline__ void key_range(bool side, int tile, const SlotGeom& g, int row,
-                                          const RowGeom& rg, int& c_lo, int& c_hi, bool& need_mask) {
+                                          const RowGeom& rg, int& c_lo, int& c_hi, bool& need_mask,
+                                          int plen = 0, int* c_px = nullptr) {
   const int k0 = tile * kBN;
+  if (PFX) *c_px = side ? plen - k0 : 0;
   if (side) {
     c_lo = rg.lo - k0;
     c_hi = rg.lim - k0;
     need_mask = (tile >= g.side_full) || (tile < g.full_lo);
+    if (PFX) need_mask = need_mask && k0 + kBN > plen;
   } else {
     c_lo = rg.ws - k0;
     c_hi = row - k0 + 1;
@@ -121,8 +142,21 @@ struct FwdParams {
   float* LSE;
   int32_t* status;
   int L, T, Hq, Hkv, n_neighbor, side_cap, side_tiles_cap, pair_heads;
+  const int32_t* pfx_len;    // kFwdPrefix: [B] or null (pfx_P for all)
+  int pfx_P;
   int d;                     // row length of Q, K, V and O in memory (<= the kernel's D)
   float scale_log2;
+};
+
+__device__ __forceinline__ int prefix_of(const FwdParams& p, int b) {
+  return p.pfx_len ? max(0, min(p.pfx_P, p.pfx_len[b])) : p.pfx_P;
+}
+
+// A prefix shared by the batch, in memory: Kp, Vp bf16 [Hkv][P][d], prefix_len [B] or null.
+struct PrefixRows {
+  const void *Kp, *Vp;
+  const int32_t* prefix_len;
+  int P;
 };
 
 // Head sizes between the kernel widths run in the next wider kernel: the tensor maps of Q, K, V and
@@ -155,10 +189,17 @@ __global__ void gather_side_kv(const __nv_bfloat16* __restrict__ K,
 
 // Forward for groups of four query heads at head size 128: two CTAs of a cluster work on the four
 // heads of one query tile as one MMA pair (attn_fwd_pair.cu).  Ks64 / K64: maps with 64-row boxes.
-sepllm_status launch_fwd_pair(const sepllm_attn_desc* d, const FwdParams& p, int n_tiles,
+sepllm_status launch_fwd_pair(const sepllm_attn_desc* d, const FwdParams& p, int mode, int n_tiles,
                               const CUtensorMap& mq, const CUtensorMap& mk64, const CUtensorMap& mv,
                               const CUtensorMap& mks64, const CUtensorMap& mvs, cudaStream_t stream);
 
+// The forward with the prefix rows in front of every sequence's side list, in a workspace of
+// attn_direct_bytes: status | K rows | V rows, both [B][Hkv][attn_direct_rows][kernel_head_dim(d)].
+int64_t attn_direct_rows(const sepllm_index_desc* id, int P);
+size_t attn_direct_bytes(const sepllm_attn_desc* d, const sepllm_index_desc* id, int P);
+sepllm_status attn_fwd_direct(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc, const void* Q,
+                              const void* K, const void* V, const void* index, const PrefixRows& pfx, void* O,
+                              float* LSE, void* workspace, cudaStream_t stream);
 // The forward with its output left in 32 bits, to be joined with another part: O32
 // [B][Hq][ceil(L / 128)][D / 4][128][4], D = kernel_head_dim(d).  Arguments as sepllm_attn_fwd, checked by the caller.
 sepllm_status attn_fwd_f32(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc, const void* Q,

@@ -110,8 +110,7 @@ struct FwdCfg {
 
 constexpr int kFwdThreads = 384;
 
-// F32: the output stays in 32 bits for a caller that joins it with another part (layout: FwdParams).
-template <int D, bool F32>
+template <int D, int MODE>
 __global__ void __launch_bounds__(kFwdThreads, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
                 const __grid_constant__ CUtensorMap mapV, const __grid_constant__ CUtensorMap mapKs,
@@ -136,7 +135,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 8 + 4 * NST);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
 
-  if (F32) let_dependents_start();   // the prefix kernel may start while this one ends
+  if (MODE == kFwdF32) let_dependents_start();   // the prefix kernel may start while this one ends
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // grid (heads x batch, tiles): consecutive CTAs take the same tile position of every head and
   // sequence, longest tiles first, so work is handed out longest-first over the whole launch and
@@ -145,17 +144,23 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
   const int heads_x = p.pair_heads ? p.Hq / 2 : p.Hq;
   const int b = int(blockIdx.x) / heads_x, hx = int(blockIdx.x) % heads_x;
 
+  constexpr bool PFX = MODE == kFwdPrefix;
+  const int plen = PFX ? prefix_of(p, b) : 0;
   // the two slots of this CTA (a slot is empty when its tile does not exist or holds only padding)
   SlotGeom g0, g1;
   const DocView dv = doc_view(p.index_header, p.cnt, p.doc_start, p.doc_end);
   if (p.pair_heads) {
     const int t = p.T - 1 - int(blockIdx.y);
-    g0 = load_slot(p.tile_meta, p.seq_len, b, p.T, t, 2 * hx, p.side_tiles_cap, dv, p.L, p.n_neighbor);
-    g1 = load_slot(p.tile_meta, p.seq_len, b, p.T, t, 2 * hx + 1, p.side_tiles_cap, dv, p.L, p.n_neighbor);
+    g0 = load_slot<PFX>(p.tile_meta, p.seq_len, b, p.T, t, 2 * hx, p.side_tiles_cap, dv, p.L, p.n_neighbor, plen,
+                        p.lim, p.side_cap);
+    g1 = load_slot<PFX>(p.tile_meta, p.seq_len, b, p.T, t, 2 * hx + 1, p.side_tiles_cap, dv, p.L, p.n_neighbor, plen,
+                        p.lim, p.side_cap);
   } else {
     const int t = p.T - 1 - 2 * int(blockIdx.y);
-    g0 = load_slot(p.tile_meta, p.seq_len, b, p.T, t - 1, hx, p.side_tiles_cap, dv, p.L, p.n_neighbor);
-    g1 = load_slot(p.tile_meta, p.seq_len, b, p.T, t, hx, p.side_tiles_cap, dv, p.L, p.n_neighbor);
+    g0 = load_slot<PFX>(p.tile_meta, p.seq_len, b, p.T, t - 1, hx, p.side_tiles_cap, dv, p.L, p.n_neighbor, plen,
+                        p.lim, p.side_cap);
+    g1 = load_slot<PFX>(p.tile_meta, p.seq_len, b, p.T, t, hx, p.side_tiles_cap, dv, p.L, p.n_neighbor, plen,
+                        p.lim, p.side_cap);
   }
   if (g0.t < 0 && g1.t < 0) return;   // both tiles are padding: nothing to do, nothing written
   const int kv_plane = b * p.Hkv + g1.hq / G;
@@ -291,7 +296,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     if (t >= 0) {
       const int row = t * kBM + r;  // this thread's query position
       const int q_plane = b * p.Hq + g.hq;
-      const RowGeom rg = row_geom(p.lim, dv, b, p.L, row, p.n_neighbor, p.side_cap);
+      const RowGeom rg = row_geom<PFX>(p.lim, dv, b, p.L, row, p.n_neighbor, p.side_cap, plen);
       float m_ref = -INFINITY;  // reference exponent (log2 units), may lag the true row maximum
       float l_sum = 0.f;
       int n_done = 0;
@@ -312,9 +317,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
 
         // kept columns of this tile for this row: [c_lo, c_hi)
         const bool side = j < ns;
-        int c_lo, c_hi;
+        int c_lo, c_hi, c_px = 0;
         bool need_mask;
-        key_range(side, side ? sbase + j : wlo + (j - ns), g, row, rg, c_lo, c_hi, need_mask);
+        key_range<PFX>(side, side ? sbase + j : wlo + (j - ns), g, row, rg, c_lo, c_hi, need_mask, plen, &c_px);
         // Reference exponent.  A tile that needs no mask and finds a reference already set skips
         // the maximum: its exponentials are taken against the old reference, which is exact as
         // long as nothing overflows (fp32 sums and bf16 P have the range for a lag of 2^64), and
@@ -363,7 +368,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
               const int col = c * 32 + e;
-              sreg[c][e] = (col >= c_lo && col < c_hi) ? sreg[c][e] : 0xff800000u;  // -inf
+              sreg[c][e] = ((col >= c_lo && col < c_hi) || (PFX && col < c_px)) ? sreg[c][e] : 0xff800000u;  // -inf
             }
         }
         float corr = 1.f;
@@ -411,20 +416,21 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
       wait(bar_o, 0);
       tc_fence_after();
       const float inv_l = (l_sum > 0.f) ? 1.f / l_sum : 0.f;
-      if (row < p.L) p.LSE[size_t(q_plane) * p.L + row] = (m_ref + log2f(l_sum)) * 0.6931471805599453f;
+      const bool store = row < (PFX ? p.seq_len[b] : p.L);
+      if (store) p.LSE[size_t(q_plane) * p.L + row] = (m_ref + log2f(l_sum)) * 0.6931471805599453f;
       __nv_bfloat16* orow = p.O + (size_t(q_plane) * p.L + row) * p.d;
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         uint32_t oreg[32];
         tmem_ld32(tO + c * 32, oreg);
         tmem_ld_wait();
-        if (F32) {
+        if (MODE == kFwdF32) {
 #pragma unroll
           for (int q8 = 0; q8 < 8; ++q8)
             reinterpret_cast<float4*>(p.O32)[((size_t(q_plane) * p.T + t) * (D / 4) + c * 8 + q8) * kBM + r] =
                 make_float4(__uint_as_float(oreg[4 * q8]) * inv_l, __uint_as_float(oreg[4 * q8 + 1]) * inv_l,
                               __uint_as_float(oreg[4 * q8 + 2]) * inv_l, __uint_as_float(oreg[4 * q8 + 3]) * inv_l);
-        } else if (row < p.L) {
+        } else if (store) {
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
             uint4 val;
@@ -495,18 +501,79 @@ void launch_gather(const sepllm_attn_desc* d, const sepllm_index_desc* id, int c
   }
 }
 
-template <int D, bool F32>
+int64_t attn_direct_rows(const sepllm_index_desc* id, int P) {
+  return (int64_t(P) + id->side_cap + 127) / 128 * 128;
+}
+size_t attn_direct_bytes(const sepllm_attn_desc* d, const sepllm_index_desc* id, int P) {
+  return kAlign + 2 * align_up(size_t(d->B) * d->Hkv * attn_direct_rows(id, P) * kernel_head_dim(d->d) * 2);
+}
+
+// grid (ceil(cap_pad / rows per block), Hkv, B): gather_side_kv with the prefix in front.  Row r of
+// sequence b is prefix row r, then K/V row side_pos[r - plen]; up to the next multiple of 128 zero.
+template <int D>
+__global__ void __launch_bounds__(256)
+gather_prefix_side(const __nv_bfloat16* __restrict__ K, const __nv_bfloat16* __restrict__ V, const PrefixRows pfx,
+                   const int32_t* __restrict__ side_pos, const int32_t* __restrict__ n_side, int L, int d, int Hkv,
+                   int side_cap, int cap_pad, __nv_bfloat16* __restrict__ Ks, __nv_bfloat16* __restrict__ Vs,
+                   int32_t* __restrict__ status) {
+  constexpr int LPR = D / 8;
+  constexpr int RPB = 256 / LPR;
+  const int b = blockIdx.z, hk = blockIdx.y;
+  if (threadIdx.x == 0 && (blockIdx.x | blockIdx.y | blockIdx.z) == 0) *status = SEPLLM_OK;
+  const int r = blockIdx.x * RPB + threadIdx.x / LPR, l = threadIdx.x % LPR;
+  const int plen = pfx.prefix_len ? max(0, min(pfx.P, pfx.prefix_len[b])) : pfx.P;
+  const int n = plen + min(n_side[b], side_cap);
+  if (r >= min(cap_pad, (n + 127) / 128 * 128)) return;
+  uint4 kv = make_uint4(0, 0, 0, 0), vv = make_uint4(0, 0, 0, 0);
+  if (r < n && l * 8 < d) {
+    if (r < plen) {
+      const size_t at = (size_t(hk) * pfx.P + r) * d + l * 8;
+      kv = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(pfx.Kp) + at);
+      vv = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(pfx.Vp) + at);
+    } else {
+      const int pos = side_pos[size_t(b) * side_cap + r - plen];
+      if (pos >= 0 && pos < L) {
+        const size_t at = ((size_t(b) * Hkv + hk) * L + pos) * d + l * 8;
+        kv = *reinterpret_cast<const uint4*>(K + at);
+        vv = *reinterpret_cast<const uint4*>(V + at);
+      }
+    }
+  }
+  const size_t to = ((size_t(b) * Hkv + hk) * cap_pad + r) * D + l * 8;
+  *reinterpret_cast<uint4*>(Ks + to) = kv;
+  *reinterpret_cast<uint4*>(Vs + to) = vv;
+}
+
+template <int D>
+static void launch_prefix_gather(const sepllm_attn_desc* d, const sepllm_index_desc* id, int cap_pad, const void* K,
+                                 const void* V, const PrefixRows& pfx, const int32_t* side_pos,
+                                 const int32_t* n_side, void* Ks, void* Vs, int32_t* status, cudaStream_t stream) {
+  constexpr int RPB = 256 / (D / 8);
+  gather_prefix_side<D><<<dim3((cap_pad + RPB - 1) / RPB, d->Hkv, d->B), 256, 0, stream>>>(
+      static_cast<const __nv_bfloat16*>(K), static_cast<const __nv_bfloat16*>(V), pfx, side_pos, n_side, d->L, d->d,
+      d->Hkv, id->side_cap, cap_pad, static_cast<__nv_bfloat16*>(Ks), static_cast<__nv_bfloat16*>(Vs), status);
+}
+
+// pfx: the prefix of kFwdPrefix, null otherwise.
+template <int D, int MODE>
 static sepllm_status launch_fwd(const sepllm_attn_desc* d, const sepllm_index_desc* id,
                                 const sepllm_index_header& ih, const void* Q, const void* K,
                                 const void* V, const uint8_t* index, void* O, float* LSE,
-                                uint8_t* ws, cudaStream_t stream) {
-  const AttnLayout lay = attn_layout(d, id);
+                                uint8_t* ws, const PrefixRows* pfx, cudaStream_t stream) {
+  AttnLayout lay = attn_layout(d, id);
+  if (MODE == kFwdPrefix) {
+    lay.cap_pad = int(attn_direct_rows(id, pfx->P));
+    lay.off_vs = lay.off_ks + (attn_direct_bytes(d, id, pfx->P) - kAlign) / 2;
+  }
   __nv_bfloat16* Ks = reinterpret_cast<__nv_bfloat16*>(ws + lay.off_ks);
   __nv_bfloat16* Vs = reinterpret_cast<__nv_bfloat16*>(ws + lay.off_vs);
   const int32_t* side_pos = reinterpret_cast<const int32_t*>(index + ih.off_side_pos);
   const int32_t* n_side = reinterpret_cast<const int32_t*>(index + ih.off_n_side);
   record_event(d, 0, stream);
-  if (!(d->flags & SEPLLM_ATTN_SIDE_READY))
+  if (MODE == kFwdPrefix)
+    launch_prefix_gather<D>(d, id, lay.cap_pad, K, V, *pfx, side_pos, n_side, Ks, Vs, reinterpret_cast<int32_t*>(ws),
+                            stream);
+  else if (!(d->flags & SEPLLM_ATTN_SIDE_READY))
     launch_gather(d, id, lay.cap_pad, K, V, side_pos, n_side, Ks, Vs, reinterpret_cast<int32_t*>(ws), stream);
   record_event(d, 1, stream);
 
@@ -529,8 +596,10 @@ static sepllm_status launch_fwd(const sepllm_attn_desc* d, const sepllm_index_de
   p.seq_len = reinterpret_cast<const int32_t*>(index + ih.off_seq_len);
   p.doc_start = reinterpret_cast<const int32_t*>(index + ih.off_doc_start);
   p.doc_end = reinterpret_cast<const int32_t*>(index + ih.off_doc_end);
-  p.O = F32 ? nullptr : static_cast<__nv_bfloat16*>(O);
-  p.O32 = F32 ? static_cast<float*>(O) : nullptr;
+  p.O = MODE == kFwdF32 ? nullptr : static_cast<__nv_bfloat16*>(O);
+  p.O32 = MODE == kFwdF32 ? static_cast<float*>(O) : nullptr;
+  p.pfx_len = MODE == kFwdPrefix ? pfx->prefix_len : nullptr;
+  p.pfx_P = MODE == kFwdPrefix ? pfx->P : 0;
   p.LSE = LSE;
   p.status = reinterpret_cast<int32_t*>(ws);
   p.L = d->L;
@@ -551,16 +620,16 @@ static sepllm_status launch_fwd(const sepllm_attn_desc* d, const sepllm_index_de
     if ((st = make_tile_map(&mk64, K, dr, L, int64_t(d->B) * d->Hkv, dr, L * dr, 64)) != SEPLLM_OK) return st;
     if ((st = make_tile_map(&mks64, Ks, D, lay.cap_pad, int64_t(d->B) * d->Hkv, D,
                             int64_t(lay.cap_pad) * D, 64)) != SEPLLM_OK) return st;
-    st = launch_fwd_pair(d, p, ih.n_tiles, mq, mk64, mv, mks64, mvs, stream);
+    st = launch_fwd_pair(d, p, MODE, ih.n_tiles, mq, mk64, mv, mks64, mvs, stream);
     record_event(d, 2, stream);
     return st;
   }
   const uint32_t smem = FwdCfg<D>::kRequest;
-  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(attn_fwd_kernel<D, F32>,
+  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(attn_fwd_kernel<D, MODE>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
   const dim3 grid = p.pair_heads ? dim3(d->Hq / 2 * d->B, ih.n_tiles)
                                  : dim3(d->Hq * d->B, (ih.n_tiles + 1) / 2);
-  attn_fwd_kernel<D, F32><<<grid, kFwdThreads, smem, stream>>>(mq, mk, mv, mks, mvs, p);
+  attn_fwd_kernel<D, MODE><<<grid, kFwdThreads, smem, stream>>>(mq, mk, mv, mks, mvs, p);
   record_event(d, 2, stream);
   SEPLLM_CUDA_TRY(cudaGetLastError());
   return SEPLLM_OK;
@@ -571,24 +640,30 @@ static sepllm_status launch_fwd(const sepllm_attn_desc* d, const sepllm_index_de
 using namespace sepllm;
 
 // (the side gather, the call's first launch, resets the status word)
-template <bool F32>
+template <int MODE>
 static sepllm_status forward(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc, const void* Q,
                              const void* K, const void* V, const void* index, void* O, float* LSE,
-                             void* workspace, cudaStream_t stream) {
+                             void* workspace, const PrefixRows* pfx, cudaStream_t stream) {
   sepllm_status st;
   sepllm_index_header ih;
   if ((st = fill_index_header(idesc, &ih)) != SEPLLM_OK) return st;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  if (desc->flags & SEPLLM_ATTN_SIDE_READY) SEPLLM_CUDA_TRY(cudaMemsetAsync(ws, 0, sizeof(int32_t), stream));
+  if (MODE == kFwdPlain && (desc->flags & SEPLLM_ATTN_SIDE_READY)) SEPLLM_CUDA_TRY(cudaMemsetAsync(ws, 0, sizeof(int32_t), stream));
   if (kernel_head_dim(desc->d) == 64)
-    return launch_fwd<64, F32>(desc, idesc, ih, Q, K, V, static_cast<const uint8_t*>(index), O, LSE, ws, stream);
-  return launch_fwd<128, F32>(desc, idesc, ih, Q, K, V, static_cast<const uint8_t*>(index), O, LSE, ws, stream);
+    return launch_fwd<64, MODE>(desc, idesc, ih, Q, K, V, static_cast<const uint8_t*>(index), O, LSE, ws, pfx, stream);
+  return launch_fwd<128, MODE>(desc, idesc, ih, Q, K, V, static_cast<const uint8_t*>(index), O, LSE, ws, pfx, stream);
 }
 
 sepllm_status sepllm::attn_fwd_f32(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc, const void* Q,
                                    const void* K, const void* V, const void* index, float* O32, float* LSE,
                                    void* workspace, cudaStream_t stream) {
-  return forward<true>(desc, idesc, Q, K, V, index, O32, LSE, workspace, stream);
+  return forward<kFwdF32>(desc, idesc, Q, K, V, index, O32, LSE, workspace, nullptr, stream);
+}
+
+sepllm_status sepllm::attn_fwd_direct(const sepllm_attn_desc* desc, const sepllm_index_desc* idesc, const void* Q,
+                                      const void* K, const void* V, const void* index, const PrefixRows& pfx, void* O,
+                                      float* LSE, void* workspace, cudaStream_t stream) {
+  return forward<kFwdPrefix>(desc, idesc, Q, K, V, index, O, LSE, workspace, &pfx, stream);
 }
 
 extern "C" sepllm_status sepllm_attn_fwd(const sepllm_attn_desc* desc,
@@ -601,5 +676,6 @@ extern "C" sepllm_status sepllm_attn_fwd(const sepllm_attn_desc* desc,
   if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(O, 16) ||
       !aligned(LSE, 4) || !aligned(index, kAlign) || !aligned(workspace, kAlign))
     return SEPLLM_INVALID_ARG;
-  return forward<false>(desc, idesc, Q, K, V, index, O, LSE, workspace, static_cast<cudaStream_t>(stream_));
+  return forward<kFwdPlain>(desc, idesc, Q, K, V, index, O, LSE, workspace, nullptr,
+                            static_cast<cudaStream_t>(stream_));
 }

@@ -52,8 +52,7 @@ static_assert(PairSmem::kRequest <= 227 * 1024, "shared memory budget");
 constexpr int kPairThreads = 384;
 constexpr long long kSlotOffsetCycles = 1600;
 
-// F32: the output stays in 32 bits for a caller that joins it with another part.
-template <bool F32>
+template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK64,
                      const __grid_constant__ CUtensorMap mapV, const __grid_constant__ CUtensorMap mapKs64,
@@ -85,7 +84,7 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_tok + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
 
-  if (F32) let_dependents_start();   // the prefix kernel may start while this one ends
+  if (MODE == kFwdF32) let_dependents_start();   // the prefix kernel may start while this one ends
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_ctarank();   // 0 = even CTA, issues the MMAs
   // grid (pairs of query heads x batch, tiles), longest tiles first; the two CTAs of a cluster are
@@ -96,8 +95,10 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
   const int G = p.Hq / p.Hkv;
   if (t * kBM >= p.seq_len[b]) return;   // a tile of padding (the same for both CTAs of the pair)
   const DocView dv = doc_view(p.index_header, p.cnt, p.doc_start, p.doc_end);
-  const SlotGeom g = load_slot(p.tile_meta, p.seq_len, b, p.T, t, 2 * hx, p.side_tiles_cap, dv, p.L,
-                               p.n_neighbor);
+  constexpr bool PFX = MODE == kFwdPrefix;
+  const int plen = PFX ? prefix_of(p, b) : 0;
+  const SlotGeom g = load_slot<PFX>(p.tile_meta, p.seq_len, b, p.T, t, 2 * hx, p.side_tiles_cap, dv, p.L,
+                                    p.n_neighbor, plen, p.lim, p.side_cap);
   const int kv_plane = b * p.Hkv + (2 * hx) / G;
   // key tiles: side tiles [sbase, sbase + ns), then window tiles [wlo, whi)
   const int sbase = g.s0, ns = max(0, g.ns - g.s0), wlo = g.wlo;
@@ -286,7 +287,7 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     const int hq = 2 * hx + x;
     const int row = t * kBM + r;  // this thread's query position
     const int q_plane = b * p.Hq + hq;
-    const RowGeom rg = row_geom(p.lim, dv, b, p.L, row, p.n_neighbor, p.side_cap);
+    const RowGeom rg = row_geom<PFX>(p.lim, dv, b, p.L, row, p.n_neighbor, p.side_cap, plen);
     float m_ref = -INFINITY;  // reference exponent (log2 units), may lag the true row maximum
     float l_sum = 0.f;
     uint32_t sreg[4][32];
@@ -301,16 +302,16 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
 
       // kept columns of this tile for this row: [c_lo, c_hi)
       const bool side = j < ns;
-      int c_lo, c_hi;
+      int c_lo, c_hi, c_px = 0;
       bool need_mask;
-      key_range(side, side ? sbase + j : wlo + (j - ns), g, row, rg, c_lo, c_hi, need_mask);
+      key_range<PFX>(side, side ? sbase + j : wlo + (j - ns), g, row, rg, c_lo, c_hi, need_mask, plen, &c_px);
       if (need_mask) {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
             const int col = c * 32 + e;
-            sreg[c][e] = (col >= c_lo && col < c_hi) ? sreg[c][e] : 0xff800000u;  // -inf
+            sreg[c][e] = ((col >= c_lo && col < c_hi) || (PFX && col < c_px)) ? sreg[c][e] : 0xff800000u;  // -inf
           }
       }
       // The reference exponent moves only when the tile's maximum exceeds it by more than 2^8
@@ -394,20 +395,21 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     wait(bar_o, 0);
     tc_fence_after();
     const float inv_l = (l_sum > 0.f) ? 1.f / l_sum : 0.f;
-    if (row < p.L) p.LSE[size_t(q_plane) * p.L + row] = (m_ref + log2f(l_sum)) * 0.6931471805599453f;
+    const bool store = row < (PFX ? p.seq_len[b] : p.L);
+    if (store) p.LSE[size_t(q_plane) * p.L + row] = (m_ref + log2f(l_sum)) * 0.6931471805599453f;
     __nv_bfloat16* orow = p.O + (size_t(q_plane) * p.L + row) * p.d;
 #pragma unroll
     for (int c = 0; c < kD / 32; ++c) {
       uint32_t oreg[32];
       tmem_ld32(tO + c * 32, oreg);
       tmem_ld_wait();
-      if (F32) {
+      if (MODE == kFwdF32) {
 #pragma unroll
         for (int q8 = 0; q8 < 8; ++q8)
           reinterpret_cast<float4*>(p.O32)[((size_t(q_plane) * p.T + t) * (kD / 4) + c * 8 + q8) * kBM + r] =
               make_float4(__uint_as_float(oreg[4 * q8]) * inv_l, __uint_as_float(oreg[4 * q8 + 1]) * inv_l,
                             __uint_as_float(oreg[4 * q8 + 2]) * inv_l, __uint_as_float(oreg[4 * q8 + 3]) * inv_l);
-      } else if (row < p.L) {
+      } else if (store) {
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
           uint4 val;
@@ -429,11 +431,13 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
 
 }  // namespace
 
-sepllm_status launch_fwd_pair(const sepllm_attn_desc* d, const FwdParams& p, int n_tiles,
+sepllm_status launch_fwd_pair(const sepllm_attn_desc* d, const FwdParams& p, int mode, int n_tiles,
                               const CUtensorMap& mq, const CUtensorMap& mk64, const CUtensorMap& mv,
                               const CUtensorMap& mks64, const CUtensorMap& mvs, cudaStream_t stream) {
   const uint32_t smem = PairSmem::kRequest;
-  auto kernel = p.O32 ? attn_fwd_pair_kernel<true> : attn_fwd_pair_kernel<false>;
+  auto kernel = mode == kFwdF32      ? attn_fwd_pair_kernel<kFwdF32>
+                : mode == kFwdPrefix ? attn_fwd_pair_kernel<kFwdPrefix>
+                                     : attn_fwd_pair_kernel<kFwdPlain>;
   SEPLLM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
   // x = pairs of query heads of every sequence: even, and a cluster never straddles two kv heads
   const dim3 grid(d->Hq / 2 * d->B, n_tiles);

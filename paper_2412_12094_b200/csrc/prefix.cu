@@ -908,13 +908,37 @@ sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const
 
 using namespace sepllm;
 
-// Workspace of a forward behind a prefix: the forward's own | O32 | LSE of the own part | parts.
 namespace {
+// How a call is carried out.  direct: the prefix rows are copied in front of every sequence's side rows
+// and the forward kernels walk them there; otherwise the forward over the rows' own tokens and the
+// prefix kernel, which shares the loads, splits long prefixes and drops padding, with a workspace of
+// the forward's own | O32 | LSE of the own part | parts.
 struct AttnPrefixLayout {
+  bool direct;
   size_t off_o, off_lse, off_parts, bytes;
 };
 AttnPrefixLayout attn_prefix_layout(const sepllm_attn_desc* d, const sepllm_index_desc* id, const PrefixParams& p) {
   AttnPrefixLayout a;
+  // Microseconds: a wave of forward CTAs (two row tiles each, one CTA per SM) takes 6 and 2 for each key
+  // tile; the copy its bytes at 5 TB/s; the prefix kernel 2 for each step of a CTA, and with the join 24
+  // (14 where there is a single row tile).  Both measured (us, direct / shared; 32 heads on 8 of 128):
+  // 1 sequence x 16 tokens behind 100 entries 17 / 28, behind 1000 32 / 25; 16 x 64 behind 100 37 / 44,
+  // behind 1000 80 / 73; 4 x 300 behind 500 54 / 60, behind 2000 107 / 100; 2 x 1024 behind 500 69 / 97,
+  // behind 2000 114 / 140, behind 8000 326 / 292; 1 x 8192 behind 500 270 / 317; 12 heads of 64: 8 x 1024
+  // behind 1000 116 / 126.  The rule takes the faster form in each of these.
+  const double own_tiles = std::min(d->L, id->n_neighbor) / 128 + 2;
+  const double waves = std::ceil(double(d->B) * d->Hq * ((d->L + 127) / 128) / 2 / kSmCount);
+  const double copy_us = double(d->B) * d->Hkv * p.P * d->d * 8 / 5e6;
+  const double direct_us = 4.0 + copy_us + waves * (6.0 + 2.0 * (own_tiles + p.key_tiles));
+  const double steps = double(all_pairs(p)) * d->Hkv * p.key_tiles * (p.alternate ? 0.5 : 1.0);
+  const double shared_us = 4.0 + waves * (6.0 + 2.0 * own_tiles) + (p.alternate ? 14.0 : 24.0) +
+                           2.0 * std::ceil(steps / kSmCount);
+  a.direct = direct_us < shared_us && attn_direct_rows(id, p.P) < (1 << 30);
+  if (a.direct) {
+    a.off_o = a.off_lse = a.off_parts = 0;
+    a.bytes = attn_direct_bytes(d, id, p.P);
+    return a;
+  }
   const size_t rows = size_t(d->B) * d->Hq * d->L;
   a.off_o = attn_layout(d, id).fwd_bytes;
   a.off_lse = a.off_o + align_up(size_t(d->B) * d->Hq * ((d->L + 127) / 128 * 128) * kernel_head_dim(d->d) * sizeof(float));
@@ -955,10 +979,14 @@ extern "C" sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, co
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const AttnPrefixLayout lay = attn_prefix_layout(desc, idesc, p);
+  if (lay.direct)
+    return attn_fwd_direct(desc, idesc, Q, K, V, index, PrefixRows{Kp, Vp, prefix_len, P}, O, LSE, ws, stream);
   float* own_O = reinterpret_cast<float*>(ws + lay.off_o);
   float* own_lse = reinterpret_cast<float*>(ws + lay.off_lse);
   // the rows' own tokens first (Eq. 2's mask); their result waits in 32 bits so that O is rounded once
-  if ((st = attn_fwd_f32(desc, idesc, Q, K, V, index, own_O, own_lse, ws, stream)) != SEPLLM_OK) return st;
+  sepllm_attn_desc fresh = *desc;
+  fresh.flags &= ~SEPLLM_ATTN_SIDE_READY;   // (the workspace's side rows are the call's own)
+  if ((st = attn_fwd_f32(&fresh, idesc, Q, K, V, index, own_O, own_lse, ws, stream)) != SEPLLM_OK) return st;
   place_prefix_parts(&p, ws + lay.off_parts);
   p.prefix_len = prefix_len;
   p.seq_len = reinterpret_cast<const int32_t*>(static_cast<const uint8_t*>(index) + ih.off_seq_len);

@@ -78,6 +78,11 @@ SHAPES = [
     (3, 6, 2, 80, 43, 200), (2, 3, 1, 96, 50, 333), (2, 5, 5, 64, 130, 128), (1, 8, 2, 128, 257, 1000),
     (2, 4, 4, 112, 129, 64), (9, 8, 1, 64, 3, 500), (5, 8, 2, 128, 100, 640), (1, 2, 1, 64, 700, 2000),
     (40, 4, 4, 128, 140, 260),
+    # prefixes long enough for the kernel that shares them
+    (2, 4, 1, 128, 1, 9000), (1, 4, 1, 128, 5, 6001), (3, 4, 2, 64, 20, 12000), (1, 8, 2, 128, 16, 5000),
+    (2, 6, 2, 80, 43, 8192), (2, 3, 1, 96, 50, 9000), (2, 5, 5, 64, 130, 7777), (1, 8, 2, 128, 257, 6000),
+    (2, 4, 4, 112, 129, 5120), (9, 8, 1, 64, 3, 14000), (5, 8, 2, 128, 100, 4000), (1, 2, 1, 64, 700, 9001),
+    (40, 4, 4, 128, 140, 2500),
 ]
 
 
@@ -101,7 +106,7 @@ def test_forward(B, Hq, Hkv, d, L, P, ragged):
     O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, pl)
     f = np.isin(ids, inputs.SEP_IDS)
     masks = [orc.mask_matrix(f[b], 0, n) for b in range(B)]
-    heads = None if B * Hq * L < 4000 else [0, Hq - 1]
+    heads = None if B * Hq * L * (P + L) < 4e6 else [0, Hq - 1]
     if B == 40:    # the many-sequence form: a few sequences are enough
         sel = slice(0, 40, 13)
         Q, K, V, O, LSE, masks, plen, seq_len = (x[sel] for x in (Q, K, V, O, LSE, masks, plen, seq_len))
@@ -112,7 +117,7 @@ def test_more_row_tiles_than_one_launch_takes():
     """Sequences and lengths whose row tiles go beyond one launch of the prefix kernel, with units cut
     between its CTAs and whole ones; sampled sequences against the oracle."""
     g = torch.Generator(device="cuda").manual_seed(12)
-    B, Hq, Hkv, d, L, P = 300, 2, 1, 64, 130, 400      # 300 sequences x 3 tiles = 450 pairs
+    B, Hq, Hkv, d, L, P = 300, 2, 1, 64, 130, 2100     # 300 sequences x 3 tiles = 450 pairs
     ids = inputs.token_ids(7, B, L, 0.1)
     lens = [int(x) for x in np.random.default_rng(7).integers(0, L + 1, B)]
     plen = [int(x) for x in np.random.default_rng(8).integers(0, P + 1, B)]
@@ -127,23 +132,25 @@ def test_more_row_tiles_than_one_launch_takes():
            [lens[b] for b in sel], O[sel], LSE[sel])
 
 
-def test_groups_wider_than_a_row_tile():
+@pytest.mark.parametrize("P", [150, 9000])
+def test_groups_wider_than_a_row_tile(P):
     """200 query heads on one kv head: a token's heads take two row tiles."""
     g = torch.Generator(device="cuda").manual_seed(13)
-    B, Hq, d, L, P = 2, 200, 64, 3, 150
+    B, Hq, d, L = 2, 200, 64, 3
     ids = inputs.token_ids(9, B, L, 0.2)
     idesc, index = _index(ids, 2, 0)
     Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, 1, L, d), _normal(g, B, 1, L, d)
     Kp, Vp = _normal(g, 1, P, d), _normal(g, 1, P, d)
     O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, torch.tensor([P, 7], dtype=torch.int32, device="cuda"))
     f = np.isin(ids, inputs.SEP_IDS)
-    _check(Q, K, V, Kp, Vp, [orc.mask_matrix(f[b], 0, 2) for b in range(B)], [P, 7], [L, L], O, LSE)
+    _check(Q, K, V, Kp, Vp, [orc.mask_matrix(f[b], 0, 2) for b in range(B)], [P, 7], [L, L], O, LSE,
+           heads=[0, 63, 127, 128, 199])
 
 
 def test_many_kv_heads_and_a_short_prefix():
     """More (kv head, pair) units than SMs, each with a single key tile."""
     g = torch.Generator(device="cuda").manual_seed(14)
-    for B, Hq, d, L, P in ((1, 400, 64, 2, 5), (3, 180, 128, 150, 128)):
+    for B, Hq, d, L, P in ((1, 400, 64, 2, 5), (3, 180, 128, 150, 128), (1, 400, 64, 2, 3000), (3, 180, 128, 150, 2900)):
         ids = inputs.token_ids(10, B, L, 0.2)
         idesc, index = _index(ids, 3, 0)
         Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hq, L, d), _normal(g, B, Hq, L, d)
@@ -154,15 +161,16 @@ def test_many_kv_heads_and_a_short_prefix():
                heads=[0, 1, 77, Hq - 1])
 
 
-def test_repeated_calls_without_waiting_use_one_workspace():
+@pytest.mark.parametrize("P", [900, 9000])
+def test_repeated_calls_without_waiting_use_one_workspace(P):
     """Calls of different prefix lengths back to back on one workspace: each gives what it gives alone."""
     g = torch.Generator(device="cuda").manual_seed(15)
-    B, Hq, Hkv, d, L, P = 2, 8, 2, 128, 300, 900
+    B, Hq, Hkv, d, L = 2, 8, 2, 128, 300
     ids = inputs.token_ids(11, B, L, 0.1)
     idesc, index = _index(ids, 32, 0)
     Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hkv, L, d), _normal(g, B, Hkv, L, d)
     Kp, Vp = _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
-    plens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([900, 10], [0, 0], [333, 900], [128, 129])]
+    plens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([P, 10], [0, 0], [333, P], [128, 129])]
     want = [_run(Q, K, V, idesc, index, Kp, Vp, p) for p in plens]
     desc = api.AttnDesc(B, Hq, Hkv, d, L, 0.0, 0)
     ws = api.alloc_bytes(api.sepllm_attn_prefix_workspace_bytes(desc, idesc, P))
@@ -174,37 +182,40 @@ def test_repeated_calls_without_waiting_use_one_workspace():
     assert all(torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) for a, b in zip(outs, want))
 
 
-def test_initial_tokens_of_their_own_and_a_scale():
+@pytest.mark.parametrize("P", [77, 9001])
+def test_initial_tokens_of_their_own_and_a_scale(P):
     g = torch.Generator(device="cuda").manual_seed(1)
     ids = inputs.token_ids(3, 2, 150, 0.1)
     idesc, index = _index(ids, 10, a=4)
     Q, K, V = _normal(g, 2, 4, 150, 64), _normal(g, 2, 2, 150, 64), _normal(g, 2, 2, 150, 64)
-    Kp, Vp = _normal(g, 2, 77, 64), _normal(g, 2, 77, 64)
+    Kp, Vp = _normal(g, 2, P, 64), _normal(g, 2, P, 64)
     O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, None, 0.2)
     f = np.isin(ids, inputs.SEP_IDS)
-    _check(Q, K, V, Kp, Vp, [orc.mask_matrix(f[b], 4, 10) for b in range(2)], [77, 77], [150, 150], O, LSE,
+    _check(Q, K, V, Kp, Vp, [orc.mask_matrix(f[b], 4, 10) for b in range(2)], [P, P], [150, 150], O, LSE,
            scale=float(np.float32(0.2)))
 
 
-def test_rows_that_pack_documents_all_continue_the_prefix():
+@pytest.mark.parametrize("P", [200, 9000])
+def test_rows_that_pack_documents_all_continue_the_prefix(P):
     g = torch.Generator(device="cuda").manual_seed(2)
     B, L, n, a = 2, 300, 16, 2
     ids, df = inputs.token_ids(4, B, L, 0.1), inputs.doc_first(4, B, L, 70.0)
     idesc, index = _index(ids, n, a, doc_first=df)
     Q, K, V = _normal(g, B, 4, L, 128), _normal(g, B, 1, L, 128), _normal(g, B, 1, L, 128)
-    Kp, Vp = _normal(g, 1, 200, 128), _normal(g, 1, 200, 128)
-    O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, torch.tensor([200, 50], dtype=torch.int32, device="cuda"))
+    Kp, Vp = _normal(g, 1, P, 128), _normal(g, 1, P, 128)
+    O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, torch.tensor([P, 50], dtype=torch.int32, device="cuda"))
     f = np.isin(ids, inputs.SEP_IDS)
-    _check(Q, K, V, Kp, Vp, [orc.packed_mask_matrix(f[b], df[b], a, n) for b in range(B)], [200, 50], [L, L], O, LSE)
+    _check(Q, K, V, Kp, Vp, [orc.packed_mask_matrix(f[b], df[b], a, n) for b in range(B)], [P, 50], [L, L], O, LSE)
 
 
-def test_no_prefix_in_sight_is_the_plain_forward():
+@pytest.mark.parametrize("P", [90, 20000])
+def test_no_prefix_in_sight_is_the_plain_forward(P):
     g = torch.Generator(device="cuda").manual_seed(3)
     for B, Hq, Hkv, d, L in ((2, 4, 2, 64, 200), (1, 8, 2, 128, 300)):
         ids = inputs.token_ids(5, B, L, 0.1)
         idesc, index = _index(ids, 20, 3)
         Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hkv, L, d), _normal(g, B, Hkv, L, d)
-        Kp = torch.full((Hkv, 90, d), float("nan"), dtype=BF, device="cuda")
+        Kp = torch.full((Hkv, P, d), float("nan"), dtype=BF, device="cuda")
         O, LSE = _run(Q, K, V, idesc, index, Kp, Kp, torch.zeros(B, dtype=torch.int32, device="cuda"))
         desc = api.AttnDesc(B, Hq, Hkv, d, L, 0.0, 0)
         ws = api.alloc_bytes(api.sepllm_attn_workspace_bytes(desc, idesc)[0])
@@ -216,9 +227,10 @@ def test_no_prefix_in_sight_is_the_plain_forward():
         assert (LSE - LSE2).abs().max() <= 1e-5
 
 
-def test_graph_and_other_stream_and_kept_side_rows():
+@pytest.mark.parametrize("P", [400, 9000])
+def test_graph_and_other_stream_and_ignored_side_flag(P):
     g = torch.Generator(device="cuda").manual_seed(4)
-    B, Hq, Hkv, d, L, P = 2, 8, 2, 128, 150, 400
+    B, Hq, Hkv, d, L = 2, 8, 2, 128, 150
     ids = inputs.token_ids(6, B, L, 0.1)
     idesc, index = _index(ids, 20, 0)
     Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hkv, L, d), _normal(g, B, Hkv, L, d)
@@ -232,7 +244,8 @@ def test_graph_and_other_stream_and_kept_side_rows():
     with torch.cuda.stream(s):
         api.sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, None, *outs[0], ws)
     torch.cuda.current_stream().wait_stream(s)
-    desc.flags = api.SIDE_READY      # the workspace holds the side rows of these K and V
+    ws.fill_(0xff)
+    desc.flags = api.SIDE_READY      # not looked at: the call gathers its side rows
     api.sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, None, *outs[1], ws)
     desc.flags = 0
     graph = torch.cuda.CUDAGraph()
@@ -316,3 +329,16 @@ def test_a_serving_run_through_a_shared_prefix(Hq, Hkv, d, rot, layout):
                                                  vv[h // (Hq // Hkv)])
                 assert np.abs(o[b, h].double().cpu().numpy() - ref).max() <= TOL_O["max_abs"], (t, b, h)
                 assert abs(float(lse[b, h]) - lref) <= TOL_LSE
+
+
+def test_packed_rows_with_many_documents_in_the_direct_form():
+    """Side tiles of earlier documents lie between the prefix and a row's own side entries."""
+    g = torch.Generator(device="cuda").manual_seed(16)
+    for Hq, Hkv, d, L, P, mean in ((4, 1, 128, 900, 130, 120.0), (2, 2, 64, 1100, 256, 60.0), (3, 1, 80, 700, 1, 300.0)):
+        ids, df = inputs.token_ids(17, 1, L, 0.5), inputs.doc_first(17, 1, L, mean)
+        idesc, index = _index(ids, 16, 3, doc_first=df)
+        Q, K, V = _normal(g, 1, Hq, L, d), _normal(g, 1, Hkv, L, d), _normal(g, 1, Hkv, L, d)
+        Kp, Vp = _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
+        O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, None)
+        f = np.isin(ids, inputs.SEP_IDS)
+        _check(Q, K, V, Kp, Vp, [orc.packed_mask_matrix(f[0], df[0], 3, 16)], [P], [L], O, LSE)

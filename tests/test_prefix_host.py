@@ -94,8 +94,10 @@ def test_attention_refusals_and_workspace():
     assert _attn(idesc=api.IndexDesc(2, 51, 0, 8, 1, 128, 128, 51)) == api.INVALID_ARG
     assert _attn(idesc=api.IndexDesc(2, 50, 0, 8, 1, 64, 128, 50)) == api.UNSUPPORTED
     desc, idesc = api.AttnDesc(2, 4, 2, 80, 50, 0.0, 0), api.IndexDesc(2, 50, 0, 8, 1, 128, 128, 50)
+    # K and V rows of prefix and side list, or the forward's own, its output in 32 bits and the parts
+    assert api.sepllm_attn_prefix_workspace_bytes(desc, idesc, 300) >= 2 * 2 * 2 * 350 * 128 * 2
     fwd, _ = api.sepllm_attn_workspace_bytes(desc, idesc)
-    assert api.sepllm_attn_prefix_workspace_bytes(desc, idesc, 300) >= fwd + 2 * 4 * 50 * (128 + 1) * 4
+    assert api.sepllm_attn_prefix_workspace_bytes(desc, idesc, 30000) >= fwd + 2 * 4 * 50 * (128 + 1) * 4
     with pytest.raises(api.SepllmError):
         api.sepllm_attn_prefix_workspace_bytes(desc, idesc, 0)
 
