@@ -490,7 +490,8 @@ sepllm_status sepllm_prefix_from_cache(const sepllm_cache_desc* desc, const void
  * b.  A sequence that sees no entry at all gets o = 0 and lse = -inf.  o 16-byte
  * aligned; workspace of sepllm_decode_prefix_workspace_bytes, 256-byte aligned
  * (its first word is the device status); other arguments as sepllm_decode and
- * above.  The prefix is read once for all sequences. */
+ * above.  The prefix is read once for all sequences, unless it is so short or they
+ * are so few that reading it with each of them is faster. */
 sepllm_status sepllm_decode_prefix_workspace_bytes(const sepllm_cache_desc* desc, int32_t P,
                                                    size_t* bytes);
 sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int32_t P, float scale,

@@ -536,18 +536,13 @@ constexpr int decode_smem_bytes() {
 //
 // PFX: the entries are those of a shared prefix, rows [0, prefix_len[b]) of Kp, Vp, followed by the
 // sequence's own.
-struct SharedPrefix {
-  const __nv_bfloat16 *Kp, *Vp;
-  const int32_t* prefix_len;  // null: P for all
-  int P;
-};
 template <int D, bool ROPE, bool WIDE, bool PFX>
 __global__ void __launch_bounds__(kDecThreads, 3)   // three CTAs per SM: at most 168 registers
 decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __restrict__ q_in,
              const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ Kc,
              const __nv_bfloat16* __restrict__ Vc, float* __restrict__ part_ml,
              float* __restrict__ part_acc, int splits, const float2* __restrict__ rope,
-             int32_t* __restrict__ status, const SharedPrefix pfx) {
+             int32_t* __restrict__ status, const PrefixRows pfx) {
   constexpr int CH = D / 8;                 // 16-byte chunks per row
   constexpr int ROWB = D * 2;               // bytes per row
   constexpr int TILEB = kDecTile * ROWB;    // bytes of one K (or V) tile
@@ -955,7 +950,7 @@ template <int D, bool ROPE, bool WIDE, bool PFX = false>
 static sepllm_status launch_decode(const sepllm_cache_header& h, float scale_log2, const void* q,
                                    const void* state, const void* Kc, const void* Vc, float* ml,
                                    float* acc, int splits, const float2* rope, int32_t* status,
-                                   cudaStream_t stream, const SharedPrefix& pfx = SharedPrefix{}) {
+                                   cudaStream_t stream, const PrefixRows& pfx = PrefixRows{}) {
   constexpr int smem = decode_smem_bytes<D>();
   static_assert(smem >= (kDecThreads / 32) * 16 * (8 + D * 4), "partials fit in the stage buffers");
   auto kernel = decode_split<D, ROPE, WIDE, PFX>;
@@ -1144,7 +1139,7 @@ extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int
   float* ml = reinterpret_cast<float*>(ws + kAlign);
   float* acc = reinterpret_cast<float*>(ws + plan.off_acc);
   if (plan.direct) {
-    const SharedPrefix pfx{static_cast<const __nv_bfloat16*>(Kp), static_cast<const __nv_bfloat16*>(Vp), prefix_len, P};
+    const PrefixRows pfx{Kp, Vp, prefix_len, P};
     const bool wide = desc->Hq / desc->Hkv > 8;
     const float scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
 #define SEPLLM_DEC(D, W)                                                                                      \
