@@ -6,7 +6,7 @@
 // not on the head, so a thread takes one token and eight pairs, computes their cos and sin once and
 // walks the heads with them; there is no table to build, size or read.  Measured: 65 536 tokens of 48
 // heads x 128 in bf16, 1.61 GB, in 248 us (6.5 TB/s, the rate of a plain copy; 267 before the loads of
-// several heads went out together), fp32 gradients of 16 384 such tokens to bf16 in 94 us (6.4 TB/s).
+// several heads went out together), fp32 gradients of 16 384 such tokens to bf16 in 93 us (6.5 TB/s).
 #include <algorithm>
 #include <cmath>
 
@@ -446,10 +446,13 @@ sepllm_status rope(const sepllm_rope_desc* d, const int64_t* positions, const se
                                                      : p.tokens * (d->d / 16);
   const int64_t blocks = (threads + kRopeThreads - 1) / kRopeThreads;
   if (blocks > 0x7fffffff) return SEPLLM_UNSUPPORTED;
-  // Heads are walked by one thread as long as that leaves enough threads to fill the SMs (2048 each);
-  // a thread of its own costs every group of heads another eight sines and cosines.
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(p.n_heads, int64_t(kSmCount) * 2048 / threads));
-  p.heads_per_block = int((p.n_heads + want - 1) / want);
+  // Heads are walked by one thread as long as that leaves threads to fill the SMs twice (2 x 2048 each); a
+  // thread of its own costs every group of heads another eight sines and cosines.  Whole batches of
+  // loads to a group.  Measured (us) with one, two, four times 1024 threads an SM: 36 heads x 64 of 8 x
+  // 2048 tokens 29.6 / 28.4 / 28.8, 48 x 128 of 16 384 (fp32 in) 100 / 95 / 93, 14 x 80 of 5997 all 6.6,
+  // and 8.5 with groups that do not fill their batches.
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(p.n_heads, int64_t(kSmCount) * 4096 / threads));
+  p.heads_per_block = int((p.n_heads + want - 1) / want + 3) / 4 * 4;
   const int64_t groups = (p.n_heads + p.heads_per_block - 1) / p.heads_per_block;
   if (groups > 65535) return SEPLLM_UNSUPPORTED;
   const dim3 grid{unsigned(blocks), unsigned(groups)};
