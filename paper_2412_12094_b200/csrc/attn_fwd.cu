@@ -61,6 +61,7 @@ gather_side_kv(const __nv_bfloat16* __restrict__ K, const __nv_bfloat16* __restr
                __nv_bfloat16* __restrict__ Vs, int32_t* __restrict__ status) {
   constexpr int LPR = D / 8;
   constexpr int RPB = 256 / LPR;
+  let_dependents_start();
   const int b = blockIdx.z, hk = blockIdx.y;
   if (threadIdx.x == 0 && (blockIdx.x | blockIdx.y | blockIdx.z) == 0) *status = SEPLLM_OK;
   const int r = blockIdx.x * RPB + threadIdx.x / LPR, l = threadIdx.x % LPR;
@@ -162,7 +163,10 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     g1 = load_slot<PFX>(p.tile_meta, p.seq_len, b, p.T, t, hx, p.side_tiles_cap, dv, p.L, p.n_neighbor, plen,
                         p.lim, p.side_cap);
   }
-  if (g0.t < 0 && g1.t < 0) return;   // both tiles are padding: nothing to do, nothing written
+  if (g0.t < 0 && g1.t < 0) {   // both tiles are padding: nothing to do, nothing written
+    if (MODE != kFwdPlain) wait_for_prior();   // (this kernel's end stands for the end of the gather)
+    return;
+  }
   const int kv_plane = b * p.Hkv + g1.hq / G;
   // key tiles of the CTA: side tiles [sbase, sbase + ns), then window tiles [wlo, whi)
   const int sbase = min(g0.s0, g1.s0);
@@ -187,6 +191,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     tmem_alloc(tmem_slot, 512);
     tmem_relinquish();
   }
+  if (MODE != kFwdPlain) wait_for_prior();   // the gather of the side rows, beside whose end this kernel starts
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -518,6 +523,7 @@ gather_prefix_side(const __nv_bfloat16* __restrict__ K, const __nv_bfloat16* __r
                    int32_t* __restrict__ status) {
   constexpr int LPR = D / 8;
   constexpr int RPB = 256 / LPR;
+  let_dependents_start();
   const int b = blockIdx.z, hk = blockIdx.y;
   if (threadIdx.x == 0 && (blockIdx.x | blockIdx.y | blockIdx.z) == 0) *status = SEPLLM_OK;
   const int r = blockIdx.x * RPB + threadIdx.x / LPR, l = threadIdx.x % LPR;
@@ -629,7 +635,11 @@ static sepllm_status launch_fwd(const sepllm_attn_desc* d, const sepllm_index_de
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
   const dim3 grid = p.pair_heads ? dim3(d->Hq / 2 * d->B, ih.n_tiles)
                                  : dim3(d->Hq * d->B, (ih.n_tiles + 1) / 2);
-  attn_fwd_kernel<D, MODE><<<grid, kFwdThreads, smem, stream>>>(mq, mk, mv, mks, mvs, p);
+  if (MODE == kFwdPlain)
+    attn_fwd_kernel<D, MODE><<<grid, kFwdThreads, smem, stream>>>(mq, mk, mv, mks, mvs, p);
+  else
+    SEPLLM_CUDA_TRY(launch_overlapped(attn_fwd_kernel<D, MODE>, grid, dim3(kFwdThreads), smem, stream, mq, mk, mv, mks,
+                                      mvs, p));
   record_event(d, 2, stream);
   SEPLLM_CUDA_TRY(cudaGetLastError());
   return SEPLLM_OK;

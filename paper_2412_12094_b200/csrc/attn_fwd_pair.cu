@@ -93,7 +93,10 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
   const int b = int(blockIdx.x) / heads_x, hx = int(blockIdx.x) % heads_x;
   const int t = p.T - 1 - int(blockIdx.y);
   const int G = p.Hq / p.Hkv;
-  if (t * kBM >= p.seq_len[b]) return;   // a tile of padding (the same for both CTAs of the pair)
+  if (t * kBM >= p.seq_len[b]) {   // a tile of padding (the same for both CTAs of the pair)
+    if (MODE != kFwdPlain) wait_for_prior();   // (this kernel's end stands for the end of the gather)
+    return;
+  }
   const DocView dv = doc_view(p.index_header, p.cnt, p.doc_start, p.doc_end);
   constexpr bool PFX = MODE == kFwdPrefix;
   const int plen = PFX ? prefix_of(p, b) : 0;
@@ -127,6 +130,7 @@ attn_fwd_pair_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     tmem_alloc_pair(tmem_slot, 512);
     tmem_relinquish_pair();
   }
+  if (MODE != kFwdPlain) wait_for_prior();   // the gather of the side rows, beside whose end this kernel starts
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();   // both CTAs' barriers and tensor memory exist before anyone signals across
@@ -441,7 +445,10 @@ sepllm_status launch_fwd_pair(const sepllm_attn_desc* d, const FwdParams& p, int
   SEPLLM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
   // x = pairs of query heads of every sequence: even, and a cluster never straddles two kv heads
   const dim3 grid(d->Hq / 2 * d->B, n_tiles);
-  kernel<<<grid, kPairThreads, smem, stream>>>(mq, mk64, mv, mks64, mvs, p);
+  if (mode == kFwdPlain)
+    kernel<<<grid, kPairThreads, smem, stream>>>(mq, mk64, mv, mks64, mvs, p);
+  else
+    SEPLLM_CUDA_TRY(launch_overlapped(kernel, grid, dim3(kPairThreads), smem, stream, mq, mk64, mv, mks64, mvs, p));
   SEPLLM_CUDA_TRY(cudaGetLastError());
   return SEPLLM_OK;
 }
