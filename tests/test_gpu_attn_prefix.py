@@ -342,3 +342,48 @@ def test_packed_rows_with_many_documents_in_the_direct_form():
         O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, None)
         f = np.isin(ids, inputs.SEP_IDS)
         _check(Q, K, V, Kp, Vp, [orc.packed_mask_matrix(f[0], df[0], 3, 16)], [P], [L], O, LSE)
+
+
+def test_two_streams_at_once():
+    """Pre-filling on one stream and decoding on another, each in its own workspace, both forms of each."""
+    g = torch.Generator(device="cuda").manual_seed(18)
+    Hq, Hkv, d, L, B = 8, 2, 128, 200, 3
+    ids = inputs.token_ids(18, B, L, 0.1)
+    idesc, index = _index(ids, 24, 0)
+    Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hkv, L, d), _normal(g, B, Hkv, L, d)
+    desc = api.AttnDesc(B, Hq, Hkv, d, L, 0.0, 0)
+    cd = api.CacheDesc(48, Hkv, Hq, d, 0, 4, 3, 16)
+    state = api.alloc_bytes(api.sepllm_cache_bytes(cd)[0])
+    api.sepllm_cache_init(cd, state)
+    Kc = torch.zeros((48, Hkv, 20, d), dtype=BF, device="cuda")
+    q = _normal(g, 48, Hq, d)
+    jobs = []
+    for P in (200, 7000):
+        Kp, Vp = _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
+        for _ in range(2):
+            wa = api.alloc_bytes(api.sepllm_attn_prefix_workspace_bytes(desc, idesc, P))
+            wd = api.alloc_bytes(api.sepllm_decode_prefix_workspace_bytes(cd, P))
+            out = (torch.empty_like(Q), torch.empty((B, Hq, L), device="cuda"), torch.empty_like(q),
+                   torch.empty((48, Hq), device="cuda"))
+            jobs.append((P, Kp, Vp, wa, wd, out))
+
+    def attn(j):
+        api.sepllm_attn_prefix_fwd(desc, idesc, j[0], Q, K, V, index, j[1], j[2], None, *j[5][:2], j[3])
+
+    def dec(j):
+        api.sepllm_decode_prefix(cd, j[0], 0.0, q, state, Kc, Kc, j[1], j[2], None, *j[5][2:], j[4])
+    for j in jobs[::2]:      # one after the other
+        attn(j), dec(j)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(20):
+        with torch.cuda.stream(s1):
+            for j in jobs[1::2]:
+                attn(j)
+        with torch.cuda.stream(s2):
+            for j in jobs[1::2]:
+                dec(j)
+    torch.cuda.synchronize()
+    for a, b in zip(jobs[::2], jobs[1::2]):
+        assert all(torch.equal(x, y) for x, y in zip(a[5], b[5]))
+        assert api.sepllm_last_device_status(b[3]) == 0 and api.sepllm_last_device_status(b[4]) == 0
