@@ -55,15 +55,18 @@ ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "llama3": 4, "fact
 
 
 class RopeDesc(C.Structure):
-    """sepllm_rope_desc.  rot_dim 0 = d; layout and scaling by name; freq_factors: a sequence of
-    rot_dim / 2 numbers; pos_stride defaults to L (positions [B][L])."""
+    """sepllm_rope_desc.  rot_dim 0 = d; layout and scaling by name; high defaults to 32 for "yarn" and
+    4 otherwise; freq_factors: a sequence of rot_dim / 2 numbers; pos_stride defaults to L (positions
+    [B][L])."""
     _fields_ = ([(n, C.c_int32) for n in ("B", "L", "Hq", "Hkv", "d", "rot_dim", "layout", "scaling")]
                 + [(n, C.c_double) for n in ("base", "factor", "low", "high", "orig_len", "attn_factor")]
                 + [("freq_factors", C.POINTER(C.c_double)), ("pos_first", C.c_int64), ("pos_stride", C.c_int64)])
 
     def __init__(self, B, L, Hq, Hkv, d, rot_dim=0, layout="half", scaling="none", base=10000.0, factor=1.0,
-                 low=1.0, high=4.0, orig_len=8192.0, attn_factor=0.0, freq_factors=None, pos_first=0,
+                 low=1.0, high=None, orig_len=8192.0, attn_factor=0.0, freq_factors=None, pos_first=0,
                  pos_stride=None):
+        if high is None:
+            high = 32.0 if scaling in ("yarn", ROPE_SCALINGS["yarn"]) else 4.0
         self._keep = None
         if freq_factors is not None:
             n = (rot_dim or d) // 2
