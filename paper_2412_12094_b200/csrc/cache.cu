@@ -530,13 +530,14 @@ constexpr int decode_smem_bytes() {
 // then carries the softmax state of rows frow and frow + 8); narrower groups leave the upper
 // half zero and skip its arithmetic.
 //
-// status null: the kernel runs beside the prefix kernel launched before it (which writes the status
+// kDecBeside: the kernel runs beside the prefix kernel launched before it (which writes the status
 // word) and shares no memory with it; its last CTA ends only when that kernel has, so that what is
 // launched next finds both complete.
 //
-// PFX: the entries are those of a shared prefix, rows [0, prefix_len[b]) of Kp, Vp, followed by the
-// sequence's own.
-template <int D, bool ROPE, bool WIDE, bool PFX>
+// kDecPrefix: the entries are those of a shared prefix, rows [0, prefix_len[b]) of Kp, Vp, followed by
+// the sequence's own.
+enum DecodeMode { kDecPlain = 0, kDecBeside = 1, kDecPrefix = 2 };
+template <int D, bool ROPE, bool WIDE, int MODE>
 __global__ void __launch_bounds__(kDecThreads, 3)   // three CTAs per SM: at most 168 registers
 decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __restrict__ q_in,
              const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ Kc,
@@ -555,7 +556,8 @@ decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __res
   const int G = d.Hq / d.Hkv;
   const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  if (status && tid == 0 && (split | hk | b) == 0) *status = SEPLLM_OK;
+  constexpr bool PFX = MODE == kDecPrefix;
+  if (MODE != kDecBeside && tid == 0 && (split | hk | b) == 0) *status = SEPLLM_OK;
   CacheView cv = cache_view(const_cast<uint8_t*>(state), h);
   const sepllm_cache_seq sq = cv.seq[b];
   const int plen = !PFX ? 0 : pfx.prefix_len ? max(0, min(pfx.P, pfx.prefix_len[b])) : pfx.P;
@@ -755,7 +757,7 @@ decode_split(sepllm_cache_header h, float scale_log2, const __nv_bfloat16* __res
     part_acc[uo * D + e] = aa;
     if (e == 0) { part_ml[uo * 2] = mm; part_ml[uo * 2 + 1] = ll; }
   }
-  if (!status && split == int(gridDim.x) - 1 && hk == int(gridDim.y) - 1 && b == int(gridDim.z) - 1)
+  if (MODE == kDecBeside && split == int(gridDim.x) - 1 && hk == int(gridDim.y) - 1 && b == int(gridDim.z) - 1)
     wait_for_prior();
 }
 
@@ -946,20 +948,20 @@ extern "C" sepllm_status sepllm_decode_workspace_bytes(const sepllm_cache_desc* 
   return SEPLLM_OK;
 }
 
-template <int D, bool ROPE, bool WIDE, bool PFX = false>
+template <int D, bool ROPE, bool WIDE, int MODE>
 static sepllm_status launch_decode(const sepllm_cache_header& h, float scale_log2, const void* q,
                                    const void* state, const void* Kc, const void* Vc, float* ml,
                                    float* acc, int splits, const float2* rope, int32_t* status,
                                    cudaStream_t stream, const PrefixRows& pfx = PrefixRows{}) {
   constexpr int smem = decode_smem_bytes<D>();
   static_assert(smem >= (kDecThreads / 32) * 16 * (8 + D * 4), "partials fit in the stage buffers");
-  auto kernel = decode_split<D, ROPE, WIDE, PFX>;
+  auto kernel = decode_split<D, ROPE, WIDE, MODE>;
   SEPLLM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   const dim3 grid(splits, h.desc.Hkv, h.desc.B);
   auto qb = static_cast<const __nv_bfloat16*>(q), kb = static_cast<const __nv_bfloat16*>(Kc),
        vb = static_cast<const __nv_bfloat16*>(Vc);
   auto sb = static_cast<const uint8_t*>(state);
-  if (status)
+  if (MODE != kDecBeside)
     kernel<<<grid, kDecThreads, smem, stream>>>(h, scale_log2, qb, sb, kb, vb, ml, acc, splits, rope, status, pfx);
   else
     SEPLLM_CUDA_TRY(launch_overlapped(kernel, grid, kDecThreads, smem, stream, h, scale_log2, qb, sb, kb, vb, ml, acc,
@@ -973,13 +975,15 @@ static sepllm_status dispatch_decode(bool with_rope, bool wide, const sepllm_cac
                                      const void* Kc, const void* Vc, float* ml, float* acc,
                                      int splits, const float2* rope, int32_t* status,
                                      cudaStream_t stream) {
-#define SEPLLM_DEC(R, W) launch_decode<D, R, W>(h, scale_log2, q, state, Kc, Vc, ml, acc, splits, rope, status, stream)
-  if (with_rope) return wide ? SEPLLM_DEC(true, true) : SEPLLM_DEC(true, false);
-  return wide ? SEPLLM_DEC(false, true) : SEPLLM_DEC(false, false);
+#define SEPLLM_DEC(R, W, M) \
+  launch_decode<D, R, W, M>(h, scale_log2, q, state, Kc, Vc, ml, acc, splits, rope, status, stream)
+  if (!status) return wide ? SEPLLM_DEC(false, true, kDecBeside) : SEPLLM_DEC(false, false, kDecBeside);
+  if (with_rope) return wide ? SEPLLM_DEC(true, true, kDecPlain) : SEPLLM_DEC(true, false, kDecPlain);
+  return wide ? SEPLLM_DEC(false, true, kDecPlain) : SEPLLM_DEC(false, false, kDecPlain);
 #undef SEPLLM_DEC
 }
 
-// The partial results of a decode over the sequences' own caches, at `parts`.
+// The partial results of a decode over the sequences' own caches (status null: beside the prefix kernel).
 static sepllm_status launch_own_parts(const sepllm_cache_header& h, float scale, const void* q, const void* state,
                                       const void* Kc, const void* Vc, const float2* rope, int splits, float* ml,
                                       float* acc, int32_t* status, cudaStream_t stream) {
@@ -1143,7 +1147,7 @@ extern "C" sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int
     const bool wide = desc->Hq / desc->Hkv > 8;
     const float scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
 #define SEPLLM_DEC(D, W)                                                                                      \
-  launch_decode<D, false, W, true>(h, scale_log2, q, state, Kc, Vc, ml, acc, own_parts, nullptr,            \
+  launch_decode<D, false, W, kDecPrefix>(h, scale_log2, q, state, Kc, Vc, ml, acc, own_parts, nullptr,            \
                                    reinterpret_cast<int32_t*>(ws), stream, pfx)
     st = desc->d == 128 ? (wide ? SEPLLM_DEC(128, true) : SEPLLM_DEC(128, false))
                         : (wide ? SEPLLM_DEC(64, true) : SEPLLM_DEC(64, false));
