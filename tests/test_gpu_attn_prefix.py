@@ -387,3 +387,38 @@ def test_two_streams_at_once():
     for a, b in zip(jobs[::2], jobs[1::2]):
         assert all(torch.equal(x, y) for x, y in zip(a[5], b[5]))
         assert api.sepllm_last_device_status(b[3]) == 0 and api.sepllm_last_device_status(b[4]) == 0
+
+
+@pytest.mark.parametrize("P", [200, 9000])
+def test_events_between_the_launches(P):
+    """The descriptor's events are recorded as by the plain forward; the results stay what they are."""
+    g = torch.Generator(device="cuda").manual_seed(19)
+    B, Hq, Hkv, d, L = 2, 4, 1, 128, 150
+    ids = inputs.token_ids(19, B, L, 0.1)
+    idesc, index = _index(ids, 24, 0)
+    Q, K, V = _normal(g, B, Hq, L, d), _normal(g, B, Hkv, L, d), _normal(g, B, Hkv, L, d)
+    Kp, Vp = _normal(g, Hkv, P, d), _normal(g, Hkv, P, d)
+    want = _run(Q, K, V, idesc, index, Kp, Vp, None)
+    desc = api.AttnDesc(B, Hq, Hkv, d, L, 0.0, 0)
+    events = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
+    for e in events:
+        e.record()
+    desc.set_events(events)
+    ws = api.alloc_bytes(api.sepllm_attn_prefix_workspace_bytes(desc, idesc, P))
+    O, LSE = torch.empty_like(Q), torch.empty((B, Hq, L), device="cuda")
+    for _ in range(3):
+        api.sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, None, O, LSE, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(O, want[0]) and torch.equal(LSE, want[1])
+    assert events[0].elapsed_time(events[1]) > 0 and events[1].elapsed_time(events[2]) > 0
+
+
+@pytest.mark.parametrize("P,B,L", [(300, 3, 200), (6000, 3, 200), (50, 2, 1)])
+def test_a_batch_of_padding_alone_writes_nothing(P, B, L):
+    g = torch.Generator(device="cuda").manual_seed(20)
+    ids = inputs.token_ids(20, B, L, 0.1)
+    idesc, index = _index(ids, 24, 0, [0] * B)
+    Q, K, V = _normal(g, B, 4, L, 128), _normal(g, B, 1, L, 128), _normal(g, B, 1, L, 128)
+    Kp, Vp = _normal(g, 1, P, 128), _normal(g, 1, P, 128)
+    O, LSE = _run(Q, K, V, idesc, index, Kp, Vp, None)
+    assert (O == 3.5).all() and (LSE == -2.5).all()
