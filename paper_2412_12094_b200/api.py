@@ -117,7 +117,7 @@ _ARGTYPES = {
     "sepllm_rope_fwd": [_P] * 5, "sepllm_rope_bwd": [_P] * 5,
     "sepllm_prefix_from_cache": [_P] * 4 + [_I] + [_P] * 3 + [_I, _P],
     "sepllm_decode_prefix": [_P, _I, C.c_float] + [_P] * 11,
-    "sepllm_attn_prefix_fwd": [_P, _P, _I] + [_P] * 10,
+    "sepllm_attn_prefix_fwd": [_P, _P, _I] + [_P] * 11,
 }
 
 _lib = None
