@@ -21,6 +21,7 @@
 #include <cmath>
 
 #include "attn_common.cuh"
+#include "prefix_sync.h"
 
 namespace sepllm {
 
@@ -495,7 +496,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         // special-function unit (16 a clock and SM), in turn one slot's exponentials run under the
         // other's loads, maxima and stores.  Warps 4 + i and 8 + i share a scheduler and its part of that
         // unit, so the turn passes between these two, over named barriers (mbarriers: 500 cycles a turn).
-        if (x == 1 ? j < n_both : j > 0 && j < n_both) named_sync(x == 0 ? 7 + (warp & 3) : 3 + (warp & 3), 64);
+        if (turn_waits(x, j, n_both)) named_sync(x == 0 ? 7 + (warp & 3) : 3 + (warp & 3), 64);
         const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
         const unsigned long long scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
         const unsigned long long negm2 = pack_f32x2(neg_m, neg_m);
@@ -511,7 +512,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
             sreg[c][e >> 1] = pack_bf16(p0, p1);
           }
         const float2 sm = unpack_f32x2(add_f32x2(add_f32x2(ps2[0], ps2[1]), add_f32x2(ps2[2], ps2[3])));
-        if (x == 0 ? j < n_both : j + 1 < n_both) named_arrive(x == 0 ? 3 + (warp & 3) : 7 + (warp & 3), 64);
+        if (turn_passes(j, n_both)) named_arrive(x == 0 ? 3 + (warp & 3) : 7 + (warp & 3), 64);
         l_sum = l_sum * corr + (sm.x + sm.y);
         // P V of the slot's previous tile is complete: the buffer of P is free and O_x is at rest
         if (j > 0) {
@@ -622,6 +623,8 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         }
       }
       tc_fence_before();   // O_x is read: the next segment's first product into it waits for P of this thread
+      // (slot 1 was through with its last exponentials long ago)
+      if (turn_returns(x, n_both)) named_sync(7 + (warp & 3), 64);
       // where the unit's parts are, from the CTA that has its first key tile
       if (sg->j0 == 0 && tid == 128) {
         // number of the unit's last key tile, and the CTA that has it
