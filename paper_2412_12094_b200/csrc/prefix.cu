@@ -158,18 +158,20 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
   uint64_t* bar_sl = bars + 6;     // [2]   S_x read into registers by the 4 softmax warps
   uint64_t* bar_p = bars + 8;      // [2]   P_x written
   uint64_t* bar_pv = bars + 10;    // [2]   P_x V complete: P_x may be rewritten, O_x is at rest
-  uint64_t* bar_g = bars + 12;     //       V of the last tile landed: clear the rows behind the prefix
-  uint64_t* bar_z = bars + 13;     //       they are cleared
-  uint64_t* bar_d = bars + 14;     // [2]   every product and arrival of slot x done
-  uint64_t* bar_f = bars + 16;     // [NST] ring stage full
+  uint64_t* bar_g = bars + 12;     // [2]   slot x asks for the rows of V behind the prefix to be cleared
+  uint64_t* bar_z = bars + 14;     // [2]   they are, for slot x
+  uint64_t* bar_d = bars + 16;     // [2]   every product and arrival of slot x done
+  uint64_t* bar_f = bars + 18;     // [NST] ring stage full
   uint64_t* bar_r = bar_f + NST;   // [NST] ring stage free (both slots)
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 16 + 2 * NST);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 18 + 2 * NST);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
   int* s_warp = reinterpret_cast<int*>(tmem_slot + 4);   // [12] key tiles per warp of the scan
   int* s_start = s_warp + 12;                            // [2] pair and offset where the run starts
   int* s_run = s_warp + 14;                              // end of the run, tiles per run, longer runs, pairs
   Segment* s_seg = reinterpret_cast<Segment*>(s_run + 4);    // [12] place of each warp in the run
   uint8_t* s_id = reinterpret_cast<uint8_t*>(s_seg + 12);    // [2 * pairs] number of those row tiles
+  static_assert((18 + 2 * NST) * 8 + 16 + 18 * 4 + 12 * sizeof(Segment) + 2 * kMaxPairs <= C::kTotal - C::kBar,
+                "barriers, places and tile numbers fit behind kBar");
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const bool alt = p.alternate != 0;
@@ -183,10 +185,8 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_q + i, 1); mbar_init(bar_qe + i, 1); mbar_init(bar_s + i, 1);
       mbar_init(bar_sl + i, 4); mbar_init(bar_p + i, 4); mbar_init(bar_pv + i, 1);
-      mbar_init(bar_d + i, 1);
+      mbar_init(bar_g + i, 1); mbar_init(bar_z + i, 1); mbar_init(bar_d + i, 1);
     }
-    mbar_init(bar_g, 1);
-    mbar_init(bar_z, 1);
     for (int i = 0; i < NST; ++i) { mbar_init(bar_f + i, 1); mbar_init(bar_r + i, 2); }
     *abort_flag = 0;
     fence_mbar_init();
@@ -339,10 +339,7 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
       int at0 = 0;                                        // tiles loaded for earlier segments
       for (int n = 0; next_segment<false>(sg, tab, s_run[3]); ++n) {
         const int n_tiles = sg->j1 - sg->j0, n_mine = slot_tiles(sg, alt, x);
-        const bool clear_v = ends_inside(sg, p.P);
-        // the slot that uses the last tile (the first such one) has its V cleared
-        const bool clears = clear_v && (alt ? ((n_tiles - 1) & 1) == x
-                                            : n_mine == n_tiles && (x == 0 || slot_tiles(sg, false, 0) < n_tiles));
+        const bool ask = ends_inside(sg, p.P) && uses_last(alt, x, n_tiles, n_mine);
         auto mine = [&](int j) { return alt ? (j & 1) == x : j < n_mine; };
         int left_s = n_mine;      // S products still to issue
         bool s_out = false;       // an S product has been issued in this segment
@@ -368,13 +365,13 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
         bool o_begun = false;
         auto values = [&](int j) {
           const int at = at0 + v_place(j, n_tiles), st = at % NST;
-          if (mine(j)) { wait(bar_p + x, ph_p); ph_p ^= 1; }
           wait(bar_f + st, (at / NST) & 1);
-          if (clear_v && j == n_tiles - 1) {
-            if (clears) mbar_arrive(bar_g);
-            if (mine(j)) wait(bar_z, ph_z);
-          }
           if (!mine(j)) { mbar_arrive(bar_r + st); return; }
+          const bool cleared = ask && j == n_tiles - 1;
+          if (cleared) mbar_arrive(bar_g + x);   // (the clearing runs under this tile's softmax)
+          wait(bar_p + x, ph_p);
+          ph_p ^= 1;
+          if (cleared) { wait(bar_z + x, ph_z); ph_z ^= 1; }
           tc_fence_after();
           const uint32_t v_lo = v_lo0 + st * (C::kTile >> 4);
           umma_ss_lo(tO, p_lo, v_lo, idesc_o, o_begun);
@@ -399,7 +396,6 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
           // (at the end, when the producer is past its wait for the segment before)
           mbar_arrive(bar_qe + x);
         }
-        if (clear_v) ph_z ^= 1;
         at0 += 2 * n_tiles;
       }
       // no arrival may be under way when the CTA ends
@@ -407,21 +403,28 @@ prefix_attn(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CU
       wait(bar_d + x, 0);
     } else if (warp == 3) {
       // ---------------- V rows behind the longest prefix ----------------
-      int n_clear = 0, at0 = 0;
+      int ph_g[2] = {0, 0}, at0 = 0;
       while (next_segment<true>(sg, tab, s_run[3])) {
         const int n_tiles = sg->j1 - sg->j0;
         const int st = (at0 + v_place(n_tiles - 1, n_tiles)) % NST;
         at0 += 2 * n_tiles;
         if (!ends_inside(sg, p.P)) continue;
         const int r0 = max(sg->len[0], sg->len[1]) - (sg->j1 - 1) * kBN;
-        wait(bar_g, n_clear++ & 1);
+        bool asks[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          asks[x] = uses_last(alt, x, n_tiles, slot_tiles(sg, alt, x));
+          if (asks[x]) { wait(bar_g + x, ph_g[x]); ph_g[x] ^= 1; }
+        }
         for (int i = lane; i < (kBN - r0) * 8 * NB; i += 32) {
           const int ch = i & 7, blk = (i >> 3) % NB, r = r0 + (i >> 3) / NB;
           *reinterpret_cast<uint4*>(sKV + st * C::kTile + blk * kTileBlockBytes + r * 128 + ch * 16) =
               make_uint4(0, 0, 0, 0);
         }
         fence_proxy_async_smem();
-        mbar_arrive_warp(bar_z);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (asks[x]) mbar_arrive_warp(bar_z + x);
       }
     }
   } else {

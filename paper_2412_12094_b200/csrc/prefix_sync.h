@@ -24,4 +24,15 @@ SEPLLM_HD bool turn_passes(int j, int n_both) { return j < n_both; }
 // and takes it back at the segment's end.
 SEPLLM_HD bool turn_returns(int x, int n_both) { return x == 0 && n_both > 0; }
 
+// V rows behind the longest prefix, in the last of a segment's n_tiles key tiles: each slot that multiplies
+// with that tile asks a fourth warp to have them cleared, once the tile has landed, and waits for the
+// answer.  Request and answer have a barrier for each slot, so that a slot is never more than one phase
+// away from the warp that clears, whatever the other slot is at: one that leaves a last tile to the other
+// goes on to the next segments at once.
+//
+// Slot x multiplies with the last tile (n_mine: its tiles of the segment; alt: the slots take them in turn).
+SEPLLM_HD bool uses_last(bool alt, int x, int n_tiles, int n_mine) {
+  return alt ? ((n_tiles - 1) & 1) == x : n_mine == n_tiles;
+}
+
 }  // namespace sepllm

@@ -101,3 +101,99 @@ SEGMENTS += [list(s) for s in itertools.product([(1, 1), (2, 1), (1, 2), (0, 1),
 @pytest.mark.parametrize("segments", SEGMENTS, ids=str)
 def test_turns_are_handed_over_one_at_a_time(turns, segments):
     _walk(turns(segments))
+
+
+CLEARS = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "prefix_sync.h"
+// arguments: alternate mode; then key tiles of slot 0 and slot 1 (in alternate mode of both together, and
+// 0), segment by segment.  Every segment ends inside its last tile.
+int main(int argc, char** argv) {
+  const bool alt = std::atoi(argv[1]);
+  int ph_z[2] = {0, 0}, ph_g[2] = {0, 0};
+  for (int who = 0; who < 3; ++who, std::printf("\n"))
+    for (int i = 2; i + 1 < argc; i += 2) {
+      const int a = std::atoi(argv[i]), b = std::atoi(argv[i + 1]), n = a > b ? a : b, seg = i / 2 - 1;
+      const int mine[2] = {alt ? (n + 1) / 2 : a, alt ? n / 2 : b};
+      if (who < 2) {
+        if (!sepllm::uses_last(alt, who, n, mine[who])) continue;
+        std::printf("ask%d:%d answer%d:%d use:%d ", who, seg, who, ph_z[who], seg);
+        ph_z[who] ^= 1;
+      } else {
+        for (int x = 0; x < 2; ++x)
+          if (sepllm::uses_last(alt, x, n, mine[x])) {
+            std::printf("request%d:%d ", x, ph_g[x]);
+            ph_g[x] ^= 1;
+          }
+        std::printf("clear:%d ", seg);
+        for (int x = 0; x < 2; ++x)
+          if (sepllm::uses_last(alt, x, n, mine[x])) std::printf("done%d:0 ", x);
+      }
+    }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def clears(tmp_path_factory):
+    exe = _compile(tmp_path_factory.mktemp("clears"), "clears", CLEARS)
+
+    def ops(alt, segments):
+        args = [str(int(alt))] + [str(n) for s in segments for n in s]
+        out = subprocess.run([exe] + args, check=True, capture_output=True, text=True).stdout
+        return [[(w.split(":")[0], int(w.split(":")[1])) for w in line.split()] for line in out.split("\n")[:3]]
+    return ops
+
+
+def _walk_clears(ops):
+    """All interleavings of the slots' issuers and the clearing warp over barriers of one arrival: a wait for
+    parity p passes when the phase under way has the other parity.  Nothing else holds them in step."""
+    todo, seen = [((0, 0, 0), (0, 0), (0, 0))], set()    # places, phases complete of requests and of answers
+    ended = False
+    while todo:
+        state = todo.pop()
+        if state in seen:
+            continue
+        seen.add(state)
+        pcs, asked, answered = state
+        done = [set(n for op, n in ops[w][:pcs[w]] if op == name) for w, name in ((0, "ask0"), (1, "ask1"), (2, "clear"))]
+        moved = False
+        for w in range(3):
+            if pcs[w] == len(ops[w]):
+                continue
+            op, n = ops[w][pcs[w]]
+            x, a, z = int(op[-1]) if op[-1].isdigit() else 0, list(asked), list(answered)
+            if op[:-1] == "ask":
+                a[x] += 1
+            elif op[:-1] == "done":
+                z[x] += 1
+            elif op[:-1] == "answer":
+                if z[x] % 2 == n:
+                    continue
+            elif op[:-1] == "request":
+                if a[x] % 2 == n:
+                    continue
+            elif op == "clear":
+                assert n in done[0] | done[1], f"segment {n} cleared before it was asked for"
+            elif op == "use":
+                assert n in done[2], f"segment {n} used before it was cleared"
+            moved = True
+            todo.append((tuple(p + (v == w) for v, p in enumerate(pcs)), tuple(a), tuple(z)))
+        if not moved:
+            assert all(pcs[w] == len(ops[w]) for w in range(3)), f"all wait: {state}"
+            ended = True
+    assert ended
+
+
+CLEAR_SEGMENTS = [list(s) for s in itertools.product([(1, 2), (2, 1), (2, 2)], repeat=4)]
+
+
+@pytest.mark.parametrize("segments", CLEAR_SEGMENTS, ids=str)
+def test_rows_behind_the_prefix_are_cleared_before_they_are_used(clears, segments):
+    _walk_clears(clears(False, segments))
+
+
+@pytest.mark.parametrize("segments", [list(s) for s in itertools.product([(1, 0), (2, 0), (5, 0)], repeat=3)], ids=str)
+def test_they_are_in_alternate_mode(clears, segments):
+    _walk_clears(clears(True, segments))
