@@ -276,9 +276,10 @@ sepllm_status sepllm_attn_bwd(const sepllm_attn_desc* desc, const sepllm_index_d
  *   NTK      base replaced by base * s^(r/(r-2))            (r > 2)
  *   YARN     f_i (1-g_i) + (f_i / s) g_i with g_i = clamp((i-lo)/(hi-lo), 0, 1),
  *            lo = max(0, floor(t(high))), hi = min(r-1, ceil(t(low))),
- *            t(n) = r ln(N / (2 pi n)) / (2 ln base): pairs that turn more than
- *            `high` times over N positions stay, those below `low` are stretched
- *            (hi = lo: hi is taken 0.001 larger)
+ *            t(n) = r ln(N / (2 pi n)) / (2 ln base): pairs up to lo, which turn more
+ *            than `high` times over N positions, stay, those from hi on, which turn
+ *            fewer than `low` times, are stretched by s (hi = lo: hi is taken 0.001
+ *            larger; lo > r-1: all stay; hi < 0: all are stretched)
  *   LLAMA3   f_i k_i + (f_i / s) (1-k_i), k_i = clamp((n_i-low)/(high-low), 0, 1),
  *            n_i = N f_i / (2 pi) the turns of the pair over N positions
  *   FACTORS  f_i / freq_factors[i]   (host array of r/2, read during the call)

@@ -783,6 +783,8 @@ def rope_frequencies(r: int, base: float, scaling: str = "none", factor: float =
     if scaling == "yarn":
         lo = max(0.0, np.floor(r * np.log(orig_len / (2 * np.pi * high)) / (2 * np.log(base))))
         hi = min(r - 1.0, np.ceil(r * np.log(orig_len / (2 * np.pi * low)) / (2 * np.log(base))))
+        if hi < lo:     # all pairs on one side of the ramp: stretched where hi is before the first, else kept
+            return f / factor if hi < 0 else f
         g = np.clip((i - lo) / (hi - lo if hi != lo else 0.001), 0.0, 1.0)
         return f * (1 - g) + f / factor * g
     if scaling == "llama3":

@@ -331,7 +331,11 @@ void rope_frequencies(const sepllm_rope_desc* d, double* f, double* m) {
     };
     lo = std::fmax(0.0, std::floor(pair_of(d->high)));
     hi = std::fmin(r - 1.0, std::ceil(pair_of(d->low)));
-    if (hi == lo) hi += 0.001;
+    // lo behind the last pair (all turn often): the ramp lies behind them; hi before the first one (all
+    // turn seldom): in front of them
+    if (hi < 0.0) lo = hi - 1.0;
+    else if (hi < lo) hi = lo + 1.0;
+    else if (hi == lo) hi += 0.001;
   }
   // base^(-2i/r) as base^(-16 (i/8)/r) * base^(-2 (i%8)/r): sixteen powers instead of sixty-four (a
   // call computes them anew), within two roundings
