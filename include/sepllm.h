@@ -490,8 +490,8 @@ sepllm_status sepllm_prefix_from_cache(const sepllm_cache_desc* desc, const void
  * softmax over prefix rows [0, prefix_len[b]) and the retained entries of sequence
  * b.  A sequence that sees no entry at all gets o = 0 and lse = -inf.  o 16-byte
  * aligned; workspace of sepllm_decode_prefix_workspace_bytes, 256-byte aligned
- * (its first word is the device status); other arguments as sepllm_decode and
- * above.  The prefix is read once for all sequences, unless it is so short or they
+ * (its first word is the device status; one sized for P rows serves every
+ * smaller P with the same desc); other arguments as sepllm_decode and above.  The prefix is read once for all sequences, unless it is so short or they
  * are so few that reading it with each of them is faster. */
 sepllm_status sepllm_decode_prefix_workspace_bytes(const sepllm_cache_desc* desc, int32_t P,
                                                    size_t* bytes);
@@ -510,7 +510,8 @@ sepllm_status sepllm_decode_prefix(const sepllm_cache_desc* desc, int32_t P, flo
  * written at all.  desc->events as there (the launches behind the attention are
  * not marked); SEPLLM_ATTN_SIDE_READY is not looked at, and the workspace holds no
  * side rows for later calls.  workspace of sepllm_attn_prefix_workspace_bytes,
- * 256-byte aligned.  Serving only: there is no gradient. */
+ * 256-byte aligned; one sized for P rows serves every smaller P with the same desc
+ * and idesc.  Serving only: there is no gradient. */
 sepllm_status sepllm_attn_prefix_workspace_bytes(const sepllm_attn_desc* desc,
                                                  const sepllm_index_desc* idesc, int32_t P,
                                                  size_t* bytes);

@@ -229,7 +229,7 @@ void launch_gather(const sepllm_attn_desc* d, const sepllm_index_desc* id, int c
                    void* Ks, void* Vs, int32_t* status, cudaStream_t stream);
 
 // Attention over a prefix shared by the batch (prefix.cu).
-constexpr int kSmCount = 148;
+constexpr int kSmCount = 148;   // (not sm_count(): plans and sizes are made without a device)
 struct PrefixParams {
   int B, Hkv, G, T, d, P;       // G query heads per kv head, T query tokens per sequence
   int key_tiles;                // 128-row tiles of the prefix
@@ -257,7 +257,8 @@ struct PrefixParams {
 // Sizes and tiles (false: too large).
 // own_us: time of the rows' own part where it runs beside the prefix kernel, 0 where it does not.
 bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, bool whole_parts, double own_us);
-size_t prefix_part_bytes(const PrefixParams& p);
+// Bytes of the parts, for any number of CTAs and any prefix of up to p.P rows.
+size_t prefix_part_bytes(PrefixParams p);
 void place_prefix_parts(PrefixParams* p, uint8_t* ws);
 // The prefix part and the join with the rows' own parts: own_parts of the decode kernel, launched by
 // beside(ctx) once the (first) prefix kernel is, or (beside null, own_parts = 0) p.own_O and p.own_lse.

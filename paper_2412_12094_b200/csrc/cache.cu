@@ -1107,7 +1107,9 @@ static sepllm_status plan_decode_prefix(const sepllm_cache_desc* desc, int P, Pr
   plan->own_parts = decode_splits(desc, plan->direct ? P : 0);
   plan->off_acc = kAlign + align_up(size_t(desc->B) * desc->Hq * plan->own_parts * 2 * sizeof(float));
   plan->off_pfx = kAlign + own_part_bytes(desc, plan->own_parts);
-  plan->bytes = plan->off_pfx + (plan->direct ? 0 : prefix_part_bytes(plan->p));
+  // for every prefix of up to P rows, whichever form the call takes there
+  plan->bytes = kAlign + std::max(own_part_bytes(desc, decode_splits(desc, P)),
+                                  own_part_bytes(desc, decode_splits(desc)) + prefix_part_bytes(plan->p));
   return SEPLLM_OK;
 }
 

@@ -826,10 +826,15 @@ int prefix_grid(const PrefixParams& p, int pairs) {
   return int(std::min<int64_t>(p.max_ctas, work));
 }
 
-int64_t max_parts(const PrefixParams& p) {
-  // two places per CTA, and one per unit where whole units leave parts (decode)
-  const int pairs = launch_pairs(p);
+// Parts of a launch over `pairs` pairs: two places per CTA, and one per unit where whole units leave parts (decode).
+int64_t max_parts(const PrefixParams& p, int pairs) {
   return 2ll * prefix_grid(p, pairs) + (p.whole_parts ? int64_t(pairs) * p.Hkv : 0);
+}
+
+size_t part_bytes(const PrefixParams& p, int pairs) {
+  const size_t rows = size_t(max_parts(p, pairs)) * 256;
+  return align_up(rows * 2 * sizeof(float)) + align_up(rows * kernel_head_dim(p.d) * sizeof(float)) +
+         align_up(size_t(pairs) * p.Hkv * sizeof(int4)) + align_up(kSmCount * sizeof(int32_t));
 }
 
 }  // namespace
@@ -870,14 +875,13 @@ bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, b
   return true;
 }
 
-size_t prefix_part_bytes(const PrefixParams& p) {
-  const size_t rows = size_t(max_parts(p)) * 256;
-  return align_up(rows * 2 * sizeof(float)) + align_up(rows * kernel_head_dim(p.d) * sizeof(float)) +
-         align_up(size_t(launch_pairs(p)) * p.Hkv * sizeof(int4)) + align_up(kSmCount * sizeof(int32_t));
+size_t prefix_part_bytes(PrefixParams p) {
+  p.max_ctas = kSmCount;
+  return part_bytes(p, std::min(all_pairs(p), kMaxPairs));
 }
 
 void place_prefix_parts(PrefixParams* p, uint8_t* ws) {
-  const size_t rows = size_t(max_parts(*p)) * 256;
+  const size_t rows = size_t(max_parts(*p, launch_pairs(*p))) * 256;
   p->part_ml = reinterpret_cast<float*>(ws);
   ws += align_up(rows * 2 * sizeof(float));
   p->part_acc = reinterpret_cast<float*>(ws);
@@ -920,11 +924,9 @@ namespace {
 // prefix kernel, which shares the loads, splits long prefixes and drops padding, with a workspace of
 // the forward's own | O32 | LSE of the own part | parts.
 struct AttnPrefixLayout {
-  bool direct;
   size_t off_o, off_lse, off_parts, bytes;
 };
-AttnPrefixLayout attn_prefix_layout(const sepllm_attn_desc* d, const sepllm_index_desc* id, const PrefixParams& p) {
-  AttnPrefixLayout a;
+bool attn_prefix_direct(const sepllm_attn_desc* d, const sepllm_index_desc* id, const PrefixParams& p) {
   // Microseconds: a wave of forward CTAs (two row tiles each, one CTA per SM) takes 6 and 2 for each key
   // tile; the copy its bytes at 5 TB/s; the prefix kernel 2 for each step of a CTA, and with the join 24
   // (14 where there is a single row tile).  Both measured (us, direct / shared; 32 heads on 8 of 128):
@@ -939,18 +941,29 @@ AttnPrefixLayout attn_prefix_layout(const sepllm_attn_desc* d, const sepllm_inde
   const double steps = double(all_pairs(p)) * d->Hkv * p.key_tiles * (p.alternate ? 0.5 : 1.0);
   const double shared_us = 4.0 + waves * (6.0 + 2.0 * own_tiles) + (p.alternate ? 14.0 : 24.0) +
                            2.0 * std::ceil(steps / kSmCount);
-  a.direct = direct_us < shared_us && attn_direct_rows(id, p.P) < (1 << 30);
-  if (a.direct) {
-    a.off_o = a.off_lse = a.off_parts = 0;
-    a.bytes = attn_direct_bytes(d, id, p.P);
-    return a;
-  }
+  return direct_us < shared_us && attn_direct_rows(id, p.P) < (1 << 30);
+}
+AttnPrefixLayout attn_shared_layout(const sepllm_attn_desc* d, const sepllm_index_desc* id, const PrefixParams& p) {
+  AttnPrefixLayout a;
   const size_t rows = size_t(d->B) * d->Hq * d->L;
   a.off_o = attn_layout(d, id).fwd_bytes;
   a.off_lse = a.off_o + align_up(size_t(d->B) * d->Hq * ((d->L + 127) / 128 * 128) * kernel_head_dim(d->d) * sizeof(float));
   a.off_parts = a.off_lse + align_up(rows * sizeof(float));
   a.bytes = a.off_parts + prefix_part_bytes(p);
   return a;
+}
+// Bytes for every prefix of up to p.P rows.  The shared form's grow with the prefix; the direct form's do
+// too, but it is not taken for all of them: the longest one that may take it counts (within a key tile
+// the rule's direct time grows with the rows, so its first row says whether any takes it).
+size_t attn_prefix_bytes(const sepllm_attn_desc* d, const sepllm_index_desc* id, PrefixParams p) {
+  const size_t shared = attn_shared_layout(d, id, p).bytes;
+  const int P = p.P;
+  for (; p.key_tiles > 0; --p.key_tiles) {
+    p.P = (p.key_tiles - 1) * kBN + 1;
+    if (attn_prefix_direct(d, id, p))
+      return std::max(shared, attn_direct_bytes(d, id, std::min(P, p.key_tiles * kBN)));
+  }
+  return shared;
 }
 }  // namespace
 
@@ -962,7 +975,7 @@ extern "C" sepllm_status sepllm_attn_prefix_workspace_bytes(const sepllm_attn_de
   if (P < 1) return SEPLLM_INVALID_ARG;
   PrefixParams p{};
   if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P, false, 0.0)) return SEPLLM_UNSUPPORTED;
-  if (bytes) *bytes = attn_prefix_layout(desc, idesc, p).bytes;
+  if (bytes) *bytes = attn_prefix_bytes(desc, idesc, p);
   return SEPLLM_OK;
 }
 
@@ -984,9 +997,9 @@ extern "C" sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, co
   if (!plan_prefix(&p, desc->B, desc->Hq, desc->Hkv, desc->L, desc->d, P, false, 0.0)) return SEPLLM_UNSUPPORTED;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  const AttnPrefixLayout lay = attn_prefix_layout(desc, idesc, p);
-  if (lay.direct)
+  if (attn_prefix_direct(desc, idesc, p))
     return attn_fwd_direct(desc, idesc, Q, K, V, index, PrefixRows{Kp, Vp, prefix_len, P}, O, LSE, ws, stream);
+  const AttnPrefixLayout lay = attn_shared_layout(desc, idesc, p);
   float* own_O = reinterpret_cast<float*>(ws + lay.off_o);
   float* own_lse = reinterpret_cast<float*>(ws + lay.off_lse);
   // the rows' own tokens first (Eq. 2's mask); their result waits in 32 bits so that O is rounded once
