@@ -853,7 +853,7 @@ bool plan_prefix(PrefixParams* p, int B, int Hq, int Hkv, int T, int d, int P, b
   p->g_tiles = (p->G + p->gt - 1) / p->gt;
   p->t_tiles = (T + p->tt - 1) / p->tt;
   const int64_t m_tiles = int64_t((B + p->bt - 1) / p->bt) * p->t_tiles * p->g_tiles;
-  if (m_tiles > 0x3fffffff || Hkv > 65535 || P > (1 << 30) || int64_t(p->key_tiles) * Hkv > (1 << 30)) return false;
+  if (int64_t(B) * Hq * T > 0x7fffffff || m_tiles > 0x3fffffff || Hkv > 65535 || P > (1 << 30) || int64_t(p->key_tiles) * Hkv > (1 << 30)) return false;
   p->m_tiles = int(m_tiles);
   p->alternate = m_tiles == 1 ? 1 : 0;
   p->whole_parts = whole_parts || p->alternate;   // alternate mode: two parts of every row, joined later
@@ -898,8 +898,6 @@ sepllm_status launch_prefix(PrefixParams p, const void* Q, const void* Kp, const
   if ((st = make_query_map(&mq, Q, p)) != SEPLLM_OK) return st;
   if ((st = make_tile_map(&mk, Kp, p.d, p.P, p.Hkv, p.d, int64_t(p.P) * p.d, 128)) != SEPLLM_OK) return st;
   if ((st = make_tile_map(&mv, Vp, p.d, p.P, p.Hkv, p.d, int64_t(p.P) * p.d, 128)) != SEPLLM_OK) return st;
-  const int64_t rows = int64_t(p.B) * p.Hkv * p.G * p.T;
-  if (rows > 0x7fffffff) return SEPLLM_UNSUPPORTED;
   const bool d64 = kernel_head_dim(p.d) == 64;
   for (p.pair_base = 0; p.pair_base < all_pairs(p); p.pair_base += p.pairs) {
     p.pairs = std::min(launch_pairs(p), all_pairs(p) - p.pair_base);

@@ -1,4 +1,6 @@
 """A workspace sized for a prefix of P rows serves every shorter one (no GPU: the size queries)."""
+import ctypes as C
+
 import numpy as np
 import pytest
 
@@ -35,3 +37,18 @@ def test_attention(B, Hq, Hkv, d, L, w):
     P = [p for p in LENGTHS if p <= 1 << 20]
     n = [api.sepllm_attn_prefix_workspace_bytes(desc, idesc, p) for p in P]
     assert all(a <= b for a, b in zip(n, n[1:])), [(p, a, b) for p, a, b in zip(P, n, n[1:]) if a > b][:5]
+
+
+@pytest.mark.parametrize("B,Hq,L,fits", [(64, 64, 1 << 19, False), (64, 64, (1 << 19) - 1, True), (3000, 64, 1 << 15, False),
+                                         # 65 536 query tiles, one more than the attention calls take
+                                         (2, 32, 1 << 23, False), (2, 32, (1 << 23) - 128, True)])
+def test_batches_of_too_many_rows_are_refused_before_anything_is_launched(B, Hq, L, fits):
+    """2^31 query rows and more, or too many tiles: by the size query and by the call (whose addresses are not used)."""
+    desc, idesc = api.AttnDesc(B, Hq, 8, 64, L, 0.0, 0), api.IndexDesc(B, L, 0, 8, 1, 128, 128, L)
+    n = C.c_size_t(0)
+    got = api.lib().sepllm_attn_prefix_workspace_bytes(C.byref(desc), C.byref(idesc), C.c_int32(60000), C.byref(n))
+    assert got == (api.OK if fits else api.UNSUPPORTED)
+    if not fits:
+        a = 1 << 20
+        assert api.lib().sepllm_attn_prefix_fwd(C.byref(desc), C.byref(idesc), 60000, a, a, a, a, a, a, None, a, a, a,
+                                                None) == api.UNSUPPORTED
