@@ -480,7 +480,12 @@ sepllm_status sepllm_decode_rope(const sepllm_cache_desc* desc, float scale, con
  * initial, separator (oldest first), neighbour (oldest first), become rows 0 ..
  * Size_run-1 of Kp and Vp, and Size_run is written to the n_len words of
  * prefix_len (n_len = 0: to none).  Other rows are left as they are.  P >= c
- * (SEPLLM_BUFFER_TOO_SMALL otherwise).  Kc may be the rotated copy Kr. */
+ * (SEPLLM_BUFFER_TOO_SMALL otherwise).  Kc may be the rotated copy Kr: its keys
+ * stand at positions 0 .. Size_run-1, so the caller turns the tokens that follow,
+ * keys and queries, to Size_run and on (sepllm_rope_fwd) and keeps them in caches
+ * of sepllm_cache_update.  Positions taken inside the cache start at 0 there and
+ * have no form behind a prefix: caches of sepllm_cache_update_rope that follow a
+ * prefix, and sepllm_decode_rope behind one, are not offered. */
 sepllm_status sepllm_prefix_from_cache(const sepllm_cache_desc* desc, const void* state,
                                        const void* Kc, const void* Vc, int32_t P, void* Kp,
                                        void* Vp, int32_t* prefix_len, int32_t n_len,
