@@ -1090,7 +1090,10 @@ static double own_part_us(const sepllm_cache_desc* d) {
 // shared; 32 heads on 8 of 128, 150 own entries): 1 sequence x 1000 entries 8.4 / 14.3, 1 x 8000 12.5 /
 // 23.7, 4 x 2000 11.1 / 15.5, 4 x 8000 24.9 / 23.6, 4 x 32 000 79 / 39, 16 x 1000 16.8 / 15.2, 64 x 1000
 // 43 / 25, 64 x 4000 125 / 31; 12 heads of 64: 8 x 1000 8.4 / 13.3, 8 x 8000 29.8 / 24.4.  The rule took
-// the faster form in each of these.
+// the faster form in each of these, and in 74 of 84 points of a grid (1 to 128 sequences, 100 to 120 000 entries, heads of
+// 128 and 64); where it did not, the two were 1 to 15 % apart (15 %: 128 sequences x 100 entries, 32 heads
+// of 64).  For one or two sequences of 32 heads x 128 the times cross slowly, from 9000 entries (two) or
+// 40 000 (one) on, and the rule, which counts whole steps of a CTA, goes back and forth there: at most 11 %.
 struct PrefixDecodePlan {
   bool direct;
   int own_parts;

@@ -776,10 +776,13 @@ cudaError_t launch_join(const PrefixParams& p, int prefix_ctas, const float* own
   if (!p.whole_parts)
     return launch_overlapped(prefix_join<D, true, D / 16, 1>, dim3(8 * prefix_ctas), dim3(kJoinThreads), 0, stream, p,
                              own_ml, own_acc, own_parts);
+  // Few rows with many parts each: four warps share the parts of a row.  Both measured (us a decode call, four
+  // warps / one; heads of 128): 1 unit behind 20 000 entries 27 / 131, 8 behind 8000 24 / 51, 16 behind 4000
+  // 34 / 34, 24 behind 4000 29 / 36 (4 sequences) and 51 / 48 (160 sequences), 32 31 / 32, 40 83 / 72, 80
+  // 147 / 119; heads of 64: 8 22 / 37, 24 25 / 29 and 34 / 33, 40 55 / 50.
   if (units >= 24)
     return launch_overlapped(prefix_join<D, false, D / 16, 1>, dim3(8 * units), dim3(kJoinThreads), 0, stream, p,
                              own_ml, own_acc, own_parts);
-  // few rows, many parts each
   return launch_overlapped(prefix_join<D, false, 1, 4>, dim3(8 * units, D / 4), dim3(kJoinThreads), 0, stream, p,
                            own_ml, own_acc, own_parts);
 }
@@ -931,7 +934,10 @@ bool attn_prefix_direct(const sepllm_attn_desc* d, const sepllm_index_desc* id, 
   // 1 sequence x 16 tokens behind 100 entries 17 / 28, behind 1000 32 / 25; 16 x 64 behind 100 37 / 44,
   // behind 1000 80 / 73; 4 x 300 behind 500 54 / 60, behind 2000 107 / 100; 2 x 1024 behind 500 69 / 97,
   // behind 2000 114 / 140, behind 8000 326 / 292; 1 x 8192 behind 500 270 / 317; 12 heads of 64: 8 x 1024
-  // behind 1000 116 / 126.  The rule takes the faster form in each of these.
+  // behind 1000 116 / 126.  The rule takes the faster form in each of these.  On a grid of 60 points (16 to 8192 tokens, 100 to
+  // 8000 entries, the two models' heads) it took the slower one in 4: by 2 % (2 x 1024 behind 4000) and 6 % (8 x
+  // 1024 behind 2000) at 128, by 6 and 14 % (1 x 16 and 16 x 64 behind 500) at 64, whose steps are shorter
+  // than the 2 us taken here.
   const double own_tiles = std::min(d->L, id->n_neighbor) / 128 + 2;
   const double waves = std::ceil(double(d->B) * d->Hq * ((d->L + 127) / 128) / 2 / kSmCount);
   const double copy_us = double(d->B) * d->Hkv * p.P * d->d * 8 / 5e6;
