@@ -935,7 +935,7 @@ bool attn_prefix_direct(const sepllm_attn_desc* d, const sepllm_index_desc* id, 
   // behind 1000 80 / 73; 4 x 300 behind 500 54 / 60, behind 2000 107 / 100; 2 x 1024 behind 500 69 / 97,
   // behind 2000 114 / 140, behind 8000 326 / 292; 1 x 8192 behind 500 270 / 317; 12 heads of 64: 8 x 1024
   // behind 1000 116 / 126.  The rule takes the faster form in each of these.  On a grid of 60 points (16 to 8192 tokens, 100 to
-  // 8000 entries, the two models' heads) it took the slower one in 4: by 2 % (2 x 1024 behind 4000) and 6 % (8 x
+  // 8000 entries, 32 heads on 8 of 128 and 12 of 64) it took the slower one in 4: by 2 % (2 x 1024 behind 4000) and 6 % (8 x
   // 1024 behind 2000) at 128, by 6 and 14 % (1 x 16 and 16 x 64 behind 500) at 64, whose steps are shorter
   // than the 2 us taken here.
   const double own_tiles = std::min(d->L, id->n_neighbor) / 128 + 2;
