@@ -7,104 +7,9 @@
 //                 the Local Window Cache, the older ones the Past Window Cache
 // Decode walks "virtual" entries 0..Size_run-1 = initial, separator (oldest first), neighbour
 // (oldest first) and maps each to its slot, so only retained rows are read.
-#include <algorithm>
-
-#include "attn_common.cuh"
+#include "cache_common.cuh"
 
 namespace sepllm {
-
-struct CacheView {
-  sepllm_cache_header* hdr;
-  sepllm_cache_seq* seq;
-  int64_t* slot_pos;
-  uint8_t* slot_is_sep;
-};
-
-__host__ __device__ inline CacheView cache_view(void* state, const sepllm_cache_header& h) {
-  uint8_t* p = static_cast<uint8_t*>(state);
-  CacheView v;
-  v.hdr = reinterpret_cast<sepllm_cache_header*>(p);
-  v.seq = reinterpret_cast<sepllm_cache_seq*>(p + h.off_seq);
-  v.slot_pos = reinterpret_cast<int64_t*>(p + h.off_slot_pos);
-  v.slot_is_sep = p + h.off_slot_is_sep;
-  return v;
-}
-
-static sepllm_status fill_cache_header(const sepllm_cache_desc* d, sepllm_cache_header* h) {
-  if (!d) return SEPLLM_INVALID_ARG;
-  if (d->B <= 0 || d->Hkv <= 0 || d->Hq <= 0 || d->a < 0 || d->s < 0 || d->w < 1 || d->c < 1)
-    return SEPLLM_INVALID_ARG;
-  if (!(static_cast<int64_t>(d->a) + d->s + d->w < d->c)) return SEPLLM_INVALID_ARG;
-  if (d->Hq % d->Hkv != 0) return SEPLLM_INVALID_ARG;
-  if (d->d != 64 && d->d != 128) return SEPLLM_UNSUPPORTED;
-  if (d->Hq / d->Hkv > 16) return SEPLLM_UNSUPPORTED;
-  if (d->flags & ~SEPLLM_CACHE_FIXED_WINDOW) return SEPLLM_INVALID_ARG;
-  *h = sepllm_cache_header{};
-  h->magic = SEPLLM_CACHE_MAGIC;
-  h->version = 1;
-  h->slots = d->c + d->s;
-  h->desc = *d;
-  size_t off = sizeof(sepllm_cache_header);
-  h->off_seq = off;
-  off = align_up(off + sizeof(sepllm_cache_seq) * size_t(d->B));
-  h->off_slot_pos = off;
-  off = align_up(off + sizeof(int64_t) * size_t(d->B) * h->slots);
-  h->off_slot_is_sep = off;
-  off = align_up(off + size_t(d->B) * h->slots);
-  h->total_bytes = off;
-  return SEPLLM_OK;
-}
-
-// What one update does to a sequence, derived from the state before the update.
-struct UpdatePlan {
-  int append_slot;   // slot that receives the new token's K/V
-  bool compact;      // Size_run reaches c with this token
-  int n_past;        // Past Window entries examined by the compaction
-  int drop;          // oldest Separator Cache entries (old and moved together) that fall out
-};
-
-__device__ __forceinline__ UpdatePlan plan_update(const sepllm_cache_seq& q,
-                                                  const sepllm_cache_desc& d) {
-  UpdatePlan p;
-  p.compact = false;
-  p.n_past = 0;
-  p.drop = 0;
-  if (q.size_init < d.a) {
-    p.append_slot = q.size_init;
-    return p;
-  }
-  const int ring = d.c - d.a;
-  p.append_slot = d.a + d.s + (q.win_start + q.size_win) % ring;
-  const int size_win = q.size_win + 1;
-  if (d.flags & SEPLLM_CACHE_FIXED_WINDOW) {
-    // fundamental design: the run is the w most recent tokens; what is older leaves at once
-    if (size_win > d.w) {
-      p.compact = true;
-      p.n_past = size_win - d.w;
-    }
-  } else if (q.size_init + q.size_sep + size_win == d.c) {
-    p.compact = true;
-    p.n_past = size_win - d.w;
-  }
-  return p;
-}
-
-// Ring starts are below the ring size and v is below the region's entry count, so one conditional
-// subtraction wraps the index (no integer division on the decode path).
-__device__ __forceinline__ int virtual_to_slot(int v, const sepllm_cache_seq& q,
-                                               const sepllm_cache_desc& d) {
-  if (v < q.size_init) return v;
-  v -= q.size_init;
-  if (v < q.size_sep) {
-    const int x = q.sep_start + v;
-    return d.a + (x >= d.s ? x - d.s : x);
-  }
-  v -= q.size_sep;
-  const int ring = d.c - d.a, x = q.win_start + v;
-  return d.a + d.s + (x >= ring ? x - ring : x);
-}
-
-constexpr int kUpdThreads = 256;
 
 // Writes the header (passed by value, so nothing on the host has to outlive the launch) and zeroes
 // the rest of the state buffer.  grid-stride over 16-byte words; the buffer is 256-byte aligned.
@@ -116,47 +21,6 @@ cache_init_kernel(sepllm_cache_header h, uint4* __restrict__ state, size_t words
        k += size_t(gridDim.x) * blockDim.x)
     state[k] = (k < kHdrWords) ? src[k] : make_uint4(0, 0, 0, 0);
 }
-
-// Exclusive rank of every separator among the Past Window entries, in position order.
-// rank_s[k] (k < n_past) = number of separators among past entries [0, k); returns the total.
-// n_past <= kMaxPast.
-__device__ int rank_past_separators(const uint8_t* slot_is_sep_b, const sepllm_cache_seq& q,
-                                    const sepllm_cache_desc& d, int n_past, int16_t* flag_s,
-                                    int* warp_buf) {
-  const int ring = d.c - d.a;
-  const int base = d.a + d.s;
-  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int per = (n_past + kUpdThreads - 1) / kUpdThreads;
-  const int k0 = tid * per, k1 = min(n_past, k0 + per);
-  int local = 0;
-  for (int k = k0; k < k1; ++k) {
-    const int f = slot_is_sep_b[base + (q.win_start + k) % ring];
-    flag_s[k] = int16_t(f);
-    local += f;
-  }
-  int incl = local;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int t = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += t;
-  }
-  if (lane == 31) warp_buf[wid] = incl;
-  __syncthreads();
-  int woff = 0, total = 0;
-  for (int k = 0; k < kUpdThreads / 32; ++k) {
-    if (k < wid) woff += warp_buf[k];
-    total += warp_buf[k];
-  }
-  int run = woff + incl - local;
-  // flag_s[k] becomes rank+1 for separators, 0 otherwise
-  for (int k = k0; k < k1; ++k) {
-    if (flag_s[k]) { flag_s[k] = int16_t(run + 1); ++run; }
-  }
-  __syncthreads();
-  return total;
-}
-
-constexpr int kMaxPast = 24576;  // int16 ranks in shared memory: 48 KB
 
 // grid (B, Hkv).  Every CTA moves the K/V rows of its kv head (append; at a compaction the ordered
 // move of Past-Window separators into the separator ring), reading the sequence's state only.
@@ -178,7 +42,6 @@ cache_update(sepllm_cache_header h, uint8_t* __restrict__ state, __nv_bfloat16* 
              SepIds sep, __nv_bfloat16* __restrict__ Kr, const float2* __restrict__ rope) {
   extern __shared__ int16_t flag_s[];
   __shared__ int warp_buf[32];
-  __shared__ int s_last;
   const sepllm_cache_desc d = h.desc;
   const int b = blockIdx.x, hk = blockIdx.y, tid = threadIdx.x;
   CacheView v = cache_view(state, h);
@@ -193,42 +56,21 @@ cache_update(sepllm_cache_header h, uint8_t* __restrict__ state, __nv_bfloat16* 
   if (tid < vec) Kp[size_t(p.append_slot) * vec + tid] = kn[tid];
   else if (tid < 2 * vec) Vp[size_t(p.append_slot) * vec + (tid - vec)] = vn[tid - vec];
 
-  const bool moves = p.compact && d.s > 0;  // the same for every thread of the block
-  const int ring = d.c - d.a, wbase = d.a + d.s;
-  int m = 0, drop = 0;
-  if (moves) {
-    m = rank_past_separators(v.slot_is_sep + size_t(b) * h.slots, q, d, p.n_past, flag_s, warp_buf);
-    drop = max(0, q.size_sep + m - d.s);
+  UpdateMoves mv{p.compact && d.s > 0, 0, 0};  // (`any` is the same for every thread of the block)
+  if (mv.any) {
+    mv.m = rank_past_separators(v.slot_is_sep + size_t(b) * h.slots, q, d, p.n_past, flag_s, warp_buf);
+    mv.drop = max(0, q.size_sep + mv.m - d.s);
     // `vec` lanes move a K row, the next `vec` lanes the V row
     const int rows_per_pass = kUpdThreads / (2 * vec);
     const int sub = tid / (2 * vec), l = tid % (2 * vec);
     for (int k = sub; k < p.n_past; k += rows_per_pass) {
-      const int r = flag_s[k];
-      if (r == 0) continue;
-      const int fifo = q.size_sep + (r - 1);  // place in the queue of old + moved separators
-      if (fifo < drop) continue;              // falls out at once
-      const int src = wbase + (q.win_start + k) % ring;
-      const int dst = d.a + (q.sep_start + fifo) % d.s;
+      int src, dst;
+      if (!past_move(k, flag_s, q, d, mv.drop, &src, &dst)) continue;
       if (l < vec) Kp[size_t(dst) * vec + l] = Kp[size_t(src) * vec + l];
       else Vp[size_t(dst) * vec + (l - vec)] = Vp[size_t(src) * vec + (l - vec)];
     }
   }
-
-  // the sequence's record after this update (every CTA derives the same one)
-  sepllm_cache_seq nq = q;
-  nq.reserved[0] = 0;  // arrival count for the next update
-  nq.next_pos = q.next_pos + 1;
-  if (q.size_init < d.a) nq.size_init = q.size_init + 1;
-  else nq.size_win = q.size_win + 1;
-  if (p.compact) {
-    if (moves) {
-      nq.sep_start = (q.sep_start + drop) % d.s;
-      nq.size_sep = q.size_sep + m - drop;
-    }
-    nq.win_start = (q.win_start + p.n_past) % ring;
-    nq.size_win = d.w;
-    nq.compactions = q.compactions + 1;
-  }
+  const sepllm_cache_seq nq = next_record(q, d, p, mv);
 
   __syncthreads();  // this CTA's append and moves are visible to all its threads
   if (ROPE) {
@@ -256,37 +98,7 @@ cache_update(sepllm_cache_header h, uint8_t* __restrict__ state, __nv_bfloat16* 
     }
   }
 
-  // last kv head of the sequence to get here updates the state
-  if (tid == 0) {
-    __threadfence();
-    const int prev = atomicAdd(&v.seq[b].reserved[0], 1);
-    s_last = (prev == d.Hkv - 1);
-  }
-  __syncthreads();
-  if (!s_last) return;
-  __threadfence();
-
-  int64_t* pos_b = v.slot_pos + size_t(b) * h.slots;
-  uint8_t* sep_b = v.slot_is_sep + size_t(b) * h.slots;
-  if (tid == 0) {
-    pos_b[p.append_slot] = q.next_pos;
-    sep_b[p.append_slot] = uint8_t(is_separator(new_token_ids[b], sep));
-    // a Separator Cache that is not meant to evict did
-    if ((d.flags & SEPLLM_CACHE_FIXED_WINDOW) && drop > 0) set_status(&v.hdr->status, SEPLLM_CAPACITY_EXCEEDED);
-  }
-  if (moves) {
-    for (int k = tid; k < p.n_past; k += kUpdThreads) {
-      const int r = flag_s[k];
-      if (r == 0) continue;
-      const int fifo = q.size_sep + (r - 1);
-      if (fifo < drop) continue;
-      const int src = wbase + (q.win_start + k) % ring;
-      const int dst = d.a + (q.sep_start + fifo) % d.s;
-      pos_b[dst] = pos_b[src];
-      sep_b[dst] = 1;
-    }
-  }
-  if (tid == 0) v.seq[b] = nq;
+  finish_update(v, h, b, q, nq, p, mv, flag_s, new_token_ids, sep);
 }
 
 // ---------------------------------------------------------------------------
@@ -417,6 +229,16 @@ prompt_plan(sepllm_cache_header h, uint8_t* __restrict__ state, const uint8_t* _
     pos_b[slot] = pos;
     sep_b[slot] = uint8_t(flag);
   }
+}
+
+sepllm_status launch_prompt_plan(const sepllm_cache_header& h, const sepllm_index_header& ih, void* state,
+                                 const void* index, const int32_t* prompt_len, cudaStream_t stream) {
+  // the status word starts clean; everything else is written by the plan kernel
+  SEPLLM_CUDA_TRY(cudaMemsetAsync(state, 0, sizeof(int32_t), stream));
+  prompt_plan<<<h.desc.B, kPlanThreads, 0, stream>>>(h, static_cast<uint8_t*>(state),
+                                                     static_cast<const uint8_t*>(index), ih, prompt_len);
+  SEPLLM_CUDA_TRY(cudaGetLastError());
+  return SEPLLM_OK;
 }
 
 constexpr int kCopyThreads = 256;
@@ -848,17 +670,13 @@ static sepllm_status update_impl(const sepllm_cache_desc* desc, void* state, voi
   if (!state || !Kc || !Vc || !new_token_ids || !k_new || !v_new) return SEPLLM_INVALID_ARG;
   if (with_rope && (!Kr || !rope_table || !aligned(Kr, 16) || !aligned(rope_table, 16)))
     return SEPLLM_INVALID_ARG;
-  if (n_sep < 0 || (n_sep > 0 && !sep_ids)) return SEPLLM_INVALID_ARG;
-  if (n_sep > SEPLLM_MAX_SEP_IDS) return SEPLLM_UNSUPPORTED;
   if (!aligned(state, kAlign) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(k_new, 16) ||
       !aligned(v_new, 16))
     return SEPLLM_INVALID_ARG;
-  const int max_past = (desc->flags & SEPLLM_CACHE_FIXED_WINDOW) ? 1 : desc->c - desc->a - desc->w;
-  if (max_past > kMaxPast || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
-  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   SepIds sep;
-  sep.n = n_sep;
-  for (int k = 0; k < SEPLLM_MAX_SEP_IDS; ++k) sep.id[k] = (k < n_sep) ? sep_ids[k] : -1;
+  int max_past;
+  if ((st = update_params(desc, sep_ids, n_sep, &sep, &max_past)) != SEPLLM_OK) return st;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   const size_t smem = size_t(max_past) * sizeof(int16_t);
   auto kernel = with_rope ? cache_update<true> : cache_update<false>;
   if (smem > 40 * 1024)
@@ -914,12 +732,7 @@ extern "C" sepllm_status sepllm_cache_from_prompt(const sepllm_cache_desc* desc,
   if (Kr && (!aligned(Kr, 16) || !aligned(rope_table, 16))) return SEPLLM_INVALID_ARG;
   if (desc->B > 65535 || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  // the status word starts clean; everything else is written by the plan kernel
-  SEPLLM_CUDA_TRY(cudaMemsetAsync(state, 0, sizeof(int32_t), stream));
-  prompt_plan<<<desc->B, kPlanThreads, 0, stream>>>(h, static_cast<uint8_t*>(state),
-                                                    static_cast<const uint8_t*>(index), ih,
-                                                    prompt_len);
-  SEPLLM_CUDA_TRY(cudaGetLastError());
+  if ((st = launch_prompt_plan(h, ih, state, index, prompt_len, stream)) != SEPLLM_OK) return st;
   const dim3 grid((h.slots + kCopyRows - 1) / kCopyRows, desc->Hkv, desc->B);
 #define SEPLLM_COPY(D, R)                                                                       \
   prompt_copy<D, R><<<grid, kCopyThreads, 0, stream>>>(                                         \
