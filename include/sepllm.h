@@ -339,6 +339,44 @@ sepllm_status sepllm_rope_bwd(const sepllm_rope_desc* desc, const int64_t* posit
                               const sepllm_rope_view* in, const sepllm_rope_view* out,
                               void* stream);
 
+/* ---- norms of query and key heads, with the rotary positions -----------------
+ * Models that normalise every query and key head before its position is encoded:
+ * these calls are sepllm_rope_fwd and its gradient with the norm in the same pass.
+ * (The paper's backbones have none.)  A head vector x of d elements becomes
+ *   y_e = x_e r (offset + w_e),   r = 1 / sqrt((sum of x_e^2) / d + eps)
+ * and y is then rotated as sepllm_rope_fwd does; V is copied.  Sums are 32 bits
+ * (|x| up to 1e18), r too; outputs are rounded once.
+ *   wq, wk  dev [d] of w_dtype (0 = bf16, 1 = fp32), shared by the query and by the
+ *           key heads; NULL: y = x r.  offset is 0, or 1 for weights stored around
+ *           zero; eps > 0. */
+typedef struct {
+  const void *wq, *wk;
+  int32_t w_dtype;
+  float eps, offset;
+} sepllm_qknorm_desc;
+
+/* Arguments as sepllm_rope_fwd; an output may be its own input there as well. */
+sepllm_status sepllm_qknorm_rope_fwd(const sepllm_rope_desc* desc, const sepllm_qknorm_desc* norm,
+                                     const int64_t* positions, const sepllm_rope_view* in,
+                                     const sepllm_rope_view* out, void* stream);
+
+/* Gradient of sepllm_qknorm_rope_fwd.  With g the gradient of the outputs rotated
+ * back, n = x r and u = g (offset + w):  dx = r (u - n mean(n u)) over the head,
+ * dw = the sum of g n over sequences, tokens and heads.
+ *   x     host array of two views, the forward's inputs Q and K (not its outputs)
+ *   in    host array of three views, dL/d(outputs); out, dL/d(inputs), of x's type
+ *   dwq, dwk  dev fp32 [d], written (not added to); NULL: not wanted, and where
+ *         there are no weights
+ *   workspace  dev, sepllm_qknorm_rope_bwd_workspace_bytes, 256-byte aligned
+ * A tensor of Q or K is there in x, in and out, or in none of them (its dw is then
+ * 0).  out may be in or x (same data, strides and dtype).  Deterministic: no
+ * floating-point atomics. */
+sepllm_status sepllm_qknorm_rope_bwd_workspace_bytes(const sepllm_rope_desc* desc, size_t* bytes);
+sepllm_status sepllm_qknorm_rope_bwd(const sepllm_rope_desc* desc, const sepllm_qknorm_desc* norm,
+                                     const int64_t* positions, const sepllm_rope_view* x,
+                                     const sepllm_rope_view* in, const sepllm_rope_view* out,
+                                     float* dwq, float* dwk, void* workspace, void* stream);
+
 /* ---- streaming cache (Section 3.3, Tailored Streaming Design) --------------
  * Kc and Vc are bf16 [B][Hkv][slots][d] with slots = c + s: slots [0,a) are the
  * Initial Cache, [a, a+s) a ring holding the Separator Cache, [a+s, c+s) a ring
@@ -525,6 +563,64 @@ sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, const sepllm_
                                      const void* index, const void* Kp, const void* Vp,
                                      const int32_t* prefix_len, void* O, float* LSE,
                                      void* workspace, void* stream);
+
+/* ---- the cache held in 4 bits ------------------------------------------------
+ * The streaming cache of sepllm_cache_update with K and V rows in 4 bits and a
+ * half an element, for caches that are to take 3.6 times less memory and decode
+ * time.  (The paper keeps them in 16 bits; what is kept, and when, is the same.)
+ * State, slots, rings and flags are those of the 16-bit cache; sepllm_cache_init
+ * empties it.  Format: 32 neighbouring elements of a row share a step s = -m / 8
+ * (bf16, exact), m their element of largest magnitude, the positive one of two
+ * equal ones; an element x is held as the whole number q nearest to x / s (the
+ * even one of two), -8 <= q <= 7, and stands for q s.  m is held exactly, others
+ * to half a step, except elements of the other sign beyond 7.5 steps (a whole
+ * one).  Groups whose largest magnitude is below 2^-100 are held as zeros, groups
+ * with a NaN or an infinity as NaN.  Rows that move keep their codes: a row is
+ * quantised once, however many compactions it goes through.
+ *   Kc, Vc  dev, 256-byte aligned, kv_bytes of sepllm_cache_bytes_quant each: codes
+ *           [B][Hkv][slots][d / 2] bytes, then, from the next multiple of 256
+ *           bytes on, steps bf16 [B][Hkv][slots][d / 32].  A row's codes q + 8
+ *           stand two to a byte, low half first; element e of group j is the row's
+ *           ((e / m) * (d / 32) + j) * m + e % m -th, m = 8 in Kc and 4 in Vc.
+ * Positions taken inside the cache (sepllm_cache_update_rope) have no 4-bit form:
+ * keys are handed over with their positions encoded. */
+
+/* state_bytes: the state buffer; kv_bytes: ONE of Kc / Vc. */
+sepllm_status sepllm_cache_bytes_quant(const sepllm_cache_desc* desc, size_t* state_bytes,
+                                       size_t* kv_bytes);
+
+/* sepllm_cache_update for a cache held in 4 bits.  Arguments as there. */
+sepllm_status sepllm_cache_update_quant(const sepllm_cache_desc* desc, void* state, void* Kc,
+                                        void* Vc, const int32_t* new_token_ids,
+                                        const int32_t* sep_ids, int32_t n_sep, const void* k_new,
+                                        const void* v_new, void* stream);
+
+/* sepllm_cache_from_prompt for a cache held in 4 bits.  Arguments as there. */
+sepllm_status sepllm_cache_from_prompt_quant(const sepllm_cache_desc* desc,
+                                             const sepllm_index_desc* idesc, const void* index,
+                                             const int32_t* prompt_len, const void* K,
+                                             const void* V, void* state, void* Kc, void* Vc,
+                                             void* stream);
+
+/* The retained entries of every sequence, in the order initial, separator (oldest
+ * first), neighbour (oldest first), become rows 0 .. Size_run-1 of K and V (dev
+ * bf16 [B][Hkv][n][d], 16-byte aligned; the held values rounded once), and
+ * Size_run goes to length[b] (dev int32 [B], or NULL).  Other rows are left as
+ * they are.  n >= c (SEPLLM_BUFFER_TOO_SMALL otherwise).  With B = 1 the result is
+ * a shared prefix of P = n rows. */
+sepllm_status sepllm_cache_entries_quant(const sepllm_cache_desc* desc, const void* state,
+                                         const void* Kc, const void* Vc, int32_t n, void* K,
+                                         void* V, int32_t* length, void* stream);
+
+/* sepllm_decode over a cache held in 4 bits: o = softmax(q K^T * scale) V of the
+ * held values.  A sequence with no entry gets o = 0 and lse = -inf.  A query
+ * element that is not finite, or beyond 2^117, makes its row NaN.  workspace of
+ * sepllm_decode_quant_workspace_bytes, 256-byte aligned (its first word is the
+ * device status; always 0); other arguments as sepllm_decode and above. */
+sepllm_status sepllm_decode_quant_workspace_bytes(const sepllm_cache_desc* desc, size_t* bytes);
+sepllm_status sepllm_decode_quant(const sepllm_cache_desc* desc, float scale, const void* q,
+                                  const void* state, const void* Kc, const void* Vc, void* o,
+                                  float* lse, void* workspace, void* stream);
 
 /* Copies the device status word at the start of an index, workspace or state
  * buffer to *out (host) after synchronising `stream`. */

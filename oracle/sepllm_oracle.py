@@ -817,3 +817,68 @@ def decode_attention_rope(q, Kc, Vc, base: float, q_pos=None, k_pos=None, scale:
     k_pos = np.arange(R) if k_pos is None else np.asarray(k_pos)
     q_pos = R - 1 if q_pos is None else q_pos
     return decode_attention(rope_rotate(q, np.asarray(q_pos), base), rope_rotate(Kc, k_pos, base), Vc, scale)
+
+
+# ----------------------------------------------------------------------------
+# Norms of query and key heads
+# ----------------------------------------------------------------------------
+
+def head_norm(x: np.ndarray, w: np.ndarray | None, eps: float, offset: float = 0.0) -> np.ndarray:
+    """x [..., d] by the root of its mean square (+ eps), times offset + w (no weights: times 1)."""
+    x = np.asarray(x, dtype=np.float64)
+    y = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    return y if w is None else y * (offset + np.asarray(w, dtype=np.float64))
+
+
+def head_norm_bwd(x: np.ndarray, w: np.ndarray | None, g: np.ndarray, eps: float, offset: float = 0.0):
+    """Gradients of head_norm for x and (summed over all but the last dimension) for w, given g."""
+    x, g = np.asarray(x, dtype=np.float64), np.asarray(g, dtype=np.float64)
+    r = 1.0 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    n = x * r
+    u = g if w is None else g * (offset + np.asarray(w, dtype=np.float64))
+    return r * (u - n * (n * u).mean(-1, keepdims=True)), (g * n).reshape(-1, x.shape[-1]).sum(0)
+
+
+# ----------------------------------------------------------------------------
+# Cache rows in 4 bits
+# ----------------------------------------------------------------------------
+
+QUANT_GROUP = 32
+
+
+def quantise_rows(x: np.ndarray):
+    """Codes (whole numbers -8 .. 7) and steps [..., d / 32] of rows of 16-bit numbers: a group's step is
+    -m / 8 with m its element of largest magnitude (the positive one of two), a code the whole number
+    nearest to x / step (the even one of two), at most 7; groups below 2^-100 are zeros, groups with a
+    number that is not finite have the step NaN and codes 0."""
+    y = np.asarray(x, dtype=np.float64)
+    y = y.reshape(*y.shape[:-1], y.shape[-1] // QUANT_GROUP, QUANT_GROUP)
+    bad = ~np.isfinite(y).all(-1)
+    z = np.where(bad[..., None], 0.0, y)
+    most, least = z.max(-1), z.min(-1)
+    m = np.where(most >= -least, most, least)
+    step = np.where(np.abs(m) < 2.0 ** -100, 0.0, -m / 8.0)
+    code = np.minimum(np.rint(z / np.where(step == 0, 1.0, step)[..., None]), 7.0)   # (rint: even at a tie)
+    code = np.where((step == 0)[..., None], 0.0, code)
+    return code.reshape(x.shape).astype(np.int64), np.where(bad, np.nan, step)
+
+
+def quant_values(code: np.ndarray, step: np.ndarray) -> np.ndarray:
+    """What codes and steps stand for."""
+    c = np.asarray(code, dtype=np.float64)
+    return (c.reshape(*c.shape[:-1], c.shape[-1] // QUANT_GROUP, QUANT_GROUP) * np.asarray(step)[..., None]).reshape(c.shape)
+
+
+def quant_places(d: int, m: int) -> np.ndarray:
+    """Place of every element's code in a held row (m: 8 for keys, 4 for values)."""
+    j, e = np.divmod(np.arange(d), QUANT_GROUP)
+    return ((e // m) * (d // QUANT_GROUP) + j) * m + e % m
+
+
+def quant_unpack(buf: np.ndarray, rows: int, d: int, m: int):
+    """Codes [rows][d] and steps (bits, uint16 [rows][d / 32]) of a cache buffer's bytes."""
+    held = buf[: rows * d // 2].reshape(rows, d // 2)
+    n = np.stack((held & 15, held >> 4), -1).reshape(rows, d).astype(np.int64) - 8
+    at = (rows * d // 2 + 255) // 256 * 256
+    steps = buf[at: at + rows * d // 16].view(np.uint16).reshape(rows, d // QUANT_GROUP)
+    return n[:, quant_places(d, m)], steps

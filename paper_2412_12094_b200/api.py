@@ -52,6 +52,7 @@ class CacheDesc(C.Structure):
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "llama3": 4, "factors": 5}
+_ROPE_DTYPES = {torch.bfloat16: 0, torch.float32: 1}
 
 
 class RopeDesc(C.Structure):
@@ -77,6 +78,19 @@ class RopeDesc(C.Structure):
                          ROPE_SCALINGS.get(scaling, scaling), base, factor, low, high, orig_len, attn_factor,
                          C.cast(self._keep, C.POINTER(C.c_double)) if self._keep else None, pos_first,
                          L if pos_stride is None else pos_stride)
+
+
+class QkNorm(C.Structure):
+    """sepllm_qknorm_desc.  wq, wk: bf16 or fp32 [d] tensors of one type, or None."""
+    _fields_ = [("wq", C.c_void_p), ("wk", C.c_void_p), ("w_dtype", C.c_int32), ("eps", C.c_float),
+                ("offset", C.c_float)]
+
+    def __init__(self, wq=None, wk=None, eps=1e-6, offset=0.0):
+        types = {w.dtype for w in (wq, wk) if w is not None}
+        if len(types) > 1 or not types <= set(_ROPE_DTYPES):
+            raise ValueError(f"the weights are bf16 or fp32, both of one type, not {sorted(map(str, types))}")
+        self.weights = (wq, wk)     # (kept alive, and looked at by every call)
+        super().__init__(None, None, _ROPE_DTYPES[types.pop()] if types else 0, eps, offset)
 
 
 class IndexHeader(C.Structure):
@@ -107,6 +121,9 @@ EXPORTS = [
     "sepllm_rope_frequencies", "sepllm_rope_fwd", "sepllm_rope_bwd",
     "sepllm_prefix_from_cache", "sepllm_decode_prefix_workspace_bytes", "sepllm_decode_prefix",
     "sepllm_attn_prefix_workspace_bytes", "sepllm_attn_prefix_fwd",
+    "sepllm_qknorm_rope_fwd", "sepllm_qknorm_rope_bwd_workspace_bytes", "sepllm_qknorm_rope_bwd",
+    "sepllm_cache_bytes_quant", "sepllm_cache_update_quant", "sepllm_cache_from_prompt_quant",
+    "sepllm_cache_entries_quant", "sepllm_decode_quant_workspace_bytes", "sepllm_decode_quant",
     "sepllm_status_string",
 ]
 
@@ -118,6 +135,11 @@ _ARGTYPES = {
     "sepllm_prefix_from_cache": [_P] * 4 + [_I] + [_P] * 3 + [_I, _P],
     "sepllm_decode_prefix": [_P, _I, C.c_float] + [_P] * 11,
     "sepllm_attn_prefix_fwd": [_P, _P, _I] + [_P] * 11,
+    "sepllm_qknorm_rope_fwd": [_P] * 6, "sepllm_qknorm_rope_bwd": [_P] * 10,
+    "sepllm_cache_update_quant": [_P] * 6 + [_I] + [_P] * 3,
+    "sepllm_cache_from_prompt_quant": [_P] * 10,
+    "sepllm_cache_entries_quant": [_P] * 4 + [_I] + [_P] * 4,
+    "sepllm_decode_quant": [_P, C.c_float] + [_P] * 8,
 }
 
 _lib = None
@@ -299,7 +321,6 @@ def sepllm_rope_frequencies(desc: RopeDesc):
     return f[:(desc.rot_dim or desc.d) // 2].copy(), m.value
 
 
-_ROPE_DTYPES = {torch.bfloat16: 0, torch.float32: 1}
 _ROPE_VIEWS = struct.Struct("=" + "Qqqqii" * 3)   # three sepllm_rope_view
 
 
@@ -327,13 +348,18 @@ def _rope_views(desc, tensors, what, device=None):
     return [_ROPE_VIEWS.pack(*vals[i:i + 18]) for i in range(0, len(vals), 18)]
 
 
+def _positions(where, desc, positions):
+    if positions is None:
+        return 0
+    pos, = _addresses(where, (positions,))
+    if positions.dtype != torch.int64 or positions.numel() < (desc.B - 1) * desc.pos_stride + desc.L:
+        raise ValueError(f"{where}: positions are contiguous int64, pos_stride elements from row to row")
+    return pos
+
+
 def _rope(fn, where, desc, positions, tensors):
     device = torch.cuda.current_device()
-    pos = 0
-    if positions is not None:
-        pos, = _addresses(where, (positions,))
-        if positions.dtype != torch.int64 or positions.numel() < (desc.B - 1) * desc.pos_stride + desc.L:
-            raise ValueError(f"{where}: positions are contiguous int64, pos_stride elements from row to row")
+    pos = _positions(where, desc, positions)
     ins, outs = _rope_views(desc, tensors, where, device)
     _check(fn(C.byref(desc), pos, ins, outs, torch._C._cuda_getCurrentRawStream(device)), where)
 
@@ -349,6 +375,45 @@ def sepllm_rope_bwd(desc: RopeDesc, positions, dq_out, dk_out, dv_out, dq, dk, d
     """Gradients of sepllm_rope_fwd's inputs from those of its outputs."""
     _rope(lib().sepllm_rope_bwd, "sepllm_rope_bwd", desc, positions,
           (dq_out, dk_out, dv_out, dq, dk, dv))
+
+
+# ---------------------------------------------------------------- head norms with rotary positions
+def _qknorm(where, desc, norm, positions, device):
+    """Puts the weights' addresses into the descriptor; the address of `positions`."""
+    for i, w in enumerate(norm.weights):
+        if w is not None and w.shape != (desc.d,):
+            raise ValueError(f"{where}: weights are [{desc.d}], not {tuple(w.shape)}")
+    norm.wq, norm.wk = (a or None for a in _addresses(where, norm.weights))
+    return _positions(where, desc, positions)
+
+
+def sepllm_qknorm_rope_fwd(desc: RopeDesc, norm: QkNorm, positions, q, k, v, q_out, k_out, v_out):
+    """sepllm_rope_fwd with every head of q and k normalised first.  Other arguments as there."""
+    where, device = "sepllm_qknorm_rope_fwd", torch.cuda.current_device()
+    pos = _qknorm(where, desc, norm, positions, device)
+    ins, outs = _rope_views(desc, (q, k, v, q_out, k_out, v_out), where, device)
+    _check(lib().sepllm_qknorm_rope_fwd(C.byref(desc), C.byref(norm), pos, ins, outs,
+                                        torch._C._cuda_getCurrentRawStream(device)), where)
+
+
+def sepllm_qknorm_rope_bwd_workspace_bytes(desc: RopeDesc):
+    b = C.c_size_t(0)
+    _check(lib().sepllm_qknorm_rope_bwd_workspace_bytes(C.byref(desc), C.byref(b)),
+           "sepllm_qknorm_rope_bwd_workspace_bytes")
+    return b.value
+
+
+def sepllm_qknorm_rope_bwd(desc: RopeDesc, norm: QkNorm, positions, q, k, dq_out, dk_out, dv_out, dq, dk, dv, dwq,
+                           dwk, workspace):
+    """Gradients of sepllm_qknorm_rope_fwd's inputs and weights; q, k: the forward's inputs; dwq, dwk: fp32 [d]
+    or None."""
+    where, device = "sepllm_qknorm_rope_bwd", torch.cuda.current_device()
+    pos = _qknorm(where, desc, norm, positions, device)
+    xs, ins, outs = _rope_views(desc, (q, k, None, dq_out, dk_out, dv_out, dq, dk, dv), where, device)
+    _expect(where, ("dwq", dwq, (desc.d,), torch.float32), ("dwk", dwk, (desc.d,), torch.float32))
+    _check(lib().sepllm_qknorm_rope_bwd(C.byref(desc), C.byref(norm), pos, xs, ins, outs,
+                                        *_addresses(where, (dwq, dwk, workspace)),
+                                        torch._C._cuda_getCurrentRawStream(device)), where)
 
 
 # ---------------------------------------------------------------- cache
@@ -466,6 +531,68 @@ def sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, prefix_len, O
             ("LSE", LSE, row[:3], torch.float32))
     _check(lib().sepllm_attn_prefix_fwd(C.byref(desc), C.byref(idesc), P, *_addresses(
         where, (Q, K, V, index, Kp, Vp, prefix_len, O, LSE, workspace)), _raw_stream()), where)
+
+
+# ---------------------------------------------------------------- cache in 4 bits
+def _quant_kv(where, desc, Kc, Vc):
+    """Refuses buffers shorter than a cache of the descriptor (they would be read past their end)."""
+    rows = desc.B * desc.Hkv * (desc.c + desc.s)
+    need = (rows * desc.d // 2 + 255 & -256) + (rows * desc.d // 16 + 255 & -256)
+    for name, t in (("Kc", Kc), ("Vc", Vc)):
+        if t.numel() * t.element_size() < need:
+            raise ValueError(f"{where}: {name} has {t.numel() * t.element_size()} bytes, the descriptor's cache {need}")
+
+
+def sepllm_cache_bytes_quant(desc: CacheDesc):
+    s, k = C.c_size_t(0), C.c_size_t(0)
+    _check(lib().sepllm_cache_bytes_quant(C.byref(desc), C.byref(s), C.byref(k)), "sepllm_cache_bytes_quant")
+    return s.value, k.value
+
+
+def sepllm_cache_update_quant(desc, state, Kc, Vc, new_token_ids, sep_ids, k_new, v_new):
+    """sepllm_cache_update for a cache held in 4 bits (Kc, Vc: sepllm_cache_bytes_quant)."""
+    where, row = "sepllm_cache_update_quant", (desc.B, desc.Hkv, desc.d)
+    arr, p, n = _sep_array(sep_ids)
+    _expect(where, ("new_token_ids", new_token_ids, (desc.B,), torch.int32), ("k_new", k_new, row, torch.bfloat16),
+            ("v_new", v_new, row, torch.bfloat16))
+    _quant_kv(where, desc, Kc, Vc)
+    st, kc, vc, ids, kn, vn = _addresses(where, (state, Kc, Vc, new_token_ids, k_new, v_new))
+    _check(lib().sepllm_cache_update_quant(C.byref(desc), st, kc, vc, ids, p, n, kn, vn, _raw_stream()), where)
+
+
+def sepllm_cache_from_prompt_quant(desc, idesc, index, prompt_len, K, V, state, Kc, Vc):
+    """sepllm_cache_from_prompt for a cache held in 4 bits; prompt_len: int32 [B] or None."""
+    where, bf, rows = "sepllm_cache_from_prompt_quant", torch.bfloat16, (desc.B, desc.Hkv, idesc.L, desc.d)
+    _expect(where, ("prompt_len", prompt_len, (desc.B,), torch.int32), ("K", K, rows, bf), ("V", V, rows, bf))
+    _quant_kv(where, desc, Kc, Vc)
+    _check(lib().sepllm_cache_from_prompt_quant(C.byref(desc), C.byref(idesc), *_addresses(
+        where, (index, prompt_len, K, V, state, Kc, Vc)), _raw_stream()), where)
+
+
+def sepllm_cache_entries_quant(desc, state, Kc, Vc, n, K, V, length=None):
+    """The retained entries of a cache held in 4 bits, in order, as bf16 rows 0 .. Size_run-1 of K, V
+    [B][Hkv][n][d]; length: int32 [B] that receives Size_run, or None."""
+    where, bf, rows = "sepllm_cache_entries_quant", torch.bfloat16, (desc.B, desc.Hkv, n, desc.d)
+    _expect(where, ("K", K, rows, bf), ("V", V, rows, bf), ("length", length, (desc.B,), torch.int32))
+    _quant_kv(where, desc, Kc, Vc)
+    st, kc, vc, k, v, ln = _addresses(where, (state, Kc, Vc, K, V, length))
+    _check(lib().sepllm_cache_entries_quant(C.byref(desc), st, kc, vc, n, k, v, ln, _raw_stream()), where)
+
+
+def sepllm_decode_quant_workspace_bytes(desc):
+    b = C.c_size_t(0)
+    _check(lib().sepllm_decode_quant_workspace_bytes(C.byref(desc), C.byref(b)),
+           "sepllm_decode_quant_workspace_bytes")
+    return b.value
+
+
+def sepllm_decode_quant(desc, scale, q, state, Kc, Vc, o, lse, workspace):
+    """sepllm_decode over a cache held in 4 bits; lse may be None."""
+    where, row = "sepllm_decode_quant", (desc.B, desc.Hq, desc.d)
+    _expect(where, ("q", q, row, torch.bfloat16), ("o", o, row, torch.bfloat16), ("lse", lse, row[:2], torch.float32))
+    _quant_kv(where, desc, Kc, Vc)
+    _check(lib().sepllm_decode_quant(C.byref(desc), scale, *_addresses(where, (q, state, Kc, Vc, o, lse, workspace)),
+                                     _raw_stream()), where)
 
 
 def read_cache_state(state: torch.Tensor) -> dict:

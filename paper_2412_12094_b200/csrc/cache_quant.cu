@@ -1,0 +1,932 @@
+// The streaming cache held in 4 bits: update, prompt hand-off, read-back and decode.
+//
+// Format.  32 neighbouring elements of a row share a step, a bf16 number s = -m / 8 with m their element
+// of largest magnitude (the positive one of two equal ones); an element x is held as the whole number
+// q in -8 .. 7 nearest to x / s (the even one of two), so m itself is held exactly and the others to
+// half a step, except one of the other sign beyond 7.5 steps.  m is a bf16 number, so s = -m / 8 is
+// too: nothing is rounded but q, and codes are the same whatever precision they are computed in.
+//
+// Buffers.  K and V have one each: codes [B][Hkv][slots][d / 2] bytes, then (256-byte aligned) steps
+// [B][Hkv][slots][d / 32].  Slots, rings and the state are those of the 16-bit cache.  Inside a row the
+// codes q + 8, two to a byte (the low half first), are ordered so that the decode kernel's threads find
+// what their matrix operands need in one word: element e of group j stands at place
+// ((e / m) * (d / 32) + j) * m + e % m with m = 8 for keys and m = 4 for values.
+#include <cuda_fp8.h>
+
+#include "cache_common.cuh"
+
+namespace sepllm {
+
+namespace {
+
+constexpr int kGroup = 32;             // elements that share a step
+constexpr float kFlush = 0x1p-100f;    // groups whose largest magnitude is below are held as zeros
+
+// One of Kc / Vc.
+template <class Byte>
+struct QuantRows {
+  Byte* codes;
+  Byte* steps;
+};
+inline size_t quant_code_bytes(const sepllm_cache_header& h) {
+  return align_up(size_t(h.desc.B) * h.desc.Hkv * h.slots * (h.desc.d / 2));
+}
+inline QuantRows<uint8_t> quant_rows(const sepllm_cache_header& h, void* buf) {
+  uint8_t* p = static_cast<uint8_t*>(buf);
+  return {p, p + quant_code_bytes(h)};
+}
+inline QuantRows<const uint8_t> quant_rows(const sepllm_cache_header& h, const void* buf) {
+  const uint8_t* p = static_cast<const uint8_t*>(buf);
+  return {p, p + quant_code_bytes(h)};
+}
+
+// Eight elements 8t .. 8t + 7 of a group, t = lane % 4; the group's four lanes are neighbours and all 32
+// lanes call.  Returns their codes, element e at bits 4e .. 4e + 3, and the group's step.
+//
+// A code is found from x * (1 / s), within 2^-20 of x / s.  x / s is either half a whole number
+// exactly, or at least 2^-10 away from one (x and s have eight significant bits): rounded to a multiple of
+// 2^-13 first (the sum with 1536), ties are ties again and nothing else has become one.
+__device__ __forceinline__ uint32_t quantise8(const uint4& raw, uint32_t* step_bits) {
+  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
+  float x[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 f = __bfloat1622float2(h[k]);
+    x[2 * k] = f.x;
+    x[2 * k + 1] = f.y;
+  }
+  float hi = x[0], lo = x[0];
+  bool bad = false;   // NaN or infinite
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    hi = fmaxf(hi, x[k]);
+    lo = fminf(lo, x[k]);
+    bad |= !(fabsf(x[k]) < INFINITY);
+  }
+  if (bad) hi = INFINITY;
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+  }
+  const float m = hi >= -lo ? hi : lo;
+  float s = m * -0.125f, r = 0.f;
+  if (hi == INFINITY) s = __int_as_float(0x7fc00000);   // reads back as NaN in every element
+  else if (fabsf(m) < kFlush) s = 0.f;
+  else r = __frcp_rn(s);
+  uint32_t w = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float t = r == 0.f ? 0.f : __fsub_rn(__fadd_rn(__fmul_rn(x[k], r), 1536.f), 1536.f);
+    w |= uint32_t(min(__float2int_rn(t), 7) + 8) << (4 * k);
+  }
+  *step_bits = __float_as_uint(s) >> 16;
+  return w;
+}
+
+// Stores the codes of elements 8t .. 8t + 7 of group j of a row (and its step from lane t = 0).
+template <int D, bool V>
+__device__ __forceinline__ void store_codes(uint8_t* codes, uint8_t* steps, int j, int t, uint32_t w, uint32_t step) {
+  constexpr int kGroups = D / kGroup;
+  if (!V) {
+    reinterpret_cast<uint32_t*>(codes)[t * kGroups + j] = w;
+  } else {
+    uint16_t* c = reinterpret_cast<uint16_t*>(codes);
+    c[2 * t * kGroups + j] = uint16_t(w);
+    c[(2 * t + 1) * kGroups + j] = uint16_t(w >> 16);
+  }
+  if (t == 0) reinterpret_cast<uint16_t*>(steps)[j] = uint16_t(step);
+}
+
+// grid (B, Hkv).  As the 16-bit cache's update: every CTA moves the rows of its kv head, the one that
+// finishes last for a sequence updates the state.  The new rows are quantised by the first warp; rows that
+// move keep their codes.  Latency: 256 CTAs of one round of loads each.
+template <int D>
+__global__ void __launch_bounds__(kUpdThreads)
+quant_update(sepllm_cache_header h, uint8_t* __restrict__ state, QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc,
+             const __nv_bfloat16* __restrict__ k_new, const __nv_bfloat16* __restrict__ v_new,
+             const int32_t* __restrict__ new_token_ids, SepIds sep) {
+  extern __shared__ int16_t flag_s[];
+  __shared__ int warp_buf[32];
+  constexpr int kVec = D / 8, kCode = D / 2, kStep = D / 16;   // 16-byte pieces of a new row; bytes of a held one
+  const sepllm_cache_desc& d = h.desc;
+  const int b = blockIdx.x, hk = blockIdx.y, tid = threadIdx.x;
+  const size_t unit = size_t(b) * d.Hkv + hk;
+  uint4 raw = make_uint4(0, 0, 0, 0);
+  const bool mine = tid < 2 * kVec, is_v = tid >= kVec;   // one warp at most
+  if (mine)
+    raw = reinterpret_cast<const uint4*>(is_v ? v_new : k_new)[unit * kVec + (is_v ? tid - kVec : tid)];
+  CacheView v = cache_view(state, h);
+  const sepllm_cache_seq q = v.seq[b];
+  const UpdatePlan p = plan_update(q, d);
+  uint8_t *kc = Kc.codes + unit * h.slots * kCode, *vc = Vc.codes + unit * h.slots * kCode;
+  uint8_t *ks = Kc.steps + unit * h.slots * kStep, *vs = Vc.steps + unit * h.slots * kStep;
+  if (tid < 32) {
+    uint32_t step;
+    const uint32_t w = quantise8(raw, &step);
+    const int ch = tid % kVec;
+    const size_t slot = p.append_slot;
+    if (mine && !is_v) store_codes<D, false>(kc + slot * kCode, ks + slot * kStep, ch / 4, ch % 4, w, step);
+    if (mine && is_v) store_codes<D, true>(vc + slot * kCode, vs + slot * kStep, ch / 4, ch % 4, w, step);
+  }
+  UpdateMoves mv{p.compact && d.s > 0, 0, 0};
+  if (mv.any) {
+    mv.m = rank_past_separators(v.slot_is_sep + size_t(b) * h.slots, q, d, p.n_past, flag_s, warp_buf);
+    mv.drop = max(0, q.size_sep + mv.m - d.s);
+    // 16 lanes to an entry: 16-byte pieces of its codes, its steps
+    constexpr int kPieces = kCode / 16;
+    const int l = tid % 16;
+    for (int k = tid / 16; k < p.n_past; k += kUpdThreads / 16) {
+      int src, dst;
+      if (!past_move(k, flag_s, q, d, mv.drop, &src, &dst)) continue;
+      if (l < 2 * kPieces) {
+        uint4* c = reinterpret_cast<uint4*>(l < kPieces ? kc : vc);
+        c[size_t(dst) * kPieces + l % kPieces] = c[size_t(src) * kPieces + l % kPieces];
+      } else if (l < 2 * kPieces + 2 * (kStep / 4)) {
+        const int x = l - 2 * kPieces;
+        uint32_t* s = reinterpret_cast<uint32_t*>(x < kStep / 4 ? ks : vs);
+        s[size_t(dst) * (kStep / 4) + x % (kStep / 4)] = s[size_t(src) * (kStep / 4) + x % (kStep / 4)];
+      }
+    }
+  }
+  __syncthreads();  // this CTA's append and moves are done
+  finish_update(v, h, b, q, next_record(q, d, p, mv), p, mv, flag_s, new_token_ids, sep);
+}
+
+constexpr int kCopyThreads = 256;
+constexpr int kCopyRows = 64;  // slots (or entries) per CTA
+
+// grid (ceil(slots / kCopyRows), Hkv, B), behind the plan of the hand-off.  Quantises the K and V rows of the
+// retained positions into their slots: 2 * D / 8 lanes take one slot's rows in 16-byte pieces.  Bound by
+// HBM: the retained rows are read once, a quarter of that is written.
+template <int D>
+__global__ void __launch_bounds__(kCopyThreads)
+quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ K,
+             const __nv_bfloat16* __restrict__ V, int L, QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc) {
+  constexpr int kVec = D / 8, kRowsPerPass = kCopyThreads / (2 * kVec), kPasses = kCopyRows / kRowsPerPass;
+  const sepllm_cache_desc& d = h.desc;
+  const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
+  CacheView v = cache_view(const_cast<uint8_t*>(state), h);
+  const sepllm_cache_seq q = v.seq[b];
+  const int64_t* pos_b = v.slot_pos + size_t(b) * h.slots;
+  const size_t unit = size_t(b) * d.Hkv + hk;
+  const int sub = tid / (2 * kVec), l = tid % (2 * kVec);
+  const bool is_v = l >= kVec;
+  const int ch = l % kVec;  // 16-byte piece of the row
+  const uint4* src = reinterpret_cast<const uint4*>(is_v ? V : K) + unit * size_t(L) * kVec + ch;
+  const int slot0 = blockIdx.x * kCopyRows + sub;
+  uint4 raw[kPasses];
+  uint32_t used = 0;
+#pragma unroll
+  for (int r = 0; r < kPasses; ++r) {
+    const int slot = slot0 + r * kRowsPerPass;
+    const bool u = slot < d.a             ? slot < q.size_init
+                   : slot < d.a + d.s     ? slot - d.a < q.size_sep
+                   : slot < h.slots       ? slot - d.a - d.s < q.size_win
+                                          : false;
+    raw[r] = u ? __ldg(src + size_t(pos_b[slot]) * kVec) : make_uint4(0, 0, 0, 0);
+    used |= uint32_t(u) << r;
+  }
+#pragma unroll
+  for (int r = 0; r < kPasses; ++r) {
+    uint32_t step;
+    const uint32_t w = quantise8(raw[r], &step);
+    if (!(used >> r & 1)) continue;
+    const size_t row = unit * h.slots + slot0 + r * kRowsPerPass;
+    if (!is_v) store_codes<D, false>(Kc.codes + row * (D / 2), Kc.steps + row * (D / 16), ch / 4, ch % 4, w, step);
+    else store_codes<D, true>(Vc.codes + row * (D / 2), Vc.steps + row * (D / 16), ch / 4, ch % 4, w, step);
+  }
+}
+
+// Eight codes (element e at bits 4e ..) times their step, rounded to bf16 once (the product has up to
+// twelve significant bits, bf16 eight).
+__device__ __forceinline__ uint4 values8(uint32_t w, float s) {
+  uint32_t out[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    out[k] = pack_bf16(float(int(w >> (8 * k) & 15) - 8) * s, float(int(w >> (8 * k + 4) & 15) - 8) * s);
+  return make_uint4(out[0], out[1], out[2], out[3]);
+}
+
+// grid (ceil(c / kCopyRows), Hkv, B).  Row v of K and V of sequence b is its retained entry v.
+template <int D>
+__global__ void __launch_bounds__(kCopyThreads)
+quant_entries(sepllm_cache_header h, const uint8_t* __restrict__ state, QuantRows<const uint8_t> Kc,
+              QuantRows<const uint8_t> Vc, int n, __nv_bfloat16* __restrict__ K, __nv_bfloat16* __restrict__ V,
+              int32_t* __restrict__ length) {
+  constexpr int kVec = D / 8, kGroups = D / kGroup, kRowsPerPass = kCopyThreads / kVec;
+  const sepllm_cache_desc& d = h.desc;
+  const int b = blockIdx.z, hk = blockIdx.y;
+  CacheView cv = cache_view(const_cast<uint8_t*>(state), h);
+  const sepllm_cache_seq q = cv.seq[b];
+  const int run = min(n, q.size_init + q.size_sep + q.size_win);
+  if (length && blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) length[b] = run;
+  const int ch = threadIdx.x % kVec, j = ch / 4, t = ch % 4;
+  const size_t unit = size_t(b) * d.Hkv + hk;
+#pragma unroll
+  for (int r = 0; r < kCopyRows; r += kRowsPerPass) {
+    const int v = blockIdx.x * kCopyRows + r + threadIdx.x / kVec;
+    if (v >= run) return;
+    const size_t row = unit * h.slots + virtual_to_slot(v, q, d);
+    const uint32_t wk = reinterpret_cast<const uint32_t*>(Kc.codes + row * (D / 2))[t * kGroups + j];
+    const uint16_t* vc = reinterpret_cast<const uint16_t*>(Vc.codes + row * (D / 2));
+    const uint32_t wv = vc[2 * t * kGroups + j] | uint32_t(vc[(2 * t + 1) * kGroups + j]) << 16;
+    const float sk = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(Kc.steps)[row * kGroups + j]);
+    const float sv = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(Vc.steps)[row * kGroups + j]);
+    const size_t dst = (unit * n + v) * kVec + ch;
+    reinterpret_cast<uint4*>(K)[dst] = values8(wk, sk);
+    reinterpret_cast<uint4*>(V)[dst] = values8(wv, sv);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Decode
+// ---------------------------------------------------------------------------
+constexpr int kDecThreads = 128, kDecWarps = kDecThreads / 32;
+constexpr int kTile = 32;                        // entries of a warp's tile
+constexpr int kStepRows = kDecWarps * kTile;     // entries of a CTA's step
+constexpr int kStages = 4;
+
+// D[16 keys x 8 heads] = A[16 x 32] B[32 x 8] + C, e4m3 operands.
+__device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2],
+                                         float c0, float c1, float c2, float c3) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+      "{%8, %9}, {%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                         uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+      "{%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Transposes an 8 x 8 matrix of 16-bit elements held two to a lane.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+template <int BYTES>
+__device__ __forceinline__ void cp_async_small(uint32_t dst, const void* src, uint32_t src_bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(src_bytes)
+               : "memory");
+}
+__device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// Place of a tile's V row r in shared memory: a read takes rows 2t + x, t < 4, of which this makes
+// neighbours (and pieces of rows of 64 bytes are turned by bit 1 of it), so that they meet different banks.
+__device__ __forceinline__ int value_row(int r) { return (r & ~7) | (r >> 1 & 3) | (r & 1) << 2; }
+
+struct QuantDecodeParams {
+  sepllm_cache_header h;
+  const uint8_t* state;
+  const __nv_bfloat16* q;
+  QuantRows<const uint8_t> Kc, Vc;
+  __nv_bfloat16* o;
+  float* lse;
+  int4* ends;        // [CTA] (b, hk) of the unit whose first steps were an earlier CTA's, and of the one whose
+                     // last steps are a later one's; -1: none
+  float2* part_ml;   // [2 * CTA + (0: the former, 1: the latter)][G] reference exponent and sum
+  float* part_acc;   // [same][G][D]
+  int32_t* status;
+  float scale_log2;
+};
+
+__device__ __forceinline__ int run_of(const sepllm_cache_seq& s) { return s.size_init + s.size_sep + s.size_win; }
+// Steps of a sequence's kv head; one for an empty sequence, whose output has to be written too.
+__device__ __forceinline__ int steps_of(const sepllm_cache_seq& s) {
+  return max(1, (run_of(s) + kStepRows - 1) / kStepRows);
+}
+
+// The CTA's share.  The steps of all (sequence, kv head) units, laid end to end, are cut into equal runs,
+// one per CTA: sequences of any lengths load the SMs evenly, and a unit is cut at most where a CTA's run
+// ends.  All threads call; false: nothing is left for this CTA.
+struct Share {
+  int b, hk, step;   // where the run starts
+  int64_t left;      // its steps
+};
+__device__ bool share_of(const sepllm_cache_seq* seq, int B, int Hkv, Share* out) {
+  __shared__ int64_t s_sum[kDecWarps];
+  __shared__ int64_t s_first;
+  __shared__ int s_b;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  int64_t sum = 0;
+  for (int b = tid; b < B; b += kDecThreads) sum += steps_of(seq[b]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_sum[wid] = sum;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kDecWarps; ++w) total += s_sum[w];
+  total *= Hkv;
+  const int64_t ctas = min(int64_t(gridDim.x), total);
+  if (blockIdx.x >= ctas) return false;
+  const int64_t first = total * blockIdx.x / ctas, last = total * (blockIdx.x + 1) / ctas;
+  const int64_t target = first / Hkv;   // in steps of one kv head
+  int64_t before = 0;                   // steps of the sequences before this chunk
+  for (int b0 = 0; b0 < B; b0 += kDecThreads) {
+    const int b = b0 + tid;
+    const int n = b < B ? steps_of(seq[b]) : 0;
+    int64_t incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    __syncthreads();
+    if (lane == 31) s_sum[wid] = incl;
+    __syncthreads();
+    int64_t chunk = 0;
+#pragma unroll
+    for (int w = 0; w < kDecWarps; ++w) {
+      if (w < wid) incl += s_sum[w];
+      chunk += s_sum[w];
+    }
+    incl += before;
+    before += chunk;
+    if (n > 0 && incl - n <= target && target < incl) {
+      s_b = b;
+      s_first = incl - n;
+    }
+    if (target < before) break;   // (the same for all threads)
+  }
+  __syncthreads();
+  out->b = s_b;
+  const int n = steps_of(seq[s_b]);
+  const int64_t in_seq = first - s_first * Hkv;
+  out->hk = int(in_seq / n);
+  out->step = int(in_seq - int64_t(out->hk) * n);
+  out->left = last - first;
+  return true;
+}
+
+// CTAs per SM (three: at most 168 registers a thread).
+template <int D, int NT>
+constexpr int decode_quant_resident() {
+  return D == 128 && NT == 2 ? 2 : 3;
+}
+template <int D, int NT>
+constexpr int decode_quant_smem() {
+  constexpr int ring = kDecWarps * kStages * 2 * kTile * (D / 2 + D / 16);
+  constexpr int merge = kDecWarps * 8 * NT * (D * 4 + 8);
+  return ring > merge ? ring : merge;
+}
+
+// 4 warps a CTA; each is a flash-decoding worker over its 32-entry tiles of the CTA's steps, which arrive
+// through a ring of cp.async stages.  The products have entries (or elements of V) as the M dimension
+// and the G query heads of the kv head as N = 8 (NT = 2: two tiles of 8).
+//
+// K q: the e4m3 number with bits 0000cccc is cccc * 2^-9 for every code c, so a word of eight codes becomes
+// two operand registers with two masks and a shift.  q is brought near 2^7 by a power of two and split into
+// two e4m3 numbers, which hold its eight bits exactly down to 2^-9 of the head's largest element (and
+// lose 2^-17 of that below); the products are exact and summed in 32 bits.  The codes' offset 8 is taken
+// off by the accumulator's start, -8 times the sum of q over the group, and the key's step multiplies
+// the group's 32-bit sum.
+//
+// P V: codes become bf16 128 + c with one mask-and-or each (two entries of a word pair to a register).  P
+// times the group's step is rounded to bf16 (2^-9), the only rounding here; the offset 136 is taken off
+// the sums by a product with ones, which sums those same rounded numbers.
+template <int D, int NT>
+__global__ void __launch_bounds__(kDecThreads, decode_quant_resident<D, NT>())
+decode_quant(const __grid_constant__ QuantDecodeParams p) {
+  constexpr int kGroups = D / kGroup;
+  constexpr int kCode = D / 2, kStep = D / 16;              // bytes of a row
+  constexpr int kStageB = 2 * kTile * (kCode + kStep);
+  constexpr int GS = 8 * NT;
+  extern __shared__ __align__(128) uint8_t dec_smem[];
+  let_dependents_start();
+  const sepllm_cache_desc& d = p.h.desc;
+  const int G = d.Hq / d.Hkv;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int g = lane >> 2, t = lane & 3;
+  if (tid == 0 && blockIdx.x == 0) *p.status = SEPLLM_OK;
+  const sepllm_cache_seq* seqs = cache_view(const_cast<uint8_t*>(p.state), p.h).seq;
+  Share sh;
+  if (!share_of(seqs, d.B, d.Hkv, &sh)) {
+    if (tid == 0) p.ends[blockIdx.x] = make_int4(-1, -1, -1, -1);
+    return;
+  }
+  uint8_t* ring = dec_smem + wid * (kStages * kStageB);
+  const uint32_t ring_u = smem_u32(ring);
+  int4 ends = make_int4(-1, -1, -1, -1);
+
+  while (sh.left > 0) {
+    const sepllm_cache_seq sq = seqs[sh.b];
+    const int run = run_of(sq), steps = steps_of(sq);
+    const int n_steps = int(min(sh.left, int64_t(steps - sh.step)));
+    const int v0 = sh.step * kStepRows, v1 = min(run, (sh.step + n_steps) * kStepRows);
+    const int n_tiles = (v1 - v0 + kTile - 1) / kTile;
+    const int my_n = n_tiles > wid ? (n_tiles - wid + kDecWarps - 1) / kDecWarps : 0;
+    const size_t unit = size_t(sh.b) * d.Hkv + sh.hk;
+    const uint8_t *kc = p.Kc.codes + unit * p.h.slots * kCode, *vc = p.Vc.codes + unit * p.h.slots * kCode;
+    const uint8_t *ks = p.Kc.steps + unit * p.h.slots * kStep, *vs = p.Vc.steps + unit * p.h.slots * kStep;
+
+    // this warp's i-th tile into stage i % kStages: codes of K and V, steps of K and V.  Rows behind v1 are
+    // zeros.
+    auto issue = [&](int i) {
+      const int vb = v0 + (wid + i * kDecWarps) * kTile;
+      const uint32_t sK = ring_u + (i % kStages) * kStageB, sV = sK + kTile * kCode;
+      const uint32_t sks = sV + kTile * kCode, svs = sks + kTile * kStep;
+      const uint32_t ok = vb + lane < v1;
+      const int slot = virtual_to_slot(min(vb + lane, v1 - 1), sq, d);
+      cp_async_small<kStep>(sks + lane * kStep, ks + size_t(slot) * kStep, ok * kStep);
+      cp_async_small<kStep>(svs + lane * kStep, vs + size_t(slot) * kStep, ok * kStep);
+      constexpr int kPieces = kCode / 16, kRows = 32 / kPieces;
+#pragma unroll
+      for (int x = 0; x < kTile / kRows; ++x) {
+        const int r = x * kRows + lane / kPieces, c = lane % kPieces;
+        const size_t off = size_t(__shfl_sync(0xffffffffu, slot, r)) * kCode + c * 16;
+        const uint32_t bytes = vb + r < v1 ? 16u : 0u;
+        cp_async16(sK + r * kCode + c * 16, kc + off, bytes);
+        const int rv = value_row(r), cv = kPieces == 4 ? c ^ (rv & 2) : c;
+        cp_async16(sV + rv * kCode + cv * 16, vc + off, bytes);
+      }
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) {
+      if (s < my_n) issue(s);
+      cp_async_commit();
+    }
+
+    // q of head 8n + g as operand registers, elements 32j + 8t ..; sums over the group and factors of the
+    // heads that this lane's accumulators belong to, 8n + 2t and 8n + 2t + 1
+    uint32_t q_hi[NT][kGroups][2], q_lo[NT][kGroups][2];
+    float start[NT][kGroups][2], factor[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int head = 8 * n + g;
+      const uint4* row = reinterpret_cast<const uint4*>(
+          p.q + (size_t(sh.b) * d.Hq + sh.hk * G + min(head, G - 1)) * D) + t;
+      uint4 raw[kGroups];
+      float most = 0.f;
+#pragma unroll
+      for (int j = 0; j < kGroups; ++j) {
+        raw[j] = head < G ? __ldg(row + j * 4) : make_uint4(0, 0, 0, 0);
+        const __nv_bfloat162* x = reinterpret_cast<const __nv_bfloat162*>(&raw[j]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 f = __bfloat1622float2(x[k]);
+          most = fmaxf(most, fmaxf(fabsf(f.x), fabsf(f.y)));
+        }
+      }
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      // 2^e with most * 2^e in [128, 256) (2^e and its inverse stay normal numbers)
+      const int e = max(-110, min(110, 134 - int(__float_as_uint(most) >> 23)));
+      const float up = __uint_as_float(uint32_t(127 + e) << 23);
+      const float back = p.scale_log2 * __uint_as_float(uint32_t(127 + 9 - e) << 23);
+#pragma unroll
+      for (int j = 0; j < kGroups; ++j) {
+        const __nv_bfloat162* x = reinterpret_cast<const __nv_bfloat162*>(&raw[j]);
+        uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 f = __bfloat1622float2(x[k]);
+#pragma unroll
+          for (int odd = 0; odd < 2; ++odd) {
+            const float y = (odd ? f.y : f.x) * up;
+            // (an infinite element, or one beyond 2^118, becomes NaN)
+            const __nv_fp8_e4m3 a(fabsf(y) < 448.f ? y : __int_as_float(0x7fc00000));
+            const __nv_fp8_e4m3 c(y - float(a));
+            sum += float(a) + float(c);
+            hi[odd] |= uint32_t(a.__x) << (8 * k);
+            lo[odd] |= uint32_t(c.__x) << (8 * k);
+          }
+        }
+        q_hi[n][j][0] = hi[0];
+        q_hi[n][j][1] = hi[1];
+        q_lo[n][j][0] = lo[0];
+        q_lo[n][j][1] = lo[1];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        start[n][j][0] = __shfl_sync(0xffffffffu, sum, 8 * t) * (-8.f * 0x1p-9f);
+        start[n][j][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4) * (-8.f * 0x1p-9f);
+      }
+      factor[n][0] = __shfl_sync(0xffffffffu, back, 8 * t);
+      factor[n][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
+    }
+
+    float oacc[2 * kGroups][NT][4], ones[kGroups][NT][4];
+    float m_ref[NT][2], l_sum[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int j = 0; j < 2 * kGroups; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) oacc[j][n][e] = 0.f;
+#pragma unroll
+      for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ones[j][n][e] = 0.f;
+      m_ref[n][0] = m_ref[n][1] = -INFINITY;
+      l_sum[n][0] = l_sum[n][1] = 0.f;
+    }
+
+    for (int i = 0; i < my_n; ++i) {
+      cp_async_wait<kStages - 2>();
+      __syncwarp();
+      if (i + kStages - 1 < my_n) issue(i + kStages - 1);
+      cp_async_commit();
+      const uint8_t* sK = ring + (i % kStages) * kStageB;
+      const uint8_t* sV = sK + kTile * kCode;
+      const uint8_t* sks = sV + kTile * kCode;
+      const uint8_t* svs = sks + kTile * kStep;
+      const int vb = v0 + (wid + i * kDecWarps) * kTile;
+
+      // scores in log2 units: entries 16x + g (+ 8), heads 8n + 2t (+ 1)
+      float sc[2][NT][4];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint32_t w[2][kGroups], st[2][(kGroups + 1) / 2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int r = 16 * x + 8 * y + g;
+          const uint32_t* src = reinterpret_cast<const uint32_t*>(sK + r * kCode) + t * kGroups;
+          const uint32_t* ssrc = reinterpret_cast<const uint32_t*>(sks + r * kStep);
+          if (kGroups == 4) {
+            *reinterpret_cast<uint4*>(w[y]) = *reinterpret_cast<const uint4*>(src);
+            *reinterpret_cast<uint2*>(st[y]) = *reinterpret_cast<const uint2*>(ssrc);
+          } else {
+            *reinterpret_cast<uint2*>(w[y]) = *reinterpret_cast<const uint2*>(src);
+            st[y][0] = *ssrc;
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[x][n][e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j) {
+          const uint32_t a[4] = {w[0][j] & 0x0f0f0f0fu, w[1][j] & 0x0f0f0f0fu, w[0][j] >> 4 & 0x0f0f0f0fu,
+                                 w[1][j] >> 4 & 0x0f0f0f0fu};
+          const float s0 = j & 1 ? bf16_high(st[0][j / 2]) : bf16_low(st[0][j / 2]);
+          const float s1 = j & 1 ? bf16_high(st[1][j / 2]) : bf16_low(st[1][j / 2]);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float c[4];
+            mma_e4m3(c, a, q_hi[n][j], start[n][j][0], start[n][j][1], start[n][j][0], start[n][j][1]);
+            mma_e4m3(c, a, q_lo[n][j], c[0], c[1], c[2], c[3]);
+            sc[x][n][0] += c[0] * s0;
+            sc[x][n][1] += c[1] * s0;
+            sc[x][n][2] += c[2] * s1;
+            sc[x][n][3] += c[3] * s1;
+          }
+        }
+      }
+      bool above = false;   // a score beyond 2^8 of the reference: it moves up
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sc[x][n][e] *= factor[n][e & 1];
+            if (vb + kTile > v1 && vb + 16 * x + 8 * (e >> 1) + g >= v1) sc[x][n][e] = -INFINITY;
+            above |= sc[x][n][e] > m_ref[n][e & 1] + 8.f;
+          }
+      if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float mx = fmaxf(fmaxf(sc[0][n][e], sc[0][n][e + 2]), fmaxf(sc[1][n][e], sc[1][n][e + 2]));
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            if (mx > m_ref[n][e] + 8.f) {
+              const float corr = m_ref[n][e] == -INFINITY ? 0.f : ex2(m_ref[n][e] - mx);
+              m_ref[n][e] = mx;
+              l_sum[n][e] *= corr;
+#pragma unroll
+              for (int j = 0; j < 2 * kGroups; ++j) {
+                oacc[j][n][e] *= corr;
+                oacc[j][n][e + 2] *= corr;
+              }
+#pragma unroll
+              for (int j = 0; j < kGroups; ++j) ones[j][n][e] *= corr;
+            }
+          }
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float m = m_ref[n][e] == -INFINITY ? 0.f : m_ref[n][e];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            sc[x][n][e] = ex2(sc[x][n][e] - m);
+            sc[x][n][e + 2] = ex2(sc[x][n][e + 2] - m);
+            l_sum[n][e] += sc[x][n][e] + sc[x][n][e + 2];
+          }
+        }
+
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        // entries 2t, 2t + 1, 2t + 8, 2t + 9 of the half tile (see issue() for their places)
+        uint32_t w[4][(kGroups + 1) / 2], st[2][(kGroups + 1) / 2];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int r = 16 * x + 2 * t + (y & 1) + 8 * (y >> 1);
+          const int rv = value_row(r);
+          if (kGroups == 4) {
+            const int piece = (g >> 1) ^ (rv & 2);
+            *reinterpret_cast<uint2*>(w[y]) =
+                *reinterpret_cast<const uint2*>(sV + rv * kCode + piece * 16 + (g & 1) * 8);
+          } else {
+            w[y][0] = *reinterpret_cast<const uint32_t*>(sV + rv * kCode + g * 4);
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t* ssrc = reinterpret_cast<const uint32_t*>(svs + (16 * x + 8 * y + g) * kStep);
+          if (kGroups == 4) *reinterpret_cast<uint2*>(st[y]) = *reinterpret_cast<const uint2*>(ssrc);
+          else st[y][0] = *ssrc;
+        }
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j) {
+          const float s0 = j & 1 ? bf16_high(st[0][j / 2]) : bf16_low(st[0][j / 2]);
+          const float s1 = j & 1 ? bf16_high(st[1][j / 2]) : bf16_low(st[1][j / 2]);
+          uint32_t pb[NT][2];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            pb[n][0] = transpose8(pack_bf16(sc[x][n][0] * s0, sc[x][n][1] * s0));
+            pb[n][1] = transpose8(pack_bf16(sc[x][n][2] * s1, sc[x][n][3] * s1));
+          }
+          const uint32_t u = __byte_perm(w[0][j / 2], w[1][j / 2], j & 1 ? 0x7632 : 0x5410);
+          const uint32_t z = __byte_perm(w[2][j / 2], w[3][j / 2], j & 1 ? 0x7632 : 0x5410);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t a0 = (u >> (8 * half) & 0x000f000fu) | 0x43004300u;
+            const uint32_t a1 = (u >> (8 * half + 4) & 0x000f000fu) | 0x43004300u;
+            const uint32_t a2 = (z >> (8 * half) & 0x000f000fu) | 0x43004300u;
+            const uint32_t a3 = (z >> (8 * half + 4) & 0x000f000fu) | 0x43004300u;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_bf16(oacc[2 * j + half][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+          }
+          // (rows 8 to 15, which nobody reads, multiply with zeros)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_bf16(ones[j][n], 0x3f803f80u, 0u, 0x3f803f80u, 0u, pb[n][0], pb[n][1]);
+        }
+      }
+      __syncwarp();  // every lane is done with this stage before a later copy overwrites it
+    }
+    cp_async_wait<0>();
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l_sum[n][e] += __shfl_xor_sync(0xffffffffu, l_sum[n][e], o);
+    __syncthreads();  // all warps are out of their rings
+
+    // the warps' results, head by head, then merged: the unit's output, or a part of it
+    float2* sm_ml = reinterpret_cast<float2*>(dec_smem);
+    float* sm_acc = reinterpret_cast<float*>(dec_smem + kDecWarps * GS * sizeof(float2));
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int head = 8 * n + 2 * t + e;
+        if (head < G) {
+          if (g == 0) sm_ml[wid * GS + head] = make_float2(m_ref[n][e], l_sum[n][e]);
+#pragma unroll
+          for (int j = 0; j < 2 * kGroups; ++j) {
+            const float off = 136.f * ones[j / 2][n][e];
+            *reinterpret_cast<float2*>(sm_acc + (wid * GS + head) * D + (j / 2) * kGroup + 4 * g + 2 * (j & 1)) =
+                make_float2(oacc[j][n][e] - off, oacc[j][n][e + 2] - off);
+          }
+        }
+      }
+    __syncthreads();
+    const bool head_cut = sh.step > 0, tail_cut = sh.step + n_steps < steps;
+    const size_t part = 2 * size_t(blockIdx.x) + (head_cut ? 0 : 1);
+    for (int idx = tid; idx < G * D; idx += kDecThreads) {
+      const int hd = idx / D, e = idx % D;
+      float mm = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kDecWarps; ++w) mm = fmaxf(mm, sm_ml[w * GS + hd].x);
+      float ll = 0.f, aa = 0.f;
+#pragma unroll
+      for (int w = 0; w < kDecWarps; ++w) {
+        const float2 ml = sm_ml[w * GS + hd];
+        if (ml.y == 0.f) continue;   // a warp without entries (a NaN goes through)
+        const float f = ml.x == -INFINITY ? 1.f : ex2(ml.x - mm);
+        ll += ml.y * f;
+        aa += sm_acc[(w * GS + hd) * D + e] * f;
+      }
+      if (head_cut || tail_cut) {
+        p.part_acc[(part * G + hd) * D + e] = aa;
+        if (e == 0) p.part_ml[part * G + hd] = make_float2(mm, ll);
+      } else {
+        const size_t row = size_t(sh.b) * d.Hq + sh.hk * G + hd;
+        p.o[row * D + e] = __float2bfloat16(ll != 0.f ? aa / ll : 0.f);
+        if (p.lse && e == 0) p.lse[row] = ll != 0.f ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
+      }
+    }
+    if (head_cut) { ends.x = sh.b; ends.y = sh.hk; }
+    else if (tail_cut) { ends.z = sh.b; ends.w = sh.hk; }
+    __syncthreads();  // the merge buffers become the rings again
+
+    sh.left -= n_steps;
+    sh.step = 0;
+    if (++sh.hk == d.Hkv) { sh.hk = 0; ++sh.b; }
+  }
+  if (tid == 0) p.ends[blockIdx.x] = ends;
+}
+
+// grid (CTAs of decode_quant, G), D threads.  Joins the parts of a unit that was cut: the block of the CTA
+// that had its first steps, with the CTAs behind it that had the others.
+template <int D>
+__global__ void __launch_bounds__(D) decode_quant_join(const __grid_constant__ QuantDecodeParams p) {
+  wait_for_prior();
+  const sepllm_cache_desc& d = p.h.desc;
+  const int G = d.Hq / d.Hkv, hd = blockIdx.y, e = threadIdx.x, i = blockIdx.x;
+  const int4 mine = p.ends[i];
+  if (mine.z < 0) return;
+  int last = i;
+  while (last + 1 < int(gridDim.x)) {
+    const int4 x = p.ends[last + 1];
+    if (x.x != mine.z || x.y != mine.w) break;
+    ++last;
+  }
+  const size_t first = 2 * size_t(i) + 1;
+  float mm = p.part_ml[first * G + hd].x;
+  for (int k = i + 1; k <= last; ++k) mm = fmaxf(mm, p.part_ml[2 * size_t(k) * G + hd].x);
+  float ll = 0.f, aa = 0.f;
+  for (int k = i; k <= last; ++k) {
+    const size_t part = k == i ? first : 2 * size_t(k);
+    const float2 ml = p.part_ml[part * G + hd];
+    const float f = ml.x == -INFINITY ? 1.f : ex2(ml.x - mm);
+    ll += ml.y * f;
+    aa += p.part_acc[(part * G + hd) * D + e] * f;
+  }
+  const size_t row = size_t(mine.z) * d.Hq + mine.w * G + hd;
+  p.o[row * D + e] = __float2bfloat16(ll != 0.f ? aa / ll : 0.f);
+  if (p.lse && e == 0) p.lse[row] = ll != 0.f ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
+}
+
+// CTAs of a decode: as many as are resident, or one per step of the fullest caches.
+int decode_quant_ctas(const sepllm_cache_desc& d) {
+  const int64_t steps = (int64_t(d.c) + kStepRows - 1) / kStepRows;
+  const bool wide = d.Hq / d.Hkv > 8;
+  const int resident = d.d == 128 ? (wide ? decode_quant_resident<128, 2>() : decode_quant_resident<128, 1>())
+                                  : (wide ? decode_quant_resident<64, 2>() : decode_quant_resident<64, 1>());
+  return int(std::min<int64_t>(resident * kSmCount, int64_t(d.B) * d.Hkv * steps));
+}
+
+struct QuantDecodeLayout {
+  size_t off_ml, off_acc, bytes;
+};
+QuantDecodeLayout decode_quant_layout(const sepllm_cache_desc& d) {
+  const size_t ctas = size_t(decode_quant_ctas(d)), rows = 2 * ctas * (d.Hq / d.Hkv);
+  QuantDecodeLayout l;
+  l.off_ml = kAlign + align_up(ctas * sizeof(int4));
+  l.off_acc = l.off_ml + align_up(rows * sizeof(float2));
+  l.bytes = l.off_acc + align_up(rows * d.d * sizeof(float));
+  return l;
+}
+
+template <int D, int NT>
+sepllm_status launch_decode_quant(const QuantDecodeParams& p, cudaStream_t stream) {
+  constexpr int smem = decode_quant_smem<D, NT>();
+  const unsigned ctas = unsigned(decode_quant_ctas(p.h.desc));
+  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(decode_quant<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  decode_quant<D, NT><<<ctas, kDecThreads, smem, stream>>>(p);
+  SEPLLM_CUDA_TRY(cudaGetLastError());
+  const dim3 grid(ctas, p.h.desc.Hq / p.h.desc.Hkv);
+  SEPLLM_CUDA_TRY(launch_overlapped(decode_quant_join<D>, grid, D, 0, stream, p));
+  return SEPLLM_OK;
+}
+
+}  // namespace
+
+}  // namespace sepllm
+
+using namespace sepllm;
+
+extern "C" sepllm_status sepllm_cache_bytes_quant(const sepllm_cache_desc* desc, size_t* state_bytes,
+                                                  size_t* kv_bytes) {
+  sepllm_cache_header h;
+  const sepllm_status st = fill_cache_header(desc, &h);
+  if (st != SEPLLM_OK) return st;
+  if (state_bytes) *state_bytes = size_t(h.total_bytes);
+  if (kv_bytes)
+    *kv_bytes = quant_code_bytes(h) + align_up(size_t(desc->B) * desc->Hkv * h.slots * (desc->d / 16));
+  return SEPLLM_OK;
+}
+
+extern "C" sepllm_status sepllm_cache_update_quant(const sepllm_cache_desc* desc, void* state, void* Kc, void* Vc,
+                                                   const int32_t* new_token_ids, const int32_t* sep_ids,
+                                                   int32_t n_sep, const void* k_new, const void* v_new,
+                                                   void* stream_) {
+  sepllm_cache_header h;
+  sepllm_status st = fill_cache_header(desc, &h);
+  if (st != SEPLLM_OK) return st;
+  if (!state || !Kc || !Vc || !new_token_ids || !k_new || !v_new) return SEPLLM_INVALID_ARG;
+  if (!aligned(state, kAlign) || !aligned(Kc, kAlign) || !aligned(Vc, kAlign) || !aligned(k_new, 16) ||
+      !aligned(v_new, 16) || !aligned(new_token_ids, 4))
+    return SEPLLM_INVALID_ARG;
+  SepIds sep;
+  int max_past;
+  if ((st = update_params(desc, sep_ids, n_sep, &sep, &max_past)) != SEPLLM_OK) return st;
+  const size_t smem = size_t(max_past) * sizeof(int16_t);
+  auto kernel = desc->d == 128 ? quant_update<128> : quant_update<64>;
+  if (smem > 40 * 1024)
+    SEPLLM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+  kernel<<<dim3(desc->B, desc->Hkv), kUpdThreads, smem, static_cast<cudaStream_t>(stream_)>>>(
+      h, static_cast<uint8_t*>(state), quant_rows(h, Kc), quant_rows(h, Vc),
+      static_cast<const __nv_bfloat16*>(k_new), static_cast<const __nv_bfloat16*>(v_new), new_token_ids, sep);
+  SEPLLM_CUDA_TRY(cudaGetLastError());
+  return SEPLLM_OK;
+}
+
+extern "C" sepllm_status sepllm_cache_from_prompt_quant(const sepllm_cache_desc* desc, const sepllm_index_desc* idesc,
+                                                        const void* index, const int32_t* prompt_len, const void* K,
+                                                        const void* V, void* state, void* Kc, void* Vc,
+                                                        void* stream_) {
+  sepllm_cache_header h;
+  sepllm_status st = fill_cache_header(desc, &h);
+  if (st != SEPLLM_OK) return st;
+  sepllm_index_header ih;
+  if ((st = fill_index_header(idesc, &ih)) != SEPLLM_OK) return st;
+  if (!index || !K || !V || !state || !Kc || !Vc) return SEPLLM_INVALID_ARG;
+  if (idesc->B != desc->B || idesc->n_init != desc->a) return SEPLLM_INVALID_ARG;
+  if (!aligned(index, kAlign) || !aligned(state, kAlign) || !aligned(K, 16) || !aligned(V, 16) ||
+      !aligned(Kc, kAlign) || !aligned(Vc, kAlign) || !aligned(prompt_len, 4))
+    return SEPLLM_INVALID_ARG;
+  if (desc->B > 65535 || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  if ((st = launch_prompt_plan(h, ih, state, index, prompt_len, stream)) != SEPLLM_OK) return st;
+  const dim3 grid((h.slots + kCopyRows - 1) / kCopyRows, desc->Hkv, desc->B);
+  auto kernel = desc->d == 128 ? quant_prompt<128> : quant_prompt<64>;
+  kernel<<<grid, kCopyThreads, 0, stream>>>(h, static_cast<const uint8_t*>(state),
+                                            static_cast<const __nv_bfloat16*>(K), static_cast<const __nv_bfloat16*>(V),
+                                            idesc->L, quant_rows(h, Kc), quant_rows(h, Vc));
+  SEPLLM_CUDA_TRY(cudaGetLastError());
+  return SEPLLM_OK;
+}
+
+extern "C" sepllm_status sepllm_cache_entries_quant(const sepllm_cache_desc* desc, const void* state, const void* Kc,
+                                                    const void* Vc, int32_t n, void* K, void* V, int32_t* length,
+                                                    void* stream_) {
+  sepllm_cache_header h;
+  const sepllm_status st = fill_cache_header(desc, &h);
+  if (st != SEPLLM_OK) return st;
+  if (n < 1 || !state || !Kc || !Vc || !K || !V) return SEPLLM_INVALID_ARG;
+  if (!aligned(state, kAlign) || !aligned(Kc, kAlign) || !aligned(Vc, kAlign) || !aligned(K, 16) || !aligned(V, 16) ||
+      !aligned(length, 4))
+    return SEPLLM_INVALID_ARG;
+  if (n < desc->c) return SEPLLM_BUFFER_TOO_SMALL;
+  if (desc->B > 65535 || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
+  const dim3 grid((desc->c + kCopyRows - 1) / kCopyRows, desc->Hkv, desc->B);   // Size_run never passes c
+  auto kernel = desc->d == 128 ? quant_entries<128> : quant_entries<64>;
+  kernel<<<grid, kCopyThreads, 0, static_cast<cudaStream_t>(stream_)>>>(
+      h, static_cast<const uint8_t*>(state), quant_rows(h, Kc), quant_rows(h, Vc), n, static_cast<__nv_bfloat16*>(K),
+      static_cast<__nv_bfloat16*>(V), length);
+  SEPLLM_CUDA_TRY(cudaGetLastError());
+  return SEPLLM_OK;
+}
+
+extern "C" sepllm_status sepllm_decode_quant_workspace_bytes(const sepllm_cache_desc* desc, size_t* bytes) {
+  sepllm_cache_header h;
+  const sepllm_status st = fill_cache_header(desc, &h);
+  if (st != SEPLLM_OK) return st;
+  if (bytes) *bytes = decode_quant_layout(*desc).bytes;
+  return SEPLLM_OK;
+}
+
+extern "C" sepllm_status sepllm_decode_quant(const sepllm_cache_desc* desc, float scale, const void* q,
+                                             const void* state, const void* Kc, const void* Vc, void* o, float* lse,
+                                             void* workspace, void* stream_) {
+  QuantDecodeParams p{};
+  const sepllm_status st = fill_cache_header(desc, &p.h);
+  if (st != SEPLLM_OK) return st;
+  if (!q || !state || !Kc || !Vc || !o || !workspace) return SEPLLM_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(state, kAlign) || !aligned(Kc, kAlign) || !aligned(Vc, kAlign) || !aligned(o, 2) ||
+      !aligned(lse, 4) || !aligned(workspace, kAlign))
+    return SEPLLM_INVALID_ARG;
+  if (desc->B > 65535 || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
+  const QuantDecodeLayout l = decode_quant_layout(*desc);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.state = static_cast<const uint8_t*>(state);
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.Kc = quant_rows(p.h, Kc);
+  p.Vc = quant_rows(p.h, Vc);
+  p.o = static_cast<__nv_bfloat16*>(o);
+  p.lse = lse;
+  p.status = reinterpret_cast<int32_t*>(ws);
+  p.ends = reinterpret_cast<int4*>(ws + kAlign);
+  p.part_ml = reinterpret_cast<float2*>(ws + l.off_ml);
+  p.part_acc = reinterpret_cast<float*>(ws + l.off_acc);
+  p.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  const bool wide = desc->Hq / desc->Hkv > 8;
+  if (desc->d == 128) return wide ? launch_decode_quant<128, 2>(p, stream) : launch_decode_quant<128, 1>(p, stream);
+  return wide ? launch_decode_quant<64, 2>(p, stream) : launch_decode_quant<64, 1>(p, stream);
+}

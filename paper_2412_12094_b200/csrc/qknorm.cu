@@ -1,0 +1,614 @@
+// Norms of every query and key head with the rotary positions in the same pass, and their gradient.
+//
+// y = x r (offset + w), r = (mean x^2 + eps)^-1/2 over the head, then the rotation.  With g the gradient
+// of the outputs rotated back, n = x r and u = g (offset + w): dx = r (u - n mean(n u)), dw = sum g n.
+// Bound by HBM like the rotation alone: x (and dy) are read once, the output is written once; the
+// gradient computes r anew from x instead of reading it.
+#include "rope_common.cuh"
+
+namespace sepllm {
+
+namespace {
+
+constexpr int kWarps = kRopeThreads / 32;
+constexpr int kBwdBlocks = 3 * kSmCount;   // of the gradient, each with a share of the rows and a sum of its own
+
+struct NormParams {
+  RopeParams r;
+  const void* w[2];          // of Q and K, or null
+  int w_dtype, half;
+  float eps, offset, inv_d;
+  // gradient: the forward's inputs, the blocks' sums [block][2][d] and their total
+  const void* x[2];
+  int64_t xb[2], xh[2], xl[2];
+  float* part;
+  float* dw[2];
+  int64_t items;             // (group of tokens, group of heads)
+  int head_groups, blocks;
+};
+
+__device__ __forceinline__ float weight_at(const NormParams& p, int w, int e) {
+  if (!p.w[w]) return 1.f;
+  return p.offset + (p.w_dtype ? static_cast<const float*>(p.w[w])[e]
+                               : __bfloat162float(static_cast<const __nv_bfloat16*>(p.w[w])[e]));
+}
+
+// A thread's part of a row in the kernels for 16-byte accesses: as in rope_rows two pieces of eight
+// elements, c0 and c1, and whether they turn; d / 16 neighbouring lanes cover a row and a warp has whole
+// rows, so that a row's sums are a few shuffles.
+struct Pieces {
+  int c0, c1;
+  bool turn;
+};
+template <bool HALF>
+__device__ __forceinline__ Pieces pieces_of(const RopeParams& p, int t) {
+  Pieces s;
+  if (HALF) {
+    const int pairs = p.rot / 16;
+    s.turn = t < pairs;
+    s.c0 = 8 * (s.turn ? t : t + pairs);
+    s.c1 = s.c0 + (s.turn ? p.rot / 2 : (p.d - p.rot) / 2);
+  } else {
+    s.c0 = 8 * t;
+    s.c1 = s.c0 + p.d / 2;
+    s.turn = s.c0 < p.rot;
+  }
+  return s;
+}
+template <bool HALF>
+__device__ __forceinline__ void angles(const RopeParams& p, const Pieces& s, double pos, float2 (&cs)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int i = HALF ? s.c0 + k : (k < 4 ? s.c0 / 2 + k : s.c1 / 2 + k - 4);
+    cs[k] = s.turn && 2 * i < p.rot ? rope_cos_sin(p, pos, i) : make_float2(1.f, 0.f);
+  }
+}
+// (where nothing turns cs is (1, 0), but the products with 0 would spread a NaN)
+template <bool HALF>
+__device__ __forceinline__ void rotate(const RopeParams& p, const Pieces& s, const float2 (&cs)[8], float (&u)[8],
+                                       float (&v)[8]) {
+  if (HALF) {
+    if (!s.turn) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float y = u[k] * cs[k].x - v[k] * cs[k].y;
+      v[k] = v[k] * cs[k].x + u[k] * cs[k].y;
+      u[k] = y;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (s.c0 + 2 * k < p.rot) {
+        const float y = u[2 * k] * cs[k].x - u[2 * k + 1] * cs[k].y;
+        u[2 * k + 1] = u[2 * k + 1] * cs[k].x + u[2 * k] * cs[k].y;
+        u[2 * k] = y;
+      }
+      if (s.c1 + 2 * k < p.rot) {
+        const float y = v[2 * k] * cs[4 + k].x - v[2 * k + 1] * cs[4 + k].y;
+        v[2 * k + 1] = v[2 * k + 1] * cs[4 + k].x + v[2 * k] * cs[4 + k].y;
+        v[2 * k] = y;
+      }
+    }
+  }
+}
+// Sum over the row's lanes, in each of them (all 32 lanes call).
+__device__ __forceinline__ float row_sum(float x, int per_row, int first) {
+  if ((per_row & (per_row - 1)) == 0) {
+    for (int o = 1; o < per_row; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+  }
+  float s = 0.f;
+  for (int k = 0; k < per_row; ++k) s += __shfl_sync(0xffffffffu, x, first + k);
+  return s;
+}
+
+template <class Tin, class Tout, bool HALF>
+__global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant__ NormParams np) {
+  const RopeParams& p = np.r;
+  const int per_row = p.d / 16, rows = 32 / per_row;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const int rr = lane / per_row;
+  const int64_t n = (int64_t(blockIdx.x) * kWarps + wid) * rows + rr;
+  const bool here = rr < rows && n < p.tokens;
+  const int64_t b = here ? n / p.L : 0;
+  const int l = here ? int(n - b * p.L) : 0;
+  const Pieces s = pieces_of<HALF>(p, lane - rr * per_row);
+  const int h0 = blockIdx.y * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
+  float2 cs[8];
+  if (here && h0 < p.t[0].heads + p.t[1].heads) angles<HALF>(p, s, rope_position(p, b, l), cs);
+  int first = 0;  // heads of the tensors before this one
+#pragma unroll
+  for (int w = 0; w < 3; ++w) {
+    const RopeTensor& x = p.t[w];
+    const int a = max(h0 - first, 0), e = min(h1 - first, x.heads);
+    first += x.heads;
+    const Tin* src = static_cast<const Tin*>(x.in) + b * x.ib + l * x.il;
+    Tout* dst = static_cast<Tout*>(x.out) + b * x.ob + l * x.ol;
+    float wu[8], wv[8];
+    if (w < 2 && a < e) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        wu[k] = weight_at(np, w, s.c0 + k);
+        wv[k] = weight_at(np, w, s.c1 + k);
+      }
+    }
+    constexpr int kBatch = sizeof(Tin) == 2 ? 4 : 2;
+    for (int h = a; h < e; h += kBatch) {
+      Eight<Tin> ru[kBatch], rv[kBatch];
+      float sum[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (here && h + i < e) {
+          ru[i] = load8(src + (h + i) * x.ih + s.c0);
+          rv[i] = load8(src + (h + i) * x.ih + s.c1);
+        } else {
+          ru[i] = rv[i] = Eight<Tin>{};
+        }
+      if (w < 2) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          float u[8], v[8];
+          to_floats(ru[i], u);
+          to_floats(rv[i], v);
+          sum[i] = 0.f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) sum[i] += u[k] * u[k] + v[k] * v[k];
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) sum[i] = row_sum(sum[i], per_row, rr * per_row);
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (!here || h + i >= e) continue;
+        float u[8], v[8];
+        to_floats(ru[i], u);
+        to_floats(rv[i], v);
+        if (w < 2) {
+          const float r = rsqrtf(sum[i] * np.inv_d + np.eps);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            u[k] *= r * wu[k];
+            v[k] *= r * wv[k];
+          }
+          rotate<HALF>(p, s, cs, u, v);
+        }
+        store8(dst + (h + i) * x.oh + s.c0, u);
+        store8(dst + (h + i) * x.oh + s.c1, v);
+      }
+    }
+  }
+}
+
+// Any rot_dim, stride and alignment: a warp has one token, a lane up to two pairs of a head and four
+// elements that are only scaled.
+struct Lane {
+  int c0[2], c1[2], e[4];   // -1: none
+};
+__device__ __forceinline__ Lane lane_elements(const RopeParams& p, bool half, int lane) {
+  Lane s;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = lane + 32 * k, n = p.rot / 2;
+    s.c0[k] = i < n ? (half ? i : 2 * i) : -1;
+    s.c1[k] = half ? i + n : 2 * i + 1;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int e = p.rot + lane + 32 * k;
+    s.e[k] = e < p.d ? e : -1;
+  }
+  return s;
+}
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+// A lane's elements in the order c0[0], c1[0], c0[1], c1[1], e[0..3].
+template <class T>
+__device__ __forceinline__ void load_lane(const T* row, const Lane& s, float (&x)[8]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    x[2 * k] = s.c0[k] >= 0 ? load1(row + s.c0[k]) : 0.f;
+    x[2 * k + 1] = s.c0[k] >= 0 ? load1(row + s.c1[k]) : 0.f;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[4 + k] = s.e[k] >= 0 ? load1(row + s.e[k]) : 0.f;
+}
+template <class T>
+__device__ __forceinline__ void store_lane(T* row, const Lane& s, const float (&x)[8]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (s.c0[k] >= 0) {
+      store1(row + s.c0[k], x[2 * k]);
+      store1(row + s.c1[k], x[2 * k + 1]);
+    }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (s.e[k] >= 0) store1(row + s.e[k], x[4 + k]);
+}
+__device__ __forceinline__ void lane_weights(const NormParams& p, int w, const Lane& s, float (&x)[8]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    x[2 * k] = s.c0[k] >= 0 ? weight_at(p, w, s.c0[k]) : 0.f;
+    x[2 * k + 1] = s.c0[k] >= 0 ? weight_at(p, w, s.c1[k]) : 0.f;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[4 + k] = s.e[k] >= 0 ? weight_at(p, w, s.e[k]) : 0.f;
+}
+__device__ __forceinline__ void lane_angles(const RopeParams& p, int64_t b, int l, int lane, float2 (&cs)[2]) {
+  const double pos = rope_position(p, b, l);
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    cs[k] = lane + 32 * k < p.rot / 2 ? rope_cos_sin(p, pos, lane + 32 * k) : make_float2(1.f, 0.f);
+}
+__device__ __forceinline__ void lane_rotate(const float2 (&cs)[2], float (&x)[8]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const float y = x[2 * k] * cs[k].x - x[2 * k + 1] * cs[k].y;
+    x[2 * k + 1] = x[2 * k + 1] * cs[k].x + x[2 * k] * cs[k].y;
+    x[2 * k] = y;
+  }
+}
+
+template <class Tin, class Tout>
+__global__ void __launch_bounds__(kRopeThreads) norm_any(const __grid_constant__ NormParams np) {
+  const RopeParams& p = np.r;
+  const int lane = threadIdx.x & 31;
+  const int64_t n = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  if (n >= p.tokens) return;
+  const int64_t b = n / p.L;
+  const int l = int(n - b * p.L);
+  const Lane s = lane_elements(p, np.half, lane);
+  const int h0 = blockIdx.y * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
+  float2 cs[2];
+  lane_angles(p, b, l, lane, cs);
+  int first = 0;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) {
+    const RopeTensor& x = p.t[w];
+    const int a = max(h0 - first, 0), e = min(h1 - first, x.heads);
+    first += x.heads;
+    const Tin* src = static_cast<const Tin*>(x.in) + b * x.ib + l * x.il;
+    Tout* dst = static_cast<Tout*>(x.out) + b * x.ob + l * x.ol;
+    float wt[8];
+    if (w < 2 && a < e) lane_weights(np, w, s, wt);
+    for (int h = a; h < e; ++h) {
+      float y[8];
+      load_lane(src + h * x.ih, s, y);
+      if (w < 2) {
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += y[k] * y[k];
+        const float r = rsqrtf(warp_sum(sum) * np.inv_d + np.eps);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] *= r * wt[k];
+        lane_rotate(cs, y);
+      }
+      store_lane(dst + h * x.oh, s, y);
+    }
+  }
+}
+
+// dx of one row's elements and the row's addition to the weights' gradient.  x, g: inputs and rotated-back
+// gradients; w: offset + weights; s1, s2: sums of x^2 and of x g w over the row.
+template <int N>
+__device__ __forceinline__ void norm_grad(float s1, float s2, const NormParams& p, const float (&w)[N],
+                                          const float (&x)[N], float (&g)[N], float (&dw)[N]) {
+  const float r = rsqrtf(s1 * p.inv_d + p.eps);
+  const float k = r * (r * (s2 * p.inv_d));
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    dw[e] += g[e] * (x[e] * r);
+    g[e] = r * (g[e] * w[e] - x[e] * k);
+  }
+}
+
+// One block of every kBwdBlocks-th item (tokens of the block's warps x a group of heads); the sums for the
+// weights stay in registers until the block's end.
+template <class Tx, class Tg, bool HALF>
+__global__ void __launch_bounds__(kRopeThreads) norm_bwd_rows(const __grid_constant__ NormParams np) {
+  __shared__ float s_part[4096];   // [row of the block][2][d]
+  const RopeParams& p = np.r;
+  const int per_row = p.d / 16, rows = 32 / per_row;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const int rr = lane / per_row;
+  const Pieces s = pieces_of<HALF>(p, lane - rr * per_row);
+  float acc_u[2][8], acc_v[2][8];
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc_u[w][k] = acc_v[w][k] = 0.f;
+  for (int64_t item = blockIdx.x; item < np.items; item += gridDim.x) {
+    const int64_t tg = item / np.head_groups;
+    const int hg = int(item - tg * np.head_groups);
+    const int64_t n = (tg * kWarps + wid) * rows + rr;
+    const bool here = rr < rows && n < p.tokens;
+    const int64_t b = here ? n / p.L : 0;
+    const int l = here ? int(n - b * p.L) : 0;
+    const int h0 = hg * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
+    float2 cs[8];
+    if (here && h0 < p.t[0].heads + p.t[1].heads) angles<HALF>(p, s, rope_position(p, b, l), cs);
+    int first = 0;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) {
+      const RopeTensor& y = p.t[w];
+      const int a = max(h0 - first, 0), e = min(h1 - first, y.heads);
+      first += y.heads;
+      const Tg* src = static_cast<const Tg*>(y.in) + b * y.ib + l * y.il;
+      Tx* dst = static_cast<Tx*>(y.out) + b * y.ob + l * y.ol;
+      if (w == 2) {
+        if (here)
+          for (int h = a; h < e; ++h) {
+            float u[8], v[8];
+            to_floats(load8(src + h * y.ih + s.c0), u);
+            to_floats(load8(src + h * y.ih + s.c1), v);
+            store8(dst + h * y.oh + s.c0, u);
+            store8(dst + h * y.oh + s.c1, v);
+          }
+        continue;
+      }
+      if (a >= e) continue;
+      const Tx* xs = static_cast<const Tx*>(np.x[w]) + b * np.xb[w] + l * np.xl[w];
+      float wu[8], wv[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        wu[k] = weight_at(np, w, s.c0 + k);
+        wv[k] = weight_at(np, w, s.c1 + k);
+      }
+      Eight<Tg> gu{}, gv{};
+      Eight<Tx> xu{}, xv{};
+      auto fetch = [&](int h) {
+        if (!here || h >= e) return;
+        gu = load8(src + h * y.ih + s.c0);
+        gv = load8(src + h * y.ih + s.c1);
+        xu = load8(xs + h * np.xh[w] + s.c0);
+        xv = load8(xs + h * np.xh[w] + s.c1);
+      };
+      fetch(a);
+      for (int h = a; h < e; ++h) {
+        float fgu[8], fgv[8], fxu[8], fxv[8];
+        to_floats(gu, fgu);
+        to_floats(gv, fgv);
+        to_floats(xu, fxu);
+        to_floats(xv, fxv);
+        fetch(h + 1);   // (on its way while this row is worked on; no output is another row's input)
+        rotate<HALF>(p, s, cs, fgu, fgv);
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          s1 += fxu[k] * fxu[k] + fxv[k] * fxv[k];
+          s2 += fxu[k] * (fgu[k] * wu[k]) + fxv[k] * (fgv[k] * wv[k]);
+        }
+        s1 = row_sum(s1, per_row, rr * per_row);
+        s2 = row_sum(s2, per_row, rr * per_row);
+        if (!here) continue;
+        norm_grad(s1, s2, np, wu, fxu, fgu, acc_u[w]);
+        norm_grad(s1, s2, np, wv, fxv, fgv, acc_v[w]);
+        store8(dst + h * y.oh + s.c0, fgu);
+        store8(dst + h * y.oh + s.c1, fgv);
+      }
+    }
+  }
+  let_dependents_start();
+  // the block's sums: rows side by side, then added column by column in a fixed order
+  if (rr < rows) {
+    float* row = s_part + (wid * rows + rr) * 2 * p.d;
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        row[w * p.d + s.c0 + k] = acc_u[w][k];
+        row[w * p.d + s.c1 + k] = acc_v[w][k];
+      }
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < 2 * p.d; c += kRopeThreads) {
+    float sum = 0.f;
+    for (int r = 0; r < kWarps * rows; ++r) sum += s_part[r * 2 * p.d + c];
+    np.part[size_t(blockIdx.x) * 2 * p.d + c] = sum;
+  }
+}
+
+template <class Tx, class Tg>
+__global__ void __launch_bounds__(kRopeThreads) norm_bwd_any(const __grid_constant__ NormParams np) {
+  __shared__ float s_part[kWarps][2][128];
+  const RopeParams& p = np.r;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const Lane s = lane_elements(p, np.half, lane);
+  float acc[2][8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) acc[0][k] = acc[1][k] = 0.f;
+  for (int64_t item = blockIdx.x; item < np.items; item += gridDim.x) {
+    const int64_t tg = item / np.head_groups;
+    const int hg = int(item - tg * np.head_groups);
+    const int64_t n = tg * kWarps + wid;
+    if (n >= p.tokens) continue;
+    const int64_t b = n / p.L;
+    const int l = int(n - b * p.L);
+    const int h0 = hg * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
+    float2 cs[2];
+    lane_angles(p, b, l, lane, cs);
+    int first = 0;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) {
+      const RopeTensor& y = p.t[w];
+      const int a = max(h0 - first, 0), e = min(h1 - first, y.heads);
+      first += y.heads;
+      const Tg* src = static_cast<const Tg*>(y.in) + b * y.ib + l * y.il;
+      Tx* dst = static_cast<Tx*>(y.out) + b * y.ob + l * y.ol;
+      float wt[8];
+      if (w < 2 && a < e) lane_weights(np, w, s, wt);
+      for (int h = a; h < e; ++h) {
+        float g[8];
+        load_lane(src + h * y.ih, s, g);
+        if (w < 2) {
+          float x[8];
+          load_lane(static_cast<const Tx*>(np.x[w]) + b * np.xb[w] + l * np.xl[w] + h * np.xh[w], s, x);
+          lane_rotate(cs, g);
+          float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            s1 += x[k] * x[k];
+            s2 += x[k] * (g[k] * wt[k]);
+          }
+          norm_grad(warp_sum(s1), warp_sum(s2), np, wt, x, g, acc[w]);
+        }
+        store_lane(dst + h * y.oh, s, g);
+      }
+    }
+  }
+  let_dependents_start();
+#pragma unroll
+  for (int w = 0; w < 2; ++w) store_lane(s_part[wid][w], s, acc[w]);
+  __syncthreads();
+  for (int c = threadIdx.x; c < 2 * p.d; c += kRopeThreads) {
+    const int w = c / p.d, e = c - w * p.d;
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < kWarps; ++r) sum += s_part[r][w][e];
+    np.part[size_t(blockIdx.x) * 2 * p.d + c] = sum;
+  }
+}
+
+// grid ceil(2 d / 32): adds the blocks' sums, a column to a lane, in a fixed order.
+__global__ void __launch_bounds__(1024) norm_bwd_sum(const __grid_constant__ NormParams np) {
+  __shared__ float s_sum[32][33];
+  wait_for_prior();
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, d = np.r.d;
+  float sum = 0.f;
+  for (int i = wid; i < np.blocks; i += 32) sum += np.part[size_t(i) * 2 * d + c];   // (2 d: a multiple of 32)
+  s_sum[wid][lane] = sum;
+  __syncthreads();
+  if (wid != 0) return;
+  sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) sum += s_sum[i][lane];
+  float* out = np.dw[c / d];
+  if (out) out[c % d] = sum;
+}
+
+sepllm_status check_norm(const sepllm_qknorm_desc* n) {
+  if (!n || (n->w_dtype != 0 && n->w_dtype != 1)) return SEPLLM_INVALID_ARG;
+  if (!finite_positive(n->eps) || !std::isfinite(n->offset)) return SEPLLM_INVALID_ARG;
+  const size_t a = n->w_dtype ? 4 : 2;
+  return aligned(n->wq, a) && aligned(n->wk, a) ? SEPLLM_OK : SEPLLM_INVALID_ARG;
+}
+
+// 16-byte accesses run unless halves end inside a 16-byte piece.
+bool by_rows(const sepllm_rope_desc* d, const RopeParams& p, bool vectors) {
+  return vectors && !(d->layout == SEPLLM_ROPE_HALF && p.rot % 16 != 0);
+}
+
+void fill_norm(const sepllm_rope_desc* d, const sepllm_qknorm_desc* n, NormParams* p) {
+  p->w[0] = n->wq;
+  p->w[1] = n->wk;
+  p->w_dtype = n->w_dtype;
+  p->half = d->layout == SEPLLM_ROPE_HALF;
+  p->eps = n->eps;
+  p->offset = n->offset;
+  p->inv_d = 1.f / float(d->d);
+}
+
+template <class Tin, class Tout>
+void launch_norm(const NormParams& p, bool rows, dim3 grid, cudaStream_t stream) {
+  if (!rows) norm_any<Tin, Tout><<<grid, kRopeThreads, 0, stream>>>(p);
+  else if (p.half) norm_rows<Tin, Tout, true><<<grid, kRopeThreads, 0, stream>>>(p);
+  else norm_rows<Tin, Tout, false><<<grid, kRopeThreads, 0, stream>>>(p);
+}
+template <class Tx, class Tg>
+void launch_norm_bwd(const NormParams& p, bool rows, cudaStream_t stream) {
+  const unsigned grid = unsigned(p.blocks);
+  if (!rows) norm_bwd_any<Tx, Tg><<<grid, kRopeThreads, 0, stream>>>(p);
+  else if (p.half) norm_bwd_rows<Tx, Tg, true><<<grid, kRopeThreads, 0, stream>>>(p);
+  else norm_bwd_rows<Tx, Tg, false><<<grid, kRopeThreads, 0, stream>>>(p);
+}
+
+}  // namespace
+
+}  // namespace sepllm
+
+using namespace sepllm;
+
+extern "C" sepllm_status sepllm_qknorm_rope_fwd(const sepllm_rope_desc* desc, const sepllm_qknorm_desc* norm,
+                                                const int64_t* positions, const sepllm_rope_view* in,
+                                                const sepllm_rope_view* out, void* stream_) {
+  NormParams p{};
+  bool vectors;
+  int dt_in, dt_out;
+  sepllm_status st = rope_params(desc, positions, in, out, 1.f, &p.r, &vectors, &dt_in, &dt_out);
+  if (st != SEPLLM_OK) return st;
+  if ((st = check_norm(norm)) != SEPLLM_OK) return st;
+  fill_norm(desc, norm, &p);
+  const bool rows = by_rows(desc, p.r, vectors);
+  const int64_t per_warp = rows ? 32 / (desc->d / 16) : 1;
+  const int64_t warps = (p.r.tokens + per_warp - 1) / per_warp, blocks = (warps + kWarps - 1) / kWarps;
+  if (blocks > 0x7fffffff) return SEPLLM_UNSUPPORTED;
+  p.r.heads_per_block = rope_heads_per_thread(p.r.n_heads, warps * 32);
+  const int64_t groups = (p.r.n_heads + p.r.heads_per_block - 1) / p.r.heads_per_block;
+  if (groups > 65535) return SEPLLM_UNSUPPORTED;
+  const dim3 grid{unsigned(blocks), unsigned(groups)};
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  if (dt_in == 0 && dt_out == 0) launch_norm<__nv_bfloat16, __nv_bfloat16>(p, rows, grid, stream);
+  else if (dt_in == 0) launch_norm<__nv_bfloat16, float>(p, rows, grid, stream);
+  else if (dt_out == 0) launch_norm<float, __nv_bfloat16>(p, rows, grid, stream);
+  else launch_norm<float, float>(p, rows, grid, stream);
+  SEPLLM_CUDA_TRY(cudaGetLastError());
+  return SEPLLM_OK;
+}
+
+extern "C" sepllm_status sepllm_qknorm_rope_bwd_workspace_bytes(const sepllm_rope_desc* desc, size_t* bytes) {
+  const sepllm_status st = check_rope(desc);
+  if (st != SEPLLM_OK) return st;
+  if (bytes) *bytes = align_up(size_t(kBwdBlocks) * 2 * desc->d * sizeof(float));
+  return SEPLLM_OK;
+}
+
+extern "C" sepllm_status sepllm_qknorm_rope_bwd(const sepllm_rope_desc* desc, const sepllm_qknorm_desc* norm,
+                                                const int64_t* positions, const sepllm_rope_view* x,
+                                                const sepllm_rope_view* in, const sepllm_rope_view* out, float* dwq,
+                                                float* dwk, void* workspace, void* stream_) {
+  NormParams p{};
+  bool vectors;
+  int dt_in, dt_out;
+  sepllm_status st = rope_params(desc, positions, in, out, -1.f, &p.r, &vectors, &dt_in, &dt_out);
+  if (st != SEPLLM_OK) return st;
+  if ((st = check_norm(norm)) != SEPLLM_OK) return st;
+  if (!x || !workspace || !aligned(workspace, kAlign) || !aligned(dwq, 4) || !aligned(dwk, 4)) return SEPLLM_INVALID_ARG;
+  if ((dwq && !norm->wq) || (dwk && !norm->wk)) return SEPLLM_INVALID_ARG;
+  for (int w = 0; w < 2; ++w) {
+    const sepllm_rope_view &a = x[w], &z = out[w];
+    if (!a.data != !z.data) return SEPLLM_INVALID_ARG;
+    if (!a.data) continue;
+    const int heads = w == 0 ? desc->Hq : desc->Hkv;
+    if (a.dtype != dt_out || !aligned(a.data, dt_out ? 4 : 2)) return SEPLLM_INVALID_ARG;
+    if (a.stride_b < 0 || a.stride_h < 0 || a.stride_l < 0) return SEPLLM_INVALID_ARG;
+    p.x[w] = a.data;
+    p.xb[w] = desc->B > 1 ? a.stride_b : 0;
+    p.xh[w] = heads > 1 ? a.stride_h : 0;
+    p.xl[w] = desc->L > 1 ? a.stride_l : 0;
+    const RopeTensor& t = p.r.t[w];
+    if (a.data == z.data && (p.xb[w] != t.ob || p.xh[w] != t.oh || p.xl[w] != t.ol)) return SEPLLM_INVALID_ARG;
+    vectors = vectors && vector_access(a.data, p.xb[w], p.xh[w], p.xl[w]);
+  }
+  fill_norm(desc, norm, &p);
+  p.dw[0] = dwq;
+  p.dw[1] = dwk;
+  p.part = static_cast<float*>(workspace);
+  const bool rows = by_rows(desc, p.r, vectors);
+  const int64_t per_warp = rows ? 32 / (desc->d / 16) : 1;
+  const int64_t warps = (p.r.tokens + per_warp - 1) / per_warp, groups = (warps + kWarps - 1) / kWarps;
+  p.r.heads_per_block = rope_heads_per_thread(p.r.n_heads, warps * 32);
+  p.head_groups = (p.r.n_heads + p.r.heads_per_block - 1) / p.r.heads_per_block;
+  p.items = groups * p.head_groups;
+  p.blocks = int(std::min<int64_t>(p.items, kBwdBlocks));
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  if (dt_out == 0 && dt_in == 0) launch_norm_bwd<__nv_bfloat16, __nv_bfloat16>(p, rows, stream);
+  else if (dt_out == 0) launch_norm_bwd<__nv_bfloat16, float>(p, rows, stream);
+  else if (dt_in == 0) launch_norm_bwd<float, __nv_bfloat16>(p, rows, stream);
+  else launch_norm_bwd<float, float>(p, rows, stream);
+  SEPLLM_CUDA_TRY(cudaGetLastError());
+  if (dwq || dwk)
+    SEPLLM_CUDA_TRY(launch_overlapped(norm_bwd_sum, dim3(2 * desc->d / 32), 1024, 0, stream, p));
+  return SEPLLM_OK;
+}
