@@ -11,7 +11,7 @@
 // codes q + 8, two to a byte (the low half first), are ordered so that the decode kernel's threads find
 // what their matrix operands need in one word: element e of group j stands at place
 // ((e / m) * (d / 32) + j) * m + e % m with m = 8 for keys and m = 4 for values.
-#include <cuda_fp8.h>
+#include <cuda_fp16.h>
 
 #include "cache_common.cuh"
 
@@ -245,9 +245,8 @@ quant_entries(sepllm_cache_header h, const uint8_t* __restrict__ state, QuantRow
 constexpr int kDecThreads = 128, kDecWarps = kDecThreads / 32;
 constexpr int kTile = 32;                        // entries of a warp's tile
 constexpr int kStepRows = kDecWarps * kTile;     // entries of a CTA's step
-constexpr int kStages = 4;
 
-// D[16 keys x 8 heads] = A[16 x 32] B[32 x 8] + C, e4m3 operands.
+// D[16 keys x 8 columns] = A[16 x 32] B[32 x 8] + C, e4m3 operands.
 __device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2],
                                          float c0, float c1, float c2, float c3) {
   asm volatile(
@@ -277,10 +276,17 @@ __device__ __forceinline__ void cp_async_small(uint32_t dst, const void* src, ui
 }
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
-// Place of a tile's V row r in shared memory: a read takes rows 2t + x, t < 4, of which this makes
-// neighbours (and pieces of rows of 64 bytes are turned by bit 1 of it), so that they meet different banks.
-__device__ __forceinline__ int value_row(int r) { return (r & ~7) | (r >> 1 & 3) | (r & 1) << 2; }
+// Two e4m3 numbers, lo in the low byte, and back.
+__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float2 unpack_e4m3(uint32_t w) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(uint16_t(w)));
+  return __half22float2(*reinterpret_cast<__half2*>(&h));
+}
 
 struct QuantDecodeParams {
   sepllm_cache_header h;
@@ -301,6 +307,19 @@ __device__ __forceinline__ int run_of(const sepllm_cache_seq& s) { return s.size
 // Steps of a sequence's kv head; one for an empty sequence, whose output has to be written too.
 __device__ __forceinline__ int steps_of(const sepllm_cache_seq& s) {
   return max(1, (run_of(s) + kStepRows - 1) / kStepRows);
+}
+// Slot of entry v, and the first entry behind v whose slot does not follow its predecessor's.
+__device__ __forceinline__ int contiguous_from(int v, const sepllm_cache_seq& q, const sepllm_cache_desc& d, int* end) {
+  const int i = q.size_init, is = i + q.size_sep;
+  *end = i;
+  if (v < i) return v;
+  const bool sep = v < is;
+  const int x = sep ? q.sep_start + v - i : q.win_start + v - is;    // place in the ring, before the turn
+  const int ring = sep ? d.s : d.c - d.a, first = sep ? d.a : d.a + d.s;
+  *end = sep ? is : 0x7fffffff;
+  if (x >= ring) return first + x - ring;
+  *end = min(*end, v + ring - x);
+  return first + x;
 }
 
 // The CTA's share.  The steps of all (sequence, kv head) units, laid end to end, are cut into equal runs,
@@ -366,40 +385,49 @@ __device__ bool share_of(const sepllm_cache_seq* seq, int B, int Hkv, Share* out
   return true;
 }
 
-// CTAs per SM (three: at most 168 registers a thread).
-template <int D, int NT>
-constexpr int decode_quant_resident() {
-  return D == 128 && NT == 2 ? 2 : 3;
-}
-template <int D, int NT>
-constexpr int decode_quant_smem() {
-  constexpr int ring = kDecWarps * kStages * 2 * kTile * (D / 2 + D / 16);
-  constexpr int merge = kDecWarps * 8 * NT * (D * 4 + 8);
-  return ring > merge ? ring : merge;
-}
+// Shapes of the kernel for groups of up to H query heads per kv head (4, 8 or 16).
+template <int D, int H>
+struct DecodeShape {
+  static constexpr bool kSplit = H == 4;                  // the two parts of q are columns of one product
+  static constexpr int NT = H == 16 ? 2 : 1;              // tiles of 8 columns
+  static constexpr int kGroups = D / kGroup;
+  static constexpr int kCode = D / 2, kStep = D / 16;     // bytes of a row
+  static constexpr int kStageB = 2 * kTile * (kCode + kStep);
+  static constexpr int kResident = D == 128 && H == 16 ? 2 : 3;   // CTAs per SM (three: at most 168 registers a thread)
+  static constexpr int kStages = 4;
+  // shared memory: the warps' rings, in their place the warps' results at a unit's end, and the queries
+  static constexpr int kRingB = kDecWarps * kStages * kStageB;
+  static constexpr int kMergeB = kDecWarps * H * (D * 4 + 8);
+  static constexpr int kUnionB = kRingB > kMergeB ? kRingB : kMergeB;
+  static constexpr int kQWords = kSplit ? kGroups * 2 * 32 : NT * kGroups * 4 * 32;
+  static constexpr int kSmem = kUnionB + kQWords * 4 + H * (kGroups + 1) * 4;
+};
 
 // 4 warps a CTA; each is a flash-decoding worker over its 32-entry tiles of the CTA's steps, which arrive
 // through a ring of cp.async stages.  The products have entries (or elements of V) as the M dimension
-// and the G query heads of the kv head as N = 8 (NT = 2: two tiles of 8).
+// and the G <= H query heads of the kv head as columns.
 //
 // K q: the e4m3 number with bits 0000cccc is cccc * 2^-9 for every code c, so a word of eight codes becomes
 // two operand registers with two masks and a shift.  q is brought near 2^7 by a power of two and split into
 // two e4m3 numbers, which hold its eight bits exactly down to 2^-9 of the head's largest element (and
 // lose 2^-17 of that below); the products are exact and summed in 32 bits.  The codes' offset 8 is taken
 // off by the accumulator's start, -8 times the sum of q over the group, and the key's step multiplies
-// the group's 32-bit sum.
+// the group's 32-bit sum.  Up to four heads: the parts are columns 2h and 2h + 1 of one product.
 //
 // P V: codes become bf16 128 + c with one mask-and-or each (two entries of a word pair to a register).  P
-// times the group's step is rounded to bf16 (2^-9), the only rounding here; the offset 136 is taken off
+// times the group's step is rounded to bf16 (2^-8), the only rounding here; the offset 136 is taken off
 // the sums by a product with ones, which sums those same rounded numbers.
-template <int D, int NT>
-__global__ void __launch_bounds__(kDecThreads, decode_quant_resident<D, NT>())
+template <int D, int H>
+__global__ void __launch_bounds__(kDecThreads, DecodeShape<D, H>::kResident)
 decode_quant(const __grid_constant__ QuantDecodeParams p) {
-  constexpr int kGroups = D / kGroup;
-  constexpr int kCode = D / 2, kStep = D / 16;              // bytes of a row
-  constexpr int kStageB = 2 * kTile * (kCode + kStep);
-  constexpr int GS = 8 * NT;
+  using S = DecodeShape<D, H>;
+  constexpr int kGroups = S::kGroups, kCode = S::kCode, kStep = S::kStep, NT = S::NT, kStages = S::kStages;
+  constexpr bool kSplit = S::kSplit;
+  constexpr int NE = kSplit ? 1 : 2;   // heads of a lane's scores: t, or 8n + 2t and 8n + 2t + 1
   extern __shared__ __align__(128) uint8_t dec_smem[];
+  uint32_t* s_q = reinterpret_cast<uint32_t*>(dec_smem + S::kUnionB);
+  float* s_start = reinterpret_cast<float*>(s_q + S::kQWords);   // [head][group]
+  float* s_factor = s_start + H * kGroups;                        // [head]
   let_dependents_start();
   const sepllm_cache_desc& d = p.h.desc;
   const int G = d.Hq / d.Hkv;
@@ -412,7 +440,7 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
     if (tid == 0) p.ends[blockIdx.x] = make_int4(-1, -1, -1, -1);
     return;
   }
-  uint8_t* ring = dec_smem + wid * (kStages * kStageB);
+  uint8_t* ring = dec_smem + wid * (kStages * S::kStageB);
   const uint32_t ring_u = smem_u32(ring);
   int4 ends = make_int4(-1, -1, -1, -1);
 
@@ -427,25 +455,44 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
     const uint8_t *kc = p.Kc.codes + unit * p.h.slots * kCode, *vc = p.Vc.codes + unit * p.h.slots * kCode;
     const uint8_t *ks = p.Kc.steps + unit * p.h.slots * kStep, *vs = p.Vc.steps + unit * p.h.slots * kStep;
 
-    // this warp's i-th tile into stage i % kStages: codes of K and V, steps of K and V.  Rows behind v1 are
-    // zeros.
+    // This warp's i-th tile into stage i % kStages: codes of K and V, steps of K and V.  Rows behind v1 are
+    // zeros.  The 16-byte pieces of V rows of 64 bytes are turned, so that the threads' reads below meet
+    // different banks.
+    constexpr int kPieces = kCode / 16, kRows = 32 / kPieces;   // of a row; rows of one copy of the warp
     auto issue = [&](int i) {
       const int vb = v0 + (wid + i * kDecWarps) * kTile;
-      const uint32_t sK = ring_u + (i % kStages) * kStageB, sV = sK + kTile * kCode;
+      const uint32_t sK = ring_u + (i % kStages) * S::kStageB, sV = sK + kTile * kCode;
       const uint32_t sks = sV + kTile * kCode, svs = sks + kTile * kStep;
-      const uint32_t ok = vb + lane < v1;
-      const int slot = virtual_to_slot(min(vb + lane, v1 - 1), sq, d);
-      cp_async_small<kStep>(sks + lane * kStep, ks + size_t(slot) * kStep, ok * kStep);
-      cp_async_small<kStep>(svs + lane * kStep, vs + size_t(slot) * kStep, ok * kStep);
-      constexpr int kPieces = kCode / 16, kRows = 32 / kPieces;
+      const int r0 = lane / kPieces, c = lane % kPieces;
+      const uint32_t dk = sK + r0 * kCode + c * 16;
+      auto dst_v = [&](int r) {
+        const int rv = kSplit ? r : (r & ~7) | (r >> 1 & 3) | (r & 1) << 2;
+        return sV + rv * kCode + (kPieces == 4 ? c ^ (rv & 2) : c) * 16;
+      };
+      int end;
+      const int slot0 = contiguous_from(vb, sq, d, &end);
+      if (vb + kTile <= min(end, v1)) {   // 32 neighbouring slots
+        const size_t off = size_t(slot0) * kCode + lane * 16, soff = size_t(slot0 + lane) * kStep;
+        cp_async_small<kStep>(sks + lane * kStep, ks + soff, kStep);
+        cp_async_small<kStep>(svs + lane * kStep, vs + soff, kStep);
 #pragma unroll
-      for (int x = 0; x < kTile / kRows; ++x) {
-        const int r = x * kRows + lane / kPieces, c = lane % kPieces;
-        const size_t off = size_t(__shfl_sync(0xffffffffu, slot, r)) * kCode + c * 16;
-        const uint32_t bytes = vb + r < v1 ? 16u : 0u;
-        cp_async16(sK + r * kCode + c * 16, kc + off, bytes);
-        const int rv = value_row(r), cv = kPieces == 4 ? c ^ (rv & 2) : c;
-        cp_async16(sV + rv * kCode + cv * 16, vc + off, bytes);
+        for (int x = 0; x < kTile / kRows; ++x) {
+          cp_async16(dk + x * kRows * kCode, kc + off + x * kRows * kCode, 16);
+          cp_async16(dst_v(x * kRows + r0), vc + off + x * kRows * kCode, 16);
+        }
+      } else {
+        const uint32_t ok = vb + lane < v1;
+        const int slot = virtual_to_slot(min(vb + lane, v1 - 1), sq, d);
+        cp_async_small<kStep>(sks + lane * kStep, ks + size_t(slot) * kStep, ok * kStep);
+        cp_async_small<kStep>(svs + lane * kStep, vs + size_t(slot) * kStep, ok * kStep);
+#pragma unroll
+        for (int x = 0; x < kTile / kRows; ++x) {
+          const int r = x * kRows + r0;
+          const size_t off = size_t(__shfl_sync(0xffffffffu, slot, r)) * kCode + c * 16;
+          const uint32_t bytes = vb + r < v1 ? 16u : 0u;
+          cp_async16(dk + x * kRows * kCode, kc + off, bytes);
+          cp_async16(dst_v(r), vc + off, bytes);
+        }
       }
     };
 #pragma unroll
@@ -454,67 +501,95 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       cp_async_commit();
     }
 
-    // q of head 8n + g as operand registers, elements 32j + 8t ..; sums over the group and factors of the
-    // heads that this lane's accumulators belong to, 8n + 2t and 8n + 2t + 1
-    uint32_t q_hi[NT][kGroups][2], q_lo[NT][kGroups][2];
-    float start[NT][kGroups][2], factor[NT][2];
+    // The queries as operand words, one thread to eight elements 32j + 8t .. of a head.
+    constexpr int kPer = D / 8;   // threads of a head
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int head = 8 * n + g;
-      const uint4* row = reinterpret_cast<const uint4*>(
-          p.q + (size_t(sh.b) * d.Hq + sh.hk * G + min(head, G - 1)) * D) + t;
-      uint4 raw[kGroups];
+    for (int c0 = 0; c0 < H * kPer; c0 += kDecThreads) {
+      const int c = c0 + tid, head = c / kPer, j = c % kPer / 4;
+      if (H * kPer < kDecThreads && c >= H * kPer) break;   // (whole warps)
+      const uint4 raw = head < G ? __ldg(reinterpret_cast<const uint4*>(
+                                             p.q + (size_t(sh.b) * d.Hq + sh.hk * G + head) * D) + c % kPer)
+                                 : make_uint4(0, 0, 0, 0);
+      const __nv_bfloat162* x = reinterpret_cast<const __nv_bfloat162*>(&raw);
+      float2 f[4];
       float most = 0.f;
 #pragma unroll
-      for (int j = 0; j < kGroups; ++j) {
-        raw[j] = head < G ? __ldg(row + j * 4) : make_uint4(0, 0, 0, 0);
-        const __nv_bfloat162* x = reinterpret_cast<const __nv_bfloat162*>(&raw[j]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float2 f = __bfloat1622float2(x[k]);
-          most = fmaxf(most, fmaxf(fabsf(f.x), fabsf(f.y)));
-        }
+      for (int k = 0; k < 4; ++k) {
+        f[k] = __bfloat1622float2(x[k]);
+        most = fmaxf(most, fmaxf(fabsf(f[k].x), fabsf(f[k].y)));
       }
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+#pragma unroll
+      for (int o = 1; o < kPer; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
       // 2^e with most * 2^e in [128, 256) (2^e and its inverse stay normal numbers)
       const int e = max(-110, min(110, 134 - int(__float_as_uint(most) >> 23)));
       const float up = __uint_as_float(uint32_t(127 + e) << 23);
-      const float back = p.scale_log2 * __uint_as_float(uint32_t(127 + 9 - e) << 23);
+      float sum = 0.f;
+      uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        f[k].x *= up;
+        f[k].y *= up;
+        // (an infinite element, or one beyond 2^118, becomes NaN)
+        if (!(fabsf(f[k].x) < 448.f)) f[k].x = __int_as_float(0x7fc00000);
+        if (!(fabsf(f[k].y) < 448.f)) f[k].y = __int_as_float(0x7fc00000);
+        const uint32_t a = pack_e4m3(f[k].x, f[k].y);
+        const float2 fa = unpack_e4m3(a);
+        const uint32_t b = pack_e4m3(f[k].x - fa.x, f[k].y - fa.y);
+        const float2 fb = unpack_e4m3(b);
+        sum += (fa.x + fb.x) + (fa.y + fb.y);
+        hi[0] |= (a & 255) << (8 * k);
+        hi[1] |= (a >> 8) << (8 * k);
+        lo[0] |= (b & 255) << (8 * k);
+        lo[1] |= (b >> 8) << (8 * k);
+      }
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      const int tt = c % 4;
+      if (kSplit) {
+        // column 2 head (+ 1): [group][register][lane]
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          s_q[(j * 2 + r) * 32 + head * 8 + tt] = hi[r];
+          s_q[(j * 2 + r) * 32 + head * 8 + 4 + tt] = lo[r];
+        }
+      } else {
+        const int n = head / 8;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          s_q[((n * kGroups + j) * 4 + r) * 32 + (head % 8) * 4 + tt] = hi[r];
+          s_q[((n * kGroups + j) * 4 + 2 + r) * 32 + (head % 8) * 4 + tt] = lo[r];
+        }
+      }
+      if (tt == 0) s_start[head * kGroups + j] = sum * (-8.f * 0x1p-9f);
+      if (c % kPer == 0) s_factor[head] = p.scale_log2 * __uint_as_float(uint32_t(127 + 9 - e) << 23);
+    }
+    __syncthreads();
+    uint32_t q_hi[NT][kGroups][2], q_lo[NT][kGroups][2];   // (kSplit: q_hi alone)
+    float start[NT][kGroups][NE], factor[NT][NE];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int j = 0; j < kGroups; ++j) {
-        const __nv_bfloat162* x = reinterpret_cast<const __nv_bfloat162*>(&raw[j]);
-        uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
-        float sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float2 f = __bfloat1622float2(x[k]);
-#pragma unroll
-          for (int odd = 0; odd < 2; ++odd) {
-            const float y = (odd ? f.y : f.x) * up;
-            // (an infinite element, or one beyond 2^118, becomes NaN)
-            const __nv_fp8_e4m3 a(fabsf(y) < 448.f ? y : __int_as_float(0x7fc00000));
-            const __nv_fp8_e4m3 c(y - float(a));
-            sum += float(a) + float(c);
-            hi[odd] |= uint32_t(a.__x) << (8 * k);
-            lo[odd] |= uint32_t(c.__x) << (8 * k);
+        for (int r = 0; r < 2; ++r) {
+          if (kSplit) {
+            q_hi[n][j][r] = s_q[(j * 2 + r) * 32 + lane];
+          } else {
+            q_hi[n][j][r] = s_q[((n * kGroups + j) * 4 + r) * 32 + lane];
+            q_lo[n][j][r] = s_q[((n * kGroups + j) * 4 + 2 + r) * 32 + lane];
           }
         }
-        q_hi[n][j][0] = hi[0];
-        q_hi[n][j][1] = hi[1];
-        q_lo[n][j][0] = lo[0];
-        q_lo[n][j][1] = lo[1];
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        start[n][j][0] = __shfl_sync(0xffffffffu, sum, 8 * t) * (-8.f * 0x1p-9f);
-        start[n][j][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4) * (-8.f * 0x1p-9f);
+#pragma unroll
+        for (int e = 0; e < NE; ++e) start[n][j][e] = s_start[(kSplit ? t : 8 * n + 2 * t + e) * kGroups + j];
       }
-      factor[n][0] = __shfl_sync(0xffffffffu, back, 8 * t);
-      factor[n][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
+#pragma unroll
+      for (int e = 0; e < NE; ++e) factor[n][e] = s_factor[kSplit ? t : 8 * n + 2 * t + e];
     }
 
+    // Sums: rows are elements of V, columns 2t and 2t + 1 the heads 8n + 2t and 8n + 2t + 1 (kSplit: columns 4 to
+    // 7 repeat 0 to 3).  m_ref: reference exponent, -inf before the first score; m_use: 0 in its place.
     float oacc[2 * kGroups][NT][4], ones[kGroups][NT][4];
-    float m_ref[NT][2], l_sum[NT][2];
+    float m_ref[NT][NE], m_use[NT][NE], l_sum[NT][NE];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -525,8 +600,11 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       for (int j = 0; j < kGroups; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) ones[j][n][e] = 0.f;
-      m_ref[n][0] = m_ref[n][1] = -INFINITY;
-      l_sum[n][0] = l_sum[n][1] = 0.f;
+#pragma unroll
+      for (int e = 0; e < NE; ++e) {
+        m_ref[n][e] = -INFINITY;
+        m_use[n][e] = l_sum[n][e] = 0.f;
+      }
     }
 
     for (int i = 0; i < my_n; ++i) {
@@ -534,23 +612,23 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       __syncwarp();
       if (i + kStages - 1 < my_n) issue(i + kStages - 1);
       cp_async_commit();
-      const uint8_t* sK = ring + (i % kStages) * kStageB;
+      const uint8_t* sK = ring + (i % kStages) * S::kStageB;
       const uint8_t* sV = sK + kTile * kCode;
       const uint8_t* sks = sV + kTile * kCode;
       const uint8_t* svs = sks + kTile * kStep;
       const int vb = v0 + (wid + i * kDecWarps) * kTile;
 
-      // scores in log2 units: entries 16x + g (+ 8), heads 8n + 2t (+ 1)
-      float sc[2][NT][4];
+      // scores in log2 units: entries 16x + 8y + g, [2x + y]
+      float sc[4][NT][NE];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        uint32_t w[2][kGroups], st[2][(kGroups + 1) / 2];
+        uint32_t w[2][kGroups], st[2][kGroups / 2];
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const int r = 16 * x + 8 * y + g;
           const uint32_t* src = reinterpret_cast<const uint32_t*>(sK + r * kCode) + t * kGroups;
           const uint32_t* ssrc = reinterpret_cast<const uint32_t*>(sks + r * kStep);
-          if (kGroups == 4) {
+          if constexpr (kGroups == 4) {
             *reinterpret_cast<uint4*>(w[y]) = *reinterpret_cast<const uint4*>(src);
             *reinterpret_cast<uint2*>(st[y]) = *reinterpret_cast<const uint2*>(ssrc);
           } else {
@@ -558,10 +636,6 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
             st[y][0] = *ssrc;
           }
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[x][n][e] = 0.f;
 #pragma unroll
         for (int j = 0; j < kGroups; ++j) {
           const uint32_t a[4] = {w[0][j] & 0x0f0f0f0fu, w[1][j] & 0x0f0f0f0fu, w[0][j] >> 4 & 0x0f0f0f0fu,
@@ -571,70 +645,92 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             float c[4];
-            mma_e4m3(c, a, q_hi[n][j], start[n][j][0], start[n][j][1], start[n][j][0], start[n][j][1]);
-            mma_e4m3(c, a, q_lo[n][j], c[0], c[1], c[2], c[3]);
-            sc[x][n][0] += c[0] * s0;
-            sc[x][n][1] += c[1] * s0;
-            sc[x][n][2] += c[2] * s1;
-            sc[x][n][3] += c[3] * s1;
+            if constexpr (kSplit) {
+              mma_e4m3(c, a, q_hi[n][j], start[n][j][0], 0.f, start[n][j][0], 0.f);
+              c[0] += c[1];
+              c[1] = c[2] + c[3];
+              sc[2 * x][n][0] = j == 0 ? c[0] * s0 : sc[2 * x][n][0] + c[0] * s0;
+              sc[2 * x + 1][n][0] = j == 0 ? c[1] * s1 : sc[2 * x + 1][n][0] + c[1] * s1;
+            } else {
+              mma_e4m3(c, a, q_hi[n][j], start[n][j][0], start[n][j][NE - 1], start[n][j][0], start[n][j][NE - 1]);
+              mma_e4m3(c, a, q_lo[n][j], c[0], c[1], c[2], c[3]);
+#pragma unroll
+              for (int e = 0; e < NE; ++e) {
+                sc[2 * x][n][e] = j == 0 ? c[e] * s0 : sc[2 * x][n][e] + c[e] * s0;
+                sc[2 * x + 1][n][e] = j == 0 ? c[2 + e] * s1 : sc[2 * x + 1][n][e] + c[2 + e] * s1;
+              }
+            }
           }
         }
       }
       bool above = false;   // a score beyond 2^8 of the reference: it moves up
+      float top[NT][NE];
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int e = 0; e < NE; ++e) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            sc[x][n][e] *= factor[n][e & 1];
-            if (vb + kTile > v1 && vb + 16 * x + 8 * (e >> 1) + g >= v1) sc[x][n][e] = -INFINITY;
-            above |= sc[x][n][e] > m_ref[n][e & 1] + 8.f;
+          for (int y = 0; y < 4; ++y) sc[y][n][e] *= factor[n][e];
+          if (vb + kTile > v1) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              if (vb + 8 * y + g >= v1) sc[y][n][e] = -INFINITY;
           }
+          top[n][e] = fmaxf(fmaxf(sc[0][n][e], sc[1][n][e]), fmaxf(sc[2][n][e], sc[3][n][e]));
+          above |= top[n][e] > m_ref[n][e] + 8.f;
+        }
       if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+          float corr[2];   // of the columns 2t and 2t + 1
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float mx = fmaxf(fmaxf(sc[0][n][e], sc[0][n][e + 2]), fmaxf(sc[1][n][e], sc[1][n][e + 2]));
+          for (int e = 0; e < NE; ++e) {
+            float mx = top[n][e];
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            corr[e] = 1.f;
             if (mx > m_ref[n][e] + 8.f) {
-              const float corr = m_ref[n][e] == -INFINITY ? 0.f : ex2(m_ref[n][e] - mx);
-              m_ref[n][e] = mx;
-              l_sum[n][e] *= corr;
-#pragma unroll
-              for (int j = 0; j < 2 * kGroups; ++j) {
-                oacc[j][n][e] *= corr;
-                oacc[j][n][e + 2] *= corr;
-              }
-#pragma unroll
-              for (int j = 0; j < kGroups; ++j) ones[j][n][e] *= corr;
+              corr[e] = m_ref[n][e] == -INFINITY ? 0.f : ex2(m_ref[n][e] - mx);
+              m_ref[n][e] = m_use[n][e] = mx;
+              l_sum[n][e] *= corr[e];
             }
           }
+          if (kSplit) {
+            const float mine = corr[0];
+            corr[0] = __shfl_sync(0xffffffffu, mine, 2 * t & 3);
+            corr[1] = __shfl_sync(0xffffffffu, mine, (2 * t + 1) & 3);
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int j = 0; j < 2 * kGroups; ++j) {
+              oacc[j][n][e] *= corr[e];
+              oacc[j][n][e + 2] *= corr[e];
+            }
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j) ones[j][n][e] *= corr[e];
+          }
+        }
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float m = m_ref[n][e] == -INFINITY ? 0.f : m_ref[n][e];
+        for (int e = 0; e < NE; ++e) {
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            sc[x][n][e] = ex2(sc[x][n][e] - m);
-            sc[x][n][e + 2] = ex2(sc[x][n][e + 2] - m);
-            l_sum[n][e] += sc[x][n][e] + sc[x][n][e + 2];
-          }
+          for (int y = 0; y < 4; ++y) sc[y][n][e] = ex2(sc[y][n][e] - m_use[n][e]);
+          l_sum[n][e] += (sc[0][n][e] + sc[1][n][e]) + (sc[2][n][e] + sc[3][n][e]);
         }
 
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        // entries 2t, 2t + 1, 2t + 8, 2t + 9 of the half tile (see issue() for their places)
-        uint32_t w[4][(kGroups + 1) / 2], st[2][(kGroups + 1) / 2];
+        // The four entries of the half tile that a lane's operand registers hold: two of a[0], a[1] and two of
+        // a[2], a[3].  kSplit: t and t + 8, t + 4 and t + 12; else 2t and 2t + 1, 2t + 8 and 2t + 9.
+        uint32_t w[4][kGroups / 2], st[2][kGroups / 2];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-          const int r = 16 * x + 2 * t + (y & 1) + 8 * (y >> 1);
-          const int rv = value_row(r);
-          if (kGroups == 4) {
+          const int r = 16 * x + (kSplit ? t + 8 * (y & 1) + 4 * (y >> 1) : 2 * t + (y & 1) + 8 * (y >> 1));
+          const int rv = kSplit ? r : (r & ~7) | (r >> 1 & 3) | (r & 1) << 2;
+          if constexpr (kGroups == 4) {
             const int piece = (g >> 1) ^ (rv & 2);
             *reinterpret_cast<uint2*>(w[y]) =
                 *reinterpret_cast<const uint2*>(sV + rv * kCode + piece * 16 + (g & 1) * 8);
@@ -645,7 +741,7 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const uint32_t* ssrc = reinterpret_cast<const uint32_t*>(svs + (16 * x + 8 * y + g) * kStep);
-          if (kGroups == 4) *reinterpret_cast<uint2*>(st[y]) = *reinterpret_cast<const uint2*>(ssrc);
+          if constexpr (kGroups == 4) *reinterpret_cast<uint2*>(st[y]) = *reinterpret_cast<const uint2*>(ssrc);
           else st[y][0] = *ssrc;
         }
 #pragma unroll
@@ -655,8 +751,15 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
           uint32_t pb[NT][2];
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            pb[n][0] = transpose8(pack_bf16(sc[x][n][0] * s0, sc[x][n][1] * s0));
-            pb[n][1] = transpose8(pack_bf16(sc[x][n][2] * s1, sc[x][n][3] * s1));
+            if constexpr (kSplit) {
+              // column g is head g % 4; its entries t and t + 8 are with the lane of row t and head g % 4
+              const uint32_t u = pack_bf16(sc[2 * x][n][0] * s0, sc[2 * x + 1][n][0] * s1);
+              pb[n][0] = __shfl_sync(0xffffffffu, u, 4 * t + (g & 3));
+              pb[n][1] = __shfl_sync(0xffffffffu, u, 4 * t + 16 + (g & 3));
+            } else {
+              pb[n][0] = transpose8(pack_bf16(sc[2 * x][n][0] * s0, sc[2 * x][n][NE - 1] * s0));
+              pb[n][1] = transpose8(pack_bf16(sc[2 * x + 1][n][0] * s1, sc[2 * x + 1][n][NE - 1] * s1));
+            }
           }
           const uint32_t u = __byte_perm(w[0][j / 2], w[1][j / 2], j & 1 ? 0x7632 : 0x5410);
           const uint32_t z = __byte_perm(w[2][j / 2], w[3][j / 2], j & 1 ? 0x7632 : 0x5410);
@@ -680,29 +783,32 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < NE; ++e)
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l_sum[n][e] += __shfl_xor_sync(0xffffffffu, l_sum[n][e], o);
     __syncthreads();  // all warps are out of their rings
 
     // the warps' results, head by head, then merged: the unit's output, or a part of it
     float2* sm_ml = reinterpret_cast<float2*>(dec_smem);
-    float* sm_acc = reinterpret_cast<float*>(dec_smem + kDecWarps * GS * sizeof(float2));
+    float* sm_acc = reinterpret_cast<float*>(dec_smem + kDecWarps * H * sizeof(float2));
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < NE; ++e)
+        if (g == 0) sm_ml[wid * H + (kSplit ? t : 8 * n + 2 * t + e)] = make_float2(m_ref[n][e], l_sum[n][e]);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int head = 8 * n + 2 * t + e;
         if (head < G) {
-          if (g == 0) sm_ml[wid * GS + head] = make_float2(m_ref[n][e], l_sum[n][e]);
 #pragma unroll
           for (int j = 0; j < 2 * kGroups; ++j) {
             const float off = 136.f * ones[j / 2][n][e];
-            *reinterpret_cast<float2*>(sm_acc + (wid * GS + head) * D + (j / 2) * kGroup + 4 * g + 2 * (j & 1)) =
+            *reinterpret_cast<float2*>(sm_acc + (wid * H + head) * D + (j / 2) * kGroup + 4 * g + 2 * (j & 1)) =
                 make_float2(oacc[j][n][e] - off, oacc[j][n][e + 2] - off);
           }
         }
       }
+    }
     __syncthreads();
     const bool head_cut = sh.step > 0, tail_cut = sh.step + n_steps < steps;
     const size_t part = 2 * size_t(blockIdx.x) + (head_cut ? 0 : 1);
@@ -710,15 +816,15 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       const int hd = idx / D, e = idx % D;
       float mm = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) mm = fmaxf(mm, sm_ml[w * GS + hd].x);
+      for (int w = 0; w < kDecWarps; ++w) mm = fmaxf(mm, sm_ml[w * H + hd].x);
       float ll = 0.f, aa = 0.f;
 #pragma unroll
       for (int w = 0; w < kDecWarps; ++w) {
-        const float2 ml = sm_ml[w * GS + hd];
+        const float2 ml = sm_ml[w * H + hd];
         if (ml.y == 0.f) continue;   // a warp without entries (a NaN goes through)
         const float f = ml.x == -INFINITY ? 1.f : ex2(ml.x - mm);
         ll += ml.y * f;
-        aa += sm_acc[(w * GS + hd) * D + e] * f;
+        aa += sm_acc[(w * H + hd) * D + e] * f;
       }
       if (head_cut || tail_cut) {
         p.part_acc[(part * G + hd) * D + e] = aa;
@@ -771,12 +877,22 @@ __global__ void __launch_bounds__(D) decode_quant_join(const __grid_constant__ Q
   if (p.lse && e == 0) p.lse[row] = ll != 0.f ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
 }
 
+// f(D, H) for the kernel that serves a descriptor, as integral constants.
+template <class F>
+auto with_shape(const sepllm_cache_desc& d, F f) {
+  const int G = d.Hq / d.Hkv;
+  auto heads = [&](auto D) {
+    if (G <= 4) return f(D, std::integral_constant<int, 4>{});
+    if (G <= 8) return f(D, std::integral_constant<int, 8>{});
+    return f(D, std::integral_constant<int, 16>{});
+  };
+  return d.d == 128 ? heads(std::integral_constant<int, 128>{}) : heads(std::integral_constant<int, 64>{});
+}
+
 // CTAs of a decode: as many as are resident, or one per step of the fullest caches.
 int decode_quant_ctas(const sepllm_cache_desc& d) {
   const int64_t steps = (int64_t(d.c) + kStepRows - 1) / kStepRows;
-  const bool wide = d.Hq / d.Hkv > 8;
-  const int resident = d.d == 128 ? (wide ? decode_quant_resident<128, 2>() : decode_quant_resident<128, 1>())
-                                  : (wide ? decode_quant_resident<64, 2>() : decode_quant_resident<64, 1>());
+  const int resident = with_shape(d, [](auto D, auto H) { return DecodeShape<D(), H()>::kResident; });
   return int(std::min<int64_t>(resident * kSmCount, int64_t(d.B) * d.Hkv * steps));
 }
 
@@ -792,12 +908,12 @@ QuantDecodeLayout decode_quant_layout(const sepllm_cache_desc& d) {
   return l;
 }
 
-template <int D, int NT>
+template <int D, int H>
 sepllm_status launch_decode_quant(const QuantDecodeParams& p, cudaStream_t stream) {
-  constexpr int smem = decode_quant_smem<D, NT>();
+  constexpr int smem = DecodeShape<D, H>::kSmem;
   const unsigned ctas = unsigned(decode_quant_ctas(p.h.desc));
-  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(decode_quant<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  decode_quant<D, NT><<<ctas, kDecThreads, smem, stream>>>(p);
+  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(decode_quant<D, H>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  decode_quant<D, H><<<ctas, kDecThreads, smem, stream>>>(p);
   SEPLLM_CUDA_TRY(cudaGetLastError());
   const dim3 grid(ctas, p.h.desc.Hq / p.h.desc.Hkv);
   SEPLLM_CUDA_TRY(launch_overlapped(decode_quant_join<D>, grid, D, 0, stream, p));
@@ -926,7 +1042,5 @@ extern "C" sepllm_status sepllm_decode_quant(const sepllm_cache_desc* desc, floa
   p.part_acc = reinterpret_cast<float*>(ws + l.off_acc);
   p.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  const bool wide = desc->Hq / desc->Hkv > 8;
-  if (desc->d == 128) return wide ? launch_decode_quant<128, 2>(p, stream) : launch_decode_quant<128, 1>(p, stream);
-  return wide ? launch_decode_quant<64, 2>(p, stream) : launch_decode_quant<64, 1>(p, stream);
+  return with_shape(*desc, [&](auto D, auto H) { return launch_decode_quant<D(), H()>(p, stream); });
 }
