@@ -249,7 +249,7 @@ constexpr int kStepRows = kDecWarps * kTile;     // entries of a CTA's step
 // D[16 keys x 8 columns] = A[16 x 32] B[32 x 8] + C, e4m3 operands.
 __device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2],
                                          float c0, float c1, float c2, float c3) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
       "{%8, %9}, {%10, %11, %12, %13};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
@@ -257,7 +257,7 @@ __device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], 
 }
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                          uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
       "{%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -266,13 +266,20 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
 // Transposes an 8 x 8 matrix of 16-bit elements held two to a lane.
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 template <int BYTES>
 __device__ __forceinline__ void cp_async_small(uint32_t dst, const void* src, uint32_t src_bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(src_bytes)
                : "memory");
+}
+// (w & mask) | bits in one instruction (of the two constants one may be part of it: `bits` is a register).
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w), "n"(MASK), "r"(bits));
+  return r;
 }
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -440,6 +447,8 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
     if (tid == 0) p.ends[blockIdx.x] = make_int4(-1, -1, -1, -1);
     return;
   }
+  uint32_t k128;   // two bf16 numbers 128 (not a constant to the compiler, which would split and_or())
+  asm volatile("mov.b32 %0, 0x43004300;" : "=r"(k128));
   uint8_t* ring = dec_smem + wid * (kStages * S::kStageB);
   const uint32_t ring_u = smem_u32(ring);
   int4 ends = make_int4(-1, -1, -1, -1);
@@ -459,42 +468,45 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
     // zeros.  The 16-byte pieces of V rows of 64 bytes are turned, so that the threads' reads below meet
     // different banks.
     constexpr int kPieces = kCode / 16, kRows = 32 / kPieces;   // of a row; rows of one copy of the warp
+    const int r0 = lane / kPieces, c0 = lane % kPieces;
+    auto dst_v = [&](int r) {   // place of this lane's piece of V row r in a stage
+      const int rv = kSplit ? r : (r & ~7) | (r >> 1 & 3) | (r & 1) << 2;
+      return kTile * kCode + rv * kCode + (kPieces == 4 ? c0 ^ (rv & 2) : c0) * 16;
+    };
+    const uint8_t *kc_l = kc + r0 * kCode + c0 * 16, *vc_l = vc + r0 * kCode + c0 * 16;
+    const uint8_t *ks_l = ks + lane * kStep, *vs_l = vs + lane * kStep;
+    const uint32_t dst0 = ring_u + r0 * kCode + c0 * 16, dst1 = ring_u + dst_v(r0);
+    const uint32_t dst2 = ring_u + 2 * kTile * kCode + lane * kStep;
+    int run_end = 0, run_slot = 0;   // entries up to run_end have slots run_slot + entry
     auto issue = [&](int i) {
       const int vb = v0 + (wid + i * kDecWarps) * kTile;
-      const uint32_t sK = ring_u + (i % kStages) * S::kStageB, sV = sK + kTile * kCode;
-      const uint32_t sks = sV + kTile * kCode, svs = sks + kTile * kStep;
-      const int r0 = lane / kPieces, c = lane % kPieces;
-      const uint32_t dk = sK + r0 * kCode + c * 16;
-      auto dst_v = [&](int r) {
-        const int rv = kSplit ? r : (r & ~7) | (r >> 1 & 3) | (r & 1) << 2;
-        return sV + rv * kCode + (kPieces == 4 ? c ^ (rv & 2) : c) * 16;
-      };
-      int end;
-      const int slot0 = contiguous_from(vb, sq, d, &end);
-      if (vb + kTile <= min(end, v1)) {   // 32 neighbouring slots
-        const size_t off = size_t(slot0) * kCode + lane * 16, soff = size_t(slot0 + lane) * kStep;
-        cp_async_small<kStep>(sks + lane * kStep, ks + soff, kStep);
-        cp_async_small<kStep>(svs + lane * kStep, vs + soff, kStep);
+      const uint32_t stage = (i % kStages) * S::kStageB;
+      if (vb >= run_end) run_slot = contiguous_from(vb, sq, d, &run_end) - vb;
+      if (vb + kTile <= min(run_end, v1)) {   // 32 neighbouring slots
+        const uint32_t slot = run_slot + vb;
+        cp_async_small<kStep>(stage + dst2, ks_l + uint64_t(slot) * kStep, kStep);
+        cp_async_small<kStep>(stage + dst2 + kTile * kStep, vs_l + uint64_t(slot) * kStep, kStep);
 #pragma unroll
         for (int x = 0; x < kTile / kRows; ++x) {
-          cp_async16(dk + x * kRows * kCode, kc + off + x * kRows * kCode, 16);
-          cp_async16(dst_v(x * kRows + r0), vc + off + x * kRows * kCode, 16);
+          cp_async16(stage + dst0 + x * kRows * kCode, kc_l + uint64_t(slot) * kCode + x * kRows * kCode, 16);
+          cp_async16(stage + dst1 + x * kRows * kCode, vc_l + uint64_t(slot) * kCode + x * kRows * kCode, 16);
         }
       } else {
         const uint32_t ok = vb + lane < v1;
         const int slot = virtual_to_slot(min(vb + lane, v1 - 1), sq, d);
-        cp_async_small<kStep>(sks + lane * kStep, ks + size_t(slot) * kStep, ok * kStep);
-        cp_async_small<kStep>(svs + lane * kStep, vs + size_t(slot) * kStep, ok * kStep);
+        cp_async_small<kStep>(stage + dst2, ks + size_t(slot) * kStep, ok * kStep);
+        cp_async_small<kStep>(stage + dst2 + kTile * kStep, vs + size_t(slot) * kStep, ok * kStep);
 #pragma unroll
         for (int x = 0; x < kTile / kRows; ++x) {
           const int r = x * kRows + r0;
-          const size_t off = size_t(__shfl_sync(0xffffffffu, slot, r)) * kCode + c * 16;
+          const size_t off = size_t(__shfl_sync(0xffffffffu, slot, r)) * kCode + c0 * 16;
           const uint32_t bytes = vb + r < v1 ? 16u : 0u;
-          cp_async16(dk + x * kRows * kCode, kc + off, bytes);
-          cp_async16(dst_v(r), vc + off, bytes);
+          cp_async16(stage + dst0 + x * kRows * kCode, kc + off, bytes);
+          cp_async16(stage + dst1 + x * kRows * kCode, vc + off, bytes);
         }
       }
     };
+    static_assert(kRows % 8 == 0, "a lane's places in the rows of a stage differ by whole copies");
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) {
       if (s < my_n) issue(s);
@@ -504,8 +516,8 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
     // The queries as operand words, one thread to eight elements 32j + 8t .. of a head.
     constexpr int kPer = D / 8;   // threads of a head
 #pragma unroll
-    for (int c0 = 0; c0 < H * kPer; c0 += kDecThreads) {
-      const int c = c0 + tid, head = c / kPer, j = c % kPer / 4;
+    for (int c1 = 0; c1 < H * kPer; c1 += kDecThreads) {
+      const int c = c1 + tid, head = c / kPer, j = c % kPer / 4;
       if (H * kPer < kDecThreads && c >= H * kPer) break;   // (whole warps)
       const uint4 raw = head < G ? __ldg(reinterpret_cast<const uint4*>(
                                              p.q + (size_t(sh.b) * d.Hq + sh.hk * G + head) * D) + c % kPer)
@@ -765,10 +777,8 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
           const uint32_t z = __byte_perm(w[2][j / 2], w[3][j / 2], j & 1 ? 0x7632 : 0x5410);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const uint32_t a0 = (u >> (8 * half) & 0x000f000fu) | 0x43004300u;
-            const uint32_t a1 = (u >> (8 * half + 4) & 0x000f000fu) | 0x43004300u;
-            const uint32_t a2 = (z >> (8 * half) & 0x000f000fu) | 0x43004300u;
-            const uint32_t a3 = (z >> (8 * half + 4) & 0x000f000fu) | 0x43004300u;
+            const uint32_t a0 = and_or<0x000f000fu>(u >> (8 * half), k128), a1 = and_or<0x000f000fu>(u >> (8 * half + 4), k128);
+            const uint32_t a2 = and_or<0x000f000fu>(z >> (8 * half), k128), a3 = and_or<0x000f000fu>(z >> (8 * half + 4), k128);
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma_bf16(oacc[2 * j + half][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
           }
