@@ -336,13 +336,18 @@ struct Share {
   int b, hk, step;   // where the run starts
   int64_t left;      // its steps
 };
+// (32-bit divisions wherever the numbers allow)
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint32_t b) {
+  return a >> 32 ? a / b : uint32_t(a) / b;
+}
 __device__ bool share_of(const sepllm_cache_seq* seq, int B, int Hkv, Share* out) {
   __shared__ int64_t s_sum[kDecWarps];
   __shared__ int64_t s_first;
-  __shared__ int s_b;
+  __shared__ int s_b, s_n;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  int64_t sum = 0;
-  for (int b = tid; b < B; b += kDecThreads) sum += steps_of(seq[b]);
+  const int n0 = tid < B ? steps_of(seq[tid]) : 0;   // of the first sequences, one to a thread
+  int64_t sum = n0;
+  for (int b = tid + kDecThreads; b < B; b += kDecThreads) sum += steps_of(seq[b]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) s_sum[wid] = sum;
@@ -351,14 +356,14 @@ __device__ bool share_of(const sepllm_cache_seq* seq, int B, int Hkv, Share* out
 #pragma unroll
   for (int w = 0; w < kDecWarps; ++w) total += s_sum[w];
   total *= Hkv;
-  const int64_t ctas = min(int64_t(gridDim.x), total);
+  const uint32_t ctas = uint32_t(min(int64_t(gridDim.x), total));
   if (blockIdx.x >= ctas) return false;
-  const int64_t first = total * blockIdx.x / ctas, last = total * (blockIdx.x + 1) / ctas;
-  const int64_t target = first / Hkv;   // in steps of one kv head
-  int64_t before = 0;                   // steps of the sequences before this chunk
+  const int64_t first = quotient(total * blockIdx.x, ctas), last = quotient(total * (blockIdx.x + 1), ctas);
+  const int64_t target = quotient(first, Hkv);   // in steps of one kv head
+  int64_t before = 0;                            // steps of the sequences before this chunk
   for (int b0 = 0; b0 < B; b0 += kDecThreads) {
     const int b = b0 + tid;
-    const int n = b < B ? steps_of(seq[b]) : 0;
+    const int n = b0 == 0 ? n0 : b < B ? steps_of(seq[b]) : 0;
     int64_t incl = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -378,15 +383,16 @@ __device__ bool share_of(const sepllm_cache_seq* seq, int B, int Hkv, Share* out
     before += chunk;
     if (n > 0 && incl - n <= target && target < incl) {
       s_b = b;
+      s_n = n;
       s_first = incl - n;
     }
     if (target < before) break;   // (the same for all threads)
   }
   __syncthreads();
   out->b = s_b;
-  const int n = steps_of(seq[s_b]);
+  const int n = s_n;
   const int64_t in_seq = first - s_first * Hkv;
-  out->hk = int(in_seq / n);
+  out->hk = int(quotient(in_seq, n));
   out->step = int(in_seq - int64_t(out->hk) * n);
   out->left = last - first;
   return true;
@@ -400,7 +406,7 @@ struct DecodeShape {
   static constexpr int kGroups = D / kGroup;
   static constexpr int kCode = D / 2, kStep = D / 16;     // bytes of a row
   static constexpr int kStageB = 2 * kTile * (kCode + kStep);
-  static constexpr int kResident = D == 128 && H == 16 ? 2 : 3;   // CTAs per SM (three: at most 168 registers a thread)
+  static constexpr int kResident = D == 128 && H == 16 ? 2 : H == 4 ? 3 : 3;   // CTAs per SM (three: at most 168 registers a thread)
   static constexpr int kStages = 4;
   // shared memory: the warps' rings, in their place the warps' results at a unit's end, and the queries
   static constexpr int kRingB = kDecWarps * kStages * kStageB;
@@ -464,6 +470,18 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
     const uint8_t *kc = p.Kc.codes + unit * p.h.slots * kCode, *vc = p.Vc.codes + unit * p.h.slots * kCode;
     const uint8_t *ks = p.Kc.steps + unit * p.h.slots * kStep, *vs = p.Vc.steps + unit * p.h.slots * kStep;
 
+    // the queries, on their way while the first copies are issued: one thread to eight elements of a head
+    constexpr int kPer = D / 8;                                          // threads of a head
+    constexpr int kQLoads = (H * kPer + kDecThreads - 1) / kDecThreads;
+    uint4 q_raw[kQLoads];
+#pragma unroll
+    for (int x = 0; x < kQLoads; ++x) {
+      const int c = x * kDecThreads + tid, head = c / kPer;
+      q_raw[x] = head < G ? __ldg(reinterpret_cast<const uint4*>(
+                                      p.q + (size_t(sh.b) * d.Hq + sh.hk * G + head) * D) + c % kPer)
+                          : make_uint4(0, 0, 0, 0);
+    }
+
     // This warp's i-th tile into stage i % kStages: codes of K and V, steps of K and V.  Rows behind v1 are
     // zeros.  The 16-byte pieces of V rows of 64 bytes are turned, so that the threads' reads below meet
     // different banks.
@@ -513,15 +531,12 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       cp_async_commit();
     }
 
-    // The queries as operand words, one thread to eight elements 32j + 8t .. of a head.
-    constexpr int kPer = D / 8;   // threads of a head
+    // The queries as operand words: elements 32j + 8t ..
 #pragma unroll
-    for (int c1 = 0; c1 < H * kPer; c1 += kDecThreads) {
-      const int c = c1 + tid, head = c / kPer, j = c % kPer / 4;
+    for (int x0 = 0; x0 < kQLoads; ++x0) {
+      const int c = x0 * kDecThreads + tid, head = c / kPer, j = c % kPer / 4;
       if (H * kPer < kDecThreads && c >= H * kPer) break;   // (whole warps)
-      const uint4 raw = head < G ? __ldg(reinterpret_cast<const uint4*>(
-                                             p.q + (size_t(sh.b) * d.Hq + sh.hk * G + head) * D) + c % kPer)
-                                 : make_uint4(0, 0, 0, 0);
+      const uint4 raw = q_raw[x0];
       const __nv_bfloat162* x = reinterpret_cast<const __nv_bfloat162*>(&raw);
       float2 f[4];
       float most = 0.f;
@@ -619,19 +634,10 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       }
     }
 
-    for (int i = 0; i < my_n; ++i) {
-      cp_async_wait<kStages - 2>();
-      __syncwarp();
-      if (i + kStages - 1 < my_n) issue(i + kStages - 1);
-      cp_async_commit();
+    // Scores of the warp's i-th tile: of entries 16x + 8y + g, [2x + y].
+    auto scores = [&](int i, float (&sc)[4][NT][NE]) {
       const uint8_t* sK = ring + (i % kStages) * S::kStageB;
-      const uint8_t* sV = sK + kTile * kCode;
-      const uint8_t* sks = sV + kTile * kCode;
-      const uint8_t* svs = sks + kTile * kStep;
-      const int vb = v0 + (wid + i * kDecWarps) * kTile;
-
-      // scores in log2 units: entries 16x + 8y + g, [2x + y]
-      float sc[4][NT][NE];
+      const uint8_t* sks = sK + 2 * kTile * kCode;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         uint32_t w[2][kGroups], st[2][kGroups / 2];
@@ -675,7 +681,11 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
           }
         }
       }
-      bool above = false;   // a score beyond 2^8 of the reference: it moves up
+    };
+    // Scores to weights, in log2 units; the reference moves up when a score is beyond 2^8 of it.
+    auto softmax = [&](int i, float (&sc)[4][NT][NE]) {
+      const int vb = v0 + (wid + i * kDecWarps) * kTile;
+      bool above = false;
       float top[NT][NE];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -733,6 +743,11 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
           l_sum[n][e] += (sc[0][n][e] + sc[1][n][e]) + (sc[2][n][e] + sc[3][n][e]);
         }
 
+    };
+    // The tile's weights times its values.
+    auto values = [&](int i, const float (&sc)[4][NT][NE]) {
+      const uint8_t* sV = ring + (i % kStages) * S::kStageB + kTile * kCode;
+      const uint8_t* svs = sV + kTile * kCode + kTile * kStep;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         // The four entries of the half tile that a lane's operand registers hold: two of a[0], a[1] and two of
@@ -787,8 +802,35 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
           for (int n = 0; n < NT; ++n) mma_bf16(ones[j][n], 0x3f803f80u, 0u, 0x3f803f80u, 0u, pb[n][0], pb[n][1]);
         }
       }
-      __syncwarp();  // every lane is done with this stage before a later copy overwrites it
+    };
+
+    // One tile's values are multiplied while the next one's scores are: two chains of matrix products and
+    // unpacking that do not wait for each other.
+    float sc[4][NT][NE];
+    if (my_n > 0) {
+      cp_async_wait<kStages - 2>();
+      __syncwarp();
+      scores(0, sc);
+      softmax(0, sc);
     }
+    for (int i = 0; i + 1 < my_n; ++i) {
+      if (i + kStages - 1 < my_n) issue(i + kStages - 1);   // (over tile i - 1, which all lanes are done with)
+      cp_async_commit();
+      cp_async_wait<kStages - 2>();
+      __syncwarp();
+      float next[4][NT][NE];
+      scores(i + 1, next);
+      values(i, sc);
+      softmax(i + 1, next);
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < NE; ++e) sc[y][n][e] = next[y][n][e];
+      __syncwarp();
+    }
+    if (my_n > 0) values(my_n - 1, sc);
     cp_async_wait<0>();
 #pragma unroll
     for (int n = 0; n < NT; ++n)

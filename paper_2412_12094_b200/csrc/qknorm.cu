@@ -11,7 +11,8 @@ namespace sepllm {
 namespace {
 
 constexpr int kWarps = kRopeThreads / 32;
-constexpr int kBwdBlocks = 3 * kSmCount;   // of the gradient, each with a share of the rows and a sum of its own
+constexpr int kBwdResident = 3;
+constexpr int kBwdBlocks = kBwdResident * kSmCount;   // of the gradient, each with a share of the rows and sums of its own
 
 struct NormParams {
   RopeParams r;
@@ -19,12 +20,12 @@ struct NormParams {
   int w_dtype, half;
   float eps, offset, inv_d;
   // gradient: the forward's inputs, the blocks' sums [block][2][d] and their total
-  const void* x[2];
-  int64_t xb[2], xh[2], xl[2];
+  const void* x[3];          // (V: null, not read)
+  int64_t xb[3], xh[3], xl[3];
   float* part;
   float* dw[2];
-  int64_t items;             // (group of tokens, group of heads)
-  int head_groups, blocks;
+  int64_t items[3];          // of each tensor: (tokens of a block's warps, group of heads)
+  int heads_per_item[3], head_groups[3], blocks;
 };
 
 __device__ __forceinline__ float weight_at(const NormParams& p, int w, int e) {
@@ -117,54 +118,46 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant_
   float2 cs[8];
   if (here && h0 < p.t[0].heads + p.t[1].heads) angles<HALF>(p, s, rope_position(p, b, l), cs);
   int first = 0;  // heads of the tensors before this one
-#pragma unroll
+#pragma unroll 1
   for (int w = 0; w < 3; ++w) {
     const RopeTensor& x = p.t[w];
     const int a = max(h0 - first, 0), e = min(h1 - first, x.heads);
     first += x.heads;
+    if (a >= e) continue;
     const Tin* src = static_cast<const Tin*>(x.in) + b * x.ib + l * x.il;
     Tout* dst = static_cast<Tout*>(x.out) + b * x.ob + l * x.ol;
     float wu[8], wv[8];
-    if (w < 2 && a < e) {
+    if (w < 2) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         wu[k] = weight_at(np, w, s.c0 + k);
         wv[k] = weight_at(np, w, s.c1 + k);
       }
     }
-    constexpr int kBatch = sizeof(Tin) == 2 ? 4 : 2;
-    for (int h = a; h < e; h += kBatch) {
-      Eight<Tin> ru[kBatch], rv[kBatch];
-      float sum[kBatch];
+    // rows of the next heads are on their way while one is worked on (an output may be its own input, but
+    // is no other head's)
+    constexpr int kDepth = sizeof(Tin) == 2 ? 4 : 2;
+    Eight<Tin> ru[kDepth]{}, rv[kDepth]{};
+    auto fetch = [&](int i, int h) {
+      if (!here || h >= e) return;
+      ru[i] = load8(src + h * x.ih + s.c0);
+      rv[i] = load8(src + h * x.ih + s.c1);
+    };
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i)
-        if (here && h + i < e) {
-          ru[i] = load8(src + (h + i) * x.ih + s.c0);
-          rv[i] = load8(src + (h + i) * x.ih + s.c1);
-        } else {
-          ru[i] = rv[i] = Eight<Tin>{};
-        }
-      if (w < 2) {
+    for (int i = 0; i < kDepth; ++i) fetch(i, a + i);
+    for (int h = a; h < e; h += kDepth) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          float u[8], v[8];
-          to_floats(ru[i], u);
-          to_floats(rv[i], v);
-          sum[i] = 0.f;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) sum[i] += u[k] * u[k] + v[k] * v[k];
-        }
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) sum[i] = row_sum(sum[i], per_row, rr * per_row);
-      }
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        if (!here || h + i >= e) continue;
+      for (int i = 0; i < kDepth; ++i) {
+        if (h + i >= e) break;
         float u[8], v[8];
         to_floats(ru[i], u);
         to_floats(rv[i], v);
+        fetch(i, h + i + kDepth);
         if (w < 2) {
-          const float r = rsqrtf(sum[i] * np.inv_d + np.eps);
+          float sum = 0.f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) sum += u[k] * u[k] + v[k] * v[k];
+          const float r = rsqrtf(row_sum(sum, per_row, rr * per_row) * np.inv_d + np.eps);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             u[k] *= r * wu[k];
@@ -172,6 +165,7 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant_
           }
           rotate<HALF>(p, s, cs, u, v);
         }
+        if (!here) continue;
         store8(dst + (h + i) * x.oh + s.c0, u);
         store8(dst + (h + i) * x.oh + s.c1, v);
       }
@@ -304,147 +298,140 @@ __device__ __forceinline__ void norm_grad(float s1, float s2, const NormParams& 
   }
 }
 
-// One block of every kBwdBlocks-th item (tokens of the block's warps x a group of heads); the sums for the
-// weights stay in registers until the block's end.
+// The tensors one after the other, so that the sums for one tensor's weights are all that stays in
+// registers; of each the block takes every gridDim.x-th item (tokens of its warps x a group of heads).
 template <class Tx, class Tg, bool HALF>
-__global__ void __launch_bounds__(kRopeThreads) norm_bwd_rows(const __grid_constant__ NormParams np) {
-  __shared__ float s_part[4096];   // [row of the block][2][d]
+__global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(const __grid_constant__ NormParams np) {
+  __shared__ float s_part[2048];   // [row of the block][d]
+  __shared__ __align__(16) float s_w[128];
   const RopeParams& p = np.r;
   const int per_row = p.d / 16, rows = 32 / per_row;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int rr = lane / per_row;
   const Pieces s = pieces_of<HALF>(p, lane - rr * per_row);
-  float acc_u[2][8], acc_v[2][8];
+#pragma unroll 1
+  for (int w = 0; w < 3; ++w) {
+    const RopeTensor& y = p.t[w];
+    const int hpi = np.heads_per_item[w], groups = np.head_groups[w];
+    float acc_u[8], acc_v[8];
 #pragma unroll
-  for (int w = 0; w < 2; ++w)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) acc_u[w][k] = acc_v[w][k] = 0.f;
-  for (int64_t item = blockIdx.x; item < np.items; item += gridDim.x) {
-    const int64_t tg = item / np.head_groups;
-    const int hg = int(item - tg * np.head_groups);
-    const int64_t n = (tg * kWarps + wid) * rows + rr;
-    const bool here = rr < rows && n < p.tokens;
-    const int64_t b = here ? n / p.L : 0;
-    const int l = here ? int(n - b * p.L) : 0;
-    const int h0 = hg * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
-    float2 cs[8];
-    if (here && h0 < p.t[0].heads + p.t[1].heads) angles<HALF>(p, s, rope_position(p, b, l), cs);
-    int first = 0;
-#pragma unroll
-    for (int w = 0; w < 3; ++w) {
-      const RopeTensor& y = p.t[w];
-      const int a = max(h0 - first, 0), e = min(h1 - first, y.heads);
-      first += y.heads;
+    for (int k = 0; k < 8; ++k) acc_u[k] = acc_v[k] = 0.f;
+    if (w < 2) {
+      for (int e = threadIdx.x; e < p.d; e += kRopeThreads) s_w[e] = weight_at(np, w, e);
+      __syncthreads();
+    }
+    for (int64_t item = blockIdx.x; item < np.items[w]; item += gridDim.x) {
+      const int64_t tg = item / groups;
+      const int a = int(item - tg * groups) * hpi, e = min(y.heads, a + hpi);
+      const int64_t n = (tg * kWarps + wid) * rows + rr;
+      const bool here = rr < rows && n < p.tokens;
+      const int64_t b = here ? n / p.L : 0;
+      const int l = here ? int(n - b * p.L) : 0;
       const Tg* src = static_cast<const Tg*>(y.in) + b * y.ib + l * y.il;
-      Tx* dst = static_cast<Tx*>(y.out) + b * y.ob + l * y.ol;
-      if (w == 2) {
-        if (here)
-          for (int h = a; h < e; ++h) {
-            float u[8], v[8];
-            to_floats(load8(src + h * y.ih + s.c0), u);
-            to_floats(load8(src + h * y.ih + s.c1), v);
-            store8(dst + h * y.oh + s.c0, u);
-            store8(dst + h * y.oh + s.c1, v);
-          }
-        continue;
-      }
-      if (a >= e) continue;
       const Tx* xs = static_cast<const Tx*>(np.x[w]) + b * np.xb[w] + l * np.xl[w];
-      float wu[8], wv[8];
+      Tx* dst = static_cast<Tx*>(y.out) + b * y.ob + l * y.ol;
+      // rows of the next heads are on their way while one is worked on (no output is another row's input)
+      constexpr int kDepth = sizeof(Tx) + sizeof(Tg) == 4 ? 3 : 2;
+      Eight<Tg> gu[kDepth]{}, gv[kDepth]{};
+      Eight<Tx> xu[kDepth]{}, xv[kDepth]{};
+      auto fetch = [&](int i, int h) {
+        if (!here || h >= e) return;
+        gu[i] = load8(src + h * y.ih + s.c0);
+        gv[i] = load8(src + h * y.ih + s.c1);
+        if (w == 2) return;
+        xu[i] = load8(xs + h * np.xh[w] + s.c0);
+        xv[i] = load8(xs + h * np.xh[w] + s.c1);
+      };
+#pragma unroll
+      for (int i = 0; i < kDepth; ++i) fetch(i, a + i);
+      float2 cs[8];
+      if (w < 2) angles<HALF>(p, s, here ? rope_position(p, b, l) : 0.0, cs);   // (rows not here add zeros below)
+      for (int h = a; h < e; h += kDepth) {
+#pragma unroll
+        for (int i = 0; i < kDepth; ++i) {
+          if (h + i >= e) break;
+          float fgu[8], fgv[8], fxu[8], fxv[8];
+          to_floats(gu[i], fgu);
+          to_floats(gv[i], fgv);
+          to_floats(xu[i], fxu);
+          to_floats(xv[i], fxv);
+          fetch(i, h + i + kDepth);
+          if (w < 2) {
+            rotate<HALF>(p, s, cs, fgu, fgv);
+            float s1 = 0.f, s2 = 0.f, wu[8], wv[8];   // (the weights stay in shared memory: 16 registers less)
+            to_floats(load8(s_w + s.c0), wu);
+            to_floats(load8(s_w + s.c1), wv);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              s1 += fxu[k] * fxu[k] + fxv[k] * fxv[k];
+              s2 += fxu[k] * (fgu[k] * wu[k]) + fxv[k] * (fgv[k] * wv[k]);
+            }
+            s1 = row_sum(s1, per_row, rr * per_row);
+            s2 = row_sum(s2, per_row, rr * per_row);
+            norm_grad(s1, s2, np, wu, fxu, fgu, acc_u);
+            norm_grad(s1, s2, np, wv, fxv, fgv, acc_v);
+          }
+          if (!here) continue;
+          store8(dst + (h + i) * y.oh + s.c0, fgu);
+          store8(dst + (h + i) * y.oh + s.c1, fgv);
+        }
+      }
+    }
+    if (w == 2) break;
+    // the block's sums: rows side by side, then added column by column in a fixed order (a row that is not
+    // here has added zeros)
+    __syncthreads();
+    if (rr < rows) {
+      float* row = s_part + (wid * rows + rr) * p.d;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        wu[k] = weight_at(np, w, s.c0 + k);
-        wv[k] = weight_at(np, w, s.c1 + k);
+        row[s.c0 + k] = acc_u[k];
+        row[s.c1 + k] = acc_v[k];
       }
-      Eight<Tg> gu{}, gv{};
-      Eight<Tx> xu{}, xv{};
-      auto fetch = [&](int h) {
-        if (!here || h >= e) return;
-        gu = load8(src + h * y.ih + s.c0);
-        gv = load8(src + h * y.ih + s.c1);
-        xu = load8(xs + h * np.xh[w] + s.c0);
-        xv = load8(xs + h * np.xh[w] + s.c1);
-      };
-      fetch(a);
-      for (int h = a; h < e; ++h) {
-        float fgu[8], fgv[8], fxu[8], fxv[8];
-        to_floats(gu, fgu);
-        to_floats(gv, fgv);
-        to_floats(xu, fxu);
-        to_floats(xv, fxv);
-        fetch(h + 1);   // (on its way while this row is worked on; no output is another row's input)
-        rotate<HALF>(p, s, cs, fgu, fgv);
-        float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          s1 += fxu[k] * fxu[k] + fxv[k] * fxv[k];
-          s2 += fxu[k] * (fgu[k] * wu[k]) + fxv[k] * (fgv[k] * wv[k]);
-        }
-        s1 = row_sum(s1, per_row, rr * per_row);
-        s2 = row_sum(s2, per_row, rr * per_row);
-        if (!here) continue;
-        norm_grad(s1, s2, np, wu, fxu, fgu, acc_u[w]);
-        norm_grad(s1, s2, np, wv, fxv, fgv, acc_v[w]);
-        store8(dst + h * y.oh + s.c0, fgu);
-        store8(dst + h * y.oh + s.c1, fgv);
-      }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.d; c += kRopeThreads) {
+      float sum = 0.f;
+      for (int r = 0; r < kWarps * rows; ++r) sum += s_part[r * p.d + c];
+      np.part[(size_t(blockIdx.x) * 2 + w) * p.d + c] = sum;
     }
   }
   let_dependents_start();
-  // the block's sums: rows side by side, then added column by column in a fixed order
-  if (rr < rows) {
-    float* row = s_part + (wid * rows + rr) * 2 * p.d;
-#pragma unroll
-    for (int w = 0; w < 2; ++w)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        row[w * p.d + s.c0 + k] = acc_u[w][k];
-        row[w * p.d + s.c1 + k] = acc_v[w][k];
-      }
-  }
-  __syncthreads();
-  for (int c = threadIdx.x; c < 2 * p.d; c += kRopeThreads) {
-    float sum = 0.f;
-    for (int r = 0; r < kWarps * rows; ++r) sum += s_part[r * 2 * p.d + c];
-    np.part[size_t(blockIdx.x) * 2 * p.d + c] = sum;
-  }
 }
 
 template <class Tx, class Tg>
 __global__ void __launch_bounds__(kRopeThreads) norm_bwd_any(const __grid_constant__ NormParams np) {
-  __shared__ float s_part[kWarps][2][128];
+  __shared__ float s_part[kWarps][128];
   const RopeParams& p = np.r;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const Lane s = lane_elements(p, np.half, lane);
-  float acc[2][8];
+#pragma unroll 1
+  for (int w = 0; w < 3; ++w) {
+    const RopeTensor& y = p.t[w];
+    const int hpi = np.heads_per_item[w], groups = np.head_groups[w];
+    float wt[8], acc[8];
+    if (w < 2) lane_weights(np, w, s, wt);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) acc[0][k] = acc[1][k] = 0.f;
-  for (int64_t item = blockIdx.x; item < np.items; item += gridDim.x) {
-    const int64_t tg = item / np.head_groups;
-    const int hg = int(item - tg * np.head_groups);
-    const int64_t n = tg * kWarps + wid;
-    if (n >= p.tokens) continue;
-    const int64_t b = n / p.L;
-    const int l = int(n - b * p.L);
-    const int h0 = hg * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
-    float2 cs[2];
-    lane_angles(p, b, l, lane, cs);
-    int first = 0;
-#pragma unroll
-    for (int w = 0; w < 3; ++w) {
-      const RopeTensor& y = p.t[w];
-      const int a = max(h0 - first, 0), e = min(h1 - first, y.heads);
-      first += y.heads;
+    for (int k = 0; k < 8; ++k) acc[k] = 0.f;
+    for (int64_t item = blockIdx.x; item < np.items[w]; item += gridDim.x) {
+      const int64_t tg = item / groups;
+      const int a = int(item - tg * groups) * hpi, e = min(y.heads, a + hpi);
+      const int64_t n = tg * kWarps + wid;
+      if (n >= p.tokens) continue;
+      const int64_t b = n / p.L;
+      const int l = int(n - b * p.L);
       const Tg* src = static_cast<const Tg*>(y.in) + b * y.ib + l * y.il;
+      const Tx* xs = static_cast<const Tx*>(np.x[w]) + b * np.xb[w] + l * np.xl[w];
       Tx* dst = static_cast<Tx*>(y.out) + b * y.ob + l * y.ol;
-      float wt[8];
-      if (w < 2 && a < e) lane_weights(np, w, s, wt);
+      float2 cs[2];
+      if (w < 2) lane_angles(p, b, l, lane, cs);
+#pragma unroll 2
       for (int h = a; h < e; ++h) {
         float g[8];
         load_lane(src + h * y.ih, s, g);
         if (w < 2) {
           float x[8];
-          load_lane(static_cast<const Tx*>(np.x[w]) + b * np.xb[w] + l * np.xl[w] + h * np.xh[w], s, x);
+          load_lane(xs + h * np.xh[w], s, x);
           lane_rotate(cs, g);
           float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -452,23 +439,23 @@ __global__ void __launch_bounds__(kRopeThreads) norm_bwd_any(const __grid_consta
             s1 += x[k] * x[k];
             s2 += x[k] * (g[k] * wt[k]);
           }
-          norm_grad(warp_sum(s1), warp_sum(s2), np, wt, x, g, acc[w]);
+          norm_grad(warp_sum(s1), warp_sum(s2), np, wt, x, g, acc);
         }
         store_lane(dst + h * y.oh, s, g);
       }
     }
+    if (w == 2) break;
+    __syncthreads();
+    store_lane(s_part[wid], s, acc);
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.d; c += kRopeThreads) {
+      float sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < kWarps; ++r) sum += s_part[r][c];
+      np.part[(size_t(blockIdx.x) * 2 + w) * p.d + c] = sum;
+    }
   }
   let_dependents_start();
-#pragma unroll
-  for (int w = 0; w < 2; ++w) store_lane(s_part[wid][w], s, acc[w]);
-  __syncthreads();
-  for (int c = threadIdx.x; c < 2 * p.d; c += kRopeThreads) {
-    const int w = c / p.d, e = c - w * p.d;
-    float sum = 0.f;
-#pragma unroll
-    for (int r = 0; r < kWarps; ++r) sum += s_part[r][w][e];
-    np.part[size_t(blockIdx.x) * 2 * p.d + c] = sum;
-  }
 }
 
 // grid ceil(2 d / 32): adds the blocks' sums, a column to a lane, in a fixed order.
@@ -598,10 +585,15 @@ extern "C" sepllm_status sepllm_qknorm_rope_bwd(const sepllm_rope_desc* desc, co
   const bool rows = by_rows(desc, p.r, vectors);
   const int64_t per_warp = rows ? 32 / (desc->d / 16) : 1;
   const int64_t warps = (p.r.tokens + per_warp - 1) / per_warp, groups = (warps + kWarps - 1) / kWarps;
-  p.r.heads_per_block = rope_heads_per_thread(p.r.n_heads, warps * 32);
-  p.head_groups = (p.r.n_heads + p.r.heads_per_block - 1) / p.r.heads_per_block;
-  p.items = groups * p.head_groups;
-  p.blocks = int(std::min<int64_t>(p.items, kBwdBlocks));
+  int64_t most = 1;
+  for (int w = 0; w < 3; ++w) {
+    const int heads = p.r.t[w].heads;   // (0: left out)
+    p.heads_per_item[w] = heads ? rope_heads_per_thread(heads, warps * 32) : 1;
+    p.head_groups[w] = std::max(1, (heads + p.heads_per_item[w] - 1) / p.heads_per_item[w]);
+    p.items[w] = heads ? groups * p.head_groups[w] : 0;
+    most = std::max(most, p.items[w]);
+  }
+  p.blocks = int(std::min<int64_t>(most, kBwdBlocks));
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   if (dt_out == 0 && dt_in == 0) launch_norm_bwd<__nv_bfloat16, __nv_bfloat16>(p, rows, stream);
   else if (dt_out == 0) launch_norm_bwd<__nv_bfloat16, float>(p, rows, stream);
