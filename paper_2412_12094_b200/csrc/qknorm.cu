@@ -56,39 +56,103 @@ __device__ __forceinline__ Pieces pieces_of(const RopeParams& p, int t) {
   }
   return s;
 }
+// Two neighbouring elements in one register pair: Blackwell's packed fp32 arithmetic does both in one
+// instruction (the gradient is bound by its instructions as much as by its loads).
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair_of(float lo, float hi) {
+  Pair r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 floats_of(Pair x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float sum2(Pair x) {
+  const float2 f = floats_of(x);
+  return f.x + f.y;
+}
+template <class T>
+__device__ __forceinline__ void to_pairs(const Eight<T>& r, Pair (&x)[4]) {
+  float f[8];
+  to_floats(r, f);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = pair_of(f[2 * k], f[2 * k + 1]);
+}
+template <class T>
+__device__ __forceinline__ void store_pairs(T* s, const Pair (&x)[4]) {
+  float f[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 y = floats_of(x[k]);
+    f[2 * k] = y.x;
+    f[2 * k + 1] = y.y;
+  }
+  store8(s, f);
+}
+
+// Angles of the thread's pairs.  HALF: elements k of its pieces are a pair, so cosines, sines and
+// their negatives stand in pairs as the elements do; else pair k is two neighbours, and (cos, sin).
 template <bool HALF>
-__device__ __forceinline__ void angles(const RopeParams& p, const Pieces& s, double pos, float2 (&cs)[8]) {
+struct Turn {
+  Pair c[4], s[4], n[4];
+};
+template <>
+struct Turn<false> {
+  float2 cs[8];
+};
+template <bool HALF>
+__device__ __forceinline__ void angles(const RopeParams& p, const Pieces& s, double pos, Turn<HALF>& t) {
+  float2 cs[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int i = HALF ? s.c0 + k : (k < 4 ? s.c0 / 2 + k : s.c1 / 2 + k - 4);
     cs[k] = s.turn && 2 * i < p.rot ? rope_cos_sin(p, pos, i) : make_float2(1.f, 0.f);
   }
-}
-// (where nothing turns cs is (1, 0), but the products with 0 would spread a NaN)
-template <bool HALF>
-__device__ __forceinline__ void rotate(const RopeParams& p, const Pieces& s, const float2 (&cs)[8], float (&u)[8],
-                                       float (&v)[8]) {
-  if (HALF) {
-    if (!s.turn) return;
+  if constexpr (HALF) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float y = u[k] * cs[k].x - v[k] * cs[k].y;
-      v[k] = v[k] * cs[k].x + u[k] * cs[k].y;
-      u[k] = y;
+    for (int k = 0; k < 4; ++k) {
+      t.c[k] = pair_of(cs[2 * k].x, cs[2 * k + 1].x);
+      t.s[k] = pair_of(cs[2 * k].y, cs[2 * k + 1].y);
+      t.n[k] = pair_of(-cs[2 * k].y, -cs[2 * k + 1].y);
     }
   } else {
 #pragma unroll
+    for (int k = 0; k < 8; ++k) t.cs[k] = cs[k];
+  }
+}
+// (where nothing turns the angle is 0, but the products with 0 would spread a NaN)
+template <bool HALF>
+__device__ __forceinline__ void rotate(const RopeParams& p, const Pieces& s, const Turn<HALF>& t, Pair (&u)[4],
+                                       Pair (&v)[4]) {
+  if constexpr (HALF) {
+    if (!s.turn) return;
+#pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if (s.c0 + 2 * k < p.rot) {
-        const float y = u[2 * k] * cs[k].x - u[2 * k + 1] * cs[k].y;
-        u[2 * k + 1] = u[2 * k + 1] * cs[k].x + u[2 * k] * cs[k].y;
-        u[2 * k] = y;
-      }
-      if (s.c1 + 2 * k < p.rot) {
-        const float y = v[2 * k] * cs[4 + k].x - v[2 * k + 1] * cs[4 + k].y;
-        v[2 * k + 1] = v[2 * k + 1] * cs[4 + k].x + v[2 * k] * cs[4 + k].y;
-        v[2 * k] = y;
-      }
+      const Pair y = fma2(v[k], t.n[k], mul2(u[k], t.c[k]));
+      v[k] = fma2(u[k], t.s[k], mul2(v[k], t.c[k]));
+      u[k] = y;
+    }
+  } else {
+    auto turn = [](Pair x, float2 cs) {
+      const float2 f = floats_of(x);
+      return pair_of(f.x * cs.x - f.y * cs.y, f.y * cs.x + f.x * cs.y);
+    };
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (s.c0 + 2 * k < p.rot) u[k] = turn(u[k], t.cs[k]);
+      if (s.c1 + 2 * k < p.rot) v[k] = turn(v[k], t.cs[4 + k]);
     }
   }
 }
@@ -115,8 +179,8 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant_
   const int l = here ? int(n - b * p.L) : 0;
   const Pieces s = pieces_of<HALF>(p, lane - rr * per_row);
   const int h0 = blockIdx.y * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
-  float2 cs[8];
-  if (here && h0 < p.t[0].heads + p.t[1].heads) angles<HALF>(p, s, rope_position(p, b, l), cs);
+  Turn<HALF> turn;
+  if (here && h0 < p.t[0].heads + p.t[1].heads) angles<HALF>(p, s, rope_position(p, b, l), turn);
   int first = 0;  // heads of the tensors before this one
 #pragma unroll 1
   for (int w = 0; w < 3; ++w) {
@@ -124,14 +188,15 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant_
     const int a = max(h0 - first, 0), e = min(h1 - first, x.heads);
     first += x.heads;
     if (a >= e) continue;
-    const Tin* src = static_cast<const Tin*>(x.in) + b * x.ib + l * x.il;
-    Tout* dst = static_cast<Tout*>(x.out) + b * x.ob + l * x.ol;
-    float wu[8], wv[8];
+    const Tin* src = static_cast<const Tin*>(x.in) + b * x.ib + l * x.il + a * x.ih + s.c0;
+    Tout* dst = static_cast<Tout*>(x.out) + b * x.ob + l * x.ol + a * x.oh + s.c0;
+    const int step = s.c1 - s.c0;
+    Pair wu[4], wv[4];
     if (w < 2) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        wu[k] = weight_at(np, w, s.c0 + k);
-        wv[k] = weight_at(np, w, s.c1 + k);
+      for (int k = 0; k < 4; ++k) {
+        wu[k] = pair_of(weight_at(np, w, s.c0 + 2 * k), weight_at(np, w, s.c0 + 2 * k + 1));
+        wv[k] = pair_of(weight_at(np, w, s.c1 + 2 * k), weight_at(np, w, s.c1 + 2 * k + 1));
       }
     }
     // rows of the next heads are on their way while one is worked on (an output may be its own input, but
@@ -140,8 +205,9 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant_
     Eight<Tin> ru[kDepth]{}, rv[kDepth]{};
     auto fetch = [&](int i, int h) {
       if (!here || h >= e) return;
-      ru[i] = load8(src + h * x.ih + s.c0);
-      rv[i] = load8(src + h * x.ih + s.c1);
+      ru[i] = load8(src);
+      rv[i] = load8(src + step);
+      src += x.ih;
     };
 #pragma unroll
     for (int i = 0; i < kDepth; ++i) fetch(i, a + i);
@@ -149,25 +215,30 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant_
 #pragma unroll
       for (int i = 0; i < kDepth; ++i) {
         if (h + i >= e) break;
-        float u[8], v[8];
-        to_floats(ru[i], u);
-        to_floats(rv[i], v);
+        Pair u[4], v[4];
+        to_pairs(ru[i], u);
+        to_pairs(rv[i], v);
         fetch(i, h + i + kDepth);
         if (w < 2) {
-          float sum = 0.f;
+          Pair sum = mul2(u[0], u[0]);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) sum += u[k] * u[k] + v[k] * v[k];
-          const float r = rsqrtf(row_sum(sum, per_row, rr * per_row) * np.inv_d + np.eps);
+          for (int k = 1; k < 4; ++k) sum = fma2(u[k], u[k], sum);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            u[k] *= r * wu[k];
-            v[k] *= r * wv[k];
+          for (int k = 0; k < 4; ++k) sum = fma2(v[k], v[k], sum);
+          const float r = rsqrtf(row_sum(sum2(sum), per_row, rr * per_row) * np.inv_d + np.eps);
+          const Pair r2 = pair_of(r, r);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            u[k] = mul2(u[k], mul2(r2, wu[k]));
+            v[k] = mul2(v[k], mul2(r2, wv[k]));
           }
-          rotate<HALF>(p, s, cs, u, v);
+          rotate<HALF>(p, s, turn, u, v);
         }
-        if (!here) continue;
-        store8(dst + (h + i) * x.oh + s.c0, u);
-        store8(dst + (h + i) * x.oh + s.c1, v);
+        if (here) {
+          store_pairs(dst, u);
+          store_pairs(dst + step, v);
+        }
+        dst += x.oh;
       }
     }
   }
@@ -302,20 +373,21 @@ __device__ __forceinline__ void norm_grad(float s1, float s2, const NormParams& 
 // registers; of each the block takes every gridDim.x-th item (tokens of its warps x a group of heads).
 template <class Tx, class Tg, bool HALF>
 __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(const __grid_constant__ NormParams np) {
-  __shared__ float s_part[2048];   // [row of the block][d]
+  __shared__ __align__(16) float s_part[2048];   // [row of the block][d]
   __shared__ __align__(16) float s_w[128];
   const RopeParams& p = np.r;
   const int per_row = p.d / 16, rows = 32 / per_row;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int rr = lane / per_row;
   const Pieces s = pieces_of<HALF>(p, lane - rr * per_row);
+  const int step = s.c1 - s.c0;
 #pragma unroll 1
   for (int w = 0; w < 3; ++w) {
     const RopeTensor& y = p.t[w];
     const int hpi = np.heads_per_item[w], groups = np.head_groups[w];
-    float acc_u[8], acc_v[8];
+    Pair acc_u[4], acc_v[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) acc_u[k] = acc_v[k] = 0.f;
+    for (int k = 0; k < 4; ++k) acc_u[k] = acc_v[k] = 0;
     if (w < 2) {
       for (int e = threadIdx.x; e < p.d; e += kRopeThreads) s_w[e] = weight_at(np, w, e);
       __syncthreads();
@@ -327,53 +399,68 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(cons
       const bool here = rr < rows && n < p.tokens;
       const int64_t b = here ? n / p.L : 0;
       const int l = here ? int(n - b * p.L) : 0;
-      const Tg* src = static_cast<const Tg*>(y.in) + b * y.ib + l * y.il;
-      const Tx* xs = static_cast<const Tx*>(np.x[w]) + b * np.xb[w] + l * np.xl[w];
-      Tx* dst = static_cast<Tx*>(y.out) + b * y.ob + l * y.ol;
+      const Tg* src = static_cast<const Tg*>(y.in) + b * y.ib + l * y.il + a * y.ih + s.c0;
+      const Tx* xs = static_cast<const Tx*>(np.x[w]) + b * np.xb[w] + l * np.xl[w] + a * np.xh[w] + s.c0;
+      Tx* dst = static_cast<Tx*>(y.out) + b * y.ob + l * y.ol + a * y.oh + s.c0;
       // rows of the next heads are on their way while one is worked on (no output is another row's input)
       constexpr int kDepth = sizeof(Tx) + sizeof(Tg) == 4 ? 3 : 2;
       Eight<Tg> gu[kDepth]{}, gv[kDepth]{};
       Eight<Tx> xu[kDepth]{}, xv[kDepth]{};
       auto fetch = [&](int i, int h) {
         if (!here || h >= e) return;
-        gu[i] = load8(src + h * y.ih + s.c0);
-        gv[i] = load8(src + h * y.ih + s.c1);
+        gu[i] = load8(src);
+        gv[i] = load8(src + step);
+        src += y.ih;
         if (w == 2) return;
-        xu[i] = load8(xs + h * np.xh[w] + s.c0);
-        xv[i] = load8(xs + h * np.xh[w] + s.c1);
+        xu[i] = load8(xs);
+        xv[i] = load8(xs + step);
+        xs += np.xh[w];
       };
 #pragma unroll
       for (int i = 0; i < kDepth; ++i) fetch(i, a + i);
-      float2 cs[8];
-      if (w < 2) angles<HALF>(p, s, here ? rope_position(p, b, l) : 0.0, cs);   // (rows not here add zeros below)
+      Turn<HALF> turn;
+      if (w < 2) angles<HALF>(p, s, here ? rope_position(p, b, l) : 0.0, turn);   // (rows not here add zeros below)
       for (int h = a; h < e; h += kDepth) {
 #pragma unroll
         for (int i = 0; i < kDepth; ++i) {
           if (h + i >= e) break;
-          float fgu[8], fgv[8], fxu[8], fxv[8];
-          to_floats(gu[i], fgu);
-          to_floats(gv[i], fgv);
-          to_floats(xu[i], fxu);
-          to_floats(xv[i], fxv);
+          Pair fgu[4], fgv[4], fxu[4], fxv[4];
+          to_pairs(gu[i], fgu);
+          to_pairs(gv[i], fgv);
+          to_pairs(xu[i], fxu);
+          to_pairs(xv[i], fxv);
           fetch(i, h + i + kDepth);
           if (w < 2) {
-            rotate<HALF>(p, s, cs, fgu, fgv);
-            float s1 = 0.f, s2 = 0.f, wu[8], wv[8];   // (the weights stay in shared memory: 16 registers less)
-            to_floats(load8(s_w + s.c0), wu);
-            to_floats(load8(s_w + s.c1), wv);
+            rotate<HALF>(p, s, turn, fgu, fgv);
+            // (the weights stay in shared memory: 16 registers less)
+            const Pair* wu = reinterpret_cast<const Pair*>(s_w + s.c0);
+            const Pair* wv = reinterpret_cast<const Pair*>(s_w + s.c1);
+            Pair s1 = 0, s2 = 0, zu[4], zv[4];   // z = g w
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              s1 += fxu[k] * fxu[k] + fxv[k] * fxv[k];
-              s2 += fxu[k] * (fgu[k] * wu[k]) + fxv[k] * (fgv[k] * wv[k]);
+            for (int k = 0; k < 4; ++k) {
+              zu[k] = mul2(fgu[k], wu[k]);
+              zv[k] = mul2(fgv[k], wv[k]);
+              s1 = fma2(fxv[k], fxv[k], fma2(fxu[k], fxu[k], s1));
+              s2 = fma2(fxv[k], zv[k], fma2(fxu[k], zu[k], s2));
             }
-            s1 = row_sum(s1, per_row, rr * per_row);
-            s2 = row_sum(s2, per_row, rr * per_row);
-            norm_grad(s1, s2, np, wu, fxu, fgu, acc_u);
-            norm_grad(s1, s2, np, wv, fxv, fgv, acc_v);
+            const float sum1 = row_sum(sum2(s1), per_row, rr * per_row);
+            const float sum2_ = row_sum(sum2(s2), per_row, rr * per_row);
+            const float r = rsqrtf(sum1 * np.inv_d + np.eps);
+            const float k1 = -r * (r * (sum2_ * np.inv_d));
+            const Pair r2 = pair_of(r, r), k2 = pair_of(k1, k1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              acc_u[k] = fma2(fgu[k], mul2(fxu[k], r2), acc_u[k]);
+              acc_v[k] = fma2(fgv[k], mul2(fxv[k], r2), acc_v[k]);
+              fgu[k] = mul2(r2, fma2(fxu[k], k2, zu[k]));
+              fgv[k] = mul2(r2, fma2(fxv[k], k2, zv[k]));
+            }
           }
-          if (!here) continue;
-          store8(dst + (h + i) * y.oh + s.c0, fgu);
-          store8(dst + (h + i) * y.oh + s.c1, fgv);
+          if (here) {
+            store_pairs(dst, fgu);
+            store_pairs(dst + step, fgv);
+          }
+          dst += y.oh;
         }
       }
     }
@@ -383,11 +470,8 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(cons
     __syncthreads();
     if (rr < rows) {
       float* row = s_part + (wid * rows + rr) * p.d;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        row[s.c0 + k] = acc_u[k];
-        row[s.c1 + k] = acc_v[k];
-      }
+      store_pairs(row + s.c0, acc_u);
+      store_pairs(row + s.c1, acc_v);
     }
     __syncthreads();
     for (int c = threadIdx.x; c < p.d; c += kRopeThreads) {
