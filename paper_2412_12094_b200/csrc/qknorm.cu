@@ -24,8 +24,9 @@ struct NormParams {
   int64_t xb[3], xh[3], xl[3];
   float* part;
   float* dw[2];
-  int64_t items[3];          // of each tensor: (tokens of a block's warps, group of heads)
-  int heads_per_item[3], head_groups[3], blocks;
+  int64_t groups;            // of the tokens that a warp takes at once
+  int blocks[3];             // that have rows of each tensor (whichever other tensors there are)
+  int grid;
 };
 
 __device__ __forceinline__ float weight_at(const NormParams& p, int w, int e) {
@@ -102,47 +103,26 @@ __device__ __forceinline__ void store_pairs(T* s, const Pair (&x)[4]) {
   store8(s, f);
 }
 
-// Angles of the thread's pairs.  HALF: elements k of its pieces are a pair, so cosines, sines and
-// their negatives stand in pairs as the elements do; else pair k is two neighbours, and (cos, sin).
 template <bool HALF>
-struct Turn {
-  Pair c[4], s[4], n[4];
-};
-template <>
-struct Turn<false> {
-  float2 cs[8];
-};
-template <bool HALF>
-__device__ __forceinline__ void angles(const RopeParams& p, const Pieces& s, double pos, Turn<HALF>& t) {
-  float2 cs[8];
+__device__ __forceinline__ void angles(const RopeParams& p, const Pieces& s, double pos, float2 (&cs)[8]) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int i = HALF ? s.c0 + k : (k < 4 ? s.c0 / 2 + k : s.c1 / 2 + k - 4);
     cs[k] = s.turn && 2 * i < p.rot ? rope_cos_sin(p, pos, i) : make_float2(1.f, 0.f);
   }
-  if constexpr (HALF) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      t.c[k] = pair_of(cs[2 * k].x, cs[2 * k + 1].x);
-      t.s[k] = pair_of(cs[2 * k].y, cs[2 * k + 1].y);
-      t.n[k] = pair_of(-cs[2 * k].y, -cs[2 * k + 1].y);
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) t.cs[k] = cs[k];
-  }
 }
-// (where nothing turns the angle is 0, but the products with 0 would spread a NaN)
+// (One by one: a packed product has no sign of its own.  Where nothing turns the angle is 0, but the products
+// with 0 would spread a NaN.)
 template <bool HALF>
-__device__ __forceinline__ void rotate(const RopeParams& p, const Pieces& s, const Turn<HALF>& t, Pair (&u)[4],
+__device__ __forceinline__ void rotate(const RopeParams& p, const Pieces& s, const float2 (&cs)[8], Pair (&u)[4],
                                        Pair (&v)[4]) {
-  if constexpr (HALF) {
+  if (HALF) {
     if (!s.turn) return;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const Pair y = fma2(v[k], t.n[k], mul2(u[k], t.c[k]));
-      v[k] = fma2(u[k], t.s[k], mul2(v[k], t.c[k]));
-      u[k] = y;
+      const float2 a = floats_of(u[k]), b = floats_of(v[k]), c0 = cs[2 * k], c1 = cs[2 * k + 1];
+      u[k] = pair_of(a.x * c0.x - b.x * c0.y, a.y * c1.x - b.y * c1.y);
+      v[k] = pair_of(b.x * c0.x + a.x * c0.y, b.y * c1.x + a.y * c1.y);
     }
   } else {
     auto turn = [](Pair x, float2 cs) {
@@ -151,15 +131,18 @@ __device__ __forceinline__ void rotate(const RopeParams& p, const Pieces& s, con
     };
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if (s.c0 + 2 * k < p.rot) u[k] = turn(u[k], t.cs[k]);
-      if (s.c1 + 2 * k < p.rot) v[k] = turn(v[k], t.cs[4 + k]);
+      if (s.c0 + 2 * k < p.rot) u[k] = turn(u[k], cs[k]);
+      if (s.c1 + 2 * k < p.rot) v[k] = turn(v[k], cs[4 + k]);
     }
   }
 }
-// Sum over the row's lanes, in each of them (all 32 lanes call).
+// Sum over the row's lanes, in each of them (all 32 lanes call).  PER_ROW: the lanes of a row, 4 or 8 (heads of 64
+// and 128), or 0 for any number.
+template <int PER_ROW>
 __device__ __forceinline__ float row_sum(float x, int per_row, int first) {
-  if ((per_row & (per_row - 1)) == 0) {
-    for (int o = 1; o < per_row; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if constexpr (PER_ROW > 0) {
+#pragma unroll
+    for (int o = 1; o < PER_ROW; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
   }
   float s = 0.f;
@@ -167,10 +150,10 @@ __device__ __forceinline__ float row_sum(float x, int per_row, int first) {
   return s;
 }
 
-template <class Tin, class Tout, bool HALF>
+template <class Tin, class Tout, bool HALF, int PER_ROW>
 __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant__ NormParams np) {
   const RopeParams& p = np.r;
-  const int per_row = p.d / 16, rows = 32 / per_row;
+  const int per_row = PER_ROW ? PER_ROW : p.d / 16, rows = 32 / per_row;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int rr = lane / per_row;
   const int64_t n = (int64_t(blockIdx.x) * kWarps + wid) * rows + rr;
@@ -179,7 +162,7 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant_
   const int l = here ? int(n - b * p.L) : 0;
   const Pieces s = pieces_of<HALF>(p, lane - rr * per_row);
   const int h0 = blockIdx.y * p.heads_per_block, h1 = min(p.n_heads, h0 + p.heads_per_block);
-  Turn<HALF> turn;
+  float2 turn[8];
   if (here && h0 < p.t[0].heads + p.t[1].heads) angles<HALF>(p, s, rope_position(p, b, l), turn);
   int first = 0;  // heads of the tensors before this one
 #pragma unroll 1
@@ -225,7 +208,7 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant_
           for (int k = 1; k < 4; ++k) sum = fma2(u[k], u[k], sum);
 #pragma unroll
           for (int k = 0; k < 4; ++k) sum = fma2(v[k], v[k], sum);
-          const float r = rsqrtf(row_sum(sum2(sum), per_row, rr * per_row) * np.inv_d + np.eps);
+          const float r = rsqrtf(row_sum<PER_ROW>(sum2(sum), per_row, rr * per_row) * np.inv_d + np.eps);
           const Pair r2 = pair_of(r, r);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -369,14 +352,40 @@ __device__ __forceinline__ void norm_grad(float s1, float s2, const NormParams& 
   }
 }
 
-// The tensors one after the other, so that the sums for one tensor's weights are all that stays in
-// registers; of each the block takes every gridDim.x-th item (tokens of its warps x a group of heads).
-template <class Tx, class Tg, bool HALF>
+// A warp's way through the rows of a tensor, head by head and then on to the warp's next tokens (`rows` of
+// them, one to a lane's group).
+struct RowWalk {
+  int64_t b;
+  int l, h;
+  bool here;   // this lane has a token
+};
+__device__ __forceinline__ RowWalk walk_from(const RopeParams& p, int64_t group, int h, int rows, int rr) {
+  RowWalk k;
+  const int64_t n = group * rows + rr;
+  k.here = rr < rows && n < p.tokens;
+  k.b = n / p.L;
+  k.l = int(n - k.b * p.L);
+  k.h = h;
+  return k;
+}
+// true: on to the next tokens
+__device__ __forceinline__ bool walk_on(const RopeParams& p, RowWalk& k, int heads, int rows, int rr) {
+  if (++k.h < heads) return false;
+  k.h = 0;
+  for (k.l += rows; k.l >= p.L; k.l -= p.L) ++k.b;
+  k.here = rr < rows && k.b * p.L + k.l < p.tokens;
+  return true;
+}
+
+// The rows of a tensor, (tokens of a warp, head), are cut into equal runs, one per warp; the next rows are on
+// their way while one is worked on, over the ends of heads and tokens.  The tensors come one after the
+// other, so that the sums for one tensor's weights are all that stays in registers.
+template <class Tx, class Tg, bool HALF, int PER_ROW>
 __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(const __grid_constant__ NormParams np) {
   __shared__ __align__(16) float s_part[2048];   // [row of the block][d]
   __shared__ __align__(16) float s_w[128];
   const RopeParams& p = np.r;
-  const int per_row = p.d / 16, rows = 32 / per_row;
+  const int per_row = PER_ROW ? PER_ROW : p.d / 16, rows = 32 / per_row;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int rr = lane / per_row;
   const Pieces s = pieces_of<HALF>(p, lane - rr * per_row);
@@ -384,7 +393,6 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(cons
 #pragma unroll 1
   for (int w = 0; w < 3; ++w) {
     const RopeTensor& y = p.t[w];
-    const int hpi = np.heads_per_item[w], groups = np.head_groups[w];
     Pair acc_u[4], acc_v[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) acc_u[k] = acc_v[k] = 0;
@@ -392,44 +400,59 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(cons
       for (int e = threadIdx.x; e < p.d; e += kRopeThreads) s_w[e] = weight_at(np, w, e);
       __syncthreads();
     }
-    for (int64_t item = blockIdx.x; item < np.items[w]; item += gridDim.x) {
-      const int64_t tg = item / groups;
-      const int a = int(item - tg * groups) * hpi, e = min(y.heads, a + hpi);
-      const int64_t n = (tg * kWarps + wid) * rows + rr;
-      const bool here = rr < rows && n < p.tokens;
-      const int64_t b = here ? n / p.L : 0;
-      const int l = here ? int(n - b * p.L) : 0;
-      const Tg* src = static_cast<const Tg*>(y.in) + b * y.ib + l * y.il + a * y.ih + s.c0;
-      const Tx* xs = static_cast<const Tx*>(np.x[w]) + b * np.xb[w] + l * np.xl[w] + a * np.xh[w] + s.c0;
-      Tx* dst = static_cast<Tx*>(y.out) + b * y.ob + l * y.ol + a * y.oh + s.c0;
-      // rows of the next heads are on their way while one is worked on (no output is another row's input)
+    const int64_t total = np.groups * y.heads, warps = int64_t(np.blocks[w]) * kWarps;
+    const int64_t mine = min(int64_t(blockIdx.x) * kWarps + wid, warps);   // (no rows behind the last of them)
+    const int64_t first = total * mine / warps;
+    const int n_rows = int(total * min(mine + 1, warps) / warps - first);
+    if (n_rows > 0) {
+      const int64_t group = first / y.heads;
+      RowWalk at = walk_from(p, group, int(first - group * y.heads), rows, rr), ahead = at;
+      const Tg* src;
+      const Tx* xs;
+      Tx* dst;
+      auto to_ahead = [&]() {
+        src = static_cast<const Tg*>(y.in) + ahead.b * y.ib + ahead.l * y.il + ahead.h * y.ih + s.c0;
+        xs = static_cast<const Tx*>(np.x[w]) + ahead.b * np.xb[w] + ahead.l * np.xl[w] + ahead.h * np.xh[w] + s.c0;
+      };
+      auto to_at = [&]() { dst = static_cast<Tx*>(y.out) + at.b * y.ob + at.l * y.ol + at.h * y.oh + s.c0; };
       constexpr int kDepth = sizeof(Tx) + sizeof(Tg) == 4 ? 3 : 2;
       Eight<Tg> gu[kDepth]{}, gv[kDepth]{};
       Eight<Tx> xu[kDepth]{}, xv[kDepth]{};
-      auto fetch = [&](int i, int h) {
-        if (!here || h >= e) return;
-        gu[i] = load8(src);
-        gv[i] = load8(src + step);
+      auto fetch = [&](int i) {
+        if (ahead.here) {
+          gu[i] = load8(src);
+          gv[i] = load8(src + step);
+          if (w < 2) {
+            xu[i] = load8(xs);
+            xv[i] = load8(xs + step);
+          }
+        }
         src += y.ih;
-        if (w == 2) return;
-        xu[i] = load8(xs);
-        xv[i] = load8(xs + step);
         xs += np.xh[w];
+        if (walk_on(p, ahead, y.heads, rows, rr)) to_ahead();
       };
+      to_ahead();
+      to_at();
 #pragma unroll
-      for (int i = 0; i < kDepth; ++i) fetch(i, a + i);
-      Turn<HALF> turn;
-      if (w < 2) angles<HALF>(p, s, here ? rope_position(p, b, l) : 0.0, turn);   // (rows not here add zeros below)
-      for (int h = a; h < e; h += kDepth) {
+      for (int i = 0; i < kDepth; ++i)
+        if (i < n_rows) fetch(i);
+      float2 turn[8];
+      bool moved = true;   // to other tokens, whose angles are not there yet (rows not here add zeros below)
+      for (int r = 0; r < n_rows; r += kDepth) {
 #pragma unroll
         for (int i = 0; i < kDepth; ++i) {
-          if (h + i >= e) break;
+          if (r + i >= n_rows) break;
+          if (moved && w < 2) angles<HALF>(p, s, at.here ? rope_position(p, at.b, at.l) : 0.0, turn);
           Pair fgu[4], fgv[4], fxu[4], fxv[4];
           to_pairs(gu[i], fgu);
           to_pairs(gv[i], fgv);
           to_pairs(xu[i], fxu);
           to_pairs(xv[i], fxv);
-          fetch(i, h + i + kDepth);
+          if (!at.here) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) fgu[k] = fgv[k] = 0;
+          }
+          if (r + i + kDepth < n_rows) fetch(i);
           if (w < 2) {
             rotate<HALF>(p, s, turn, fgu, fgv);
             // (the weights stay in shared memory: 16 registers less)
@@ -443,11 +466,11 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(cons
               s1 = fma2(fxv[k], fxv[k], fma2(fxu[k], fxu[k], s1));
               s2 = fma2(fxv[k], zv[k], fma2(fxu[k], zu[k], s2));
             }
-            const float sum1 = row_sum(sum2(s1), per_row, rr * per_row);
-            const float sum2_ = row_sum(sum2(s2), per_row, rr * per_row);
-            const float r = rsqrtf(sum1 * np.inv_d + np.eps);
-            const float k1 = -r * (r * (sum2_ * np.inv_d));
-            const Pair r2 = pair_of(r, r), k2 = pair_of(k1, k1);
+            const float sum1 = row_sum<PER_ROW>(sum2(s1), per_row, rr * per_row);
+            const float sum2_ = row_sum<PER_ROW>(sum2(s2), per_row, rr * per_row);
+            const float r1 = rsqrtf(sum1 * np.inv_d + np.eps);
+            const float k1 = -r1 * (r1 * (sum2_ * np.inv_d));
+            const Pair r2 = pair_of(r1, r1), k2 = pair_of(k1, k1);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               acc_u[k] = fma2(fgu[k], mul2(fxu[k], r2), acc_u[k]);
@@ -456,17 +479,18 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(cons
               fgv[k] = mul2(r2, fma2(fxv[k], k2, zv[k]));
             }
           }
-          if (here) {
+          if (at.here) {
             store_pairs(dst, fgu);
             store_pairs(dst + step, fgv);
           }
           dst += y.oh;
+          moved = walk_on(p, at, y.heads, rows, rr);
+          if (moved) to_at();
         }
       }
     }
     if (w == 2) break;
-    // the block's sums: rows side by side, then added column by column in a fixed order (a row that is not
-    // here has added zeros)
+    // the block's sums: rows side by side, then added column by column in a fixed order
     __syncthreads();
     if (rr < rows) {
       float* row = s_part + (wid * rows + rr) * p.d;
@@ -492,30 +516,25 @@ __global__ void __launch_bounds__(kRopeThreads) norm_bwd_any(const __grid_consta
 #pragma unroll 1
   for (int w = 0; w < 3; ++w) {
     const RopeTensor& y = p.t[w];
-    const int hpi = np.heads_per_item[w], groups = np.head_groups[w];
     float wt[8], acc[8];
     if (w < 2) lane_weights(np, w, s, wt);
 #pragma unroll
     for (int k = 0; k < 8; ++k) acc[k] = 0.f;
-    for (int64_t item = blockIdx.x; item < np.items[w]; item += gridDim.x) {
-      const int64_t tg = item / groups;
-      const int a = int(item - tg * groups) * hpi, e = min(y.heads, a + hpi);
-      const int64_t n = tg * kWarps + wid;
-      if (n >= p.tokens) continue;
-      const int64_t b = n / p.L;
-      const int l = int(n - b * p.L);
-      const Tg* src = static_cast<const Tg*>(y.in) + b * y.ib + l * y.il;
-      const Tx* xs = static_cast<const Tx*>(np.x[w]) + b * np.xb[w] + l * np.xl[w];
-      Tx* dst = static_cast<Tx*>(y.out) + b * y.ob + l * y.ol;
+    const int64_t total = np.groups * y.heads, warps = int64_t(np.blocks[w]) * kWarps;
+    const int64_t mine = min(int64_t(blockIdx.x) * kWarps + wid, warps);   // (no rows behind the last of them)
+    const int64_t first = total * mine / warps, last = total * min(mine + 1, warps) / warps;
+    if (first < last) {
+      const int64_t group = first / y.heads;
+      RowWalk at = walk_from(p, group, int(first - group * y.heads), 1, 0);
       float2 cs[2];
-      if (w < 2) lane_angles(p, b, l, lane, cs);
-#pragma unroll 2
-      for (int h = a; h < e; ++h) {
+      bool moved = true;
+      for (int64_t r = first; r < last; ++r) {
+        if (moved && w < 2) lane_angles(p, at.b, at.l, lane, cs);
         float g[8];
-        load_lane(src + h * y.ih, s, g);
+        load_lane(static_cast<const Tg*>(y.in) + at.b * y.ib + at.l * y.il + at.h * y.ih, s, g);
         if (w < 2) {
           float x[8];
-          load_lane(xs + h * np.xh[w], s, x);
+          load_lane(static_cast<const Tx*>(np.x[w]) + at.b * np.xb[w] + at.l * np.xl[w] + at.h * np.xh[w], s, x);
           lane_rotate(cs, g);
           float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -525,7 +544,8 @@ __global__ void __launch_bounds__(kRopeThreads) norm_bwd_any(const __grid_consta
           }
           norm_grad(warp_sum(s1), warp_sum(s2), np, wt, x, g, acc);
         }
-        store_lane(dst + h * y.oh, s, g);
+        store_lane(static_cast<Tx*>(y.out) + at.b * y.ob + at.l * y.ol + at.h * y.oh, s, g);
+        moved = walk_on(p, at, y.heads, 1, 0);
       }
     }
     if (w == 2) break;
@@ -548,7 +568,7 @@ __global__ void __launch_bounds__(1024) norm_bwd_sum(const __grid_constant__ Nor
   wait_for_prior();
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, d = np.r.d;
   float sum = 0.f;
-  for (int i = wid; i < np.blocks; i += 32) sum += np.part[size_t(i) * 2 * d + c];   // (2 d: a multiple of 32)
+  for (int i = wid; i < np.grid; i += 32) sum += np.part[size_t(i) * 2 * d + c];   // (2 d: a multiple of 32)
   s_sum[wid][lane] = sum;
   __syncthreads();
   if (wid != 0) return;
@@ -583,16 +603,24 @@ void fill_norm(const sepllm_rope_desc* d, const sepllm_qknorm_desc* n, NormParam
 
 template <class Tin, class Tout>
 void launch_norm(const NormParams& p, bool rows, dim3 grid, cudaStream_t stream) {
-  if (!rows) norm_any<Tin, Tout><<<grid, kRopeThreads, 0, stream>>>(p);
-  else if (p.half) norm_rows<Tin, Tout, true><<<grid, kRopeThreads, 0, stream>>>(p);
-  else norm_rows<Tin, Tout, false><<<grid, kRopeThreads, 0, stream>>>(p);
+  if (!rows) {
+    norm_any<Tin, Tout><<<grid, kRopeThreads, 0, stream>>>(p);
+    return;
+  }
+#define SEPLLM_NORM(N) (p.half ? norm_rows<Tin, Tout, true, N> : norm_rows<Tin, Tout, false, N>)
+  auto kernel = p.r.d == 128 ? SEPLLM_NORM(8) : p.r.d == 64 ? SEPLLM_NORM(4) : SEPLLM_NORM(0);
+#undef SEPLLM_NORM
+  kernel<<<grid, kRopeThreads, 0, stream>>>(p);
 }
 template <class Tx, class Tg>
 void launch_norm_bwd(const NormParams& p, bool rows, cudaStream_t stream) {
-  const unsigned grid = unsigned(p.blocks);
-  if (!rows) norm_bwd_any<Tx, Tg><<<grid, kRopeThreads, 0, stream>>>(p);
-  else if (p.half) norm_bwd_rows<Tx, Tg, true><<<grid, kRopeThreads, 0, stream>>>(p);
-  else norm_bwd_rows<Tx, Tg, false><<<grid, kRopeThreads, 0, stream>>>(p);
+#define SEPLLM_NORM(N) (p.half ? norm_bwd_rows<Tx, Tg, true, N> : norm_bwd_rows<Tx, Tg, false, N>)
+  auto kernel = !rows           ? norm_bwd_any<Tx, Tg>
+                : p.r.d == 128 ? SEPLLM_NORM(8)
+                : p.r.d == 64  ? SEPLLM_NORM(4)
+                               : SEPLLM_NORM(0);
+#undef SEPLLM_NORM
+  kernel<<<unsigned(p.grid), kRopeThreads, 0, stream>>>(p);
 }
 
 }  // namespace
@@ -668,16 +696,13 @@ extern "C" sepllm_status sepllm_qknorm_rope_bwd(const sepllm_rope_desc* desc, co
   p.part = static_cast<float*>(workspace);
   const bool rows = by_rows(desc, p.r, vectors);
   const int64_t per_warp = rows ? 32 / (desc->d / 16) : 1;
-  const int64_t warps = (p.r.tokens + per_warp - 1) / per_warp, groups = (warps + kWarps - 1) / kWarps;
-  int64_t most = 1;
+  p.groups = (p.r.tokens + per_warp - 1) / per_warp;
+  p.grid = 1;
   for (int w = 0; w < 3; ++w) {
-    const int heads = p.r.t[w].heads;   // (0: left out)
-    p.heads_per_item[w] = heads ? rope_heads_per_thread(heads, warps * 32) : 1;
-    p.head_groups[w] = std::max(1, (heads + p.heads_per_item[w] - 1) / p.heads_per_item[w]);
-    p.items[w] = heads ? groups * p.head_groups[w] : 0;
-    most = std::max(most, p.items[w]);
+    p.blocks[w] = int(std::min<int64_t>((p.groups * p.r.t[w].heads + kWarps - 1) / kWarps, kBwdBlocks));
+    p.blocks[w] = std::max(p.blocks[w], 1);
+    p.grid = std::max(p.grid, p.blocks[w]);
   }
-  p.blocks = int(std::min<int64_t>(most, kBwdBlocks));
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   if (dt_out == 0 && dt_in == 0) launch_norm_bwd<__nv_bfloat16, __nv_bfloat16>(p, rows, stream);
   else if (dt_out == 0) launch_norm_bwd<__nv_bfloat16, float>(p, rows, stream);
