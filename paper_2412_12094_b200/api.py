@@ -216,6 +216,13 @@ def _sep_array(sep_ids):
     return arr, arr.ctypes.data_as(C.c_void_p), int(arr.size)
 
 
+def _sep_bytes(sep_ids):
+    """Separator ids as the int32 array that a C entry point reads during the call, and their number."""
+    if isinstance(sep_ids, np.ndarray) and sep_ids.dtype == np.int32 and sep_ids.ndim == 1:
+        return sep_ids.tobytes(), sep_ids.size
+    return struct.pack(f"={len(sep_ids)}i", *sep_ids), len(sep_ids)
+
+
 def status_string(code: int) -> str:
     return lib().sepllm_status_string(code).decode()
 
@@ -536,11 +543,10 @@ def sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, prefix_len, O
 # ---------------------------------------------------------------- cache in 4 bits
 def _quant_kv(where, desc, Kc, Vc):
     """Refuses buffers shorter than a cache of the descriptor (they would be read past their end)."""
-    rows = desc.B * desc.Hkv * (desc.c + desc.s)
-    need = (rows * desc.d // 2 + 255 & -256) + (rows * desc.d // 16 + 255 & -256)
-    for name, t in (("Kc", Kc), ("Vc", Vc)):
-        if t.numel() * t.element_size() < need:
-            raise ValueError(f"{where}: {name} has {t.numel() * t.element_size()} bytes, the descriptor's cache {need}")
+    n = desc.B * desc.Hkv * (desc.c + desc.s) * desc.d
+    need = (n // 2 + 255 & -256) + (n // 16 + 255 & -256)
+    if Kc.nbytes < need or Vc.nbytes < need:
+        raise ValueError(f"{where}: Kc and Vc have {Kc.nbytes} and {Vc.nbytes} bytes, the descriptor's cache {need} each")
 
 
 def sepllm_cache_bytes_quant(desc: CacheDesc):
@@ -552,7 +558,7 @@ def sepllm_cache_bytes_quant(desc: CacheDesc):
 def sepllm_cache_update_quant(desc, state, Kc, Vc, new_token_ids, sep_ids, k_new, v_new):
     """sepllm_cache_update for a cache held in 4 bits (Kc, Vc: sepllm_cache_bytes_quant)."""
     where, row = "sepllm_cache_update_quant", (desc.B, desc.Hkv, desc.d)
-    arr, p, n = _sep_array(sep_ids)
+    p, n = _sep_bytes(sep_ids)
     _expect(where, ("new_token_ids", new_token_ids, (desc.B,), torch.int32), ("k_new", k_new, row, torch.bfloat16),
             ("v_new", v_new, row, torch.bfloat16))
     _quant_kv(where, desc, Kc, Vc)

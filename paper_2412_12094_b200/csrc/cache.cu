@@ -123,6 +123,7 @@ prompt_plan(sepllm_cache_header h, uint8_t* __restrict__ state, const uint8_t* _
             sepllm_index_header ih, const int32_t* __restrict__ prompt_len) {
   __shared__ PromptPlan s_plan;
   __shared__ int s_bad;
+  let_dependents_start();   // (a launch that waits for this kernel itself)
   const sepllm_cache_desc d = h.desc;
   const int b = blockIdx.x, tid = threadIdx.x;
   const int L = ih.desc.L;

@@ -40,48 +40,61 @@ inline QuantRows<const uint8_t> quant_rows(const sepllm_cache_header& h, const v
   return {p, p + quant_code_bytes(h)};
 }
 
+// Blackwell's packed fp32 arithmetic, two numbers to an instruction, and an approximate reciprocal (2^-23).
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{.reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mul.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x;}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 sum2(float2 a, float2 b) {
+  float2 r;
+  asm("{.reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x;}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
 // Eight elements 8t .. 8t + 7 of a group, t = lane % 4; the group's four lanes are neighbours and all 32
 // lanes call.  Returns their codes, element e at bits 4e .. 4e + 3, and the group's step.
 //
 // A code is found from x * (1 / s), within 2^-20 of x / s.  x / s is either half a whole number
 // exactly, or at least 2^-10 away from one (x and s have eight significant bits): rounded to a multiple of
-// 2^-13 first (the sum with 1536), ties are ties again and nothing else has become one.
+// 2^-13 first (the sum with 1536), ties are ties again and nothing else has become one.  The sum with
+// 1.5 * 2^23 + 8 rounds to whole numbers, even at a tie, and leaves q + 8 in the low bits.
 __device__ __forceinline__ uint32_t quantise8(const uint4& raw, uint32_t* step_bits) {
   const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
-  float x[8];
+  // largest and smallest element, as (largest, -smallest); a NaN stays one
+  const __nv_bfloat162 hi = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+  const __nv_bfloat162 lo = __hneg2(__hmin2_nan(__hmin2_nan(h[0], h[1]), __hmin2_nan(h[2], h[3])));
+  __nv_bfloat162 m2 = __hmax2_nan(__lows2bfloat162(hi, lo), __highs2bfloat162(hi, lo));
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<uint32_t*>(&m2), o);
+    m2 = __hmax2_nan(m2, *reinterpret_cast<const __nv_bfloat162*>(&other));
+  }
+  const float2 ends = __bfloat1622float2(m2);
+  float s = ends.x >= ends.y ? ends.x * -0.125f : ends.y * 0.125f, r = 0.f;
+  if (!(fmaxf(fabsf(ends.x), fabsf(ends.y)) < INFINITY) || ends.x != ends.x || ends.y != ends.y)
+    s = __int_as_float(0x7fc00000);   // reads back as NaN in every element
+  else if (fabsf(s) < kFlush * 0.125f) s = 0.f;
+  else r = reciprocal(s);
+  uint32_t w = 0, offset = 0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const float2 f = __bfloat1622float2(h[k]);
-    x[2 * k] = f.x;
-    x[2 * k + 1] = f.y;
-  }
-  float hi = x[0], lo = x[0];
-  bool bad = false;   // NaN or infinite
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    hi = fmaxf(hi, x[k]);
-    lo = fminf(lo, x[k]);
-    bad |= !(fabsf(x[k]) < INFINITY);
-  }
-  if (bad) hi = INFINITY;
-#pragma unroll
-  for (int o = 1; o < 4; o <<= 1) {
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-  }
-  const float m = hi >= -lo ? hi : lo;
-  float s = m * -0.125f, r = 0.f;
-  if (hi == INFINITY) s = __int_as_float(0x7fc00000);   // reads back as NaN in every element
-  else if (fabsf(m) < kFlush) s = 0.f;
-  else r = __frcp_rn(s);
-  uint32_t w = 0;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float t = r == 0.f ? 0.f : __fsub_rn(__fadd_rn(__fmul_rn(x[k], r), 1536.f), 1536.f);
-    w |= uint32_t(min(__float2int_rn(t), 7) + 8) << (4 * k);
+    const float2 t = sum2(sum2(mul2(f, make_float2(r, r)), make_float2(1536.f, 1536.f)), make_float2(-1536.f, -1536.f));
+    // (a NaN, of a group whose step is one, goes with it)
+    const float2 n = sum2(make_float2(fminf(t.x, 7.f), fminf(t.y, 7.f)), make_float2(12582920.f, 12582920.f));
+    w += (__float_as_uint(n.x) << (8 * k)) + (__float_as_uint(n.y) << (8 * k + 4));
+    offset += (0x4b400000u << (8 * k)) + (0x4b400000u << (8 * k + 4));
   }
   *step_bits = __float_as_uint(s) >> 16;
-  return w;
+  return r == 0.f ? 0x88888888u : w - offset;
 }
 
 // Stores the codes of elements 8t .. 8t + 7 of group j of a row (and its step from lane t = 0).
@@ -105,8 +118,8 @@ template <int D>
 __global__ void __launch_bounds__(kUpdThreads)
 quant_update(sepllm_cache_header h, uint8_t* __restrict__ state, QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc,
              const __nv_bfloat16* __restrict__ k_new, const __nv_bfloat16* __restrict__ v_new,
-             const int32_t* __restrict__ new_token_ids, SepIds sep) {
-  extern __shared__ int16_t flag_s[];
+             const int32_t* __restrict__ new_token_ids, SepIds sep, int max_past) {
+  extern __shared__ int16_t flag_s[];   // [max_past] ranks, [max_past] entries that move
   __shared__ int warp_buf[32];
   constexpr int kVec = D / 8, kCode = D / 2, kStep = D / 16;   // 16-byte pieces of a new row; bytes of a held one
   const sepllm_cache_desc& d = h.desc;
@@ -133,19 +146,46 @@ quant_update(sepllm_cache_header h, uint8_t* __restrict__ state, QuantRows<uint8
   if (mv.any) {
     mv.m = rank_past_separators(v.slot_is_sep + size_t(b) * h.slots, q, d, p.n_past, flag_s, warp_buf);
     mv.drop = max(0, q.size_sep + mv.m - d.s);
-    // 16 lanes to an entry: 16-byte pieces of its codes, its steps
-    constexpr int kPieces = kCode / 16;
-    const int l = tid % 16;
-    for (int k = tid / 16; k < p.n_past; k += kUpdThreads / 16) {
-      int src, dst;
-      if (!past_move(k, flag_s, q, d, mv.drop, &src, &dst)) continue;
-      if (l < 2 * kPieces) {
-        uint4* c = reinterpret_cast<uint4*>(l < kPieces ? kc : vc);
-        c[size_t(dst) * kPieces + l % kPieces] = c[size_t(src) * kPieces + l % kPieces];
-      } else if (l < 2 * kPieces + 2 * (kStep / 4)) {
-        const int x = l - 2 * kPieces;
-        uint32_t* s = reinterpret_cast<uint32_t*>(x < kStep / 4 ? ks : vs);
-        s[size_t(dst) * (kStep / 4) + x % (kStep / 4)] = s[size_t(src) * (kStep / 4) + x % (kStep / 4)];
+    // The entries that move, in order, then all their pieces over all threads: an entry of 16-byte pieces of its
+    // codes and its steps.  (Entry by entry, with most entries staying, the copies of a warp waited for one
+    // another: 16 sequences, some at a compaction of 690 entries, took 17 us instead of 8.)
+    constexpr int kPieces = kCode / 16, kPer = 2 * kPieces + 2;
+    int16_t* list = flag_s + max_past;
+    const int first = max(0, mv.drop - q.size_sep), n = mv.m - first;   // of the past separators, those kept
+    for (int k = tid; k < p.n_past; k += kUpdThreads)
+      if (flag_s[k] > first) list[flag_s[k] - 1 - first] = int16_t(k);
+    __syncthreads();
+    constexpr int kBatch = 4;   // copies of a thread that are on their way at once
+    for (int x0 = tid; x0 < n * kPer; x0 += kBatch * kUpdThreads) {
+      uint4 v16[kBatch];
+      int dst[kBatch], piece[kBatch];
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) {
+        const int x = x0 + y * kUpdThreads;
+        if (x >= n * kPer) break;
+        int src;
+        past_move(list[x / kPer], flag_s, q, d, mv.drop, &src, &dst[y]);
+        piece[y] = x % kPer;
+        if (piece[y] < 2 * kPieces) {
+          const uint4* c = reinterpret_cast<const uint4*>(piece[y] < kPieces ? kc : vc);
+          v16[y] = c[size_t(src) * kPieces + piece[y] % kPieces];
+        } else {
+          const uint32_t* st = reinterpret_cast<const uint32_t*>(piece[y] == 2 * kPieces ? ks : vs) + size_t(src) * (kStep / 4);
+          v16[y].x = st[0];
+          if (kStep == 8) v16[y].y = st[1];
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) {
+        if (x0 + y * kUpdThreads >= n * kPer) break;
+        if (piece[y] < 2 * kPieces) {
+          uint4* c = reinterpret_cast<uint4*>(piece[y] < kPieces ? kc : vc);
+          c[size_t(dst[y]) * kPieces + piece[y] % kPieces] = v16[y];
+        } else {
+          uint32_t* st = reinterpret_cast<uint32_t*>(piece[y] == 2 * kPieces ? ks : vs) + size_t(dst[y]) * (kStep / 4);
+          st[0] = v16[y].x;
+          if (kStep == 8) st[1] = v16[y].y;
+        }
       }
     }
   }
@@ -164,6 +204,7 @@ __global__ void __launch_bounds__(kCopyThreads)
 quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ K,
              const __nv_bfloat16* __restrict__ V, int L, QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc) {
   constexpr int kVec = D / 8, kRowsPerPass = kCopyThreads / (2 * kVec), kPasses = kCopyRows / kRowsPerPass;
+  wait_for_prior();   // (the plan)
   const sepllm_cache_desc& d = h.desc;
   const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
   CacheView v = cache_view(const_cast<uint8_t*>(state), h);
@@ -189,6 +230,7 @@ quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __n
   }
 #pragma unroll
   for (int r = 0; r < kPasses; ++r) {
+    if (!__any_sync(0xffffffffu, used >> r & 1)) continue;
     uint32_t step;
     const uint32_t w = quantise8(raw[r], &step);
     if (!(used >> r & 1)) continue;
@@ -198,14 +240,33 @@ quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __n
   }
 }
 
+// (w & mask) | bits in one instruction (of the two constants one may be part of it: `bits` is a register).
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w), "n"(MASK), "r"(bits));
+  return r;
+}
+// Two bf16 numbers 128 (not a constant to the compiler, which would split and_or()).
+__device__ __forceinline__ uint32_t two_128() {
+  uint32_t r;
+  asm volatile("mov.b32 %0, 0x43004300;" : "=r"(r));
+  return r;
+}
+
 // Eight codes (element e at bits 4e ..) times their step, rounded to bf16 once (the product has up to
-// twelve significant bits, bf16 eight).
-__device__ __forceinline__ uint4 values8(uint32_t w, float s) {
-  uint32_t out[4];
+// twelve significant bits, bf16 eight): 128 + c as bf16, minus 136 (exact), times the step.
+__device__ __forceinline__ uint4 values8(uint32_t w, __nv_bfloat16 step, uint32_t k128) {
+  uint32_t p[4];   // elements k and k + 4
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    out[k] = pack_bf16(float(int(w >> (8 * k) & 15) - 8) * s, float(int(w >> (8 * k + 4) & 15) - 8) * s);
-  return make_uint4(out[0], out[1], out[2], out[3]);
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t n = and_or<0x000f000fu>(w >> (4 * k), k128);
+    const __nv_bfloat162 q = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&n), __float2bfloat162_rn(136.f));
+    const __nv_bfloat162 v = __hmul2(q, __bfloat162bfloat162(step));
+    p[k] = *reinterpret_cast<const uint32_t*>(&v);
+  }
+  return make_uint4(__byte_perm(p[0], p[1], 0x5410), __byte_perm(p[2], p[3], 0x5410), __byte_perm(p[0], p[1], 0x7632),
+                    __byte_perm(p[2], p[3], 0x7632));
 }
 
 // grid (ceil(c / kCopyRows), Hkv, B).  Row v of K and V of sequence b is its retained entry v.
@@ -223,6 +284,7 @@ quant_entries(sepllm_cache_header h, const uint8_t* __restrict__ state, QuantRow
   if (length && blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) length[b] = run;
   const int ch = threadIdx.x % kVec, j = ch / 4, t = ch % 4;
   const size_t unit = size_t(b) * d.Hkv + hk;
+  const uint32_t k128 = two_128();
 #pragma unroll
   for (int r = 0; r < kCopyRows; r += kRowsPerPass) {
     const int v = blockIdx.x * kCopyRows + r + threadIdx.x / kVec;
@@ -231,11 +293,11 @@ quant_entries(sepllm_cache_header h, const uint8_t* __restrict__ state, QuantRow
     const uint32_t wk = reinterpret_cast<const uint32_t*>(Kc.codes + row * (D / 2))[t * kGroups + j];
     const uint16_t* vc = reinterpret_cast<const uint16_t*>(Vc.codes + row * (D / 2));
     const uint32_t wv = vc[2 * t * kGroups + j] | uint32_t(vc[(2 * t + 1) * kGroups + j]) << 16;
-    const float sk = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(Kc.steps)[row * kGroups + j]);
-    const float sv = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(Vc.steps)[row * kGroups + j]);
+    const __nv_bfloat16 sk = reinterpret_cast<const __nv_bfloat16*>(Kc.steps)[row * kGroups + j];
+    const __nv_bfloat16 sv = reinterpret_cast<const __nv_bfloat16*>(Vc.steps)[row * kGroups + j];
     const size_t dst = (unit * n + v) * kVec + ch;
-    reinterpret_cast<uint4*>(K)[dst] = values8(wk, sk);
-    reinterpret_cast<uint4*>(V)[dst] = values8(wv, sv);
+    reinterpret_cast<uint4*>(K)[dst] = values8(wk, sk, k128);
+    reinterpret_cast<uint4*>(V)[dst] = values8(wv, sv, k128);
   }
 }
 
@@ -273,13 +335,6 @@ template <int BYTES>
 __device__ __forceinline__ void cp_async_small(uint32_t dst, const void* src, uint32_t src_bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(src_bytes)
                : "memory");
-}
-// (w & mask) | bits in one instruction (of the two constants one may be part of it: `bits` is a register).
-template <uint32_t MASK>
-__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t bits) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w), "n"(MASK), "r"(bits));
-  return r;
 }
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -453,8 +508,7 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
     if (tid == 0) p.ends[blockIdx.x] = make_int4(-1, -1, -1, -1);
     return;
   }
-  uint32_t k128;   // two bf16 numbers 128 (not a constant to the compiler, which would split and_or())
-  asm volatile("mov.b32 %0, 0x43004300;" : "=r"(k128));
+  const uint32_t k128 = two_128();
   uint8_t* ring = dec_smem + wid * (kStages * S::kStageB);
   const uint32_t ring_u = smem_u32(ring);
   int4 ends = make_int4(-1, -1, -1, -1);
@@ -964,7 +1018,8 @@ template <int D, int H>
 sepllm_status launch_decode_quant(const QuantDecodeParams& p, cudaStream_t stream) {
   constexpr int smem = DecodeShape<D, H>::kSmem;
   const unsigned ctas = unsigned(decode_quant_ctas(p.h.desc));
-  SEPLLM_CUDA_TRY(cudaFuncSetAttribute(decode_quant<D, H>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  if (smem > 48 * 1024)
+    SEPLLM_CUDA_TRY(cudaFuncSetAttribute(decode_quant<D, H>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   decode_quant<D, H><<<ctas, kDecThreads, smem, stream>>>(p);
   SEPLLM_CUDA_TRY(cudaGetLastError());
   const dim3 grid(ctas, p.h.desc.Hq / p.h.desc.Hkv);
@@ -1003,13 +1058,13 @@ extern "C" sepllm_status sepllm_cache_update_quant(const sepllm_cache_desc* desc
   SepIds sep;
   int max_past;
   if ((st = update_params(desc, sep_ids, n_sep, &sep, &max_past)) != SEPLLM_OK) return st;
-  const size_t smem = size_t(max_past) * sizeof(int16_t);
+  const size_t smem = size_t(max_past) * 2 * sizeof(int16_t);
   auto kernel = desc->d == 128 ? quant_update<128> : quant_update<64>;
   if (smem > 40 * 1024)
     SEPLLM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
   kernel<<<dim3(desc->B, desc->Hkv), kUpdThreads, smem, static_cast<cudaStream_t>(stream_)>>>(
       h, static_cast<uint8_t*>(state), quant_rows(h, Kc), quant_rows(h, Vc),
-      static_cast<const __nv_bfloat16*>(k_new), static_cast<const __nv_bfloat16*>(v_new), new_token_ids, sep);
+      static_cast<const __nv_bfloat16*>(k_new), static_cast<const __nv_bfloat16*>(v_new), new_token_ids, sep, max_past);
   SEPLLM_CUDA_TRY(cudaGetLastError());
   return SEPLLM_OK;
 }
@@ -1033,10 +1088,9 @@ extern "C" sepllm_status sepllm_cache_from_prompt_quant(const sepllm_cache_desc*
   if ((st = launch_prompt_plan(h, ih, state, index, prompt_len, stream)) != SEPLLM_OK) return st;
   const dim3 grid((h.slots + kCopyRows - 1) / kCopyRows, desc->Hkv, desc->B);
   auto kernel = desc->d == 128 ? quant_prompt<128> : quant_prompt<64>;
-  kernel<<<grid, kCopyThreads, 0, stream>>>(h, static_cast<const uint8_t*>(state),
-                                            static_cast<const __nv_bfloat16*>(K), static_cast<const __nv_bfloat16*>(V),
-                                            idesc->L, quant_rows(h, Kc), quant_rows(h, Vc));
-  SEPLLM_CUDA_TRY(cudaGetLastError());
+  SEPLLM_CUDA_TRY(launch_overlapped(kernel, grid, kCopyThreads, 0, stream, h, static_cast<const uint8_t*>(state),
+                                    static_cast<const __nv_bfloat16*>(K), static_cast<const __nv_bfloat16*>(V),
+                                    idesc->L, quant_rows(h, Kc), quant_rows(h, Vc)));
   return SEPLLM_OK;
 }
 
