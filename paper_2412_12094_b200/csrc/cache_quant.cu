@@ -59,42 +59,51 @@ __device__ __forceinline__ float reciprocal(float x) {
   return r;
 }
 
-// Eight elements 8t .. 8t + 7 of a group, t = lane % 4; the group's four lanes are neighbours and all 32
-// lanes call.  Returns their codes, element e at bits 4e .. 4e + 3, and the group's step.
+// N x 8 neighbouring elements of a group, whose 4 / N lanes are neighbours; all 32 lanes call.  Returns
+// their codes, element e of a word at bits 4e .. 4e + 3, and the bits of the group's step.
 //
 // A code is found from x * (1 / s), within 2^-20 of x / s.  x / s is either half a whole number
 // exactly, or at least 2^-10 away from one (x and s have eight significant bits): rounded to a multiple of
 // 2^-13 first (the sum with 1536), ties are ties again and nothing else has become one.  The sum with
 // 1.5 * 2^23 + 8 rounds to whole numbers, even at a tie, and leaves q + 8 in the low bits.
-__device__ __forceinline__ uint32_t quantise8(const uint4& raw, uint32_t* step_bits) {
-  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
+template <int N>
+__device__ __forceinline__ uint32_t quantise(const uint4 (&raw)[N], uint32_t (&codes)[N]) {
+  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(raw);
   // largest and smallest element, as (largest, -smallest); a NaN stays one
-  const __nv_bfloat162 hi = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-  const __nv_bfloat162 lo = __hneg2(__hmin2_nan(__hmin2_nan(h[0], h[1]), __hmin2_nan(h[2], h[3])));
+  __nv_bfloat162 hi = h[0], lo = h[0];
+#pragma unroll
+  for (int k = 1; k < 4 * N; ++k) {
+    hi = __hmax2_nan(hi, h[k]);
+    lo = __hmin2_nan(lo, h[k]);
+  }
+  lo = __hneg2(lo);
   __nv_bfloat162 m2 = __hmax2_nan(__lows2bfloat162(hi, lo), __highs2bfloat162(hi, lo));
 #pragma unroll
-  for (int o = 1; o < 4; o <<= 1) {
+  for (int o = 1; o < 4 / N; o <<= 1) {
     const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<uint32_t*>(&m2), o);
     m2 = __hmax2_nan(m2, *reinterpret_cast<const __nv_bfloat162*>(&other));
   }
   const float2 ends = __bfloat1622float2(m2);
   float s = ends.x >= ends.y ? ends.x * -0.125f : ends.y * 0.125f, r = 0.f;
-  if (!(fmaxf(fabsf(ends.x), fabsf(ends.y)) < INFINITY) || ends.x != ends.x || ends.y != ends.y)
+  if (!(fabsf(ends.x) < INFINITY && fabsf(ends.y) < INFINITY))
     s = __int_as_float(0x7fc00000);   // reads back as NaN in every element
   else if (fabsf(s) < kFlush * 0.125f) s = 0.f;
   else r = reciprocal(s);
-  uint32_t w = 0, offset = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float2 f = __bfloat1622float2(h[k]);
-    const float2 t = sum2(sum2(mul2(f, make_float2(r, r)), make_float2(1536.f, 1536.f)), make_float2(-1536.f, -1536.f));
-    // (a NaN, of a group whose step is one, goes with it)
-    const float2 n = sum2(make_float2(fminf(t.x, 7.f), fminf(t.y, 7.f)), make_float2(12582920.f, 12582920.f));
-    w += (__float_as_uint(n.x) << (8 * k)) + (__float_as_uint(n.y) << (8 * k + 4));
-    offset += (0x4b400000u << (8 * k)) + (0x4b400000u << (8 * k + 4));
+  for (int n = 0; n < N; ++n) {
+    uint32_t w = 0, offset = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 f = __bfloat1622float2(h[4 * n + k]);
+      const float2 t = sum2(sum2(mul2(f, make_float2(r, r)), make_float2(1536.f, 1536.f)), make_float2(-1536.f, -1536.f));
+      // (a NaN, of a group whose step is one, goes with it)
+      const float2 q = sum2(make_float2(fminf(t.x, 7.f), fminf(t.y, 7.f)), make_float2(12582920.f, 12582920.f));
+      w += (__float_as_uint(q.x) << (8 * k)) + (__float_as_uint(q.y) << (8 * k + 4));
+      offset += (0x4b400000u << (8 * k)) + (0x4b400000u << (8 * k + 4));
+    }
+    codes[n] = r == 0.f ? 0x88888888u : w - offset;
   }
-  *step_bits = __float_as_uint(s) >> 16;
-  return r == 0.f ? 0x88888888u : w - offset;
+  return __float_as_uint(s) >> 16;
 }
 
 // Stores the codes of elements 8t .. 8t + 7 of group j of a row (and its step from lane t = 0).
@@ -125,22 +134,22 @@ quant_update(sepllm_cache_header h, uint8_t* __restrict__ state, QuantRows<uint8
   const sepllm_cache_desc& d = h.desc;
   const int b = blockIdx.x, hk = blockIdx.y, tid = threadIdx.x;
   const size_t unit = size_t(b) * d.Hkv + hk;
-  uint4 raw = make_uint4(0, 0, 0, 0);
+  uint4 raw[1] = {make_uint4(0, 0, 0, 0)};
   const bool mine = tid < 2 * kVec, is_v = tid >= kVec;   // one warp at most
   if (mine)
-    raw = reinterpret_cast<const uint4*>(is_v ? v_new : k_new)[unit * kVec + (is_v ? tid - kVec : tid)];
+    raw[0] = reinterpret_cast<const uint4*>(is_v ? v_new : k_new)[unit * kVec + (is_v ? tid - kVec : tid)];
   CacheView v = cache_view(state, h);
   const sepllm_cache_seq q = v.seq[b];
   const UpdatePlan p = plan_update(q, d);
   uint8_t *kc = Kc.codes + unit * h.slots * kCode, *vc = Vc.codes + unit * h.slots * kCode;
   uint8_t *ks = Kc.steps + unit * h.slots * kStep, *vs = Vc.steps + unit * h.slots * kStep;
   if (tid < 32) {
-    uint32_t step;
-    const uint32_t w = quantise8(raw, &step);
+    uint32_t w[1];
+    const uint32_t step = quantise(raw, w);
     const int ch = tid % kVec;
     const size_t slot = p.append_slot;
-    if (mine && !is_v) store_codes<D, false>(kc + slot * kCode, ks + slot * kStep, ch / 4, ch % 4, w, step);
-    if (mine && is_v) store_codes<D, true>(vc + slot * kCode, vs + slot * kStep, ch / 4, ch % 4, w, step);
+    if (mine && !is_v) store_codes<D, false>(kc + slot * kCode, ks + slot * kStep, ch / 4, ch % 4, w[0], step);
+    if (mine && is_v) store_codes<D, true>(vc + slot * kCode, vs + slot * kStep, ch / 4, ch % 4, w[0], step);
   }
   UpdateMoves mv{p.compact && d.s > 0, 0, 0};
   if (mv.any) {
@@ -197,13 +206,12 @@ constexpr int kCopyThreads = 256;
 constexpr int kCopyRows = 64;  // slots (or entries) per CTA
 
 // grid (ceil(slots / kCopyRows), Hkv, B), behind the plan of the hand-off.  Quantises the K and V rows of the
-// retained positions into their slots: 2 * D / 8 lanes take one slot's rows in 16-byte pieces.  Bound by
-// HBM: the retained rows are read once, a quarter of that is written.
+// retained positions into their slots: D / 8 lanes take one slot's rows, sixteen elements each.
 template <int D>
 __global__ void __launch_bounds__(kCopyThreads)
 quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ K,
              const __nv_bfloat16* __restrict__ V, int L, QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc) {
-  constexpr int kVec = D / 8, kRowsPerPass = kCopyThreads / (2 * kVec), kPasses = kCopyRows / kRowsPerPass;
+  constexpr int kHalf = D / 16, kRowsPerPass = kCopyThreads / (2 * kHalf), kPasses = kCopyRows / kRowsPerPass;
   wait_for_prior();   // (the plan)
   const sepllm_cache_desc& d = h.desc;
   const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
@@ -211,12 +219,12 @@ quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __n
   const sepllm_cache_seq q = v.seq[b];
   const int64_t* pos_b = v.slot_pos + size_t(b) * h.slots;
   const size_t unit = size_t(b) * d.Hkv + hk;
-  const int sub = tid / (2 * kVec), l = tid % (2 * kVec);
-  const bool is_v = l >= kVec;
-  const int ch = l % kVec;  // 16-byte piece of the row
-  const uint4* src = reinterpret_cast<const uint4*>(is_v ? V : K) + unit * size_t(L) * kVec + ch;
+  const int sub = tid / (2 * kHalf), l = tid % (2 * kHalf);
+  const bool is_v = l >= kHalf;
+  const int ch = l % kHalf;  // sixteen elements of the row
+  const uint4* src = reinterpret_cast<const uint4*>(is_v ? V : K) + unit * size_t(L) * (D / 8) + 2 * ch;
   const int slot0 = blockIdx.x * kCopyRows + sub;
-  uint4 raw[kPasses];
+  uint4 raw[kPasses][2];
   uint32_t used = 0;
 #pragma unroll
   for (int r = 0; r < kPasses; ++r) {
@@ -225,18 +233,30 @@ quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __n
                    : slot < d.a + d.s     ? slot - d.a < q.size_sep
                    : slot < h.slots       ? slot - d.a - d.s < q.size_win
                                           : false;
-    raw[r] = u ? __ldg(src + size_t(pos_b[slot]) * kVec) : make_uint4(0, 0, 0, 0);
+    raw[r][0] = raw[r][1] = make_uint4(0, 0, 0, 0);
+    if (u) {
+      const uint4* row = src + size_t(pos_b[slot]) * (D / 8);
+      raw[r][0] = __ldg(row);
+      raw[r][1] = __ldg(row + 1);
+    }
     used |= uint32_t(u) << r;
   }
+  const QuantRows<uint8_t> out = is_v ? Vc : Kc;
 #pragma unroll
   for (int r = 0; r < kPasses; ++r) {
-    if (!__any_sync(0xffffffffu, used >> r & 1)) continue;
-    uint32_t step;
-    const uint32_t w = quantise8(raw[r], &step);
-    if (!(used >> r & 1)) continue;
+    const bool u = used >> r & 1;
+    if (!__any_sync(0xffffffffu, u)) continue;
+    uint32_t w[2];
+    const uint32_t step = quantise(raw[r], w);
+    if (!u) continue;
     const size_t row = unit * h.slots + slot0 + r * kRowsPerPass;
-    if (!is_v) store_codes<D, false>(Kc.codes + row * (D / 2), Kc.steps + row * (D / 16), ch / 4, ch % 4, w, step);
-    else store_codes<D, true>(Vc.codes + row * (D / 2), Vc.steps + row * (D / 16), ch / 4, ch % 4, w, step);
+    uint8_t *codes = out.codes + row * (D / 2), *steps = out.steps + row * (D / 16);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int j = ch / 2, t = 2 * (ch % 2) + n;
+      if (!is_v) store_codes<D, false>(codes, steps, j, t, w[n], step);
+      else store_codes<D, true>(codes, steps, j, t, w[n], step);
+    }
   }
 }
 
