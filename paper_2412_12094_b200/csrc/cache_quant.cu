@@ -19,6 +19,8 @@ namespace sepllm {
 
 namespace {
 
+// Every kernel is launched while the one before it ends (it waits for it first), and lets the next one in.
+
 constexpr int kGroup = 32;             // elements that share a step
 constexpr float kFlush = 0x1p-100f;    // groups whose largest magnitude is below are held as zeros
 
@@ -131,6 +133,8 @@ quant_update(sepllm_cache_header h, uint8_t* __restrict__ state, QuantRows<uint8
   extern __shared__ int16_t flag_s[];   // [max_past] ranks, [max_past] entries that move
   __shared__ int warp_buf[32];
   constexpr int kVec = D / 8, kCode = D / 2, kStep = D / 16;   // 16-byte pieces of a new row; bytes of a held one
+  let_dependents_start();
+  wait_for_prior();
   const sepllm_cache_desc& d = h.desc;
   const int b = blockIdx.x, hk = blockIdx.y, tid = threadIdx.x;
   const size_t unit = size_t(b) * d.Hkv + hk;
@@ -212,6 +216,7 @@ __global__ void __launch_bounds__(kCopyThreads)
 quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ K,
              const __nv_bfloat16* __restrict__ V, int L, QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc) {
   constexpr int kHalf = D / 16, kRowsPerPass = kCopyThreads / (2 * kHalf), kPasses = kCopyRows / kRowsPerPass;
+  let_dependents_start();
   wait_for_prior();   // (the plan)
   const sepllm_cache_desc& d = h.desc;
   const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
@@ -296,6 +301,8 @@ quant_entries(sepllm_cache_header h, const uint8_t* __restrict__ state, QuantRow
               QuantRows<const uint8_t> Vc, int n, __nv_bfloat16* __restrict__ K, __nv_bfloat16* __restrict__ V,
               int32_t* __restrict__ length) {
   constexpr int kVec = D / 8, kGroups = D / kGroup, kRowsPerPass = kCopyThreads / kVec;
+  let_dependents_start();
+  wait_for_prior();
   const sepllm_cache_desc& d = h.desc;
   const int b = blockIdx.z, hk = blockIdx.y;
   CacheView cv = cache_view(const_cast<uint8_t*>(state), h);
@@ -377,12 +384,12 @@ struct QuantDecodeParams {
   QuantRows<const uint8_t> Kc, Vc;
   __nv_bfloat16* o;
   float* lse;
-  int4* ends;        // [CTA] (b, hk) of the unit whose first steps were an earlier CTA's, and of the one whose
-                     // last steps are a later one's; -1: none
+  int4* ends;        // [CTA] b, hk of the unit that began with this CTA and ends with a later one, and that CTA; -1: none
   float2* part_ml;   // [2 * CTA + (0: the former, 1: the latter)][G] reference exponent and sum
   float* part_acc;   // [same][G][D]
   int32_t* status;
   float scale_log2;
+  int whole;         // 1: a CTA for every unit, and no parts
 };
 
 __device__ __forceinline__ int run_of(const sepllm_cache_seq& s) { return s.size_init + s.size_sep + s.size_win; }
@@ -408,8 +415,9 @@ __device__ __forceinline__ int contiguous_from(int v, const sepllm_cache_seq& q,
 // one per CTA: sequences of any lengths load the SMs evenly, and a unit is cut at most where a CTA's run
 // ends.  All threads call; false: nothing is left for this CTA.
 struct Share {
-  int b, hk, step;   // where the run starts
-  int64_t left;      // its steps
+  int b, hk, step;            // where the run starts
+  int64_t left;               // its steps
+  int64_t total, end;         // all steps, and where the run ends among them
 };
 // (32-bit divisions wherever the numbers allow)
 __device__ __forceinline__ uint64_t quotient(uint64_t a, uint32_t b) {
@@ -470,6 +478,8 @@ __device__ bool share_of(const sepllm_cache_seq* seq, int B, int Hkv, Share* out
   out->hk = int(quotient(in_seq, n));
   out->step = int(in_seq - int64_t(out->hk) * n);
   out->left = last - first;
+  out->total = total;
+  out->end = last;
   return true;
 }
 
@@ -481,14 +491,17 @@ struct DecodeShape {
   static constexpr int kGroups = D / kGroup;
   static constexpr int kCode = D / 2, kStep = D / 16;     // bytes of a row
   static constexpr int kStageB = 2 * kTile * (kCode + kStep);
-  static constexpr int kResident = D == 128 && H == 16 ? 2 : H == 4 ? 3 : 3;   // CTAs per SM (three: at most 168 registers a thread)
-  static constexpr int kStages = 4;
-  // shared memory: the warps' rings, in their place the warps' results at a unit's end, and the queries
+  // CTAs per SM.  Three: at most 168 registers a thread; four spill (D = 128, H = 4: 61 us instead of 33 for 32
+  // caches of 2750 entries).  A fourth stage would take the L1 from what little is spilled (35 us).
+  static constexpr int kResident = D == 128 && H == 16 ? 2 : 3;
+  static constexpr int kStages = 3;
+  // shared memory: the warps' rings, in whose last stages the warps' results stand at a unit's end while the
+  // first tiles of the next unit are on their way into the others, and the queries
   static constexpr int kRingB = kDecWarps * kStages * kStageB;
-  static constexpr int kMergeB = kDecWarps * H * (D * 4 + 8);
-  static constexpr int kUnionB = kRingB > kMergeB ? kRingB : kMergeB;
+  static constexpr int kEarly = kStages - (H * (D * 4 + 8) + kStageB - 1) / kStageB;   // tiles that may be on their way
+  static_assert(kEarly >= 1 && kEarly < kStages, "a warp's results fit into its last stages");
   static constexpr int kQWords = kSplit ? kGroups * 2 * 32 : NT * kGroups * 4 * 32;
-  static constexpr int kSmem = kUnionB + kQWords * 4 + H * (kGroups + 1) * 4;
+  static constexpr int kSmem = kRingB + kQWords * 4 + H * (kGroups + 1) * 4;
 };
 
 // 4 warps a CTA; each is a flash-decoding worker over its 32-entry tiles of the CTA's steps, which arrive
@@ -513,18 +526,23 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
   constexpr bool kSplit = S::kSplit;
   constexpr int NE = kSplit ? 1 : 2;   // heads of a lane's scores: t, or 8n + 2t and 8n + 2t + 1
   extern __shared__ __align__(128) uint8_t dec_smem[];
-  uint32_t* s_q = reinterpret_cast<uint32_t*>(dec_smem + S::kUnionB);
+  uint32_t* s_q = reinterpret_cast<uint32_t*>(dec_smem + S::kRingB);
   float* s_start = reinterpret_cast<float*>(s_q + S::kQWords);   // [head][group]
   float* s_factor = s_start + H * kGroups;                        // [head]
   let_dependents_start();
+  wait_for_prior();
   const sepllm_cache_desc& d = p.h.desc;
   const int G = d.Hq / d.Hkv;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int g = lane >> 2, t = lane & 3;
   if (tid == 0 && blockIdx.x == 0) *p.status = SEPLLM_OK;
   const sepllm_cache_seq* seqs = cache_view(const_cast<uint8_t*>(p.state), p.h).seq;
-  Share sh;
-  if (!share_of(seqs, d.B, d.Hkv, &sh)) {
+  Share sh{};
+  if (p.whole) {
+    sh.b = blockIdx.x / d.Hkv;
+    sh.hk = blockIdx.x - sh.b * d.Hkv;
+    sh.left = steps_of(seqs[sh.b]);
+  } else if (!share_of(seqs, d.B, d.Hkv, &sh)) {
     if (tid == 0) p.ends[blockIdx.x] = make_int4(-1, -1, -1, -1);
     return;
   }
@@ -533,21 +551,27 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
   const uint32_t ring_u = smem_u32(ring);
   int4 ends = make_int4(-1, -1, -1, -1);
 
-  while (sh.left > 0) {
-    const sepllm_cache_seq sq = seqs[sh.b];
-    const int run = run_of(sq), steps = steps_of(sq);
-    const int n_steps = int(min(sh.left, int64_t(steps - sh.step)));
-    const int v0 = sh.step * kStepRows, v1 = min(run, (sh.step + n_steps) * kStepRows);
+  // The unit at hand: entries v0 to v1 of sequence sh.b's kv head sh.hk are this CTA's.
+  constexpr int kPieces = kCode / 16, kRows = 32 / kPieces;   // 16-byte pieces of a row; rows of one copy of the warp
+  static_assert(kRows % 8 == 0, "a lane's places in the rows of a stage differ by whole copies");
+  constexpr int kPer = D / 8;                                 // threads that load a query head, eight elements each
+  constexpr int kQLoads = (H * kPer + kDecThreads - 1) / kDecThreads;
+  const int r0 = lane / kPieces, c0 = lane % kPieces;
+  sepllm_cache_seq sq;
+  int steps, n_steps, v0, v1, my_n;
+  uint32_t row0;            // of slot 0 among all rows
+  int run_end, run_slot;    // entries up to run_end have slots run_slot + entry
+  uint4 q_raw[kQLoads];
+  auto begin_unit = [&]() {
+    sq = seqs[sh.b];
+    steps = steps_of(sq);
+    n_steps = int(min(sh.left, int64_t(steps - sh.step)));
+    v0 = sh.step * kStepRows;
+    v1 = min(run_of(sq), (sh.step + n_steps) * kStepRows);
     const int n_tiles = (v1 - v0 + kTile - 1) / kTile;
-    const int my_n = n_tiles > wid ? (n_tiles - wid + kDecWarps - 1) / kDecWarps : 0;
-    const size_t unit = size_t(sh.b) * d.Hkv + sh.hk;
-    const uint8_t *kc = p.Kc.codes + unit * p.h.slots * kCode, *vc = p.Vc.codes + unit * p.h.slots * kCode;
-    const uint8_t *ks = p.Kc.steps + unit * p.h.slots * kStep, *vs = p.Vc.steps + unit * p.h.slots * kStep;
-
-    // the queries, on their way while the first copies are issued: one thread to eight elements of a head
-    constexpr int kPer = D / 8;                                          // threads of a head
-    constexpr int kQLoads = (H * kPer + kDecThreads - 1) / kDecThreads;
-    uint4 q_raw[kQLoads];
+    my_n = n_tiles > wid ? (n_tiles - wid + kDecWarps - 1) / kDecWarps : 0;
+    row0 = uint32_t((size_t(sh.b) * d.Hkv + sh.hk) * p.h.slots);
+    run_end = run_slot = 0;
 #pragma unroll
     for (int x = 0; x < kQLoads; ++x) {
       const int c = x * kDecThreads + tid, head = c / kPer;
@@ -555,56 +579,55 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
                                       p.q + (size_t(sh.b) * d.Hq + sh.hk * G + head) * D) + c % kPer)
                           : make_uint4(0, 0, 0, 0);
     }
-
-    // This warp's i-th tile into stage i % kStages: codes of K and V, steps of K and V.  Rows behind v1 are
-    // zeros.  The 16-byte pieces of V rows of 64 bytes are turned, so that the threads' reads below meet
-    // different banks.
-    constexpr int kPieces = kCode / 16, kRows = 32 / kPieces;   // of a row; rows of one copy of the warp
-    const int r0 = lane / kPieces, c0 = lane % kPieces;
-    auto dst_v = [&](int r) {   // place of this lane's piece of V row r in a stage
-      const int rv = kSplit ? r : (r & ~7) | (r >> 1 & 3) | (r & 1) << 2;
-      return kTile * kCode + rv * kCode + (kPieces == 4 ? c0 ^ (rv & 2) : c0) * 16;
-    };
-    const uint8_t *kc_l = kc + r0 * kCode + c0 * 16, *vc_l = vc + r0 * kCode + c0 * 16;
-    const uint8_t *ks_l = ks + lane * kStep, *vs_l = vs + lane * kStep;
-    const uint32_t dst0 = ring_u + r0 * kCode + c0 * 16, dst1 = ring_u + dst_v(r0);
-    const uint32_t dst2 = ring_u + 2 * kTile * kCode + lane * kStep;
-    int run_end = 0, run_slot = 0;   // entries up to run_end have slots run_slot + entry
-    auto issue = [&](int i) {
-      const int vb = v0 + (wid + i * kDecWarps) * kTile;
-      const uint32_t stage = (i % kStages) * S::kStageB;
-      if (vb >= run_end) run_slot = contiguous_from(vb, sq, d, &run_end) - vb;
-      if (vb + kTile <= min(run_end, v1)) {   // 32 neighbouring slots
-        const uint32_t slot = run_slot + vb;
-        cp_async_small<kStep>(stage + dst2, ks_l + uint64_t(slot) * kStep, kStep);
-        cp_async_small<kStep>(stage + dst2 + kTile * kStep, vs_l + uint64_t(slot) * kStep, kStep);
+  };
+  // This warp's i-th tile into stage i % kStages: codes of K and V, steps of K and V.  Rows behind v1 are
+  // zeros.  The 16-byte pieces of V rows of 64 bytes are turned, so that the threads' reads below meet
+  // different banks.
+  auto dst_v = [&](int r) {   // place of this lane's piece of V row r in a stage
+    const int rv = kSplit ? r : (r & ~7) | (r >> 1 & 3) | (r & 1) << 2;
+    return kTile * kCode + rv * kCode + (kPieces == 4 ? c0 ^ (rv & 2) : c0) * 16;
+  };
+  const uint32_t dst0 = ring_u + r0 * kCode + c0 * 16, dst1 = ring_u + dst_v(r0);
+  const uint32_t dst2 = ring_u + 2 * kTile * kCode + lane * kStep;
+  auto issue = [&](int i) {
+    const int vb = v0 + (wid + i * kDecWarps) * kTile;
+    const uint32_t stage = (i % kStages) * S::kStageB;
+    if (vb >= run_end) run_slot = contiguous_from(vb, sq, d, &run_end) - vb;
+    if (vb + kTile <= min(run_end, v1)) {   // 32 neighbouring slots
+      const uint32_t row = row0 + run_slot + vb;
+      const uint64_t codes = uint64_t(row) * kCode + lane * 16, steps_at = uint64_t(row + lane) * kStep;
+      cp_async_small<kStep>(stage + dst2, p.Kc.steps + steps_at, kStep);
+      cp_async_small<kStep>(stage + dst2 + kTile * kStep, p.Vc.steps + steps_at, kStep);
 #pragma unroll
-        for (int x = 0; x < kTile / kRows; ++x) {
-          cp_async16(stage + dst0 + x * kRows * kCode, kc_l + uint64_t(slot) * kCode + x * kRows * kCode, 16);
-          cp_async16(stage + dst1 + x * kRows * kCode, vc_l + uint64_t(slot) * kCode + x * kRows * kCode, 16);
-        }
-      } else {
-        const uint32_t ok = vb + lane < v1;
-        const int slot = virtual_to_slot(min(vb + lane, v1 - 1), sq, d);
-        cp_async_small<kStep>(stage + dst2, ks + size_t(slot) * kStep, ok * kStep);
-        cp_async_small<kStep>(stage + dst2 + kTile * kStep, vs + size_t(slot) * kStep, ok * kStep);
-#pragma unroll
-        for (int x = 0; x < kTile / kRows; ++x) {
-          const int r = x * kRows + r0;
-          const size_t off = size_t(__shfl_sync(0xffffffffu, slot, r)) * kCode + c0 * 16;
-          const uint32_t bytes = vb + r < v1 ? 16u : 0u;
-          cp_async16(stage + dst0 + x * kRows * kCode, kc + off, bytes);
-          cp_async16(stage + dst1 + x * kRows * kCode, vc + off, bytes);
-        }
+      for (int x = 0; x < kTile / kRows; ++x) {
+        cp_async16(stage + dst0 + x * kRows * kCode, p.Kc.codes + codes + x * kRows * kCode, 16);
+        cp_async16(stage + dst1 + x * kRows * kCode, p.Vc.codes + codes + x * kRows * kCode, 16);
       }
-    };
-    static_assert(kRows % 8 == 0, "a lane's places in the rows of a stage differ by whole copies");
+    } else {
+      const uint32_t ok = vb + lane < v1;
+      const uint32_t row = row0 + virtual_to_slot(min(vb + lane, v1 - 1), sq, d);
+      cp_async_small<kStep>(stage + dst2, p.Kc.steps + uint64_t(row) * kStep, ok * kStep);
+      cp_async_small<kStep>(stage + dst2 + kTile * kStep, p.Vc.steps + uint64_t(row) * kStep, ok * kStep);
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) {
-      if (s < my_n) issue(s);
+      for (int x = 0; x < kTile / kRows; ++x) {
+        const int r = x * kRows + r0;
+        const uint64_t off = uint64_t(__shfl_sync(0xffffffffu, row, r)) * kCode + c0 * 16;
+        const uint32_t bytes = vb + r < v1 ? 16u : 0u;
+        cp_async16(stage + dst0 + x * kRows * kCode, p.Kc.codes + off, bytes);
+        cp_async16(stage + dst1 + x * kRows * kCode, p.Vc.codes + off, bytes);
+      }
+    }
+  };
+  auto issue_tiles = [&](int from, int to) {
+    for (int i = from; i < to; ++i) {
+      if (i < my_n) issue(i);
       cp_async_commit();
     }
+  };
 
+  begin_unit();
+  issue_tiles(0, S::kEarly);
+  while (true) {
     // The queries as operand words: elements 32j + 8t ..
 #pragma unroll
     for (int x0 = 0; x0 < kQLoads; ++x0) {
@@ -664,7 +687,8 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       if (tt == 0) s_start[head * kGroups + j] = sum * (-8.f * 0x1p-9f);
       if (c % kPer == 0) s_factor[head] = p.scale_log2 * __uint_as_float(uint32_t(127 + 9 - e) << 23);
     }
-    __syncthreads();
+    __syncthreads();   // (and the merge before this unit is over: the last stages are free)
+    issue_tiles(S::kEarly, kStages - 1);
     uint32_t q_hi[NT][kGroups][2], q_lo[NT][kGroups][2];   // (kSplit: q_hi alone)
     float start[NT][kGroups][NE], factor[NT][NE];
 #pragma unroll
@@ -878,33 +902,17 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       }
     };
 
-    // One tile's values are multiplied while the next one's scores are: two chains of matrix products and
-    // unpacking that do not wait for each other.
     float sc[4][NT][NE];
-    if (my_n > 0) {
+    for (int i = 0; i < my_n; ++i) {
       cp_async_wait<kStages - 2>();
       __syncwarp();
-      scores(0, sc);
-      softmax(0, sc);
-    }
-    for (int i = 0; i + 1 < my_n; ++i) {
       if (i + kStages - 1 < my_n) issue(i + kStages - 1);   // (over tile i - 1, which all lanes are done with)
       cp_async_commit();
-      cp_async_wait<kStages - 2>();
-      __syncwarp();
-      float next[4][NT][NE];
-      scores(i + 1, next);
+      scores(i, sc);
+      softmax(i, sc);
       values(i, sc);
-      softmax(i + 1, next);
-#pragma unroll
-      for (int y = 0; y < 4; ++y)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < NE; ++e) sc[y][n][e] = next[y][n][e];
       __syncwarp();
     }
-    if (my_n > 0) values(my_n - 1, sc);
     cp_async_wait<0>();
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -912,16 +920,17 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       for (int e = 0; e < NE; ++e)
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l_sum[n][e] += __shfl_xor_sync(0xffffffffu, l_sum[n][e], o);
-    __syncthreads();  // all warps are out of their rings
 
-    // the warps' results, head by head, then merged: the unit's output, or a part of it
-    float2* sm_ml = reinterpret_cast<float2*>(dec_smem);
-    float* sm_acc = reinterpret_cast<float*>(dec_smem + kDecWarps * H * sizeof(float2));
+    // The warps' results, head by head, behind the stages that the next unit's first tiles go to; then merged:
+    // the unit's output, or a part of it.
+    constexpr int kWarpB = kStages * S::kStageB, kResultB = S::kEarly * S::kStageB;
+    auto ml_of = [&](int w) { return reinterpret_cast<float2*>(dec_smem + w * kWarpB + kResultB); };
+    auto acc_of = [&](int w) { return reinterpret_cast<float*>(dec_smem + w * kWarpB + kResultB + H * 8); };
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int e = 0; e < NE; ++e)
-        if (g == 0) sm_ml[wid * H + (kSplit ? t : 8 * n + 2 * t + e)] = make_float2(m_ref[n][e], l_sum[n][e]);
+        if (g == 0) ml_of(wid)[kSplit ? t : 8 * n + 2 * t + e] = make_float2(m_ref[n][e], l_sum[n][e]);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int head = 8 * n + 2 * t + e;
@@ -929,76 +938,95 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
 #pragma unroll
           for (int j = 0; j < 2 * kGroups; ++j) {
             const float off = 136.f * ones[j / 2][n][e];
-            *reinterpret_cast<float2*>(sm_acc + (wid * H + head) * D + (j / 2) * kGroup + 4 * g + 2 * (j & 1)) =
+            *reinterpret_cast<float2*>(acc_of(wid) + head * D + (j / 2) * kGroup + 4 * g + 2 * (j & 1)) =
                 make_float2(oacc[j][n][e] - off, oacc[j][n][e + 2] - off);
           }
         }
       }
     }
-    __syncthreads();
     const bool head_cut = sh.step > 0, tail_cut = sh.step + n_steps < steps;
-    const size_t part = 2 * size_t(blockIdx.x) + (head_cut ? 0 : 1);
+    const size_t part = 2 * size_t(blockIdx.x) + (head_cut ? 0 : 1), out0 = size_t(sh.b) * d.Hq + sh.hk * G;
+    if (tail_cut && !head_cut) {
+      // the CTA that has step e - 1, where e = end + what is left of the unit: the last one that starts before e
+      const int64_t e = sh.end + steps - (sh.step + n_steps), ctas = min(int64_t(gridDim.x), sh.total);
+      ends = make_int4(sh.b, sh.hk, int((e * ctas + sh.total - 1) / sh.total) - 1, 0);
+    }
+    sh.left -= n_steps;
+    sh.step = 0;
+    if (++sh.hk == d.Hkv) { sh.hk = 0; ++sh.b; }
+    const bool more = sh.left > 0;
+    if (more) {
+      begin_unit();
+      issue_tiles(0, S::kEarly);
+    }
+    __syncthreads();
     for (int idx = tid; idx < G * D; idx += kDecThreads) {
       const int hd = idx / D, e = idx % D;
       float mm = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) mm = fmaxf(mm, sm_ml[w * H + hd].x);
+      for (int w = 0; w < kDecWarps; ++w) mm = fmaxf(mm, ml_of(w)[hd].x);
       float ll = 0.f, aa = 0.f;
 #pragma unroll
       for (int w = 0; w < kDecWarps; ++w) {
-        const float2 ml = sm_ml[w * H + hd];
+        const float2 ml = ml_of(w)[hd];
         if (ml.y == 0.f) continue;   // a warp without entries (a NaN goes through)
         const float f = ml.x == -INFINITY ? 1.f : ex2(ml.x - mm);
         ll += ml.y * f;
-        aa += sm_acc[(w * H + hd) * D + e] * f;
+        aa += acc_of(w)[hd * D + e] * f;
       }
       if (head_cut || tail_cut) {
         p.part_acc[(part * G + hd) * D + e] = aa;
         if (e == 0) p.part_ml[part * G + hd] = make_float2(mm, ll);
       } else {
-        const size_t row = size_t(sh.b) * d.Hq + sh.hk * G + hd;
-        p.o[row * D + e] = __float2bfloat16(ll != 0.f ? aa / ll : 0.f);
-        if (p.lse && e == 0) p.lse[row] = ll != 0.f ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
+        p.o[(out0 + hd) * D + e] = __float2bfloat16(ll != 0.f ? aa / ll : 0.f);
+        if (p.lse && e == 0) p.lse[out0 + hd] = ll != 0.f ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
       }
     }
-    if (head_cut) { ends.x = sh.b; ends.y = sh.hk; }
-    else if (tail_cut) { ends.z = sh.b; ends.w = sh.hk; }
-    __syncthreads();  // the merge buffers become the rings again
-
-    sh.left -= n_steps;
-    sh.step = 0;
-    if (++sh.hk == d.Hkv) { sh.hk = 0; ++sh.b; }
+    if (!more) break;
   }
-  if (tid == 0) p.ends[blockIdx.x] = ends;
+  if (tid == 0 && !p.whole) p.ends[blockIdx.x] = ends;
 }
 
-// grid (CTAs of decode_quant, G), D threads.  Joins the parts of a unit that was cut: the block of the CTA
-// that had its first steps, with the CTAs behind it that had the others.
-template <int D>
-__global__ void __launch_bounds__(D) decode_quant_join(const __grid_constant__ QuantDecodeParams p) {
+// grid (CTAs of decode_quant, G).  Joins the parts of a unit that was cut: the block of the CTA that began it,
+// with the parts of the CTAs behind.  LANES threads share an element's parts.
+template <int D, int LANES>
+__global__ void __launch_bounds__(D* LANES) decode_quant_join(const __grid_constant__ QuantDecodeParams p) {
+  constexpr int kLanes = LANES;
+  __shared__ float2 s_ml[kLanes];
+  __shared__ float s_acc[kLanes][D];
   wait_for_prior();
   const sepllm_cache_desc& d = p.h.desc;
-  const int G = d.Hq / d.Hkv, hd = blockIdx.y, e = threadIdx.x, i = blockIdx.x;
-  const int4 mine = p.ends[i];
-  if (mine.z < 0) return;
-  int last = i;
-  while (last + 1 < int(gridDim.x)) {
-    const int4 x = p.ends[last + 1];
-    if (x.x != mine.z || x.y != mine.w) break;
-    ++last;
+  const int G = d.Hq / d.Hkv, hd = blockIdx.y, e = threadIdx.x % D, y = threadIdx.x / D, i = blockIdx.x;
+  const int4 unit = p.ends[i];
+  if (unit.x < 0) return;
+  float mm = -INFINITY, ll = 0.f, aa = 0.f;
+#pragma unroll 4
+  for (int k = i + y; k <= unit.z; k += kLanes) {
+    const size_t part = (2 * size_t(k) + (k == i)) * G + hd;
+    const float2 ml = p.part_ml[part];
+    const float acc = p.part_acc[part * D + e];
+    const float m = fmaxf(mm, ml.x);
+    const float f0 = mm == m ? 1.f : ex2(mm - m), f1 = ml.x == m ? 1.f : ex2(ml.x - m);
+    ll = ll * f0 + ml.y * f1;
+    aa = aa * f0 + acc * f1;
+    mm = m;
   }
-  const size_t first = 2 * size_t(i) + 1;
-  float mm = p.part_ml[first * G + hd].x;
-  for (int k = i + 1; k <= last; ++k) mm = fmaxf(mm, p.part_ml[2 * size_t(k) * G + hd].x);
-  float ll = 0.f, aa = 0.f;
-  for (int k = i; k <= last; ++k) {
-    const size_t part = k == i ? first : 2 * size_t(k);
-    const float2 ml = p.part_ml[part * G + hd];
-    const float f = ml.x == -INFINITY ? 1.f : ex2(ml.x - mm);
+  if (e == 0) s_ml[y] = make_float2(mm, ll);
+  s_acc[y][e] = aa;
+  __syncthreads();
+  if (y != 0) return;
+#pragma unroll
+  for (int k = 1; k < kLanes; ++k) mm = fmaxf(mm, s_ml[k].x);
+  ll = aa = 0.f;
+#pragma unroll
+  for (int k = 0; k < kLanes; ++k) {
+    const float2 ml = s_ml[k];
+    if (ml.y == 0.f) continue;   // no parts (a NaN goes through)
+    const float f = ml.x == mm ? 1.f : ex2(ml.x - mm);
     ll += ml.y * f;
-    aa += p.part_acc[(part * G + hd) * D + e] * f;
+    aa += s_acc[k][e] * f;
   }
-  const size_t row = size_t(mine.z) * d.Hq + mine.w * G + hd;
+  const size_t row = size_t(unit.x) * d.Hq + unit.y * G + hd;
   p.o[row * D + e] = __float2bfloat16(ll != 0.f ? aa / ll : 0.f);
   if (p.lse && e == 0) p.lse[row] = ll != 0.f ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
 }
@@ -1015,18 +1043,22 @@ auto with_shape(const sepllm_cache_desc& d, F f) {
   return d.d == 128 ? heads(std::integral_constant<int, 128>{}) : heads(std::integral_constant<int, 64>{});
 }
 
-// CTAs of a decode: as many as are resident, or one per step of the fullest caches.
-int decode_quant_ctas(const sepllm_cache_desc& d) {
-  const int64_t steps = (int64_t(d.c) + kStepRows - 1) / kStepRows;
+// Caches of few steps: every unit is one CTA's, and nothing is left to join (WHOLE).
+bool decode_quant_whole(const sepllm_cache_desc& d) { return d.c <= 4 * kStepRows; }
+
+// CTAs of a decode: one per unit, or as many as are resident, or one per step of the fullest caches.
+int64_t decode_quant_ctas(const sepllm_cache_desc& d) {
+  const int64_t units = int64_t(d.B) * d.Hkv, steps = (int64_t(d.c) + kStepRows - 1) / kStepRows;
+  if (decode_quant_whole(d)) return units;
   const int resident = with_shape(d, [](auto D, auto H) { return DecodeShape<D(), H()>::kResident; });
-  return int(std::min<int64_t>(resident * kSmCount, int64_t(d.B) * d.Hkv * steps));
+  return std::min<int64_t>(resident * kSmCount, units * steps);
 }
 
 struct QuantDecodeLayout {
   size_t off_ml, off_acc, bytes;
 };
 QuantDecodeLayout decode_quant_layout(const sepllm_cache_desc& d) {
-  const size_t ctas = size_t(decode_quant_ctas(d)), rows = 2 * ctas * (d.Hq / d.Hkv);
+  const size_t ctas = decode_quant_whole(d) ? 0 : size_t(decode_quant_ctas(d)), rows = 2 * ctas * (d.Hq / d.Hkv);
   QuantDecodeLayout l;
   l.off_ml = kAlign + align_up(ctas * sizeof(int4));
   l.off_acc = l.off_ml + align_up(rows * sizeof(float2));
@@ -1037,13 +1069,18 @@ QuantDecodeLayout decode_quant_layout(const sepllm_cache_desc& d) {
 template <int D, int H>
 sepllm_status launch_decode_quant(const QuantDecodeParams& p, cudaStream_t stream) {
   constexpr int smem = DecodeShape<D, H>::kSmem;
-  const unsigned ctas = unsigned(decode_quant_ctas(p.h.desc));
+  const unsigned ctas = unsigned(decode_quant_ctas(p.h.desc));   // (65 535^2 at most, checked by the caller)
   if (smem > 48 * 1024)
     SEPLLM_CUDA_TRY(cudaFuncSetAttribute(decode_quant<D, H>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  decode_quant<D, H><<<ctas, kDecThreads, smem, stream>>>(p);
-  SEPLLM_CUDA_TRY(cudaGetLastError());
+  SEPLLM_CUDA_TRY(launch_overlapped(decode_quant<D, H>, dim3(ctas), kDecThreads, smem, stream, p));
+  if (p.whole) return SEPLLM_OK;
   const dim3 grid(ctas, p.h.desc.Hq / p.h.desc.Hkv);
-  SEPLLM_CUDA_TRY(launch_overlapped(decode_quant_join<D>, grid, D, 0, stream, p));
+  // Few units, cut over many CTAs, are joined by several threads to an element (28 parts: 5 us less than by one);
+  // otherwise by one, so that all blocks find room beside decode_quant (4 us less for 256 units in two parts).
+  const int64_t units = int64_t(p.h.desc.B) * p.h.desc.Hkv;
+  const bool many = ctas > 8 * units;
+  auto join = many ? decode_quant_join<D, 512 / D> : decode_quant_join<D, 1>;
+  SEPLLM_CUDA_TRY(launch_overlapped(join, grid, many ? 512 : D, 0, stream, p));
   return SEPLLM_OK;
 }
 
@@ -1082,10 +1119,10 @@ extern "C" sepllm_status sepllm_cache_update_quant(const sepllm_cache_desc* desc
   auto kernel = desc->d == 128 ? quant_update<128> : quant_update<64>;
   if (smem > 40 * 1024)
     SEPLLM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
-  kernel<<<dim3(desc->B, desc->Hkv), kUpdThreads, smem, static_cast<cudaStream_t>(stream_)>>>(
-      h, static_cast<uint8_t*>(state), quant_rows(h, Kc), quant_rows(h, Vc),
-      static_cast<const __nv_bfloat16*>(k_new), static_cast<const __nv_bfloat16*>(v_new), new_token_ids, sep, max_past);
-  SEPLLM_CUDA_TRY(cudaGetLastError());
+  SEPLLM_CUDA_TRY(launch_overlapped(kernel, dim3(desc->B, desc->Hkv), kUpdThreads, smem, static_cast<cudaStream_t>(stream_),
+                                    h, static_cast<uint8_t*>(state), quant_rows(h, Kc), quant_rows(h, Vc),
+                                    static_cast<const __nv_bfloat16*>(k_new),
+                                    static_cast<const __nv_bfloat16*>(v_new), new_token_ids, sep, max_past));
   return SEPLLM_OK;
 }
 
@@ -1128,10 +1165,9 @@ extern "C" sepllm_status sepllm_cache_entries_quant(const sepllm_cache_desc* des
   if (desc->B > 65535 || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
   const dim3 grid((desc->c + kCopyRows - 1) / kCopyRows, desc->Hkv, desc->B);   // Size_run never passes c
   auto kernel = desc->d == 128 ? quant_entries<128> : quant_entries<64>;
-  kernel<<<grid, kCopyThreads, 0, static_cast<cudaStream_t>(stream_)>>>(
-      h, static_cast<const uint8_t*>(state), quant_rows(h, Kc), quant_rows(h, Vc), n, static_cast<__nv_bfloat16*>(K),
-      static_cast<__nv_bfloat16*>(V), length);
-  SEPLLM_CUDA_TRY(cudaGetLastError());
+  SEPLLM_CUDA_TRY(launch_overlapped(kernel, grid, kCopyThreads, 0, static_cast<cudaStream_t>(stream_), h,
+                                    static_cast<const uint8_t*>(state), quant_rows(h, Kc), quant_rows(h, Vc), n,
+                                    static_cast<__nv_bfloat16*>(K), static_cast<__nv_bfloat16*>(V), length));
   return SEPLLM_OK;
 }
 
@@ -1154,6 +1190,7 @@ extern "C" sepllm_status sepllm_decode_quant(const sepllm_cache_desc* desc, floa
       !aligned(lse, 4) || !aligned(workspace, kAlign))
     return SEPLLM_INVALID_ARG;
   if (desc->B > 65535 || desc->Hkv > 65535) return SEPLLM_UNSUPPORTED;
+  if (size_t(desc->B) * desc->Hkv * p.h.slots > 0xffffffffu) return SEPLLM_UNSUPPORTED;   // rows have 32-bit numbers
   const QuantDecodeLayout l = decode_quant_layout(*desc);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p.state = static_cast<const uint8_t*>(state);
@@ -1167,6 +1204,7 @@ extern "C" sepllm_status sepllm_decode_quant(const sepllm_cache_desc* desc, floa
   p.part_ml = reinterpret_cast<float2*>(ws + l.off_ml);
   p.part_acc = reinterpret_cast<float*>(ws + l.off_acc);
   p.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(float(desc->d))) * 1.4426950408889634f;
+  p.whole = decode_quant_whole(*desc);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   return with_shape(*desc, [&](auto D, auto H) { return launch_decode_quant<D(), H()>(p, stream); });
 }

@@ -152,6 +152,8 @@ __device__ __forceinline__ float row_sum(float x, int per_row, int first) {
 
 template <class Tin, class Tout, bool HALF, int PER_ROW>
 __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant__ NormParams np) {
+  let_dependents_start();
+  wait_for_prior();
   const RopeParams& p = np.r;
   const int per_row = PER_ROW ? PER_ROW : p.d / 16, rows = 32 / per_row;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
@@ -301,6 +303,8 @@ __device__ __forceinline__ void lane_rotate(const float2 (&cs)[2], float (&x)[8]
 
 template <class Tin, class Tout>
 __global__ void __launch_bounds__(kRopeThreads) norm_any(const __grid_constant__ NormParams np) {
+  let_dependents_start();
+  wait_for_prior();
   const RopeParams& p = np.r;
   const int lane = threadIdx.x & 31;
   const int64_t n = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
@@ -384,6 +388,7 @@ template <class Tx, class Tg, bool HALF, int PER_ROW>
 __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(const __grid_constant__ NormParams np) {
   __shared__ __align__(16) float s_part[2048];   // [row of the block][d]
   __shared__ __align__(16) float s_w[128];
+  wait_for_prior();
   const RopeParams& p = np.r;
   const int per_row = PER_ROW ? PER_ROW : p.d / 16, rows = 32 / per_row;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
@@ -510,6 +515,7 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(cons
 template <class Tx, class Tg>
 __global__ void __launch_bounds__(kRopeThreads) norm_bwd_any(const __grid_constant__ NormParams np) {
   __shared__ float s_part[kWarps][128];
+  wait_for_prior();
   const RopeParams& p = np.r;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const Lane s = lane_elements(p, np.half, lane);
@@ -565,6 +571,7 @@ __global__ void __launch_bounds__(kRopeThreads) norm_bwd_any(const __grid_consta
 // grid ceil(2 d / 32): adds the blocks' sums, a column to a lane, in a fixed order.
 __global__ void __launch_bounds__(1024) norm_bwd_sum(const __grid_constant__ NormParams np) {
   __shared__ float s_sum[32][33];
+  let_dependents_start();
   wait_for_prior();
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, d = np.r.d;
   float sum = 0.f;
@@ -601,26 +608,26 @@ void fill_norm(const sepllm_rope_desc* d, const sepllm_qknorm_desc* n, NormParam
   p->inv_d = 1.f / float(d->d);
 }
 
+// (every kernel is launched while the one before it ends, and waits for it first)
 template <class Tin, class Tout>
-void launch_norm(const NormParams& p, bool rows, dim3 grid, cudaStream_t stream) {
-  if (!rows) {
-    norm_any<Tin, Tout><<<grid, kRopeThreads, 0, stream>>>(p);
-    return;
-  }
+cudaError_t launch_norm(const NormParams& p, bool rows, dim3 grid, cudaStream_t stream) {
 #define SEPLLM_NORM(N) (p.half ? norm_rows<Tin, Tout, true, N> : norm_rows<Tin, Tout, false, N>)
-  auto kernel = p.r.d == 128 ? SEPLLM_NORM(8) : p.r.d == 64 ? SEPLLM_NORM(4) : SEPLLM_NORM(0);
+  auto kernel = !rows           ? norm_any<Tin, Tout>
+                : p.r.d == 128 ? SEPLLM_NORM(8)
+                : p.r.d == 64  ? SEPLLM_NORM(4)
+                               : SEPLLM_NORM(0);
 #undef SEPLLM_NORM
-  kernel<<<grid, kRopeThreads, 0, stream>>>(p);
+  return launch_overlapped(kernel, grid, kRopeThreads, 0, stream, p);
 }
 template <class Tx, class Tg>
-void launch_norm_bwd(const NormParams& p, bool rows, cudaStream_t stream) {
+cudaError_t launch_norm_bwd(const NormParams& p, bool rows, cudaStream_t stream) {
 #define SEPLLM_NORM(N) (p.half ? norm_bwd_rows<Tx, Tg, true, N> : norm_bwd_rows<Tx, Tg, false, N>)
   auto kernel = !rows           ? norm_bwd_any<Tx, Tg>
                 : p.r.d == 128 ? SEPLLM_NORM(8)
                 : p.r.d == 64  ? SEPLLM_NORM(4)
                                : SEPLLM_NORM(0);
 #undef SEPLLM_NORM
-  kernel<<<unsigned(p.grid), kRopeThreads, 0, stream>>>(p);
+  return launch_overlapped(kernel, dim3(unsigned(p.grid)), kRopeThreads, 0, stream, p);
 }
 
 }  // namespace
@@ -648,11 +655,10 @@ extern "C" sepllm_status sepllm_qknorm_rope_fwd(const sepllm_rope_desc* desc, co
   if (groups > 65535) return SEPLLM_UNSUPPORTED;
   const dim3 grid{unsigned(blocks), unsigned(groups)};
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  if (dt_in == 0 && dt_out == 0) launch_norm<__nv_bfloat16, __nv_bfloat16>(p, rows, grid, stream);
-  else if (dt_in == 0) launch_norm<__nv_bfloat16, float>(p, rows, grid, stream);
-  else if (dt_out == 0) launch_norm<float, __nv_bfloat16>(p, rows, grid, stream);
-  else launch_norm<float, float>(p, rows, grid, stream);
-  SEPLLM_CUDA_TRY(cudaGetLastError());
+  SEPLLM_CUDA_TRY(dt_in == 0 ? (dt_out == 0 ? launch_norm<__nv_bfloat16, __nv_bfloat16>(p, rows, grid, stream)
+                                            : launch_norm<__nv_bfloat16, float>(p, rows, grid, stream))
+                             : (dt_out == 0 ? launch_norm<float, __nv_bfloat16>(p, rows, grid, stream)
+                                            : launch_norm<float, float>(p, rows, grid, stream)));
   return SEPLLM_OK;
 }
 
@@ -704,11 +710,10 @@ extern "C" sepllm_status sepllm_qknorm_rope_bwd(const sepllm_rope_desc* desc, co
     p.grid = std::max(p.grid, p.blocks[w]);
   }
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  if (dt_out == 0 && dt_in == 0) launch_norm_bwd<__nv_bfloat16, __nv_bfloat16>(p, rows, stream);
-  else if (dt_out == 0) launch_norm_bwd<__nv_bfloat16, float>(p, rows, stream);
-  else if (dt_in == 0) launch_norm_bwd<float, __nv_bfloat16>(p, rows, stream);
-  else launch_norm_bwd<float, float>(p, rows, stream);
-  SEPLLM_CUDA_TRY(cudaGetLastError());
+  SEPLLM_CUDA_TRY(dt_out == 0 ? (dt_in == 0 ? launch_norm_bwd<__nv_bfloat16, __nv_bfloat16>(p, rows, stream)
+                                            : launch_norm_bwd<__nv_bfloat16, float>(p, rows, stream))
+                              : (dt_in == 0 ? launch_norm_bwd<float, __nv_bfloat16>(p, rows, stream)
+                                            : launch_norm_bwd<float, float>(p, rows, stream)));
   if (dwq || dwk)
     SEPLLM_CUDA_TRY(launch_overlapped(norm_bwd_sum, dim3(2 * desc->d / 32), 1024, 0, stream, p));
   return SEPLLM_OK;
