@@ -335,24 +335,26 @@ def _rope_views(desc, tensors, what, device=None):
     """The views of (q, k, v), or of inputs and outputs, one bytes object per three tensors."""
     B, L, d = desc.B, desc.L, desc.d
     q_shape, k_shape = (B, desc.Hq, L, d), (B, desc.Hkv, L, d)
-    vals = []
-    for i, t in enumerate(tensors):
+    vals, shapes, dtypes = [], (q_shape, k_shape, k_shape) * 3, _ROPE_DTYPES
+    for t, shape in zip(tensors, shapes):
         if t is None:
             vals += (0, 0, 0, 0, 0, 0)
             continue
         sb, sh, sl, se = t.stride()
-        dtype = _ROPE_DTYPES.get(t.dtype)
-        if t.shape != (k_shape if i % 3 else q_shape):
-            raise ValueError(f"{what}: shape {tuple(t.shape)}, the descriptor says "
-                             f"{k_shape if i % 3 else q_shape}")
-        if dtype is None or se != 1:
-            raise ValueError(f"{what}: bf16 or fp32 with contiguous head vectors, not {t.dtype} with strides "
-                             f"{t.stride()}")
-        if device is not None and t.get_device() != device:
-            raise ValueError(f"{what}: tensor on {t.device}, current device is cuda:{device}: make the tensors' "
-                             "device current for the call")
+        dtype = dtypes.get(t.dtype)
+        if t.shape != shape or dtype is None or se != 1 or (device is not None and t.get_device() != device):
+            _refuse_view(t, shape, what, device)
         vals += (t.data_ptr(), sb, sh, sl, dtype, 0)
     return [_ROPE_VIEWS.pack(*vals[i:i + 18]) for i in range(0, len(vals), 18)]
+
+
+def _refuse_view(t, shape, what, device):
+    if t.shape != shape:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, the descriptor says {shape}")
+    if t.dtype not in _ROPE_DTYPES or t.stride(3) != 1:
+        raise ValueError(f"{what}: bf16 or fp32 with contiguous head vectors, not {t.dtype} with strides {t.stride()}")
+    raise ValueError(f"{what}: tensor on {t.device}, current device is cuda:{device}: make the tensors' device current "
+                     "for the call")
 
 
 def _positions(where, desc, positions):
@@ -385,19 +387,25 @@ def sepllm_rope_bwd(desc: RopeDesc, positions, dq_out, dk_out, dv_out, dq, dk, d
 
 
 # ---------------------------------------------------------------- head norms with rotary positions
-def _qknorm(where, desc, norm, positions, device):
-    """Puts the weights' addresses into the descriptor; the address of `positions`."""
-    for i, w in enumerate(norm.weights):
-        if w is not None and w.shape != (desc.d,):
-            raise ValueError(f"{where}: weights are [{desc.d}], not {tuple(w.shape)}")
-    norm.wq, norm.wk = (a or None for a in _addresses(where, norm.weights))
-    return _positions(where, desc, positions)
+def _weights(where, desc, norm, device):
+    """Puts the weights' addresses into the descriptor."""
+    addresses = []
+    for w in norm.weights:
+        if w is None:
+            addresses.append(None)
+            continue
+        if w.shape != (desc.d,) or not w.is_contiguous() or w.get_device() != device:
+            raise ValueError(f"{where}: weights are contiguous [{desc.d}] tensors of the current device, not {tuple(w.shape)} "
+                             f"with stride {w.stride()} on {w.device}")
+        addresses.append(w.data_ptr())
+    norm.wq, norm.wk = addresses
 
 
 def sepllm_qknorm_rope_fwd(desc: RopeDesc, norm: QkNorm, positions, q, k, v, q_out, k_out, v_out):
     """sepllm_rope_fwd with every head of q and k normalised first.  Other arguments as there."""
     where, device = "sepllm_qknorm_rope_fwd", torch.cuda.current_device()
-    pos = _qknorm(where, desc, norm, positions, device)
+    _weights(where, desc, norm, device)
+    pos = _positions(where, desc, positions)
     ins, outs = _rope_views(desc, (q, k, v, q_out, k_out, v_out), where, device)
     _check(lib().sepllm_qknorm_rope_fwd(C.byref(desc), C.byref(norm), pos, ins, outs,
                                         torch._C._cuda_getCurrentRawStream(device)), where)
@@ -415,7 +423,8 @@ def sepllm_qknorm_rope_bwd(desc: RopeDesc, norm: QkNorm, positions, q, k, dq_out
     """Gradients of sepllm_qknorm_rope_fwd's inputs and weights; q, k: the forward's inputs; dwq, dwk: fp32 [d]
     or None."""
     where, device = "sepllm_qknorm_rope_bwd", torch.cuda.current_device()
-    pos = _qknorm(where, desc, norm, positions, device)
+    _weights(where, desc, norm, device)
+    pos = _positions(where, desc, positions)
     xs, ins, outs = _rope_views(desc, (q, k, None, dq_out, dk_out, dv_out, dq, dk, dv), where, device)
     _expect(where, ("dwq", dwq, (desc.d,), torch.float32), ("dwk", dwk, (desc.d,), torch.float32))
     _check(lib().sepllm_qknorm_rope_bwd(C.byref(desc), C.byref(norm), pos, xs, ins, outs,

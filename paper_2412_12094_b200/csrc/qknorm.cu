@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(cons
         xs = static_cast<const Tx*>(np.x[w]) + ahead.b * np.xb[w] + ahead.l * np.xl[w] + ahead.h * np.xh[w] + s.c0;
       };
       auto to_at = [&]() { dst = static_cast<Tx*>(y.out) + at.b * y.ob + at.l * y.ol + at.h * y.oh + s.c0; };
-      constexpr int kDepth = sizeof(Tx) + sizeof(Tg) == 4 ? 3 : 2;
+      constexpr int kDepth = 2;
       Eight<Tg> gu[kDepth]{}, gv[kDepth]{};
       Eight<Tx> xu[kDepth]{}, xv[kDepth]{};
       auto fetch = [&](int i) {
