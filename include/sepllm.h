@@ -367,7 +367,8 @@ sepllm_status sepllm_qknorm_rope_fwd(const sepllm_rope_desc* desc, const sepllm_
  *   in    host array of three views, dL/d(outputs); out, dL/d(inputs), of x's type
  *   dwq, dwk  dev fp32 [d], written (not added to); NULL: not wanted, and where
  *         there are no weights
- *   workspace  dev, sepllm_qknorm_rope_bwd_workspace_bytes, 256-byte aligned
+ *   workspace  dev, sepllm_qknorm_rope_bwd_workspace_bytes, 256-byte aligned; calls
+ *         that may overlap need one each
  * A tensor of Q or K is there in x, in and out, or in none of them (its dw is then
  * 0).  out may be in or x (same data, strides and dtype).  Deterministic: no
  * floating-point atomics. */
@@ -582,8 +583,8 @@ sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, const sepllm_
  *           bytes on, steps bf16 [B][Hkv][slots][d / 32].  A row's codes q + 8
  *           stand two to a byte, low half first; element e of group j is the row's
  *           ((e / m) * (d / 32) + j) * m + e % m -th, m = 8 in Kc and 4 in Vc.
- * Positions taken inside the cache (sepllm_cache_update_rope) have no 4-bit form:
- * keys are handed over with their positions encoded. */
+ * c + s up to 2^30.  Positions taken inside the cache (sepllm_cache_update_rope)
+ * have no 4-bit form: keys are handed over with their positions encoded. */
 
 /* state_bytes: the state buffer; kv_bytes: ONE of Kc / Vc. */
 sepllm_status sepllm_cache_bytes_quant(const sepllm_cache_desc* desc, size_t* state_bytes,
@@ -616,7 +617,8 @@ sepllm_status sepllm_cache_entries_quant(const sepllm_cache_desc* desc, const vo
  * held values.  A sequence with no entry gets o = 0 and lse = -inf.  A query
  * element that is not finite, or beyond 2^117, makes its row NaN.  workspace of
  * sepllm_decode_quant_workspace_bytes, 256-byte aligned (its first word is the
- * device status; always 0); other arguments as sepllm_decode and above. */
+ * device status; always 0); calls that may overlap need one each.  Other arguments
+ * as sepllm_decode and above. */
 sepllm_status sepllm_decode_quant_workspace_bytes(const sepllm_cache_desc* desc, size_t* bytes);
 sepllm_status sepllm_decode_quant(const sepllm_cache_desc* desc, float scale, const void* q,
                                   const void* state, const void* Kc, const void* Vc, void* o,

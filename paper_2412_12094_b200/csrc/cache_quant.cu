@@ -33,6 +33,12 @@ struct QuantRows {
 inline size_t quant_code_bytes(const sepllm_cache_header& h) {
   return align_up(size_t(h.desc.B) * h.desc.Hkv * h.slots * (h.desc.d / 2));
 }
+// What the calls take: ring starts and entries are added in 32 bits.
+inline sepllm_status check_quant(const sepllm_cache_desc* d, sepllm_cache_header* h) {
+  const sepllm_status st = fill_cache_header(d, h);
+  if (st != SEPLLM_OK) return st;
+  return int64_t(d->c) + d->s > 1 << 30 ? SEPLLM_UNSUPPORTED : SEPLLM_OK;
+}
 inline QuantRows<uint8_t> quant_rows(const sepllm_cache_header& h, void* buf) {
   uint8_t* p = static_cast<uint8_t*>(buf);
   return {p, p + quant_code_bytes(h)};
@@ -1043,7 +1049,7 @@ auto with_shape(const sepllm_cache_desc& d, F f) {
   return d.d == 128 ? heads(std::integral_constant<int, 128>{}) : heads(std::integral_constant<int, 64>{});
 }
 
-// Caches of few steps: every unit is one CTA's, and nothing is left to join (WHOLE).
+// Caches of few steps: every unit is one CTA's, and nothing is left to join.
 bool decode_quant_whole(const sepllm_cache_desc& d) { return d.c <= 4 * kStepRows; }
 
 // CTAs of a decode: one per unit, or as many as are resident, or one per step of the fullest caches.
@@ -1075,8 +1081,8 @@ sepllm_status launch_decode_quant(const QuantDecodeParams& p, cudaStream_t strea
   SEPLLM_CUDA_TRY(launch_overlapped(decode_quant<D, H>, dim3(ctas), kDecThreads, smem, stream, p));
   if (p.whole) return SEPLLM_OK;
   const dim3 grid(ctas, p.h.desc.Hq / p.h.desc.Hkv);
-  // Few units, cut over many CTAs, are joined by several threads to an element (28 parts: 5 us less than by one);
-  // otherwise by one, so that all blocks find room beside decode_quant (4 us less for 256 units in two parts).
+  // Few units, cut over many CTAs, are joined by several threads to an element (28 parts: 8 us less than by one);
+  // otherwise by one, so that all blocks find room beside decode_quant (1 us less for 256 units in two parts).
   const int64_t units = int64_t(p.h.desc.B) * p.h.desc.Hkv;
   const bool many = ctas > 8 * units;
   auto join = many ? decode_quant_join<D, 512 / D> : decode_quant_join<D, 1>;
@@ -1106,7 +1112,7 @@ extern "C" sepllm_status sepllm_cache_update_quant(const sepllm_cache_desc* desc
                                                    int32_t n_sep, const void* k_new, const void* v_new,
                                                    void* stream_) {
   sepllm_cache_header h;
-  sepllm_status st = fill_cache_header(desc, &h);
+  sepllm_status st = check_quant(desc, &h);
   if (st != SEPLLM_OK) return st;
   if (!state || !Kc || !Vc || !new_token_ids || !k_new || !v_new) return SEPLLM_INVALID_ARG;
   if (!aligned(state, kAlign) || !aligned(Kc, kAlign) || !aligned(Vc, kAlign) || !aligned(k_new, 16) ||
@@ -1131,7 +1137,7 @@ extern "C" sepllm_status sepllm_cache_from_prompt_quant(const sepllm_cache_desc*
                                                         const void* V, void* state, void* Kc, void* Vc,
                                                         void* stream_) {
   sepllm_cache_header h;
-  sepllm_status st = fill_cache_header(desc, &h);
+  sepllm_status st = check_quant(desc, &h);
   if (st != SEPLLM_OK) return st;
   sepllm_index_header ih;
   if ((st = fill_index_header(idesc, &ih)) != SEPLLM_OK) return st;
@@ -1155,7 +1161,7 @@ extern "C" sepllm_status sepllm_cache_entries_quant(const sepllm_cache_desc* des
                                                     const void* Vc, int32_t n, void* K, void* V, int32_t* length,
                                                     void* stream_) {
   sepllm_cache_header h;
-  const sepllm_status st = fill_cache_header(desc, &h);
+  const sepllm_status st = check_quant(desc, &h);
   if (st != SEPLLM_OK) return st;
   if (n < 1 || !state || !Kc || !Vc || !K || !V) return SEPLLM_INVALID_ARG;
   if (!aligned(state, kAlign) || !aligned(Kc, kAlign) || !aligned(Vc, kAlign) || !aligned(K, 16) || !aligned(V, 16) ||
@@ -1183,7 +1189,7 @@ extern "C" sepllm_status sepllm_decode_quant(const sepllm_cache_desc* desc, floa
                                              const void* state, const void* Kc, const void* Vc, void* o, float* lse,
                                              void* workspace, void* stream_) {
   QuantDecodeParams p{};
-  const sepllm_status st = fill_cache_header(desc, &p.h);
+  const sepllm_status st = check_quant(desc, &p.h);
   if (st != SEPLLM_OK) return st;
   if (!q || !state || !Kc || !Vc || !o || !workspace) return SEPLLM_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(state, kAlign) || !aligned(Kc, kAlign) || !aligned(Vc, kAlign) || !aligned(o, 2) ||

@@ -236,3 +236,52 @@ def test_captured_with_the_update_and_two_streams_at_once():
         for qc, _, _, _, _, q, o, lse, *_ in runs:
             o2, lse2, _ = check_decode(qc, q)
             assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("d,Hq,Hkv", [(64, 4, 2), (128, 6, 1)])
+@pytest.mark.parametrize("c", [511, 512, 513, 1025])
+def test_capacities_about_the_change_from_one_cta_a_unit(d, Hq, Hkv, c):
+    """Short caches are one CTA's each, longer ones are cut into equal runs: both, full and nearly empty."""
+    qc, g = filled(3, Hkv, Hq, d, 2, 40, 30, c, [c - 1, 1, 300], 480 + c)
+    check_decode(qc, _normal(g, 3, Hq, d))
+
+
+def test_offsets_past_two_to_the_32():
+    """The last sequence's rows start more than 2^32 bytes into the buffers: hand-off, updates, read-back, decode.
+    (In the fundamental design: an update of the streaming one looks at no more than 24 576 entries.)"""
+    B, Hkv, Hq, d, a, s, w, c, L = 36, 2, 4, 128, 2, 1000, 60, 10 ** 6, 300
+    g = torch.Generator(device="cuda").manual_seed(490)
+    ids = inputs.token_ids(490, B, L, 0.2)
+    idesc, index = build_index(ids, inputs.SEP_IDS, a, 16)
+    qc = QuantCache(B, Hkv, Hq, d, a, s, w, c, api.CACHE_FIXED_WINDOW)
+    assert (B * Hkv - 1) * (c + s) * d // 2 > 2 ** 32
+    K, V = (_normal(g, B, Hkv, L, d) for _ in "kv")
+    lens = [0] * (B - 1) + [L]
+    api.sepllm_cache_from_prompt_quant(qc.desc, idesc, index, torch.tensor(lens, dtype=torch.int32, device="cuda"), K, V,
+                                       qc.state, qc.Kc, qc.Vc)
+    k1, v1 = (_normal(g, B, Hkv, d) for _ in "kv")
+    qc.update(torch.full((B,), 60, dtype=torch.int32, device="cuda"), k1, v1)
+    q = _normal(g, B, Hq, d)
+    o, lse = qc.decode(q)
+    Ke, Ve = (torch.empty((B, Hkv, c, d), dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    n = torch.empty(B, dtype=torch.int32, device="cuda")
+    api.sepllm_cache_entries_quant(qc.desc, qc.state, qc.Kc, qc.Vc, c, Ke, Ve, n)
+    assert api.sepllm_last_device_status(qc.state) == 0
+    for b in (0, B - 1):
+        oc = orc.FundamentalCache(a, w)
+        for t in range(lens[b] + 1):
+            oc.update(t < lens[b] and bool(np.isin(ids[b, t], inputs.SEP_IDS)))
+        kept = oc.retained()
+        assert n[b] == len(kept) and (b == 0 or len(oc.sep) > 20)
+        rows = [torch.cat((x[b, :, : lens[b]], y[b][:, None]), 1)[:, kept].double().cpu().numpy()
+                for x, y in ((K, k1), (V, v1))]
+        for h in range(Hkv):
+            (kc, ks), (vc, vs) = (orc.quantise_rows(x[h]) for x in rows)
+            for out, code, step in ((Ke, kc, ks), (Ve, vc, vs)):
+                val = torch.from_numpy(orc.quant_values(code, step)).float().to(torch.bfloat16)
+                assert torch.equal(out[b, h, : len(kept)].cpu(), val)
+            G = Hq // Hkv
+            qn = q[b, h * G:h * G + G].double().cpu().numpy()
+            ref, lref, eo, el = reference(qn, kc, ks, vc, vs, d ** -0.5)
+            assert (np.abs(o[b, h * G:h * G + G].double().cpu().numpy() - ref) <= eo).all()
+            assert (np.abs(lse[b, h * G:h * G + G].double().cpu().numpy() - lref) <= el).all()

@@ -156,6 +156,14 @@ def test_other_refusals():
     assert _prompt(idesc=api.IndexDesc(3, 50, 3, 8, 0, 128, 128, 50)) == api.INVALID_ARG
 
 
+@pytest.mark.parametrize("fn", [_decode, _update, _prompt])
+def test_caches_of_more_slots_than_32_bits_can_wrap_are_refused(fn):
+    assert fn(_desc(B=3, s=2 ** 30 - 40, c=2 ** 30, flags=1)) == api.UNSUPPORTED
+    assert _entries(_desc(s=0, c=2 ** 30 + 1), n=2 ** 30 + 1) == api.UNSUPPORTED
+    # more rows than 32 bits number
+    assert _decode(_desc(B=65535, Hkv=64, Hq=64, s=0, c=1025)) == api.UNSUPPORTED
+
+
 def test_arguments_arrive_whole(binding):  # noqa: F811
     bf = torch.bfloat16
     d = _desc()
