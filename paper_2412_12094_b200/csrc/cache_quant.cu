@@ -49,10 +49,11 @@ inline QuantRows<const uint8_t> quant_rows(const sepllm_cache_header& h, const v
 }
 
 // Blackwell's packed fp32 arithmetic, two numbers to an instruction, and an approximate reciprocal (2^-23).
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   float2 r;
-  asm("{.reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mul.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x;}"
-      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 x, x, y, z; "
+      "mov.b64 {%0, %1}, x;}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return r;
 }
 __device__ __forceinline__ float2 sum2(float2 a, float2 b) {
@@ -73,7 +74,7 @@ __device__ __forceinline__ float reciprocal(float x) {
 // A code is found from x * (1 / s), within 2^-20 of x / s.  x / s is either half a whole number
 // exactly, or at least 2^-10 away from one (x and s have eight significant bits): rounded to a multiple of
 // 2^-13 first (the sum with 1536), ties are ties again and nothing else has become one.  The sum with
-// 1.5 * 2^23 + 8 rounds to whole numbers, even at a tie, and leaves q + 8 in the low bits.
+// 1.5 * 2^23 + 8 - 1536 rounds to whole numbers, even at a tie, and leaves q + 8 in the low bits.
 template <int N>
 __device__ __forceinline__ uint32_t quantise(const uint4 (&raw)[N], uint32_t (&codes)[N]) {
   const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(raw);
@@ -103,9 +104,9 @@ __device__ __forceinline__ uint32_t quantise(const uint4 (&raw)[N], uint32_t (&c
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float2 f = __bfloat1622float2(h[4 * n + k]);
-      const float2 t = sum2(sum2(mul2(f, make_float2(r, r)), make_float2(1536.f, 1536.f)), make_float2(-1536.f, -1536.f));
+      const float2 t = fma2(f, make_float2(r, r), make_float2(1536.f, 1536.f));
       // (a NaN, of a group whose step is one, goes with it)
-      const float2 q = sum2(make_float2(fminf(t.x, 7.f), fminf(t.y, 7.f)), make_float2(12582920.f, 12582920.f));
+      const float2 q = sum2(make_float2(fminf(t.x, 1543.f), fminf(t.y, 1543.f)), make_float2(12581384.f, 12581384.f));
       w += (__float_as_uint(q.x) << (8 * k)) + (__float_as_uint(q.y) << (8 * k + 4));
       offset += (0x4b400000u << (8 * k)) + (0x4b400000u << (8 * k + 4));
     }
@@ -235,6 +236,10 @@ quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __n
   const int ch = l % kHalf;  // sixteen elements of the row
   const uint4* src = reinterpret_cast<const uint4*>(is_v ? V : K) + unit * size_t(L) * (D / 8) + 2 * ch;
   const int slot0 = blockIdx.x * kCopyRows + sub;
+  // (a slot's position is read beside the sizes that say whether there is one)
+  int64_t pos[kPasses];
+#pragma unroll
+  for (int r = 0; r < kPasses; ++r) pos[r] = pos_b[min(slot0 + r * kRowsPerPass, h.slots - 1)];
   uint4 raw[kPasses][2];
   uint32_t used = 0;
 #pragma unroll
@@ -246,7 +251,7 @@ quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __n
                                           : false;
     raw[r][0] = raw[r][1] = make_uint4(0, 0, 0, 0);
     if (u) {
-      const uint4* row = src + size_t(pos_b[slot]) * (D / 8);
+      const uint4* row = src + size_t(pos[r]) * (D / 8);
       raw[r][0] = __ldg(row);
       raw[r][1] = __ldg(row + 1);
     }
