@@ -131,7 +131,8 @@ __device__ __forceinline__ void store_codes(uint8_t* codes, uint8_t* steps, int 
 
 // grid (B, Hkv).  As the 16-bit cache's update: every CTA moves the rows of its kv head, the one that
 // finishes last for a sequence updates the state.  The new rows are quantised by the first warp; rows that
-// move keep their codes.  Latency: 256 CTAs of one round of loads each.
+// move keep their codes.  Bound by latency, one round of loads after another: 4 us for 2 small caches, 8 us for 16
+// of 1200 slots, some of them at a compaction.
 template <int D>
 __global__ void __launch_bounds__(kUpdThreads)
 quant_update(sepllm_cache_header h, uint8_t* __restrict__ state, QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc,
@@ -214,10 +215,13 @@ quant_update(sepllm_cache_header h, uint8_t* __restrict__ state, QuantRows<uint8
 }
 
 constexpr int kCopyThreads = 256;
-constexpr int kCopyRows = 64;  // slots (or entries) per CTA
+constexpr int kCopyRows = 32;  // slots (or entries) per CTA (64: hand-off 22.5 us instead of 21.5, read-back 13 instead of 12)
 
 // grid (ceil(slots / kCopyRows), Hkv, B), behind the plan of the hand-off.  Quantises the K and V rows of the
-// retained positions into their slots: D / 8 lanes take one slot's rows, sixteen elements each.
+// retained positions into their slots: D / 8 lanes take one slot's rows, sixteen elements each (eight each: 34 us
+// instead of 26).  All loads of a thread are under way at once.  Bound by three dependent reads to a CTA and by
+// instructions, about 16 an element, more than by HBM: 21.5 us for 4 caches of 2700 entries (45 MB read, 2.4 TB/s
+// with the codes written).
 template <int D>
 __global__ void __launch_bounds__(kCopyThreads)
 quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ K,
@@ -305,7 +309,8 @@ __device__ __forceinline__ uint4 values8(uint32_t w, __nv_bfloat16 step, uint32_
                     __byte_perm(p[2], p[3], 0x7632));
 }
 
-// grid (ceil(c / kCopyRows), Hkv, B).  Row v of K and V of sequence b is its retained entry v.
+// grid (ceil(c / kCopyRows), Hkv, B).  Row v of K and V of sequence b is its retained entry v.  Bound by HBM: 18.8 us
+// for 16 caches of 1195 entries (100 MB), 12 us for 4 of 2700, 5 us for the smallest.
 template <int D>
 __global__ void __launch_bounds__(kCopyThreads)
 quant_entries(sepllm_cache_header h, const uint8_t* __restrict__ state, QuantRows<const uint8_t> Kc,
@@ -529,6 +534,13 @@ struct DecodeShape {
 // P V: codes become bf16 128 + c with one mask-and-or each (two entries of a word pair to a register).  P
 // times the group's step is rounded to bf16 (2^-8), the only rounding here; the offset 136 is taken off
 // the sums by a product with ones, which sums those same rounded numbers.
+//
+// The tensor work is small (16 columns at most; the pipe is a quarter busy), so the products are those whose operands
+// come from registers: codes go from the ring through a mask each into an operand, never back to shared memory.
+// Measured, H = 4, D = 128: 32 caches of 2750 entries in 32 us, 2 of 112 000 in 63 us (4.0 TB/s; reading those
+// bytes cold takes 49 to 53), then the join, 2 us behind it.  ALU pipe 57 % and issue slots 57 % busy, DRAM 49 %: about as much
+// time goes to unpacking as to reading, and 12 warps an SM do not overlap them fully.  H = 8: 42 and 80 us, H = 16: 67
+// and 135 us; D = 64: 20, 24 and 36 us for the 32 caches.
 template <int D, int H>
 __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, H>::kResident)
 decode_quant(const __grid_constant__ QuantDecodeParams p) {
