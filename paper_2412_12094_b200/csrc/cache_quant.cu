@@ -219,7 +219,7 @@ constexpr int kCopyRows = 32;  // slots (or entries) per CTA (64: hand-off 22.5 
 
 // grid (ceil(slots / kCopyRows), Hkv, B), behind the plan of the hand-off.  Quantises the K and V rows of the
 // retained positions into their slots: D / 8 lanes take one slot's rows, sixteen elements each (eight each: 34 us
-// instead of 26).  All loads of a thread are under way at once.  Bound by three dependent reads to a CTA and by
+// instead of 26).  All loads of a thread are under way at once.  Bound by two dependent reads to a CTA and by
 // instructions, about 16 an element, more than by HBM: 21.5 us for 4 caches of 2700 entries (45 MB read, 2.4 TB/s
 // with the codes written).
 template <int D>

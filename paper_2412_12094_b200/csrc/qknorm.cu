@@ -3,7 +3,8 @@
 // y = x r (offset + w), r = (mean x^2 + eps)^-1/2 over the head, then the rotation.  With g the gradient
 // of the outputs rotated back, n = x r and u = g (offset + w): dx = r (u - n mean(n u)), dw = sum g n.
 // Bound by HBM like the rotation alone: x (and dy) are read once, the output is written once; the
-// gradient computes r anew from x instead of reading it.
+// gradient computes r anew from x instead of reading it.  Everything is computed in 32 bits (angles as in the
+// rotation alone) and rounded once, to the output's type.
 #include "rope_common.cuh"
 
 namespace sepllm {
@@ -150,6 +151,10 @@ __device__ __forceinline__ float row_sum(float x, int per_row, int first) {
   return s;
 }
 
+// A thread has sixteen elements of a row, d / 16 lanes a row, and walks the heads of its token with the cos and sin that
+// it computed once; the next heads' rows are on their way while one is worked on.  48 heads of 128 on 65 536
+// tokens take 252 us: 1.61 GB at 6.4 TB/s, the measured copy rate.  14 heads of 80 on 5997 tokens (27 MB): 13 us; a warp has 6
+// such rows at once, and there is no second wave to hide the first one's loads and angles.
 template <class Tin, class Tout, bool HALF, int PER_ROW>
 __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant__ NormParams np) {
   let_dependents_start();
@@ -301,6 +306,7 @@ __device__ __forceinline__ void lane_rotate(const float2 (&cs)[2], float (&x)[8]
   }
 }
 
+// Any strides and alignment: a warp per token, its lanes along the head's pairs, element by element.
 template <class Tin, class Tout>
 __global__ void __launch_bounds__(kRopeThreads) norm_any(const __grid_constant__ NormParams np) {
   let_dependents_start();
@@ -384,6 +390,11 @@ __device__ __forceinline__ bool walk_on(const RopeParams& p, RowWalk& k, int hea
 // The rows of a tensor, (tokens of a warp, head), are cut into equal runs, one per warp; the next rows are on
 // their way while one is worked on, over the ends of heads and tokens.  The tensors come one after the
 // other, so that the sums for one tensor's weights are all that stays in registers.
+//
+// 48 heads of 128 on 16 384 tokens, fp32 to bf16: 134.6 us (5.7 TB/s; DRAM 69 % of its cycles).  36 heads of 64 on 8 x 2048
+// tokens, bf16: 53 us against 31 of its bytes; issue slots 43 %, DRAM 40 %: 12 warps an SM (168 registers: x and dy, their next
+// rows, angles and sums) wait in turn for loads, the two row sums and the cos and sin of a new token (9 %).
+// Four or two CTAs an SM, rows through shared memory (186 and 58 us) and a longer or shorter register ring were slower.
 template <class Tx, class Tg, bool HALF, int PER_ROW>
 __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(const __grid_constant__ NormParams np) {
   __shared__ __align__(16) float s_part[2048];   // [row of the block][d]
@@ -512,6 +523,7 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(cons
   let_dependents_start();
 }
 
+// The gradient for any strides and alignment, laid out as norm_any.
 template <class Tx, class Tg>
 __global__ void __launch_bounds__(kRopeThreads) norm_bwd_any(const __grid_constant__ NormParams np) {
   __shared__ float s_part[kWarps][128];
@@ -568,7 +580,7 @@ __global__ void __launch_bounds__(kRopeThreads) norm_bwd_any(const __grid_consta
   let_dependents_start();
 }
 
-// grid ceil(2 d / 32): adds the blocks' sums, a column to a lane, in a fixed order.
+// grid ceil(2 d / 32): adds the blocks' sums, a column to a lane, in a fixed order.  Latency: 2 us behind the rows.
 __global__ void __launch_bounds__(1024) norm_bwd_sum(const __grid_constant__ NormParams np) {
   __shared__ float s_sum[32][33];
   let_dependents_start();
