@@ -567,8 +567,8 @@ sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, const sepllm_
 
 /* ---- the cache held in 4 bits ------------------------------------------------
  * The streaming cache of sepllm_cache_update with K and V rows in 4 bits and a
- * half an element, for caches that are to take 3.6 times less memory and decode
- * time.  (The paper keeps them in 16 bits; what is kept, and when, is the same.)
+ * half an element: 3.6 times less memory, and about half the time for a decode
+ * step.  (The paper keeps them in 16 bits; what is kept, and when, is the same.)
  * State, slots, rings and flags are those of the 16-bit cache; sepllm_cache_init
  * empties it.  Format: 32 neighbouring elements of a row share a step s = -m / 8
  * (bf16, exact), m their element of largest magnitude, the positive one of two

@@ -1116,7 +1116,7 @@ using namespace sepllm;
 extern "C" sepllm_status sepllm_cache_bytes_quant(const sepllm_cache_desc* desc, size_t* state_bytes,
                                                   size_t* kv_bytes) {
   sepllm_cache_header h;
-  const sepllm_status st = fill_cache_header(desc, &h);
+  const sepllm_status st = check_quant(desc, &h);
   if (st != SEPLLM_OK) return st;
   if (state_bytes) *state_bytes = size_t(h.total_bytes);
   if (kv_bytes)

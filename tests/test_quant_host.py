@@ -164,6 +164,13 @@ def test_caches_of_more_slots_than_32_bits_can_wrap_are_refused(fn):
     assert _decode(_desc(B=65535, Hkv=64, Hq=64, s=0, c=1025)) == api.UNSUPPORTED
 
 
+def test_the_size_query_refuses_what_the_calls_refuse():
+    with pytest.raises(api.SepllmError) as e:
+        api.sepllm_cache_bytes_quant(_desc(s=2 ** 30 - 40, c=2 ** 30, flags=1))
+    assert e.value.code == api.UNSUPPORTED
+    assert api.sepllm_cache_bytes_quant(_desc(s=0, c=2 ** 30))[1] > 2 ** 30
+
+
 def test_arguments_arrive_whole(binding):  # noqa: F811
     bf = torch.bfloat16
     d = _desc()
