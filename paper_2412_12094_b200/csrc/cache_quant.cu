@@ -235,9 +235,9 @@ quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __n
   const sepllm_cache_seq q = v.seq[b];
   const int64_t* pos_b = v.slot_pos + size_t(b) * h.slots;
   const size_t unit = size_t(b) * d.Hkv + hk;
-  const int sub = tid / (2 * kHalf), l = tid % (2 * kHalf);
-  const bool is_v = l >= kHalf;
-  const int ch = l % kHalf;  // sixteen elements of the row
+  const bool is_v = tid >= kCopyThreads / 2;   // (a warp has rows of one of them: their stores differ)
+  const int sub = tid % (kCopyThreads / 2) / kHalf;
+  const int ch = tid % kHalf;  // sixteen elements of the row
   const uint4* src = reinterpret_cast<const uint4*>(is_v ? V : K) + unit * size_t(L) * (D / 8) + 2 * ch;
   const int slot0 = blockIdx.x * kCopyRows + sub;
   // (a slot's position is read beside the sizes that say whether there is one)
