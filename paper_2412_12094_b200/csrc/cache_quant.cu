@@ -215,13 +215,12 @@ quant_update(sepllm_cache_header h, uint8_t* __restrict__ state, QuantRows<uint8
 }
 
 constexpr int kCopyThreads = 256;
-constexpr int kCopyRows = 32;  // slots (or entries) per CTA (64: hand-off 22.5 us instead of 21.5, read-back 13 instead of 12)
+constexpr int kCopyRows = 32;  // slots (or entries) per CTA (64: hand-off 22.5 us, not 21.5; read-back 13, not 12)
 
 // grid (ceil(slots / kCopyRows), Hkv, B), behind the plan of the hand-off.  Quantises the K and V rows of the
-// retained positions into their slots: D / 8 lanes take one slot's rows, sixteen elements each (eight each: 34 us
-// instead of 26).  All loads of a thread are under way at once.  Bound by two dependent reads to a CTA and by
-// instructions, about 16 an element, more than by HBM: 21.5 us for 4 caches of 2700 entries (45 MB read, 2.4 TB/s
-// with the codes written).
+// retained positions into their slots, sixteen elements to a lane (eight: 34 us instead of 26).  All loads of a
+// thread are under way at once.  Bound by instructions, 15 an element (issue slots 77 % busy), more than by HBM: 21 us for
+// 4 caches of 2700 entries (45 MB read), of which the kernel takes 17 behind the plan.
 template <int D>
 __global__ void __launch_bounds__(kCopyThreads)
 quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ K,
