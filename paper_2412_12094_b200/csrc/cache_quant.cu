@@ -293,15 +293,21 @@ __device__ __forceinline__ uint32_t two_128() {
   return r;
 }
 
+// The low four bits of w's halves, less 8, as two bf16 numbers: 128 + c by a mask, minus 136 (exact).
+__device__ __forceinline__ uint32_t two_codes(uint32_t w, uint32_t k128) {
+  const uint32_t n = and_or<0x000f000fu>(w, k128);
+  const __nv_bfloat162 q = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&n), __float2bfloat162_rn(136.f));
+  return *reinterpret_cast<const uint32_t*>(&q);
+}
+
 // Eight codes (element e at bits 4e ..) times their step, rounded to bf16 once (the product has up to
-// twelve significant bits, bf16 eight): 128 + c as bf16, minus 136 (exact), times the step.
+// twelve significant bits, bf16 eight).
 __device__ __forceinline__ uint4 values8(uint32_t w, __nv_bfloat16 step, uint32_t k128) {
   uint32_t p[4];   // elements k and k + 4
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const uint32_t n = and_or<0x000f000fu>(w >> (4 * k), k128);
-    const __nv_bfloat162 q = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&n), __float2bfloat162_rn(136.f));
-    const __nv_bfloat162 v = __hmul2(q, __bfloat162bfloat162(step));
+    const uint32_t q = two_codes(w >> (4 * k), k128);
+    const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&q), __bfloat162bfloat162(step));
     p[k] = *reinterpret_cast<const uint32_t*>(&v);
   }
   return make_uint4(__byte_perm(p[0], p[1], 0x5410), __byte_perm(p[2], p[3], 0x5410), __byte_perm(p[0], p[1], 0x7632),
@@ -530,16 +536,20 @@ struct DecodeShape {
 // off by the accumulator's start, -8 times the sum of q over the group, and the key's step multiplies
 // the group's 32-bit sum.  Up to four heads: the parts are columns 2h and 2h + 1 of one product.
 //
-// P V: codes become bf16 128 + c with one mask-and-or each (two entries of a word pair to a register).  P
-// times the group's step is rounded to bf16 (2^-8), the only rounding here; the offset 136 is taken off
-// the sums by a product with ones, which sums those same rounded numbers.
+// P V: codes become bf16 128 + c with one mask-and-or (two entries of a word pair to a register), and exact whole
+// numbers -8 .. 7 with one packed subtraction.  (The offset 136 could instead be taken off the sums at the end, by a
+// product with ones.  But a product's sum is cut off, not rounded, when it is added to an accumulator: with the offset
+// in the sums, thirty times a typical code, the output of a CTA that walks 100 000 entries alone was off by
+// 3 % where weights are spread out, and no faster: 33.0 and 64.4 us against 32.1 and 62.5 for the two cases below.)
+// P times the group's step is rounded to bf16 (2^-8), the only rounding here.
 //
 // The tensor work is small (16 columns at most; the pipe is a quarter busy), so the products are those whose operands
 // come from registers: codes go from the ring through a mask each into an operand, never back to shared memory.
-// Measured, H = 4, D = 128: 32 caches of 2750 entries in 32 us, 2 of 112 000 in 63 us (4.0 TB/s; reading those
-// bytes cold takes 49 to 53), then the join, 2 us behind it.  ALU pipe 57 % and issue slots 57 % busy, DRAM 49 %: about as much
-// time goes to unpacking as to reading, and 12 warps an SM do not overlap them fully.  H = 8: 42 and 80 us, H = 16: 67
-// and 135 us; D = 64: 20, 24 and 36 us for the 32 caches.
+// Measured, H = 4, D = 128: 32 caches of 2750 entries in 31 us, 2 of 112 000 in 62 us (4.1 TB/s; reading those
+// bytes cold takes 49 to 53), then the join, 2 us behind it.  ALU pipe 59 % and issue slots 61 % busy, DRAM 49 %: nothing
+// is full.  A warp's tile is one chain (copy, scores, softmax, shuffles, values) and 12 warps an SM do not overlap
+// the chains fully.  H = 8: 40 and 76 us, H = 16: 59 and 116 us (two score products for each group, transposes, and at D =
+// 128, H = 16 two CTAs an SM); D = 64: 20, 24 and 34 us for the 32 caches.
 template <int D, int H>
 __global__ void __launch_bounds__(kDecThreads, DecodeShape<D, H>::kResident)
 decode_quant(const __grid_constant__ QuantDecodeParams p) {
@@ -735,7 +745,7 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
 
     // Sums: rows are elements of V, columns 2t and 2t + 1 the heads 8n + 2t and 8n + 2t + 1 (kSplit: columns 4 to
     // 7 repeat 0 to 3).  m_ref: reference exponent, -inf before the first score; m_use: 0 in its place.
-    float oacc[2 * kGroups][NT][4], ones[kGroups][NT][4];
+    float oacc[2 * kGroups][NT][4];
     float m_ref[NT][NE], m_use[NT][NE], l_sum[NT][NE];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -743,10 +753,6 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       for (int j = 0; j < 2 * kGroups; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) oacc[j][n][e] = 0.f;
-#pragma unroll
-      for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) ones[j][n][e] = 0.f;
 #pragma unroll
       for (int e = 0; e < NE; ++e) {
         m_ref[n][e] = -INFINITY;
@@ -849,8 +855,6 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
               oacc[j][n][e] *= corr[e];
               oacc[j][n][e + 2] *= corr[e];
             }
-#pragma unroll
-            for (int j = 0; j < kGroups; ++j) ones[j][n][e] *= corr[e];
           }
         }
       }
@@ -912,14 +916,11 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
           const uint32_t z = __byte_perm(w[2][j / 2], w[3][j / 2], j & 1 ? 0x7632 : 0x5410);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const uint32_t a0 = and_or<0x000f000fu>(u >> (8 * half), k128), a1 = and_or<0x000f000fu>(u >> (8 * half + 4), k128);
-            const uint32_t a2 = and_or<0x000f000fu>(z >> (8 * half), k128), a3 = and_or<0x000f000fu>(z >> (8 * half + 4), k128);
+            const uint32_t a0 = two_codes(u >> (8 * half), k128), a1 = two_codes(u >> (8 * half + 4), k128);
+            const uint32_t a2 = two_codes(z >> (8 * half), k128), a3 = two_codes(z >> (8 * half + 4), k128);
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma_bf16(oacc[2 * j + half][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
           }
-          // (rows 8 to 15, which nobody reads, multiply with zeros)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) mma_bf16(ones[j][n], 0x3f803f80u, 0u, 0x3f803f80u, 0u, pb[n][0], pb[n][1]);
         }
       }
     };
@@ -958,11 +959,9 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
         const int head = 8 * n + 2 * t + e;
         if (head < G) {
 #pragma unroll
-          for (int j = 0; j < 2 * kGroups; ++j) {
-            const float off = 136.f * ones[j / 2][n][e];
+          for (int j = 0; j < 2 * kGroups; ++j)
             *reinterpret_cast<float2*>(acc_of(wid) + head * D + (j / 2) * kGroup + 4 * g + 2 * (j & 1)) =
-                make_float2(oacc[j][n][e] - off, oacc[j][n][e + 2] - off);
-          }
+                make_float2(oacc[j][n][e], oacc[j][n][e + 2]);
         }
       }
     }
