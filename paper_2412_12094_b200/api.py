@@ -81,16 +81,20 @@ class RopeDesc(C.Structure):
 
 
 class QkNorm(C.Structure):
-    """sepllm_qknorm_desc.  wq, wk: bf16 or fp32 [d] tensors of one type, or None."""
+    """sepllm_qknorm_desc.  wq, wk: bf16 or fp32 [d] tensors of one type, or None.  Every call takes the tensors as they
+    are then: their address and their type (Module.to() changes both in place)."""
     _fields_ = [("wq", C.c_void_p), ("wk", C.c_void_p), ("w_dtype", C.c_int32), ("eps", C.c_float),
                 ("offset", C.c_float)]
 
     def __init__(self, wq=None, wk=None, eps=1e-6, offset=0.0):
-        types = {w.dtype for w in (wq, wk) if w is not None}
-        if len(types) > 1 or not types <= set(_ROPE_DTYPES):
-            raise ValueError(f"the weights are bf16 or fp32, both of one type, not {sorted(map(str, types))}")
         self.weights = (wq, wk)     # (kept alive, and looked at by every call)
-        super().__init__(None, None, _ROPE_DTYPES[types.pop()] if types else 0, eps, offset)
+        super().__init__(None, None, self.type_now(), eps, offset)
+
+    def type_now(self) -> int:
+        types = {w.dtype for w in self.weights if w is not None}
+        if len(types) > 1 or not types <= _ROPE_DTYPES.keys():
+            raise ValueError(f"the weights are bf16 or fp32, both of one type, not {sorted(map(str, types))}")
+        return _ROPE_DTYPES[types.pop()] if types else 0
 
 
 class IndexHeader(C.Structure):
@@ -388,8 +392,8 @@ def sepllm_rope_bwd(desc: RopeDesc, positions, dq_out, dk_out, dv_out, dq, dk, d
 
 # ---------------------------------------------------------------- head norms with rotary positions
 def _weights(where, desc, norm, device):
-    """Puts the weights' addresses into the descriptor."""
-    addresses = []
+    """Puts the weights' type and addresses into the descriptor."""
+    dtype, addresses = None, []
     for w in norm.weights:
         if w is None:
             addresses.append(None)
@@ -397,7 +401,12 @@ def _weights(where, desc, norm, device):
         if w.shape != (desc.d,) or not w.is_contiguous() or w.get_device() != device:
             raise ValueError(f"{where}: weights are contiguous [{desc.d}] tensors of the current device, not {tuple(w.shape)} "
                              f"with stride {w.stride()} on {w.device}")
+        if w.dtype is not dtype:
+            if dtype is not None or w.dtype not in _ROPE_DTYPES:
+                norm.type_now()     # (refuses them)
+            dtype = w.dtype
         addresses.append(w.data_ptr())
+    norm.w_dtype = _ROPE_DTYPES.get(dtype, 0)
     norm.wq, norm.wk = addresses
 
 
