@@ -680,9 +680,7 @@ static sepllm_status update_impl(const sepllm_cache_desc* desc, void* state, voi
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   const size_t smem = size_t(max_past) * sizeof(int16_t);
   auto kernel = with_rope ? cache_update<true> : cache_update<false>;
-  if (smem > 40 * 1024)
-    SEPLLM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         int(smem)));
+  SEPLLM_CUDA_TRY(allow_update_smem(kernel, smem, sizeof(int16_t)));
   kernel<<<dim3(desc->B, desc->Hkv), kUpdThreads, smem, stream>>>(
       h, static_cast<uint8_t*>(state), static_cast<__nv_bfloat16*>(Kc),
       static_cast<__nv_bfloat16*>(Vc), static_cast<const __nv_bfloat16*>(k_new),

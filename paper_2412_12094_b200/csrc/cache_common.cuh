@@ -232,6 +232,14 @@ inline sepllm_status update_params(const sepllm_cache_desc* desc, const int32_t*
   return SEPLLM_OK;
 }
 
+// Lets an update's kernel use `bytes` of shared memory.  The limit is the kernel's, for all calls on the device: it is
+// only ever set to what the largest update needs, so that no call takes away another thread's.
+template <class Kernel>
+cudaError_t allow_update_smem(Kernel kernel, size_t bytes, int bytes_per_entry) {
+  if (bytes <= 40 * 1024) return cudaSuccess;   // (48 KB, static memory included, need no leave)
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxPast * bytes_per_entry);
+}
+
 // The state that a pre-filled prompt leaves (cache.cu): sizes, positions and flags, rings from slot 0.
 sepllm_status launch_prompt_plan(const sepllm_cache_header& h, const sepllm_index_header& ih, void* state,
                                  const void* index, const int32_t* prompt_len, cudaStream_t stream);

@@ -1138,8 +1138,7 @@ extern "C" sepllm_status sepllm_cache_update_quant(const sepllm_cache_desc* desc
   if ((st = update_params(desc, sep_ids, n_sep, &sep, &max_past)) != SEPLLM_OK) return st;
   const size_t smem = size_t(max_past) * 2 * sizeof(int16_t);
   auto kernel = desc->d == 128 ? quant_update<128> : quant_update<64>;
-  if (smem > 40 * 1024)
-    SEPLLM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+  SEPLLM_CUDA_TRY(allow_update_smem(kernel, smem, 2 * sizeof(int16_t)));
   SEPLLM_CUDA_TRY(launch_overlapped(kernel, dim3(desc->B, desc->Hkv), kUpdThreads, smem, static_cast<cudaStream_t>(stream_),
                                     h, static_cast<uint8_t*>(state), quant_rows(h, Kc), quant_rows(h, Vc),
                                     static_cast<const __nv_bfloat16*>(k_new),
