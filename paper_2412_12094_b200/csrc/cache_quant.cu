@@ -19,7 +19,9 @@ namespace sepllm {
 
 namespace {
 
-// Every kernel is launched while the one before it ends (it waits for it first), and lets the next one in.
+// Every kernel is launched while the one before it ends (it waits for it first), and lets the next one in.  What
+// it reads may therefore still be written when it starts: plain loads behind the wait, none that the compiler or the
+// cache may take for constant (const __restrict__, __ldg).
 
 constexpr int kGroup = 32;             // elements that share a step
 constexpr float kFlush = 0x1p-100f;    // groups whose largest magnitude is below are held as zeros
@@ -135,9 +137,9 @@ __device__ __forceinline__ void store_codes(uint8_t* codes, uint8_t* steps, int 
 // of 1200 slots, some of them at a compaction.
 template <int D>
 __global__ void __launch_bounds__(kUpdThreads)
-quant_update(sepllm_cache_header h, uint8_t* __restrict__ state, QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc,
-             const __nv_bfloat16* __restrict__ k_new, const __nv_bfloat16* __restrict__ v_new,
-             const int32_t* __restrict__ new_token_ids, SepIds sep, int max_past) {
+quant_update(sepllm_cache_header h, uint8_t* state, QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc,
+             const __nv_bfloat16* k_new, const __nv_bfloat16* v_new, const int32_t* new_token_ids, SepIds sep,
+             int max_past) {
   extern __shared__ int16_t flag_s[];   // [max_past] ranks, [max_past] entries that move
   __shared__ int warp_buf[32];
   constexpr int kVec = D / 8, kCode = D / 2, kStep = D / 16;   // 16-byte pieces of a new row; bytes of a held one
@@ -223,8 +225,8 @@ constexpr int kCopyRows = 32;  // slots (or entries) per CTA (64: hand-off 22.5 
 // 4 caches of 2700 entries (45 MB read), of which the kernel takes 17 behind the plan.
 template <int D>
 __global__ void __launch_bounds__(kCopyThreads)
-quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __nv_bfloat16* __restrict__ K,
-             const __nv_bfloat16* __restrict__ V, int L, QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc) {
+quant_prompt(sepllm_cache_header h, const uint8_t* state, const __nv_bfloat16* K, const __nv_bfloat16* V, int L,
+             QuantRows<uint8_t> Kc, QuantRows<uint8_t> Vc) {
   constexpr int kHalf = D / 16, kRowsPerPass = kCopyThreads / (2 * kHalf), kPasses = kCopyRows / kRowsPerPass;
   let_dependents_start();
   wait_for_prior();   // (the plan)
@@ -255,8 +257,8 @@ quant_prompt(sepllm_cache_header h, const uint8_t* __restrict__ state, const __n
     raw[r][0] = raw[r][1] = make_uint4(0, 0, 0, 0);
     if (u) {
       const uint4* row = src + size_t(pos[r]) * (D / 8);
-      raw[r][0] = __ldg(row);
-      raw[r][1] = __ldg(row + 1);
+      raw[r][0] = row[0];
+      raw[r][1] = row[1];
     }
     used |= uint32_t(u) << r;
   }
@@ -318,9 +320,8 @@ __device__ __forceinline__ uint4 values8(uint32_t w, __nv_bfloat16 step, uint32_
 // for 16 caches of 1195 entries (100 MB), 12 us for 4 of 2700, 5 us for the smallest.
 template <int D>
 __global__ void __launch_bounds__(kCopyThreads)
-quant_entries(sepllm_cache_header h, const uint8_t* __restrict__ state, QuantRows<const uint8_t> Kc,
-              QuantRows<const uint8_t> Vc, int n, __nv_bfloat16* __restrict__ K, __nv_bfloat16* __restrict__ V,
-              int32_t* __restrict__ length) {
+quant_entries(sepllm_cache_header h, const uint8_t* state, QuantRows<const uint8_t> Kc, QuantRows<const uint8_t> Vc,
+              int n, __nv_bfloat16* __restrict__ K, __nv_bfloat16* __restrict__ V, int32_t* length) {
   constexpr int kVec = D / 8, kGroups = D / kGroup, kRowsPerPass = kCopyThreads / kVec;
   let_dependents_start();
   wait_for_prior();
@@ -607,8 +608,7 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
 #pragma unroll
     for (int x = 0; x < kQLoads; ++x) {
       const int c = x * kDecThreads + tid, head = c / kPer;
-      q_raw[x] = head < G ? __ldg(reinterpret_cast<const uint4*>(
-                                      p.q + (size_t(sh.b) * d.Hq + sh.hk * G + head) * D) + c % kPer)
+      q_raw[x] = head < G ? reinterpret_cast<const uint4*>(p.q + (size_t(sh.b) * d.Hq + sh.hk * G + head) * D)[c % kPer]
                           : make_uint4(0, 0, 0, 0);
     }
   };
