@@ -7,6 +7,7 @@ Nothing here computes: if the shared library is missing the import fails.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import struct
 
@@ -436,6 +437,7 @@ def sepllm_qknorm_rope_bwd(desc: RopeDesc, norm: QkNorm, positions, q, k, dq_out
     pos = _positions(where, desc, positions)
     xs, ins, outs = _rope_views(desc, (q, k, None, dq_out, dk_out, dv_out, dq, dk, dv), where, device)
     _expect(where, ("dwq", dwq, (desc.d,), torch.float32), ("dwk", dwk, (desc.d,), torch.float32))
+    _room(where, ("workspace", workspace, sepllm_qknorm_rope_bwd_workspace_bytes(desc)))
     _check(lib().sepllm_qknorm_rope_bwd(C.byref(desc), C.byref(norm), pos, xs, ins, outs,
                                         *_addresses(where, (dwq, dwk, workspace)),
                                         torch._C._cuda_getCurrentRawStream(device)), where)
@@ -559,12 +561,37 @@ def sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, prefix_len, O
 
 
 # ---------------------------------------------------------------- cache in 4 bits
-def _quant_kv(where, desc, Kc, Vc):
-    """Refuses buffers shorter than a cache of the descriptor (they would be read past their end)."""
-    n = desc.B * desc.Hkv * (desc.c + desc.s) * desc.d
-    need = (n // 2 + 255 & -256) + (n // 16 + 255 & -256)
-    if Kc.nbytes < need or Vc.nbytes < need:
-        raise ValueError(f"{where}: Kc and Vc have {Kc.nbytes} and {Vc.nbytes} bytes, the descriptor's cache {need} each")
+def _room(where, *buffers):
+    """Refuses buffers, (name, tensor, bytes needed), that a call would write or read past their end (None: the
+    library's to refuse)."""
+    for what, t, need in buffers:
+        if t is not None and t.nbytes < need:
+            raise ValueError(f"{where}: {what} has {t.nbytes} bytes, the descriptor needs {need}")
+
+
+# (sizes by the descriptor's bytes: short calls are bound by the host)
+@functools.lru_cache(maxsize=256)
+def _quant_sizes(desc):
+    d = CacheDesc.from_buffer_copy(desc)
+    rows = d.B * (d.c + d.s)
+    n = rows * d.Hkv * d.d
+    state = 256 + (64 * d.B + 255 & -256) + (8 * rows + 255 & -256) + (rows + 255 & -256)
+    return state, (n // 2 + 255 & -256) + (n // 16 + 255 & -256)
+
+
+@functools.lru_cache(maxsize=256)
+def _decode_quant_workspace(library, desc):
+    return sepllm_decode_quant_workspace_bytes(CacheDesc.from_buffer_copy(desc))
+
+
+@functools.lru_cache(maxsize=256)
+def _index_size(library, idesc):
+    return sepllm_index_bytes(IndexDesc.from_buffer_copy(idesc))[0]
+
+
+def _quant_room(where, desc, state, Kc, Vc):
+    n, kv = _quant_sizes(bytes(desc))
+    _room(where, ("state", state, n), ("Kc", Kc, kv), ("Vc", Vc, kv))
 
 
 def sepllm_cache_bytes_quant(desc: CacheDesc):
@@ -579,7 +606,7 @@ def sepllm_cache_update_quant(desc, state, Kc, Vc, new_token_ids, sep_ids, k_new
     p, n = _sep_bytes(sep_ids)
     _expect(where, ("new_token_ids", new_token_ids, (desc.B,), torch.int32), ("k_new", k_new, row, torch.bfloat16),
             ("v_new", v_new, row, torch.bfloat16))
-    _quant_kv(where, desc, Kc, Vc)
+    _quant_room(where, desc, state, Kc, Vc)
     st, kc, vc, ids, kn, vn = _addresses(where, (state, Kc, Vc, new_token_ids, k_new, v_new))
     _check(lib().sepllm_cache_update_quant(C.byref(desc), st, kc, vc, ids, p, n, kn, vn, _raw_stream()), where)
 
@@ -588,7 +615,8 @@ def sepllm_cache_from_prompt_quant(desc, idesc, index, prompt_len, K, V, state, 
     """sepllm_cache_from_prompt for a cache held in 4 bits; prompt_len: int32 [B] or None."""
     where, bf, rows = "sepllm_cache_from_prompt_quant", torch.bfloat16, (desc.B, desc.Hkv, idesc.L, desc.d)
     _expect(where, ("prompt_len", prompt_len, (desc.B,), torch.int32), ("K", K, rows, bf), ("V", V, rows, bf))
-    _quant_kv(where, desc, Kc, Vc)
+    _quant_room(where, desc, state, Kc, Vc)
+    _room(where, ("index", index, _index_size(lib(), bytes(idesc))))
     _check(lib().sepllm_cache_from_prompt_quant(C.byref(desc), C.byref(idesc), *_addresses(
         where, (index, prompt_len, K, V, state, Kc, Vc)), _raw_stream()), where)
 
@@ -598,7 +626,7 @@ def sepllm_cache_entries_quant(desc, state, Kc, Vc, n, K, V, length=None):
     [B][Hkv][n][d]; length: int32 [B] that receives Size_run, or None."""
     where, bf, rows = "sepllm_cache_entries_quant", torch.bfloat16, (desc.B, desc.Hkv, n, desc.d)
     _expect(where, ("K", K, rows, bf), ("V", V, rows, bf), ("length", length, (desc.B,), torch.int32))
-    _quant_kv(where, desc, Kc, Vc)
+    _quant_room(where, desc, state, Kc, Vc)
     st, kc, vc, k, v, ln = _addresses(where, (state, Kc, Vc, K, V, length))
     _check(lib().sepllm_cache_entries_quant(C.byref(desc), st, kc, vc, n, k, v, ln, _raw_stream()), where)
 
@@ -614,7 +642,8 @@ def sepllm_decode_quant(desc, scale, q, state, Kc, Vc, o, lse, workspace):
     """sepllm_decode over a cache held in 4 bits; lse may be None."""
     where, row = "sepllm_decode_quant", (desc.B, desc.Hq, desc.d)
     _expect(where, ("q", q, row, torch.bfloat16), ("o", o, row, torch.bfloat16), ("lse", lse, row[:2], torch.float32))
-    _quant_kv(where, desc, Kc, Vc)
+    _quant_room(where, desc, state, Kc, Vc)
+    _room(where, ("workspace", workspace, _decode_quant_workspace(lib(), bytes(desc))))
     _check(lib().sepllm_decode_quant(C.byref(desc), scale, *_addresses(where, (q, state, Kc, Vc, o, lse, workspace)),
                                      _raw_stream()), where)
 
