@@ -615,7 +615,8 @@ sepllm_status sepllm_cache_entries_quant(const sepllm_cache_desc* desc, const vo
 
 /* sepllm_decode over a cache held in 4 bits: o = softmax(q K^T * scale) V of the
  * held values.  A sequence with no entry gets o = 0 and lse = -inf.  A query
- * element that is not finite, or beyond 2^117, makes its row NaN.  workspace of
+ * element that is not finite, or of magnitude 1.75 * 2^118 and more, makes its row
+ * NaN.  Sums are 32 bits (elements of V up to 2^90).  workspace of
  * sepllm_decode_quant_workspace_bytes, 256-byte aligned (its first word is the
  * device status; always 0); calls that may overlap need one each.  Other arguments
  * as sepllm_decode and above. */

@@ -685,7 +685,7 @@ decode_quant(const __grid_constant__ QuantDecodeParams p) {
       for (int k = 0; k < 4; ++k) {
         f[k].x *= up;
         f[k].y *= up;
-        // (an infinite element, or one beyond 2^118, becomes NaN)
+        // (e4m3 ends at 448: where e is at its end, elements from 1.75 * 2^118 on and infinite ones become NaN)
         if (!(fabsf(f[k].x) < 448.f)) f[k].x = __int_as_float(0x7fc00000);
         if (!(fabsf(f[k].y) < 448.f)) f[k].y = __int_as_float(0x7fc00000);
         const uint32_t a = pack_e4m3(f[k].x, f[k].y);
