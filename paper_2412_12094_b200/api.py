@@ -216,6 +216,17 @@ def _addresses(where, tensors):
     return out
 
 
+def _short(t, need):
+    """Whether a call would write or read past the buffer's end (None: the library's to refuse)."""
+    return t is not None and t.nbytes < need
+
+
+def _refuse_short(where, *buffers):
+    for what, t, need in buffers:
+        if _short(t, need):
+            raise ValueError(f"{where}: {what} has {t.nbytes} bytes, the descriptor needs {need}")
+
+
 def _sep_array(sep_ids):
     arr = np.ascontiguousarray(np.asarray(sep_ids, dtype=np.int32))
     return arr, arr.ctypes.data_as(C.c_void_p), int(arr.size)
@@ -428,6 +439,11 @@ def sepllm_qknorm_rope_bwd_workspace_bytes(desc: RopeDesc):
     return b.value
 
 
+@functools.lru_cache(maxsize=16)
+def _norm_workspace(library, d):
+    return sepllm_qknorm_rope_bwd_workspace_bytes(RopeDesc(1, 1, 1, 1, d))
+
+
 def sepllm_qknorm_rope_bwd(desc: RopeDesc, norm: QkNorm, positions, q, k, dq_out, dk_out, dv_out, dq, dk, dv, dwq,
                            dwk, workspace):
     """Gradients of sepllm_qknorm_rope_fwd's inputs and weights; q, k: the forward's inputs; dwq, dwk: fp32 [d]
@@ -437,7 +453,7 @@ def sepllm_qknorm_rope_bwd(desc: RopeDesc, norm: QkNorm, positions, q, k, dq_out
     pos = _positions(where, desc, positions)
     xs, ins, outs = _rope_views(desc, (q, k, None, dq_out, dk_out, dv_out, dq, dk, dv), where, device)
     _expect(where, ("dwq", dwq, (desc.d,), torch.float32), ("dwk", dwk, (desc.d,), torch.float32))
-    _room(where, ("workspace", workspace, sepllm_qknorm_rope_bwd_workspace_bytes(desc)))
+    _refuse_short(where, ("workspace", workspace, _norm_workspace(lib(), desc.d)))
     _check(lib().sepllm_qknorm_rope_bwd(C.byref(desc), C.byref(norm), pos, xs, ins, outs,
                                         *_addresses(where, (dwq, dwk, workspace)),
                                         torch._C._cuda_getCurrentRawStream(device)), where)
@@ -561,14 +577,6 @@ def sepllm_attn_prefix_fwd(desc, idesc, P, Q, K, V, index, Kp, Vp, prefix_len, O
 
 
 # ---------------------------------------------------------------- cache in 4 bits
-def _room(where, *buffers):
-    """Refuses buffers, (name, tensor, bytes needed), that a call would write or read past their end (None: the
-    library's to refuse)."""
-    for what, t, need in buffers:
-        if t is not None and t.nbytes < need:
-            raise ValueError(f"{where}: {what} has {t.nbytes} bytes, the descriptor needs {need}")
-
-
 # (sizes by the descriptor's bytes: short calls are bound by the host)
 @functools.lru_cache(maxsize=256)
 def _quant_sizes(desc):
@@ -590,8 +598,11 @@ def _index_size(library, idesc):
 
 
 def _quant_room(where, desc, state, Kc, Vc):
-    n, kv = _quant_sizes(bytes(desc))
-    _room(where, ("state", state, n), ("Kc", Kc, kv), ("Vc", Vc, kv))
+    raw = bytes(desc)
+    n, kv = _quant_sizes(raw)
+    if _short(state, n) or _short(Kc, kv) or _short(Vc, kv):
+        _refuse_short(where, ("state", state, n), ("Kc", Kc, kv), ("Vc", Vc, kv))
+    return raw
 
 
 def sepllm_cache_bytes_quant(desc: CacheDesc):
@@ -616,7 +627,7 @@ def sepllm_cache_from_prompt_quant(desc, idesc, index, prompt_len, K, V, state, 
     where, bf, rows = "sepllm_cache_from_prompt_quant", torch.bfloat16, (desc.B, desc.Hkv, idesc.L, desc.d)
     _expect(where, ("prompt_len", prompt_len, (desc.B,), torch.int32), ("K", K, rows, bf), ("V", V, rows, bf))
     _quant_room(where, desc, state, Kc, Vc)
-    _room(where, ("index", index, _index_size(lib(), bytes(idesc))))
+    _refuse_short(where, ("index", index, _index_size(lib(), bytes(idesc))))
     _check(lib().sepllm_cache_from_prompt_quant(C.byref(desc), C.byref(idesc), *_addresses(
         where, (index, prompt_len, K, V, state, Kc, Vc)), _raw_stream()), where)
 
@@ -642,9 +653,11 @@ def sepllm_decode_quant(desc, scale, q, state, Kc, Vc, o, lse, workspace):
     """sepllm_decode over a cache held in 4 bits; lse may be None."""
     where, row = "sepllm_decode_quant", (desc.B, desc.Hq, desc.d)
     _expect(where, ("q", q, row, torch.bfloat16), ("o", o, row, torch.bfloat16), ("lse", lse, row[:2], torch.float32))
-    _quant_room(where, desc, state, Kc, Vc)
-    _room(where, ("workspace", workspace, _decode_quant_workspace(lib(), bytes(desc))))
-    _check(lib().sepllm_decode_quant(C.byref(desc), scale, *_addresses(where, (q, state, Kc, Vc, o, lse, workspace)),
+    raw, library = _quant_room(where, desc, state, Kc, Vc), lib()
+    need = _decode_quant_workspace(library, raw)
+    if _short(workspace, need):
+        _refuse_short(where, ("workspace", workspace, need))
+    _check(library.sepllm_decode_quant(C.byref(desc), scale, *_addresses(where, (q, state, Kc, Vc, o, lse, workspace)),
                                      _raw_stream()), where)
 
 
