@@ -583,8 +583,10 @@ sepllm_status sepllm_attn_prefix_fwd(const sepllm_attn_desc* desc, const sepllm_
  *           bytes on, steps bf16 [B][Hkv][slots][d / 32].  A row's codes q + 8
  *           stand two to a byte, low half first; element e of group j is the row's
  *           ((e / m) * (d / 32) + j) * m + e % m -th, m = 8 in Kc and 4 in Vc.
- * c + s up to 2^30.  Positions taken inside the cache (sepllm_cache_update_rope)
- * have no 4-bit form: keys are handed over with their positions encoded. */
+ * c + s up to 2^30, and B * Hkv * (c + s) below 2^32 for the decode (the query of its
+ * workspace answers for larger ones as well; the calls refuse them).  Positions
+ * taken inside the cache (sepllm_cache_update_rope) have no 4-bit form: keys are
+ * handed over with their positions encoded. */
 
 /* state_bytes: the state buffer; kv_bytes: ONE of Kc / Vc. */
 sepllm_status sepllm_cache_bytes_quant(const sepllm_cache_desc* desc, size_t* state_bytes,

@@ -316,8 +316,10 @@ __device__ __forceinline__ uint4 values8(uint32_t w, __nv_bfloat16 step, uint32_
                     __byte_perm(p[2], p[3], 0x7632));
 }
 
-// grid (ceil(c / kCopyRows), Hkv, B).  Row v of K and V of sequence b is its retained entry v.  Bound by HBM: 18.8 us
-// for 16 caches of 1195 entries (100 MB), 12 us for 4 of 2700, 5 us for the smallest.
+// grid (ceil(c / kCopyRows), Hkv, B).  Row v of K and V of sequence b is its retained entry v.  18.6 us for 16 caches
+// of 1195 entries (100 MB), 12 us for 4 of 2700, 5 us for the smallest.  Bound by instructions and their latency, not by HBM
+// (issue slots 55 and 63 % busy, DRAM 26 and 13 %: most of what it writes is still in L2 when it ends): a lane turns
+// eight elements from one word and two half words of codes and two steps.
 template <int D>
 __global__ void __launch_bounds__(kCopyThreads)
 quant_entries(sepllm_cache_header h, const uint8_t* state, QuantRows<const uint8_t> Kc, QuantRows<const uint8_t> Vc,

@@ -153,8 +153,9 @@ __device__ __forceinline__ float row_sum(float x, int per_row, int first) {
 
 // A thread has sixteen elements of a row, d / 16 lanes a row, and walks the heads of its token with the cos and sin that
 // it computed once; the next heads' rows are on their way while one is worked on.  48 heads of 128 on 65 536
-// tokens take 252 us: 1.61 GB at 6.4 TB/s, the measured copy rate.  14 heads of 80 on 5997 tokens (27 MB): 13 us; a warp has 6
-// such rows at once, and there is no second wave to hide the first one's loads and angles.
+// tokens take 252 us: 1.61 GB at 6.4 TB/s, the measured copy rate.  16 384 of them: 75 us (fp32 to bf16 104, bf16 to fp32
+// 102, fp32 to fp32 133).  14 heads of 80 on 5997 tokens (27 MB): 12.7 us, where the rotation alone takes 9.9: latency.  A
+// warp has 6 such rows at once and one wave of CTAs, in which angles, weights and the first rows come one after the other.
 template <class Tin, class Tout, bool HALF, int PER_ROW>
 __global__ void __launch_bounds__(kRopeThreads) norm_rows(const __grid_constant__ NormParams np) {
   let_dependents_start();
@@ -306,7 +307,9 @@ __device__ __forceinline__ void lane_rotate(const float2 (&cs)[2], float (&x)[8]
   }
 }
 
-// Any strides and alignment: a warp per token, its lanes along the head's pairs, element by element.
+// Any strides and alignment: a warp per token, its lanes along the head's pairs, element by element and with no row on
+// its way ahead.  48 heads of 128 on 16 384 tokens, 118 elements turned in halves: 228 us (norm_rows with all
+// 128 turned: 75); 14 heads of 80 on 5997 tokens, 20 turned in halves: 33 us.
 template <class Tin, class Tout>
 __global__ void __launch_bounds__(kRopeThreads) norm_any(const __grid_constant__ NormParams np) {
   let_dependents_start();
@@ -391,9 +394,11 @@ __device__ __forceinline__ bool walk_on(const RopeParams& p, RowWalk& k, int hea
 // their way while one is worked on, over the ends of heads and tokens.  The tensors come one after the
 // other, so that the sums for one tensor's weights are all that stays in registers.
 //
-// 48 heads of 128 on 16 384 tokens, fp32 to bf16: 134.6 us (5.7 TB/s; DRAM 69 % of its cycles).  36 heads of 64 on 8 x 2048
-// tokens, bf16: 53 us against 31 of its bytes; issue slots 43 %, DRAM 40 %: 12 warps an SM (168 registers: x and dy, their next
-// rows, angles and sums) wait in turn for loads, the two row sums and the cos and sin of a new token (9 %).
+// 48 heads of 128 on 16 384 tokens, fp32 to bf16: 134 us (5.7 TB/s; DRAM 69 % of its cycles); bf16 to bf16 119, bf16 to
+// fp32 164, fp32 to fp32 218 (spills 126 to 250 bytes).  36 heads of 64 on 8 x 2048 tokens, bf16: 53 us against 31 of its
+// bytes; issue slots 43 %, DRAM 40 %: nothing is full, 12 warps an SM (168 registers: x and dy, their next
+// rows, angles and sums, of sixteen elements a lane) wait in turn for loads, the two row sums and the cos and sin of
+// a new token (9 %).  Fewer elements to a lane, and so more warps, were not tried.
 // Four or two CTAs an SM, rows through shared memory (186 and 58 us) and a longer or shorter register ring were slower.
 template <class Tx, class Tg, bool HALF, int PER_ROW>
 __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(const __grid_constant__ NormParams np) {
@@ -523,7 +528,8 @@ __global__ void __launch_bounds__(kRopeThreads, kBwdResident) norm_bwd_rows(cons
   let_dependents_start();
 }
 
-// The gradient for any strides and alignment, laid out as norm_any.
+// The gradient for any strides and alignment, laid out as norm_any.  The two cases named there: 646 and 78 us
+// (norm_bwd_rows with all 128 turned: 119).
 template <class Tx, class Tg>
 __global__ void __launch_bounds__(kRopeThreads) norm_bwd_any(const __grid_constant__ NormParams np) {
   __shared__ float s_part[kWarps][128];
@@ -605,7 +611,8 @@ sepllm_status check_norm(const sepllm_qknorm_desc* n) {
   return aligned(n->wq, a) && aligned(n->wk, a) ? SEPLLM_OK : SEPLLM_INVALID_ARG;
 }
 
-// 16-byte accesses run unless halves end inside a 16-byte piece.
+// 16-byte accesses run unless halves end inside a 16-byte piece (these take the kernels for any strides, three to five
+// times as long: norm_any).
 bool by_rows(const sepllm_rope_desc* d, const RopeParams& p, bool vectors) {
   return vectors && !(d->layout == SEPLLM_ROPE_HALF && p.rot % 16 != 0);
 }
