@@ -9,9 +9,9 @@ pytestmark = pytest.mark.gpu
 CTAS = 3 * 148    # of the largest grid: as many units are not cut
 
 
-def long_caches(B, Hkv, Hq, d, n, seed):
-    """Caches of n entries, all units alike: keys of zeros (all weights are equal, and exact), codes of V that
-    are as often positive as negative, steps that are powers of two between 2^-10 and 1 (a weight times a step
+def long_caches(B, Hkv, Hq, d, n, seed, lowest):
+    """Caches of n entries, all units alike: keys of zeros (all weights are equal, and exact), codes of V from
+    `lowest` to 7, steps that are powers of two between 2^-10 and 1 (a weight times a step
     is exact in 16 bits).  Returns the calls' buffers and the held values of V [n][d], 64 bits."""
     g = torch.Generator(device="cuda").manual_seed(seed)
     desc = api.CacheDesc(B, Hkv, Hq, d, 0, 4, 8, n + 20)
@@ -21,7 +21,7 @@ def long_caches(B, Hkv, Hq, d, n, seed):
     api.sepllm_cache_init(desc, state)
     head = api.CacheHeader.from_buffer_copy(bytes(state[:256].tolist()))
     state[head.off_seq:head.off_seq + 64 * B].view(torch.int32).view(B, 16)[:, 4] = n      # neighbours alone
-    code = torch.randint(-7, 8, (slots, d), generator=g, device="cuda")
+    code = torch.randint(lowest, 8, (slots, d), generator=g, device="cuda")
     step = -torch.exp2(torch.randint(-10, 1, (slots, d // 32), generator=g, device="cuda").double())
     e = torch.arange(d, device="cuda")
     place = ((e % 32 // 4) * (d // 32) + e // 32) * 4 + e % 4
@@ -37,13 +37,14 @@ def long_caches(B, Hkv, Hq, d, n, seed):
 
 
 @pytest.mark.parametrize("d,G", [(128, 1), (128, 8), (128, 16), (64, 4), (64, 6), (64, 12)])
-def test_sums_over_100_000_entries(d, G):
+@pytest.mark.parametrize("lowest", [-7, 1])       # values of both signs, which cancel, and of one
+def test_sums_over_100_000_entries(d, G, lowest):
     """The output is rounded once (2^-8).  Products are exact.  A warp adds up the tiles of 32 entries w, w + 4, ..,
     sixteen products at a time; these and what they are added to may be cut off, each of the seventeen at one unit
     in the last of 24 bits of the largest, which is no more than the largest sum on the way plus sixteen products
     of 7: 17 * 2^-23 of that, n / 64 times for each of four warps, and 2^-22 of it for the merge; over n."""
     n, B, Hkv = 100_000, CTAS // 4, 4
-    desc, state, Kc, Vc, values = long_caches(B, Hkv, Hkv * G, d, n, 500 + d + G)
+    desc, state, Kc, Vc, values = long_caches(B, Hkv, Hkv * G, d, n, 500 + d + G, lowest)
     q = torch.randn((B, Hkv * G, d), device="cuda").to(torch.bfloat16)
     o, lse = torch.empty_like(q), torch.empty((B, Hkv * G), device="cuda")
     ws = api.alloc_bytes(api.sepllm_decode_quant_workspace_bytes(desc))
